@@ -355,6 +355,205 @@ int dckv_dense_decode(int32_t num_q_heads, int32_t num_kv_heads, int32_t head_di
                       void* stream);
 
 /* ------------------------------------------------------------------------
+ * Serving over the paged caches: what a step needs around the attention
+ * calls.  Page maps serve every cache of this library; the rotation and the
+ * appends below serve the bf16 and the 8-bit K/V caches.  Arguments,
+ * ownership, streams and errors as above: everything is validated on the
+ * host before a launch, nothing is allocated, copied or waited for.
+ *
+ * Page map: where the new tokens of a step go.  Sequence b holds cached[b]
+ * tokens and gets added[b] more, packed one sequence after another into rows
+ * 0 .. sum(added) - 1 of the step's activations.  New pages are taken from a
+ * stack of free page ids, the one on top first, sequence after sequence:
+ *   served     sequence b is served unless cached or added is negative or
+ *              cached + added exceeds max_pages*64 (status 2), its rows pass
+ *              n_rows (status 3), or it needs pages and they and those of the
+ *              sequences before it that have status 0 or 1 are more than the
+ *              stack holds (status 1)
+ *   page_table entries of a served sequence's new pages are written, no others
+ *   seq_lens   cached + added of a served sequence, else cached
+ *   row r      of sequence b, its j-th: position cached + j, slot page*64 +
+ *              position%64; -1 both where b is not served and behind the last
+ *              row, so that the appends and the rotation skip the row
+ * Arguments (device, int32 unless said otherwise):
+ *   cached, added [batch]   page_table [batch, max_pages]
+ *   free_pages [free_capacity]   the stack, free_pages[0] at its bottom; not
+ *              written
+ *   free_count [1] ids on the stack (clamped to [0, free_capacity]);
+ *   free_left  [1] out: ids left, the taken ones cut off the top
+ *   seq_lens, status [batch] out   row_start [batch + 1] out: first row of each
+ *              sequence (at most n_rows)
+ *   slot       int64 [n_rows] out   position, seq_of_row [n_rows] out (seq_of_row
+ *              -1 behind the last row)
+ * seq_lens may be cached and free_left may be free_count (a step then updates
+ * them in place); other outputs overlap nothing.  1 <= batch <= 65535 (0 is a
+ * no-op), n_rows >= 0.  Same inputs give the same pages. */
+int dckv_page_map(const int32_t* cached, const int32_t* added, int32_t batch, int32_t* page_table,
+                  int32_t max_pages, const int32_t* free_pages, int32_t free_capacity,
+                  const int32_t* free_count, int32_t* free_left, int32_t* seq_lens,
+                  int32_t* row_start, int64_t* slot, int32_t* position, int32_t* seq_of_row,
+                  int32_t n_rows, int32_t* status, void* stream);
+
+/* Gives the pages of finished sequences back: for every b with finished[b]
+ * not 0, in ascending b, the ids of its ceil(seq_lens[b]/64) pages (at most
+ * max_pages) go onto the stack in order, those entries of page_table become
+ * -1 and seq_lens[b] 0.  Negative entries of the table are not pushed; ids past
+ * free_capacity are dropped.  free_count is updated in place.  1 <= batch <=
+ * 65535 (0 is a no-op). */
+int dckv_page_release(const int32_t* finished, int32_t batch, int32_t* page_table, int32_t max_pages,
+                      int32_t* seq_lens, int32_t* free_pages, int32_t free_capacity,
+                      int32_t* free_count, void* stream);
+
+/* Rotary positions.  The first rotary_dim coordinates of a head are turned in
+ * rotary_dim/2 planes, plane i by the angle position * theta_i:
+ *   x'_a = m (x_a cos - x_b sin),   x'_b = m (x_b cos + x_a sin),
+ * (a, b) = (i, i + rotary_dim/2) in the half layout, (2i, 2i + 1) in the
+ * interleaved one; the other coordinates stay as they are.  m is `magnitude`.
+ * theta_i = base^(-2i/rotary_dim), for contexts longer than the trained one
+ * scaled by factor s >= 1 (original_context L, turns of a plane over it
+ * n_i = L theta_i / (2 pi)):
+ *   DCKV_ROTARY_LINEAR  theta_i / s
+ *   DCKV_ROTARY_BASE    base s^(r/(r-2)) in place of base, r = rotary_dim > 2:
+ *                       the slowest plane is slowed by s, the fastest kept
+ *   DCKV_ROTARY_TURNS   theta_i (g + (1 - g)/s), g = (n_i - low)/(high - low)
+ *                       clipped to [0, 1]: planes of at least `high` turns are
+ *                       kept, those of at most `low` slowed by s
+ *   DCKV_ROTARY_PLANES  theta_i (1 - g + g/s), g = (i - i0)/(i1 - i0) clipped to
+ *                       [0, 1], i0 = floor(plane(high)), i1 = ceil(plane(low)),
+ *                       clipped to [0, r - 1], plane(n) = r ln(L/(2 pi n)) /
+ *                       (2 ln base): the same in plane indices (a step at i0
+ *                       where i1 <= i0, as of width 1/1000)
+ * Angles are formed and reduced in fp64, the rotation is fp32. */
+typedef enum { DCKV_ROTARY_HALF = 0, DCKV_ROTARY_INTERLEAVED = 1 } dckv_rotary_layout;
+typedef enum {
+  DCKV_ROTARY_UNSCALED = 0,
+  DCKV_ROTARY_LINEAR = 1,
+  DCKV_ROTARY_BASE = 2,
+  DCKV_ROTARY_TURNS = 3,
+  DCKV_ROTARY_PLANES = 4
+} dckv_rotary_scaling;
+typedef struct dckv_rotary_desc {
+  int32_t head_dim;         /* d_h, 2..DCKV_MAX_HEAD_DIM */
+  int32_t rotary_dim;       /* even, 2..head_dim */
+  int32_t layout;           /* dckv_rotary_layout */
+  int32_t scaling;          /* dckv_rotary_scaling */
+  double base;              /* finite, above 1 */
+  double factor;            /* s, finite, at least 1; read by every scaling but UNSCALED */
+  double original_context;  /* L, finite, above 0; read by TURNS and PLANES */
+  double low, high;         /* finite, 0 < low < high; read by TURNS and PLANES */
+  double magnitude;         /* m, finite; 0 means 1 */
+} dckv_rotary_desc;
+typedef struct dckv_rotary dckv_rotary; /* opaque, host memory only */
+
+/* Validate a description and form its angles (EINVAL, ENOMEM; no HIP call).
+ * dckv_rotary_info copies theta_i, [rotary_dim/2], out.  A handle may be
+ * shared by threads. */
+int dckv_rotary_create(const dckv_rotary_desc* desc, dckv_rotary** out);
+void dckv_rotary_destroy(dckv_rotary* rotary);
+int dckv_rotary_info(const dckv_rotary* rotary, double* theta);
+
+/* Turn n_tok tokens of num_heads heads:
+ *   x, out     device, head h of token t at t*token_stride + h*head_stride
+ *              (elements), d_h elements one after another; dtypes DCKV_F32 or
+ *              DCKV_BF16, in any pairing.  out may be x (same dtype and strides);
+ *              otherwise they must not overlap.  Heads of `out` must not overlap
+ *              each other; those of x may (strides of 0 broadcast).  Strides are
+ *              not negative.  Rows in whole 16-byte pieces are fastest.
+ *   position   device int32 [n_tok]; a token of negative position is skipped, its
+ *              row of `out` left as it was
+ *   inverse    nonzero: by the angles -position*theta_i, still times m: the
+ *              transpose of the rotation, which takes the gradient of the output
+ *              to that of the input
+ * n_tok == 0 is a no-op; n_tok at most 2^23, num_heads 1..65535. */
+int dckv_rotary_apply(const dckv_rotary* rotary, const void* x, int32_t x_dtype,
+                      int64_t x_token_stride, int64_t x_head_stride, void* out, int32_t out_dtype,
+                      int64_t out_token_stride, int64_t out_head_stride, const int32_t* position,
+                      int32_t n_tok, int32_t num_heads, int32_t inverse, void* stream);
+
+/* dckv_decode_rope with any rotation whose head_dim is the plan's: keys of
+ * cache position t are turned by t, the query by the newest position. */
+int dckv_decode_rotary(const dckv_plan* plan, const float* q, int32_t batch, const void* pool,
+                       int64_t num_pages, const int32_t* page_table, int32_t max_pages,
+                       const int32_t* seq_lens, int32_t max_context, const void* R_keys,
+                       const void* R_value, const dckv_rotary* rotary, float* out, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
+/* Append of new tokens to the uncompressed bf16 cache of dckv_dense_decode:
+ * keys (turned by their positions where `rotary` is given) and values rounded
+ * to nearest-even into their slots.
+ *   k, v       device, dtype DCKV_F32 or DCKV_BF16, head h of token t at
+ *              t*token_stride + h*head_stride (elements, not negative), d_h
+ *              elements one after another
+ *   slot       device int64 [n_tok]; a negative slot, or one at or beyond
+ *              num_pages*64, skips the token
+ *   rotary     NULL: keys as they are; position is then not read and may be NULL
+ *   position   device int32 [n_tok], not negative where slot is not
+ * Pools are 16-byte aligned; d_h 64, 128 or 256, 1..64 KV heads; n_tok at
+ * most 2^23 (0 is a no-op).  Two tokens with the same slot race. */
+int dckv_dense_append(int32_t num_kv_heads, int32_t head_dim, const void* k, const void* v,
+                      int32_t dtype, int64_t k_token_stride, int64_t k_head_stride,
+                      int64_t v_token_stride, int64_t v_head_stride, const int64_t* slot,
+                      int32_t n_tok, const dckv_rotary* rotary, const int32_t* position,
+                      void* kv_pool, int64_t num_pages, void* stream);
+
+/* ------------------------------------------------------------------------
+ * 8-bit K/V cache: every cached key and value row (one token, one KV head) is
+ * e4m3 (OCP, no infinities) under a power of two of its own, half the bytes of
+ * the bf16 cache:
+ *   x ~ 2^e byte,  e the least integer in [-112, 119] with max|x| <= 448 * 2^e,
+ *   byte = x 2^-e rounded to nearest-even and clamped to +-448.  The row's
+ *   maximum is over its numbers, an infinity counting as the largest finite
+ *   one; a NaN becomes the byte 0x7F.  e is stored as the byte e + 127.
+ * Page of 64 tokens: one block of 128*d_h + 128 bytes per KV head (slot
+ * s = 16 n + 4 q + v, n, q, v < 4; column j):
+ *   key        16 d_h (s/16) + 256 (j/16) + 16 (s%16) + j%16
+ *   value      64 d_h + 1024 (j/16) + 256 q + 16 (j%16) + 4 n + v
+ *   key scale  128 d_h + 16 q + 4 n + v;   value scale 64 bytes further
+ * so that a wave's 16-byte loads are MFMA operands: 16 tokens by 16 columns of
+ * keys, and 16 tokens of a value column in the order in which the scores of
+ * those tokens leave the matrix unit.
+ * d_h 64, 128 or 256; 1..64 KV heads; pools 16-byte aligned. */
+int dckv_quant_page_bytes(int32_t num_kv_heads, int32_t head_dim, int64_t* bytes);
+
+/* Append: arguments as for dckv_dense_append. */
+int dckv_quant_append(int32_t num_kv_heads, int32_t head_dim, const void* k, const void* v,
+                      int32_t dtype, int64_t k_token_stride, int64_t k_head_stride,
+                      int64_t v_token_stride, int64_t v_head_stride, const int64_t* slot,
+                      int32_t n_tok, const dckv_rotary* rotary, const int32_t* position, void* pool,
+                      int64_t num_pages, void* stream);
+
+/* Cached keys and values of given slots (prefix reuse, moving a sequence to
+ * another cache): k, v device [n_tok, H_kv, d_h] of `dtype` (both hold the
+ * values exactly), 16-byte aligned; a slot outside the pool gives zeros.  At most 2^34
+ * values a call. */
+int dckv_quant_read(int32_t num_kv_heads, int32_t head_dim, const void* pool, int64_t num_pages,
+                    const int64_t* slot, int32_t n_tok, void* k, void* v, int32_t dtype,
+                    void* stream);
+
+/* Decode over the 8-bit cache, Q = queries_per_seq (1..DCKV_MAX_QUERIES) causal
+ * queries a sequence as for dckv_decode: q and out fp32 [batch, Q, H_q, d_h],
+ * scale 1/sqrt(d_h), query head h on KV head floor(h / (H_q/H_kv)), any
+ * multiple H_q <= 64 of H_kv.  Query i sits at position seq_len - Q + i and sees
+ * every position up to its own; one that sees none gets zeros, as does a
+ * sequence of length 0.  Page-table entries outside [0, num_pages) are empty
+ * pages.  Whatever lies in slots that a query does not see (NaN included) does
+ * not reach its result.  Products are taken in f16 halves of the fp32 queries
+ * and weights (22 bits and more) and summed in fp32.
+ * split_tokens: context tokens a work split, a multiple of 64, or 0 to choose
+ * from the shape.  A workspace (256-byte aligned; its contents do not matter) of
+ * dckv_quant_workspace_bytes also serves fewer sequences and shorter contexts;
+ * a call of one split a sequence uses none and takes NULL.  batch * Q at most 65535; batch == 0 is a no-op.  Results are
+ * bitwise reproducible for a fixed shape. */
+int dckv_quant_workspace_bytes(int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                               int32_t queries_per_seq, int32_t split_tokens, int32_t batch,
+                               int32_t max_context, size_t* bytes);
+int dckv_quant_decode(int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                      int32_t queries_per_seq, int32_t split_tokens, const float* q, int32_t batch,
+                      const void* pool, int64_t num_pages, const int32_t* page_table,
+                      int32_t max_pages, const int32_t* seq_lens, int32_t max_context, float* out,
+                      void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
  * Offline compression: run once per layer before serving, never on the
  * decode path.
  *

@@ -23,6 +23,8 @@ Modules
               agglomerative clustering, energy ranks, greedy budget
               adjustment, per-group SVD, the cluster-count objective
               (Sec. III-A, III-C)
+  serving     the operators around the caches: page maps, rotary positions, the
+              8-bit K/V pages and attention over them (stated readings)
   calibrate   value calibration refinement: calibration error and the two
               closed-form factor updates (Sec. III-D)
 
@@ -33,4 +35,4 @@ the rotary reading by RoFormer's complex form and hand-worked rotations).
 """
 
 from . import bf16, bookkeeping, params, layout, append, attention, dense  # noqa: F401
-from . import compress, calibrate, rope  # noqa: F401
+from . import compress, calibrate, rope, serving  # noqa: F401

@@ -24,8 +24,9 @@ LIB = os.path.join(PKG, "libdckv.so")
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 ARCH = "gfx950"
 
-HOST_SOURCES = ["plan.cpp", "offline.cpp"]
-HIP_SOURCES = ["append.hip", "decode.hip", "decode_mfma.hip", "dense.hip", "gram.hip", "rope.hip", "noalloc.hip", "decode_pass.hip"]
+HOST_SOURCES = ["plan.cpp", "offline.cpp", "serve.cpp"]
+HIP_SOURCES = ["append.hip", "decode.hip", "decode_mfma.hip", "dense.hip", "gram.hip", "rope.hip", "noalloc.hip", "decode_pass.hip",
+               "page_map.hip", "rotary.hip", "kv_append.hip", "quant_decode.hip"]
 
 HIPCC_FLAGS = [
     "-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",

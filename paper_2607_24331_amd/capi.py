@@ -85,6 +85,21 @@ class LaunchInfo(ctypes.Structure):
     ]
 
 
+class RotaryDesc(ctypes.Structure):
+    _fields_ = [
+        ("head_dim", ctypes.c_int32),
+        ("rotary_dim", ctypes.c_int32),
+        ("layout", ctypes.c_int32),
+        ("scaling", ctypes.c_int32),
+        ("base", ctypes.c_double),
+        ("factor", ctypes.c_double),
+        ("original_context", ctypes.c_double),
+        ("low", ctypes.c_double),
+        ("high", ctypes.c_double),
+        ("magnitude", ctypes.c_double),
+    ]
+
+
 _vp = ctypes.c_void_p
 _i32 = ctypes.c_int32
 _i64 = ctypes.c_int64
@@ -111,6 +126,26 @@ SIGNATURES = {
                                                   ctypes.POINTER(ctypes.c_size_t)]),
     "dckv_dense_decode": (ctypes.c_int, [_i32, _i32, _i32, _i32, _vp, _i32, _vp, _i64, _vp, _i32,
                                          _vp, _i32, _vp, _vp, ctypes.c_size_t, _vp, _vp, _vp]),
+    "dckv_page_map": (ctypes.c_int, [_vp, _vp, _i32, _vp, _i32, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _vp,
+                                     _vp, _i32, _vp, _vp]),
+    "dckv_page_release": (ctypes.c_int, [_vp, _i32, _vp, _i32, _vp, _vp, _i32, _vp, _vp]),
+    "dckv_rotary_create": (ctypes.c_int, [ctypes.POINTER(RotaryDesc), ctypes.POINTER(_vp)]),
+    "dckv_rotary_destroy": (None, [_vp]),
+    "dckv_rotary_info": (ctypes.c_int, [_vp, ctypes.POINTER(ctypes.c_double)]),
+    "dckv_rotary_apply": (ctypes.c_int, [_vp, _vp, _i32, _i64, _i64, _vp, _i32, _i64, _i64, _vp, _i32, _i32,
+                                         _i32, _vp]),
+    "dckv_decode_rotary": (ctypes.c_int, [_vp, _vp, _i32, _vp, _i64, _vp, _i32, _vp, _i32, _vp, _vp,
+                                          _vp, _vp, _vp, ctypes.c_size_t, _vp]),
+    "dckv_dense_append": (ctypes.c_int, [_i32, _i32, _vp, _vp, _i32, _i64, _i64, _i64, _i64, _vp, _i32, _vp,
+                                         _vp, _vp, _i64, _vp]),
+    "dckv_quant_page_bytes": (ctypes.c_int, [_i32, _i32, ctypes.POINTER(ctypes.c_int64)]),
+    "dckv_quant_append": (ctypes.c_int, [_i32, _i32, _vp, _vp, _i32, _i64, _i64, _i64, _i64, _vp, _i32, _vp,
+                                         _vp, _vp, _i64, _vp]),
+    "dckv_quant_read": (ctypes.c_int, [_i32, _i32, _vp, _i64, _vp, _i32, _vp, _vp, _i32, _vp]),
+    "dckv_quant_workspace_bytes": (ctypes.c_int, [_i32, _i32, _i32, _i32, _i32, _i32, _i32,
+                                                  ctypes.POINTER(ctypes.c_size_t)]),
+    "dckv_quant_decode": (ctypes.c_int, [_i32, _i32, _i32, _i32, _i32, _vp, _i32, _vp, _i64, _vp, _i32, _vp,
+                                         _i32, _vp, _vp, ctypes.c_size_t, _vp]),
     "dckv_gram_workspace_bytes": (ctypes.c_int, [_i64, _i32, _i32, ctypes.POINTER(ctypes.c_size_t)]),
     "dckv_gram": (ctypes.c_int, [_vp, _i32, _i64, _i32, _i32, _vp, _vp, ctypes.c_size_t, _vp]),
     "dckv_head_similarity": (ctypes.c_int, [_vp, _i32, _i32, _vp, _vp]),

@@ -1275,17 +1275,17 @@ size_t rope_value_lds_bytes(const dckv_plan& p, int32_t split_tokens) {
 hipError_t launch_decode_rope(const dckv_plan& p, const DecodeShape& sh, const float* q,
                               const void* pool, int64_t num_pages, const int32_t* page_table,
                               int32_t max_pages, const int32_t* seq_lens, const void* R_keys,
-                              const void* R_value, double rope_base, float* out, void* workspace,
-                              hipStream_t stream) {
+                              const void* R_value, const RopeTurns& turns, float* out,
+                              void* workspace, hipStream_t stream) {
   char* ws = static_cast<char*>(workspace);
   void* rt = ws + sh.off_rt;
   bf16* pw = reinterpret_cast<bf16*>(ws + sh.off_p);
   float* part_ml = reinterpret_cast<float*>(ws + sh.off_ml);
   float* part = reinterpret_cast<float*>(ws + sh.off_acc);
   float* amerged = reinterpret_cast<float*>(ws + sh.off_opart);
-  hipError_t e = launch_rope_factors(p, R_keys, rt, stream);
+  hipError_t e = launch_rope_factors(p, turns, R_keys, rt, stream);
   if (e != hipSuccess) return e;
-  e = launch_rope_scores(p, sh, q, pool, num_pages, page_table, max_pages, seq_lens, rt, rope_base,
+  e = launch_rope_scores(p, sh, q, pool, num_pages, page_table, max_pages, seq_lens, rt, turns,
                          pw, part_ml, stream);
   if (e != hipSuccess) return e;
   const size_t lds = rope_value_lds_bytes(p, sh.split_tokens);

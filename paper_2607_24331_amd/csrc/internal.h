@@ -79,6 +79,19 @@ struct RopeTables {
   int64_t roff[DCKV_MAX_HEADS];             // per KV head: element offset of R_g
 };
 
+// The rotation of a rotary decode.  n == 0: every plane (i, i + d_h/2) by
+// pos * base^(-2i/d_h), formed in the kernel.  Otherwise the first n planes take
+// the coordinates that the layout pairs, by turns[i] turns a position, and the
+// coordinates left pair up in planes that are not turned: the score of a key does
+// not depend on the order of its coordinates, so the factors' columns and the
+// query's coordinates are taken in plane order.
+struct RopeTurns {
+  int32_t n, interleaved;
+  float weight;                            // of the turned planes in a score: magnitude^2
+  double log2_base;                        // n == 0
+  double turns[64];                        // d_h / 2 at most
+};
+
 // Launch shape of one decode call, fixed by the plan and (batch, max_context).
 struct DecodeShape {
   int32_t batch;
@@ -228,16 +241,23 @@ void build_rope_tables(dckv_plan& p);
 DecodeShape rope_shape(const dckv_plan& p, int32_t batch, int32_t max_context);
 int rope_max_q_per_kv();
 size_t rope_value_lds_bytes(const dckv_plan& p, int32_t split_tokens);
-hipError_t launch_rope_factors(const dckv_plan& p, const void* R_keys, void* rt, hipStream_t stream);
+hipError_t launch_rope_factors(const dckv_plan& p, const RopeTurns& turns, const void* R_keys, void* rt,
+                               hipStream_t stream);
 hipError_t launch_rope_scores(const dckv_plan& p, const DecodeShape& sh, const float* q,
                               const void* pool, int64_t num_pages, const int32_t* page_table,
                               int32_t max_pages, const int32_t* seq_lens, const void* rt,
-                              double rope_base, void* pbuf, float* part_ml, hipStream_t stream);
+                              const RopeTurns& turns, void* pbuf, float* part_ml, hipStream_t stream);
 hipError_t launch_decode_rope(const dckv_plan& p, const DecodeShape& sh, const float* q,
                               const void* pool, int64_t num_pages, const int32_t* page_table,
                               int32_t max_pages, const int32_t* seq_lens, const void* R_keys,
-                              const void* R_value, double rope_base, float* out, void* workspace,
-                              hipStream_t stream);
+                              const void* R_value, const RopeTurns& turns, float* out,
+                              void* workspace, hipStream_t stream);
+// The whole rotary decode call: checks (messages name `where`), then the kernels.
+int rope_decode(const char* where, const dckv_plan* p, const float* q, int32_t batch, const void* pool,
+                int64_t num_pages, const int32_t* page_table, int32_t max_pages,
+                const int32_t* seq_lens, int32_t max_context, const void* R_keys, const void* R_value,
+                const RopeTurns& turns, float* out, void* workspace, size_t workspace_bytes,
+                void* stream);
 
 // Defined in the kernel sources.
 // plain: fixed splits and one value slice (the rotary decode's)

@@ -11,6 +11,7 @@
 #include <string>
 
 #include "internal.h"
+#include "serve.h"
 
 namespace {
 
@@ -586,6 +587,40 @@ int dckv_rope_workspace_bytes(const dckv_plan* p, int32_t batch, int32_t max_con
   return DCKV_OK;
 }
 
+}  // extern "C"
+
+int dckv::rope_decode(const char* where, const dckv_plan* p, const float* q, int32_t batch,
+                      const void* pool, int64_t num_pages, const int32_t* page_table,
+                      int32_t max_pages, const int32_t* seq_lens, int32_t max_context,
+                      const void* R_keys, const void* R_value, const RopeTurns& turns, float* out,
+                      void* workspace, size_t workspace_bytes, void* stream) {
+  if (batch < 0) return fail(DCKV_EINVAL, "%s: batch %d < 0", where, batch);
+  if (batch == 0) return DCKV_OK;
+  if (!q || !pool || !page_table || !seq_lens || !R_keys || !R_value || !out || !workspace)
+    return fail(DCKV_EINVAL, "%s: null device pointer", where);
+  if (batch > 65535) return fail(DCKV_EINVAL, "%s: batch %d above 65535", where, batch);
+  if (num_pages < 1) return fail(DCKV_EINVAL, "%s: num_pages %lld < 1", where, (long long)num_pages);
+  if (max_pages < 1) return fail(DCKV_EINVAL, "%s: max_pages %d < 1", where, max_pages);
+  if (max_context < 0 || int64_t(max_context) > int64_t(max_pages) * DCKV_PAGE_TOKENS)
+    return fail(DCKV_EINVAL, "%s: max_context %d outside [0, max_pages*64 = %lld]", where, max_context,
+                (long long)max_pages * DCKV_PAGE_TOKENS);
+  if (!aligned(q, 16) || !aligned(pool, 16) || !aligned(R_keys, 16) || !aligned(R_value, 16) ||
+      !aligned(out, 16) || !aligned(page_table, 4) || !aligned(seq_lens, 4))
+    return fail(DCKV_EALIGN, "%s: q, pool, R_keys, R_value and out must be 16-byte aligned", where);
+  if (!aligned(workspace, 256)) return fail(DCKV_EALIGN, "%s: workspace must be 256-byte aligned", where);
+  const dckv::DecodeShape shape = dckv::rope_shape(*p, batch, max_context);
+  if (workspace_bytes < shape.bytes)
+    return fail(DCKV_EWORKSPACE, "%s: workspace of %zu bytes, %zu needed", where, workspace_bytes,
+                shape.bytes);
+  hipError_t e = dckv::launch_decode_rope(*p, shape, q, pool, num_pages, page_table, max_pages,
+                                          seq_lens, R_keys, R_value, turns, out, workspace,
+                                          static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return fail(DCKV_EHIP, "%s: %s", where, hipGetErrorString(e));
+  return DCKV_OK;
+}
+
+extern "C" {
+
 int dckv_decode_rope(const dckv_plan* p, const float* q, int32_t batch, const void* pool,
                      int64_t num_pages, const int32_t* page_table, int32_t max_pages,
                      const int32_t* seq_lens, int32_t max_context, const void* R_keys,
@@ -595,29 +630,32 @@ int dckv_decode_rope(const dckv_plan* p, const float* q, int32_t batch, const vo
   if (st != DCKV_OK) return st;
   if (!(rope_base > 1.0) || !std::isfinite(rope_base))
     return fail(DCKV_EINVAL, "decode_rope: rope_base %g is not a finite number above 1", rope_base);
-  if (batch < 0) return fail(DCKV_EINVAL, "decode_rope: batch %d < 0", batch);
-  if (batch == 0) return DCKV_OK;
-  if (!q || !pool || !page_table || !seq_lens || !R_keys || !R_value || !out || !workspace)
-    return fail(DCKV_EINVAL, "decode_rope: null device pointer");
-  if (batch > 65535) return fail(DCKV_EINVAL, "decode_rope: batch %d above 65535", batch);
-  if (num_pages < 1) return fail(DCKV_EINVAL, "decode_rope: num_pages %lld < 1", (long long)num_pages);
-  if (max_pages < 1) return fail(DCKV_EINVAL, "decode_rope: max_pages %d < 1", max_pages);
-  if (max_context < 0 || int64_t(max_context) > int64_t(max_pages) * DCKV_PAGE_TOKENS)
-    return fail(DCKV_EINVAL, "decode_rope: max_context %d outside [0, max_pages*64 = %lld]", max_context,
-                (long long)max_pages * DCKV_PAGE_TOKENS);
-  if (!aligned(q, 16) || !aligned(pool, 16) || !aligned(R_keys, 16) || !aligned(R_value, 16) ||
-      !aligned(out, 16) || !aligned(page_table, 4) || !aligned(seq_lens, 4))
-    return fail(DCKV_EALIGN, "decode_rope: q, pool, R_keys, R_value and out must be 16-byte aligned");
-  if (!aligned(workspace, 256)) return fail(DCKV_EALIGN, "decode_rope: workspace must be 256-byte aligned");
-  const dckv::DecodeShape shape = dckv::rope_shape(*p, batch, max_context);
-  if (workspace_bytes < shape.bytes)
-    return fail(DCKV_EWORKSPACE, "decode_rope: workspace of %zu bytes, %zu needed", workspace_bytes,
-                shape.bytes);
-  hipError_t e = dckv::launch_decode_rope(*p, shape, q, pool, num_pages, page_table, max_pages,
-                                          seq_lens, R_keys, R_value, rope_base, out, workspace,
-                                          static_cast<hipStream_t>(stream));
-  if (e != hipSuccess) return fail(DCKV_EHIP, "decode_rope: %s", hipGetErrorString(e));
-  return DCKV_OK;
+  dckv::RopeTurns turns{};
+  turns.weight = 1.f;
+  turns.log2_base = std::log2(rope_base);
+  return dckv::rope_decode("decode_rope", p, q, batch, pool, num_pages, page_table, max_pages, seq_lens,
+                           max_context, R_keys, R_value, turns, out, workspace, workspace_bytes, stream);
+}
+
+int dckv_decode_rotary(const dckv_plan* p, const float* q, int32_t batch, const void* pool,
+                       int64_t num_pages, const int32_t* page_table, int32_t max_pages,
+                       const int32_t* seq_lens, int32_t max_context, const void* R_keys,
+                       const void* R_value, const dckv_rotary* rotary, float* out, void* workspace,
+                       size_t workspace_bytes, void* stream) {
+  int st = rope_check("decode_rotary", p);
+  if (st != DCKV_OK) return st;
+  if (!rotary) return fail(DCKV_EINVAL, "decode_rotary: null rotation");
+  if (rotary->desc.head_dim != p->dh)
+    return fail(DCKV_EINVAL, "decode_rotary: a rotation of head_dim %d for a plan of %d",
+                rotary->desc.head_dim, p->dh);
+  dckv::RopeTurns turns{};
+  turns.n = rotary->table.planes;
+  turns.interleaved = rotary->table.interleaved;
+  turns.weight = rotary->table.magnitude * rotary->table.magnitude;
+  std::copy(rotary->table.turns, rotary->table.turns + turns.n, turns.turns);
+  return dckv::rope_decode("decode_rotary", p, q, batch, pool, num_pages, page_table, max_pages,
+                           seq_lens, max_context, R_keys, R_value, turns, out, workspace,
+                           workspace_bytes, stream);
 }
 
 // ------------------------------------------------ uncompressed baseline

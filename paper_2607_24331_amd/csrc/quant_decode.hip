@@ -1,0 +1,543 @@
+// Decode over 8-bit K/V pages on MFMA (gfx950).
+//
+//   o_r = sum_t softmax_t(q_r k_t / sqrt(d)) v_t,  k_t = 2^a_t K_t, v_t = 2^b_t V_t
+//
+// with K_t, V_t e4m3 rows and a_t, b_t their exponents.  e4m3 values are f16
+// values, so both products run on the f16 matrix unit with exact cache operands;
+// the fp32 operands of the other side, the queries and the weights p_t 2^b_t, are
+// split into two f16 halves (22 bits and more; each brought below 2^14 by a
+// power of two, so that the halves stay clear of f16's ends) and cost two MFMAs
+// each.  Sums are fp32.
+//
+// Per (context split, KV head, row slice) a work-group of four waves; wave w
+// takes pages w, w + 4, ... of the split and meets the others only at the end.
+//   scores  S[token][row] = K[token][:] Q[row][:]: a lane's 16-byte key load is 16
+//           columns of one token, the A operand of two MFMA 16x16x32 steps.
+//   softmax base 2, running maximum and sum a row (a row's 64 scores of a page lie
+//           in four lanes, 16 each: two shuffles for the maximum).
+//   output  O[column][row] += V^T[column][token] P[token][row]: the scores of a
+//           lane are those of tokens 16 n + 4 (lane / 16) + v, and the page holds a
+//           value column's tokens in that order, so the weights feed the second
+//           product from the registers they were made in: no LDS, no shuffle.
+// The keys of a wave's next page are loaded when the current ones are used up,
+// its values likewise, so a page's bytes are in flight all the time.
+// Reads 2 d + 2 bytes a token and KV head; bound by those bytes as long as the
+// rows fit one 16-row tile.
+//   merge   one work-group per (query, head, sequence): fixed ascending-split
+//           log-sum-exp sum.
+#include <algorithm>
+#include <cmath>
+
+#include "device.h"
+#include "internal.h"
+#include "serve.h"
+
+namespace dckv {
+namespace {
+
+typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kWaves = 4;
+constexpr int kTop = 14;                   // split operands lie below 2^kTop
+
+__device__ __forceinline__ floatx4 mfma(u32x4 a, u32x4 b, floatx4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, a), __builtin_bit_cast(half8, b),
+                                                c, 0, 0, 0);
+}
+
+// Two dwords of e4m3 bytes (8 values) as f16, exactly.
+__device__ __forceinline__ u32x4 widen(uint32_t lo, uint32_t hi) {
+  return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, false)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, true)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, false)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, true))};
+}
+
+// x, y = hi + lo in f16 halves: hi truncated to 11 bits, lo what is left of the
+// 24, truncated to 11 again: off by at most 2^-21 relative.
+__device__ __forceinline__ void halves(float x, float y, uint32_t& hi, uint32_t& lo) {
+  const auto h = __builtin_amdgcn_cvt_pkrtz(x, y);
+  const auto l = __builtin_amdgcn_cvt_pkrtz(x - float(h[0]), y - float(h[1]));
+  hi = __builtin_bit_cast(uint32_t, h);
+  lo = __builtin_bit_cast(uint32_t, l);
+}
+
+__device__ __forceinline__ int byte_of(uint32_t w, int v) { return int((w >> (8 * v)) & 0xFFu); }
+
+// Bytes v of a dword with v < n kept.
+__device__ __forceinline__ uint32_t keep_bytes(uint32_t w, int n) {
+  return n >= 4 ? w : (n <= 0 ? 0u : w & ((1u << (8 * n)) - 1u));
+}
+
+// D = d_h; RT 16-row tiles of (query, head) rows.
+template <int D, int RT>
+__global__ __launch_bounds__(kWaves * 64, (D == 256 || RT == 2) ? 1 : 2) void quant_split(
+    const float* __restrict__ q, const uint8_t* __restrict__ pool, int64_t num_pages,
+    const int32_t* __restrict__ page_table, int max_pages, const int32_t* __restrict__ seq_lens,
+    int max_context, int split_pages, int n_split, int n_units, int slices, int n_q_heads,
+    int n_kv_heads, int queries, float scale, float* __restrict__ part_o, float* __restrict__ part_ml,
+    float* __restrict__ out) {
+  constexpr int KL = D / 64;               // 16-byte key loads a 16-token tile
+  constexpr int DT = D / 16;               // 16-column value tiles, a load each
+  __shared__ float red_o[kWaves][16][D + 4];
+  __shared__ float red_m[kWaves][16], red_l[kWaves][16];
+
+  // Ids u, u + 8, ... run on one XCD: the slices of a unit are neighbours there
+  // and share its bytes in one L2.
+  const int id = blockIdx.x;
+  const int u = (id / (8 * slices)) * 8 + (id & 7);
+  const int slice = (id >> 3) % slices;
+  if (u >= n_units) return;
+  const int kv = u % n_kv_heads;
+  const int b = (u / n_kv_heads) % (n_units / (n_kv_heads * n_split));
+  const int split = u / (n_units / n_split);
+  const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lq = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int per = n_q_heads / n_kv_heads, rows = queries * per;
+  const int row0 = slice * RT * 16;
+  int T = seq_lens[b];
+  T = T < 0 ? 0 : (T > max_context ? max_context : T);
+  const int np_all = (T + 63) >> 6;
+  const int p0 = split * split_pages, p1 = min(p0 + split_pages, np_all);
+  if (p0 >= p1 && n_split > 1) return;     // the merge reads only splits holding pages
+
+  // ---- queries: row row0 + 16 t + lr, columns 64 i + 16 lq .. + 15, in halves of
+  // q 2^(kTop - 1 - floor(log2 max|q|)); rowscale takes that and the scale back
+  u32x4 qh[RT][KL][2], ql[RT][KL][2];
+  float rowscale[RT];
+  int limit[RT];                           // tokens the row sees
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    const int r = row0 + 16 * t + lr;
+    const bool in = r < rows;
+    const int i = in ? r / per : 0, j = in ? r % per : 0;
+    limit[t] = in ? T - queries + i + 1 : 0;
+    const float* src = q + ((int64_t(b) * queries + i) * n_q_heads + kv * per + j) * D + 16 * lq;
+    float x[KL][16];
+    float top = 0.f;
+#pragma unroll
+    for (int c = 0; c < KL; ++c)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const floatx4 f = *reinterpret_cast<const floatx4*>(src + 64 * c + 4 * e);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          x[c][4 * e + k] = in ? f[k] : 0.f;
+          top = fmaxf(top, fabsf(x[c][4 * e + k]));
+        }
+      }
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    // exponent of top, kept where its inverse is a normal number
+    const int ex = min(126, max(-100, int(__float_as_uint(top) >> 23) - 127));
+    const int sh = kTop - 1 - ex;          // -113 .. 113
+    const float up = __uint_as_float(uint32_t(127 + sh) << 23);
+    rowscale[t] = __uint_as_float(uint32_t(127 - sh) << 23) * scale;
+#pragma unroll
+    for (int c = 0; c < KL; ++c)
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          uint32_t hi, lo;
+          halves(x[c][8 * s + 2 * k] * up, x[c][8 * s + 2 * k + 1] * up, hi, lo);
+          qh[t][c][s][k] = hi;
+          ql[t][c][s][k] = lo;
+        }
+  }
+
+  floatx4 acc[RT][DT];
+  // running state of a row: maximum m of the scores, um of score - m + value scale
+  // byte, sum l of 2^(score - m).  acc is in units of 2^(k - 127 - kTop), k = ceil(um):
+  // its weights 2^(score - m + byte - k + kTop) reach 2^kTop whatever the scales are.
+  float m[RT], um[RT], l[RT];
+  int k[RT];
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    m[t] = um[t] = -INFINITY;
+    l[t] = 0.f;
+    k[t] = 0;
+#pragma unroll
+    for (int i = 0; i < DT; ++i) acc[t][i] = floatx4{0.f, 0.f, 0.f, 0.f};
+  }
+  const int64_t block = 128 * (D + 1);
+  const int32_t* table = page_table + int64_t(b) * max_pages;
+  const int first = p0 + w;                // this wave's pages: first, first + 4, ...
+  const int mine = p1 > first ? (p1 - first + kWaves - 1) / kWaves : 0;
+  int ids = -1;                            // lane i: the page of step (64-step window) + i
+  auto load_ids = [&](int step0) {
+    const int i = step0 + lane;
+    ids = i < mine ? table[first + i * kWaves] : -1;
+    if (ids >= num_pages) ids = -1;
+  };
+  auto page_ptr = [&](int step, bool& valid) {
+    const int page = __builtin_amdgcn_readlane(ids, step & 63);
+    valid = page >= 0;
+    return pool + (int64_t(valid ? page : 0) * n_kv_heads + kv) * block;   // an empty page is masked
+  };
+  u32x4 kr[4 * KL], vr[DT], ksc, vsc;
+  auto load_keys = [&](const uint8_t* p) {
+#pragma unroll
+    for (int i = 0; i < 4 * KL; ++i) kr[i] = *reinterpret_cast<const u32x4*>(p + 1024 * i + 16 * lane);
+    ksc = *reinterpret_cast<const u32x4*>(p + 128 * D + 16 * lq);
+  };
+  auto load_values = [&](const uint8_t* p) {
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+      vr[i] = *reinterpret_cast<const u32x4*>(p + 64 * D + 1024 * i + 16 * lane);
+    vsc = *reinterpret_cast<const u32x4*>(p + 128 * D + 64 + 16 * lq);
+  };
+  bool valid = false;
+  const uint8_t* ptr = pool;
+  if (mine > 0) {
+    load_ids(0);
+    ptr = page_ptr(0, valid);
+    load_keys(ptr);
+    load_values(ptr);
+  }
+
+  for (int step = 0; step < mine; ++step) {
+    bool next_valid = valid;
+    const uint8_t* next = ptr;
+    const bool more = step + 1 < mine;
+    if (more) {
+      if (((step + 1) & 63) == 0) load_ids(step + 1);
+      next = page_ptr(step + 1, next_valid);
+    }
+    const int pos0 = (first + step * kWaves) * 64;
+    const int there = valid ? min(64, T - pos0) : 0;        // tokens of the page
+
+    // ---- scores, 16 tokens a tile: token 16 n + 4 lq + v, row lr
+    floatx4 s[RT][4];
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+#pragma unroll
+      for (int t = 0; t < RT; ++t) s[t][n] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < KL; ++c)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const u32x4 a = widen(kr[n * KL + c][2 * h], kr[n * KL + c][2 * h + 1]);
+#pragma unroll
+          for (int t = 0; t < RT; ++t) {
+            s[t][n] = mfma(a, ql[t][c][h], s[t][n]);
+            s[t][n] = mfma(a, qh[t][c][h], s[t][n]);
+          }
+        }
+    }
+    const u32x4 kscale = ksc;
+    if (more) load_keys(next);
+
+    // ---- the page's value scales; slots behind the sequence hold anything
+    u32x4 vscale = vsc;
+    const int tail = there - 4 * lq;       // of tile n: tail - 16 n tokens of this lane are there
+    if (there < 64) {
+#pragma unroll
+      for (int n = 0; n < 4; ++n) vscale[n] = keep_bytes(vscale[n], tail - 16 * n);
+    }
+
+    // ---- softmax
+    u32x4 ph[RT][2], pl[RT][2];            // weights of steps 0, 1 in halves
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      const int see = min(there, limit[t] - pos0) - 4 * lq;
+      float top = -INFINITY;
+#pragma unroll
+      for (int n = 0; n < 4; ++n)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          const float ks = __uint_as_float(uint32_t(byte_of(kscale[n], v)) << 23);
+          const float x = s[t][n][v] * (rowscale[t] * ks);
+          s[t][n][v] = 16 * n + v < see ? x : -INFINITY;
+          top = fmaxf(top, s[t][n][v]);
+        }
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float m_new = fmaxf(m[t], top);
+      const float base = m_new == -INFINITY ? 0.f : m_new;   // nothing seen yet: weights 0
+      const float down = m[t] - base;
+      float sum = 0.f, utop = -INFINITY;
+#pragma unroll
+      for (int n = 0; n < 4; ++n)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          const float e = s[t][n][v] - base;
+          utop = fmaxf(utop, e + float(byte_of(vscale[n], v)));
+          s[t][n][v] = exp2f(e);
+          sum += s[t][n][v];
+        }
+      utop = fmaxf(utop, __shfl_xor(utop, 16));
+      utop = fmaxf(utop, __shfl_xor(utop, 32));
+      um[t] = fmaxf(um[t] + down, utop);
+      const int k_new = um[t] == -INFINITY ? 0 : int(ceilf(um[t]));
+      const float keep = exp2f(down + float(k[t] - k_new));
+      l[t] = fmaf(l[t], exp2f(down), sum);
+      m[t] = m_new;
+      k[t] = k_new;
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        float p[4];
+#pragma unroll
+        for (int v = 0; v < 4; ++v) p[v] = ldexpf(s[t][n][v], byte_of(vscale[n], v) - k_new + kTop);
+#pragma unroll
+        for (int k2 = 0; k2 < 2; ++k2) {
+          uint32_t hi, lo;
+          halves(p[2 * k2], p[2 * k2 + 1], hi, lo);
+          ph[t][n >> 1][2 * (n & 1) + k2] = hi;
+          pl[t][n >> 1][2 * (n & 1) + k2] = lo;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < DT; ++i)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) acc[t][i][v] *= keep;
+    }
+
+    // ---- output
+    if (there < 64) {
+#pragma unroll
+      for (int i = 0; i < DT; ++i)
+#pragma unroll
+        for (int n = 0; n < 4; ++n) vr[i][n] = keep_bytes(vr[i][n], tail - 16 * n);
+    }
+    // A token that one query of the page sees and another does not has weight 0
+    // for the other; 0 times a NaN is none, so a page of such tokens that holds a
+    // NaN is added query by query, each over the tokens that it sees.
+    bool apart = false;
+    if (queries > 1 && pos0 + 64 > T - queries + 1) {
+      uint32_t nan = 0;
+#pragma unroll
+      for (int i = 0; i < DT; ++i)
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+          const uint32_t low = vr[i][n] & 0x7F7F7F7Fu;       // 0x7F: the only NaN
+          nan |= (low + 0x01010101u) & 0x80808080u;
+        }
+      apart = __any(nan != 0);
+    }
+    if (!apart) {
+#pragma unroll
+      for (int i = 0; i < DT; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const u32x4 a = widen(vr[i][2 * h], vr[i][2 * h + 1]);
+#pragma unroll
+          for (int t = 0; t < RT; ++t) {
+            acc[t][i] = mfma(a, pl[t][h], acc[t][i]);
+            acc[t][i] = mfma(a, ph[t][h], acc[t][i]);
+          }
+        }
+    } else {
+      for (int qi = 0; qi < queries; ++qi) {
+        const int see = min(there, T - queries + qi + 1 - pos0) - 4 * lq;
+#pragma unroll
+        for (int i = 0; i < DT; ++i) {
+          u32x4 x;
+#pragma unroll
+          for (int n = 0; n < 4; ++n) x[n] = keep_bytes(vr[i][n], see - 16 * n);
+#pragma unroll
+          for (int t = 0; t < RT; ++t) {
+            floatx4 y = acc[t][i];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const u32x4 a = widen(x[2 * h], x[2 * h + 1]);
+              y = mfma(a, pl[t][h], y);
+              y = mfma(a, ph[t][h], y);
+            }
+            const bool mine_q = (row0 + 16 * t + lr) / per == qi;
+#pragma unroll
+            for (int v = 0; v < 4; ++v) acc[t][i][v] = mine_q ? y[v] : acc[t][i][v];
+          }
+        }
+      }
+    }
+    if (more) load_values(next);
+    ptr = next;
+    valid = next_valid;
+  }
+
+  // ---- the four waves' states, one row tile at a time
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    float sum = l[t];
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    const float unit = ldexpf(1.f, k[t] - 127 - kTop);
+    if (t > 0) __syncthreads();
+    if (lq == 0) {
+      red_m[w][lr] = m[t];
+      red_l[w][lr] = sum;
+    }
+#pragma unroll
+    for (int i = 0; i < DT; ++i) {
+      floatx4 y;
+#pragma unroll
+      for (int v = 0; v < 4; ++v) y[v] = acc[t][i][v] * unit;
+      *reinterpret_cast<floatx4*>(&red_o[w][lr][16 * i + 4 * lq]) = y;
+    }
+    __syncthreads();
+    for (int e = tid; e < 16 * D; e += kWaves * 64) {
+      const int r = e / D, d = e % D;
+      const int row = row0 + 16 * t + r;
+      if (row >= rows) continue;
+      float M = red_m[0][r];
+#pragma unroll
+      for (int k = 1; k < kWaves; ++k) M = fmaxf(M, red_m[k][r]);
+      float L = 0.f, o = 0.f;
+#pragma unroll
+      for (int k = 0; k < kWaves; ++k) {
+        if (red_l[k][r] == 0.f) continue;  // the wave saw nothing of the row
+        const float f = exp2f(red_m[k][r] - M);
+        L = fmaf(f, red_l[k][r], L);
+        o = fmaf(f, red_o[k][r][d], o);
+      }
+      const int64_t orow = (int64_t(b) * queries + row / per) * n_q_heads + kv * per + row % per;
+      if (n_split == 1) {
+        out[orow * D + d] = L == 0.f ? 0.f : o / L;
+      } else {
+        const int64_t prow = orow * n_split + split;
+        part_o[prow * D + d] = o;
+        if (d == 0) {
+          part_ml[prow * 2] = M;
+          part_ml[prow * 2 + 1] = L;
+        }
+      }
+    }
+  }
+}
+
+// One work-group a (query, head) row: part_o rows of its splits, ascending.
+template <int D>
+__global__ __launch_bounds__(256) void quant_merge(const float* __restrict__ part_o,
+                                                   const float* __restrict__ part_ml,
+                                                   const int32_t* __restrict__ seq_lens, int max_context,
+                                                   int split_pages, int n_split, int rows_per_seq,
+                                                   float* __restrict__ out) {
+  constexpr int G = 256 / (D / 4);         // splits in flight: D/4 threads a split, four columns each
+  __shared__ floatx4 red[G][D / 4];
+  const int64_t row = blockIdx.x;
+  const int b = int(row / rows_per_seq);
+  const int tid = threadIdx.x, g = tid / (D / 4), c = tid % (D / 4);
+  int T = seq_lens[b];
+  T = T < 0 ? 0 : (T > max_context ? max_context : T);
+  const int ns = ((T + 63) / 64 + split_pages - 1) / split_pages;
+  const float* ml = part_ml + row * n_split * 2;
+  float M = -INFINITY;
+  for (int s = 0; s < ns; ++s) M = fmaxf(M, ml[2 * s]);
+  float L = 0.f;
+  for (int s = 0; s < ns; ++s)
+    if (ml[2 * s + 1] != 0.f) L = fmaf(exp2f(ml[2 * s] - M), ml[2 * s + 1], L);
+  floatx4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int s = g; s < ns; s += G) {
+    if (ml[2 * s + 1] == 0.f) continue;    // nothing seen
+    const float f = exp2f(ml[2 * s] - M);
+    const floatx4 x = *reinterpret_cast<const floatx4*>(part_o + (row * n_split + s) * D + 4 * c);
+#pragma unroll
+    for (int v = 0; v < 4; ++v) o[v] = fmaf(f, x[v], o[v]);
+  }
+  red[g][c] = o;
+  __syncthreads();
+  if (g == 0) {
+    for (int k = 1; k < G; ++k)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) o[v] += red[k][c][v];
+#pragma unroll
+    for (int v = 0; v < 4; ++v) o[v] = L == 0.f ? 0.f : o[v] / L;
+    *reinterpret_cast<floatx4*>(out + row * D + 4 * c) = o;
+  }
+}
+
+size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
+
+template <int D, int RT>
+hipError_t launch_t(const QuantShape& sh, const float* q, const void* pool, int64_t num_pages,
+                    const int32_t* page_table, int32_t max_pages, const int32_t* seq_lens, float* out,
+                    void* workspace, hipStream_t stream) {
+  char* ws = static_cast<char*>(workspace);
+  float* part_o = reinterpret_cast<float*>(ws + sh.off_o);
+  float* part_ml = reinterpret_cast<float*>(ws + sh.off_ml);
+  const float scale = kLog2e / std::sqrt(float(D));
+  const int64_t units = int64_t(sh.batch) * sh.kv_heads * sh.n_split;
+  const int64_t groups = (units + 7) / 8 * 8 * sh.slices;
+  hipLaunchKernelGGL((quant_split<D, RT>), dim3(uint32_t(groups)), dim3(kWaves * 64), 0, stream, q,
+                     static_cast<const uint8_t*>(pool), num_pages, page_table, max_pages, seq_lens,
+                     sh.max_context, sh.split_pages, sh.n_split, int(units), sh.slices, sh.q_heads,
+                     sh.kv_heads, sh.queries, scale, part_o, part_ml, out);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || sh.n_split == 1) return e;
+  hipLaunchKernelGGL((quant_merge<D>), dim3(uint32_t(sh.batch) * sh.queries * sh.q_heads), dim3(256), 0,
+                     stream, part_o, part_ml, seq_lens, sh.max_context, sh.split_pages, sh.n_split,
+                     sh.queries * sh.q_heads, out);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+// Splits where the library chooses: about kTargetGroups work-groups in all.
+constexpr int64_t kTargetGroups = 1024;
+
+QuantShape quant_shape(int32_t q_heads, int32_t kv_heads, int32_t head_dim, int32_t queries,
+                       int32_t split_tokens, int32_t batch, int32_t max_context) {
+  QuantShape s{};
+  s.q_heads = q_heads;
+  s.kv_heads = kv_heads;
+  s.head_dim = head_dim;
+  s.queries = queries;
+  s.batch = batch;
+  s.max_context = max_context;
+  s.rows = queries * (q_heads / kv_heads);
+  s.tiles = (s.rows > 16 && head_dim < 256) ? 2 : 1;
+  s.slices = (s.rows + 16 * s.tiles - 1) / (16 * s.tiles);
+  const int64_t pages = std::max<int64_t>(1, (int64_t(max_context) + 63) / 64);
+  int64_t per = split_tokens / DCKV_PAGE_TOKENS;
+  if (per == 0) {   // about four work-groups a compute unit, at least a page a wave
+    const int64_t work = pages * batch * kv_heads * s.slices;
+    per = std::max<int64_t>(4, (work + kTargetGroups - 1) / kTargetGroups);
+    per = (per + 3) / 4 * 4;
+  }
+  s.split_pages = int32_t(std::min(per, pages));
+  s.n_split = int32_t((pages + s.split_pages - 1) / s.split_pages);
+  if (s.n_split > 1) {
+    const size_t rows = size_t(batch) * queries * q_heads * s.n_split;
+    s.off_ml = align_up(rows * head_dim * sizeof(float), 256);
+    s.bytes = s.off_ml + align_up(rows * 2 * sizeof(float), 256);
+  }
+  return s;
+}
+
+// A call's splits in all, batch * n_split, are at most batch * ceil(pages / 4) and
+// at most kTargetGroups / (kv_heads * slices) + batch where the library chooses:
+// neither bound shrinks with the batch or the context.
+size_t quant_workspace_bytes(const QuantShape& s, bool chosen) {
+  const int64_t pages = std::max<int64_t>(1, (int64_t(s.max_context) + 63) / 64);
+  int64_t splits = int64_t(s.batch) * s.n_split;
+  if (chosen)
+    splits = std::min(int64_t(s.batch) * ((pages + 3) / 4),
+                      kTargetGroups / (int64_t(s.kv_heads) * s.slices) + s.batch);
+  const size_t rows = size_t(splits) * s.queries * s.q_heads;
+  return align_up(rows * s.head_dim * sizeof(float), 256) + align_up(rows * 2 * sizeof(float), 256);
+}
+
+hipError_t launch_quant_decode(const QuantShape& sh, const float* q, const void* pool,
+                               int64_t num_pages, const int32_t* page_table, int32_t max_pages,
+                               const int32_t* seq_lens, float* out, void* workspace,
+                               hipStream_t stream) {
+#define DCKV_GO(D, RT)                                                                                \
+  return launch_t<D, RT>(sh, q, pool, num_pages, page_table, max_pages, seq_lens, out, workspace, stream)
+  switch (sh.head_dim) {
+    case 64:
+      if (sh.tiles == 2) DCKV_GO(64, 2);
+      DCKV_GO(64, 1);
+    case 128:
+      if (sh.tiles == 2) DCKV_GO(128, 2);
+      DCKV_GO(128, 1);
+    case 256: DCKV_GO(256, 1);
+  }
+#undef DCKV_GO
+  return hipErrorInvalidValue;
+}
+
+}  // namespace dckv

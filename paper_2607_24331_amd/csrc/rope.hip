@@ -77,12 +77,29 @@ __device__ __forceinline__ void turn(int pos, double omega, float& c, float& s) 
   s = __builtin_amdgcn_sinf(f);
 }
 
+// Coordinate of the head at place `dim` of plane order: a plane's first
+// coordinates in places 0 .. d/2 - 1, its second ones d/2 further.
+__device__ __forceinline__ int rope_coord(const RopeTurns& t, int half, int dim) {
+  if (t.n == 0) return dim;
+  const bool second = dim >= half;
+  const int i = second ? dim - half : dim;
+  if (i >= t.n) return 2 * t.n + (i - t.n) + (second ? half - t.n : 0);
+  return t.interleaved ? 2 * i + (second ? 1 : 0) : i + (second ? t.n : 0);
+}
+
+// Turns a position of plane i (of d/2).
+__device__ __forceinline__ double rope_omega(const RopeTurns& t, int d, int i) {
+  if (t.n == 0) return exp2(-(2.0 * i / d) * t.log2_base) * kInv2Pi;
+  return i < t.n ? t.turns[i] : 0.0;
+}
+
 // ---------------------------------------------------------------------------
 // Grid (blocks of 256 threads over the head's transposed blocks, KV heads).
 // Thread: one lane of one 16 x 32 block: row 16 it + l % 16 of R^T (a column
 // of R_{g,h}), key columns 32 c + 8 (l / 16) .. + 7.
 __global__ __launch_bounds__(256) void rope_factors(const bf16* __restrict__ Rk,
-                                                    bf16* __restrict__ rt, RopeTables tb) {
+                                                    bf16* __restrict__ rt, RopeTurns turns,
+                                                    RopeTables tb) {
   const int kv = blockIdx.y;
   const int e = blockIdx.x * 256 + threadIdx.x;
   const int dt = tb.head_dim / 16;
@@ -93,7 +110,7 @@ __global__ __launch_bounds__(256) void rope_factors(const bf16* __restrict__ Rk,
   const int ci = blk / dt, it = blk % dt;
   const int dim = 16 * it + (l & 15);
   const int col0 = 32 * (c_lo + ci) + 8 * (l >> 4);
-  const bf16* src = Rk + tb.roff[kv] + tb.rcol[kv] + dim;
+  const bf16* src = Rk + tb.roff[kv] + tb.rcol[kv] + rope_coord(turns, tb.head_dim / 2, dim);
   uint32_t w[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
@@ -264,8 +281,9 @@ __global__ __launch_bounds__(256, 1) void rope_scores(
     const float* __restrict__ q, const bf16* __restrict__ pool, int64_t num_pages,
     const int32_t* __restrict__ page_table, int max_pages, const int32_t* __restrict__ seq_lens,
     int max_context, int split_tokens, int n_split, int n_work, const bf16* __restrict__ rt,
-    int RK, int64_t page_elems, double log2_base, float scale, int n_slices,
-    bf16* __restrict__ pbuf, float* __restrict__ part_ml, RopeTables tb) {
+    int RK, int64_t page_elems, float scale, int n_slices,
+    bf16* __restrict__ pbuf, float* __restrict__ part_ml, RopeTurns turns,
+    RopeTables tb) {
   constexpr int D = 16 * DT, HALF = DT / 2;
   constexpr int FPT = DT / 4;                     // 16-byte factor loads a thread per chunk
   constexpr int P = kDepth;
@@ -307,7 +325,7 @@ __global__ __launch_bounds__(256, 1) void rope_scores(
 
   // ---- prologue: plane frequencies, the split's pages, turned queries
   if (tid < D / 2) {
-    const double om = exp2(-(2.0 * tid / D) * log2_base) * kInv2Pi;
+    const double om = rope_omega(turns, D, tid);
     omega[tid] = om;
     float c16, s16;
     turn(16, om, c16, s16);
@@ -326,9 +344,10 @@ __global__ __launch_bounds__(256, 1) void rope_scores(
       const float* qh = q + (int64_t(b) * Hq + kv * qpk + hh) * D;
       float c, s;
       turn(pq, omega[i], c, s);
-      const float xa = qh[i], xb = qh[i + D / 2];
-      qr[hh][i] = (xa * c - xb * s) * scale;
-      qr[hh][i + D / 2] = (xb * c + xa * s) * scale;
+      const float xa = qh[rope_coord(turns, D / 2, i)], xb = qh[rope_coord(turns, D / 2, i + D / 2)];
+      const float sc_i = i < turns.n ? scale * turns.weight : scale;
+      qr[hh][i] = (xa * c - xb * s) * sc_i;
+      qr[hh][i + D / 2] = (xb * c + xa * s) * sc_i;
     }
   }
 
@@ -464,8 +483,9 @@ __global__ __launch_bounds__(512, 1) void rope_scores_res(
     const float* __restrict__ q, const bf16* __restrict__ pool, int64_t num_pages,
     const int32_t* __restrict__ page_table, int max_pages, const int32_t* __restrict__ seq_lens,
     int max_context, int split_tokens, int n_split, int spw, int n_ranges, int n_work,
-    const bf16* __restrict__ rt, int RK, int64_t page_elems, double log2_base, float scale,
-    int n_slices, bf16* __restrict__ pbuf, float* __restrict__ part_ml, RopeTables tb) {
+    const bf16* __restrict__ rt, int RK, int64_t page_elems, float scale,
+    int n_slices, bf16* __restrict__ pbuf, float* __restrict__ part_ml, RopeTurns turns,
+    RopeTables tb) {
   constexpr int W = kResWaves, D = 16 * DT, P = kResDepth;
   extern __shared__ __align__(16) unsigned char smem[];
   bf16* fac = reinterpret_cast<bf16*>(smem);                                // [nch][DT][512]
@@ -509,7 +529,7 @@ __global__ __launch_bounds__(512, 1) void rope_scores_res(
   // ---- prologue: frequencies and pages; then the turned queries and the
   // head's factor blocks (eight 16-byte loads in flight a thread)
   if (tid < D / 2) {
-    const double om = exp2(-(2.0 * tid / D) * log2_base) * kInv2Pi;
+    const double om = rope_omega(turns, D, tid);
     omega[tid] = om;
     float c16, s16;
     turn(16, om, c16, s16);
@@ -528,9 +548,10 @@ __global__ __launch_bounds__(512, 1) void rope_scores_res(
       const float* qh = q + (int64_t(b) * Hq + kv * qpk + hh) * D;
       float c, s;
       turn(pq, omega[i], c, s);
-      const float xa = qh[i], xb = qh[i + D / 2];
-      qr[hh * D + i] = (xa * c - xb * s) * scale;
-      qr[hh * D + i + D / 2] = (xb * c + xa * s) * scale;
+      const float xa = qh[rope_coord(turns, D / 2, i)], xb = qh[rope_coord(turns, D / 2, i + D / 2)];
+      const float sc_i = i < turns.n ? scale * turns.weight : scale;
+      qr[hh * D + i] = (xa * c - xb * s) * sc_i;
+      qr[hh * D + i + D / 2] = (xb * c + xa * s) * sc_i;
     }
     const int nvec = nch * DT * 64;
     for (int base = tid; base < nvec; base += 8 * W * 64) {
@@ -678,7 +699,8 @@ DecodeShape rope_shape(const dckv_plan& p, int32_t batch, int32_t max_context) {
 int rope_max_split_tokens() { return kRopeMaxSplit; }
 int rope_max_q_per_kv() { return kMaxQpk; }
 
-hipError_t launch_rope_factors(const dckv_plan& p, const void* R_keys, void* rt, hipStream_t stream) {
+hipError_t launch_rope_factors(const dckv_plan& p, const RopeTurns& turns, const void* R_keys, void* rt,
+                               hipStream_t stream) {
   int max_blocks = 0;
   for (int kv = 0; kv < p.Hkv; ++kv) {
     const int koff = p.rope.koff[kv], rank = p.rope.rank[kv];
@@ -686,7 +708,7 @@ hipError_t launch_rope_factors(const dckv_plan& p, const void* R_keys, void* rt,
     max_blocks = std::max(max_blocks, nch * (p.dh / 16));
   }
   hipLaunchKernelGGL(rope_factors, dim3((max_blocks * 64 + 255) / 256, p.Hkv), dim3(256), 0, stream,
-                     static_cast<const bf16*>(R_keys), static_cast<bf16*>(rt), p.rope);
+                     static_cast<const bf16*>(R_keys), static_cast<bf16*>(rt), turns, p.rope);
   return hipGetLastError();
 }
 
@@ -698,8 +720,7 @@ size_t rope_res_lds_bytes(int dh) {
 hipError_t launch_rope_scores(const dckv_plan& p, const DecodeShape& sh, const float* q,
                               const void* pool, int64_t num_pages, const int32_t* page_table,
                               int32_t max_pages, const int32_t* seq_lens, const void* rt,
-                              double rope_base, void* pbuf, float* part_ml, hipStream_t stream) {
-  const double log2_base = std::log2(rope_base);
+                              const RopeTurns& turns, void* pbuf, float* part_ml, hipStream_t stream) {
   const float scale = kLog2e / std::sqrt(float(p.dh));
   const bool events = p.prof_before && p.prof_after;   // stamped by the kernel's own dispatch
   int max_nch = 0;
@@ -726,14 +747,14 @@ hipError_t launch_rope_scores(const dckv_plan& p, const DecodeShape& sh, const f
                               p.prof_before, p.prof_after, 0u, q, static_cast<const bf16*>(pool),
                               num_pages, page_table, max_pages, seq_lens, sh.max_context, L,
                               sh.n_split, spw, n_ranges, n_work, static_cast<const bf16*>(rt), p.RK,
-                              p.page_elems, log2_base, scale, p.mfma.n_slices,
-                              static_cast<bf16*>(pbuf), part_ml, p.rope);
+                              p.page_elems, scale, p.mfma.n_slices,
+                              static_cast<bf16*>(pbuf), part_ml, turns, p.rope);
       else
         hipLaunchKernelGGL(kern, dim3(n_work), dim3(kResWaves * 64), lds, stream, q,
                            static_cast<const bf16*>(pool), num_pages, page_table, max_pages,
                            seq_lens, sh.max_context, L, sh.n_split, spw, n_ranges, n_work,
-                           static_cast<const bf16*>(rt), p.RK, p.page_elems, log2_base, scale,
-                           p.mfma.n_slices, static_cast<bf16*>(pbuf), part_ml, p.rope);
+                           static_cast<const bf16*>(rt), p.RK, p.page_elems, scale,
+                           p.mfma.n_slices, static_cast<bf16*>(pbuf), part_ml, turns, p.rope);
       return hipGetLastError();
     };
     if (p.dh == 128) return go(rope_scores_res<8>);
@@ -746,14 +767,14 @@ hipError_t launch_rope_scores(const dckv_plan& p, const DecodeShape& sh, const f
       hipExtLaunchKernelGGL(kern, dim3(n_work), dim3(256), 0, stream, p.prof_before, p.prof_after,
                             0u, q, static_cast<const bf16*>(pool), num_pages, page_table, max_pages,
                             seq_lens, sh.max_context, sh.split_tokens, sh.n_split, n_work,
-                            static_cast<const bf16*>(rt), p.RK, p.page_elems, log2_base, scale,
-                            p.mfma.n_slices, static_cast<bf16*>(pbuf), part_ml, p.rope);
+                            static_cast<const bf16*>(rt), p.RK, p.page_elems, scale,
+                            p.mfma.n_slices, static_cast<bf16*>(pbuf), part_ml, turns, p.rope);
     else
       hipLaunchKernelGGL(kern, dim3(n_work), dim3(256), 0, stream, q,
                          static_cast<const bf16*>(pool), num_pages, page_table, max_pages, seq_lens,
                          sh.max_context, sh.split_tokens, sh.n_split, n_work,
-                         static_cast<const bf16*>(rt), p.RK, p.page_elems, log2_base, scale,
-                         p.mfma.n_slices, static_cast<bf16*>(pbuf), part_ml, p.rope);
+                         static_cast<const bf16*>(rt), p.RK, p.page_elems, scale,
+                         p.mfma.n_slices, static_cast<bf16*>(pbuf), part_ml, turns, p.rope);
     return hipGetLastError();
   };
   if (p.dh == 128) return go(rope_scores<8>);
