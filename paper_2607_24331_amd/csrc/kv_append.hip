@@ -2,15 +2,17 @@
 // positions, and values into bf16 pages or into e4m3 pages under a power of
 // two a row; and cached rows read back.
 //
-// append_rows  a work-group takes up to 64 consecutive tokens of one head, keys
-//   or values (grid: token blocks, heads, keys / values).  d/8 lanes hold a row,
-//   8 columns each, in fp32; a key's partners in the half layout come through
-//   LDS.  For e4m3 the row's maximum (shuffles) gives the exponent, exact in
+// append_rows  a work-group takes a block of consecutive tokens and a few heads, keys
+//   or values.  d/8 lanes hold four rows at a time, 8 columns of each, in fp32.  The
+//   sines and cosines of the block's tokens are formed once, in LDS, for all its
+//   heads; a key's partners in the half layout are loaded a second time (cache
+//   hits).  For e4m3 the row's maximum (shuffles) gives the exponent, exact in
 //   integer arithmetic on the maximum's bits; the conversion is the hardware's
 //   round-to-nearest-even after an exact multiplication by 2^-e.
 //   Key bytes go out 8 at a time.  A value column holds its tokens side by side
-//   (slots 4a .. 4a + 3 in one dword), so value bytes are gathered in LDS and
-//   written as dwords where the block holds all four slots, as bytes elsewhere.
+//   (slots 4a .. 4a + 3 in one dword): where four consecutive rows fill those slots,
+//   their bytes are transposed in registers and go out as dwords, else as bytes.
+// read_rows  the same blocks the other way.
 // Each element is read once and written once: memory bounds long prompts,
 // latency single tokens.
 #include <algorithm>
@@ -20,8 +22,9 @@
 namespace dckv {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kMaxRows = 64;              // tokens a work-group
+constexpr int kMaxRows = 128;             // tokens a work-group
+constexpr int64_t kAppendGroups = 512;    // work-groups an append aims for: angles and slots serve many heads
+constexpr int64_t kReadGroups = 2048;     // and a read, which has neither
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -35,27 +38,71 @@ __device__ __forceinline__ int scale_exponent(float amax) {
   return min(119, max(-112, e));
 }
 
-// x / 2^e as e4m3 bytes in pairs (x within 448 * 2^e, clamped; a NaN stays one).
-__device__ __forceinline__ float scaled(float x, float inv) {
-  const float y = x * inv;
-  const float z = fminf(fmaxf(y, -448.f), 448.f);
-  return y == y ? z : y;
+// Four values times inv = 2^-e as e4m3 bytes.  Every |x| inv is at most 448 unless
+// the row holds infinities or numbers above 448 * 2^119 (clamp).  A NaN is the byte
+// 0x7F whatever its sign: no other byte has its seven low bits set.
+__device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d, float inv, bool clamp) {
+  a *= inv;
+  b *= inv;
+  c *= inv;
+  d *= inv;
+  if (clamp) {
+    a = a == a ? fminf(fmaxf(a, -448.f), 448.f) : a;
+    b = b == b ? fminf(fmaxf(b, -448.f), 448.f) : b;
+    c = c == c ? fminf(fmaxf(c, -448.f), 448.f) : c;
+    d = d == d ? fminf(fmaxf(d, -448.f), 448.f) : d;
+  }
+  int q = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  q = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, q, true);
+  const uint32_t w = uint32_t(q);
+  return w & ~(((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u);
 }
 
+// Columns j .. j + 7 of a row as loaded.
 template <typename T>
-__device__ __forceinline__ void load8(const T* p, bool wide, float (&x)[8]) {
-  if (wide) {
-    constexpr int N = 16 / sizeof(T);
+struct Row8 {
+  static constexpr int N = sizeof(T) / 2;  // 16-byte pieces
+  u32x4 w[N];
+  __device__ __forceinline__ void load(const T* src, bool wide) {
+    if (wide) {
 #pragma unroll
-    for (int i = 0; i < 8 / N; ++i) {
-      const Piece<T, N> a = reinterpret_cast<const Piece<T, N>*>(p)[i];
+      for (int k = 0; k < N; ++k) w[k] = reinterpret_cast<const u32x4*>(src)[k];
+    } else {
 #pragma unroll
-      for (int e = 0; e < N; ++e) x[i * N + e] = to_f32(a.v[e]);
+      for (int k = 0; k < 4 * N; ++k) {
+        if constexpr (sizeof(T) == 4) {
+          w[k / 4][k % 4] = reinterpret_cast<const uint32_t*>(src)[k];
+        } else {
+          const uint16_t* p = reinterpret_cast<const uint16_t*>(src) + 2 * k;
+          w[k / 4][k % 4] = uint32_t(p[0]) | uint32_t(p[1]) << 16;
+        }
+      }
     }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = to_f32(p[e]);
   }
+  __device__ __forceinline__ float get(int e) const {
+    if constexpr (sizeof(T) == 4) {
+      return __uint_as_float(w[e / 4][e % 4]);
+    } else {
+      const uint32_t d = w[0][e / 2];
+      return __uint_as_float(e % 2 ? d & 0xFFFF0000u : d << 16);
+    }
+  }
+};
+
+// Bytes of a row's 8 columns and the row's exponent, from L lanes that hold it.
+template <int L>
+__device__ __forceinline__ int quantize8(const float (&x)[8], uint32_t& lo, uint32_t& hi) {
+  float amax = 0.f;                        // fmaxf passes a NaN over
+#pragma unroll
+  for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(x[e]));
+#pragma unroll
+  for (int o = 1; o < L; o <<= 1) amax = fmaxf(amax, __shfl_xor(amax, o));
+  const int e2 = scale_exponent(amax);
+  const float inv = __uint_as_float(uint32_t(127 - e2) << 23);
+  const bool clamp = __any(e2 == 119);
+  lo = pack4(x[0], x[1], x[2], x[3], inv, clamp);
+  hi = pack4(x[4], x[5], x[6], x[7], inv, clamp);
+  return e2;
 }
 
 // Byte offsets inside a head's block of an e4m3 page.
@@ -73,185 +120,457 @@ __device__ __forceinline__ int scale_at(int s, bool value) {
   return 128 * D + (value ? 64 : 0) + 16 * ((s & 15) >> 2) + token_at(s);
 }
 
-template <typename T, int D, bool QUANT>
-__global__ __launch_bounds__(kThreads) void append_rows(
-    RotaryTable rot, const T* __restrict__ k, RowStrides ks, const T* __restrict__ v, RowStrides vs,
-    bool k_wide, bool v_wide, const int64_t* __restrict__ slot, const int32_t* __restrict__ position,
-    int n_tok, int rows, int n_heads, void* pool, int64_t n_slots) {
-  constexpr int L = D / 8;                 // lanes a row
-  constexpr int RPI = kThreads / L;        // rows an iteration
-  constexpr int PITCH = D + 4;
-  __shared__ float xrow[RPI][PITCH];       // rows of the iteration (keys of the half layout)
-  __shared__ __align__(16) uint8_t vbytes[QUANT ? kMaxRows : 1][QUANT ? D : 16];
-  __shared__ int64_t slot_s[kMaxRows];
-  const int tid = threadIdx.x;
-  const int t0 = blockIdx.x * rows, h = blockIdx.y;
-  const bool value = blockIdx.z != 0;
-  const int n = min(rows, n_tok - t0);
-  const int row_in = tid / L, c = tid % L, j0 = 8 * c;
-  if (tid < kMaxRows) {
-    const int64_t s = tid < n ? slot[t0 + tid] : -1;
-    slot_s[tid] = s >= 0 && s < n_slots ? s : -1;
+// ---------------------------------------------------------------------------
+// Threads of a work-group and what it takes at once: d/8 lanes a row, 8 columns
+// each, four rows a lane.
+template <int D>
+struct Block {
+  static constexpr int kThreads = D == 256 ? 512 : 256;
+  static constexpr int kLanes = D / 8;
+  static constexpr int kGroups = kThreads / kLanes;
+  static constexpr int kRows = 4 * kGroups;            // tokens: 128 at d = 64, else 64
+};
+
+// Slots of a block of n tokens from t0 on with three more on either side
+// (slot_s[r + 3] is that of row r; -1 outside the pool or the call).
+__device__ __forceinline__ void load_slots(const int64_t* slot, int n_tok, int64_t n_slots, int t0,
+                                           int n, int64_t* slot_s) {
+  for (int i = threadIdx.x; i < n + 6; i += blockDim.x) {
+    const int t = t0 + i - 3;
+    const int64_t s = t >= 0 && t < n_tok ? slot[t] : -1;
+    slot_s[i] = s >= 0 && s < n_slots ? s : -1;
+  }
+}
+
+// Where a block of tokens that nominally begins at token t does: at the next token of
+// a page's first slot where t's sequence reaches one within 63 tokens, so that a long
+// run of tokens is cut at its pages and a page has one writer.
+__device__ __forceinline__ int block_start(const int64_t* slot, int n_tok, int t) {
+  if (t >= n_tok) return n_tok;
+  const int64_t s = slot[t];
+  const int u = t + int(-s & 63);
+  return s >= 0 && u < n_tok && slot[u] >= 0 && (slot[u] & 63) == 0 ? u : t;
+}
+
+// Work units of the block's values.  Four consecutive rows in slots 4a .. 4a + 3 of
+// a page make one (a quad: 4 r + 1, r the first row, whose block writes all four),
+// any other live row one by itself (4 r).  The first kGroups units are worked on
+// together; a quad of them has a place in its half's tile, where a page's 16 quads
+// lie as the page has them, unless another quad of the half has it (tile[half][4 q +
+// n] is its first slot, kNobody: nobody's).
+constexpr unsigned long long kNobody = ~0ull;
+struct Units {
+  int unit[kMaxRows];
+  int count[kMaxRows / 64];
+  int tiled;                               // whether the tiles hold any
+  unsigned long long tile[kMaxRows / 64][16];
+};
+__device__ __forceinline__ int tile_place(int64_t slot) {   // of the quad that starts at `slot`
+  const int s = int(slot & 63);
+  return 4 * ((s >> 2) & 3) + (s >> 4);
+}
+template <int GROUPS>
+__device__ __forceinline__ int make_units(const int64_t* slot_s, int n, Units& un) {
+  const int r = threadIdx.x, lane = r & 63, w = r >> 6;
+  int u = -1;
+  int64_t sl = -1;
+  if (r < n) {
+    sl = slot_s[r + 3];
+    if (sl >= 0) {
+      const int m = int(sl & 3);
+      const int64_t* f = slot_s + (r + 3 - m);
+      const bool four = f[0] == sl - m && f[1] == sl - m + 1 && f[2] == sl - m + 2 && f[3] == sl - m + 3;
+      if (!four)
+        u = 4 * r;
+      else if (m == 0)
+        u = 4 * r + 1;
+    }
+  }
+  const uint64_t live = __ballot(u >= 0);
+  if (w < kMaxRows / 64 && lane == 0) un.count[w] = __popcll(live);
+  if (r < kMaxRows / 64 * 16) un.tile[r >> 4][r & 15] = kNobody;
+  if (r == 0) un.tiled = 0;
+  __syncthreads();
+  int at = __popcll(live & ((uint64_t(1) << lane) - 1)), all = 0;
+#pragma unroll
+  for (int k = 0; k < kMaxRows / 64; ++k) {
+    if (k < w) at += un.count[k];
+    all += un.count[k];
+  }
+  if (u >= 0) un.unit[at] = u;
+  if (u >= 0 && (u & 1) && at < GROUPS) {
+    atomicMin(&un.tile[r >> 6][tile_place(sl)], (unsigned long long)sl);   // the lowest slot has it
+    un.tiled = 1;
   }
   __syncthreads();
-  const bool turned = !value && rot.planes > 0;
-  const int64_t page_bytes = int64_t(n_heads) * 128 * (D + 1);
-  for (int r0 = 0; r0 < n; r0 += RPI) {
-    const int r = r0 + row_in;
-    const int64_t sl = r < n ? slot_s[r] : -1;
-    float x[8];
+  return all;
+}
+
+// Rows a .. d of four bytes each to columns: byte i of out[j] is byte j of row i.
+__device__ __forceinline__ void transpose4(uint32_t a, uint32_t b, uint32_t c, uint32_t d,
+                                           uint32_t (&out)[4]) {
+  const uint32_t ab0 = __builtin_amdgcn_perm(b, a, 0x05010400u), ab1 = __builtin_amdgcn_perm(b, a, 0x07030602u);
+  const uint32_t cd0 = __builtin_amdgcn_perm(d, c, 0x05010400u), cd1 = __builtin_amdgcn_perm(d, c, 0x07030602u);
+  out[0] = __builtin_amdgcn_perm(cd0, ab0, 0x05040100u);
+  out[1] = __builtin_amdgcn_perm(cd0, ab0, 0x07060302u);
+  out[2] = __builtin_amdgcn_perm(cd1, ab1, 0x05040100u);
+  out[3] = __builtin_amdgcn_perm(cd1, ab1, 0x07060302u);
+}
+
+// A half's tile of value bytes in LDS: column j = 8 c + e, dword 4 q + n of it.
+// Columns of one e lie together, shifted by four dwords an e, so that the lanes of
+// a store (one e, all c) and of a load (all e) spread over the banks.
+template <int D>
+__device__ __forceinline__ int tile_at(int j, int place) {
+  return (j & 7) * (2 * D + 4) + (j >> 3) * 16 + place;
+}
+
+// What a work-group of append_rows works on.
+template <typename T>
+struct AppendBlock {
+  const T* src;                            // keys or values of the block's first token
+  RowStrides st;
+  bool wide, value;
+  int n, n_heads, h0, h1;
+  char* pool;
+};
+
+// Keys, and values of bf16 pages: a row a group of lanes, head after head.  The sines
+// and cosines of a lane's columns are formed once and stay in registers: twice as many
+// as the planes have in the half layout, but no lane waits for another.
+template <typename T, int D, bool QUANT>
+__device__ __forceinline__ void append_by_row(const AppendBlock<T>& b, const RotaryTable& rot,
+                                              const int64_t* slot, int64_t n_slots,
+                                              const int32_t* position) {
+  constexpr int L = Block<D>::kLanes;
+  const int r = threadIdx.x / L, c = threadIdx.x % L, j0 = 8 * c;
+  if (r >= b.n) return;
+  int64_t sl = slot[r];
+  if (sl >= n_slots) sl = -1;
+  if (sl < 0) return;                      // the lanes of a row leave together
+  const int P = rot.planes;
+  const bool turn = !b.value && j0 < 2 * P, low = j0 < P;
+  // half layout, whole pieces: the partners are another lane's 8 columns
+  const bool pair = turn && !rot.interleaved && P % 8 == 0;
+  const int jp = low ? j0 + P : j0 - P;
+  const T* src = b.src + r * b.st.token + b.h0 * b.st.head;
+  Row8<T> own[2], partner[2];              // of two heads: their rows are on their way
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = 0.f;
-    if (sl >= 0) {
-      if (value)
-        load8(v + int64_t(t0 + r) * vs.token + h * vs.head + j0, v_wide, x);
-      else
-        load8(k + int64_t(t0 + r) * ks.token + h * ks.head + j0, k_wide, x);
+  for (int i = 0; i < 2; ++i)
+    if (b.h0 + i < b.h1) {
+      own[i].load(src + i * b.st.head + j0, b.wide);
+      if (pair) partner[i].load(src + i * b.st.head + jp, b.wide);
     }
-    if (turned) {
-      const int pos = sl >= 0 ? position[t0 + r] : 0;
-      if (rot.interleaved) {
+  float2 g[8];                             // of the columns' planes; an interleaved one's at its first column
+  if (turn) {
+    const int pos = position[r];
+    if (rot.interleaved) {
+#pragma unroll
+      for (int e = 0; e < 8; e += 2) {
+        const int plane = (j0 + e) / 2;
+        g[e] = plane < P ? rotary_factor(rot, plane, pos) : make_float2(1.f, 0.f);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {        // a plane's second coordinate takes the sine the other way
+        const int j = j0 + e;
+        g[e] = make_float2(1.f, 0.f);
+        if (j < 2 * P) {
+          g[e] = rotary_factor(rot, j < P ? j : j - P, pos);
+          g[e].y = j < P ? -g[e].y : g[e].y;
+        }
+      }
+    }
+  }
+  const int s = int(sl & 63);
+  char* at = b.pool + (sl >> 6) * (int64_t(b.n_heads) * (QUANT ? 128 * (D + 1) : 256 * D));
+  for (int h2 = b.h0; h2 < b.h1; h2 += 2) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int h = h2 + i;
+      if (h >= b.h1) break;
+      float x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = own[i].get(e);
+      if (pair) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = x[e] * g[e].x + partner[i].get(e) * g[e].y;
+      } else if (turn && rot.interleaved) {
 #pragma unroll
         for (int e = 0; e < 8; e += 2) {
-          const int plane = (j0 + e) >> 1;
-          if (plane < rot.planes) {
-            const float2 f = rotary_factor(rot, plane, pos);
-            const float a = x[e], b = x[e + 1];
-            x[e] = a * f.x - b * f.y;
-            x[e + 1] = b * f.x + a * f.y;
-          }
+          const float u = x[e], w = x[e + 1];
+          x[e] = u * g[e].x - w * g[e].y;
+          x[e + 1] = w * g[e].x + u * g[e].y;
         }
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) xrow[row_in][j0 + e] = x[e];
-        __syncthreads();
+      } else if (turn) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const int j = j0 + e;
-          if (j < rot.planes) {
-            const float2 f = rotary_factor(rot, j, pos);
-            x[e] = x[e] * f.x - xrow[row_in][j + rot.planes] * f.y;
-          } else if (j < 2 * rot.planes) {
-            const float2 f = rotary_factor(rot, j - rot.planes, pos);
-            x[e] = x[e] * f.x + xrow[row_in][j - rot.planes] * f.y;
-          }
+          if (j < 2 * P) x[e] = x[e] * g[e].x + to_f32(src[j < P ? j + P : j - P]) * g[e].y;
         }
-        __syncthreads();                   // xrow is rewritten
       }
-    }
-    if constexpr (!QUANT) {
-      if (sl >= 0) {
+      if (h + 2 < b.h1) {
+        own[i].load(src + 2 * b.st.head + j0, b.wide);
+        if (pair) partner[i].load(src + 2 * b.st.head + jp, b.wide);
+      }
+      src += b.st.head;
+      if constexpr (QUANT) {
+        uint32_t lo, hi;
+        const int e2 = quantize8<L>(x, lo, hi);
+        char* blk = at + int64_t(h) * 128 * (D + 1);
+        *reinterpret_cast<u32x2*>(blk + key_at<D>(s, j0)) = u32x2{lo, hi};
+        if (c == 0) blk[scale_at<D>(s, false)] = char(e2 + 127);
+      } else {
         Piece<bf16, 8> y;
 #pragma unroll
         for (int e = 0; e < 8; ++e) y.v[e] = from_f32<bf16>(x[e]);
-        bf16* page = static_cast<bf16*>(pool) + (sl >> 6) * (int64_t(n_heads) * 128 * D);
-        *reinterpret_cast<Piece<bf16, 8>*>(
-            page + (value ? int64_t(64) * n_heads * D : 0) + (int64_t(h) * 64 + (sl & 63)) * D + j0) = y;
-      }
-    } else {
-      float amax = 0.f;                    // fmaxf passes a NaN over
-#pragma unroll
-      for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(x[e]));
-#pragma unroll
-      for (int o = 1; o < L; o <<= 1) amax = fmaxf(amax, __shfl_xor(amax, o));
-      const int e2 = scale_exponent(amax);
-      const float inv = __uint_as_float(uint32_t(127 - e2) << 23);
-      u32x2 w;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        int q = __builtin_amdgcn_cvt_pk_fp8_f32(scaled(x[4 * i], inv), scaled(x[4 * i + 1], inv), 0, false);
-        q = __builtin_amdgcn_cvt_pk_fp8_f32(scaled(x[4 * i + 2], inv), scaled(x[4 * i + 3], inv), q, true);
-        w[i] = uint32_t(q);
-#pragma unroll
-        for (int e = 0; e < 4; ++e)        // one NaN byte, 0x7F, whatever the sign
-          if (x[4 * i + e] != x[4 * i + e]) w[i] &= ~(0x80u << (8 * e));
-      }
-      if (value && r < n) *reinterpret_cast<u32x2*>(&vbytes[r][j0]) = w;
-      if (sl >= 0) {
-        uint8_t* blk = static_cast<uint8_t*>(pool) + (sl >> 6) * page_bytes + int64_t(h) * 128 * (D + 1);
-        const int s = int(sl & 63);
-        if (!value) *reinterpret_cast<u32x2*>(blk + key_at<D>(s, j0)) = w;
-        if (c == 0) blk[scale_at<D>(s, value)] = uint8_t(e2 + 127);
-      }
-    }
-  }
-  if constexpr (QUANT) {
-    if (!value) return;                    // the whole work-group
-    __syncthreads();
-    // a thread a column and row: the row of slot 4a writes all four where the
-    // block holds slots 4a .. 4a + 3 in consecutive rows, else each its byte
-    for (int i = tid; i < n * D; i += kThreads) {
-      const int r = i / D, j = i % D;
-      const int64_t sl = slot_s[r];
-      if (sl < 0) continue;
-      const int s = int(sl & 63), first = r - (s & 3);
-      const int64_t s4 = sl & ~int64_t(3);
-      const bool four = first >= 0 && first + 3 < n && slot_s[first] == s4 && slot_s[first + 1] == s4 + 1 &&
-                        slot_s[first + 2] == s4 + 2 && slot_s[first + 3] == s4 + 3;
-      uint8_t* at = static_cast<uint8_t*>(pool) + (sl >> 6) * page_bytes +
-                    int64_t(h) * 128 * (D + 1) + value_at<D>(s, j);
-      if (!four) {
-        *at = vbytes[r][j];
-      } else if ((s & 3) == 0) {
-        *reinterpret_cast<uint32_t*>(at) = uint32_t(vbytes[r][j]) | uint32_t(vbytes[r + 1][j]) << 8 |
-                                           uint32_t(vbytes[r + 2][j]) << 16 |
-                                           uint32_t(vbytes[r + 3][j]) << 24;
+        *reinterpret_cast<Piece<bf16, 8>*>(at + 2 * ((b.value ? int64_t(64) * b.n_heads * D : 0) +
+                                                     (int64_t(h) * 64 + s) * D + j0)) = y;
       }
     }
   }
 }
 
-// Cached rows as values: D/8 lanes a (token, head), 8 columns each of key and value.
+// Values of e4m3 pages, by units; tiles are filled for one head while those of the
+// head before are written out.
+template <typename T, int D, int HALVES, int TILE>
+__device__ __forceinline__ void append_by_unit(const AppendBlock<T>& b, const int64_t* slot_s, Units& un,
+                                               uint32_t (*tiles)[HALVES][TILE]) {
+  constexpr int L = Block<D>::kLanes, GROUPS = Block<D>::kGroups, THREADS = Block<D>::kThreads;
+  const int units = make_units<GROUPS>(slot_s, b.n, un);
+  const int tid = threadIdx.x, grp = tid / L, c = tid % L, j0 = 8 * c;
+  const int64_t page = int64_t(b.n_heads) * 128 * (D + 1);
+  // this thread's 16-byte pieces of the tiles (a column's four places), and where they
+  // go if one page has all four
+  constexpr int PIECES = HALVES * 4 * D / THREADS;
+  int piece_lds[PIECES];
+  int64_t piece_at[PIECES];
+  bool whole[PIECES];
+#pragma unroll
+  for (int i = 0; i < PIECES; ++i) {
+    const int g = tid + i * THREADS, hf = g / (4 * D), p = g % (4 * D);
+    const int j = 16 * (p >> 6) + (p & 15), q = (p >> 4) & 3;
+    const unsigned long long* t4 = &un.tile[hf][4 * q];
+    const unsigned long long pg = t4[0] >> 6;
+    whole[i] = t4[3] != kNobody && t4[1] >> 6 == pg && t4[2] >> 6 == pg && t4[3] >> 6 == pg;
+    piece_lds[i] = hf * TILE + tile_at<D>(j, 4 * q);
+    piece_at[i] = (whole[i] ? int64_t(pg) * page : 0) + value_at<D>(4 * q, j);
+  }
+  for (int u0 = 0; u0 < units; u0 += GROUPS) {   // once where the rows are consecutive slots
+    const int u = u0 + grp;
+    const int code = u < units ? un.unit[u] : 0;
+    const bool live = u < units, four = live && (code & 1);
+    const int r0 = code >> 2;
+    const int64_t sl = live ? slot_s[r0 + 3] : 0;
+    const int s = int(sl & 63), half = r0 >> 6, place = tile_place(sl);
+    const bool tiled = four && u0 == 0 && un.tile[half][place] == (unsigned long long)sl;
+    // a quad's rows past the block belong to it; a row by itself stands in for four
+    const T* src = b.src + r0 * b.st.token + b.h0 * b.st.head + j0;
+    const int64_t step = four ? b.st.token : 0;
+    Row8<T> own[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) own[i].load(src + i * step, b.wide);
+    for (int h = b.h0; h < b.h1; ++h) {
+      uint32_t w[4][2];
+      char* blk = b.pool + (sl >> 6) * page + int64_t(h) * 128 * (D + 1);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = own[i].get(e);
+        const int e2 = quantize8<L>(x, w[i][0], w[i][1]);
+        if (c == 0 && live && (four || i == 0)) blk[scale_at<D>(s, true) + i] = char(e2 + 127);
+      }
+      src += b.st.head;
+      if (h + 1 < b.h1)                    // the next head's rows are on their way
+#pragma unroll
+        for (int i = 0; i < 4; ++i) own[i].load(src + i * step, b.wide);
+      auto& tile = tiles[(h - b.h0) & 1];
+      if (four) {
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+          uint32_t col[4];
+          transpose4(w[0][p], w[1][p], w[2][p], w[3][p], col);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int j = j0 + 4 * p + e;
+            if (tiled)
+              tile[half][tile_at<D>(j, place)] = col[e];
+            else
+              *reinterpret_cast<uint32_t*>(blk + value_at<D>(s, j)) = col[e];
+          }
+        }
+      } else if (live) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) blk[value_at<D>(s, j0 + e)] = char(w[0][e / 4] >> (8 * (e % 4)));
+      }
+      if (u0 > 0 || !un.tiled) continue;
+      // 16 bytes of a column: the quads of its four places, together where they are
+      // one page's
+      __syncthreads();
+      char* head = b.pool + int64_t(h) * 128 * (D + 1);
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i) {
+        const u32x4 x4 = *reinterpret_cast<const u32x4*>(&tile[0][0] + piece_lds[i]);
+        if (whole[i]) {
+          *reinterpret_cast<u32x4*>(head + piece_at[i]) = x4;
+        } else {
+          const unsigned long long* t4 = &un.tile[0][0] + (tid + i * THREADS) / (4 * D) * 16 + (tid >> 4 & 3) * 4;
+#pragma unroll
+          for (int m = 0; m < 4; ++m)
+            if (t4[m] != kNobody)
+              *reinterpret_cast<uint32_t*>(head + piece_at[i] + int64_t(t4[m] >> 6) * page + 4 * m) = x4[m];
+        }
+      }
+    }
+  }
+}
+
+// What a launch of append_rows writes.
+enum Part { kBoth, kKeys, kValues };
+
+// Grid (token blocks, head blocks, keys / values of kBoth).  Blocks of `rows` tokens by
+// `hb` heads, rows at most the row groups of a work-group, of kValues Block<D>::kRows;
+// kValues cuts its blocks at pages (one block more: the tokens before the first cut).
+template <typename T, int D, bool QUANT, Part PART>
+__global__ __launch_bounds__(Block<D>::kThreads) void append_rows(
+    RotaryTable rot, const T* __restrict__ k, RowStrides ks, const T* __restrict__ v, RowStrides vs,
+    bool k_wide, bool v_wide, const int64_t* __restrict__ slot, const int32_t* __restrict__ position,
+    int n_tok, int rows, int hb, int n_heads, void* pool, int64_t n_slots) {
+  using B = Block<D>;
+  constexpr bool UNITS = QUANT && PART != kKeys;
+  constexpr int HALVES = B::kRows / 64, TILE = UNITS ? 8 * (2 * D + 4) : 1;
+  __shared__ __align__(16) uint32_t tiles[UNITS ? 2 : 1][HALVES][TILE];
+  __shared__ int64_t slot_s[UNITS ? kMaxRows + 6 : 1];
+  __shared__ Units un;
+  const bool value = PART == kBoth ? blockIdx.z != 0 : PART == kValues;
+  const int h0 = blockIdx.y * hb;
+  AppendBlock<T> b{value ? v : k, value ? vs : ks, value ? v_wide : k_wide, value, 0, n_heads, h0,
+                   min(n_heads, h0 + hb), static_cast<char*>(pool)};
+  int t0 = blockIdx.x * rows, t1 = min(n_tok, t0 + rows);
+  if constexpr (UNITS) {
+    if (value) {
+      if constexpr (PART == kValues) {
+        t1 = block_start(slot, n_tok, t0);
+        t0 = blockIdx.x == 0 ? 0 : block_start(slot, n_tok, t0 - rows);
+      }
+      const T* src = b.src;
+      for (; t0 < t1; t0 += B::kRows) {    // twice at most: a cut moves by up to 63 tokens
+        b.n = min(B::kRows, t1 - t0);
+        b.src = src + t0 * b.st.token;
+        load_slots(slot, n_tok, n_slots, t0, b.n, slot_s);
+        __syncthreads();
+        append_by_unit<T, D, HALVES, TILE>(b, slot_s, un, tiles);
+        __syncthreads();                   // LDS is written again
+      }
+      return;
+    }
+  }
+  if constexpr (PART != kValues) {
+    b.n = t1 - t0;
+    b.src += t0 * b.st.token;
+    append_by_row<T, D, QUANT>(b, rot, slot + t0, n_slots, position + t0);
+  }
+}
+
+// Cached rows as values, in the same blocks and units; grid as append_rows.
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads) void read_rows(const uint8_t* __restrict__ pool, int64_t n_slots,
-                                                      const int64_t* __restrict__ slot, int n_heads,
-                                                      int64_t n_items, T* __restrict__ k,
+__global__ __launch_bounds__(Block<D>::kThreads) void read_rows(const uint8_t* __restrict__ pool, int64_t n_slots,
+                                                      const int64_t* __restrict__ slot, int n_tok, int rows,
+                                                      int hb, int n_heads, T* __restrict__ k,
                                                       T* __restrict__ v) {
-  constexpr int L = D / 8;
-  const int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x;
-  if (i >= n_items) return;
-  const int64_t row = i / L;               // token * n_heads + head
-  const int j0 = 8 * int(i % L);
-  const int64_t tok = row / n_heads;
-  const int h = int(row - tok * n_heads);
-  const int64_t sl = slot[tok];
-  float kf[8], vf[8];
+  constexpr int L = Block<D>::kLanes, GROUPS = Block<D>::kGroups;
+  __shared__ int64_t slot_s[kMaxRows + 6];
+  __shared__ Units un;
+  const int tid = threadIdx.x;
+  const int t0 = blockIdx.x * rows;
+  const bool value = blockIdx.z != 0;
+  const int n = min(rows, n_tok - t0);
+  const int grp = tid / L, j0 = 8 * (tid % L);
+  load_slots(slot, n_tok, n_slots, t0, n, slot_s);
+  __syncthreads();
+  const int units = value ? make_units<GROUPS>(slot_s, n, un) : (n + 3) / 4;
+  const int64_t page = int64_t(n_heads) * 128 * (D + 1);
+  const int h1 = min(n_heads, int(blockIdx.y + 1) * hb);
+  T* out = value ? v : k;
+  auto store = [&](int r, int h, const uint32_t (&w)[2], float scale) {
+    constexpr int N = 16 / sizeof(T);
+    T* at = out + (int64_t(t0 + r) * n_heads + h) * D + j0;
+    float x[8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) kf[e] = vf[e] = 0.f;
-  if (sl >= 0 && sl < n_slots) {
-    const uint8_t* blk = pool + (sl >> 6) * (int64_t(n_heads) * 128 * (D + 1)) + int64_t(h) * 128 * (D + 1);
-    const int s = int(sl & 63);
-    const u32x2 w = *reinterpret_cast<const u32x2*>(blk + key_at<D>(s, j0));
-    u32x2 u = {0u, 0u};
+    for (int p = 0; p < 2; ++p) {
+      x[4 * p] = __builtin_amdgcn_cvt_f32_fp8(int(w[p]), 0) * scale;
+      x[4 * p + 1] = __builtin_amdgcn_cvt_f32_fp8(int(w[p]), 1) * scale;
+      x[4 * p + 2] = __builtin_amdgcn_cvt_f32_fp8(int(w[p]), 2) * scale;
+      x[4 * p + 3] = __builtin_amdgcn_cvt_f32_fp8(int(w[p]), 3) * scale;
+    }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) u[e / 4] |= uint32_t(blk[value_at<D>(s, j0 + e)]) << (8 * (e % 4));
-    const float sk = ldexpf(1.f, int(blk[scale_at<D>(s, false)]) - 127);
-    const float sv = ldexpf(1.f, int(blk[scale_at<D>(s, true)]) - 127);
+    for (int p = 0; p < 8 / N; ++p) {
+      Piece<T, N> a;
 #pragma unroll
-    for (int e = 0; e < 8; e += 4) {
-      const int wk = int(w[e / 4]), wv = int(u[e / 4]);
-      kf[e] = __builtin_amdgcn_cvt_f32_fp8(wk, 0) * sk;
-      kf[e + 1] = __builtin_amdgcn_cvt_f32_fp8(wk, 1) * sk;
-      kf[e + 2] = __builtin_amdgcn_cvt_f32_fp8(wk, 2) * sk;
-      kf[e + 3] = __builtin_amdgcn_cvt_f32_fp8(wk, 3) * sk;
-      vf[e] = __builtin_amdgcn_cvt_f32_fp8(wv, 0) * sv;
-      vf[e + 1] = __builtin_amdgcn_cvt_f32_fp8(wv, 1) * sv;
-      vf[e + 2] = __builtin_amdgcn_cvt_f32_fp8(wv, 2) * sv;
-      vf[e + 3] = __builtin_amdgcn_cvt_f32_fp8(wv, 3) * sv;
+      for (int e = 0; e < N; ++e) a.v[e] = from_f32<T>(x[p * N + e]);
+      *reinterpret_cast<Piece<T, N>*>(at + p * N) = a;
+    }
+  };
+  for (int h = blockIdx.y * hb; h < h1; ++h) {
+    if (value) {
+      // rows outside the pool make no unit: zeros
+      const uint32_t none[2] = {0u, 0u};
+      for (int r = grp; r < n; r += GROUPS)
+        if (slot_s[r + 3] < 0) store(r, h, none, 0.f);
+    }
+    for (int u = grp; u < units; u += GROUPS) {
+      uint32_t w[4][2];
+      float scale[4];
+      int r0 = 4 * u, nr = min(4, n - 4 * u);
+      if (value) {
+        r0 = un.unit[u] >> 2;
+        nr = un.unit[u] & 1 ? 4 : 1;
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        w[i][0] = w[i][1] = 0u;
+        scale[i] = 0.f;
+        const int64_t sl = i < nr ? slot_s[r0 + i + 3] : -1;
+        if (sl < 0) continue;
+        const uint8_t* blk = pool + (sl >> 6) * page + int64_t(h) * 128 * (D + 1);
+        const int s = int(sl & 63);
+        scale[i] = ldexpf(1.f, int(blk[scale_at<D>(s, value)]) - 127);
+        if (!value) {
+          const u32x2 a = *reinterpret_cast<const u32x2*>(blk + key_at<D>(s, j0));
+          w[i][0] = a[0];
+          w[i][1] = a[1];
+        } else if (nr == 1) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) w[i][e / 4] |= uint32_t(blk[value_at<D>(s, j0 + e)]) << (8 * (e % 4));
+        }
+      }
+      if (value && nr == 4) {
+        const int64_t sl = slot_s[r0 + 3];
+        const uint8_t* blk = pool + (sl >> 6) * page + int64_t(h) * 128 * (D + 1);
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+          uint32_t col[4], row[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            col[e] = *reinterpret_cast<const uint32_t*>(blk + value_at<D>(int(sl & 63), j0 + 4 * p + e));
+          transpose4(col[0], col[1], col[2], col[3], row);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) w[i][p] = row[i];
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (i < nr) store(r0 + i, h, w[i], scale[i]);
     }
   }
-  constexpr int N = 16 / sizeof(T);
-#pragma unroll
-  for (int p = 0; p < 8 / N; ++p) {
-    Piece<T, N> a, b;
-#pragma unroll
-    for (int e = 0; e < N; ++e) {
-      a.v[e] = from_f32<T>(kf[p * N + e]);
-      b.v[e] = from_f32<T>(vf[p * N + e]);
-    }
-    *reinterpret_cast<Piece<T, N>*>(k + row * D + j0 + p * N) = a;
-    *reinterpret_cast<Piece<T, N>*>(v + row * D + j0 + p * N) = b;
-  }
+}
+
+// Heads a work-group: several while `target` work-groups are left.
+int heads_for(int64_t blocks, int n_heads, int64_t target) {
+  int hb = 8;
+  while (hb > 1 && blocks * ((n_heads + hb - 1) / hb) < target) hb /= 2;
+  return hb;
 }
 
 template <typename T, int D, bool QUANT>
@@ -262,15 +581,24 @@ hipError_t launch_append_t(int kv_heads, const void* k, const void* v, RowStride
     const int64_t n = 16 / sizeof(T);
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && s.token % n == 0 && s.head % n == 0;
   };
-  // long prompts: whole pages' worth of tokens a work-group (dword value
-  // stores); few tokens: one iteration of rows, more work-groups
-  const int rpi = kThreads / (D / 8);
-  const int rows = int64_t(n_tok) * kv_heads >= 32768 ? kMaxRows : rpi;
-  hipLaunchKernelGGL((append_rows<T, D, QUANT>), dim3((n_tok + rows - 1) / rows, kv_heads, 2),
-                     dim3(kThreads), 0, stream, rot, static_cast<const T*>(k), ks,
-                     static_cast<const T*>(v), vs, wide(k, ks), wide(v, vs), slot, position, n_tok, rows,
-                     kv_heads, pool, num_pages * 64);
-  return hipGetLastError();
+  auto go = [&](auto kern, int64_t blocks, int rows, int parts) {
+    const int hb = heads_for(blocks * parts, kv_heads, kAppendGroups);
+    hipLaunchKernelGGL(kern, dim3(uint32_t(blocks), (kv_heads + hb - 1) / hb, parts), dim3(Block<D>::kThreads),
+                       0, stream, rot, static_cast<const T*>(k), ks, static_cast<const T*>(v), vs, wide(k, ks),
+                       wide(v, vs), slot, position, n_tok, rows, hb, kv_heads, pool, num_pages * 64);
+    return hipGetLastError();
+  };
+  constexpr int G = Block<D>::kGroups, R = Block<D>::kRows;
+  // Long runs of 8-bit values go out by pages, in a launch of their own: 4093 tokens of
+  // 32 heads take 37 us in two launches and 48 in one, whose blocks hold a quarter of a
+  // page and whose registers are those of the larger part.  Short calls are one launch.
+  if constexpr (QUANT) {
+    if (n_tok >= 256 && int64_t(n_tok) * kv_heads >= 8192) {
+      hipError_t e = go(append_rows<T, D, QUANT, kKeys>, (n_tok + G - 1) / G, G, 1);
+      return e != hipSuccess ? e : go(append_rows<T, D, QUANT, kValues>, (n_tok + R - 1) / R + 1, R, 1);
+    }
+  }
+  return go(append_rows<T, D, QUANT, kBoth>, (n_tok + G - 1) / G, G, 2);
 }
 
 template <typename T, bool QUANT>
@@ -288,10 +616,13 @@ hipError_t launch_append_d(int kv_heads, int head_dim, const void* k, const void
 template <typename T, int D>
 hipError_t launch_read_t(int kv_heads, const void* pool, int64_t num_pages, const int64_t* slot,
                          int n_tok, void* k, void* v, hipStream_t stream) {
-  const int64_t items = int64_t(n_tok) * kv_heads * (D / 8);
-  hipLaunchKernelGGL((read_rows<T, D>), dim3((items + kThreads - 1) / kThreads), dim3(kThreads), 0, stream,
-                     static_cast<const uint8_t*>(pool), num_pages * 64, slot, kv_heads, items,
-                     static_cast<T*>(k), static_cast<T*>(v));
+  constexpr int R = Block<D>::kRows;
+  const int rows = n_tok >= 256 ? R : 8;
+  const int64_t blocks = (n_tok + rows - 1) / rows;
+  const int hb = heads_for(2 * blocks, kv_heads, kReadGroups);
+  hipLaunchKernelGGL((read_rows<T, D>), dim3(uint32_t(blocks), (kv_heads + hb - 1) / hb, 2),
+                     dim3(Block<D>::kThreads), 0, stream, static_cast<const uint8_t*>(pool), num_pages * 64, slot,
+                     n_tok, rows, hb, kv_heads, static_cast<T*>(k), static_cast<T*>(v));
   return hipGetLastError();
 }
 

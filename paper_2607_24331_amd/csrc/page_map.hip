@@ -6,13 +6,13 @@
 // sequences give the rows [end_b - n_b, end_b) and the stack places
 // [pend_b - need_b, pend_b) counted from the top.
 //
-// map_sequences  one work-group of 1024 threads: both sums by wave scans, 1024
-//                sequences a round; then all threads share the round's new table
-//                entries, finding the sequence of an entry by bisection.
-// map_rows       rows of the step, four a thread, each by bisection of row_start.
-//                A row's page is read from the table that map_sequences wrote.
-// All numbers are small; the calls are bound by the two launches and a few
-// dependent loads each.
+// map_sequences  one work-group of up to 1024 threads: both sums by wave scans, a
+//                sequence a thread and round; then all threads share the round's new
+//                table entries, finding the sequence of an entry by bisection.  Steps
+//                of at most kFusedRows rows and one round write their rows here too.
+// map_rows       rows of longer steps, each by bisection of row_start, its page read
+//                from the table that map_sequences wrote.
+// All numbers are small: the calls are bound by launches and a few dependent loads.
 #include <algorithm>
 
 #include "device.h"
@@ -23,6 +23,7 @@ namespace {
 
 constexpr int kSeqThreads = 1024;
 constexpr int kRowThreads = 256;
+constexpr int kFusedRows = 4096;           // four rows a thread of the one work-group
 
 // Running sums of two int64 values over the work-group; totals in t0, t1.
 struct Sums {
@@ -45,7 +46,7 @@ __device__ __forceinline__ void scan2(int64_t& a, int64_t& b, int64_t& ta, int64
   __syncthreads();
   int64_t ba = 0, bb = 0;
   ta = tb = 0;
-  for (int k = 0; k < kSeqThreads / 64; ++k) {
+  for (int k = 0; k < int(blockDim.x >> 6); ++k) {
     if (k < w) {
       ba += sm.wave0[k];
       bb += sm.wave1[k];
@@ -72,17 +73,18 @@ __device__ __forceinline__ int first_above(const T* end, int n, T x) {
   return lo;
 }
 
-__global__ __launch_bounds__(kSeqThreads) void map_sequences(PageMapArgs a) {
+__global__ __launch_bounds__(kSeqThreads) void map_sequences(PageMapArgs a, int fused_rows) {
   __shared__ Sums sums;
   __shared__ int64_t pend_s[kSeqThreads];  // stack places of the round, from its start
+  __shared__ int64_t end_s[kSeqThreads];   // rows of the round, from its start
   __shared__ int first_s[kSeqThreads];     // first new page's column, -1: not served
+  __shared__ int len_s[kSeqThreads];       // tokens cached before
   __shared__ int64_t taken_s[kSeqThreads / 64];
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, threads = blockDim.x;
   const int64_t count = min(max(*a.free_count, 0), a.free_capacity);
   const int64_t most = int64_t(a.max_pages) * 64;
   int64_t row_run = 0, page_run = 0, taken = 0;
-  if (tid == 0) a.row_start[0] = 0;
-  for (int base = 0; base < a.batch; base += kSeqThreads) {
+  for (int base = 0; base < a.batch; base += threads) {
     const int b = base + tid;
     const bool in = b < a.batch;
     const int64_t c = in ? a.cached[b] : 0, n = in ? a.added[b] : 0;
@@ -91,6 +93,7 @@ __global__ __launch_bounds__(kSeqThreads) void map_sequences(PageMapArgs a) {
     const int64_t rows = n > 0 ? n : 0;
     int64_t end = rows, none = 0, rows_all, none_all;
     scan2(end, none, rows_all, none_all, sums);
+    end_s[tid] = end;
     end += row_run;
     const bool fits = end <= a.n_rows;
     const int first = int((c + 63) >> 6);
@@ -108,21 +111,44 @@ __global__ __launch_bounds__(kSeqThreads) void map_sequences(PageMapArgs a) {
     if (served && need > 0 && page_run + pend > taken) taken = page_run + pend;
     pend_s[tid] = pend;
     first_s[tid] = served ? first : -1;
+    len_s[tid] = int(c);
     __syncthreads();
     // the round's new pages: those on the stack below what earlier rounds took
     const int64_t there = count - page_run < pages_all ? count - page_run : pages_all;
-    for (int64_t p = tid; p < there; p += kSeqThreads) {
-      const int i = first_above(pend_s, kSeqThreads, p);
+    for (int64_t p = tid; p < there; p += threads) {
+      const int i = first_above(pend_s, threads, p);
       if (first_s[i] >= 0) {
         const int64_t j = p - (i > 0 ? pend_s[i - 1] : 0);
         a.page_table[int64_t(base + i) * a.max_pages + first_s[i] + j] =
             a.free_pages[count - 1 - (page_run + p)];
       }
     }
+    // rows of a step of one round: a row's page is one of the stack's, or of the
+    // table's entries that were there before
+    for (int r = tid; r < fused_rows; r += threads) {
+      int64_t slot = -1;
+      int pos = -1, seq = -1;
+      const int i = first_above(end_s, threads, int64_t(r));
+      if (i < threads && i < a.batch) {
+        seq = i;
+        if (first_s[i] >= 0) {
+          pos = len_s[i] + int(r - (i > 0 ? end_s[i - 1] : 0));
+          const int at = pos >> 6;
+          const int64_t p0 = i > 0 ? pend_s[i - 1] : 0;
+          const int page = at >= first_s[i] ? a.free_pages[count - 1 - (p0 + at - first_s[i])]
+                                            : a.page_table[int64_t(i) * a.max_pages + at];
+          slot = int64_t(page) * 64 + (pos & 63);
+        }
+      }
+      a.slot[r] = slot;
+      a.position[r] = pos;
+      a.seq_of_row[r] = seq;
+    }
     row_run += rows_all;
     page_run += pages_all;
-    __syncthreads();                       // pend_s, first_s are rewritten
+    __syncthreads();                       // the round's arrays are rewritten
   }
+  if (tid == 0) a.row_start[0] = 0;
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) {
     const int64_t x = __shfl_xor((long long)taken, o);
@@ -131,7 +157,7 @@ __global__ __launch_bounds__(kSeqThreads) void map_sequences(PageMapArgs a) {
   if ((tid & 63) == 0) taken_s[tid >> 6] = taken;
   __syncthreads();
   if (tid == 0) {
-    for (int k = 1; k < kSeqThreads / 64; ++k)
+    for (int k = 1; k < threads >> 6; ++k)
       if (taken_s[k] > taken) taken = taken_s[k];
     *a.free_left = int32_t(count - taken);
   }
@@ -214,9 +240,11 @@ __global__ __launch_bounds__(kSeqThreads) void release_pages(
 }  // namespace
 
 hipError_t launch_page_map(const PageMapArgs& a, hipStream_t stream) {
-  hipLaunchKernelGGL(map_sequences, dim3(1), dim3(kSeqThreads), 0, stream, a);
+  const int threads = a.batch <= 256 && a.n_rows <= 1024 ? 256 : kSeqThreads;
+  const bool fused = a.batch <= threads && a.n_rows <= kFusedRows;
+  hipLaunchKernelGGL(map_sequences, dim3(1), dim3(threads), 0, stream, a, fused ? a.n_rows : 0);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.n_rows == 0) return e;
+  if (e != hipSuccess || fused || a.n_rows == 0) return e;
   hipLaunchKernelGGL(map_rows, dim3((int64_t(a.n_rows) + kRowThreads - 1) / kRowThreads),
                      dim3(kRowThreads), 0, stream, a);
   return hipGetLastError();

@@ -23,8 +23,8 @@
 // its values likewise, so a page's bytes are in flight all the time.
 // Reads 2 d + 2 bytes a token and KV head; bound by those bytes as long as the
 // rows fit one 16-row tile.
-//   merge   one work-group per (query, head, sequence): fixed ascending-split
-//           log-sum-exp sum.
+//   merge   one work-group per (query, head, sequence), a log-sum-exp sum in a fixed
+//           order.
 #include <algorithm>
 #include <cmath>
 
@@ -409,38 +409,68 @@ __global__ __launch_bounds__(kWaves * 64, (D == 256 || RT == 2) ? 1 : 2) void qu
   }
 }
 
-// One work-group a (query, head) row: part_o rows of its splits, ascending.
+// One work-group a (query, head) row.  The (m, l) of 256 splits at a time become
+// weights in LDS; D/4 threads take four columns of a split, 1024/D splits in flight,
+// their sums joined in a fixed order.
 template <int D>
 __global__ __launch_bounds__(256) void quant_merge(const float* __restrict__ part_o,
                                                    const float* __restrict__ part_ml,
                                                    const int32_t* __restrict__ seq_lens, int max_context,
                                                    int split_pages, int n_split, int rows_per_seq,
                                                    float* __restrict__ out) {
-  constexpr int G = 256 / (D / 4);         // splits in flight: D/4 threads a split, four columns each
-  __shared__ floatx4 red[G][D / 4];
+  constexpr int C = D / 4, G = 256 / C, U = 4;
+  __shared__ floatx4 red[G][C];
+  __shared__ float weight[256], wave_m[4], wave_l[4];
   const int64_t row = blockIdx.x;
   const int b = int(row / rows_per_seq);
-  const int tid = threadIdx.x, g = tid / (D / 4), c = tid % (D / 4);
+  const int tid = threadIdx.x, g = tid / C, c = tid % C;
   int T = seq_lens[b];
   T = T < 0 ? 0 : (T > max_context ? max_context : T);
   const int ns = ((T + 63) / 64 + split_pages - 1) / split_pages;
-  const float* ml = part_ml + row * n_split * 2;
-  float M = -INFINITY;
-  for (int s = 0; s < ns; ++s) M = fmaxf(M, ml[2 * s]);
-  float L = 0.f;
-  for (int s = 0; s < ns; ++s)
-    if (ml[2 * s + 1] != 0.f) L = fmaf(exp2f(ml[2 * s] - M), ml[2 * s + 1], L);
-  floatx4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int s = g; s < ns; s += G) {
-    if (ml[2 * s + 1] == 0.f) continue;    // nothing seen
-    const float f = exp2f(ml[2 * s] - M);
-    const floatx4 x = *reinterpret_cast<const floatx4*>(part_o + (row * n_split + s) * D + 4 * c);
+  const float2* ml = reinterpret_cast<const float2*>(part_ml) + row * n_split;
+  const float* po = part_o + row * n_split * D + 4 * c;
+  float2 own = tid < ns ? ml[tid] : make_float2(-INFINITY, 0.f);
+  float M = own.x;
+  for (int s = 256 + tid; s < ns; s += 256) M = fmaxf(M, ml[s].x);
 #pragma unroll
-    for (int v = 0; v < 4; ++v) o[v] = fmaf(f, x[v], o[v]);
+  for (int o = 32; o >= 1; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
+  if ((tid & 63) == 0) wave_m[tid >> 6] = M;
+  __syncthreads();
+  M = fmaxf(fmaxf(wave_m[0], wave_m[1]), fmaxf(wave_m[2], wave_m[3]));
+  float L = 0.f;
+  floatx4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int s0 = 0; s0 < ns; s0 += 256) {
+    if (s0 > 0) {
+      __syncthreads();                       // the weights before are used up
+      own = s0 + tid < ns ? ml[s0 + tid] : make_float2(-INFINITY, 0.f);
+    }
+    const float f = own.y == 0.f ? 0.f : exp2f(own.x - M);   // l = 0: nothing seen
+    weight[tid] = f;
+    L = fmaf(f, own.y, L);
+    __syncthreads();
+    const int n = min(256, ns - s0);
+    for (int s = g; s < n; s += U * G) {
+      floatx4 x[U];
+#pragma unroll
+      for (int i = 0; i < U; ++i)
+        if (s + i * G < n) x[i] = *reinterpret_cast<const floatx4*>(po + int64_t(s0 + s + i * G) * D);
+#pragma unroll
+      for (int i = 0; i < U; ++i)
+        if (s + i * G < n) {
+          const float y = weight[s + i * G];
+          if (y != 0.f)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) o[v] = fmaf(y, x[i][v], o[v]);
+        }
+    }
   }
+#pragma unroll
+  for (int i = 32; i >= 1; i >>= 1) L += __shfl_xor(L, i);
+  if ((tid & 63) == 0) wave_l[tid >> 6] = L;
   red[g][c] = o;
   __syncthreads();
   if (g == 0) {
+    L = (wave_l[0] + wave_l[1]) + (wave_l[2] + wave_l[3]);
     for (int k = 1; k < G; ++k)
 #pragma unroll
       for (int v = 0; v < 4; ++v) o[v] += red[k][c][v];

@@ -59,14 +59,19 @@ def _heads(t: torch.Tensor, name: str, device=None):
 def _launch(fn, what: str, device: torch.device, stream, *args) -> None:
     """fn(*args, stream) with the tensors' device current, on `stream` or on
     that device's current stream."""
-    if device.index != torch.cuda.current_device():
+    index = device.index
+    if index != torch.cuda.current_device():
         with torch.cuda.device(device):
             return _launch(fn, what, device, stream, *args)
     if stream is None:
-        stream = torch.cuda.current_stream(device)
+        handle = torch._C._cuda_getCurrentRawStream(index)   # current_stream() builds an object: 2 us
     elif stream.device != device:
         raise ValueError(f"{what}: the stream is of {stream.device}, the tensors of {device}")
-    _check(fn(*args, stream.cuda_stream), what)
+    else:
+        handle = stream.cuda_stream
+    status = fn(*args, handle)
+    if status:
+        _check(status, what)
 
 
 def _new(shape, dtype, device, stream) -> torch.Tensor:
@@ -114,9 +119,21 @@ def page_map(cached: torch.Tensor, added: torch.Tensor, page_table: torch.Tensor
     pn = _vector(free_count, "free_count", i32, 1, dev)
     if out is None:
         slot = _new((rows,), torch.int64, dev, stream)
-        lens, start, pos, seq, status, left = _new((3 * B + 2 + 2 * rows,), i32, dev, stream).split(
-            (B, B + 1, rows, rows, B, 1))
+        block = _new((3 * B + 2 + 2 * rows,), i32, dev, stream)
+        lens, start, pos, seq, status, left = block.split((B, B + 1, rows, rows, B, 1))
         out = PageMap(lens, start, slot, pos, seq, status, left)
+        at = block.data_ptr()
+        p_lens, p_start, p_pos = at, at + 4 * B, at + 4 * (2 * B + 1)
+        p_seq, p_status = p_pos + 4 * rows, p_pos + 8 * rows
+        p_left, p_slot = p_status + 4 * B, slot.data_ptr()
+    else:
+        p_lens = _vector(out.seq_lens, "seq_lens", i32, B, dev)
+        p_start = _vector(out.row_start, "row_start", i32, B + 1, dev)
+        p_slot = _vector(out.slot, "slot", torch.int64, rows, dev)
+        p_pos = _vector(out.position, "position", i32, rows, dev)
+        p_seq = _vector(out.seq_of_row, "seq_of_row", i32, rows, dev)
+        p_status = _vector(out.status, "status", i32, B, dev)
+        p_left = _vector(out.free_left, "free_left", i32, 1, dev)
     if B == 0:       # no sequences: every row lies behind the last one
         out.row_start.zero_()
         for t in (out.slot, out.position, out.seq_of_row):
@@ -124,13 +141,7 @@ def page_map(cached: torch.Tensor, added: torch.Tensor, page_table: torch.Tensor
         out.free_left.copy_(free_count)
         return out
     _launch(_lib.dckv_page_map, "page_map", dev, stream, pc, pa, B, pt, page_table.shape[1], pf,
-            free_pages.shape[0], pn, _vector(out.free_left, "free_left", i32, 1, dev),
-            _vector(out.seq_lens, "seq_lens", i32, B, dev),
-            _vector(out.row_start, "row_start", i32, B + 1, dev),
-            _vector(out.slot, "slot", torch.int64, rows, dev),
-            _vector(out.position, "position", i32, rows, dev),
-            _vector(out.seq_of_row, "seq_of_row", i32, rows, dev), rows,
-            _vector(out.status, "status", i32, B, dev))
+            free_pages.shape[0], pn, p_left, p_lens, p_start, p_slot, p_pos, p_seq, rows, p_status)
     return out
 
 
@@ -217,12 +228,17 @@ def rotary(rotation: Rotary, x: torch.Tensor, position: torch.Tensor, out: Optio
         raise ValueError(f"x has heads of {d}, the rotation of {rotation.head_dim}")
     pp = _vector(position, "position", torch.int32, n, x.device)
     if out is None:
+        oc = xc if out_dtype is None else _CODE.get(out_dtype)
+        if oc is None:
+            raise TypeError(f"out_dtype must be float32 or bfloat16, got {out_dtype}")
         out = _new((n, H, d), x.dtype if out_dtype is None else out_dtype, x.device, stream)
-    elif out_dtype is not None and out.dtype != out_dtype:
-        raise TypeError(f"out is {out.dtype}, not {out_dtype}")
-    po, oc, ot, oh = _heads(out, "out", x.device)
-    if tuple(out.shape) != (n, H, d):
-        raise ValueError(f"out has shape {tuple(out.shape)}, expected {(n, H, d)}")
+        po, ot, oh = out.data_ptr(), H * d, d
+    else:
+        if out_dtype is not None and out.dtype != out_dtype:
+            raise TypeError(f"out is {out.dtype}, not {out_dtype}")
+        po, oc, ot, oh = _heads(out, "out", x.device)
+        if tuple(out.shape) != (n, H, d):
+            raise ValueError(f"out has shape {tuple(out.shape)}, expected {(n, H, d)}")
     if n and H:
         _launch(_lib.dckv_rotary_apply, "rotary_apply", x.device, stream, rotation.handle, px, xc, xt, xh,
                 po, oc, ot, oh, pp, n, H, 1 if inverse else 0)
