@@ -41,11 +41,20 @@ typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kWaves = 4;
+constexpr int kFill = 512;                 // work-groups that fill the chip (two a compute unit)
+constexpr int kMost = 4096;                // and those that long splits are cut into
+constexpr int kLongPages = 32;
+constexpr int32_t kMaxBalanced = 256;      // sequences that are cut by their lengths
 constexpr int kTop = 14;                   // split operands lie below 2^kTop
 
 __device__ __forceinline__ floatx4 mfma(u32x4 a, u32x4 b, floatx4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, a), __builtin_bit_cast(half8, b),
                                                 c, 0, 0, 0);
+}
+
+// Cache bytes are read once: past the caches that the next ones need.
+__device__ __forceinline__ u32x4 load16(const uint8_t* p) {
+  return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
 }
 
 // Two dwords of e4m3 bytes (8 values) as f16, exactly.
@@ -72,28 +81,114 @@ __device__ __forceinline__ uint32_t keep_bytes(uint32_t w, int n) {
   return n >= 4 ? w : (n <= 0 ? 0u : w & ((1u << (8 * n)) - 1u));
 }
 
+// The pages a split takes of each sequence, from all sequences' pages in all
+// (`pages` of the work's `shares`, work-groups a split and sequence): enough splits to
+// fill the chip once, at least a page a wave; splits that get longer than kLongPages
+// by this are cut again where there are other sequences, so that the last ones
+// running are short.
+__host__ __device__ inline int64_t split_size(int64_t pages, int64_t shares, int batch) {
+  int64_t per = (pages * shares + kFill - 1) / kFill;
+  if (per > kLongPages && batch > 1) {
+    const int64_t most = (pages * shares + kMost - 1) / kMost;
+    per = most > kLongPages ? most : kLongPages;
+  }
+  per = (per + kWaves - 1) / kWaves * kWaves;
+  return per < kWaves ? int64_t(kWaves) : per;
+}
+
+// Unit u of the batch's splits, cut by the sequences' actual lengths (at most
+// kMaxBalanced sequences, four a lane; every wave of every work-group finds the same).
+struct Unit {
+  int b, split, pages, per, splits, first;   // first: unit of the sequence's split 0; b < 0: no unit
+};
+__device__ __forceinline__ Unit find_unit(int u, const int32_t* seq_lens, int batch, int max_context,
+                                          int shares) {
+  const int lane = threadIdx.x & 63;
+  Unit r{-1, 0, 0, 0, 0, 0};
+  if (batch == 1) {
+    const int T = min(max(seq_lens[0], 0), max_context);
+    r.pages = (T + 63) >> 6;
+    r.per = int(split_size(r.pages, shares, 1));
+    r.splits = (r.pages + r.per - 1) / r.per;
+    if (u < r.splits) {
+      r.b = 0;
+      r.split = u;
+    }
+    return r;
+  }
+  int np[4];
+  int64_t all = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int b = 4 * lane + i;
+    const int T = b < batch ? min(max(seq_lens[b], 0), max_context) : 0;
+    np[i] = (T + 63) >> 6;
+    all += np[i];
+  }
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) all += __shfl_xor((long long)all, o);
+  r.per = int(split_size(all, shares, batch));
+  int own = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) own += (np[i] + r.per - 1) / r.per;
+  int end = own;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int x = __shfl_up(end, o);
+    if (lane >= o) end += x;
+  }
+  const uint64_t above = __ballot(end > u);
+  if (above == 0) return r;
+  const int at = __builtin_ctzll(above);
+  int first = __shfl(end - own, at);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int n = __shfl(np[i], at), k = (n + r.per - 1) / r.per;
+    if (r.b < 0 && u < first + k) {
+      r.b = 4 * at + i;
+      r.pages = n;
+      r.splits = k;
+      r.first = first;
+      r.split = u - first;
+    }
+    first += k;
+  }
+  return r;
+}
+
 // D = d_h; RT 16-row tiles of (query, head) rows.
 template <int D, int RT>
 __global__ __launch_bounds__(kWaves * 64, (D == 256 || RT == 2) ? 1 : 2) void quant_split(
     const float* __restrict__ q, const uint8_t* __restrict__ pool, int64_t num_pages,
     const int32_t* __restrict__ page_table, int max_pages, const int32_t* __restrict__ seq_lens,
-    int max_context, int split_pages, int n_split, int n_units, int slices, int n_q_heads,
-    int n_kv_heads, int queries, float scale, float* __restrict__ part_o, float* __restrict__ part_ml,
-    float* __restrict__ out) {
+    int max_context, int batch, int split_pages, int n_split, int n_units, int slices, int n_q_heads,
+    int n_kv_heads, int queries, float scale, int2* __restrict__ records, float* __restrict__ part_o,
+    float* __restrict__ part_ml, float* __restrict__ out) {
   constexpr int KL = D / 64;               // 16-byte key loads a 16-token tile
   constexpr int DT = D / 16;               // 16-column value tiles, a load each
   __shared__ float red_o[kWaves][16][D + 4];
   __shared__ float red_m[kWaves][16], red_l[kWaves][16];
 
-  // Ids u, u + 8, ... run on one XCD: the slices of a unit are neighbours there
-  // and share its bytes in one L2.
+  // Ids w, w + 8, ... run on one XCD: the slices of a (unit, KV head) are neighbours
+  // there and share its bytes in one L2.
   const int id = blockIdx.x;
-  const int u = (id / (8 * slices)) * 8 + (id & 7);
+  const int wi = (id / (8 * slices)) * 8 + (id & 7);
   const int slice = (id >> 3) % slices;
-  if (u >= n_units) return;
-  const int kv = u % n_kv_heads;
-  const int b = (u / n_kv_heads) % (n_units / (n_kv_heads * n_split));
-  const int split = u / (n_units / n_split);
+  if (wi >= n_units * n_kv_heads) return;
+  const int kv = wi % n_kv_heads, u = wi / n_kv_heads;
+  Unit un;
+  if (split_pages == 0) {                  // cut by the lengths
+    un = find_unit(u, seq_lens, batch, max_context, n_kv_heads * slices);
+    if (un.b < 0) return;
+    if (kv == 0 && slice == 0 && un.split == 0 && threadIdx.x == 0)
+      records[un.b] = make_int2(un.first, un.splits);
+  } else {
+    un = Unit{u / n_split, u % n_split, 0, split_pages, 0, 0};
+  }
+  const int b = __builtin_amdgcn_readfirstlane(un.b);
+  un.split = __builtin_amdgcn_readfirstlane(un.split);
+  un.per = __builtin_amdgcn_readfirstlane(un.per);
+  un.splits = __builtin_amdgcn_readfirstlane(un.splits);
   const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lq = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int per = n_q_heads / n_kv_heads, rows = queries * per;
@@ -101,8 +196,9 @@ __global__ __launch_bounds__(kWaves * 64, (D == 256 || RT == 2) ? 1 : 2) void qu
   int T = seq_lens[b];
   T = T < 0 ? 0 : (T > max_context ? max_context : T);
   const int np_all = (T + 63) >> 6;
-  const int p0 = split * split_pages, p1 = min(p0 + split_pages, np_all);
-  if (p0 >= p1 && n_split > 1) return;     // the merge reads only splits holding pages
+  const int p0 = un.split * un.per, p1 = min(p0 + un.per, np_all);
+  if (p0 >= p1 && n_split != 1) return;    // the merge reads only splits holding pages
+  const bool whole = n_split == 1 || (split_pages == 0 && un.splits == 1);
 
   // ---- queries: row row0 + 16 t + lr, columns 64 i + 16 lq .. + 15, in halves of
   // q 2^(kTop - 1 - floor(log2 max|q|)); rowscale takes that and the scale back
@@ -181,14 +277,14 @@ __global__ __launch_bounds__(kWaves * 64, (D == 256 || RT == 2) ? 1 : 2) void qu
   u32x4 kr[4 * KL], vr[DT], ksc, vsc;
   auto load_keys = [&](const uint8_t* p) {
 #pragma unroll
-    for (int i = 0; i < 4 * KL; ++i) kr[i] = *reinterpret_cast<const u32x4*>(p + 1024 * i + 16 * lane);
-    ksc = *reinterpret_cast<const u32x4*>(p + 128 * D + 16 * lq);
+    for (int i = 0; i < 4 * KL; ++i) kr[i] = load16(p + 1024 * i + 16 * lane);
+    ksc = load16(p + 128 * D + 16 * lq);
   };
   auto load_values = [&](const uint8_t* p) {
 #pragma unroll
     for (int i = 0; i < DT; ++i)
-      vr[i] = *reinterpret_cast<const u32x4*>(p + 64 * D + 1024 * i + 16 * lane);
-    vsc = *reinterpret_cast<const u32x4*>(p + 128 * D + 64 + 16 * lq);
+      vr[i] = load16(p + 64 * D + 1024 * i + 16 * lane);
+    vsc = load16(p + 128 * D + 64 + 16 * lq);
   };
   bool valid = false;
   const uint8_t* ptr = pool;
@@ -266,15 +362,15 @@ __global__ __launch_bounds__(kWaves * 64, (D == 256 || RT == 2) ? 1 : 2) void qu
         for (int v = 0; v < 4; ++v) {
           const float e = s[t][n][v] - base;
           utop = fmaxf(utop, e + float(byte_of(vscale[n], v)));
-          s[t][n][v] = exp2f(e);
+          s[t][n][v] = __builtin_amdgcn_exp2f(e);
           sum += s[t][n][v];
         }
       utop = fmaxf(utop, __shfl_xor(utop, 16));
       utop = fmaxf(utop, __shfl_xor(utop, 32));
       um[t] = fmaxf(um[t] + down, utop);
       const int k_new = um[t] == -INFINITY ? 0 : int(ceilf(um[t]));
-      const float keep = exp2f(down + float(k[t] - k_new));
-      l[t] = fmaf(l[t], exp2f(down), sum);
+      const float keep = __builtin_amdgcn_exp2f(down + float(k[t] - k_new));
+      l[t] = fmaf(l[t], __builtin_amdgcn_exp2f(down), sum);
       m[t] = m_new;
       k[t] = k_new;
 #pragma unroll
@@ -390,15 +486,15 @@ __global__ __launch_bounds__(kWaves * 64, (D == 256 || RT == 2) ? 1 : 2) void qu
 #pragma unroll
       for (int k = 0; k < kWaves; ++k) {
         if (red_l[k][r] == 0.f) continue;  // the wave saw nothing of the row
-        const float f = exp2f(red_m[k][r] - M);
+        const float f = __builtin_amdgcn_exp2f(red_m[k][r] - M);
         L = fmaf(f, red_l[k][r], L);
         o = fmaf(f, red_o[k][r][d], o);
       }
       const int64_t orow = (int64_t(b) * queries + row / per) * n_q_heads + kv * per + row % per;
-      if (n_split == 1) {
+      if (whole) {
         out[orow * D + d] = L == 0.f ? 0.f : o / L;
       } else {
-        const int64_t prow = orow * n_split + split;
+        const int64_t prow = (int64_t(u) * queries + row / per) * n_q_heads + kv * per + row % per;
         part_o[prow * D + d] = o;
         if (d == 0) {
           part_ml[prow * 2] = M;
@@ -417,7 +513,7 @@ __global__ __launch_bounds__(256) void quant_merge(const float* __restrict__ par
                                                    const float* __restrict__ part_ml,
                                                    const int32_t* __restrict__ seq_lens, int max_context,
                                                    int split_pages, int n_split, int rows_per_seq,
-                                                   float* __restrict__ out) {
+                                                   const int2* __restrict__ records, float* __restrict__ out) {
   constexpr int C = D / 4, G = 256 / C, U = 4;
   __shared__ floatx4 red[G][C];
   __shared__ float weight[256], wave_m[4], wave_l[4];
@@ -426,12 +522,24 @@ __global__ __launch_bounds__(256) void quant_merge(const float* __restrict__ par
   const int tid = threadIdx.x, g = tid / C, c = tid % C;
   int T = seq_lens[b];
   T = T < 0 ? 0 : (T > max_context ? max_context : T);
-  const int ns = ((T + 63) / 64 + split_pages - 1) / split_pages;
-  const float2* ml = reinterpret_cast<const float2*>(part_ml) + row * n_split;
-  const float* po = part_o + row * n_split * D + 4 * c;
-  float2 own = tid < ns ? ml[tid] : make_float2(-INFINITY, 0.f);
+  // the sequence's units, where its splits' rows lie
+  int u0 = b * n_split, ns = 0;
+  if (T > 0) {
+    if (split_pages == 0) {
+      const int2 rec = records[b];
+      u0 = rec.x;
+      ns = rec.y;
+      if (ns == 1) return;                   // written by its split
+    } else {
+      ns = ((T + 63) / 64 + split_pages - 1) / split_pages;
+    }
+  }
+  const int64_t first = int64_t(u0) * rows_per_seq + row - int64_t(b) * rows_per_seq;
+  const float2* ml = reinterpret_cast<const float2*>(part_ml) + first;
+  const float* po = part_o + first * D + 4 * c;
+  float2 own = tid < ns ? ml[int64_t(tid) * rows_per_seq] : make_float2(-INFINITY, 0.f);
   float M = own.x;
-  for (int s = 256 + tid; s < ns; s += 256) M = fmaxf(M, ml[s].x);
+  for (int s = 256 + tid; s < ns; s += 256) M = fmaxf(M, ml[int64_t(s) * rows_per_seq].x);
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
   if ((tid & 63) == 0) wave_m[tid >> 6] = M;
@@ -442,9 +550,9 @@ __global__ __launch_bounds__(256) void quant_merge(const float* __restrict__ par
   for (int s0 = 0; s0 < ns; s0 += 256) {
     if (s0 > 0) {
       __syncthreads();                       // the weights before are used up
-      own = s0 + tid < ns ? ml[s0 + tid] : make_float2(-INFINITY, 0.f);
+      own = s0 + tid < ns ? ml[int64_t(s0 + tid) * rows_per_seq] : make_float2(-INFINITY, 0.f);
     }
-    const float f = own.y == 0.f ? 0.f : exp2f(own.x - M);   // l = 0: nothing seen
+    const float f = own.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(own.x - M);   // l = 0: nothing seen
     weight[tid] = f;
     L = fmaf(f, own.y, L);
     __syncthreads();
@@ -453,7 +561,7 @@ __global__ __launch_bounds__(256) void quant_merge(const float* __restrict__ par
       floatx4 x[U];
 #pragma unroll
       for (int i = 0; i < U; ++i)
-        if (s + i * G < n) x[i] = *reinterpret_cast<const floatx4*>(po + int64_t(s0 + s + i * G) * D);
+        if (s + i * G < n) x[i] = *reinterpret_cast<const floatx4*>(po + int64_t(s0 + s + i * G) * rows_per_seq * D);
 #pragma unroll
       for (int i = 0; i < U; ++i)
         if (s + i * G < n) {
@@ -489,25 +597,40 @@ hipError_t launch_t(const QuantShape& sh, const float* q, const void* pool, int6
   char* ws = static_cast<char*>(workspace);
   float* part_o = reinterpret_cast<float*>(ws + sh.off_o);
   float* part_ml = reinterpret_cast<float*>(ws + sh.off_ml);
+  int2* records = reinterpret_cast<int2*>(ws + sh.off_rec);
   const float scale = kLog2e / std::sqrt(float(D));
-  const int64_t units = int64_t(sh.batch) * sh.kv_heads * sh.n_split;
-  const int64_t groups = (units + 7) / 8 * 8 * sh.slices;
+  const int64_t items = int64_t(sh.n_units) * sh.kv_heads;
+  const int64_t groups = (items + 7) / 8 * 8 * sh.slices;
   hipLaunchKernelGGL((quant_split<D, RT>), dim3(uint32_t(groups)), dim3(kWaves * 64), 0, stream, q,
                      static_cast<const uint8_t*>(pool), num_pages, page_table, max_pages, seq_lens,
-                     sh.max_context, sh.split_pages, sh.n_split, int(units), sh.slices, sh.q_heads,
-                     sh.kv_heads, sh.queries, scale, part_o, part_ml, out);
+                     sh.max_context, sh.batch, sh.split_pages, sh.n_split, sh.n_units, sh.slices, sh.q_heads,
+                     sh.kv_heads, sh.queries, scale, records, part_o, part_ml, out);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || sh.n_split == 1) return e;
   hipLaunchKernelGGL((quant_merge<D>), dim3(uint32_t(sh.batch) * sh.queries * sh.q_heads), dim3(256), 0,
                      stream, part_o, part_ml, seq_lens, sh.max_context, sh.split_pages, sh.n_split,
-                     sh.queries * sh.q_heads, out);
+                     sh.queries * sh.q_heads, records, out);
   return hipGetLastError();
 }
 
-}  // namespace
+int64_t pages_of(int32_t max_context) { return std::max<int64_t>(1, (int64_t(max_context) + 63) / 64); }
 
-// Splits where the library chooses: about kTargetGroups work-groups in all.
-constexpr int64_t kTargetGroups = 1024;
+// Most units of splits cut by the lengths of `batch` sequences: by split_size, units
+// are at most pages / size + batch in all and ceil(pages / size) a sequence.
+int64_t most_units(int64_t batch, int64_t pages, int64_t shares) {
+  const int64_t filled = std::min(batch * ((pages + kWaves - 1) / kWaves), kFill / shares + batch);
+  const int64_t longs = batch > 1 ? std::min(batch * ((pages + kLongPages - 1) / kLongPages), kMost / shares + batch) : 0;
+  return std::max(filled, longs);
+}
+
+size_t part_bytes(const QuantShape& s, int64_t units, size_t* off_ml, size_t* off_rec) {
+  const size_t rows = size_t(units) * s.queries * s.q_heads;
+  *off_ml = align_up(rows * s.head_dim * sizeof(float), 256);
+  *off_rec = *off_ml + align_up(rows * 2 * sizeof(float), 256);
+  return *off_rec + align_up(size_t(s.batch) * sizeof(int2), 256);
+}
+
+}  // namespace
 
 QuantShape quant_shape(int32_t q_heads, int32_t kv_heads, int32_t head_dim, int32_t queries,
                        int32_t split_tokens, int32_t batch, int32_t max_context) {
@@ -521,34 +644,32 @@ QuantShape quant_shape(int32_t q_heads, int32_t kv_heads, int32_t head_dim, int3
   s.rows = queries * (q_heads / kv_heads);
   s.tiles = (s.rows > 16 && head_dim < 256) ? 2 : 1;
   s.slices = (s.rows + 16 * s.tiles - 1) / (16 * s.tiles);
-  const int64_t pages = std::max<int64_t>(1, (int64_t(max_context) + 63) / 64);
-  int64_t per = split_tokens / DCKV_PAGE_TOKENS;
-  if (per == 0) {   // about four work-groups a compute unit, at least a page a wave
-    const int64_t work = pages * batch * kv_heads * s.slices;
-    per = std::max<int64_t>(4, (work + kTargetGroups - 1) / kTargetGroups);
-    per = (per + 3) / 4 * 4;
+  const int64_t pages = pages_of(max_context), shares = int64_t(kv_heads) * s.slices;
+  int64_t per = split_tokens / DCKV_PAGE_TOKENS, units;
+  if (per == 0 && pages > kWaves && batch <= kMaxBalanced) {
+    s.split_pages = 0;                     // cut on the device
+    s.n_split = 0;
+    units = most_units(batch, pages, shares);
+  } else {
+    if (per == 0) per = split_size(pages * batch, shares, batch);
+    s.split_pages = int32_t(std::min(per, pages));
+    s.n_split = int32_t((pages + s.split_pages - 1) / s.split_pages);
+    units = int64_t(batch) * s.n_split;
   }
-  s.split_pages = int32_t(std::min(per, pages));
-  s.n_split = int32_t((pages + s.split_pages - 1) / s.split_pages);
-  if (s.n_split > 1) {
-    const size_t rows = size_t(batch) * queries * q_heads * s.n_split;
-    s.off_ml = align_up(rows * head_dim * sizeof(float), 256);
-    s.bytes = s.off_ml + align_up(rows * 2 * sizeof(float), 256);
-  }
+  s.groups = (units * kv_heads + 7) / 8 * 8 * s.slices;
+  s.n_units = int32_t(std::min<int64_t>(units, INT32_MAX));
+  if (s.n_split != 1) s.bytes = part_bytes(s, units, &s.off_ml, &s.off_rec);
   return s;
 }
 
-// A call's splits in all, batch * n_split, are at most batch * ceil(pages / 4) and
-// at most kTargetGroups / (kv_heads * slices) + batch where the library chooses:
-// neither bound shrinks with the batch or the context.
+// Neither bound of most_units shrinks with the batch or the context (and a batch above
+// kMaxBalanced, all its sequences taken as the longest, keeps to it too).
 size_t quant_workspace_bytes(const QuantShape& s, bool chosen) {
-  const int64_t pages = std::max<int64_t>(1, (int64_t(s.max_context) + 63) / 64);
-  int64_t splits = int64_t(s.batch) * s.n_split;
-  if (chosen)
-    splits = std::min(int64_t(s.batch) * ((pages + 3) / 4),
-                      kTargetGroups / (int64_t(s.kv_heads) * s.slices) + s.batch);
-  const size_t rows = size_t(splits) * s.queries * s.q_heads;
-  return align_up(rows * s.head_dim * sizeof(float), 256) + align_up(rows * 2 * sizeof(float), 256);
+  const int64_t pages = pages_of(s.max_context), shares = int64_t(s.kv_heads) * s.slices;
+  if (chosen ? pages <= kWaves : s.n_split == 1) return 0;   // every smaller call is one split a sequence
+  const int64_t units = chosen ? most_units(s.batch, pages, shares) : int64_t(s.batch) * s.n_split;
+  size_t off_ml, off_rec;
+  return part_bytes(s, units, &off_ml, &off_rec);
 }
 
 hipError_t launch_quant_decode(const QuantShape& sh, const float* q, const void* pool,

@@ -16,7 +16,7 @@ namespace dckv {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kUnroll = 4;                    // heads in flight a thread
+constexpr int kUnroll = 2;                    // heads in flight a thread (pairs of pieces)
 constexpr int64_t kTargetThreads = 262144;    // four waves a SIMD over 256 compute units
 
 template <typename TI, typename TO, int V>
@@ -36,12 +36,20 @@ __global__ __launch_bounds__(kThreads) void rotary_rows(
   TO* yr = out + tok * os.token;
   if (piece >= plane_pieces) {                // coordinates that are not turned
     const int at = 2 * rot.planes + (piece - plane_pieces) * V;
-    for (int h = g; h < n_heads; h += groups) {
-      const Piece<TI, V> a = *reinterpret_cast<const Piece<TI, V>*>(xr + h * xs.head + at);
-      Piece<TO, V> b;
+    for (int h0 = g; h0 < n_heads; h0 += 2 * kUnroll * groups) {
+      Piece<TI, V> a[2 * kUnroll];
 #pragma unroll
-      for (int e = 0; e < V; ++e) b.v[e] = from_f32<TO>(to_f32(a.v[e]));
-      *reinterpret_cast<Piece<TO, V>*>(yr + h * os.head + at) = b;
+      for (int u = 0; u < 2 * kUnroll; ++u)
+        if (h0 + u * groups < n_heads)
+          a[u] = *reinterpret_cast<const Piece<TI, V>*>(xr + (h0 + u * groups) * xs.head + at);
+#pragma unroll
+      for (int u = 0; u < 2 * kUnroll; ++u)
+        if (h0 + u * groups < n_heads) {
+          Piece<TO, V> b;
+#pragma unroll
+          for (int e = 0; e < V; ++e) b.v[e] = from_f32<TO>(to_f32(a[u].v[e]));
+          *reinterpret_cast<Piece<TO, V>*>(yr + (h0 + u * groups) * os.head + at) = b;
+        }
     }
     return;
   }

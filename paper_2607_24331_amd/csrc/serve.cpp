@@ -90,9 +90,9 @@ int check_quant(const char* where, int32_t Hq, int32_t Hkv, int32_t dh, int32_t 
     return fail(DCKV_EINVAL, "%s: batch %d of %d queries outside 0..65535", where, batch, Q);
   if (max_context < 0) return fail(DCKV_EINVAL, "%s: max_context %d < 0", where, max_context);
   const dckv::QuantShape sh = dckv::quant_shape(Hq, Hkv, dh, Q, split, batch, max_context);
-  if ((int64_t(batch) * Hkv * sh.n_split + 8) * sh.slices > kMaxGroups)
-    return fail(DCKV_EINVAL, "%s: %d splits of %d sequences, %d KV heads and %d row slices are more than %lld work-groups",
-                where, sh.n_split, batch, Hkv, sh.slices, (long long)kMaxGroups);
+  if (sh.groups > kMaxGroups)
+    return fail(DCKV_EINVAL, "%s: the splits of %d sequences, %d KV heads and %d row slices take %lld work-groups, above %lld",
+                where, batch, Hkv, sh.slices, (long long)sh.groups, (long long)kMaxGroups);
   return DCKV_OK;
 }
 

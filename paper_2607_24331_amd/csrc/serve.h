@@ -41,9 +41,12 @@ struct QuantShape {
   int32_t rows;            // (query, head) rows of a KV head: Q * H_q / H_kv
   int32_t tiles;           // 16-row tiles a work-group (1 or 2)
   int32_t slices;          // work-groups that share a KV head's rows
-  int32_t split_pages;     // pages a split
-  int32_t n_split;
-  size_t off_o, off_ml;    // workspace: unnormalised outputs, then (m, l)
+  int32_t split_pages;     // pages a split; 0: cut on the device by the sequences' lengths
+  int32_t n_split;         // splits a sequence (0 where split_pages is)
+  int32_t n_units;         // splits in all, at most
+  int64_t groups;          // work-groups
+  size_t off_o, off_ml;    // workspace: unnormalised outputs of (unit, query, head), then (m, l)
+  size_t off_rec;          // and a record a sequence (its first unit, its units)
   size_t bytes;
 };
 

@@ -369,6 +369,16 @@ def test_quant_decode(Hq, H, d, Q, lens, split):
     _check_decode(q, pool, table, lens, H, split)
 
 
+@pytest.mark.parametrize("B, top, H", [(70, 700, 1), (256, 320, 2), (257, 400, 1)])
+def test_quant_decode_many_sequences(B, top, H):
+    # cut by the lengths of up to 256 sequences, by the longest of more
+    g = np.random.default_rng(B)
+    lens = [int(x) for x in g.integers(0, top + 1, B)]
+    lens[3], lens[B - 1] = 0, top
+    pool, table = _cache(g, lens, H, 64)
+    _check_decode(g.standard_normal((B, 1, H, 64)).astype(np.float32), pool, table, lens, H)
+
+
 def test_quant_decode_long_split():
     # over 64 pages a wave in one split, and splits of a sequence that end early
     g = np.random.default_rng(1)
