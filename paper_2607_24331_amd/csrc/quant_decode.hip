@@ -19,8 +19,9 @@
 //           lane are those of tokens 16 n + 4 (lane / 16) + v, and the page holds a
 //           value column's tokens in that order, so the weights feed the second
 //           product from the registers they were made in: no LDS, no shuffle.
-// The keys of a wave's next page are loaded when the current ones are used up,
-// its values likewise, so a page's bytes are in flight all the time.
+// A wave's values are loaded when its keys are used up and the next page's keys when
+// the values are, into the same registers; three waves a SIMD (two of the wide shapes)
+// keep the memory busy meanwhile.
 // Reads 2 d + 2 bytes a token and KV head; bound by those bytes as long as the
 // rows fit one 16-row tile.
 //   merge   one work-group per (query, head, sequence), a log-sum-exp sum in a fixed
@@ -75,6 +76,11 @@ __device__ __forceinline__ void halves(float x, float y, uint32_t& hi, uint32_t&
 }
 
 __device__ __forceinline__ int byte_of(uint32_t w, int v) { return int((w >> (8 * v)) & 0xFFu); }
+
+// 0x80 in every byte that is a NaN (0x7F or 0xFF).
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
+  return ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
+}
 
 // Bytes v of a dword with v < n kept.
 __device__ __forceinline__ uint32_t keep_bytes(uint32_t w, int n) {
@@ -158,7 +164,7 @@ __device__ __forceinline__ Unit find_unit(int u, const int32_t* seq_lens, int ba
 
 // D = d_h; RT 16-row tiles of (query, head) rows.
 template <int D, int RT>
-__global__ __launch_bounds__(kWaves * 64, (D == 256 || RT == 2) ? 1 : 2) void quant_split(
+__global__ __launch_bounds__(kWaves * 64, 2) void quant_split(
     const float* __restrict__ q, const uint8_t* __restrict__ pool, int64_t num_pages,
     const int32_t* __restrict__ page_table, int max_pages, const int32_t* __restrict__ seq_lens,
     int max_context, int batch, int split_pages, int n_split, int n_units, int slices, int n_q_heads,
@@ -166,7 +172,10 @@ __global__ __launch_bounds__(kWaves * 64, (D == 256 || RT == 2) ? 1 : 2) void qu
     float* __restrict__ part_ml, float* __restrict__ out) {
   constexpr int KL = D / 64;               // 16-byte key loads a 16-token tile
   constexpr int DT = D / 16;               // 16-column value tiles, a load each
-  __shared__ float red_o[kWaves][16][D + 4];
+  __shared__ __align__(16) union {
+    u32x4 q[RT][KL][2][2][64];             // [tile][64 columns][8 of a lane's 16][high, low][lane]
+    float o[kWaves][16][D + 4];            // the waves' outputs, once the queries are used up
+  } sm;
   __shared__ float red_m[kWaves][16], red_l[kWaves][16];
 
   // Ids w, w + 8, ... run on one XCD: the slices of a (unit, KV head) are neighbours
@@ -201,8 +210,9 @@ __global__ __launch_bounds__(kWaves * 64, (D == 256 || RT == 2) ? 1 : 2) void qu
   const bool whole = n_split == 1 || (split_pages == 0 && un.splits == 1);
 
   // ---- queries: row row0 + 16 t + lr, columns 64 i + 16 lq .. + 15, in halves of
-  // q 2^(kTop - 1 - floor(log2 max|q|)); rowscale takes that and the scale back
-  u32x4 qh[RT][KL][2], ql[RT][KL][2];
+  // q 2^(kTop - 1 - floor(log2 max|q|)); rowscale takes that and the scale back.  They lie
+  // in LDS, read once a page for its four token tiles: in registers they would halve
+  // the waves of the wider shapes.
   float rowscale[RT];
   int limit[RT];                           // tokens the row sees
 #pragma unroll
@@ -235,14 +245,19 @@ __global__ __launch_bounds__(kWaves * 64, (D == 256 || RT == 2) ? 1 : 2) void qu
 #pragma unroll
     for (int c = 0; c < KL; ++c)
 #pragma unroll
-      for (int s = 0; s < 2; ++s)
+      for (int s = 0; s < 2; ++s) {
+        if (((2 * c + s) & (kWaves - 1)) != w) continue;     // every wave has them, one writes
+        u32x4 hi4, lo4;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           uint32_t hi, lo;
           halves(x[c][8 * s + 2 * k] * up, x[c][8 * s + 2 * k + 1] * up, hi, lo);
-          qh[t][c][s][k] = hi;
-          ql[t][c][s][k] = lo;
+          hi4[k] = hi;
+          lo4[k] = lo;
         }
+        sm.q[t][c][s][0][lane] = hi4;
+        sm.q[t][c][s][1][lane] = lo4;
+      }
   }
 
   floatx4 acc[RT][DT];
@@ -274,17 +289,19 @@ __global__ __launch_bounds__(kWaves * 64, (D == 256 || RT == 2) ? 1 : 2) void qu
     valid = page >= 0;
     return pool + (int64_t(valid ? page : 0) * n_kv_heads + kv) * block;   // an empty page is masked
   };
-  u32x4 kr[4 * KL], vr[DT], ksc, vsc;
+  // keys and values of a page take turns in one set of registers: the bytes in flight
+  // are those of half a page, but three waves a SIMD have theirs instead of two
+  u32x4 kv_page[DT], scales;
   auto load_keys = [&](const uint8_t* p) {
 #pragma unroll
-    for (int i = 0; i < 4 * KL; ++i) kr[i] = load16(p + 1024 * i + 16 * lane);
-    ksc = load16(p + 128 * D + 16 * lq);
+    for (int i = 0; i < DT; ++i) kv_page[i] = load16(p + 1024 * i + 16 * lane);
+    scales = load16(p + 128 * D + 16 * lq);
   };
   auto load_values = [&](const uint8_t* p) {
 #pragma unroll
     for (int i = 0; i < DT; ++i)
-      vr[i] = load16(p + 64 * D + 1024 * i + 16 * lane);
-    vsc = load16(p + 128 * D + 64 + 16 * lq);
+      kv_page[i] = load16(p + 64 * D + 1024 * i + 16 * lane);
+    scales = load16(p + 128 * D + 64 + 16 * lq);
   };
   bool valid = false;
   const uint8_t* ptr = pool;
@@ -292,8 +309,9 @@ __global__ __launch_bounds__(kWaves * 64, (D == 256 || RT == 2) ? 1 : 2) void qu
     load_ids(0);
     ptr = page_ptr(0, valid);
     load_keys(ptr);
-    load_values(ptr);
   }
+
+  __syncthreads();                         // the queries are in LDS
 
   for (int step = 0; step < mine; ++step) {
     bool next_valid = valid;
@@ -309,26 +327,45 @@ __global__ __launch_bounds__(kWaves * 64, (D == 256 || RT == 2) ? 1 : 2) void qu
     // ---- scores, 16 tokens a tile: token 16 n + 4 lq + v, row lr
     floatx4 s[RT][4];
 #pragma unroll
-    for (int n = 0; n < 4; ++n) {
+    for (int t = 0; t < RT; ++t)
 #pragma unroll
-      for (int t = 0; t < RT; ++t) s[t][n] = floatx4{0.f, 0.f, 0.f, 0.f};
+      for (int n = 0; n < 4; ++n) s[t][n] = floatx4{0.f, 0.f, 0.f, 0.f};
+    // the queries of a step are read while the step before multiplies, no earlier
+    u32x4 qv[RT][2];
 #pragma unroll
-      for (int c = 0; c < KL; ++c)
+    for (int t = 0; t < RT; ++t)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const u32x4 a = widen(kr[n * KL + c][2 * h], kr[n * KL + c][2 * h + 1]);
+      for (int k2 = 0; k2 < 2; ++k2) qv[t][k2] = sm.q[t][0][0][k2][lane];
 #pragma unroll
-          for (int t = 0; t < RT; ++t) {
-            s[t][n] = mfma(a, ql[t][c][h], s[t][n]);
-            s[t][n] = mfma(a, qh[t][c][h], s[t][n]);
-          }
-        }
+    for (int st = 0; st < 2 * KL; ++st) {
+      const int c = st >> 1, h = st & 1;
+      u32x4 qn[RT][2];
+      if (st + 1 < 2 * KL)
+#pragma unroll
+        for (int t = 0; t < RT; ++t)
+#pragma unroll
+          for (int k2 = 0; k2 < 2; ++k2) qn[t][k2] = sm.q[t][(st + 1) >> 1][(st + 1) & 1][k2][lane];
+      u32x4 a[4];
+#pragma unroll
+      for (int n = 0; n < 4; ++n) a[n] = widen(kv_page[n * KL + c][2 * h], kv_page[n * KL + c][2 * h + 1]);
+#pragma unroll
+      for (int k2 = 1; k2 >= 0; --k2)
+#pragma unroll
+        for (int t = 0; t < RT; ++t)
+#pragma unroll
+          for (int n = 0; n < 4; ++n) s[t][n] = mfma(a[n], qv[t][k2], s[t][n]);
+      if (st + 1 < 2 * KL)
+#pragma unroll
+        for (int t = 0; t < RT; ++t)
+#pragma unroll
+          for (int k2 = 0; k2 < 2; ++k2) qv[t][k2] = qn[t][k2];
+      __builtin_amdgcn_sched_barrier(0);
     }
-    const u32x4 kscale = ksc;
-    if (more) load_keys(next);
+    const u32x4 kscale = scales;
+    load_values(ptr);
 
     // ---- the page's value scales; slots behind the sequence hold anything
-    u32x4 vscale = vsc;
+    u32x4 vscale = scales;
     const int tail = there - 4 * lq;       // of tile n: tail - 16 n tokens of this lane are there
     if (there < 64) {
 #pragma unroll
@@ -397,60 +434,57 @@ __global__ __launch_bounds__(kWaves * 64, (D == 256 || RT == 2) ? 1 : 2) void qu
 #pragma unroll
       for (int i = 0; i < DT; ++i)
 #pragma unroll
-        for (int n = 0; n < 4; ++n) vr[i][n] = keep_bytes(vr[i][n], tail - 16 * n);
+        for (int n = 0; n < 4; ++n) kv_page[i][n] = keep_bytes(kv_page[i][n], tail - 16 * n);
     }
-    // A token that one query of the page sees and another does not has weight 0
-    // for the other; 0 times a NaN is none, so a page of such tokens that holds a
-    // NaN is added query by query, each over the tokens that it sees.
-    bool apart = false;
+    // A token that one query of the page sees and another does not has weight 0 for the
+    // other, and 0 times a NaN is none: such a page's NaNs are taken out and given to
+    // the rows that see them, found by a product of the NaNs' and the rows' marks.
     if (queries > 1 && pos0 + 64 > T - queries + 1) {
       uint32_t nan = 0;
 #pragma unroll
       for (int i = 0; i < DT; ++i)
 #pragma unroll
-        for (int n = 0; n < 4; ++n) {
-          const uint32_t low = vr[i][n] & 0x7F7F7F7Fu;       // 0x7F: the only NaN
-          nan |= (low + 0x01010101u) & 0x80808080u;
-        }
-      apart = __any(nan != 0);
-    }
-    if (!apart) {
+        for (int n = 0; n < 4; ++n) nan |= nan_bytes(kv_page[i][n]);
+      if (__any(nan != 0)) {
 #pragma unroll
-      for (int i = 0; i < DT; ++i)
+        for (int t = 0; t < RT; ++t) {
+          const int see = min(there, limit[t] - pos0) - 4 * lq;
+          u32x4 marks[2];                  // 1 for the tokens that the row sees
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const u32x4 a = widen(vr[i][2 * h], vr[i][2 * h + 1]);
+          for (int n = 0; n < 4; ++n)
 #pragma unroll
-          for (int t = 0; t < RT; ++t) {
-            acc[t][i] = mfma(a, pl[t][h], acc[t][i]);
-            acc[t][i] = mfma(a, ph[t][h], acc[t][i]);
+            for (int v = 0; v < 4; v += 2)
+              marks[n >> 1][2 * (n & 1) + v / 2] = (16 * n + v < see ? 0x3C00u : 0u) |
+                                                   (16 * n + v + 1 < see ? 0x3C000000u : 0u);
+#pragma unroll
+          for (int i = 0; i < DT; ++i) {
+            floatx4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int h = 0; h < 2; ++h)    // 0x38: 1 in e4m3
+              y = mfma(widen((nan_bytes(kv_page[i][2 * h]) >> 7) * 0x38u, (nan_bytes(kv_page[i][2 * h + 1]) >> 7) * 0x38u),
+                       marks[h], y);
+#pragma unroll
+            for (int v = 0; v < 4; ++v) acc[t][i][v] = y[v] > 0.f ? __builtin_nanf("") : acc[t][i][v];
           }
         }
-    } else {
-      for (int qi = 0; qi < queries; ++qi) {
-        const int see = min(there, T - queries + qi + 1 - pos0) - 4 * lq;
 #pragma unroll
-        for (int i = 0; i < DT; ++i) {
-          u32x4 x;
+        for (int i = 0; i < DT; ++i)
 #pragma unroll
-          for (int n = 0; n < 4; ++n) x[n] = keep_bytes(vr[i][n], see - 16 * n);
-#pragma unroll
-          for (int t = 0; t < RT; ++t) {
-            floatx4 y = acc[t][i];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const u32x4 a = widen(x[2 * h], x[2 * h + 1]);
-              y = mfma(a, pl[t][h], y);
-              y = mfma(a, ph[t][h], y);
-            }
-            const bool mine_q = (row0 + 16 * t + lr) / per == qi;
-#pragma unroll
-            for (int v = 0; v < 4; ++v) acc[t][i][v] = mine_q ? y[v] : acc[t][i][v];
-          }
-        }
+          for (int n = 0; n < 4; ++n) kv_page[i][n] &= ~((nan_bytes(kv_page[i][n]) >> 7) * 0xFFu);
       }
     }
-    if (more) load_values(next);
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const u32x4 a = widen(kv_page[i][2 * h], kv_page[i][2 * h + 1]);
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+          acc[t][i] = mfma(a, pl[t][h], acc[t][i]);
+          acc[t][i] = mfma(a, ph[t][h], acc[t][i]);
+        }
+      }
+    if (more) load_keys(next);
     ptr = next;
     valid = next_valid;
   }
@@ -462,7 +496,7 @@ __global__ __launch_bounds__(kWaves * 64, (D == 256 || RT == 2) ? 1 : 2) void qu
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
     const float unit = ldexpf(1.f, k[t] - 127 - kTop);
-    if (t > 0) __syncthreads();
+    __syncthreads();                       // queries, or the tile before, are used up
     if (lq == 0) {
       red_m[w][lr] = m[t];
       red_l[w][lr] = sum;
@@ -472,7 +506,7 @@ __global__ __launch_bounds__(kWaves * 64, (D == 256 || RT == 2) ? 1 : 2) void qu
       floatx4 y;
 #pragma unroll
       for (int v = 0; v < 4; ++v) y[v] = acc[t][i][v] * unit;
-      *reinterpret_cast<floatx4*>(&red_o[w][lr][16 * i + 4 * lq]) = y;
+      *reinterpret_cast<floatx4*>(&sm.o[w][lr][16 * i + 4 * lq]) = y;
     }
     __syncthreads();
     for (int e = tid; e < 16 * D; e += kWaves * 64) {
@@ -488,7 +522,7 @@ __global__ __launch_bounds__(kWaves * 64, (D == 256 || RT == 2) ? 1 : 2) void qu
         if (red_l[k][r] == 0.f) continue;  // the wave saw nothing of the row
         const float f = __builtin_amdgcn_exp2f(red_m[k][r] - M);
         L = fmaf(f, red_l[k][r], L);
-        o = fmaf(f, red_o[k][r][d], o);
+        o = fmaf(f, sm.o[k][r][d], o);
       }
       const int64_t orow = (int64_t(b) * queries + row / per) * n_q_heads + kv * per + row % per;
       if (whole) {
