@@ -77,20 +77,13 @@ __device__ __forceinline__ void turn(int pos, double omega, float& c, float& s) 
   s = __builtin_amdgcn_sinf(f);
 }
 
-// Coordinate of the head at place `dim` of plane order: a plane's first
+// Coordinate of the head at place `dim` of plane order (t.n > 0): a plane's first
 // coordinates in places 0 .. d/2 - 1, its second ones d/2 further.
 __device__ __forceinline__ int rope_coord(const RopeTurns& t, int half, int dim) {
-  if (t.n == 0) return dim;
   const bool second = dim >= half;
   const int i = second ? dim - half : dim;
   if (i >= t.n) return 2 * t.n + (i - t.n) + (second ? half - t.n : 0);
   return t.interleaved ? 2 * i + (second ? 1 : 0) : i + (second ? t.n : 0);
-}
-
-// Turns a position of plane i (of d/2).
-__device__ __forceinline__ double rope_omega(const RopeTurns& t, int d, int i) {
-  if (t.n == 0) return exp2(-(2.0 * i / d) * t.log2_base) * kInv2Pi;
-  return i < t.n ? t.turns[i] : 0.0;
 }
 
 // ---------------------------------------------------------------------------
@@ -110,7 +103,7 @@ __global__ __launch_bounds__(256) void rope_factors(const bf16* __restrict__ Rk,
   const int ci = blk / dt, it = blk % dt;
   const int dim = 16 * it + (l & 15);
   const int col0 = 32 * (c_lo + ci) + 8 * (l >> 4);
-  const bf16* src = Rk + tb.roff[kv] + tb.rcol[kv] + rope_coord(turns, tb.head_dim / 2, dim);
+  const bf16* src = Rk + tb.roff[kv] + tb.rcol[kv] + (turns.n ? rope_coord(turns, tb.head_dim / 2, dim) : dim);
   uint32_t w[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
@@ -267,7 +260,8 @@ __device__ __forceinline__ void wave_split_softmax(const float* srow, int ntok, 
 
 // ---------------------------------------------------------------------------
 // The general kernel (any group width): the chunk's factor blocks staged per
-// step.  DT: 16-row tiles of d_h (4 for d_h = 64, 8 for d_h = 128).
+// step.  DT: 16-row tiles of d_h (4 for d_h = 64, 8 for d_h = 128).  TURNS: any
+// rotation (turns.n > 0); without, every plane by its power of the base.
 //
 // Pipeline: the work-group's steps run over (page round, key chunk); step
 // s stages the factor blocks of the next chunk into the LDS buffer the
@@ -276,7 +270,7 @@ __device__ __forceinline__ void wave_split_softmax(const float* srow, int ntok, 
 // own page's key loads for the chunk kDepth steps ahead, so the two streams
 // come due in the order they were issued and one wait never holds back a
 // younger load.
-template <int DT>
+template <int DT, bool TURNS>
 __global__ __launch_bounds__(256, 1) void rope_scores(
     const float* __restrict__ q, const bf16* __restrict__ pool, int64_t num_pages,
     const int32_t* __restrict__ page_table, int max_pages, const int32_t* __restrict__ seq_lens,
@@ -325,7 +319,11 @@ __global__ __launch_bounds__(256, 1) void rope_scores(
 
   // ---- prologue: plane frequencies, the split's pages, turned queries
   if (tid < D / 2) {
-    const double om = rope_omega(turns, D, tid);
+    double om;
+    if constexpr (TURNS)
+      om = tid < turns.n ? turns.turns[tid] : 0.0;
+    else
+      om = exp2(-(2.0 * tid / D) * turns.log2_base) * kInv2Pi;
     omega[tid] = om;
     float c16, s16;
     turn(16, om, c16, s16);
@@ -344,10 +342,16 @@ __global__ __launch_bounds__(256, 1) void rope_scores(
       const float* qh = q + (int64_t(b) * Hq + kv * qpk + hh) * D;
       float c, s;
       turn(pq, omega[i], c, s);
-      const float xa = qh[rope_coord(turns, D / 2, i)], xb = qh[rope_coord(turns, D / 2, i + D / 2)];
-      const float sc_i = i < turns.n ? scale * turns.weight : scale;
-      qr[hh][i] = (xa * c - xb * s) * sc_i;
-      qr[hh][i + D / 2] = (xb * c + xa * s) * sc_i;
+      if constexpr (TURNS) {
+        const float xa = qh[rope_coord(turns, D / 2, i)], xb = qh[rope_coord(turns, D / 2, i + D / 2)];
+        const float weighted = i < turns.n ? scale * turns.weight : scale;
+        qr[hh][i] = (xa * c - xb * s) * weighted;
+        qr[hh][i + D / 2] = (xb * c + xa * s) * weighted;
+      } else {
+        const float xa = qh[i], xb = qh[i + D / 2];
+        qr[hh][i] = (xa * c - xb * s) * scale;
+        qr[hh][i + D / 2] = (xb * c + xa * s) * scale;
+      }
     }
   }
 
@@ -478,7 +482,7 @@ __global__ __launch_bounds__(256, 1) void rope_scores(
 // chunks ahead.  Scores of the whole range stay in LDS (qpk * spw * L <=
 // kResScores floats); at the end each wave takes whole splits for their
 // softmax, so the waves meet only twice: after staging and before the tail.
-template <int DT>
+template <int DT, bool TURNS>
 __global__ __launch_bounds__(512, 1) void rope_scores_res(
     const float* __restrict__ q, const bf16* __restrict__ pool, int64_t num_pages,
     const int32_t* __restrict__ page_table, int max_pages, const int32_t* __restrict__ seq_lens,
@@ -529,7 +533,11 @@ __global__ __launch_bounds__(512, 1) void rope_scores_res(
   // ---- prologue: frequencies and pages; then the turned queries and the
   // head's factor blocks (eight 16-byte loads in flight a thread)
   if (tid < D / 2) {
-    const double om = rope_omega(turns, D, tid);
+    double om;
+    if constexpr (TURNS)
+      om = tid < turns.n ? turns.turns[tid] : 0.0;
+    else
+      om = exp2(-(2.0 * tid / D) * turns.log2_base) * kInv2Pi;
     omega[tid] = om;
     float c16, s16;
     turn(16, om, c16, s16);
@@ -548,10 +556,16 @@ __global__ __launch_bounds__(512, 1) void rope_scores_res(
       const float* qh = q + (int64_t(b) * Hq + kv * qpk + hh) * D;
       float c, s;
       turn(pq, omega[i], c, s);
-      const float xa = qh[rope_coord(turns, D / 2, i)], xb = qh[rope_coord(turns, D / 2, i + D / 2)];
-      const float sc_i = i < turns.n ? scale * turns.weight : scale;
-      qr[hh * D + i] = (xa * c - xb * s) * sc_i;
-      qr[hh * D + i + D / 2] = (xb * c + xa * s) * sc_i;
+      if constexpr (TURNS) {
+        const float xa = qh[rope_coord(turns, D / 2, i)], xb = qh[rope_coord(turns, D / 2, i + D / 2)];
+        const float weighted = i < turns.n ? scale * turns.weight : scale;
+        qr[hh * D + i] = (xa * c - xb * s) * weighted;
+        qr[hh * D + i + D / 2] = (xb * c + xa * s) * weighted;
+      } else {
+        const float xa = qh[i], xb = qh[i + D / 2];
+        qr[hh * D + i] = (xa * c - xb * s) * scale;
+        qr[hh * D + i + D / 2] = (xb * c + xa * s) * scale;
+      }
     }
     const int nvec = nch * DT * 64;
     for (int base = tid; base < nvec; base += 8 * W * 64) {
@@ -757,8 +771,8 @@ hipError_t launch_rope_scores(const dckv_plan& p, const DecodeShape& sh, const f
                            p.mfma.n_slices, static_cast<bf16*>(pbuf), part_ml, turns, p.rope);
       return hipGetLastError();
     };
-    if (p.dh == 128) return go(rope_scores_res<8>);
-    if (p.dh == 64) return go(rope_scores_res<4>);
+    if (p.dh == 128) return turns.n ? go(rope_scores_res<8, true>) : go(rope_scores_res<8, false>);
+    if (p.dh == 64) return turns.n ? go(rope_scores_res<4, true>) : go(rope_scores_res<4, false>);
     return hipErrorInvalidValue;
   }
   const int n_work = sh.batch * sh.n_split * p.Hkv;
@@ -777,8 +791,8 @@ hipError_t launch_rope_scores(const dckv_plan& p, const DecodeShape& sh, const f
                          p.mfma.n_slices, static_cast<bf16*>(pbuf), part_ml, turns, p.rope);
     return hipGetLastError();
   };
-  if (p.dh == 128) return go(rope_scores<8>);
-  if (p.dh == 64) return go(rope_scores<4>);
+  if (p.dh == 128) return turns.n ? go(rope_scores<8, true>) : go(rope_scores<8, false>);
+  if (p.dh == 64) return turns.n ? go(rope_scores<4, true>) : go(rope_scores<4, false>);
   return hipErrorInvalidValue;
 }
 
