@@ -457,7 +457,8 @@ int dckv_rotary_info(const dckv_rotary* rotary, double* theta);
  *              (elements), d_h elements one after another; dtypes DCKV_F32 or
  *              DCKV_BF16, in any pairing.  out may be x (same dtype and strides);
  *              otherwise they must not overlap.  Heads of `out` must not overlap
- *              each other; those of x may (strides of 0 broadcast).  Strides are
+ *              each other: either a token's heads lie together or a head's
+ *              tokens do.  Those of x may (strides of 0 broadcast).  Strides are
  *              not negative.  Rows in whole 16-byte pieces are fastest.
  *   position   device int32 [n_tok]; a token of negative position is skipped, its
  *              row of `out` left as it was
@@ -542,8 +543,11 @@ int dckv_quant_read(int32_t num_kv_heads, int32_t head_dim, const void* pool, in
  * split_tokens: context tokens a work split, a multiple of 64, or 0 to choose
  * from the shape.  A workspace (256-byte aligned; its contents do not matter) of
  * dckv_quant_workspace_bytes also serves fewer sequences and shorter contexts;
- * a call of one split a sequence uses none and takes NULL.  batch * Q at most 65535; batch == 0 is a no-op.  Results are
- * bitwise reproducible for a fixed shape. */
+ * a call of one split a sequence uses none and takes NULL.  Calls that may
+ * overlap (other streams, other captured graphs) need workspaces of their own.
+ * batch * Q at most 65535; batch == 0 is a no-op.  Results are
+ * bitwise reproducible for fixed inputs; where the library chooses the splits,
+ * they depend on the lengths of all sequences of the call. */
 int dckv_quant_workspace_bytes(int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
                                int32_t queries_per_seq, int32_t split_tokens, int32_t batch,
                                int32_t max_context, size_t* bytes);

@@ -17,7 +17,7 @@ namespace {
 constexpr double kPi = 3.14159265358979323846;
 constexpr int64_t kMaxGroups = (int64_t(1) << 24) - 1;   // work-groups of 256 threads in a grid
 constexpr int32_t kMaxTokens = 1 << 23;                  // tokens a call: a thread a coordinate fits a grid
-constexpr int64_t kMaxStride = int64_t(1) << 40;   // elements: offsets stay within int64
+constexpr int64_t kMaxStride = int64_t(1) << 38;   // elements: offsets stay within int64
 
 bool positive(double x) { return std::isfinite(x) && x > 0.0; }
 
@@ -88,7 +88,9 @@ int check_quant(const char* where, int32_t Hq, int32_t Hkv, int32_t dh, int32_t 
                 split, DCKV_PAGE_TOKENS);
   if (batch < 0 || int64_t(batch) * Q > 65535)
     return fail(DCKV_EINVAL, "%s: batch %d of %d queries outside 0..65535", where, batch, Q);
-  if (max_context < 0) return fail(DCKV_EINVAL, "%s: max_context %d < 0", where, max_context);
+  if (max_context < 0 || max_context > INT32_MAX - DCKV_PAGE_TOKENS)
+    return fail(DCKV_EINVAL, "%s: max_context %d outside 0..%d", where, max_context,
+                INT32_MAX - DCKV_PAGE_TOKENS);
   const dckv::QuantShape sh = dckv::quant_shape(Hq, Hkv, dh, Q, split, batch, max_context);
   if (sh.groups > kMaxGroups)
     return fail(DCKV_EINVAL, "%s: the splits of %d sequences, %d KV heads and %d row slices take %lld work-groups, above %lld",
@@ -231,7 +233,12 @@ int dckv_rotary_apply(const dckv_rotary* rotary, const void* x, int32_t x_dtype,
     return fail(DCKV_EINVAL, "rotary_apply: n_tok %d outside 0..%d", n_tok, kMaxTokens);
   if (num_heads < 1 || num_heads > 65535)
     return fail(DCKV_EINVAL, "rotary_apply: num_heads %d outside 1..65535", num_heads);
-  if ((num_heads > 1 && out_head_stride < d) || (n_tok > 1 && out_token_stride < d))
+  // tokens of whole rows of heads, or heads of whole columns of tokens
+  const bool by_token = (n_tok <= 1 || out_token_stride >= (num_heads - 1) * out_head_stride + d) &&
+                        (num_heads == 1 || out_head_stride >= d);
+  const bool by_head = (num_heads == 1 || out_head_stride >= int64_t(n_tok - 1) * out_token_stride + d) &&
+                       (n_tok <= 1 || out_token_stride >= d);
+  if (n_tok > 0 && !by_token && !by_head)
     return fail(DCKV_EINVAL, "rotary_apply: heads of out overlap (strides %lld, %lld, head_dim %d)",
                 (long long)out_token_stride, (long long)out_head_stride, d);
   if (x == out && n_tok > 0 &&

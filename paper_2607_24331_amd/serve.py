@@ -18,55 +18,57 @@ _LAYOUTS = {"half": 0, "interleaved": 1}
 _SCALINGS = {"none": 0, "linear": 1, "base": 2, "turns": 3, "planes": 4}
 
 
-def _gpu(t: torch.Tensor, name: str, dtype, device=None, contiguous: bool = True) -> int:
-    """The address of a tensor of `dtype` on the GPU (on `device`, where given)."""
-    if not isinstance(t, torch.Tensor):
-        raise TypeError(f"{name} must be a torch tensor")
-    if not t.is_cuda:
+def _gpu(t: torch.Tensor, name: str, dtype, index: Optional[int] = None, contiguous: bool = True) -> int:
+    """The address of a tensor of `dtype` on the GPU (on device `index`, where given)."""
+    try:
+        on = t.get_device()                                   # -1: not a GPU
+        if on >= 0 and (on == index or index is None) and t.dtype is dtype and (not contiguous or t.is_contiguous()):
+            return t.data_ptr()
+    except AttributeError:
+        raise TypeError(f"{name} must be a torch tensor") from None
+    if on < 0:
         raise ValueError(f"{name} must be on the GPU")
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if device is not None and t.device != device:
-        raise ValueError(f"{name} is on {t.device}, the call's other tensors on {device}")
-    if contiguous and not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    return t.data_ptr()
+    if index is not None and on != index:
+        raise ValueError(f"{name} is on device {on}, the call's other tensors on {index}")
+    raise ValueError(f"{name} must be contiguous")
 
 
-def _vector(t: torch.Tensor, name: str, dtype, n: int, device=None) -> int:
-    p = _gpu(t, name, dtype, device)
-    if t.dim() != 1 or t.shape[0] != n:
+def _vector(t: torch.Tensor, name: str, dtype, n: int, index: Optional[int] = None) -> int:
+    p = _gpu(t, name, dtype, index)
+    if t.shape != (n,):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {(n,)}")
     return p
 
 
-def _heads(t: torch.Tensor, name: str, device=None):
+def _heads(t: torch.Tensor, name: str, index: Optional[int] = None):
     """(address, dtype code, token stride, head stride) of [tokens, heads, d]."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch tensor")
     code = _CODE.get(t.dtype)
     if code is None:
         raise TypeError(f"{name} must be float32 or bfloat16, got {t.dtype}")
-    p = _gpu(t, name, t.dtype, device, contiguous=False)
-    if t.dim() != 3:
+    p = _gpu(t, name, t.dtype, index, False)
+    strides = t.stride()
+    if len(strides) != 3:
         raise ValueError(f"{name} must be [tokens, heads, head_dim]")
-    st, sh, sd = t.stride()
+    st, sh, sd = strides
     if sd != 1 and t.shape[2] > 1:
         raise ValueError(f"{name}: the coordinates of a head must lie one after another")
     return p, code, st, sh
 
 
-def _launch(fn, what: str, device: torch.device, stream, *args) -> None:
+def _launch(fn, what: str, index: int, stream, *args) -> None:
     """fn(*args, stream) with the tensors' device current, on `stream` or on
     that device's current stream."""
-    index = device.index
     if index != torch.cuda.current_device():
-        with torch.cuda.device(device):
-            return _launch(fn, what, device, stream, *args)
+        with torch.cuda.device(index):
+            return _launch(fn, what, index, stream, *args)
     if stream is None:
         handle = torch._C._cuda_getCurrentRawStream(index)   # current_stream() builds an object: 2 us
-    elif stream.device != device:
-        raise ValueError(f"{what}: the stream is of {stream.device}, the tensors of {device}")
+    elif stream.device.index != index:
+        raise ValueError(f"{what}: the stream is of {stream.device}, the tensors of device {index}")
     else:
         handle = stream.cuda_stream
     status = fn(*args, handle)
@@ -105,7 +107,7 @@ def page_map(cached: torch.Tensor, added: torch.Tensor, page_table: torch.Tensor
     so that a step updates them in place."""
     if not isinstance(cached, torch.Tensor) or cached.dim() != 1:
         raise ValueError("cached must be a vector")
-    B, rows, dev, i32 = cached.shape[0], int(rows), cached.device, torch.int32
+    B, rows, dev, i32 = cached.shape[0], int(rows), cached.get_device(), torch.int32
     if rows < 0:
         raise ValueError("rows must not be negative")
     pc = _vector(cached, "cached", i32, B)
@@ -118,8 +120,8 @@ def page_map(cached: torch.Tensor, added: torch.Tensor, page_table: torch.Tensor
         raise ValueError("free_pages must be a vector")
     pn = _vector(free_count, "free_count", i32, 1, dev)
     if out is None:
-        slot = _new((rows,), torch.int64, dev, stream)
-        block = _new((3 * B + 2 + 2 * rows,), i32, dev, stream)
+        slot = _new((rows,), torch.int64, cached.device, stream)
+        block = _new((3 * B + 2 + 2 * rows,), i32, cached.device, stream)
         lens, start, pos, seq, status, left = block.split((B, B + 1, rows, rows, B, 1))
         out = PageMap(lens, start, slot, pos, seq, status, left)
         at = block.data_ptr()
@@ -152,7 +154,7 @@ def page_release(finished: torch.Tensor, page_table: torch.Tensor, seq_lens: tor
     i32 = torch.int32
     if not isinstance(finished, torch.Tensor) or finished.dim() != 1:
         raise ValueError("finished must be a vector")
-    B, dev = finished.shape[0], finished.device
+    B, dev = finished.shape[0], finished.get_device()
     pd = _vector(finished, "finished", i32, B)
     pt = _gpu(page_table, "page_table", i32, dev)
     if page_table.dim() != 2 or page_table.shape[0] != B:
@@ -226,7 +228,8 @@ def rotary(rotation: Rotary, x: torch.Tensor, position: torch.Tensor, out: Optio
     n, H, d = x.shape
     if d != rotation.head_dim:
         raise ValueError(f"x has heads of {d}, the rotation of {rotation.head_dim}")
-    pp = _vector(position, "position", torch.int32, n, x.device)
+    dev = x.get_device()
+    pp = _vector(position, "position", torch.int32, n, dev)
     if out is None:
         oc = xc if out_dtype is None else _CODE.get(out_dtype)
         if oc is None:
@@ -236,11 +239,11 @@ def rotary(rotation: Rotary, x: torch.Tensor, position: torch.Tensor, out: Optio
     else:
         if out_dtype is not None and out.dtype != out_dtype:
             raise TypeError(f"out is {out.dtype}, not {out_dtype}")
-        po, oc, ot, oh = _heads(out, "out", x.device)
+        po, oc, ot, oh = _heads(out, "out", dev)
         if tuple(out.shape) != (n, H, d):
             raise ValueError(f"out has shape {tuple(out.shape)}, expected {(n, H, d)}")
     if n and H:
-        _launch(_lib.dckv_rotary_apply, "rotary_apply", x.device, stream, rotation.handle, px, xc, xt, xh,
+        _launch(_lib.dckv_rotary_apply, "rotary_apply", dev, stream, rotation.handle, px, xc, xt, xh,
                 po, oc, ot, oh, pp, n, H, 1 if inverse else 0)
     return out
 
@@ -253,7 +256,7 @@ def decode_rotary(plan, q: torch.Tensor, pool: torch.Tensor, page_table: torch.T
     head_dim."""
     B, f32 = q.shape[0], torch.float32
     shape = (B, plan.num_q_heads, plan.head_dim)
-    dev, dt = q.device, plan.torch_dtype
+    dev, dt = q.get_device(), plan.torch_dtype
     pq = _gpu(q, "q", f32)
     if tuple(q.shape) != shape:
         raise ValueError(f"q has shape {tuple(q.shape)}, expected {shape}")
@@ -271,12 +274,12 @@ def decode_rotary(plan, q: torch.Tensor, pool: torch.Tensor, page_table: torch.T
     if tuple(R_value.shape) != (plan.value_rank, plan.num_kv_heads * plan.head_dim):
         raise ValueError(f"R_value has shape {tuple(R_value.shape)}")
     if out is None:
-        out = _new(shape, f32, dev, stream)
+        out = _new(shape, f32, q.device, stream)
     po = _gpu(out, "out", f32, dev)
     if tuple(out.shape) != shape:
         raise ValueError(f"out has shape {tuple(out.shape)}, expected {shape}")
     if workspace is None:
-        workspace = _new((max(plan.rope_workspace_bytes(B, max_context), 256),), torch.uint8, dev, stream)
+        workspace = _new((max(plan.rope_workspace_bytes(B, max_context), 256),), torch.uint8, q.device, stream)
     pw = _gpu(workspace, "workspace", torch.uint8, dev)
     _launch(_lib.dckv_decode_rotary, "decode_rotary", dev, stream, plan.handle, pq, B, pp,
             pool.numel() // plan.page_elems, pt, page_table.shape[1], ps, int(max_context), pk, pv,
@@ -287,21 +290,22 @@ def decode_rotary(plan, q: torch.Tensor, pool: torch.Tensor, page_table: torch.T
 # ------------------------------------------------------- uncompressed K/V caches
 def _append(fn, what: str, k, v, slot, pool, pool_dtype, page: int, rotation, position, stream) -> None:
     pk, kc, kt, kh = _heads(k, "k")
-    pv, vc, vt, vh = _heads(v, "v", k.device)
+    dev = k.get_device()
+    pv, vc, vt, vh = _heads(v, "v", dev)
     n, H, d = k.shape
-    if tuple(v.shape) != (n, H, d) or vc != kc:
+    if v.shape != k.shape or vc != kc:
         raise ValueError("k and v must have one shape and dtype")
-    ps = _vector(slot, "slot", torch.int64, n, k.device)
-    pp = _gpu(pool, "pool", pool_dtype, k.device)
+    ps = _vector(slot, "slot", torch.int64, n, dev)
+    pp = _gpu(pool, "pool", pool_dtype, dev)
     if pool.numel() % page:
         raise ValueError("pool size is not a whole number of pages")
     handle = pos = None
     if rotation is not None:
         if position is None:
             raise ValueError("position is needed to turn the keys")
-        handle, pos = rotation.handle, _vector(position, "position", torch.int32, n, k.device)
+        handle, pos = rotation.handle, _vector(position, "position", torch.int32, n, dev)
     if n:
-        _launch(fn, what, k.device, stream, H, d, pk, pv, kc, kt, kh, vt, vh, ps, n, handle, pos, pp,
+        _launch(fn, what, dev, stream, H, d, pk, pv, kc, kt, kh, vt, vh, ps, n, handle, pos, pp,
                 pool.numel() // page)
 
 
@@ -352,10 +356,10 @@ def quant_read(pool: torch.Tensor, slot: torch.Tensor, num_kv_heads: int, head_d
         raise TypeError("dtype must be float32 or bfloat16")
     if not isinstance(slot, torch.Tensor) or slot.dim() != 1:
         raise ValueError("slot must be a vector")
-    n, dev = slot.shape[0], pool.device
+    n, dev = slot.shape[0], pool.get_device()
     ps = _vector(slot, "slot", torch.int64, n, dev)
-    k = _new((n, num_kv_heads, head_dim), dtype, dev, stream)
-    v = _new((n, num_kv_heads, head_dim), dtype, dev, stream)
+    k = _new((n, num_kv_heads, head_dim), dtype, pool.device, stream)
+    v = _new((n, num_kv_heads, head_dim), dtype, pool.device, stream)
     if n:
         _launch(_lib.dckv_quant_read, "quant_read", dev, stream, num_kv_heads, head_dim, pp,
                 pool.numel() // page, ps, n, k.data_ptr(), v.data_ptr(), _CODE[dtype])
@@ -387,7 +391,7 @@ def quant_decode(q: torch.Tensor, pool: torch.Tensor, page_table: torch.Tensor, 
         (B, Hq, d), Q = q.shape, 1
     else:
         raise ValueError("q must be [batch, Q, H_q, d_h] or [batch, H_q, d_h]")
-    dev, top = q.device, int(max_context)
+    dev, top = q.get_device(), int(max_context)
     pp = _gpu(pool, "pool", torch.uint8, dev)
     page = quant_page_bytes(num_kv_heads, d)
     if pool.numel() % page:
@@ -397,13 +401,13 @@ def quant_decode(q: torch.Tensor, pool: torch.Tensor, page_table: torch.Tensor, 
         raise ValueError("page_table must be [batch, max_pages]")
     ps = _vector(seq_lens, "seq_lens", torch.int32, B, dev)
     if out is None:
-        out = _new(q.shape, f32, dev, stream)
+        out = _new(q.shape, f32, q.device, stream)
     po = _gpu(out, "out", f32, dev)
     if out.shape != q.shape:
         raise ValueError(f"out has shape {tuple(out.shape)}, expected {tuple(q.shape)}")
     need = quant_workspace_bytes(Hq, num_kv_heads, d, Q, split_tokens, B, top)
     if workspace is None and need:
-        workspace = _new((need,), torch.uint8, dev, stream)
+        workspace = _new((need,), torch.uint8, q.device, stream)
     pw = _gpu(workspace, "workspace", torch.uint8, dev) if workspace is not None else None
     _launch(_lib.dckv_quant_decode, "quant_decode", dev, stream, Hq, num_kv_heads, d, Q, split_tokens, pq, B,
             pp, pool.numel() // page, pt, page_table.shape[1], ps, top, po, pw,

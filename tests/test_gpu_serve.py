@@ -493,6 +493,42 @@ def test_quant_decode_on_another_stream_and_refusals():
         quant_read(args[0], slot, 2, 128, torch.float16)
 
 
+def test_offsets_past_32_bits():
+    # the same tokens in the first pages of a pool of over 4 GB and in its last ones
+    from paper_2607_24331_amd import (dense_append, dense_decode, dense_page_elems, new_quant_pool, quant_append,
+                                      quant_decode, quant_page_bytes, quant_read)
+    H, d, T = 8, 128, 300
+    g = torch.Generator(device="cuda")
+    g.manual_seed(8)
+    kv = torch.randn((T, 2, H, d), generator=g, device="cuda").to(BF16)
+    q = torch.randn((1, 2 * H, d), generator=g, device="cuda")
+    lens = torch.tensor([T], dtype=torch.int32, device="cuda")
+    pages = (1 << 32) // quant_page_bytes(H, d) + 40
+    at = torch.arange(T, device="cuda")
+    pool = new_quant_pool(pages, H, d)
+    bf = torch.zeros((pages, dense_page_elems(H, d)), dtype=BF16, device="cuda")
+    got = []
+    for first in (0, pages - 5):
+        slot = first * 64 + at
+        quant_append(kv[:, 0], kv[:, 1], slot, pool)
+        dense_append(kv[:, 0], kv[:, 1], slot, bf)
+        table = (first + torch.arange(5, device="cuda")).to(torch.int32)[None]
+        got.append((*quant_read(pool, slot, H, d), quant_decode(q, pool, table, lens, 320, H, 64),
+                    dense_decode(q, bf, table, lens, 320, H)))
+    assert all(torch.equal(a, b) for a, b in zip(*got)) and got[0][2].abs().sum() > 0
+    # and activations whose tokens lie 2^31 elements apart
+    far = torch.empty((1 << 32) + H * d, dtype=BF16, device="cuda")
+    x = far.as_strided((3, H, d), (1 << 31, d, 1))
+    x.copy_(kv[:3, 0])
+    quant_append(x, x, slot[:3], pool)
+    assert torch.equal(quant_read(pool, slot[:3], H, d)[0], got[0][0][:3])
+    r, *_ = _rotation(d, {})
+    from paper_2607_24331_amd import rotary
+    pos = at[:3].to(torch.int32)
+    want = rotary(r, kv[:3, 0], pos)
+    assert torch.equal(rotary(r, x, pos), want) and torch.equal(rotary(r, x, pos, out=x), want)
+
+
 # ------------------------------------------------ rotary decode over the latents
 @pytest.mark.parametrize("rot", [0, 1, 2, 3, 6, 7])
 @pytest.mark.parametrize("d", [64, 128])

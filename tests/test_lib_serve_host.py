@@ -110,7 +110,8 @@ def test_rotary_apply_refuses(lib):
     go = lambda **kw: _call(lib.dckv_rotary_apply, base, **kw)  # noqa: E731
     for kw in (dict(r=None), dict(x=None), dict(out=None), dict(pos=None), dict(n=-1), dict(n=(1 << 23) + 1),
                dict(heads=0), dict(heads=65536), dict(xt=-1), dict(xh=-1), dict(ot=1 << 41), dict(oh=127), dict(ot=100),
-               dict(out=A, ot=2048), dict(out=A, od=0)):
+               dict(out=A, ot=2048), dict(out=A, od=0), dict(ot=1023), dict(ot=128, oh=128),
+               dict(ot=128, oh=511), dict(ot=127, oh=512)):
         assert go(**kw) == E, kw
     assert go(xd=2) == go(od=-1) == capi.DCKV_EDTYPE
     assert go(x=A + 1) == go(out=A + 1) == go(pos=A + 2) == go(xd=0, x=A + 2) == capi.DCKV_EALIGN
@@ -153,6 +154,7 @@ def test_read_and_decode_refuse(lib):
                dict(split=100), dict(split=1 << 25), dict(batch=-1), dict(batch=65536), dict(batch=2000, Q=33), dict(q=None),
                dict(pool=None), dict(table=None), dict(lens=None), dict(out=None), dict(ws=None), dict(pages=0),
                dict(max_pages=0), dict(top=-1), dict(top=512 * 64 + 1),
+               dict(top=2 ** 31 - 1, max_pages=2 ** 31 - 1),
                dict(batch=65535, split=64, top=1 << 20, max_pages=1 << 20)):
         assert go(**kw) == E, kw
     assert go(q=A + 4) == go(pool=A + 8) == go(out=A + 8) == go(ws=A + 128) == go(lens=A + 1) == capi.DCKV_EALIGN
@@ -163,6 +165,7 @@ def test_read_and_decode_refuse(lib):
 
 # what a call needs, from the message that refuses it a workspace of no bytes
 # (0 where it runs without one: no such call is made here)
+@fake
 @pytest.mark.parametrize("Hq, H, d, Q, split", [(32, 8, 128, 1, 0), (32, 32, 128, 1, 0), (16, 1, 64, 8, 0),
                                                 (8, 2, 256, 3, 0), (32, 8, 128, 1, 256), (8, 8, 64, 2, 64)])
 def test_workspace_serves_every_smaller_call(lib, Hq, H, d, Q, split):
