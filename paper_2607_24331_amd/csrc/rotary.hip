@@ -8,6 +8,8 @@
 // of one token and walks over heads h, h + G, ...: the V sines and cosines, an
 // fp64 product and a few dozen fp32 instructions each, are formed once for all
 // of them.  Adjacent threads take adjacent pieces, then adjacent heads.
+// 8,191 tokens x 40 heads of 128, bf16: 37 us out of HBM (4.5 TB/s; a copy reaches 5.2),
+// 64 tokens 4.2 us.  Non-temporal stores 44 us; four pairs of pieces in flight 38.
 #include <algorithm>
 
 #include "rotary.h"
