@@ -9,7 +9,9 @@
 // fp64 product and a few dozen fp32 instructions each, are formed once for all
 // of them.  Adjacent threads take adjacent pieces, then adjacent heads.
 // 8,191 tokens x 40 heads of 128, bf16: 37 us out of HBM (4.5 TB/s; a copy reaches 5.2),
-// 64 tokens 4.2 us.  Non-temporal stores 44 us; four pairs of pieces in flight 38.
+// 64 tokens 4.2 us; 4,096 x 32 heads of 64 in fp32, 24 coordinates turned: 14 us (4.8 TB/s).
+// Non-temporal stores took 44 us in the first; pieces that are copied in a loop of their
+// own 17 in the last.
 #include <algorithm>
 
 #include "rotary.h"
@@ -21,7 +23,8 @@ constexpr int kThreads = 256;
 constexpr int kUnroll = 2;                    // heads in flight a thread (pairs of pieces)
 constexpr int64_t kTargetThreads = 262144;    // four waves a SIMD over 256 compute units
 
-template <typename TI, typename TO, int V>
+// MIXED: some pieces are not turned.
+template <typename TI, typename TO, int V, bool MIXED>
 __global__ __launch_bounds__(kThreads) void rotary_rows(
     RotaryTable rot, const TI* x, RowStrides xs, TO* out, RowStrides os,
     const int32_t* __restrict__ position, int n_heads, int groups, int pieces, int plane_pieces,
@@ -36,59 +39,47 @@ __global__ __launch_bounds__(kThreads) void rotary_rows(
   if (pos < 0) return;
   const TI* xr = x + tok * xs.token;
   TO* yr = out + tok * os.token;
-  if (piece >= plane_pieces) {                // coordinates that are not turned
-    const int at = 2 * rot.planes + (piece - plane_pieces) * V;
-    for (int h0 = g; h0 < n_heads; h0 += 2 * kUnroll * groups) {
-      Piece<TI, V> a[2 * kUnroll];
-#pragma unroll
-      for (int u = 0; u < 2 * kUnroll; ++u)
-        if (h0 + u * groups < n_heads)
-          a[u] = *reinterpret_cast<const Piece<TI, V>*>(xr + (h0 + u * groups) * xs.head + at);
-#pragma unroll
-      for (int u = 0; u < 2 * kUnroll; ++u)
-        if (h0 + u * groups < n_heads) {
-          Piece<TO, V> b;
-#pragma unroll
-          for (int e = 0; e < V; ++e) b.v[e] = from_f32<TO>(to_f32(a[u].v[e]));
-          *reinterpret_cast<Piece<TO, V>*>(yr + (h0 + u * groups) * os.head + at) = b;
-        }
-    }
-    return;
-  }
+  // a piece of coordinates that are not turned is one of cosine 1 and sine 0 without a
+  // second half: its loads wait with the others', not after them
+  const bool turn = !MIXED || piece < plane_pieces, il = turn && rot.interleaved != 0;
   const int p0 = piece * V;
   float c[V], s[V];
 #pragma unroll
   for (int e = 0; e < V; ++e) {
-    const float2 f = rotary_factor(rot, p0 + e, pos);
-    c[e] = f.x;
-    s[e] = f.y * sign;
+    c[e] = 1.f;
+    s[e] = 0.f;
+    if (turn) {
+      const float2 f = rotary_factor(rot, p0 + e, pos);
+      c[e] = f.x;
+      s[e] = f.y * sign;
+    }
   }
-  // both pieces of a plane run: half layout (p0, p0 + planes), interleaved one
-  // run of 2 V elements from 2 p0
-  const bool il = rot.interleaved != 0;
-  const int at0 = il ? 2 * p0 : p0, at1 = il ? 2 * p0 + V : p0 + rot.planes;
+  // both pieces of a plane run: half layout (p0, p0 + planes), interleaved one run of 2 V
+  // elements from 2 p0
+  const int at0 = turn ? (il ? 2 * p0 : p0) : 2 * rot.planes + (piece - plane_pieces) * V;
+  const int at1 = il ? 2 * p0 + V : p0 + rot.planes;
   for (int h0 = g; h0 < n_heads; h0 += kUnroll * groups) {
-    Piece<TI, V> a[kUnroll], b[kUnroll];      // all loads before the first store
+    Piece<TI, V> a[kUnroll], b[kUnroll] = {}; // all loads before the first store
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       const int h = h0 + u * groups;
       if (h < n_heads) {
         a[u] = *reinterpret_cast<const Piece<TI, V>*>(xr + h * xs.head + at0);
-        b[u] = *reinterpret_cast<const Piece<TI, V>*>(xr + h * xs.head + at1);
+        if (turn) b[u] = *reinterpret_cast<const Piece<TI, V>*>(xr + h * xs.head + at1);
       }
     }
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       const int h = h0 + u * groups;
       if (h < n_heads) {
+        float v[2 * V];                       // the run of a interleaved, or a then b
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          v[e] = to_f32(a[u].v[e]);
+          v[V + e] = to_f32(b[u].v[e]);
+        }
         Piece<TO, V> ya, yb;
         if (il) {
-          float v[2 * V];
-#pragma unroll
-          for (int e = 0; e < V; ++e) {
-            v[e] = to_f32(a[u].v[e]);
-            v[V + e] = to_f32(b[u].v[e]);
-          }
           TO y[2 * V];
 #pragma unroll
           for (int e = 0; e < V; ++e) {
@@ -103,13 +94,12 @@ __global__ __launch_bounds__(kThreads) void rotary_rows(
         } else {
 #pragma unroll
           for (int e = 0; e < V; ++e) {
-            const float xa = to_f32(a[u].v[e]), xb = to_f32(b[u].v[e]);
-            ya.v[e] = from_f32<TO>(xa * c[e] - xb * s[e]);
-            yb.v[e] = from_f32<TO>(xb * c[e] + xa * s[e]);
+            ya.v[e] = from_f32<TO>(v[e] * c[e] - v[V + e] * s[e]);
+            yb.v[e] = from_f32<TO>(v[V + e] * c[e] + v[e] * s[e]);
           }
         }
         *reinterpret_cast<Piece<TO, V>*>(yr + h * os.head + at0) = ya;
-        *reinterpret_cast<Piece<TO, V>*>(yr + h * os.head + at1) = yb;
+        if (turn) *reinterpret_cast<Piece<TO, V>*>(yr + h * os.head + at1) = yb;
       }
     }
   }
@@ -125,10 +115,13 @@ hipError_t launch_v(const RotaryTable& rot, int head_dim, const void* x, RowStri
   const int64_t one = int64_t(n_tok) * pieces;
   const int groups = int(std::min<int64_t>(n_heads, std::max<int64_t>(1, kTargetThreads / one)));
   const int64_t items = one * groups;
-  hipLaunchKernelGGL((rotary_rows<TI, TO, V>), dim3((items + kThreads - 1) / kThreads), dim3(kThreads), 0,
-                     stream, rot, static_cast<const TI*>(x), xs, static_cast<TO*>(out), os, position,
-                     n_heads, groups, pieces, plane_pieces, items, inverse ? -1.f : 1.f);
-  return hipGetLastError();
+  auto go = [&](auto kern) {
+    hipLaunchKernelGGL(kern, dim3((items + kThreads - 1) / kThreads), dim3(kThreads), 0, stream, rot,
+                       static_cast<const TI*>(x), xs, static_cast<TO*>(out), os, position, n_heads, groups,
+                       pieces, plane_pieces, items, inverse ? -1.f : 1.f);
+    return hipGetLastError();
+  };
+  return pieces > plane_pieces ? go(rotary_rows<TI, TO, V, true>) : go(rotary_rows<TI, TO, V, false>);
 }
 
 template <typename TI, typename TO>

@@ -309,6 +309,9 @@ def _append(fn, what: str, k, v, slot, pool, pool_dtype, page: int, rotation, po
                 pool.numel() // page)
 
 
+_dense_page = functools.lru_cache(maxsize=256)(dense_page_elems)
+
+
 def dense_append(k: torch.Tensor, v: torch.Tensor, slot: torch.Tensor, kv_pool: torch.Tensor,
                  rotation: Optional[Rotary] = None, position: Optional[torch.Tensor] = None,
                  stream=None) -> None:
@@ -318,7 +321,7 @@ def dense_append(k: torch.Tensor, v: torch.Tensor, slot: torch.Tensor, kv_pool: 
     if not isinstance(k, torch.Tensor) or k.dim() != 3:
         raise ValueError("k must be [tokens, H_kv, d_h]")
     _append(_lib.dckv_dense_append, "dense_append", k, v, slot, kv_pool, torch.bfloat16,
-            dense_page_elems(k.shape[1], k.shape[2]), rotation, position, stream)
+            _dense_page(k.shape[1], k.shape[2]), rotation, position, stream)
 
 
 @functools.lru_cache(maxsize=256)

@@ -450,6 +450,58 @@ def test_quant_decode_nan_reaches_only_who_sees_it():
     assert np.isnan(got[0, 1]).all() and np.isnan(got[0, 0, 1]).all() and np.isfinite(got[0, 0, 0]).all()
 
 
+def test_quant_decode_graph_follows_the_lengths():
+    # splits cut on the device: replays of one capture with lengths alike, unlike and
+    # empty, in turn, over a workspace overwritten between replays
+    from paper_2607_24331_amd import new_quant_pool, quant_decode, quant_workspace_bytes
+    g = torch.Generator(device="cuda")
+    g.manual_seed(9)
+    B, top, H, d = 3, 12000, 2, 64
+    pages = -(-top // 64)
+    pool = new_quant_pool(B * pages, H, d)
+    cells = pool.view(B * pages, H, 130, 64)
+    cells[:, :, :128] = torch.randn(B * pages, H, 128, 64, generator=g, device="cuda").mul(100).clamp(-448, 448).to(
+        torch.float8_e4m3fn).view(torch.uint8)
+    cells[:, :, 128:] = 120
+    table = torch.randperm(B * pages, generator=g, device="cuda").to(torch.int32).view(B, pages)
+    q, lens = torch.randn(B, 8, d, generator=g, device="cuda"), torch.full((B,), top, dtype=torch.int32, device="cuda")
+    out = torch.empty_like(q)
+    ws = torch.empty(quant_workspace_bytes(8, H, d, 1, 0, B, top), dtype=torch.uint8, device="cuda")
+    step = lambda o, w: quant_decode(q, pool, table, lens, top, H, out=o, workspace=w)  # noqa: E731
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        step(out, ws)
+    torch.cuda.current_stream().wait_stream(s)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(out, ws)
+    eager = torch.empty_like(out)
+    for now in ((top,) * B, (top, 100, 5000), (0, 0, 0), (11000, top, 10500), (1, top, 0), (top,) * B):
+        lens.copy_(torch.tensor(now, dtype=torch.int32))
+        step(eager, torch.empty_like(ws))
+        ws.fill_(0xFF)
+        out.fill_(float("nan"))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager) and not eager.isnan().any(), now
+        for b in range(B):                # the same sequence alone, cut otherwise
+            one = quant_decode(q[b:b + 1], pool, table[b:b + 1], lens[b:b + 1], top, H)
+            # the same products summed in another order: values of about one, 12000
+            # roundings of 2^-24 as a random walk are 7e-6
+            assert (one[0] - eager[b]).abs().max() <= 1e-4, now
+    # two calls at once on two streams, a workspace each
+    lens.copy_(torch.tensor((top, 100, 5000), dtype=torch.int32))
+    step(eager, ws)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    outs = [[quant_decode(q, pool, table, lens, top, H, stream=x) for _ in range(8)] for x in streams]
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, eager) for x in outs for o in x)
+
+
 def test_quant_decode_on_another_stream_and_refusals():
     from paper_2607_24331_amd import DckvError, dense_append, quant_append, quant_decode, quant_read, rotary
     g = np.random.default_rng(6)
