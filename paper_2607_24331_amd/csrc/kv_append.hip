@@ -15,8 +15,8 @@
 //   goes out in 16-byte pieces; other rows (single tokens) go out as bytes.
 // read_rows  the same units the other way.
 // Each element is read once and written once: memory bounds long prompts, latency single
-// tokens.  4,093 tokens of 32 heads of 128: keys 15.9 us, values 16.4, read back 24.7
-// (2 x 50 MB, 101 MB); 64 tokens of 8 heads: 6.4 us and 4.6.
+// tokens.  4,093 tokens of 32 heads of 128: 23.5 us (101 MB, 4.3 TB/s), read back 24.7;
+// 64 tokens of 8 heads: 5.3 us and 4.6.
 #include <algorithm>
 
 #include "rotary.h"
@@ -25,10 +25,13 @@ namespace dckv {
 namespace {
 
 constexpr int kMaxRows = 128;             // tokens a work-group
-// Work-groups that a call aims for.  An append forms angles or finds units once for the
-// heads of a work-group: 4093 x 32 rows take 17.4 us (keys) and 15.5 (values) with 512,
-// 20.7 and 17.3 with 2048.  A read has less to share: 28 us with 512, 23 with 2048.
-constexpr int64_t kAppendGroups = 512;
+// Work-groups that a part of a call aims for.  An append forms angles or finds units once
+// for the heads of a work-group, a read has less to share: 4093 x 32 rows take 29 us (a call)
+// with 1024 for the keys and 512 for the values, 31 with 1024 both, 33 with 512 both and 34
+// with 2048 both; into bf16 pages 27.5 with 512 to 2048; read back 26 with 512 and 24
+// with 2048.
+constexpr int64_t kKeyGroups = 1024;
+constexpr int64_t kValueGroups = 512;
 constexpr int64_t kReadGroups = 2048;
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
@@ -442,33 +445,42 @@ __device__ __forceinline__ void append_by_unit(const AppendBlock<T>& b, const in
   }
 }
 
-// What a launch of append_rows writes.
-enum Part { kBoth, kKeys, kValues };
+// How a launch of append_rows cuts its values: like its keys, or by pages.
+enum Part { kBoth, kPaged };
 
-// Grid (token blocks, head blocks, keys / values of kBoth).  Blocks of `rows` tokens by
-// `hb` heads, rows at most the row groups of a work-group, of kValues Block<D>::kRows;
-// kValues cuts its blocks at pages (one block more: the tokens before the first cut).
+// Blocks of `rows` tokens (at most the row groups of a work-group) by `hb` heads.  kBoth:
+// grid (token blocks, head blocks, keys / values).  kPaged: the values in `value_items`
+// blocks of Block<D>::kRows tokens, cut at pages (one more: the tokens before the first cut),
+// by `vhb` heads, and after them, their work-groups being the shorter, the keys.
 template <typename T, int D, bool QUANT, Part PART>
 __global__ __launch_bounds__(Block<D>::kThreads) void append_rows(
     RotaryTable rot, const T* __restrict__ k, RowStrides ks, const T* __restrict__ v, RowStrides vs,
     bool k_wide, bool v_wide, const int64_t* __restrict__ slot, const int32_t* __restrict__ position,
-    int n_tok, int rows, int hb, int n_heads, void* pool, int64_t n_slots) {
+    int n_tok, int rows, int value_items, int hb, int vhb, int n_heads, void* pool, int64_t n_slots) {
   using B = Block<D>;
-  constexpr bool UNITS = QUANT && PART != kKeys;
-  constexpr int HALVES = B::kRows / 64, TILE = UNITS ? 8 * (2 * D + 4) : 1;
-  __shared__ __align__(16) uint32_t tiles[UNITS ? 2 : 1][HALVES][TILE];
-  __shared__ int64_t slot_s[UNITS ? kMaxRows + 6 : 1];
+  constexpr int HALVES = B::kRows / 64, TILE = QUANT ? 8 * (2 * D + 4) : 1;
+  __shared__ __align__(16) uint32_t tiles[QUANT ? 2 : 1][HALVES][TILE];
+  __shared__ int64_t slot_s[QUANT ? kMaxRows + 6 : 1];
   __shared__ Units un;
-  const bool value = PART == kBoth ? blockIdx.z != 0 : PART == kValues;
-  const int h0 = blockIdx.y * hb;
+  const bool value = PART == kBoth ? blockIdx.z != 0 : int(blockIdx.x) < value_items;
+  int bx = blockIdx.x, by = blockIdx.y;
+  if constexpr (PART == kPaged) {
+    const int blocks = value ? (n_tok + B::kRows - 1) / B::kRows + 1 : (n_tok + rows - 1) / rows;
+    const int i = value ? bx : bx - value_items;
+    by = i / blocks;
+    bx = i - by * blocks;
+    if (value) hb = vhb;
+  }
+  const int h0 = by * hb;
   AppendBlock<T> b{value ? v : k, value ? vs : ks, value ? v_wide : k_wide, value, 0, n_heads, h0,
                    min(n_heads, h0 + hb), static_cast<char*>(pool)};
-  int t0 = blockIdx.x * rows, t1 = min(n_tok, t0 + rows);
-  if constexpr (UNITS) {
+  int t0 = bx * rows, t1 = min(n_tok, t0 + rows);
+  if constexpr (QUANT) {
     if (value) {
-      if constexpr (PART == kValues) {
-        t1 = block_start(slot, n_tok, t0);
-        t0 = blockIdx.x == 0 ? 0 : block_start(slot, n_tok, t0 - rows);
+      if constexpr (PART == kPaged) {
+        const int at = bx * B::kRows;
+        t1 = block_start(slot, n_tok, at);
+        t0 = at == 0 ? 0 : block_start(slot, n_tok, at - B::kRows);
       }
       const T* src = b.src;
       for (; t0 < t1; t0 += B::kRows) {    // twice at most: a cut moves by up to 63 tokens
@@ -482,11 +494,9 @@ __global__ __launch_bounds__(Block<D>::kThreads) void append_rows(
       return;
     }
   }
-  if constexpr (PART != kValues) {
-    b.n = t1 - t0;
-    b.src += t0 * b.st.token;
-    append_by_row<T, D, QUANT>(b, rot, slot + t0, n_slots, position + t0);
-  }
+  b.n = t1 - t0;
+  b.src += t0 * b.st.token;
+  append_by_row<T, D, QUANT>(b, rot, slot + t0, n_slots, position + t0);
 }
 
 // Cached rows as values, in the same blocks and units; grid as append_rows.
@@ -597,25 +607,31 @@ hipError_t launch_append_t(int kv_heads, const void* k, const void* v, RowStride
     const int64_t n = 16 / sizeof(T);
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && s.token % n == 0 && s.head % n == 0;
   };
-  auto go = [&](auto kern, int64_t blocks, int rows, int parts) {
-    const int hb = heads_for(blocks * parts, kv_heads, kAppendGroups);
-    hipLaunchKernelGGL(kern, dim3(uint32_t(blocks), (kv_heads + hb - 1) / hb, parts), dim3(Block<D>::kThreads),
-                       0, stream, rot, static_cast<const T*>(k), ks, static_cast<const T*>(v), vs, wide(k, ks),
-                       wide(v, vs), slot, position, n_tok, rows, hb, kv_heads, pool, num_pages * 64);
+  constexpr int G = Block<D>::kGroups, R = Block<D>::kRows;
+  const int64_t blocks = (n_tok + G - 1) / G;
+  auto go = [&](auto kern, dim3 grid, int64_t value_items, int hb, int vhb) {
+    hipLaunchKernelGGL(kern, grid, dim3(Block<D>::kThreads), 0, stream, rot, static_cast<const T*>(k), ks,
+                       static_cast<const T*>(v), vs, wide(k, ks), wide(v, vs), slot, position, n_tok, G,
+                       int(value_items), hb, vhb, kv_heads, pool, num_pages * 64);
     return hipGetLastError();
   };
-  constexpr int G = Block<D>::kGroups, R = Block<D>::kRows;
-  // Long runs of 8-bit values go out by pages, in a launch of their own: 4093 tokens of
-  // 32 heads took 37 us in two launches and 48 in one, whose registers are those of the
-  // larger part.  Below that a second launch costs what it gives (64 tokens of 8 heads:
-  // 6.4 us in one).
+  // Many 8-bit values go out by pages.  In a graph, back to back, against blocks like the
+  // keys': 4093 tokens of 32 heads 23.5 us and 48, 8192 of 8 heads in five runs 22 and 28, 256
+  // of 32 heads 5.7 and 8.8.  Where no page's run is long it loses (1024 tokens of 8
+  // heads at random 18 and 13.5), and a cut in the middle of a page costs a second pass,
+  // which few rows cannot hide (256 tokens of 16 heads in five runs 8.9 and 6.4).
+  // The values have the longer work-groups: 26.5 us with the keys first; 33 in two launches.
   if constexpr (QUANT) {
     if (n_tok >= 256 && int64_t(n_tok) * kv_heads >= 8192) {
-      hipError_t e = go(append_rows<T, D, QUANT, kKeys>, (n_tok + G - 1) / G, G, 1);
-      return e != hipSuccess ? e : go(append_rows<T, D, QUANT, kValues>, (n_tok + R - 1) / R + 1, R, 1);
+      const int64_t vb = (n_tok + R - 1) / R + 1;
+      const int hb = heads_for(blocks, kv_heads, kKeyGroups), vhb = heads_for(vb, kv_heads, kValueGroups);
+      const int64_t value_items = vb * ((kv_heads + vhb - 1) / vhb);
+      const int64_t items = value_items + blocks * ((kv_heads + hb - 1) / hb);
+      return go(append_rows<T, D, QUANT, kPaged>, dim3(uint32_t(items)), value_items, hb, vhb);
     }
   }
-  return go(append_rows<T, D, QUANT, kBoth>, (n_tok + G - 1) / G, G, 2);
+  const int hb = heads_for(blocks * 2, kv_heads, kValueGroups);
+  return go(append_rows<T, D, QUANT, kBoth>, dim3(uint32_t(blocks), (kv_heads + hb - 1) / hb, 2), 0, hb, hb);
 }
 
 template <typename T, bool QUANT>
