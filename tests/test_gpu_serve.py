@@ -96,6 +96,26 @@ def test_page_map_of_nothing_and_a_wild_count():
         assert t[0, 0] == (2 if left else -1) and m.slot.tolist() == [2 * 64 if left else -1]
 
 
+def test_page_map_of_nothing_keeps_its_stream():
+    # outputs of an earlier call, written last on the stream the call is given
+    from paper_2607_24331_amd import page_map
+    i32 = dict(dtype=torch.int32, device="cuda")
+    none, table, free, count = torch.empty(0, **i32), torch.empty((0, 4), **i32), torch.arange(3, **i32), torch.tensor([3], **i32)
+    m = page_map(none, none, table, free, count, 5)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        big = torch.ones(4096, 4096, device="cuda")
+        for _ in range(20):
+            big = big @ big * 1e-9
+        for t in m:
+            t.fill_(7)
+    page_map(none, none, table, free, count, 5, out=m, stream=s)
+    torch.cuda.synchronize()
+    assert m.slot.tolist() == m.position.tolist() == m.seq_of_row.tolist() == [-1] * 5
+    assert m.row_start.tolist() == [0] and m.free_left.tolist() == [3]
+
+
 @pytest.mark.parametrize("B, width, cap", [(1, 3, 10), (40, 70, 5000), (1030, 5, 3000), (40, 70, 100)])
 def test_page_release(B, width, cap):
     from paper_2607_24331_amd import page_release
