@@ -15,8 +15,8 @@
 //   goes out in 16-byte pieces; other rows (single tokens) go out as bytes.
 // read_rows  the same units the other way.
 // Each element is read once and written once: memory bounds long prompts, latency single
-// tokens.  4,093 tokens of 32 heads of 128: 23.5 us (101 MB, 4.3 TB/s), read back 24.7;
-// 64 tokens of 8 heads: 5.3 us and 4.6.
+// tokens.  4,093 tokens of 32 heads of 128, back to back in a graph: 24 us (101 MB,
+// 4.2 TB/s), read back 22; 64 tokens of 8 heads: 5.3 us and 3.7.
 #include <algorithm>
 
 #include "rotary.h"
@@ -28,8 +28,8 @@ constexpr int kMaxRows = 128;             // tokens a work-group
 // Work-groups that a part of a call aims for.  An append forms angles or finds units once
 // for the heads of a work-group, a read has less to share: 4093 x 32 rows take 29 us (a call)
 // with 1024 for the keys and 512 for the values, 31 with 1024 both, 33 with 512 both and 34
-// with 2048 both; into bf16 pages 27.5 with 512 to 2048; read back 26 with 512 and 24
-// with 2048.
+// with 2048 both; into bf16 pages 27.5 with 512 to 2048; read back 19.8 with 2048 for
+// the keys and 512 for the values, 21.7 with 1024 and 23.8 with 2048 for these.
 constexpr int64_t kKeyGroups = 1024;
 constexpr int64_t kValueGroups = 512;
 constexpr int64_t kReadGroups = 2048;
@@ -158,6 +158,29 @@ __device__ __forceinline__ int block_start(const int64_t* slot, int n_tok, int t
   const int64_t s = slot[t];
   const int u = t + int(-s & 63);
   return s >= 0 && u < n_tok && slot[u] >= 0 && (slot[u] & 63) == 0 ? u : t;
+}
+
+// The values of a call that are cut at pages: `main` work-groups a head block with the first
+// kRows rows of a block each, then `rest` with what a cut leaves of a block past those, of
+// kRest blocks one after another.
+constexpr int kRest = 4;
+struct PagedSpans {
+  int main, rest;
+  __host__ __device__ PagedSpans(int n_tok, int rows) : main((n_tok + rows - 1) / rows + 1), rest((main + kRest - 1) / kRest) {}
+};
+template <int ROWS, typename F>
+__device__ __forceinline__ void paged_spans(const PagedSpans& ps, int bx, const int64_t* slot, int n_tok, const F& f) {
+  const bool rest = bx >= ps.main;
+  const int first = rest ? kRest * (bx - ps.main) : bx, last = rest ? min(ps.main, first + kRest) : bx + 1;
+  int t0 = first == 0 ? 0 : block_start(slot, n_tok, (first - 1) * ROWS);
+  for (int b = first; b < last; ++b) {
+    const int t1 = block_start(slot, n_tok, b * ROWS);
+    if (!rest)
+      f(t0, min(t1, t0 + ROWS));
+    else if (t0 + ROWS < t1)
+      f(t0 + ROWS, t1);
+    t0 = t1;
+  }
 }
 
 // Work units of the block's values.  Four consecutive rows in slots 4a .. 4a + 3 of
@@ -450,8 +473,7 @@ enum Part { kBoth, kPaged };
 
 // Blocks of `rows` tokens (at most the row groups of a work-group) by `hb` heads.  kBoth:
 // grid (token blocks, head blocks, keys / values).  kPaged: the values in `value_items`
-// blocks of Block<D>::kRows tokens, cut at pages (one more: the tokens before the first cut),
-// by `vhb` heads, and after them, their work-groups being the shorter, the keys.
+// work-groups of PagedSpans by `vhb` heads, then the keys.
 template <typename T, int D, bool QUANT, Part PART>
 __global__ __launch_bounds__(Block<D>::kThreads) void append_rows(
     RotaryTable rot, const T* __restrict__ k, RowStrides ks, const T* __restrict__ v, RowStrides vs,
@@ -465,7 +487,8 @@ __global__ __launch_bounds__(Block<D>::kThreads) void append_rows(
   const bool value = PART == kBoth ? blockIdx.z != 0 : int(blockIdx.x) < value_items;
   int bx = blockIdx.x, by = blockIdx.y;
   if constexpr (PART == kPaged) {
-    const int blocks = value ? (n_tok + B::kRows - 1) / B::kRows + 1 : (n_tok + rows - 1) / rows;
+    const PagedSpans ps(n_tok, B::kRows);
+    const int blocks = value ? ps.main + ps.rest : (n_tok + rows - 1) / rows;
     const int i = value ? bx : bx - value_items;
     by = i / blocks;
     bx = i - by * blocks;
@@ -477,20 +500,19 @@ __global__ __launch_bounds__(Block<D>::kThreads) void append_rows(
   int t0 = bx * rows, t1 = min(n_tok, t0 + rows);
   if constexpr (QUANT) {
     if (value) {
-      if constexpr (PART == kPaged) {
-        const int at = bx * B::kRows;
-        t1 = block_start(slot, n_tok, at);
-        t0 = at == 0 ? 0 : block_start(slot, n_tok, at - B::kRows);
-      }
-      const T* src = b.src;
-      for (; t0 < t1; t0 += B::kRows) {    // twice at most: a cut moves by up to 63 tokens
-        b.n = min(B::kRows, t1 - t0);
-        b.src = src + t0 * b.st.token;
-        load_slots(slot, n_tok, n_slots, t0, b.n, slot_s);
+      auto span = [&](int r0, int r1) {
+        AppendBlock<T> sb = b;
+        sb.n = r1 - r0;
+        sb.src += r0 * b.st.token;
+        load_slots(slot, n_tok, n_slots, r0, sb.n, slot_s);
         __syncthreads();
-        append_by_unit<T, D, HALVES, TILE>(b, slot_s, un, tiles);
+        append_by_unit<T, D, HALVES, TILE>(sb, slot_s, un, tiles);
         __syncthreads();                   // LDS is written again
-      }
+      };
+      if constexpr (PART == kPaged)
+        paged_spans<B::kRows>(PagedSpans(n_tok, B::kRows), bx, slot, n_tok, span);
+      else
+        span(t0, t1);
       return;
     }
   }
@@ -499,97 +521,190 @@ __global__ __launch_bounds__(Block<D>::kThreads) void append_rows(
   append_by_row<T, D, QUANT>(b, rot, slot + t0, n_slots, position + t0);
 }
 
-// Cached rows as values, in the same blocks and units; grid as append_rows.
+// Writes columns j0 .. j0 + 7 of a cached row, in T, at `at`.
+template <typename T>
+__device__ __forceinline__ void store_row8(T* at, uint32_t lo, uint32_t hi, float scale) {
+  constexpr int N = 16 / sizeof(T);
+  const uint32_t w[2] = {lo, hi};
+  float x[8];
+#pragma unroll
+  for (int p = 0; p < 2; ++p) {
+    x[4 * p] = __builtin_amdgcn_cvt_f32_fp8(int(w[p]), 0) * scale;
+    x[4 * p + 1] = __builtin_amdgcn_cvt_f32_fp8(int(w[p]), 1) * scale;
+    x[4 * p + 2] = __builtin_amdgcn_cvt_f32_fp8(int(w[p]), 2) * scale;
+    x[4 * p + 3] = __builtin_amdgcn_cvt_f32_fp8(int(w[p]), 3) * scale;
+  }
+#pragma unroll
+  for (int p = 0; p < 8 / N; ++p) {
+    Piece<T, N> a;
+#pragma unroll
+    for (int e = 0; e < N; ++e) a.v[e] = from_f32<T>(x[p * N + e]);
+    *reinterpret_cast<Piece<T, N>*>(at + p * N) = a;
+  }
+}
+__device__ __forceinline__ float scale_of(uint32_t byte) { return ldexpf(1.f, int(byte & 255u) - 127); }
+
+// What a work-group of read_rows works on.
+template <typename T>
+struct ReadBlock {
+  const uint8_t* pool;
+  T* out;                                  // of the block's first token
+  int n, n_heads, h0, h1;
+};
+
+// Keys: a group of lanes has four rows on their way.
 template <typename T, int D>
-__global__ __launch_bounds__(Block<D>::kThreads) void read_rows(const uint8_t* __restrict__ pool, int64_t n_slots,
-                                                      const int64_t* __restrict__ slot, int n_tok, int rows,
-                                                      int hb, int n_heads, T* __restrict__ k,
-                                                      T* __restrict__ v) {
+__device__ __forceinline__ void read_keys(const ReadBlock<T>& b, const int64_t* slot_s) {
   constexpr int L = Block<D>::kLanes, GROUPS = Block<D>::kGroups;
-  __shared__ int64_t slot_s[kMaxRows + 6];
-  __shared__ Units un;
-  const int tid = threadIdx.x;
-  const int t0 = blockIdx.x * rows;
-  const bool value = blockIdx.z != 0;
-  const int n = min(rows, n_tok - t0);
-  const int grp = tid / L, j0 = 8 * (tid % L);
-  load_slots(slot, n_tok, n_slots, t0, n, slot_s);
-  __syncthreads();
-  const int units = value ? make_units<GROUPS>(slot_s, n, un) : (n + 3) / 4;
-  const int64_t page = int64_t(n_heads) * 128 * (D + 1);
-  const int h1 = min(n_heads, int(blockIdx.y + 1) * hb);
-  T* out = value ? v : k;
-  auto store = [&](int r, int h, const uint32_t (&w)[2], float scale) {
-    constexpr int N = 16 / sizeof(T);
-    T* at = out + (int64_t(t0 + r) * n_heads + h) * D + j0;
-    float x[8];
-#pragma unroll
-    for (int p = 0; p < 2; ++p) {
-      x[4 * p] = __builtin_amdgcn_cvt_f32_fp8(int(w[p]), 0) * scale;
-      x[4 * p + 1] = __builtin_amdgcn_cvt_f32_fp8(int(w[p]), 1) * scale;
-      x[4 * p + 2] = __builtin_amdgcn_cvt_f32_fp8(int(w[p]), 2) * scale;
-      x[4 * p + 3] = __builtin_amdgcn_cvt_f32_fp8(int(w[p]), 3) * scale;
-    }
-#pragma unroll
-    for (int p = 0; p < 8 / N; ++p) {
-      Piece<T, N> a;
-#pragma unroll
-      for (int e = 0; e < N; ++e) a.v[e] = from_f32<T>(x[p * N + e]);
-      *reinterpret_cast<Piece<T, N>*>(at + p * N) = a;
-    }
-  };
-  for (int h = blockIdx.y * hb; h < h1; ++h) {
-    if (value) {
-      // rows outside the pool make no unit: zeros
-      const uint32_t none[2] = {0u, 0u};
-      for (int r = grp; r < n; r += GROUPS)
-        if (slot_s[r + 3] < 0) store(r, h, none, 0.f);
-    }
-    for (int u = grp; u < units; u += GROUPS) {
-      uint32_t w[4][2];
-      float scale[4];
-      int r0 = 4 * u, nr = min(4, n - 4 * u);
-      if (value) {
-        r0 = un.unit[u] >> 2;
-        nr = un.unit[u] & 1 ? 4 : 1;
-      }
+  const int grp = threadIdx.x / L, j0 = 8 * (threadIdx.x % L);
+  const int64_t page = int64_t(b.n_heads) * 128 * (D + 1);
+  for (int h = b.h0; h < b.h1; ++h) {
+    for (int r0 = 4 * grp; r0 < b.n; r0 += 4 * GROUPS) {
+      u32x2 w[4];
+      uint32_t e2[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        w[i][0] = w[i][1] = 0u;
-        scale[i] = 0.f;
-        const int64_t sl = i < nr ? slot_s[r0 + i + 3] : -1;
+        const int64_t sl = r0 + i < b.n ? slot_s[r0 + i + 3] : -1;
+        w[i] = u32x2{0u, 0u};
+        e2[i] = 0u;
         if (sl < 0) continue;
-        const uint8_t* blk = pool + (sl >> 6) * page + int64_t(h) * 128 * (D + 1);
-        const int s = int(sl & 63);
-        scale[i] = ldexpf(1.f, int(blk[scale_at<D>(s, value)]) - 127);
-        if (!value) {
-          const u32x2 a = *reinterpret_cast<const u32x2*>(blk + key_at<D>(s, j0));
-          w[i][0] = a[0];
-          w[i][1] = a[1];
-        } else if (nr == 1) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) w[i][e / 4] |= uint32_t(blk[value_at<D>(s, j0 + e)]) << (8 * (e % 4));
-        }
+        const uint8_t* blk = b.pool + (sl >> 6) * page + int64_t(h) * 128 * (D + 1);
+        w[i] = *reinterpret_cast<const u32x2*>(blk + key_at<D>(int(sl & 63), j0));
+        e2[i] = blk[scale_at<D>(int(sl & 63), false)];
       }
-      if (value && nr == 4) {
-        const int64_t sl = slot_s[r0 + 3];
-        const uint8_t* blk = pool + (sl >> 6) * page + int64_t(h) * 128 * (D + 1);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (r0 + i < b.n)
+          store_row8(b.out + (int64_t(r0 + i) * b.n_heads + h) * D + j0, w[i][0], w[i][1], scale_of(e2[i]));
+    }
+  }
+}
+
+// Values, by the units of an append: the pieces of the next head's tile are on their way
+// while this head's quads go out.
+template <typename T, int D, int HALVES, int TILE>
+__device__ __forceinline__ void read_values(const ReadBlock<T>& b, const int64_t* slot_s, Units& un,
+                                            uint32_t (*tiles)[HALVES][TILE]) {
+  constexpr int L = Block<D>::kLanes, GROUPS = Block<D>::kGroups, THREADS = Block<D>::kThreads;
+  constexpr bool TILED = TILE > 1;         // else every unit by itself
+  const int units = make_units<GROUPS>(slot_s, b.n, un);
+  const int tid = threadIdx.x, grp = tid / L, j0 = 8 * (tid % L);
+  const int64_t page = int64_t(b.n_heads) * 128 * (D + 1);
+  auto at = [&](int r, int h) { return b.out + (int64_t(r) * b.n_heads + h) * D + j0; };
+  for (int r = grp; r < b.n; r += GROUPS)  // rows outside the pool make no unit: zeros
+    if (slot_s[r + 3] < 0)
+      for (int h = b.h0; h < b.h1; ++h) store_row8(at(r, h), 0u, 0u, 0.f);
+  constexpr int PIECES = HALVES * 4 * D / THREADS;
+  u32x4 next[PIECES];
+  auto fetch = [&](int h) {
+    const uint8_t* head = b.pool + int64_t(h) * 128 * (D + 1);
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+      const int g = tid + i * THREADS, hf = g / (4 * D), p = g % (4 * D);
+      const int j = 16 * (p >> 6) + (p & 15), q = (p >> 4) & 3;
+      const unsigned long long* t4 = &un.tile[hf][4 * q];
+      const unsigned long long pg = t4[0] >> 6;
+      const int off = value_at<D>(4 * q, j);
+      if (t4[3] != kNobody && t4[1] >> 6 == pg && t4[2] >> 6 == pg && t4[3] >> 6 == pg) {
+        next[i] = *reinterpret_cast<const u32x4*>(head + int64_t(pg) * page + off);
+      } else {
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+          next[i][m] = t4[m] == kNobody ? 0u : *reinterpret_cast<const uint32_t*>(head + int64_t(t4[m] >> 6) * page + off + 4 * m);
+      }
+    }
+  };
+  const bool tiled = TILED && un.tiled;
+  if (tiled) fetch(b.h0);
+  for (int u0 = 0; u0 < units; u0 += GROUPS) {   // once where the rows are consecutive slots
+    const int u = u0 + grp;
+    const int code = u < units ? un.unit[u] : 0;
+    const bool live = u < units, four = live && (code & 1);
+    const int r0 = code >> 2;
+    const int64_t sl = live ? slot_s[r0 + 3] : 0;
+    const int s = int(sl & 63), half = r0 >> 6, place = tile_place(sl);
+    const bool mine = TILED && four && u0 == 0 && un.tile[half][place] == (unsigned long long)sl;
+    for (int h = b.h0; h < b.h1; ++h) {
+      const uint8_t* blk = b.pool + (sl >> 6) * page + int64_t(h) * 128 * (D + 1);
+      uint32_t e2 = 0u;
+      if (four)
+        e2 = *reinterpret_cast<const uint32_t*>(blk + scale_at<D>(s, true));
+      else if (live)
+        e2 = blk[scale_at<D>(s, true)];
+      auto& tile = tiles[(h - b.h0) & 1];
+      if (u0 == 0 && tiled) {
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+          const int g = tid + i * THREADS, hf = g / (4 * D), p = g % (4 * D);
+          *reinterpret_cast<u32x4*>(&tile[hf][tile_at<D>(16 * (p >> 6) + (p & 15), 4 * (p >> 4 & 3))]) = next[i];
+        }
+        if (h + 1 < b.h1) fetch(h + 1);
+        __syncthreads();
+      }
+      if (four) {
+        uint32_t w[4][2];
 #pragma unroll
         for (int p = 0; p < 2; ++p) {
           uint32_t col[4], row[4];
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            col[e] = *reinterpret_cast<const uint32_t*>(blk + value_at<D>(int(sl & 63), j0 + 4 * p + e));
+          for (int e = 0; e < 4; ++e) {
+            const int j = j0 + 4 * p + e;
+            col[e] = mine ? tile[half][tile_at<D>(j, place)]
+                          : *reinterpret_cast<const uint32_t*>(blk + value_at<D>(s, j));
+          }
           transpose4(col[0], col[1], col[2], col[3], row);
 #pragma unroll
           for (int i = 0; i < 4; ++i) w[i][p] = row[i];
         }
-      }
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (i < nr) store(r0 + i, h, w[i], scale[i]);
+        for (int i = 0; i < 4; ++i) store_row8(at(r0 + i, h), w[i][0], w[i][1], scale_of(e2 >> (8 * i)));
+      } else if (live) {
+        uint32_t w[2] = {0u, 0u};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e / 4] |= uint32_t(blk[value_at<D>(s, j0 + e)]) << (8 * (e % 4));
+        store_row8(at(r0, h), w[0], w[1], scale_of(e2));
+      }
     }
   }
+}
+
+// Cached rows as values, in blocks as append_rows has them.
+template <typename T, int D, Part PART>
+__global__ __launch_bounds__(Block<D>::kThreads) void read_rows(const uint8_t* __restrict__ pool, int64_t n_slots,
+                                                      const int64_t* __restrict__ slot, int n_tok, int rows,
+                                                      int value_items, int hb, int vhb, int n_heads,
+                                                      T* __restrict__ k, T* __restrict__ v) {
+  using B = Block<D>;
+  constexpr int HALVES = B::kRows / 64, TILE = PART == kPaged ? 8 * (2 * D + 4) : 1;
+  __shared__ __align__(16) uint32_t tiles[2][HALVES][TILE];
+  __shared__ int64_t slot_s[kMaxRows + 6];
+  __shared__ Units un;
+  const bool value = PART == kBoth ? blockIdx.z != 0 : int(blockIdx.x) < value_items;
+  int bx = blockIdx.x, by = blockIdx.y;
+  const PagedSpans ps(n_tok, B::kRows);
+  if constexpr (PART == kPaged) {
+    const int blocks = value ? ps.main + ps.rest : (n_tok + rows - 1) / rows;
+    const int i = value ? bx : bx - value_items;
+    by = i / blocks;
+    bx = i - by * blocks;
+    if (value) hb = vhb;
+  }
+  const int h0 = by * hb;
+  auto span = [&](int r0, int r1) {
+    const ReadBlock<T> b{pool, (value ? v : k) + int64_t(r0) * n_heads * D, r1 - r0, n_heads, h0,
+                         min(n_heads, h0 + hb)};
+    load_slots(slot, n_tok, n_slots, r0, b.n, slot_s);
+    __syncthreads();
+    if (value)
+      read_values<T, D, HALVES, TILE>(b, slot_s, un, tiles);
+    else
+      read_keys<T, D>(b, slot_s);
+    __syncthreads();                       // LDS is written again
+  };
+  if (PART == kPaged && value)
+    paged_spans<B::kRows>(ps, bx, slot, n_tok, span);
+  else
+    span(bx * rows, min(n_tok, bx * rows + rows));
 }
 
 // Heads a work-group: several while `target` work-groups are left.
@@ -598,6 +713,15 @@ int heads_for(int64_t blocks, int n_heads, int64_t target) {
   while (hb > 1 && blocks * ((n_heads + hb - 1) / hb) < target) hb /= 2;
   return hb;
 }
+
+// Whether the 8-bit values of a call are cut at pages, in the launch's first work-groups
+// (they are the longer ones).  Appends in a graph, back to back, against blocks like the
+// keys': 4093 tokens of 32 heads 24.2 us and 48 (26.5 with the keys first, 33 in two launches),
+// 8192 of 8 heads in five runs 17 and 28, 256 of 32 heads 5.8 and 8.8.  Where no page's run is
+// long it loses (1024 tokens of 8 heads at random 18 and 13.5), and so do few rows, which
+// cannot hide what a cut leaves over (256 tokens of 16 heads in five runs 8.1 and 6.4).  Reads
+// of the same: 22 and 36, 16 and 21, 5.7 and 5.3, 12 and 7.
+bool by_pages(int n_tok, int kv_heads) { return n_tok >= 256 && int64_t(n_tok) * kv_heads >= 8192; }
 
 template <typename T, int D, bool QUANT>
 hipError_t launch_append_t(int kv_heads, const void* k, const void* v, RowStrides ks, RowStrides vs,
@@ -615,17 +739,11 @@ hipError_t launch_append_t(int kv_heads, const void* k, const void* v, RowStride
                        int(value_items), hb, vhb, kv_heads, pool, num_pages * 64);
     return hipGetLastError();
   };
-  // Many 8-bit values go out by pages.  In a graph, back to back, against blocks like the
-  // keys': 4093 tokens of 32 heads 23.5 us and 48, 8192 of 8 heads in five runs 22 and 28, 256
-  // of 32 heads 5.7 and 8.8.  Where no page's run is long it loses (1024 tokens of 8
-  // heads at random 18 and 13.5), and a cut in the middle of a page costs a second pass,
-  // which few rows cannot hide (256 tokens of 16 heads in five runs 8.9 and 6.4).
-  // The values have the longer work-groups: 26.5 us with the keys first; 33 in two launches.
   if constexpr (QUANT) {
-    if (n_tok >= 256 && int64_t(n_tok) * kv_heads >= 8192) {
-      const int64_t vb = (n_tok + R - 1) / R + 1;
-      const int hb = heads_for(blocks, kv_heads, kKeyGroups), vhb = heads_for(vb, kv_heads, kValueGroups);
-      const int64_t value_items = vb * ((kv_heads + vhb - 1) / vhb);
+    if (by_pages(n_tok, kv_heads)) {
+      const PagedSpans ps(n_tok, R);
+      const int hb = heads_for(blocks, kv_heads, kKeyGroups), vhb = heads_for(ps.main, kv_heads, kValueGroups);
+      const int64_t value_items = int64_t(ps.main + ps.rest) * ((kv_heads + vhb - 1) / vhb);
       const int64_t items = value_items + blocks * ((kv_heads + hb - 1) / hb);
       return go(append_rows<T, D, QUANT, kPaged>, dim3(uint32_t(items)), value_items, hb, vhb);
     }
@@ -649,14 +767,25 @@ hipError_t launch_append_d(int kv_heads, int head_dim, const void* k, const void
 template <typename T, int D>
 hipError_t launch_read_t(int kv_heads, const void* pool, int64_t num_pages, const int64_t* slot,
                          int n_tok, void* k, void* v, hipStream_t stream) {
-  constexpr int R = Block<D>::kRows;
-  const int rows = n_tok >= 256 ? R : 8;
+  auto go = [&](auto kern, dim3 grid, int rows, int64_t value_items, int hb, int vhb) {
+    hipLaunchKernelGGL(kern, grid, dim3(Block<D>::kThreads), 0, stream, static_cast<const uint8_t*>(pool),
+                       num_pages * 64, slot, n_tok, rows, int(value_items), hb, vhb, kv_heads, static_cast<T*>(k),
+                       static_cast<T*>(v));
+    return hipGetLastError();
+  };
+  if (by_pages(n_tok, kv_heads)) {
+    const int R = Block<D>::kRows;
+    const PagedSpans ps(n_tok, R);
+    const int64_t blocks = (n_tok + R - 1) / R;
+    const int hb = heads_for(blocks, kv_heads, kReadGroups), vhb = heads_for(ps.main, kv_heads, kValueGroups);
+    const int64_t value_items = int64_t(ps.main + ps.rest) * ((kv_heads + vhb - 1) / vhb);
+    const int64_t items = value_items + blocks * ((kv_heads + hb - 1) / hb);
+    return go(read_rows<T, D, kPaged>, dim3(uint32_t(items)), R, value_items, hb, vhb);
+  }
+  const int rows = 8;
   const int64_t blocks = (n_tok + rows - 1) / rows;
   const int hb = heads_for(2 * blocks, kv_heads, kReadGroups);
-  hipLaunchKernelGGL((read_rows<T, D>), dim3(uint32_t(blocks), (kv_heads + hb - 1) / hb, 2),
-                     dim3(Block<D>::kThreads), 0, stream, static_cast<const uint8_t*>(pool), num_pages * 64, slot,
-                     n_tok, rows, hb, kv_heads, static_cast<T*>(k), static_cast<T*>(v));
-  return hipGetLastError();
+  return go(read_rows<T, D, kBoth>, dim3(uint32_t(blocks), (kv_heads + hb - 1) / hb, 2), rows, 0, hb, hb);
 }
 
 }  // namespace

@@ -276,6 +276,44 @@ def test_quant_append_bytes(n, H, d, run, dtype):
             assert np.array_equal(host(got), val, equal_nan=True)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n, H, d", [(1100, 8, 64), (1031, 8, 128), (600, 16, 256), (4200, 2, 128), (8192, 1, 64)])
+@pytest.mark.parametrize("first", [0, 4, 37])
+def test_quant_append_of_runs_in_one_call(n, H, d, dtype, first):
+    # sequences that begin and end inside pages, of one to some 200 tokens, alone or
+    # between rows without a slot: one call and calls of 200 rows write the same bytes
+    # and read the same values
+    from paper_2607_24331_amd import new_quant_pool, quant_append, quant_read
+    g = np.random.default_rng(n + first)
+    slot = np.full(n, -1, np.int64)
+    pages = g.permutation(3 * n // 64 + n // 4 + 8)
+    at = used = 0
+    while at < n:
+        off = first if at == 0 else int(g.choice([0, 0, 4, int(g.integers(0, 64))]))
+        want = int(g.choice([1, 2, 4, 63, 64, 65, 120, 128, 129, 191, int(g.integers(1, 220))]))
+        for i in range(min(want, n - at)):
+            slot[at + i] = pages[used + (off + i) // 64] * 64 + (off + i) % 64
+        used += (off + want - 1) // 64 + 1
+        at += want + int(g.choice([0, 0, 0, 1, 3]))
+    assert used <= len(pages) and len(set(slot[slot >= 0])) == (slot >= 0).sum()
+    kv = cu(g.standard_normal((n, 2, H, d)).astype(np.float32), dtype)
+    ts = cu(slot)
+    pool, part = (new_quant_pool(len(pages), H, d).fill_(201) for _ in range(2))
+    quant_append(kv[:, 0], kv[:, 1], ts, pool)
+    for i in range(0, n, 200):
+        quant_append(kv[i:i + 200, 0], kv[i:i + 200, 1], ts[i:i + 200], part)
+    assert torch.equal(pool, part)
+    k, v = quant_read(pool, ts, H, d, dtype)
+    for i in range(0, n, 200):
+        a, b = quant_read(pool, ts[i:i + 200], H, d, dtype)
+        assert torch.equal(k[i:i + 200], a) and torch.equal(v[i:i + 200], b)
+    some = np.flatnonzero(np.arange(n) % 17 == 5)
+    live = slot[some] >= 0
+    for got, src in ((k, kv[:, 0]), (v, kv[:, 1])):
+        b, e = sv.quantize(host(src[torch.from_numpy(some).cuda()]))
+        assert np.array_equal(host(got)[some], np.where(live[:, None, None], sv.E4M3[b] * 2.0 ** e[..., None], 0))
+
+
 @pytest.mark.parametrize("rot", range(len(ROTS)))
 @pytest.mark.parametrize("n, H, d, run", [(1, 1, 64, 1), (70, 3, 128, 33), (40, 2, 256, 40)])
 def test_appends_turn_keys(n, H, d, run, rot):
