@@ -122,7 +122,7 @@ def page_map(cached: torch.Tensor, added: torch.Tensor, page_table: torch.Tensor
     if out is None:
         slot = _new((rows,), torch.int64, cached.device, stream)
         block = _new((3 * B + 2 + 2 * rows,), i32, cached.device, stream)
-        lens, start, pos, seq, status, left = block.split((B, B + 1, rows, rows, B, 1))
+        lens, start, pos, seq, status, left = block.split_with_sizes((B, B + 1, rows, rows, B, 1))
         out = PageMap(lens, start, slot, pos, seq, status, left)
         at = block.data_ptr()
         p_lens, p_start, p_pos = at, at + 4 * B, at + 4 * (2 * B + 1)
