@@ -441,7 +441,7 @@ typedef struct dckv_rotary_desc {
   double factor;            /* s, finite, at least 1; read by every scaling but UNSCALED */
   double original_context;  /* L, finite, above 0; read by TURNS and PLANES */
   double low, high;         /* finite, 0 < low < high; read by TURNS and PLANES */
-  double magnitude;         /* m, finite; 0 means 1 */
+  double magnitude;         /* m, finite in fp32; 0 means 1 */
 } dckv_rotary_desc;
 typedef struct dckv_rotary dckv_rotary; /* opaque, host memory only */
 
@@ -526,7 +526,7 @@ int dckv_quant_append(int32_t num_kv_heads, int32_t head_dim, const void* k, con
 /* Cached keys and values of given slots (prefix reuse, moving a sequence to
  * another cache): k, v device [n_tok, H_kv, d_h] of `dtype` (both hold the
  * values exactly), 16-byte aligned; a slot outside the pool gives zeros.  At most 2^34
- * values a call. */
+ * elements of each. */
 int dckv_quant_read(int32_t num_kv_heads, int32_t head_dim, const void* pool, int64_t num_pages,
                     const int64_t* slot, int32_t n_tok, void* k, void* v, int32_t dtype,
                     void* stream);

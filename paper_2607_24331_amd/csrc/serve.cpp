@@ -3,6 +3,7 @@
 #include <hip/hip_runtime_api.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <new>
 
@@ -17,6 +18,7 @@ namespace {
 constexpr double kPi = 3.14159265358979323846;
 constexpr int64_t kMaxGroups = (int64_t(1) << 24) - 1;   // work-groups of 256 threads in a grid
 constexpr int32_t kMaxTokens = 1 << 23;                  // tokens a call: a thread a coordinate fits a grid
+constexpr int64_t kMaxRead = int64_t(1) << 34;     // keys (and values) a call: its work-groups fit a grid
 constexpr int64_t kMaxStride = int64_t(1) << 38;   // elements: offsets stay within int64
 
 bool positive(double x) { return std::isfinite(x) && x > 0.0; }
@@ -164,7 +166,8 @@ int dckv_rotary_create(const dckv_rotary_desc* d, dckv_rotary** out) {
     return fail(DCKV_EINVAL, "rotary_create: scaling %d", d->scaling);
   if (!std::isfinite(d->base) || !(d->base > 1.0))
     return fail(DCKV_EINVAL, "rotary_create: base %g is not a finite number above 1", d->base);
-  if (!std::isfinite(d->magnitude)) return fail(DCKV_EINVAL, "rotary_create: magnitude %g", d->magnitude);
+  if (!(std::fabs(d->magnitude) <= FLT_MAX))
+    return fail(DCKV_EINVAL, "rotary_create: magnitude %g is not a finite fp32 number", d->magnitude);
   const double s = d->scaling == DCKV_ROTARY_UNSCALED ? 1.0 : d->factor;
   if (!std::isfinite(s) || !(s >= 1.0))
     return fail(DCKV_EINVAL, "rotary_create: factor %g is not a finite number of at least 1", s);
@@ -290,7 +293,7 @@ int dckv_quant_read(int32_t num_kv_heads, int32_t head_dim, const void* pool, in
   int st = check_kv("quant_read", num_kv_heads, head_dim);
   if (st == DCKV_OK) st = check_dtype("quant_read", "k and v", dtype);
   if (st != DCKV_OK) return st;
-  if (n_tok < 0 || int64_t(n_tok) * num_kv_heads * head_dim > kMaxGroups * 256 * 8)
+  if (n_tok < 0 || int64_t(n_tok) * num_kv_heads * head_dim > kMaxRead)
     return fail(DCKV_EINVAL, "quant_read: n_tok %d is negative or too large", n_tok);
   if (n_tok == 0) return DCKV_OK;
   if (!pool || !slot || !k || !v) return fail(DCKV_EINVAL, "quant_read: null device pointer");

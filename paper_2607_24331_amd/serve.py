@@ -13,6 +13,7 @@ import torch
 from . import capi
 from .dckv import _check, _lib, dense_page_elems
 
+_INT32_MAX = 2 ** 31 - 1
 _CODE = {torch.float32: capi.DCKV_F32, torch.bfloat16: capi.DCKV_BF16}
 _LAYOUTS = {"half": 0, "interleaved": 1}
 _SCALINGS = {"none": 0, "linear": 1, "base": 2, "turns": 3, "planes": 4}
@@ -76,6 +77,13 @@ def _launch(fn, what: str, index: int, stream, *args) -> None:
         _check(status, what)
 
 
+def _context(max_context) -> int:
+    top = int(max_context)
+    if not 0 <= top <= _INT32_MAX:             # ctypes would take the low 32 bits
+        raise ValueError(f"max_context {top} is outside 0 .. 2^31 - 1")
+    return top
+
+
 def _new(shape, dtype, device, stream) -> torch.Tensor:
     """Uninitialised memory that belongs to the stream the call runs on."""
     if stream is None:
@@ -108,8 +116,8 @@ def page_map(cached: torch.Tensor, added: torch.Tensor, page_table: torch.Tensor
     if not isinstance(cached, torch.Tensor) or cached.dim() != 1:
         raise ValueError("cached must be a vector")
     B, rows, dev, i32 = cached.shape[0], int(rows), cached.get_device(), torch.int32
-    if rows < 0:
-        raise ValueError("rows must not be negative")
+    if not 0 <= rows <= _INT32_MAX:            # ctypes would take the low 32 bits
+        raise ValueError("rows must be in 0 .. 2^31 - 1")
     pc = _vector(cached, "cached", i32, B)
     pa = _vector(added, "added", i32, B, dev)
     pt = _gpu(page_table, "page_table", i32, dev)
@@ -255,7 +263,7 @@ def decode_rotary(plan, q: torch.Tensor, pool: torch.Tensor, page_table: torch.T
                   workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """decode_rope() over the latent cache with any rotation of the plan's
     head_dim."""
-    B, f32 = q.shape[0], torch.float32
+    B, f32, max_context = q.shape[0], torch.float32, _context(max_context)
     shape = (B, plan.num_q_heads, plan.head_dim)
     dev, dt = q.get_device(), plan.torch_dtype
     pq = _gpu(q, "q", f32)
@@ -283,7 +291,7 @@ def decode_rotary(plan, q: torch.Tensor, pool: torch.Tensor, page_table: torch.T
         workspace = _new((max(plan.rope_workspace_bytes(B, max_context), 256),), torch.uint8, q.device, stream)
     pw = _gpu(workspace, "workspace", torch.uint8, dev)
     _launch(_lib.dckv_decode_rotary, "decode_rotary", dev, stream, plan.handle, pq, B, pp,
-            pool.numel() // plan.page_elems, pt, page_table.shape[1], ps, int(max_context), pk, pv,
+            pool.numel() // plan.page_elems, pt, page_table.shape[1], ps, max_context, pk, pv,
             rotation.handle, po, pw, workspace.numel())
     return out
 
@@ -395,7 +403,7 @@ def quant_decode(q: torch.Tensor, pool: torch.Tensor, page_table: torch.Tensor, 
         (B, Hq, d), Q = q.shape, 1
     else:
         raise ValueError("q must be [batch, Q, H_q, d_h] or [batch, H_q, d_h]")
-    dev, top = q.get_device(), int(max_context)
+    dev, top = q.get_device(), _context(max_context)
     pp = _gpu(pool, "pool", torch.uint8, dev)
     page = quant_page_bytes(num_kv_heads, d)
     if pool.numel() % page:

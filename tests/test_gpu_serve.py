@@ -560,6 +560,15 @@ def test_quant_decode_graph_follows_the_lengths():
     assert all(torch.equal(o, eager) for x in outs for o in x)
 
 
+def test_contexts_fit_32_bits():
+    from paper_2607_24331_amd import new_quant_pool, quant_decode
+    pool, table = new_quant_pool(1, 1, 64), torch.zeros((1, 1), dtype=torch.int32, device="cuda")
+    q, lens = torch.randn(1, 1, 64, device="cuda"), torch.ones(1, dtype=torch.int32, device="cuda")
+    for top in (-1, 2 ** 31, 2 ** 32 + 64):
+        with pytest.raises(ValueError, match="max_context"):
+            quant_decode(q, pool, table, lens, top, 1)
+
+
 def test_quant_decode_on_another_stream_and_refusals():
     from paper_2607_24331_amd import DckvError, dense_append, quant_append, quant_decode, quant_read, rotary
     g = np.random.default_rng(6)

@@ -60,6 +60,30 @@ def test_rotary_create_rejects(lib, kw):
     assert lib.dckv_last_error().decode().startswith("rotary_create:")
 
 
+@pytest.mark.parametrize("m", [3.5e38, -1e300, math.nan, -math.inf])
+def test_rotary_magnitude_is_an_fp32_number(lib, m):
+    st, out = _rotary(lib, magnitude=m)
+    assert st == E and out.value is None and "magnitude" in lib.dckv_last_error().decode()
+    for m in (3.4e38, -1.0, 1e-50):
+        st, out = _rotary(lib, magnitude=m)
+        assert st == capi.DCKV_OK
+        lib.dckv_rotary_destroy(out)
+
+
+@fake
+def test_read_of_too_many_elements(lib):
+    base = dict(H=64, d=256, pool=A, pages=4, slot=A, n=(1 << 20) + 1, k=A, v=A, dt=1, stream=None)
+    assert _call(lib.dckv_quant_read, base) == E and "n_tok" in lib.dckv_last_error().decode()
+
+
+@pytest.mark.parametrize("rows", [-1, 2 ** 31, 2 ** 32 + 5])
+def test_page_map_rows_fit_32_bits(rows):
+    from paper_2607_24331_amd import page_map
+    t = torch.zeros(1, dtype=torch.int32)
+    with pytest.raises(ValueError, match="rows"):
+        page_map(t, t, t.view(1, 1), t, t, rows)
+
+
 def test_rotary_ignores_what_its_scaling_does_not_read(lib):
     st, out = _rotary(lib, factor=math.nan, original_context=math.nan, low=math.nan)
     assert st == 0
