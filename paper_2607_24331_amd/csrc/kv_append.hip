@@ -5,7 +5,7 @@
 // append_rows  d/8 lanes hold a row, 8 columns each, in fp32.
 //   Keys (and values of bf16 pages): a lane group walks over the heads of one token with
 //   the next heads' rows on their way, and turns them by factors that stay in
-//   registers.  For e4m3 the row's maximum (shuffles) gives the exponent, exact in
+//   registers; a plane's other coordinate comes from the lane that holds it.  For e4m3 the row's maximum gives the exponent, exact in
 //   integer arithmetic on the maximum's bits; the conversion is the hardware's
 //   round-to-nearest-even after an exact multiplication by 2^-e.  Key bytes go out 8 at
 //   a time, 16 columns of a token side by side in the page.
@@ -15,8 +15,8 @@
 //   goes out in 16-byte pieces; other rows (single tokens) go out as bytes.
 // read_rows  the same units the other way.
 // Each element is read once and written once: memory bounds long prompts, latency single
-// tokens.  4,093 tokens of 32 heads of 128, back to back in a graph: 24 us (101 MB,
-// 4.2 TB/s), read back 22; 64 tokens of 8 heads: 5.3 us and 3.7.
+// tokens.  4,093 tokens of 32 heads of 128, back to back in a graph: 22 us (101 MB,
+// 4.6 TB/s), read back 22; 64 tokens of 8 heads: 4.7 us and 3.7.
 #include <algorithm>
 
 #include "rotary.h"
@@ -25,10 +25,12 @@ namespace dckv {
 namespace {
 
 constexpr int kMaxRows = 128;             // tokens a work-group
+constexpr int kAhead = 4;                 // heads whose rows are on their way to a lane group: 27.5 us for
+                                          // 4093 x 32 rows (a call), 28.5 with 2
 // Work-groups that a part of a call aims for.  An append forms angles or finds units once
-// for the heads of a work-group, a read has less to share: 4093 x 32 rows take 29 us (a call)
-// with 1024 for the keys and 512 for the values, 31 with 1024 both, 33 with 512 both and 34
-// with 2048 both; into bf16 pages 27.5 with 512 to 2048; read back 19.8 with 2048 for
+// for the heads of a work-group, a read has less to share: 4093 x 32 rows took 28.5 us (a
+// call) with 1024 for the keys and 512 for the values, 31 with 1024 both, 32.5 with 512 both and
+// 34 with 2048 both; into bf16 pages 27.5 with 512 to 2048; read back 19.8 with 2048 for
 // the keys and 512 for the values, 21.7 with 1024 and 23.8 with 2048 for these.
 constexpr int64_t kKeyGroups = 1024;
 constexpr int64_t kValueGroups = 512;
@@ -37,11 +39,10 @@ constexpr int64_t kReadGroups = 2048;
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-// Least e in [-112, 119] with amax <= 448 * 2^e: with amax = f 2^p, f in
-// [1, 2), and 448 = 1.75 * 2^8, e = p - 8, one more where f > 1.75.  Zeros and
+// Least e in [-112, 119] with amax <= 448 * 2^e, from amax's bits u: with amax = f 2^p,
+// f in [1, 2), and 448 = 1.75 * 2^8, e = p - 8, one more where f > 1.75.  Zeros and
 // fp32 subnormals give -112, an infinity the largest.
-__device__ __forceinline__ int scale_exponent(float amax) {
-  const uint32_t u = __float_as_uint(amax);
+__device__ __forceinline__ int scale_exponent(uint32_t u) {
   const int e = int(u >> 23) - 127 - 8 + ((u & 0x7FFFFFu) > 0x600000u ? 1 : 0);
   return min(119, max(-112, e));
 }
@@ -87,6 +88,12 @@ struct Row8 {
       }
     }
   }
+  __device__ __forceinline__ Row8 of(int lane) const {   // what another lane holds
+    Row8 r;
+#pragma unroll
+    for (int k = 0; k < 4 * N; ++k) r.w[k / 4][k % 4] = __shfl(int(w[k / 4][k % 4]), lane);
+    return r;
+  }
   __device__ __forceinline__ float get(int e) const {
     if constexpr (sizeof(T) == 4) {
       return __uint_as_float(w[e / 4][e % 4]);
@@ -97,15 +104,29 @@ struct Row8 {
   }
 };
 
+// Greatest u over the L lanes of a row, by data-parallel moves within 16 lanes:
+// neighbours, pairs, halves, ends.  Through LDS (shuffles) long appends took 5% more.
+template <int CTRL>
+__device__ __forceinline__ uint32_t moved(uint32_t u) {
+  return __builtin_amdgcn_update_dpp(0, u, CTRL, 0xF, 0xF, true);
+}
+template <int L>
+__device__ __forceinline__ uint32_t row_max(uint32_t u) {
+  u = max(u, moved<0xB1>(u));
+  u = max(u, moved<0x4E>(u));
+  u = max(u, moved<0x141>(u));
+  if constexpr (L > 8) u = max(u, moved<0x140>(u));
+  if constexpr (L > 16) u = max(u, uint32_t(__shfl_xor(int(u), 16)));
+  return u;
+}
+
 // Bytes of a row's 8 columns and the row's exponent, from L lanes that hold it.
 template <int L>
 __device__ __forceinline__ int quantize8(const float (&x)[8], uint32_t& lo, uint32_t& hi) {
   float amax = 0.f;                        // fmaxf passes a NaN over
 #pragma unroll
   for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(x[e]));
-#pragma unroll
-  for (int o = 1; o < L; o <<= 1) amax = fmaxf(amax, __shfl_xor(amax, o));
-  const int e2 = scale_exponent(amax);
+  const int e2 = scale_exponent(row_max<L>(__float_as_uint(amax)));   // bits order as numbers do from 0 up
   const float inv = __uint_as_float(uint32_t(127 - e2) << 23);
   const bool clamp = __any(e2 == 119);
   lo = pack4(x[0], x[1], x[2], x[3], inv, clamp);
@@ -283,15 +304,12 @@ __device__ __forceinline__ void append_by_row(const AppendBlock<T>& b, const Rot
   const bool turn = !b.value && j0 < 2 * P, low = j0 < P;
   // half layout, whole pieces: the partners are another lane's 8 columns
   const bool pair = turn && !rot.interleaved && P % 8 == 0;
-  const int jp = low ? j0 + P : j0 - P;
   const T* src = b.src + r * b.st.token + b.h0 * b.st.head;
-  Row8<T> own[2], partner[2];              // of two heads: their rows are on their way
+  const int other = (threadIdx.x & 63) + (low ? P / 8 : -P / 8);
+  Row8<T> own[kAhead];                      // of the next heads: their rows are on their way
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
-    if (b.h0 + i < b.h1) {
-      own[i].load(src + i * b.st.head + j0, b.wide);
-      if (pair) partner[i].load(src + i * b.st.head + jp, b.wide);
-    }
+  for (int i = 0; i < kAhead; ++i)
+    if (b.h0 + i < b.h1) own[i].load(src + i * b.st.head + j0, b.wide);
   float2 g[8];                             // of the columns' planes; an interleaved one's at its first column
   if (turn) {
     const int pos = position[r];
@@ -305,7 +323,6 @@ __device__ __forceinline__ void append_by_row(const AppendBlock<T>& b, const Rot
       float2 mine[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) mine[e] = rotary_factor(rot, low ? j0 + e : j0 - P + 4 + e, pos);
-      const int other = (threadIdx.x & 63) + (low ? P / 8 : -P / 8);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {        // a plane's second coordinate takes the sine the other way
         const float2 f = make_float2(__shfl(mine[e].x, other), __shfl(mine[e].y, other));
@@ -326,17 +343,18 @@ __device__ __forceinline__ void append_by_row(const AppendBlock<T>& b, const Rot
   }
   const int s = int(sl & 63);
   char* at = b.pool + (sl >> 6) * (int64_t(b.n_heads) * (QUANT ? 128 * (D + 1) : 256 * D));
-  for (int h2 = b.h0; h2 < b.h1; h2 += 2) {
+  for (int h2 = b.h0; h2 < b.h1; h2 += kAhead) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < kAhead; ++i) {
       const int h = h2 + i;
       if (h >= b.h1) break;
       float x[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] = own[i].get(e);
       if (pair) {
+        const Row8<T> partner = own[i].of(other);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = x[e] * g[e].x + partner[i].get(e) * g[e].y;
+        for (int e = 0; e < 8; ++e) x[e] = x[e] * g[e].x + partner.get(e) * g[e].y;
       } else if (turn && rot.interleaved) {
 #pragma unroll
         for (int e = 0; e < 8; e += 2) {
@@ -351,10 +369,7 @@ __device__ __forceinline__ void append_by_row(const AppendBlock<T>& b, const Rot
           if (j < 2 * P) x[e] = x[e] * g[e].x + to_f32(src[j < P ? j + P : j - P]) * g[e].y;
         }
       }
-      if (h + 2 < b.h1) {
-        own[i].load(src + 2 * b.st.head + j0, b.wide);
-        if (pair) partner[i].load(src + 2 * b.st.head + jp, b.wide);
-      }
+      if (h + kAhead < b.h1) own[i].load(src + kAhead * b.st.head + j0, b.wide);
       src += b.st.head;
       if constexpr (QUANT) {
         uint32_t lo, hi;
@@ -716,7 +731,7 @@ int heads_for(int64_t blocks, int n_heads, int64_t target) {
 
 // Whether the 8-bit values of a call are cut at pages, in the launch's first work-groups
 // (they are the longer ones).  Appends in a graph, back to back, against blocks like the
-// keys': 4093 tokens of 32 heads 24.2 us and 48 (26.5 with the keys first, 33 in two launches),
+// keys': 4093 tokens of 32 heads 24 us and 48 (26.5 with the keys first, 33 in two launches),
 // 8192 of 8 heads in five runs 17 and 28, 256 of 32 heads 5.8 and 8.8.  Where no page's run is
 // long it loses (1024 tokens of 8 heads at random 18 and 13.5), and so do few rows, which
 // cannot hide what a cut leaves over (256 tokens of 16 heads in five runs 8.1 and 6.4).  Reads
