@@ -608,9 +608,11 @@ __global__ __launch_bounds__(256) void quant_merge(const float* __restrict__ par
       for (int i = 0; i < U; ++i)
         if (s + i * G < n) {
           const float y = weight[s + i * G];
-          if (y != 0.f)
+          // a weight that is 0 keeps infinite sums out, not the NaN that a row has seen: 0
+          // times a NaN is one, however the context is cut
 #pragma unroll
-            for (int v = 0; v < 4; ++v) o[v] = fmaf(y, x[i][v], o[v]);
+          for (int v = 0; v < 4; ++v)
+            if (y != 0.f || x[i][v] != x[i][v]) o[v] = fmaf(y, x[i][v], o[v]);
         }
     }
   }

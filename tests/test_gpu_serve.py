@@ -508,6 +508,29 @@ def test_quant_decode_nan_reaches_only_who_sees_it():
     assert np.isnan(got[0, 1]).all() and np.isnan(got[0, 0, 1]).all() and np.isfinite(got[0, 0, 0]).all()
 
 
+def test_quant_decode_nan_of_little_weight():
+    # a NaN that the query sees is in its result however the context is cut, also where the
+    # weight of its token, or of its whole split, is below the smallest fp32 number
+    from paper_2607_24331_amd import quant_decode
+    g = np.random.default_rng(12)
+    H, d, T = 1, 64, 1000
+    pool, table = _cache(g, [T], H, d, spread=0.0)
+    slot = table[0, np.array([3, T - 1]) // 64].astype(np.int64) * 64 + np.array([3, T - 1]) % 64
+    last = sv.read(pool, slot[1:], H, d)[0][0, 0]
+    q = np.zeros((1, 2, 2, d), np.float32)
+    q[0, :, 0] = 40 * last                                 # all weight on the last token
+    q[0, :, 1] = g.standard_normal(d)
+    _, val, _, _ = sv.offsets(int(slot[0] % 64), d, H, 0)
+    pool[slot[0] // 64, val[5]] = 0x7F
+    k = sv.read(pool, table[0, np.arange(T) // 64].astype(np.int64) * 64 + np.arange(T) % 64, H, d)[0][:, 0]
+    s = np.sort(k @ q[0, 1, 0].astype(np.float64)) / 8 / np.log(2)
+    assert s[-1] - s[-2] > 200
+    for split in (0, 64, 256, 1 << 16):
+        out = host(quant_decode(cu(q), cu(pool), cu(table), cu(np.array([T], np.int32)), 64 * table.shape[1], H, split))
+        bad = np.isnan(out)
+        assert bad[..., 5].all() and not bad[..., :5].any() and not bad[..., 6:].any(), split
+
+
 def test_quant_decode_graph_follows_the_lengths():
     # splits cut on the device: replays of one capture with lengths alike, unlike and
     # empty, in turn, over a workspace overwritten between replays
