@@ -36,6 +36,31 @@ def _gpu(t: torch.Tensor, name: str, dtype, index: Optional[int] = None, contigu
     raise ValueError(f"{name} must be contiguous")
 
 
+def _count(value, name: str):
+    """`value` where the C call's 32-bit argument holds it: ctypes would take the low 32 bits."""
+    if not -_INT32_MAX - 1 <= value <= _INT32_MAX:
+        raise ValueError(f"{name} {value} does not fit 32 bits")
+    return value
+
+
+def _width(page_table: torch.Tensor, B: int) -> int:
+    """Pages a row of the page table of B sequences."""
+    if not isinstance(page_table, torch.Tensor):
+        raise TypeError("page_table must be a torch tensor")
+    if page_table.dim() != 2 or page_table.shape[0] != B:
+        raise ValueError("page_table must be [batch, max_pages]")
+    return _count(page_table.shape[1], "max_pages")
+
+
+def _capacity(free_pages: torch.Tensor) -> int:
+    """Places of a stack of free pages."""
+    if not isinstance(free_pages, torch.Tensor):
+        raise TypeError("free_pages must be a torch tensor")
+    if free_pages.dim() != 1:
+        raise ValueError("free_pages must be a vector")
+    return _count(free_pages.shape[0], "the capacity of free_pages")
+
+
 def _vector(t: torch.Tensor, name: str, dtype, n: int, index: Optional[int] = None) -> int:
     p = _gpu(t, name, dtype, index)
     if t.shape != (n,):
@@ -50,10 +75,12 @@ def _heads(t: torch.Tensor, name: str, index: Optional[int] = None):
     code = _CODE.get(t.dtype)
     if code is None:
         raise TypeError(f"{name} must be float32 or bfloat16, got {t.dtype}")
-    p = _gpu(t, name, t.dtype, index, False)
     strides = t.stride()
     if len(strides) != 3:
         raise ValueError(f"{name} must be [tokens, heads, head_dim]")
+    if max(t.shape) > _INT32_MAX:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, sizes that do not fit 32 bits")
+    p = _gpu(t, name, t.dtype, index, False)
     st, sh, sd = strides
     if sd != 1 and t.shape[2] > 1:
         raise ValueError(f"{name}: the coordinates of a head must lie one after another")
@@ -115,17 +142,14 @@ def page_map(cached: torch.Tensor, added: torch.Tensor, page_table: torch.Tensor
     so that a step updates them in place."""
     if not isinstance(cached, torch.Tensor) or cached.dim() != 1:
         raise ValueError("cached must be a vector")
-    B, rows, dev, i32 = cached.shape[0], int(rows), cached.get_device(), torch.int32
+    B, rows, dev, i32 = _count(cached.shape[0], "batch"), int(rows), cached.get_device(), torch.int32
     if not 0 <= rows <= _INT32_MAX:            # ctypes would take the low 32 bits
         raise ValueError("rows must be in 0 .. 2^31 - 1")
+    width, capacity = _width(page_table, B), _capacity(free_pages)
     pc = _vector(cached, "cached", i32, B)
     pa = _vector(added, "added", i32, B, dev)
     pt = _gpu(page_table, "page_table", i32, dev)
-    if page_table.dim() != 2 or page_table.shape[0] != B:
-        raise ValueError("page_table must be [batch, max_pages]")
     pf = _gpu(free_pages, "free_pages", i32, dev)
-    if free_pages.dim() != 1:
-        raise ValueError("free_pages must be a vector")
     pn = _vector(free_count, "free_count", i32, 1, dev)
     if out is None:
         slot = _new((rows,), torch.int64, cached.device, stream)
@@ -151,8 +175,8 @@ def page_map(cached: torch.Tensor, added: torch.Tensor, page_table: torch.Tensor
                 t.fill_(-1)
             out.free_left.copy_(free_count)
         return out
-    _launch(_lib.dckv_page_map, "page_map", dev, stream, pc, pa, B, pt, page_table.shape[1], pf,
-            free_pages.shape[0], pn, p_left, p_lens, p_start, p_slot, p_pos, p_seq, rows, p_status)
+    _launch(_lib.dckv_page_map, "page_map", dev, stream, pc, pa, B, pt, width, pf,
+            capacity, pn, p_left, p_lens, p_start, p_slot, p_pos, p_seq, rows, p_status)
     return out
 
 
@@ -163,16 +187,13 @@ def page_release(finished: torch.Tensor, page_table: torch.Tensor, seq_lens: tor
     i32 = torch.int32
     if not isinstance(finished, torch.Tensor) or finished.dim() != 1:
         raise ValueError("finished must be a vector")
-    B, dev = finished.shape[0], finished.get_device()
+    B, dev = _count(finished.shape[0], "batch"), finished.get_device()
+    width, capacity = _width(page_table, B), _capacity(free_pages)
     pd = _vector(finished, "finished", i32, B)
     pt = _gpu(page_table, "page_table", i32, dev)
-    if page_table.dim() != 2 or page_table.shape[0] != B:
-        raise ValueError("page_table must be [batch, max_pages]")
     pf = _gpu(free_pages, "free_pages", i32, dev)
-    if free_pages.dim() != 1:
-        raise ValueError("free_pages must be a vector")
-    _launch(_lib.dckv_page_release, "page_release", dev, stream, pd, B, pt, page_table.shape[1],
-            _vector(seq_lens, "seq_lens", i32, B, dev), pf, free_pages.shape[0],
+    _launch(_lib.dckv_page_release, "page_release", dev, stream, pd, B, pt, width,
+            _vector(seq_lens, "seq_lens", i32, B, dev), pf, capacity,
             _vector(free_count, "free_count", i32, 1, dev))
 
 
@@ -193,8 +214,8 @@ class Rotary:
             raise ValueError(f"layout must be one of {sorted(_LAYOUTS)}")
         if scaling not in _SCALINGS:
             raise ValueError(f"scaling must be one of {sorted(_SCALINGS)}")
-        self.head_dim = int(head_dim)
-        self.rotary_dim = self.head_dim if rotary_dim is None else int(rotary_dim)
+        self.head_dim = _count(int(head_dim), "head_dim")
+        self.rotary_dim = self.head_dim if rotary_dim is None else _count(int(rotary_dim), "rotary_dim")
         desc = capi.RotaryDesc(self.head_dim, self.rotary_dim, _LAYOUTS[layout], _SCALINGS[scaling],
                                base, factor, original_context, low, high, magnitude)
         handle = ctypes.c_void_p()
@@ -272,9 +293,8 @@ def decode_rotary(plan, q: torch.Tensor, pool: torch.Tensor, page_table: torch.T
     pp = _gpu(pool, "pool", dt, dev)
     if pool.numel() % plan.page_elems:
         raise ValueError("pool size is not a whole number of pages")
+    width = _width(page_table, B)
     pt = _gpu(page_table, "page_table", torch.int32, dev)
-    if page_table.dim() != 2 or page_table.shape[0] != B:
-        raise ValueError("page_table must be [batch, max_pages]")
     ps = _vector(seq_lens, "seq_lens", torch.int32, B, dev)
     pk = _gpu(R_keys, "R_keys", dt, dev)
     if R_keys.numel() != plan.key_factor_elems:
@@ -291,7 +311,7 @@ def decode_rotary(plan, q: torch.Tensor, pool: torch.Tensor, page_table: torch.T
         workspace = _new((max(plan.rope_workspace_bytes(B, max_context), 256),), torch.uint8, q.device, stream)
     pw = _gpu(workspace, "workspace", torch.uint8, dev)
     _launch(_lib.dckv_decode_rotary, "decode_rotary", dev, stream, plan.handle, pq, B, pp,
-            pool.numel() // plan.page_elems, pt, page_table.shape[1], ps, max_context, pk, pv,
+            pool.numel() // plan.page_elems, pt, width, ps, max_context, pk, pv,
             rotation.handle, po, pw, workspace.numel())
     return out
 
@@ -318,7 +338,9 @@ def _append(fn, what: str, k, v, slot, pool, pool_dtype, page: int, rotation, po
                 pool.numel() // page)
 
 
-_dense_page = functools.lru_cache(maxsize=256)(dense_page_elems)
+@functools.lru_cache(maxsize=256)
+def _dense_page(num_kv_heads: int, head_dim: int) -> int:
+    return dense_page_elems(_count(num_kv_heads, "num_kv_heads"), _count(head_dim, "head_dim"))
 
 
 def dense_append(k: torch.Tensor, v: torch.Tensor, slot: torch.Tensor, kv_pool: torch.Tensor,
@@ -337,6 +359,8 @@ def dense_append(k: torch.Tensor, v: torch.Tensor, slot: torch.Tensor, kv_pool: 
 def quant_page_bytes(num_kv_heads: int, head_dim: int) -> int:
     """Bytes of one page (64 tokens) of the 8-bit K/V cache."""
     n = ctypes.c_int64()
+    _count(num_kv_heads, "num_kv_heads")
+    _count(head_dim, "head_dim")
     _check(_lib.dckv_quant_page_bytes(num_kv_heads, head_dim, ctypes.byref(n)), "quant_page_bytes")
     return n.value
 
@@ -360,15 +384,16 @@ def quant_read(pool: torch.Tensor, slot: torch.Tensor, num_kv_heads: int, head_d
                dtype=torch.bfloat16, stream=None):
     """Cached keys and values [tokens, H_kv, d_h] of the given slots (zeros for
     a slot outside the pool), exactly, as bfloat16 or float32."""
+    if not isinstance(slot, torch.Tensor) or slot.dim() != 1:
+        raise ValueError("slot must be a vector")
+    n = _count(slot.shape[0], "the length of slot")
     pp = _gpu(pool, "pool", torch.uint8)
     page = quant_page_bytes(num_kv_heads, head_dim)
     if pool.numel() % page:
         raise ValueError("pool size is not a whole number of pages")
     if dtype not in _CODE:
         raise TypeError("dtype must be float32 or bfloat16")
-    if not isinstance(slot, torch.Tensor) or slot.dim() != 1:
-        raise ValueError("slot must be a vector")
-    n, dev = slot.shape[0], pool.get_device()
+    dev = pool.get_device()
     ps = _vector(slot, "slot", torch.int64, n, dev)
     k = _new((n, num_kv_heads, head_dim), dtype, pool.device, stream)
     v = _new((n, num_kv_heads, head_dim), dtype, pool.device, stream)
@@ -382,6 +407,10 @@ def quant_read(pool: torch.Tensor, slot: torch.Tensor, num_kv_heads: int, head_d
 def quant_workspace_bytes(num_q_heads: int, num_kv_heads: int, head_dim: int, queries_per_seq: int,
                           split_tokens: int, batch: int, max_context: int) -> int:
     n = ctypes.c_size_t()
+    for value, name in ((num_q_heads, "num_q_heads"), (num_kv_heads, "num_kv_heads"), (head_dim, "head_dim"),
+                        (queries_per_seq, "queries_per_seq"), (split_tokens, "split_tokens"), (batch, "batch"),
+                        (max_context, "max_context")):
+        _count(value, name)
     _check(_lib.dckv_quant_workspace_bytes(num_q_heads, num_kv_heads, head_dim, queries_per_seq, split_tokens,
                                            batch, max_context, ctypes.byref(n)), "quant_workspace_bytes")
     return n.value
@@ -408,9 +437,8 @@ def quant_decode(q: torch.Tensor, pool: torch.Tensor, page_table: torch.Tensor, 
     page = quant_page_bytes(num_kv_heads, d)
     if pool.numel() % page:
         raise ValueError("pool size is not a whole number of pages")
+    width = _width(page_table, B)
     pt = _gpu(page_table, "page_table", torch.int32, dev)
-    if page_table.dim() != 2 or page_table.shape[0] != B:
-        raise ValueError("page_table must be [batch, max_pages]")
     ps = _vector(seq_lens, "seq_lens", torch.int32, B, dev)
     if out is None:
         out = _new(q.shape, f32, q.device, stream)
@@ -422,6 +450,6 @@ def quant_decode(q: torch.Tensor, pool: torch.Tensor, page_table: torch.Tensor, 
         workspace = _new((need,), torch.uint8, q.device, stream)
     pw = _gpu(workspace, "workspace", torch.uint8, dev) if workspace is not None else None
     _launch(_lib.dckv_quant_decode, "quant_decode", dev, stream, Hq, num_kv_heads, d, Q, split_tokens, pq, B,
-            pp, pool.numel() // page, pt, page_table.shape[1], ps, top, po, pw,
+            pp, pool.numel() // page, pt, width, ps, top, po, pw,
             workspace.numel() if workspace is not None else 0)
     return out

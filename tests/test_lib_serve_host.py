@@ -84,6 +84,55 @@ def test_page_map_rows_fit_32_bits(rows):
         page_map(t, t, t.view(1, 1), t, t, rows)
 
 
+W = 1 << 32           # ctypes keeps the low 32 bits of a 32-bit argument
+
+
+def test_counts_fit_32_bits():
+    from paper_2607_24331_amd import DckvError, Rotary, dense_append, quant_append, quant_page_bytes, quant_workspace_bytes
+    good = dict(num_q_heads=32, num_kv_heads=8, head_dim=128, queries_per_seq=1, split_tokens=64, batch=2, max_context=4096)
+    assert quant_workspace_bytes(**good) > 0
+    for name, value in good.items():
+        for bad in (W + value, value - W, 2 ** 31):
+            with pytest.raises(ValueError, match=name):
+                quant_workspace_bytes(**{**good, name: bad})
+    with pytest.raises(ValueError, match="split_tokens"):      # not 0, which lets the library choose
+        quant_workspace_bytes(**{**good, "split_tokens": W})
+    for kw in (dict(head_dim=W + 128), dict(head_dim=128, rotary_dim=W + 64)):
+        with pytest.raises(ValueError, match="32 bits"):
+            Rotary(**kw)
+    for H, d in ((W + 8, 128), (8, W + 128)):
+        with pytest.raises(ValueError, match="32 bits"):
+            quant_page_bytes(H, d)
+    one = torch.zeros(1, 1, 1)
+    pool, slot = torch.zeros(64), torch.zeros(1, dtype=torch.int64)
+    for append in (dense_append, quant_append):
+        for shape in ((1, W + 8, 64), (1, 8, W + 64), (W + 1, 8, 64)):
+            k = one.expand(shape)
+            with pytest.raises(ValueError, match="32 bits"):
+                append(k, k, slot, pool)
+    with pytest.raises(DckvError):                             # in 32 bits the library refuses
+        quant_page_bytes(-8, 128)
+
+
+def test_tensor_sizes_fit_32_bits():
+    from paper_2607_24331_amd import Rotary, page_map, page_release, quant_read, rotary
+    i32 = torch.zeros(1, dtype=torch.int32)
+    table, far = i32.view(1, 1), i32.expand(W + 1)
+    for args in ((i32, i32, table.expand(1, W + 1), i32, i32, 1), (i32, i32, table, far, i32, 1),
+                 (far, far, table, i32, i32, 1)):
+        with pytest.raises(ValueError, match="32 bits"):
+            page_map(*args)
+    for args in ((i32, table.expand(1, W + 1), i32, i32, i32), (i32, table, i32, far, i32),
+                 (far, table, far, i32, i32)):
+        with pytest.raises(ValueError, match="32 bits"):
+            page_release(*args)
+    for shape in ((W + 1, 1, 64), (1, W + 1, 64)):
+        with pytest.raises(ValueError, match="32 bits"):
+            rotary(Rotary(64), torch.zeros(1, 1, 1).expand(shape), i32)
+    with pytest.raises(ValueError, match="32 bits"):
+        quant_read(torch.zeros(1, dtype=torch.uint8), torch.zeros(1, dtype=torch.int64).expand(W + 1), 1, 64)
+
+
 def test_rotary_ignores_what_its_scaling_does_not_read(lib):
     st, out = _rotary(lib, factor=math.nan, original_context=math.nan, low=math.nan)
     assert st == 0
