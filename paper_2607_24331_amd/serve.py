@@ -253,7 +253,12 @@ def rotary(rotation: Rotary, x: torch.Tensor, position: torch.Tensor, out: Optio
     `out` may be x; a new one has out_dtype (x's by default).  A token of
     negative position is skipped: its row of `out` stays as it was, that of a
     new tensor undefined.  `inverse` turns back (times the magnitude still):
-    the gradient of x from that of the result."""
+    the gradient of x from that of the result.  The call itself is outside
+    autograd and refuses tensors that record gradients: a torch.autograd.Function
+    calls it in its forward and, with `inverse`, in its backward pass."""
+    if torch.is_grad_enabled() and (getattr(x, "requires_grad", False) or getattr(out, "requires_grad", False)):
+        raise ValueError("rotary is outside autograd: x and out must not require gradients here (call it under "
+                         "torch.no_grad() or from a torch.autograd.Function; inverse=True gives the gradient of x)")
     px, xc, xt, xh = _heads(x, "x")
     n, H, d = x.shape
     if d != rotation.head_dim:

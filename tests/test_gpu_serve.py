@@ -227,6 +227,42 @@ def test_rotary_gradient():
         assert abs((f(x + e) - f(x - e)) - grad[at]) <= 2.0 ** -19 * (np.abs(x) @ np.ones(64)).max() * np.abs(w).max() * 4
 
 
+def test_rotary_in_an_autograd_function():
+    # forward and transpose as a training program wraps them, against autograd of the plain
+    # formula in fp64; a head broadcast to three gathers the gradients of all
+    from paper_2607_24331_amd import rotary
+    r, theta, layout, m = _rotation(64, dict(rotary_dim=48, magnitude=1.25))
+    g = np.random.default_rng(6)
+    pos = g.integers(0, 4000, 7).astype(np.int32)
+    at = cu(pos)
+
+    class Turn(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x):
+            return rotary(r, x, at)
+
+        @staticmethod
+        def backward(ctx, grad):
+            return rotary(r, grad, at, inverse=True)
+
+    x, w = g.standard_normal((7, 1, 64)).astype(np.float32), g.standard_normal((7, 3, 64)).astype(np.float32)
+    leaf = cu(x).requires_grad_()
+    y = Turn.apply(leaf.expand(7, 3, 64))
+    (y * cu(w)).sum().backward()
+    z = torch.from_numpy(x).double().requires_grad_()
+    ang = torch.from_numpy(pos.astype(np.float64)[:, None] * theta)[:, None]
+    a, b, c, s = z[..., :24], z[..., 24:48], m * torch.cos(ang), m * torch.sin(ang)
+    want = torch.cat([a * c - b * s, b * c + a * s, z[..., 48:]], -1).expand(7, 3, 64)
+    (want * torch.from_numpy(w).double()).sum().backward()
+    tol = 1.01 * _turn_tol(x.repeat(3, 1), 24, layout, m) + 1e-40
+    assert np.all(np.abs(host(y) - want.detach().numpy()) <= tol)
+    # three gradients of the tolerance each and two roundings of their sum
+    tol = _turn_tol(w, 24, layout, m).sum(1, keepdims=True) + 2 * 2.0 ** -24 * m * 2 * np.abs(w).sum(1, keepdims=True)
+    assert np.all(np.abs(host(leaf.grad) - z.grad.numpy()) <= tol + 1e-40)
+    with pytest.raises(ValueError, match="autograd"):
+        rotary(r, leaf, at)
+
+
 # --------------------------------------------------------------------- appends
 def _slots(g, n, pages, run):
     """n distinct slots: runs of consecutive ones from anywhere, in any order."""

@@ -133,6 +133,17 @@ def test_tensor_sizes_fit_32_bits():
         quant_read(torch.zeros(1, dtype=torch.uint8), torch.zeros(1, dtype=torch.int64).expand(W + 1), 1, 64)
 
 
+def test_rotary_refuses_to_drop_a_gradient():
+    from paper_2607_24331_amd import Rotary, rotary
+    r, pos = Rotary(64), torch.zeros(1, dtype=torch.int32)
+    plain, leaf = torch.zeros(1, 1, 64), torch.zeros(1, 1, 64, requires_grad=True)
+    for kw in (dict(x=leaf), dict(x=2 * leaf), dict(x=plain, out=leaf)):
+        with pytest.raises(ValueError, match="autograd"):
+            rotary(r, position=pos, **kw)
+    with torch.no_grad(), pytest.raises(ValueError, match="GPU"):   # no gradient is recorded: the next check
+        rotary(r, leaf, pos)
+
+
 def test_rotary_ignores_what_its_scaling_does_not_read(lib):
     st, out = _rotary(lib, factor=math.nan, original_context=math.nan, low=math.nan)
     assert st == 0
