@@ -472,7 +472,9 @@ int dckv_rotary_apply(const dckv_rotary* rotary, const void* x, int32_t x_dtype,
                       int32_t n_tok, int32_t num_heads, int32_t inverse, void* stream);
 
 /* dckv_decode_rope with any rotation whose head_dim is the plan's: keys of
- * cache position t are turned by t, the query by the newest position. */
+ * cache position t are turned by t, the query by the newest position.  Turned
+ * coordinates weigh magnitude^2 in a score; EINVAL where that is not finite in
+ * fp32. */
 int dckv_decode_rotary(const dckv_plan* plan, const float* q, int32_t batch, const void* pool,
                        int64_t num_pages, const int32_t* page_table, int32_t max_pages,
                        const int32_t* seq_lens, int32_t max_context, const void* R_keys,

@@ -4,6 +4,7 @@
 #include <hip/hip_runtime_api.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -648,6 +649,10 @@ int dckv_decode_rotary(const dckv_plan* p, const float* q, int32_t batch, const 
   if (rotary->desc.head_dim != p->dh)
     return fail(DCKV_EINVAL, "decode_rotary: a rotation of head_dim %d for a plan of %d",
                 rotary->desc.head_dim, p->dh);
+  // turned queries and keys both carry the magnitude: a score's weight is its square
+  if (!(rotary->table.magnitude * rotary->table.magnitude <= FLT_MAX))
+    return fail(DCKV_EINVAL, "decode_rotary: the square of magnitude %g is not a finite fp32 number",
+                double(rotary->table.magnitude));
   dckv::RopeTurns turns{};
   turns.n = rotary->table.planes;
   turns.interleaved = rotary->table.interleaved;

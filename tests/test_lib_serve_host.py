@@ -144,6 +144,16 @@ def test_rotary_refuses_to_drop_a_gradient():
         rotary(r, leaf, pos)
 
 
+def test_decode_rotary_refuses_a_weight_beyond_fp32(lib):
+    # a score weighs the square of the magnitude; a batch of 0 launches nothing
+    from paper_2607_24331_amd import Plan, Rotary
+    plan = Plan(512, 8, 4, 128, [0, 1, 1, 0], [100, 77], 144)
+    for m, want in ((1.8e19, capi.DCKV_OK), (-1.8e19, capi.DCKV_OK), (1.9e19, E), (-3e38, E), (1e-30, capi.DCKV_OK)):
+        st = lib.dckv_decode_rotary(plan.handle, None, 0, None, 1, None, 1, None, 64, None, None,
+                                    Rotary(128, magnitude=m).handle, None, None, 0, None)
+        assert st == want and (st == capi.DCKV_OK or "magnitude" in lib.dckv_last_error().decode()), m
+
+
 def test_rotary_ignores_what_its_scaling_does_not_read(lib):
     st, out = _rotary(lib, factor=math.nan, original_context=math.nan, low=math.nan)
     assert st == 0
