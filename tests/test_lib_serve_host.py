@@ -149,8 +149,9 @@ def test_decode_rotary_refuses_a_weight_beyond_fp32(lib):
     from paper_2607_24331_amd import Plan, Rotary
     plan = Plan(512, 8, 4, 128, [0, 1, 1, 0], [100, 77], 144)
     for m, want in ((1.8e19, capi.DCKV_OK), (-1.8e19, capi.DCKV_OK), (1.9e19, E), (-3e38, E), (1e-30, capi.DCKV_OK)):
+        r = Rotary(128, magnitude=m)                           # alive until the call is over
         st = lib.dckv_decode_rotary(plan.handle, None, 0, None, 1, None, 1, None, 64, None, None,
-                                    Rotary(128, magnitude=m).handle, None, None, 0, None)
+                                    r.handle, None, None, 0, None)
         assert st == want and (st == capi.DCKV_OK or "magnitude" in lib.dckv_last_error().decode()), m
 
 
