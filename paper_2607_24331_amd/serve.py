@@ -169,11 +169,13 @@ def page_map(cached: torch.Tensor, added: torch.Tensor, page_table: torch.Tensor
         p_status = _vector(out.status, "status", i32, B, dev)
         p_left = _vector(out.free_left, "free_left", i32, 1, dev)
     if B == 0:       # no sequences: every row lies behind the last one
+        if stream is not None and stream.device.index != dev:
+            raise ValueError(f"page_map: the stream is of {stream.device}, the tensors of device {dev}")
         with torch.cuda.stream(stream):          # None: the current one
             out.row_start.zero_()
             for t in (out.slot, out.position, out.seq_of_row):
                 t.fill_(-1)
-            out.free_left.copy_(free_count)
+            torch.clamp(free_count, 0, capacity, out=out.free_left)
         return out
     _launch(_lib.dckv_page_map, "page_map", dev, stream, pc, pa, B, pt, width, pf,
             capacity, pn, p_left, p_lens, p_start, p_slot, p_pos, p_seq, rows, p_status)

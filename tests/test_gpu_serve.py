@@ -116,6 +116,23 @@ def test_page_map_of_nothing_keeps_its_stream():
     assert m.row_start.tolist() == [0] and m.free_left.tolist() == [3]
 
 
+def test_page_map_of_nothing_clamps_the_count():
+    # as a map of sequences does; also in place
+    from types import SimpleNamespace
+
+    from paper_2607_24331_amd import page_map
+    i32 = dict(dtype=torch.int32, device="cuda")
+    none, table, free = torch.empty(0, **i32), torch.empty((0, 4), **i32), torch.arange(3, **i32)
+    for count, left in ((10 ** 9, 3), (-4, 0), (2, 2)):
+        n = torch.tensor([count], **i32)
+        m = page_map(none, none, table, free, n, 2)
+        assert m.free_left.tolist() == [left] and n.tolist() == [count]
+        m = page_map(none, none, table, free, n, 2, out=m._replace(free_left=n))
+        assert n.tolist() == [left]
+    with pytest.raises(ValueError, match="stream"):
+        page_map(none, none, table, free, n, 2, out=m, stream=SimpleNamespace(device=torch.device("cuda", 1)))
+
+
 @pytest.mark.parametrize("B, width, cap", [(1, 3, 10), (40, 70, 5000), (1030, 5, 3000), (40, 70, 100)])
 def test_page_release(B, width, cap):
     from paper_2607_24331_amd import page_release
