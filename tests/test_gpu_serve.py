@@ -206,6 +206,34 @@ def test_rotary(rot, types, inverse):
         assert np.array_equal(rest, host(x[..., 2 * len(theta):].to(types[1])))
 
 
+@pytest.mark.parametrize("inverse", [False, True])
+@pytest.mark.parametrize("rot", range(len(ROTS)))
+def test_rotary_error_is_that_of_its_fp32_operations(rot, inverse):
+    """fp32 to fp32.  Sine and cosine are formed in fp64 and rounded once, 2^-24 of their
+    size; a product's and the sum's rounding are 2^-24 each: 3 * 2^-24 (2% more for their
+    products) of |x_a cos| + |x_b sin|.  Angles: theta to 64 eps = 2^-46, positions below
+    2^16, the product and the turns to a few eps more: below 2^-29 radians."""
+    from paper_2607_24331_amd import rotary
+    g = np.random.default_rng(rot)
+    for n, H, d in ((3, 2, 64), (200, 4, 128), (65, 1, 256)):
+        r, theta, layout, m = _rotation(d, ROTS[rot])
+        m = np.float64(np.float32(m))
+        x = g.standard_normal((n, H, d)).astype(np.float32)
+        pos = g.integers(0, 1 << 16, n).astype(np.int32)
+        y = host(rotary(r, cu(x), cu(pos), inverse=inverse))
+        want = sv.turn(x, pos, theta, layout, m, inverse)
+        k = len(theta)
+        a, b = ((slice(0, k), slice(k, 2 * k)) if layout == "half" else (slice(0, 2 * k, 2), slice(1, 2 * k, 2)))
+        ang, ab = (pos.astype(np.float64)[:, None] * theta)[:, None], np.abs(x).astype(np.float64)
+        c, s = np.abs(np.cos(ang)), np.abs(np.sin(ang))
+        tol = np.zeros(x.shape)
+        tol[..., a], tol[..., b] = ab[..., a] * c + ab[..., b] * s, ab[..., b] * c + ab[..., a] * s
+        tol *= 3 * 2.0 ** -24 * 1.02
+        tol[..., a] += 2.0 ** -29 * (ab[..., a] + ab[..., b])
+        tol[..., b] += 2.0 ** -29 * (ab[..., a] + ab[..., b])
+        assert np.all(np.abs(y - want) <= m * tol + 1e-40), float((np.abs(y - want) / (m * tol + 1e-40)).max())
+
+
 def test_rotary_in_place_strides_and_skipped_rows():
     from paper_2607_24331_amd import rotary
     r, theta, layout, m = _rotation(128, dict(rotary_dim=64))
@@ -403,6 +431,85 @@ def test_appends_turn_keys(n, H, d, run, rot):
         assert np.array_equal(cells, was)
 
 
+# heads a work-group, size after size: bf16 pages 8 of 30, 5, 2 of 17, 5, 5, 12, 1; 8-bit keys
+# 1, 1, 1, 4 of 5, 5, 2 of 12, 1, all but the last in the launch that is cut at pages
+@pytest.mark.parametrize("rot", [0, 1, 2, 3, 4, 8])
+@pytest.mark.parametrize("n, H, d, run", [(1029, 30, 128, 1029), (8200, 5, 64, 77), (600, 17, 256, 600), (8200, 5, 128, 900),
+                                          (16500, 5, 128, 16500), (8200, 12, 64, 64), (255, 13, 128, 100)])
+def test_appends_turn_keys_of_many_heads(n, H, d, run, rot):
+    from paper_2607_24331_amd import dense_append, dense_page_elems, quant_append, quant_read
+    g = np.random.default_rng(n + rot)
+    r, theta, layout, m = _rotation(d, ROTS[rot])
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(n + rot)
+    some = np.unique(np.concatenate([[0, n - 1, n // 2], g.integers(0, n, 60), np.arange(min(n, 33))]))
+    at = torch.from_numpy(some).cuda()
+    for dtype, V in ((BF16, d), (F32, d), (BF16, d + 3)):
+        full = torch.randn((n, 2, H, V), generator=gen, device="cuda").to(dtype)
+        kk, vv = full[:, 0, :, :d], full[:, 1, :, :d]
+        pages = -(-n // 64) + 17
+        slot = _slots(g, n, pages, run)
+        pos = g.integers(0, 100000, n).astype(np.int32)
+        ts, tp = cu(slot), cu(pos)
+        y = sv.turn(host(kk[at]), pos[some], theta, layout, np.float64(np.float32(m)))
+        tol = _turn_tol(host(kk[at]), len(theta), layout, m)
+        pool = torch.zeros((pages, H * (128 * d + 128)), dtype=torch.uint8, device="cuda")
+        quant_append(kk, vv, ts, pool, r, tp)
+        k8, v8 = quant_read(pool, ts[at], H, d, F32)
+        amax = np.abs(y).max(-1, keepdims=True) + tol.max(-1, keepdims=True)
+        unit = 2.0 ** np.ceil(np.log2(amax / 448))         # as in test_appends_turn_keys
+        assert np.all(np.abs(host(k8) - y) <= tol + np.maximum((np.abs(y) + tol) * 2.0 ** -4, unit * 2.0 ** -10))
+        b, e = sv.quantize(host(vv[at]))
+        assert np.array_equal(host(v8), sv.E4M3[b] * 2.0 ** e[..., None])
+        pool = torch.zeros((pages, dense_page_elems(H, d)), dtype=BF16, device="cuda")
+        dense_append(kk, vv, ts, pool, r, tp)
+        cells = pool.view(pages, 2, H, 64, d)
+        assert np.all(np.abs(host(cells[ts[at] // 64, 0, :, ts[at] % 64]) - y) <= tol + _half_step(np.abs(y) + tol, BF16))
+        assert torch.equal(cells[ts // 64, 1, :, ts % 64], vv.to(BF16))
+
+
+def test_page_map_serves_the_latent_cache():
+    # a prompt and two tokens of three sequences through page_map, latent_append and decode,
+    # against slots worked out on the host
+    from gpu_common import dev, plan_for
+    from paper_2607_24331_amd import decode, latent_append, page_map
+    from workloads.configs import custom_workload
+    from workloads.inputs import make_inputs
+    lens = (130, 64, 1)
+    wl = custom_workload(name="mapped", seed=5, hidden=512, num_q_heads=8, num_kv_heads=4, head_dim=64,
+                         group_of_kv=(0, 1, 1, 0), group_rank=(100, 77), value_rank=144, dtype="bf16", batch=3,
+                         seq_lens=lens, prefill_lens=lens, append_tokens=0, factor_scheme="orthonormal")
+    inp, plan = make_inputs(wl), plan_for(wl)
+    factors = dev(inp.L_keys.T, "bf16"), dev(inp.L_value.T, "bf16")
+    up = dev(inp.R_keys_flat, "bf16"), dev(inp.R_value, "bf16")
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    pool, other = plan.new_pool(12), plan.new_pool(12)
+    table, cached, free, left = torch.full((3, 4), -1, **i32), torch.zeros(3, **i32), torch.arange(12, **i32), torch.tensor([12], **i32)
+    have, pages = [0, 0, 0], [[], [], []]
+    ids = list(range(12))
+    for added, pad in ((lens, 5), ((1, 1, 1), 0), ((1, 0, 1), 1)):
+        x = torch.randn((sum(added) + pad, 512), generator=g, device="cuda").to(BF16)
+        m = page_map(cached, torch.tensor(added, **i32), table, free, left, x.shape[0])
+        latent_append(plan, x, *factors, m.slot, pool)
+        slot = []
+        for b, n in enumerate(added):
+            for t in range(have[b], have[b] + n):
+                if t // 64 == len(pages[b]):
+                    pages[b].append(ids.pop())
+                slot.append(pages[b][t // 64] * 64 + t % 64)
+            have[b] += n
+        assert m.slot.tolist() == slot + [-1] * pad and m.seq_lens.tolist() == have
+        latent_append(plan, x[:len(slot)], *factors, torch.tensor(slot, device="cuda"), other)
+        assert torch.equal(pool, other)
+        cached, left = m.seq_lens, m.free_left
+    q = torch.from_numpy(inp.q).cuda()
+    flat = torch.tensor([p + [0] * (4 - len(p)) for p in pages], **i32)
+    got = decode(plan, q, pool, table, cached, 256, *up)
+    assert torch.equal(got, decode(plan, q, other, flat, torch.tensor(have, **i32), 256, *up)) and got.abs().sum() > 0
+
+
 def test_dense_append_feeds_dense_decode():
     from oracle import dense as odense
     from paper_2607_24331_amd import dense_append, dense_decode, dense_page_elems
@@ -496,6 +603,69 @@ def test_quant_decode_long_split():
     for lens, split in (([20000], 1 << 16), ([16385, 700], 8192)):
         pool, table = _cache(g, lens, 1, 64)
         _check_decode(g.standard_normal((len(lens), 1, 2, 64)).astype(np.float32), pool, table, lens, 1, split)
+
+
+@pytest.mark.parametrize("Hq, H, d, Q, lens", [
+    (4, 1, 128, 1, [2300, 1]), (2, 1, 128, 4, [1500, 700]), (20, 1, 128, 1, [1700, 4200]), (20, 1, 128, 4, [1400, 66]),
+    (18, 1, 128, 1, [17000]), (3, 1, 256, 1, [1500, 900]), (20, 1, 256, 1, [2100]), (5, 1, 256, 4, [1300]),
+    (20, 1, 64, 1, [4800, 300]), (10, 1, 64, 4, [1700]), (48, 2, 64, 1, [1100])])
+def test_quant_decode_many_pages_a_wave(Hq, H, d, Q, lens):
+    # each wave takes 4 to over 64 pages of one split: the sums between pages, keys and
+    # values in turn in one register set, the queries read again, in every instance
+    g = np.random.default_rng(Hq * 1000 + d + Q)
+    pool, table = _cache(g, lens, H, d)
+    q = (g.standard_normal((len(lens), Q, Hq, d)) * 2.0 ** g.uniform(-1, 1, (len(lens), Q, Hq, 1))).astype(np.float32)
+    _check_decode(q, pool, table, lens, H, 1 << 16)
+    if max(lens) < 5000:
+        _check_decode(q, pool, table, lens, H, 1024)
+
+
+@pytest.mark.parametrize("order", ["up", "down", "any"])
+@pytest.mark.parametrize("Hq, d, Q", [(2, 128, 1), (20, 128, 1), (3, 256, 2), (20, 64, 1)])
+def test_quant_decode_value_scales_by_page(Hq, d, Q, order):
+    # values of one page 2^60 times those of another: a wave's sums follow the largest
+    # weight x scale through its pages, whichever way they come
+    g = np.random.default_rng(Hq + d)
+    lens = [1900]
+    pool, table = _cache(g, lens, 1, d, spread=0.5)
+    n = table.shape[1]
+    shift = np.linspace(-30, 30, n).astype(np.int64)
+    shift = {"up": shift, "down": shift[::-1], "any": g.permutation(shift)}[order]
+    at = slice(128 * d + 64, 128 * d + 128)                # the value scales' bytes
+    pool[table[0], at] = (pool[table[0], at].astype(np.int64) + shift[:, None]).clip(15, 246).astype(np.uint8)
+    q = g.standard_normal((1, Q, Hq, d)).astype(np.float32)
+    for split in (1 << 16, 1024, 0):
+        _check_decode(q, pool, table, lens, 1, split)
+
+
+@pytest.mark.parametrize("Hq, H, d, Q, lens", [(64, 64, 64, 1, [9000, 64, 7000, 0, 2500]),
+                                               (64, 32, 128, 9, [20000, 1000, 13000])])
+def test_quant_decode_long_splits_are_cut_again(Hq, H, d, Q, lens):
+    # sequences whose shares of the chip are over 32 pages long: splits of 32.  Random
+    # bytes and scales; the heads compared are those at the ends and one between
+    from paper_2607_24331_amd import quant_decode
+    assert sum(-(-n // 64) for n in lens) * H > 512 * 32
+    gen, g = torch.Generator(device="cuda"), np.random.default_rng(H)
+    gen.manual_seed(H)
+    width = -(-max(lens) // 64)
+    pages = sum(-(-n // 64) for n in lens) + 2
+    cells = torch.randint(0, 256, (pages, H, 128 * d + 128), generator=gen, device="cuda", dtype=torch.uint8)
+    cells[(cells & 0x7F) == 0x7F] = 0x35
+    cells[..., 128 * d:] = 118 + cells[..., 128 * d:] % 4
+    ids, table, at = g.permutation(pages).astype(np.int32), np.full((len(lens), width), -1, np.int32), 0
+    for b, n in enumerate(lens):
+        table[b, :-(-n // 64)] = ids[at:at - (-n // 64)]
+        at -= -n // 64
+    q = (g.standard_normal((len(lens), Q, Hq, d)) * 2.0 ** -4).astype(np.float32)
+    args = cells.view(pages, -1), cu(table), cu(np.array(lens, np.int32)), width * 64, H
+    got = quant_decode(cu(q), *args)
+    assert torch.equal(got, quant_decode(cu(q), *args))
+    per = Hq // H
+    for h in (0, H // 3, H - 1):
+        heads = slice(h * per, (h + 1) * per)
+        want, mag, dot = sv.decode(q[:, :, heads], cells[:, h].cpu().numpy(), table, lens, 1)
+        err, tol = np.abs(host(got)[:, :, heads] - want), _decode_tol(d, max(lens), mag, dot)
+        assert np.all(err <= tol), (h, float((err / tol).max()))
 
 
 def test_quant_decode_missing_pages():
@@ -762,6 +932,35 @@ def test_decode_rotary(d, rot):
             # the bound that the rotary decode is held to: 2e-2 of the row's largest value
             assert np.max(np.abs(got[b, h] - ref)) <= 2e-2 * np.max(np.abs(ref)), (b, h)
     assert oattn is not None
+
+
+@pytest.mark.parametrize("rot", [1, 2, 7])
+@pytest.mark.parametrize("split, d", [(512, 128), (256, 64)])
+def test_decode_rotary_of_wide_groups(split, d, rot):
+    # groups wider than the kernel that keeps their factors resident takes
+    from gpu_common import TOL_REL_ROW, dev, gpu_pool_with_append, plan_for, row_rel_err, seq_latents
+    from oracle.bookkeeping import book_for
+    from paper_2607_24331_amd import decode_rotary
+    from test_gpu_rope import _wide_inputs
+    wl, inp = _wide_inputs(d)
+    plan, bk = plan_for(wl, split), book_for(wl)
+    r, theta, layout, m = _rotation(d, ROTS[rot])
+    got = host(decode_rotary(plan, torch.from_numpy(np.ascontiguousarray(inp.q)).cuda(), gpu_pool_with_append(inp, plan),
+                             cu(inp.page_table), cu(inp.seq_lens), int(max(wl.seq_lens)), dev(inp.R_keys_flat, "bf16"),
+                             dev(inp.R_value, "bf16"), r))
+    for b in range(wl.batch):
+        Zk, Zv = seq_latents(inp, b)
+        T = Zk.shape[0]
+        for kv in range(wl.num_kv_heads):
+            g, j = bk.group_of_kv[kv], bk.pos_in_group[kv]
+            K = Zk[:, bk.koff[g]:bk.koff[g] + bk.ranks[g]].astype(np.float64) @ inp.R_blocks[g][:, j * d:(j + 1) * d].astype(np.float64)
+            V = Zv.astype(np.float64) @ inp.R_value[:, kv * d:(kv + 1) * d].astype(np.float64)
+            K = sv.turn(K[:, None], np.arange(T), theta, layout, m)[:, 0]
+            for h in (2 * kv, 2 * kv + 1):
+                qt = sv.turn(inp.q[b, h].astype(np.float64)[None, None], [T - 1], theta, layout, m)[0, 0]
+                s = K @ qt / np.sqrt(d)
+                p = np.exp(s - s.max())
+                assert row_rel_err(got[b, h], p @ V / p.sum()) <= TOL_REL_ROW, (b, h)
 
 
 # -------------------------------------------------------- a serving loop of them
