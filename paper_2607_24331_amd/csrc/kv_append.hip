@@ -730,13 +730,22 @@ int heads_for(int64_t blocks, int n_heads, int64_t target) {
 }
 
 // Whether the 8-bit values of a call are cut at pages, in the launch's first work-groups
-// (they are the longer ones).  Appends in a graph, back to back, against blocks like the
-// keys': 4093 tokens of 32 heads 24 us and 48 (26.5 with the keys first, 33 in two launches),
-// 8192 of 8 heads in five runs 17 and 28, 256 of 32 heads 5.8 and 8.8.  Where no page's run is
-// long it loses (1024 tokens of 8 heads at random 18 and 13.5), and so do few rows, which
-// cannot hide what a cut leaves over (256 tokens of 16 heads in five runs 8.1 and 6.4).  Reads
-// of the same: 22 and 36, 16 and 21, 5.7 and 5.3, 12 and 7.
-bool by_pages(int n_tok, int kv_heads) { return n_tok >= 256 && int64_t(n_tok) * kv_heads >= 8192; }
+// (they are the longer ones).  Back to back in a graph, us cut at pages and in blocks like
+// the keys', d = 128: one run of slots, five runs that begin inside pages, slots at random:
+//   append   256 x 16 heads   5.2  5.4     7.2  5.7    12.9  8.4
+//           1024 x  8         5.4  7.6     7.2  7.7    15.9 12.1
+//           2048 x  8         6.2 11.7     8.1 12.4    22.7 17.8
+//           4093 x 32        21.4 39.5    26.4 41.9     106   97
+//   read    1024 x  8         5.7  5.3     7.0  5.6    11.5  6.8
+//           2048 x  8         6.9  7.0     8.1  8.1    17.7 10.8
+//           4096 x  8         8.4 11.3    10.0 13.0    22.3 18.3
+//           4093 x 32        20.9 40.7    25.7 39.5      76   65
+// and 1024 x 8 heads of 64, appended 5.0 and 5.1, 6.8 and 5.2, 12.5 and 7.8.  The host does not
+// see the slots: prompts decide, and steps of so many single tokens pay.
+bool by_pages(int n_tok, int kv_heads, int head_dim, bool read) {
+  const int64_t rows = int64_t(n_tok) * kv_heads;
+  return n_tok >= 256 && rows >= 8192 && rows * head_dim >= (read ? 1 << 21 : 1 << 20);
+}
 
 template <typename T, int D, bool QUANT>
 hipError_t launch_append_t(int kv_heads, const void* k, const void* v, RowStrides ks, RowStrides vs,
@@ -755,7 +764,7 @@ hipError_t launch_append_t(int kv_heads, const void* k, const void* v, RowStride
     return hipGetLastError();
   };
   if constexpr (QUANT) {
-    if (by_pages(n_tok, kv_heads)) {
+    if (by_pages(n_tok, kv_heads, D, false)) {
       const PagedSpans ps(n_tok, R);
       const int hb = heads_for(blocks, kv_heads, kKeyGroups), vhb = heads_for(ps.main, kv_heads, kValueGroups);
       const int64_t value_items = int64_t(ps.main + ps.rest) * ((kv_heads + vhb - 1) / vhb);
@@ -788,7 +797,7 @@ hipError_t launch_read_t(int kv_heads, const void* pool, int64_t num_pages, cons
                        static_cast<T*>(v));
     return hipGetLastError();
   };
-  if (by_pages(n_tok, kv_heads)) {
+  if (by_pages(n_tok, kv_heads, D, true)) {
     const int R = Block<D>::kRows;
     const PagedSpans ps(n_tok, R);
     const int64_t blocks = (n_tok + R - 1) / R;

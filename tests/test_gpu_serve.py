@@ -395,6 +395,13 @@ def test_quant_append_of_runs_in_one_call(n, H, d, dtype, first):
         assert np.array_equal(host(got)[some], np.where(live[:, None, None], sv.E4M3[b] * 2.0 ** e[..., None], 0))
 
 
+@pytest.mark.parametrize("n, H, d", [(2060, 8, 128), (4100, 8, 64), (1030, 33, 128), (16500, 1, 64)])
+@pytest.mark.parametrize("first", [0, 37])
+def test_quant_append_of_long_runs_in_one_call(n, H, d, first):
+    # where reads are cut at pages too, and just below
+    test_quant_append_of_runs_in_one_call(n, H, d, BF16, first)
+
+
 @pytest.mark.parametrize("rot", range(len(ROTS)))
 @pytest.mark.parametrize("n, H, d, run", [(1, 1, 64, 1), (70, 3, 128, 33), (40, 2, 256, 40)])
 def test_appends_turn_keys(n, H, d, run, rot):
