@@ -45,20 +45,26 @@ def _count(value, name: str):
 
 def _width(page_table: torch.Tensor, B: int) -> int:
     """Pages a row of the page table of B sequences."""
-    if not isinstance(page_table, torch.Tensor):
-        raise TypeError("page_table must be a torch tensor")
-    if page_table.dim() != 2 or page_table.shape[0] != B:
+    try:
+        own, width = page_table.shape
+    except AttributeError:
+        raise TypeError("page_table must be a torch tensor") from None
+    except ValueError:
+        own = -1
+    if own != B:
         raise ValueError("page_table must be [batch, max_pages]")
-    return _count(page_table.shape[1], "max_pages")
+    return width if width <= _INT32_MAX else _count(width, "max_pages")
 
 
 def _capacity(free_pages: torch.Tensor) -> int:
     """Places of a stack of free pages."""
-    if not isinstance(free_pages, torch.Tensor):
-        raise TypeError("free_pages must be a torch tensor")
-    if free_pages.dim() != 1:
-        raise ValueError("free_pages must be a vector")
-    return _count(free_pages.shape[0], "the capacity of free_pages")
+    try:
+        capacity, = free_pages.shape
+    except AttributeError:
+        raise TypeError("free_pages must be a torch tensor") from None
+    except ValueError:
+        raise ValueError("free_pages must be a vector") from None
+    return capacity if capacity <= _INT32_MAX else _count(capacity, "the capacity of free_pages")
 
 
 def _vector(t: torch.Tensor, name: str, dtype, n: int, index: Optional[int] = None) -> int:
@@ -78,7 +84,7 @@ def _heads(t: torch.Tensor, name: str, index: Optional[int] = None):
     strides = t.stride()
     if len(strides) != 3:
         raise ValueError(f"{name} must be [tokens, heads, head_dim]")
-    if max(t.shape) > _INT32_MAX:
+    if t.numel() > _INT32_MAX and max(t.shape) > _INT32_MAX:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, sizes that do not fit 32 bits")
     p = _gpu(t, name, t.dtype, index, False)
     st, sh, sd = strides
