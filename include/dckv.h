@@ -540,8 +540,10 @@ int dckv_quant_read(int32_t num_kv_heads, int32_t head_dim, const void* pool, in
  * every position up to its own; one that sees none gets zeros, as does a
  * sequence of length 0.  Page-table entries outside [0, num_pages) are empty
  * pages.  Whatever lies in slots that a query does not see (NaN included) does
- * not reach its result.  Products are taken in f16 halves of the fp32 queries
- * and weights (22 bits and more) and summed in fp32.
+ * not reach its result; a NaN in one that it sees does, however small its weight.
+ * Products are taken in f16 halves of the fp32 queries and weights (22 bits and
+ * more) and summed in fp32: sums over tokens of 2^(score - greatest) |v| beyond
+ * it (infinities that were appended count as 448 * 2^119) are infinite.
  * split_tokens: context tokens a work split, a multiple of 64, or 0 to choose
  * from the shape.  A workspace (256-byte aligned; its contents do not matter) of
  * dckv_quant_workspace_bytes also serves fewer sequences and shorter contexts;

@@ -5,18 +5,20 @@
 // append_rows  d/8 lanes hold a row, 8 columns each, in fp32.
 //   Keys (and values of bf16 pages): a lane group walks over the heads of one token with
 //   the next heads' rows on their way, and turns them by factors that stay in
-//   registers; a plane's other coordinate comes from the lane that holds it.  For e4m3 the row's maximum gives the exponent, exact in
-//   integer arithmetic on the maximum's bits; the conversion is the hardware's
-//   round-to-nearest-even after an exact multiplication by 2^-e.  Key bytes go out 8 at
-//   a time, 16 columns of a token side by side in the page.
+//   registers; a plane's other coordinate comes from the lane that holds it.  For e4m3
+//   the row's maximum gives the exponent, exact in integer arithmetic on the maximum's
+//   bits; the conversion is the hardware's round-to-nearest-even after an exact
+//   multiplication by 2^-e.  Key bytes go out 8 at a time, 16 columns of a token side by
+//   side in the page.
 //   e4m3 values: a column holds a page's tokens side by side (slots 4a .. 4a + 3 in one
 //   dword, four of those in 16 bytes), so a lane group takes four rows that fill such a
 //   dword, transposes their bytes in registers and puts them into a tile in LDS, which
 //   goes out in 16-byte pieces; other rows (single tokens) go out as bytes.
 // read_rows  the same units the other way.
 // Each element is read once and written once: memory bounds long prompts, latency single
-// tokens.  4,093 tokens of 32 heads of 128, back to back in a graph: 22 us (101 MB,
-// 4.6 TB/s), read back 22; 64 tokens of 8 heads: 4.7 us and 3.7.
+// tokens.  4,093 tokens of 32 heads of 128, turned, back to back in a graph: 22.8 us (101
+// MB, 4.4 TB/s), read back 21.3, into bf16 pages 22.2; 64 tokens of 8 heads 4.9, 3.8 and
+// 3.6.  A kernel alone, by its trace: 23.2 and 19.4 us, and 5.8 and 4.4 for 64 tokens.
 #include <algorithm>
 
 #include "rotary.h"
@@ -25,13 +27,14 @@ namespace dckv {
 namespace {
 
 constexpr int kMaxRows = 128;             // tokens a work-group
-constexpr int kAhead = 4;                 // heads whose rows are on their way to a lane group: 27.5 us for
-                                          // 4093 x 32 rows (a call), 28.5 with 2
+constexpr int kAhead = 4;                 // heads whose rows are on their way to a lane group: 22.8 us for
+                                          // 4093 x 32 rows in a graph, 23.6 with 2
 // Work-groups that a part of a call aims for.  An append forms angles or finds units once
-// for the heads of a work-group, a read has less to share: 4093 x 32 rows took 28.5 us (a
-// call) with 1024 for the keys and 512 for the values, 31 with 1024 both, 32.5 with 512 both and
-// 34 with 2048 both; into bf16 pages 27.5 with 512 to 2048; read back 19.8 with 2048 for
-// the keys and 512 for the values, 21.7 with 1024 and 23.8 with 2048 for these.
+// for the heads of a work-group, a read has less to share: 4093 x 32 rows, in a graph, take
+// 22.8 us with 1024 for the keys and 512 for the values, 23.8 with 1024 both, 24.1 with 512
+// both and 27.8 with 2048 both; into bf16 pages 22.2 with 512 or 1024, 23.6 with 2048; read
+// back 21.3 with 2048 for the keys and 512 for the values, 22.1 with 1024 for either and 25.0
+// with 2048 for both.
 constexpr int64_t kKeyGroups = 1024;
 constexpr int64_t kValueGroups = 512;
 constexpr int64_t kReadGroups = 2048;
@@ -289,7 +292,8 @@ struct AppendBlock {
 
 // Keys, and values of bf16 pages: a row a group of lanes, head after head.  The sines
 // and cosines of a lane's columns are formed once and stay in registers (a table in LDS
-// for whole blocks of tokens was slower: 21 us against 17 for 4093 tokens of 32 heads).
+// for whole blocks of tokens was slower: the keys of 4093 tokens of 32 heads took 21 us
+// against 17).
 template <typename T, int D, bool QUANT>
 __device__ __forceinline__ void append_by_row(const AppendBlock<T>& b, const RotaryTable& rot,
                                               const int64_t* slot, int64_t n_slots,

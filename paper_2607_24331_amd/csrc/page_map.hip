@@ -14,6 +14,9 @@
 //                from the table that map_sequences wrote.
 // All numbers are small: the calls are bound by launches and a few dependent loads.
 // One new token of 64 sequences: 5.1 us on the GPU; 53,000 rows of 48 prompts: 7.9 + 4.2.
+// release_pages  one work-group, a wave a sequence in turn, which counts the row's live ids
+//                and then, its places known, writes them: one sequence of 512 pages of 64
+//                takes 21 us, all 64 40, 256 of 128 pages 39, 1,024 of 128 pages 98.
 #include <algorithm>
 
 #include "device.h"

@@ -21,12 +21,14 @@
 //           product from the registers they were made in: no LDS, no shuffle.
 // A wave's values are loaded when its keys are used up and the next page's keys when
 // the values are, into the same registers; three waves a SIMD (two of the wide shapes)
-// keep the memory busy meanwhile.
+// keep the memory busy meanwhile.  Two shapes need more than their 256 registers: two tiles
+// at d = 128 spill 19 (80 bytes a lane, some of them in the page loop), d = 256 spills 3.
 // Reads 2 d + 2 bytes a token and KV head; bound by those bytes as long as the
 // rows fit one 16-row tile: 131,072 tokens of 32 heads of 128, four queries, 164 us
 // (6.6 TB/s); 64 sequences of 1,024 to 8,192 tokens 392 us (6.2 TB/s); 4 x 32,768 tokens
-// of 8 heads 47 us (5.8 TB/s) and 4 for the join.  64 rows a KV head: 100 to 126 us there,
-// matrix products and softmax.
+// of 8 heads 47 us (5.8 TB/s) and 4 for the join; of 256, 99 us a call (5.4 TB/s).  More rows
+// a KV head are bound by conversions, softmax and products: 32 of them 77 us a call there
+// and 64 128, where the bytes take 45; at d = 256 32 take 178.
 //   merge   one work-group per (query, head, sequence), a log-sum-exp sum in a fixed
 //           order.
 #include <algorithm>
@@ -53,7 +55,10 @@ constexpr int kWaves = 4;
 constexpr int kFill = 512;
 constexpr int kMost = 4096;                // work-groups that long splits are cut into
 constexpr int kLongPages = 32;
-constexpr int32_t kMaxBalanced = 256;      // sequences that are cut by their lengths
+// Sequences that are cut by their lengths: four a lane of a wave.  More are cut as if all had
+// the longest context: 256 of 1 to 4,096 tokens, 8 heads, take 200 us (5.5 TB/s), 257 of them
+// 229 (4.9); of 4,096 tokens each 368 and 376.
+constexpr int32_t kMaxBalanced = 256;
 constexpr int kTop = 14;                   // split operands lie below 2^kTop
 
 __device__ __forceinline__ floatx4 mfma(u32x4 a, u32x4 b, floatx4 c) {
@@ -687,7 +692,9 @@ QuantShape quant_shape(int32_t q_heads, int32_t kv_heads, int32_t head_dim, int3
   s.max_context = max_context;
   s.rows = queries * (q_heads / kv_heads);
   // 17 rows and more share a page's conversions, two 16-row tiles a work-group; at d =
-  // 256 a second tile's sums do not fit the registers of two waves a SIMD
+  // 256 a second tile's sums do not fit the registers of two waves a SIMD.  4 x 32,768 tokens
+  // of 8 heads of 128, 32 rows: 80 us and 91 with a tile a work-group (of 64: 50 and 52), 64
+  // rows 132 and 147; a little work loses, 64 x 2,048 tokens of one head with 32 rows 34 and 26
   s.tiles = (s.rows > 16 && head_dim < 256) ? 2 : 1;
   s.slices = (s.rows + 16 * s.tiles - 1) / (16 * s.tiles);
   const int64_t pages = pages_of(max_context), shares = int64_t(kv_heads) * s.slices;

@@ -211,7 +211,8 @@ class Rotary:
     by default) in planes paired by `layout` ("half": (i, i + rotary_dim/2),
     "interleaved": (2i, 2i + 1)), by angles position * base^(-2i/rotary_dim),
     scaled for long contexts by `scaling` ("none", "linear", "base", "turns",
-    "planes"; include/dckv.h gives the formulas), times `magnitude`."""
+    "planes"; include/dckv.h gives the formulas), times `magnitude` (0 counts
+    as 1)."""
 
     def __init__(self, head_dim: int, rotary_dim: Optional[int] = None, layout: str = "half",
                  base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
