@@ -288,7 +288,7 @@ def test_rotary_in_an_autograd_function():
 
         @staticmethod
         def backward(ctx, grad):
-            return rotary(r, grad, at, inverse=True)
+            return rotary(r, grad.contiguous(), at, inverse=True)
 
     x, w = g.standard_normal((7, 1, 64)).astype(np.float32), g.standard_normal((7, 3, 64)).astype(np.float32)
     leaf = cu(x).requires_grad_()
@@ -306,6 +306,13 @@ def test_rotary_in_an_autograd_function():
     assert np.all(np.abs(host(leaf.grad) - z.grad.numpy()) <= tol + 1e-40)
     with pytest.raises(ValueError, match="autograd"):
         rotary(r, leaf, at)
+    # the gradient of a plain sum is one number broadcast: not a head's coordinates in a row
+    leaf.grad = None
+    Turn.apply(leaf).sum().backward()
+    ones = torch.ones((7, 1, 64), device="cuda")
+    assert torch.equal(leaf.grad, rotary(r, ones, at, inverse=True))
+    with pytest.raises(ValueError, match="coordinates"):
+        rotary(r, ones[:1, :, :1].expand(7, 1, 64), at)
 
 
 # --------------------------------------------------------------------- appends
