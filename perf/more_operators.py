@@ -1,0 +1,457 @@
+"""The operators of the joint-latent cache, as cases to be timed.
+
+The cache keeps one latent c of width `rank` and one position key of width
+`rope_dim` a token, shared by all heads: head h's key is [W_keys[h] c, key], its
+value W_values[h] c.  A serving program writes new tokens into its pages in
+bf16 or e4m3 (`joint_append`, read back by `joint_read`), decodes over them in
+the absorbed form, with or without a prefix that the batch shares
+(`joint_decode`), and runs prompts in the expanded form (`joint_prefill`).
+Layers are this repository's (tiny 8 x 64, 32 x 128) at its contexts; `draw`
+gives more of the same ranges.
+
+With `own` false `run` computes the plain form: elementary torch operations in
+32 bits (angles in 64), from the page layouts that include/dckv.h documents.
+`exact` computes the same from the definitions in 64 bits, the decode in the
+expanded form and the prompts in the absorbed one.
+"""
+
+from __future__ import annotations
+
+import functools
+import math
+import random
+
+import torch
+
+own = False
+PAGE = 64
+
+# ---------------------------------------------------------------- the layers
+_TINY = dict(heads=8, head_dim=64, rank=128, rope_dim=0)
+_SMALL = dict(heads=16, head_dim=64, rank=256, rope_dim=32)
+_LAYER = dict(heads=32, head_dim=128, rank=512, rope_dim=64)
+
+
+def listed():
+    """The listed cases.  Lengths named (min, max) are drawn uniformly between
+    the two by lens_seed, one a sequence."""
+    return [
+        # a decode step writes one token of each of 64 sequences into 8-bit pages, read back
+        dict(name="append_step_b64", kind="append", cache="e4m3", tokens=64, run=1, dtype="bf16",
+             layout="interleaved", **_LAYER),
+        # a whole prompt, not a multiple of any tile, into 8-bit pages, read back
+        dict(name="append_prompt_8191", kind="append", cache="e4m3", tokens=8191, run=8191, dtype="bf16",
+             layout="interleaved", **_LAYER),
+        # a chunk of a long prompt into bf16 pages
+        dict(name="append_chunk_512", kind="append", cache="bf16", tokens=512, run=512, dtype="f32",
+             layout="half", **_SMALL),
+        # the smallest attention: a small layer without positions, one short sequence; bound by latency
+        dict(name="decode_tiny_t256", kind="decode", cache="bf16", batch=1, context_min=256, context_max=256,
+             queries=1, prefix=0, lens_seed=1, **_TINY),
+        # four long contexts
+        dict(name="decode_b4_t32k", kind="decode", cache="bf16", batch=4, context_min=32768, context_max=32768,
+             queries=1, prefix=0, lens_seed=2, **_LAYER),
+        # a deep batch of ragged contexts in 8 bits, pages anywhere in the pool
+        dict(name="decode_ragged_b64", kind="decode", cache="e4m3", batch=64, context_min=1024, context_max=8192,
+             queries=1, prefix=0, lens_seed=3, **_LAYER),
+        # four causal queries of one very long sequence: speculative verification
+        dict(name="decode_q4_t128k", kind="decode", cache="bf16", batch=1, context_min=131072,
+             context_max=131072, queries=4, prefix=0, lens_seed=4, **_LAYER),
+        # 64 answers to one long document, each some way into its own text
+        dict(name="prefix_16k_b64", kind="decode", cache="bf16", batch=64, context_min=1, context_max=1024,
+             queries=1, prefix=16384, lens_seed=5, **_LAYER),
+        # a few samples of one prompt that ends inside a page, in 8 bits
+        dict(name="prefix_4093_b8", kind="decode", cache="e4m3", batch=8, context_min=1, context_max=300,
+             queries=1, prefix=4093, lens_seed=6, **_SMALL),
+        # two short prompts: bound by latency
+        dict(name="prompt_short_b2", kind="prompt", cache="bf16", batch=2, cached_min=0, cached_max=0,
+             added_min=77, added_max=130, pad_rows=0, lens_seed=7, **_SMALL),
+        # prompts and chunks of prompts of uneven lengths packed into one batch, a padded tail
+        dict(name="prompt_packed_b16", kind="prompt", cache="e4m3", batch=16, cached_min=0, cached_max=3000,
+             added_min=1, added_max=1024, pad_rows=77, lens_seed=8, **_LAYER),
+        # one long prompt, not a multiple of any tile
+        dict(name="prompt_8191", kind="prompt", cache="bf16", batch=1, cached_min=0, cached_max=0,
+             added_min=8191, added_max=8191, pad_rows=0, lens_seed=9, **_LAYER),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    """One more case: the listed kinds, 1 to 8191 tokens written, contexts of 1
+    to 131072 tokens of 1 to 64 sequences, one to eight queries a sequence, shared
+    prefixes of 1 to 16384 tokens, prompts of 1 to 8191 tokens, 1 to 64 heads."""
+    kind = rng.choice(["append", "append", "decode", "decode", "prefix", "prefix", "prompt", "prompt"])
+    layer = dict(heads=rng.choice([1, 5, 8, 16, 16, 32, 32, 64]), head_dim=rng.choice([64, 128]),
+                 rank=rng.choice([128, 256, 512]), rope_dim=rng.choice([0, 32, 64, 64]),
+                 cache=rng.choice(["bf16", "e4m3"]), lens_seed=rng.randrange(1 << 20))
+    if kind == "append":
+        tokens = _log_int(rng, 1, 8191)
+        return dict(kind="append", tokens=tokens, run=rng.choice([1, tokens, rng.randint(1, tokens)]),
+                    dtype=rng.choice(["bf16", "bf16", "f32"]), layout=rng.choice(["half", "interleaved"]), **layer)
+    if kind == "prompt":
+        batch = _log_int(rng, 1, 16)
+        top = min(8191, 16384 * 16 // (batch * max(layer["heads"], 16)))
+        added, cached = _log_int(rng, 1, top), rng.choice([0, _log_int(rng, 1, top)])
+        return dict(kind="prompt", batch=batch, cached_min=0, cached_max=cached,
+                    added_min=rng.choice([0, 1, added]), added_max=added, pad_rows=rng.choice([0, rng.randint(1, 99)]),
+                    **layer)
+    batch = _log_int(rng, 1, 64)
+    queries = rng.choice([1, 1, 1, 2, 3, 4, 8]) if layer["heads"] <= 16 or batch <= 4 else 1
+    # at most the tokens x rows of the largest listed cases
+    top = max(64, min(131072 if kind == "decode" else 1024, 131072 * 128 // (batch * max(32, queries * layer["heads"]))))
+    longest = _log_int(rng, 1, top)
+    prefix = 0
+    if kind == "prefix":
+        prefix = _log_int(rng, 1, min(16384, 16384 * 2048 // (batch * queries * layer["heads"])))
+    return dict(kind="decode", batch=batch, context_min=rng.choice([0, longest, (longest + 1) // 2]),
+                context_max=longest, queries=queries, prefix=prefix, **layer)
+
+
+# ------------------------------------------------------------------- sizes
+def _lens(lo, hi, n, seed):
+    r = random.Random(seed)
+    got = [r.randint(lo, hi) for _ in range(n)]
+    if got:
+        got[-1] = hi                       # the longest is always there
+    return got
+
+
+def _prompt_lens(case):
+    cached = _lens(case["cached_min"], case["cached_max"], case["batch"], case["lens_seed"])
+    added = _lens(case["added_min"], case["added_max"], case["batch"], case["lens_seed"] + 1)
+    return cached, added
+
+
+def _scale(case):
+    return 1.0 / math.sqrt(case["head_dim"] + case["rope_dim"])
+
+
+_DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+_SIZE = {"f32": 4, "bf16": 2}
+
+
+def work(case):
+    """Bytes and operations of one pass: every input read once, every output
+    written once."""
+    r, p, H, d = case["rank"], case["rope_dim"], case["heads"], case["head_dim"]
+    if case["kind"] == "append":
+        n = case["tokens"]
+        # e4m3: written as bytes with two scale bytes, then read back and given out as bf16
+        out = 2 * (r + p) if case["cache"] == "bf16" else 2 * (r + p + 2) + 2 * (r + p)
+        return {"bytes": n * ((r + p) * _SIZE[case["dtype"]] + out + 12),
+                "flops": n * (3 * p + (6 * (r + p) if case["cache"] == "e4m3" else 0))}
+    token = 2 * (r + p) if case["cache"] == "bf16" else r + p + 2
+    factors = 4 * H * d * r
+    if case["kind"] == "decode":
+        lens = _lens(case["context_min"], case["context_max"], case["batch"], case["lens_seed"])
+        rows = case["queries"] * H
+        tokens = sum(lens) + case["prefix"]
+        pairs = rows * (sum(lens) + case["batch"] * case["prefix"])
+        return {"bytes": tokens * token + tokens // 16 + factors + case["batch"] * rows * 2 * (2 * d + p),
+                "flops": 2 * pairs * (2 * r + p) + 4 * case["batch"] * rows * d * r}
+    cached, added = _prompt_lens(case)
+    tokens = sum(cached) + sum(added)
+    pairs = sum(a * c + a * (a + 1) // 2 for c, a in zip(cached, added))
+    return {"bytes": tokens * token + factors + sum(added) * H * 2 * (2 * d + p),
+            "flops": 4 * tokens * r * d * H + 2 * pairs * H * (2 * d + p)}
+
+
+# ----------------------------------------------------------------- prepare
+def _pool(case, pages, g):
+    """Pages filled with latents and keys of about unit size, as the append leaves them."""
+    width = case["rank"] + case["rope_dim"]
+    some = min(pages, 512)
+    pick = torch.randint(0, some, (pages,), generator=g, device="cuda")
+    if case["cache"] == "bf16":
+        return torch.randn(some, PAGE * width, generator=g, device="cuda").to(torch.bfloat16)[pick]
+    block = torch.randn(some, PAGE * width, generator=g, device="cuda").mul_(110.0).clamp_(-448.0, 448.0)
+    pool = torch.empty(pages, PAGE * (width + 2), dtype=torch.uint8, device="cuda")
+    pool[:, :PAGE * width] = block.to(torch.float8_e4m3fn).view(torch.uint8)[pick]
+    pool[:, PAGE * width:] = torch.randint(119, 122, (pages, 2 * PAGE), generator=g, device="cuda", dtype=torch.uint8)
+    return pool
+
+
+def prepare(case, seed):
+    """The inputs in hand before the call, on the GPU, from the seed."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    i32 = functools.partial(torch.tensor, dtype=torch.int32, device="cuda")
+    rnd = lambda *shape: torch.randn(shape, generator=g, device="cuda")  # noqa: E731
+    r, p, H, d = case["rank"], case["rope_dim"], case["heads"], case["head_dim"]
+    if case["kind"] == "append":
+        n = case["tokens"]
+        x = rnd(n, r + p + 64).to(_DT[case["dtype"]])          # the down-projection's latent and key, among more
+        runs = -(-n // case["run"])
+        pages_run = -(-case["run"] // PAGE) + 1
+        pages = runs * pages_run
+        perm = torch.randperm(pages, generator=g, device="cuda")
+        row = torch.arange(n, device="cuda")
+        start = torch.randint(0, PAGE, (runs,), generator=g, device="cuda")
+        at = start[row // case["run"]] + row % case["run"]
+        slot = perm[(row // case["run"]) * pages_run + at // PAGE] * PAGE + at % PAGE
+        base = torch.randint(0, 131072 - case["run"], (runs,), generator=g, device="cuda")
+        pos = (base[row // case["run"]] + row % case["run"]).to(torch.int32)
+        if case["cache"] == "bf16":
+            pool = torch.zeros(pages, PAGE * (r + p), dtype=torch.bfloat16, device="cuda")
+        else:
+            pool = torch.zeros(pages, PAGE * (r + p + 2), dtype=torch.uint8, device="cuda")
+        return dict(case=case, c=x[:, :r], k=x[:, r:r + p] if p else None, slot=slot, position=pos, pool=pool)
+    wk = (rnd(H, d, r) / math.sqrt(r)).to(torch.bfloat16)
+    wv = (rnd(H, d, r) / math.sqrt(r)).to(torch.bfloat16)
+    B = case["batch"]
+    if case["kind"] == "decode":
+        lens, top = _lens(case["context_min"], case["context_max"], B, case["lens_seed"]), case["context_max"]
+        q = rnd(B, case["queries"], H, d + p).to(torch.bfloat16)
+    else:
+        cached, added = _prompt_lens(case)
+        lens = [c + a for c, a in zip(cached, added)]
+        top = max(lens)
+        q = rnd(sum(added) + case["pad_rows"], H, d + p).to(torch.bfloat16)
+    width = max(1, -(-top // PAGE))
+    shared = -(-case.get("prefix", 0) // PAGE)
+    perm = torch.randperm(B * width + shared, generator=g, device="cuda").to(torch.int32)
+    st = dict(case=case, q=q, wk=wk, wv=wv, pool=_pool(case, B * width + shared, g),
+              table=perm[shared:].view(B, width).contiguous(), lens=i32(lens), top=top)
+    if case["kind"] == "decode":
+        return dict(st, prefix=perm[:shared].contiguous() if shared else None)
+    start = [sum(added[:b]) for b in range(B + 1)]
+    return dict(st, cached=cached, added=added, row_start=i32(start), total=sum(lens), out=torch.zeros_like(q[..., :d]))
+
+
+# --------------------------------------------------------- the plain forms
+def _turn(case, x, position):
+    """The rotation in 32 bits of x [n, p], all coordinates, base 10000."""
+    p = case["rope_dim"]
+    theta = 10000.0 ** (-torch.arange(0, p, 2, dtype=torch.float64, device=x.device) / p)
+    angle = position.double()[:, None] * theta
+    c, s = angle.cos().float(), angle.sin().float()
+    x = x.float()
+    if case["layout"] == "half":
+        a, b = x[:, :p // 2], x[:, p // 2:]
+        return torch.cat([a * c - b * s, b * c + a * s], -1)
+    a, b = x[:, 0::2], x[:, 1::2]
+    return torch.stack([a * c - b * s, b * c + a * s], -1).flatten(1)
+
+
+def _plain_quantized(x):
+    """x [n, w] in 32 bits to e4m3 values and exponents: the least power of two
+    that brings the row's largest magnitude to at most 448."""
+    frac, e = torch.frexp(x.abs().amax(-1, keepdim=True))
+    e = torch.where(frac <= 0.875, e - 9, e - 8).clamp(-112, 119)
+    return torch.ldexp(x, -e).clamp(-448.0, 448.0).to(torch.float8_e4m3fn), e
+
+
+def _plain_append(st):
+    case, pool, slot = st["case"], st["pool"], st["slot"]
+    r, p = case["rank"], case["rope_dim"]
+    parts = [st["c"].float()] + ([_turn(case, st["k"], st["position"])] if p else [])
+    page, s = slot // PAGE, slot % PAGE
+    if case["cache"] == "bf16":
+        pool.view(-1, PAGE, r + p)[page, s] = torch.cat(parts, -1).to(torch.bfloat16)
+        return dict(pool=pool)
+    n, out = pool.shape[0], []
+    cells = pool[:, :PAGE * (r + p)].view(n, PAGE, r + p)
+    for i, x in enumerate(parts):
+        q8, e = _plain_quantized(x)
+        cells[page, s, i * r:i * r + x.shape[1]] = q8.view(torch.uint8)
+        pool[page, PAGE * (r + p + i) + s] = (e[:, 0] + 127).to(torch.uint8)
+        # what a reader of the pages finds there
+        out.append(torch.ldexp(q8.float(), e).to(torch.bfloat16))
+    return dict(c=out[0], k=out[1] if p else None)
+
+
+def _tokens(case, pool, ids):
+    """Latents and keys [..., 64 a page, r + p] in 32 bits of the pages `ids` [..., n]."""
+    r, p = case["rank"], case["rope_dim"]
+    got = pool[ids.long().reshape(-1)]
+    if case["cache"] == "bf16":
+        x = got.float()
+    else:
+        n = got.shape[0]
+        x = got[:, :PAGE * (r + p)].contiguous().view(torch.float8_e4m3fn).float().view(n, PAGE, r + p)
+        e = got[:, PAGE * (r + p):].view(n, 2, PAGE).int() - 127
+        one = torch.ones((), device=pool.device)
+        x = torch.cat([x[..., :r] * torch.ldexp(one, e[:, 0])[..., None], x[..., r:] * torch.ldexp(one, e[:, 1])[..., None]], -1)
+    return x.view(*ids.shape[:-1], ids.shape[-1] * PAGE, r + p)
+
+
+def _plain_decode(st):
+    case = st["case"]
+    r, p, H, d, n = case["rank"], case["rope_dim"], case["heads"], case["head_dim"], case["prefix"]
+    B, Q = st["q"].shape[:2]
+    q = st["q"].float()
+    qa = torch.matmul(q[..., :d].permute(2, 0, 1, 3).reshape(H, B * Q, d), st["wk"].float())
+    qa = torch.cat([qa.view(H, B, Q, r).permute(1, 2, 0, 3), q[..., d:]], -1).reshape(B, Q * H, r + p) * _scale(case)
+    own_ctx = _tokens(case, st["pool"], st["table"])
+    s = torch.matmul(qa, own_ctx.transpose(1, 2))
+    last = (st["lens"].long()[:, None] - Q + torch.arange(Q, device="cuda")).repeat_interleave(H, 1)[..., None]
+    s = s.masked_fill(torch.arange(s.shape[-1], device="cuda") > last, -math.inf)
+    if n:
+        pre = _tokens(case, st["pool"], st["prefix"])[:n]
+        sp = torch.matmul(qa.view(B * Q * H, r + p), pre.t()).view(B, Q * H, n)
+        s = torch.cat([sp.masked_fill(torch.arange(n, device="cuda") > n + last, -math.inf), s], -1)
+    w = (s - s.amax(-1, keepdim=True).clamp(min=-3e38)).exp()
+    a = torch.matmul(w[..., n:], own_ctx[..., :r])
+    if n:
+        a = a + torch.matmul(w[..., :n].reshape(B * Q * H, n), pre[:, :r]).view(B, Q * H, r)
+    a = a / w.sum(-1, keepdim=True).clamp(min=1e-30)
+    o = torch.matmul(a.view(B * Q, H, r).transpose(0, 1), st["wv"].float().transpose(1, 2))
+    return o.transpose(0, 1).reshape(B, Q, H, d).to(torch.bfloat16)
+
+
+def _plain_prompt(st):
+    case = st["case"]
+    r, H, d = case["rank"], case["heads"], case["head_dim"]
+    out, at = torch.zeros_like(st["out"]), 0
+    wk, wv = st["wk"].float(), st["wv"].float()
+    for b, (c, a) in enumerate(zip(st["cached"], st["added"])):
+        if a == 0:
+            continue
+        x = _tokens(case, st["pool"], st["table"][b, :-(-(c + a) // PAGE)])[:c + a]
+        q = st["q"][at:at + a].float().transpose(0, 1) * _scale(case)
+        hidden = torch.arange(c + a, device="cuda") > torch.arange(c, c + a, device="cuda")[:, None]
+        for h in range(0, H, 8):                      # some heads at a time: their scores fit
+            k = torch.matmul(x[:, :r], wk[h:h + 8].transpose(1, 2))
+            v = torch.matmul(x[:, :r], wv[h:h + 8].transpose(1, 2))
+            s = torch.matmul(q[h:h + 8, :, :d], k.transpose(1, 2)) + torch.matmul(q[h:h + 8, :, d:], x[:, r:].t())
+            s = s.masked_fill_(hidden, -math.inf)
+            w = (s - s.amax(-1, keepdim=True)).exp_()
+            o = torch.matmul(w, v) / w.sum(-1, keepdim=True)
+            out[at:at + a, h:h + 8] = o.transpose(0, 1).to(out.dtype)
+        at += a
+    return out
+
+
+# ------------------------------------------------------------------- passes
+@functools.lru_cache(maxsize=64)
+def _joint(heads, head_dim, rank, rope_dim, cache):
+    """The description that a program keeps for its model's layers."""
+    from paper_2607_24331_amd import Joint
+    return Joint(heads, head_dim, rank, rope_dim, cache=cache)
+
+
+@functools.lru_cache(maxsize=64)
+def _rotary(rope_dim, layout):
+    """The handle that a program keeps for its model's rotation."""
+    from paper_2607_24331_amd import Rotary
+    return Rotary(rope_dim, layout=layout)
+
+
+def run(state):
+    """One call of a serving program."""
+    case = state["case"]
+    kind = case["kind"]
+    if not own:
+        return {"append": _plain_append, "decode": _plain_decode, "prompt": _plain_prompt}[kind](state)
+    import paper_2607_24331_amd as dckv
+    joint = _joint(case["heads"], case["head_dim"], case["rank"], case["rope_dim"], case["cache"])
+    if kind == "append":
+        rot = _rotary(case["rope_dim"], case["layout"]) if case["rope_dim"] else None
+        dckv.joint_append(joint, state["c"], state["k"], state["slot"], state["pool"], rot,
+                          state["position"] if rot else None)
+        if case["cache"] == "bf16":
+            return dict(pool=state["pool"])
+        c, k = dckv.joint_read(joint, state["pool"], state["slot"])
+        return dict(c=c, k=k)
+    if kind == "decode":
+        return dckv.joint_decode(joint, state["q"], state["pool"], state["table"], state["lens"], state["top"],
+                                 state["wk"], state["wv"], prefix_pages=state["prefix"], prefix_len=case["prefix"])
+    return dckv.joint_prefill(joint, state["q"], state["row_start"], state["pool"], state["table"], state["lens"],
+                              state["top"], state["wk"], state["wv"], total_context=state["total"], out=state["out"])
+
+
+# ---------------------------------------------------------- in 64 bits
+def _exact_turn(case, x, position):
+    p = case["rope_dim"]
+    theta = [math.exp(-2.0 * i / p * math.log(10000.0)) for i in range(p // 2)]
+    angle = position.double()[:, None] * torch.tensor(theta, dtype=torch.float64, device=x.device)
+    f = torch.polar(torch.ones_like(angle), angle)
+    y = x.double().clone()
+    if case["layout"] == "half":
+        z = torch.complex(y[:, :p // 2].clone(), y[:, p // 2:].clone()) * f
+        return torch.cat([z.real, z.imag], -1)
+    return torch.view_as_real(torch.view_as_complex(y.view(-1, p // 2, 2)) * f).reshape(-1, p)
+
+
+def _exact_quantized(x):
+    """x [n, w] rounded to e4m3 (steps of 1/8 of a power of two, 2^-9 at least)
+    under its row's power of two."""
+    e = torch.ceil(torch.log2(x.abs().amax(-1, keepdim=True) / 448.0)).clamp(-112, 119)
+    y = x / torch.exp2(e)
+    step = torch.exp2(torch.floor(torch.log2(y.abs())).clamp(min=-6.0) - 3.0)
+    return torch.round(y / step) * step * torch.exp2(e)
+
+
+def _exact_tokens(case, pool, ids, n):
+    """Latents [n, r] and keys [n, p] in 64 bits, each token by its place."""
+    r, p = case["rank"], case["rope_dim"]
+    t = torch.arange(n, device=pool.device)
+    rows = pool[ids.long()[t // PAGE]] if n else pool[:0]
+    s, j = (t % PAGE)[:, None], torch.arange(r + p, device=pool.device)[None, :]
+    x = rows.gather(1, s * (r + p) + j)
+    if case["cache"] == "bf16":
+        x = x.double()
+        return x[:, :r], x[:, r:]
+    x = x.view(torch.float8_e4m3fn).double()
+    e = [torch.exp2(rows.gather(1, PAGE * (r + p + i) + s).double() - 127.0) for i in (0, 1)]
+    return x[:, :r] * e[0], x[:, r:] * e[1]
+
+
+def _exact_decode(st):
+    """Expanded: every head's keys and values of one sequence at a time."""
+    case = st["case"]
+    H, d, n = case["heads"], case["head_dim"], case["prefix"]
+    B, Q = st["q"].shape[:2]
+    out = torch.zeros(B, Q, H, d, dtype=torch.float64, device="cuda")
+    pre = _exact_tokens(case, st["pool"], st["prefix"], n) if n else None
+    for b, T in enumerate(st["lens"].tolist()):
+        c, k = _exact_tokens(case, st["pool"], st["table"][b], T)
+        if n:
+            c, k = torch.cat([pre[0], c]), torch.cat([pre[1], k])
+        for h in range(H):
+            keys = torch.cat([c @ st["wk"][h].double().t(), k], -1)
+            values = c @ st["wv"][h].double().t()
+            for i in range(Q):
+                seen = n + T - Q + i + 1
+                if seen > 0:
+                    s = keys[:seen] @ st["q"][b, i, h].double() * _scale(case)
+                    out[b, i, h] = torch.softmax(s, -1) @ values[:seen]
+    return out
+
+
+def _exact_prompt(st):
+    """Absorbed: one sequence and head at a time."""
+    case = st["case"]
+    out, at = torch.zeros(st["out"].shape, dtype=torch.float64, device="cuda"), 0
+    d = case["head_dim"]
+    for b, (cached, added) in enumerate(zip(st["cached"], st["added"])):
+        if added == 0:
+            continue
+        c, k = _exact_tokens(case, st["pool"], st["table"][b], cached + added)
+        row = torch.arange(added, device="cuda")[:, None] + cached
+        seen = torch.arange(cached + added, device="cuda")[None, :] <= row
+        for h in range(case["heads"]):
+            q = st["q"][at:at + added, h].double()
+            s = (q[:, :d] @ st["wk"][h].double()) @ c.t() + q[:, d:] @ k.t()
+            w = torch.softmax(torch.where(seen, s * _scale(case), -math.inf), -1)
+            out[at:at + added, h] = (w @ c) @ st["wv"][h].double().t()
+        at += added
+    return out
+
+
+def exact(case, seed):
+    """The outputs of `run` from the definitions, in 64 bits."""
+    st = prepare(case, seed)
+    if case["kind"] == "append":
+        r, p = case["rank"], case["rope_dim"]
+        c = st["c"].double()
+        k = _exact_turn(case, st["k"], st["position"]) if p else c[:, :0]
+        if case["cache"] == "bf16":
+            cells = torch.zeros(st["pool"].shape[0], PAGE, r + p, dtype=torch.float64, device="cuda")
+            cells[st["slot"] // PAGE, st["slot"] % PAGE] = torch.cat([c, k], -1)
+            return dict(pool=cells.view(st["pool"].shape))
+        return dict(c=_exact_quantized(c), k=_exact_quantized(k) if p else None)
+    return _exact_decode(st) if case["kind"] == "decode" else _exact_prompt(st)
