@@ -125,6 +125,20 @@ def _prompt_lens(case):
     return cached, added
 
 
+@functools.lru_cache(maxsize=64)
+def _place_table(width, per):
+    """Where a page's row s (a token) and column j lie, [64, width] elements from its start: the 16-byte
+    pieces (`per` elements) of a row change places by the row, i and i ^ (s / (16 / g) mod g), g = gcd(pieces, 16)."""
+    g = math.gcd(width // per, 16)
+    s, j = torch.arange(PAGE, device="cuda")[:, None], torch.arange(width, device="cuda")[None, :]
+    return s * width + (j // per ^ s // (16 // g) % g) * per + j % per
+
+
+def _places(case):
+    """The table of a case's pages, which a program forms once for a layer."""
+    return _place_table(case["rank"] + case["rope_dim"], 8 if case["cache"] == "bf16" else 16)
+
+
 def _scale(case):
     return 1.0 / math.sqrt(case["head_dim"] + case["rope_dim"])
 
@@ -249,14 +263,14 @@ def _plain_append(st):
     r, p = case["rank"], case["rope_dim"]
     parts = [st["c"].float()] + ([_turn(case, st["k"], st["position"])] if p else [])
     page, s = slot // PAGE, slot % PAGE
+    at = _places(case)[s]
     if case["cache"] == "bf16":
-        pool.view(-1, PAGE, r + p)[page, s] = torch.cat(parts, -1).to(torch.bfloat16)
+        pool[page[:, None], at] = torch.cat(parts, -1).to(torch.bfloat16)
         return dict(pool=pool)
-    n, out = pool.shape[0], []
-    cells = pool[:, :PAGE * (r + p)].view(n, PAGE, r + p)
+    out = []
     for i, x in enumerate(parts):
         q8, e = _plain_quantized(x)
-        cells[page, s, i * r:i * r + x.shape[1]] = q8.view(torch.uint8)
+        pool[page[:, None], at[:, i * r:i * r + x.shape[1]]] = q8.view(torch.uint8)
         pool[page, PAGE * (r + p + i) + s] = (e[:, 0] + 127).to(torch.uint8)
         # what a reader of the pages finds there
         out.append(torch.ldexp(q8.float(), e).to(torch.bfloat16))
@@ -267,11 +281,12 @@ def _tokens(case, pool, ids):
     """Latents and keys [..., 64 a page, r + p] in 32 bits of the pages `ids` [..., n]."""
     r, p = case["rank"], case["rope_dim"]
     got = pool[ids.long().reshape(-1)]
+    x = got[:, _places(case).view(-1)]
     if case["cache"] == "bf16":
-        x = got.float()
+        x = x.float()
     else:
         n = got.shape[0]
-        x = got[:, :PAGE * (r + p)].contiguous().view(torch.float8_e4m3fn).float().view(n, PAGE, r + p)
+        x = x.view(torch.float8_e4m3fn).float().view(n, PAGE, r + p)
         e = got[:, PAGE * (r + p):].view(n, 2, PAGE).int() - 127
         one = torch.ones((), device=pool.device)
         x = torch.cat([x[..., :r] * torch.ldexp(one, e[:, 0])[..., None], x[..., r:] * torch.ldexp(one, e[:, 1])[..., None]], -1)
@@ -389,14 +404,13 @@ def _exact_tokens(case, pool, ids, n):
     """Latents [n, r] and keys [n, p] in 64 bits, each token by its place."""
     r, p = case["rank"], case["rope_dim"]
     t = torch.arange(n, device=pool.device)
-    rows = pool[ids.long()[t // PAGE]] if n else pool[:0]
-    s, j = (t % PAGE)[:, None], torch.arange(r + p, device=pool.device)[None, :]
-    x = rows.gather(1, s * (r + p) + j)
+    page = (ids.long()[t // PAGE] * pool.shape[1])[:, None]
+    x = pool.view(-1)[page + _places(case)[t % PAGE]]
     if case["cache"] == "bf16":
         x = x.double()
         return x[:, :r], x[:, r:]
     x = x.view(torch.float8_e4m3fn).double()
-    e = [torch.exp2(rows.gather(1, PAGE * (r + p + i) + s).double() - 127.0) for i in (0, 1)]
+    e = [torch.exp2(pool.view(-1)[page + PAGE * (r + p + i) + (t % PAGE)[:, None]].double() - 127.0) for i in (0, 1)]
     return x[:, :r] * e[0], x[:, r:] * e[1]
 
 
@@ -450,8 +464,8 @@ def exact(case, seed):
         c = st["c"].double()
         k = _exact_turn(case, st["k"], st["position"]) if p else c[:, :0]
         if case["cache"] == "bf16":
-            cells = torch.zeros(st["pool"].shape[0], PAGE, r + p, dtype=torch.float64, device="cuda")
-            cells[st["slot"] // PAGE, st["slot"] % PAGE] = torch.cat([c, k], -1)
-            return dict(pool=cells.view(st["pool"].shape))
+            cells = torch.zeros(st["pool"].shape, dtype=torch.float64, device="cuda")
+            cells[(st["slot"] // PAGE)[:, None], _places(case)[st["slot"] % PAGE]] = torch.cat([c, k], -1)
+            return dict(pool=cells)
         return dict(c=_exact_quantized(c), k=_exact_quantized(k) if p else None)
     return _exact_decode(st) if case["kind"] == "decode" else _exact_prompt(st)
