@@ -562,6 +562,111 @@ int dckv_quant_decode(int32_t num_q_heads, int32_t num_kv_heads, int32_t head_di
                       void* workspace, size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
+ * Joint-latent cache: one latent c (rank r) and one position key k (rope_dim p)
+ * a token, shared by all heads.  Head h's key and value of a token are
+ *   key_h = [W_keys[h] c ; k],   value_h = W_values[h] c,
+ * W_keys, W_values bf16 [H, d, r], its query [q_n ; q_p] (d + p coordinates, q_p
+ * turned by its position as k is), the score scale (q_n . W_keys[h] c + q_p . k).
+ * Pages of 64 tokens in bf16, or in e4m3 under a power of two a row of c and of k
+ * (x ~ 2^e byte as for dckv_quant_append).  A page holds 64 rows of w = r + p
+ * elements, c then k, slot s's from byte s*w*(2 or 1) on; their 16-byte pieces
+ * change places by the slot: piece i lies at piece
+ *   i ^ (s / (16 / g)) % g,   g = gcd(pieces of a row, 16),
+ * so that 32 rows copied to LDS as they lie are read without bank conflicts.
+ * e4m3 pages go on with the exponent bytes e + 127 of the latents (64*w + s) and of
+ * the keys (64*w + 64 + s); 64*(w + 2) bytes in all.
+ * The description is read during a call only. */
+typedef enum { DCKV_JOINT_BF16 = 0, DCKV_JOINT_E4M3 = 1 } dckv_joint_cache;
+typedef struct dckv_joint_desc {
+  int32_t num_heads; /* H, 1..DCKV_MAX_HEADS */
+  int32_t head_dim;  /* d: 64 or 128 */
+  int32_t rank;      /* r: 128, 256 or 512 */
+  int32_t rope_dim;  /* p: 0, 32 or 64 */
+  int32_t cache;     /* dckv_joint_cache */
+  float scale;       /* finite, above 0; 0 means 1/sqrt(d + p) */
+} dckv_joint_desc;
+
+int dckv_joint_page_bytes(const dckv_joint_desc* desc, int64_t* bytes);
+
+/* Append of new tokens.
+ *   c, k       device, dtype DCKV_F32 or DCKV_BF16: token t's latent at
+ *              c + t*c_stride, its key at k + t*k_stride (elements, not negative);
+ *              k is not read and may be NULL where p is 0
+ *   slot       device int64 [n_tok]; a slot outside 0 .. num_pages*64 - 1 skips the
+ *              token
+ *   rotary     NULL: keys as they are, position is not read; else of head_dim p
+ *   position   device int32 [n_tok], not negative where slot is not
+ * Roundings are to nearest-even.  Pools are 16-byte aligned; n_tok at most 2^23 (0
+ * is a no-op).  Two tokens with the same slot race. */
+int dckv_joint_append(const dckv_joint_desc* desc, const void* c, int64_t c_stride, const void* k,
+                      int64_t k_stride, int32_t dtype, const int64_t* slot, int32_t n_tok,
+                      const dckv_rotary* rotary, const int32_t* position, void* pool,
+                      int64_t num_pages, void* stream);
+
+/* Cached tokens of given slots: c [n_tok, r] and k [n_tok, p] (not written where p
+ * is 0) of `dtype`, 16-byte aligned, exactly; a slot outside the pool gives zeros.
+ * n_tok at most 2^23. */
+int dckv_joint_read(const dckv_joint_desc* desc, const void* pool, int64_t num_pages,
+                    const int64_t* slot, int32_t n_tok, void* c, void* k, int32_t dtype,
+                    void* stream);
+
+/* Decode in the absorbed form: queries are folded into the latent space
+ * (W_keys[h]^T q_n), attend over the latents themselves and their means are taken
+ * through W_values[h]; keys and values are never formed.  Q = queries (1..
+ * DCKV_MAX_QUERIES) causal queries a sequence, the newest: query i sits at position
+ * seq_len - Q + i and sees every position up to its own; one that sees none gets
+ * zeros.  Page-table entries outside [0, num_pages) are empty pages.
+ *   q          device bf16 [batch, Q, H, d + p]
+ *   prefix     prefix_len > 0: every sequence goes on from the same prefix_len tokens
+ *              (slots 0, 1, ... of prefix_pages, int32 [ceil(prefix_len/64)]), which
+ *              are read once for all; page_table, seq_lens and max_context then count a
+ *              sequence's own tokens, whose positions start at prefix_len.  0: NULL
+ *   out        device bf16 [batch, Q, H, d]
+ * Folded queries and softmax weights are rounded to bf16 (relative 2^-9 each), sums
+ * are fp32.  Whatever lies in slots that a query does not see (NaN included) does not
+ * reach its result; a token that it sees and that is not finite makes it NaN, as does
+ * an infinite score.
+ * A workspace (256-byte aligned; its contents do not matter) of
+ * dckv_joint_workspace_bytes also serves fewer sequences, shorter contexts and shorter
+ * prefixes (not a prefix where none was named).  Calls that may overlap need workspaces
+ * of their own.  batch * Q at most 65535; batch == 0 is a no-op.  q, pool, W_keys,
+ * W_values and out are 16-byte aligned.  Results are bitwise reproducible for fixed
+ * inputs; they depend, within rounding, on all sequences' lengths. */
+int dckv_joint_workspace_bytes(const dckv_joint_desc* desc, int32_t queries, int32_t batch,
+                               int32_t max_context, int32_t prefix_len, size_t* bytes);
+int dckv_joint_decode(const dckv_joint_desc* desc, int32_t queries, const void* q, int32_t batch,
+                      const void* pool, int64_t num_pages, const int32_t* page_table,
+                      int32_t max_pages, const int32_t* seq_lens, int32_t max_context,
+                      const int32_t* prefix_pages, int32_t prefix_len, const void* W_keys,
+                      const void* W_values, void* out, void* workspace, size_t workspace_bytes,
+                      void* stream);
+
+/* Prompts in the expanded form: every head's keys and values are formed once for a
+ * sequence's cached tokens (in the workspace) and attended over, which takes fewer
+ * products than the absorbed form from some tens of new tokens a sequence on.
+ *   q          device bf16 [n_rows, H, d + p], packed: rows row_start[b] ..
+ *              row_start[b+1] - 1 are the newest tokens of sequence b, already in the
+ *              cache (dckv_page_map gives row_start, int32 [batch + 1], and seq_lens);
+ *              each sees every token up to its own.  Rows behind the last sequence are
+ *              left alone.  row_start ascends; a sequence's rows beyond its length see
+ *              nothing and get zeros
+ *   total_context  at least the sum over the sequences of seq_lens (each clipped to
+ *              0 .. max_context) that have rows; a sequence that does not fit it gets
+ *              NaN
+ *   out        device bf16 [n_rows, H, d]
+ * Keys, values and softmax weights are rounded to bf16 (values beyond its range to
+ * its greatest), sums are fp32.  Unseen slots, NaN, pages, alignment and errors as for
+ * dckv_joint_decode; the workspace serves fewer sequences, rows and tokens too. */
+int dckv_joint_prefill_workspace_bytes(const dckv_joint_desc* desc, int32_t batch, int32_t n_rows,
+                                       int32_t max_context, int64_t total_context, size_t* bytes);
+int dckv_joint_prefill(const dckv_joint_desc* desc, const void* q, int32_t n_rows,
+                       const int32_t* row_start, int32_t batch, const void* pool,
+                       int64_t num_pages, const int32_t* page_table, int32_t max_pages,
+                       const int32_t* seq_lens, int32_t max_context, int64_t total_context,
+                       const void* W_keys, const void* W_values, void* out, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
  * Offline compression: run once per layer before serving, never on the
  * decode path.
  *

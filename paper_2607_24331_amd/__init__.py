@@ -11,10 +11,11 @@ from .dckv import (DckvError, Plan, allocate_ranks, cluster_heads, cluster_merge
 from .serve import (PageMap, Rotary, decode_rotary, dense_append, new_quant_pool, page_map,  # noqa: F401
                     page_release, quant_append, quant_decode, quant_page_bytes, quant_read,
                     quant_workspace_bytes, rotary)
+from .joint import Joint, joint_append, joint_decode, joint_prefill, joint_read  # noqa: F401
 from . import capi  # noqa: F401
 
 __all__ = ["Plan", "latent_append", "decode", "decode_noalloc", "decode_rope", "dense_decode", "dense_page_elems", "DckvError", "capi",
            "gram", "gram_workspace_bytes", "head_similarity", "cluster_heads", "cluster_merges", "allocate_ranks",
            "PageMap", "page_map", "page_release", "Rotary", "rotary", "decode_rotary", "dense_append",
            "new_quant_pool", "quant_page_bytes", "quant_append", "quant_read", "quant_workspace_bytes",
-           "quant_decode"]
+           "quant_decode", "Joint", "joint_append", "joint_read", "joint_decode", "joint_prefill"]

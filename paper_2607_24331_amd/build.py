@@ -24,9 +24,11 @@ LIB = os.path.join(PKG, "libdckv.so")
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 ARCH = "gfx950"
 
-HOST_SOURCES = ["plan.cpp", "offline.cpp", "serve.cpp"]
+HOST_SOURCES = ["plan.cpp", "offline.cpp", "serve.cpp", "joint.cpp"]
 HIP_SOURCES = ["append.hip", "decode.hip", "decode_mfma.hip", "dense.hip", "gram.hip", "rope.hip", "noalloc.hip", "decode_pass.hip",
-               "page_map.hip", "rotary.hip", "kv_append.hip", "quant_decode.hip"]
+               "page_map.hip", "rotary.hip", "kv_append.hip", "quant_decode.hip",
+               "joint_kv.hip", "joint_decode.hip", "joint_prompt.hip", "joint_attend_128.hip", "joint_attend_256.hip",
+               "joint_attend_512.hip"]
 
 HIPCC_FLAGS = [
     "-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
@@ -38,7 +40,11 @@ HIPCC_FLAGS = [
 # ordinary VGPRs: with the default AGPR form the register allocator rotated
 # accumulators through AGPR copies inside the k loop, each copy waiting for
 # an in-flight MFMA.
-HIPCC_EXTRA = {"append.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+# The joint decode's 256 accumulators a lane beside its queries fit the
+# registers in that form only (in the other one 300 to 400 are spilled).
+VGPR_FORM = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
+HIPCC_EXTRA = {src: VGPR_FORM for src in ("append.hip", "joint_attend_128.hip", "joint_attend_256.hip",
+                                          "joint_attend_512.hip")}
 HOST_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-D__HIP_PLATFORM_AMD__", "-Wall", "-Wextra"]
 
 

@@ -25,6 +25,8 @@ DCKV_EHIP = -5
 DCKV_ENOMEM = -6
 DCKV_F32 = 0
 DCKV_BF16 = 1
+DCKV_JOINT_BF16 = 0
+DCKV_JOINT_E4M3 = 1
 PAGE_TOKENS = 64
 NOALLOC_SCRATCH_BYTES = 64 << 20
 
@@ -100,6 +102,17 @@ class RotaryDesc(ctypes.Structure):
     ]
 
 
+class JointDesc(ctypes.Structure):
+    _fields_ = [
+        ("num_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("rank", ctypes.c_int32),
+        ("rope_dim", ctypes.c_int32),
+        ("cache", ctypes.c_int32),
+        ("scale", ctypes.c_float),
+    ]
+
+
 _vp = ctypes.c_void_p
 _i32 = ctypes.c_int32
 _i64 = ctypes.c_int64
@@ -146,6 +159,18 @@ SIGNATURES = {
                                                   ctypes.POINTER(ctypes.c_size_t)]),
     "dckv_quant_decode": (ctypes.c_int, [_i32, _i32, _i32, _i32, _i32, _vp, _i32, _vp, _i64, _vp, _i32, _vp,
                                          _i32, _vp, _vp, ctypes.c_size_t, _vp]),
+    "dckv_joint_page_bytes": (ctypes.c_int, [ctypes.POINTER(JointDesc), ctypes.POINTER(ctypes.c_int64)]),
+    "dckv_joint_append": (ctypes.c_int, [ctypes.POINTER(JointDesc), _vp, _i64, _vp, _i64, _i32, _vp, _i32, _vp,
+                                         _vp, _vp, _i64, _vp]),
+    "dckv_joint_read": (ctypes.c_int, [ctypes.POINTER(JointDesc), _vp, _i64, _vp, _i32, _vp, _vp, _i32, _vp]),
+    "dckv_joint_workspace_bytes": (ctypes.c_int, [ctypes.POINTER(JointDesc), _i32, _i32, _i32, _i32,
+                                                  ctypes.POINTER(ctypes.c_size_t)]),
+    "dckv_joint_decode": (ctypes.c_int, [ctypes.POINTER(JointDesc), _i32, _vp, _i32, _vp, _i64, _vp, _i32, _vp,
+                                         _i32, _vp, _i32, _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]),
+    "dckv_joint_prefill_workspace_bytes": (ctypes.c_int, [ctypes.POINTER(JointDesc), _i32, _i32, _i32, _i64,
+                                                          ctypes.POINTER(ctypes.c_size_t)]),
+    "dckv_joint_prefill": (ctypes.c_int, [ctypes.POINTER(JointDesc), _vp, _i32, _vp, _i32, _vp, _i64, _vp, _i32,
+                                          _vp, _i32, _i64, _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]),
     "dckv_gram_workspace_bytes": (ctypes.c_int, [_i64, _i32, _i32, ctypes.POINTER(ctypes.c_size_t)]),
     "dckv_gram": (ctypes.c_int, [_vp, _i32, _i64, _i32, _i32, _vp, _vp, ctypes.c_size_t, _vp]),
     "dckv_head_similarity": (ctypes.c_int, [_vp, _i32, _i32, _vp, _vp]),

@@ -1,0 +1,97 @@
+// Internal declarations of the joint-latent cache: appends, reads, the absorbed
+// decode and the expanded prompts.
+#pragma once
+
+#include "serve.h"
+
+namespace dckv {
+
+constexpr int kJointTile = 32;          // tokens a tile of the decode
+constexpr int kJointMaxUnits = 512;     // work-groups of a row slice, at most (the join holds 2 a row)
+
+// Pieces (16 bytes) of a row change places by the row, so that the 16 rows that a
+// quarter of a wave reads at one column lie in different LDS banks: piece i of slot s
+// lies at piece i ^ joint_swap(s), g = gcd(pieces, 16).
+__host__ __device__ constexpr int joint_gcd16(int n) { return n % 16 == 0 ? 16 : n % 8 == 0 ? 8 : n % 4 == 0 ? 4 : n % 2 == 0 ? 2 : 1; }
+__host__ __device__ constexpr int joint_swap(int g, int s) { return (s / (16 / g)) & (g - 1); }
+
+// Waves of a work-group whose slice is row_waves x 16 rows.
+__host__ __device__ constexpr int joint_waves(int row_waves) { return row_waves <= 2 ? 4 : 8; }
+
+// Launch shape of one absorbed decode.
+struct JointShape {
+  dckv_joint_desc d;
+  int32_t queries, batch, max_context, prefix_len;
+  int32_t rows;                 // (query, head) rows of a sequence
+  int32_t row_waves, slices;    // own tokens: waves that take 16 rows each of a work-group's slice; slices
+  int32_t units;                // work-groups a slice
+  int32_t pre_row_waves, pre_slices, pre_units;   // the same for the prefix, its rows those of all sequences
+  size_t off_start, off_o, off_ml, off_pre_o, off_pre_ml;   // workspace: queries first
+  size_t bytes;                 // what this call uses
+};
+
+// What an attend kernel reads and writes.
+struct JointAttend {
+  const void* q;                // bf16 [rows of all sequences][r + p]
+  const uint8_t* pool;
+  int64_t num_pages, page_bytes;
+  const int32_t* table;         // page_table, or the prefix's pages
+  int32_t max_pages;            // of a row of the table
+  const int64_t* start;         // first tile of each sequence among all, [batch + 1]
+  const int32_t* seq_lens;
+  int32_t max_context, batch, queries, heads;
+  int32_t units, slices;
+  int32_t prefix_len;           // above 0: this launch attends over the prefix
+  float scale;                  // times log2(e)
+  float* part_o;                // [segment][slice][rows of a work-group][r]
+  float4* part_ml;              // [segment][slice][rows]: m, l, u, 0
+};
+
+// Tiles that a unit takes of `total`, whole rounds of a work-group's token groups.
+__host__ __device__ inline int64_t joint_tiles_a_unit(int64_t total, int units, int groups) {
+  const int64_t per = (total + units - 1) / units;
+  const int64_t n = (per + groups - 1) / groups * groups;
+  return n < groups ? groups : n;
+}
+
+struct JointPrompt {
+  dckv_joint_desc d;
+  int32_t n_rows, batch, max_context;
+  int64_t total_context;
+  int64_t kv_tiles, q_tiles;    // 64-token tiles and row tiles, at most
+  size_t off_qtile, off_kvtile, off_flags, off_c, off_rope, off_k, off_v;
+  size_t bytes;
+};
+
+int64_t joint_page_bytes(const dckv_joint_desc& d);
+
+hipError_t launch_joint_append(const dckv_joint_desc& d, const void* c, int64_t c_stride, const void* k,
+                               int64_t k_stride, int32_t dtype, const int64_t* slot, int32_t n_tok,
+                               const RotaryTable& rot, const int32_t* position, void* pool,
+                               int64_t num_pages, hipStream_t stream);
+hipError_t launch_joint_read(const dckv_joint_desc& d, const void* pool, int64_t num_pages,
+                             const int64_t* slot, int32_t n_tok, void* c, void* k, int32_t dtype,
+                             hipStream_t stream);
+
+JointShape joint_shape(const dckv_joint_desc& d, int32_t queries, int32_t batch, int32_t max_context,
+                       int32_t prefix_len);
+// Bytes that serve this call and every one of fewer sequences, shorter contexts
+// and a shorter prefix.
+size_t joint_workspace_bytes(const JointShape& s);
+hipError_t launch_joint_decode(const JointShape& s, const void* q, const void* pool, int64_t num_pages,
+                               const int32_t* page_table, int32_t max_pages, const int32_t* seq_lens,
+                               const int32_t* prefix_pages, const void* W_keys, const void* W_values,
+                               void* out, void* workspace, hipStream_t stream);
+// One launch of the attend kernel (joint_attend_*.hip).
+hipError_t launch_joint_attend_128(const dckv_joint_desc& d, int row_waves, const JointAttend& a, hipStream_t stream);
+hipError_t launch_joint_attend_256(const dckv_joint_desc& d, int row_waves, const JointAttend& a, hipStream_t stream);
+hipError_t launch_joint_attend_512(const dckv_joint_desc& d, int row_waves, const JointAttend& a, hipStream_t stream);
+
+JointPrompt joint_prompt(const dckv_joint_desc& d, int32_t batch, int32_t n_rows, int32_t max_context,
+                         int64_t total_context);
+hipError_t launch_joint_prefill(const JointPrompt& s, const void* q, const int32_t* row_start,
+                                const void* pool, int64_t num_pages, const int32_t* page_table,
+                                int32_t max_pages, const int32_t* seq_lens, const void* W_keys,
+                                const void* W_values, void* out, void* workspace, hipStream_t stream);
+
+}  // namespace dckv

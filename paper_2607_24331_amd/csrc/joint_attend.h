@@ -1,0 +1,497 @@
+// The absorbed decode over the joint cache on MFMA (gfx950).
+//
+//   s_rt = scale q_r . [c_t ; k_t],   a_r = sum_t softmax_t(s_rt) c_t
+//
+// for the (query, head) rows r of a sequence, or of all sequences over a shared prefix;
+// q_r is the query folded into the latent space, in bf16.  One copy of a token serves
+// as key and value, so a tile of 32 tokens is brought into LDS once (by the loads' LDS
+// path, pages being laid out as LDS wants them) and read twice:
+//   scores  S[token][row] = C[token][:] Q[row][:], MFMA 16x16x32: the A operand of a step
+//           is 16 bytes of a token a lane, the queries stay in registers.
+//   output  O[column][row] += C^T[column][token] P[token][row]: a lane holds the scores of one
+//           row and tokens 16 n + 4 (lane / 16) + v, and the transposing LDS load brings a
+//           column's tokens in that order, so the weights (bf16, from fp32 scores) feed the
+//           second product from the registers they were made in.
+// A wave owns 16 rows and all r columns of their sums: 128 accumulators a lane at r = 512
+// and 72 registers of queries (32 rows, twice that, read LDS half as often but do not fit
+// the registers: 200 and more were spilled).  Of a work-group's waves WR take WR x 16
+// rows of the same tiles; the NG token groups take tiles in turn and are joined at the
+// end.  The running maximum of a row is raised, and the sums scaled down, only when a
+// score passes it by more than kSlack (in powers of two), so that the r sums of a row
+// are rarely touched.
+// e4m3 tokens are widened to bf16 on their way from LDS to the matrix unit: as keys
+// under their power of two (exactly), as values without it: the weights take it, held
+// against a maximum u of score + exponent of their own, so that they are at most
+// 2^kSlack whatever the exponents are.
+// Work is cut into `units` equal shares of all sequences' tiles, whatever their lengths;
+// a unit walks over the sequences that it meets (segments, numbered unit + sequence).
+#pragma once
+
+#include <type_traits>
+
+#include "device.h"
+#include "joint.h"
+
+namespace dckv {
+namespace joint {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef int v2i __attribute__((ext_vector_type(2)));
+typedef short short4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) short4_t* lds_short4;
+typedef __attribute__((address_space(3))) v2i* lds_v2i;
+
+constexpr float kSlack = 6.f;          // weights reach 2^6: the sums stay far from fp32's end
+
+__device__ __forceinline__ floatx4 mfma(u32x4 a, u32x4 b, floatx4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c,
+                                                 0, 0, 0);
+}
+
+// 16 bytes a lane from global memory to LDS, in lane order from p on.
+__device__ __forceinline__ void load_lds16(const uint8_t* g, unsigned char* p) {
+  __builtin_amdgcn_global_load_lds(g, p, 16, 0, 0);
+}
+
+// Eight e4m3 values times `scale`, a power of two, as bf16.
+__device__ __forceinline__ u32x4 widen(uint32_t lo, uint32_t hi, float scale) {
+  return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true))};
+}
+
+__device__ __forceinline__ uint32_t pair(float a, float b) {
+  return uint32_t(__builtin_bit_cast(uint16_t, from_f32<bf16>(a))) |
+         uint32_t(__builtin_bit_cast(uint16_t, from_f32<bf16>(b))) << 16;
+}
+
+// Place of pieces 4 i + lq from that of lq (four pieces keep their places among
+// themselves where fewer than four change them).
+template <int G>
+__device__ __forceinline__ int place(int at, int i) {
+  return G >= 4 ? (at ^ ((i & (G / 4 - 1)) * 64)) + i / (G / 4 > 0 ? G / 4 : 1) * (G * 16) : at + i * 64;
+}
+
+// Over the four lanes that hold a row.
+__device__ __forceinline__ float row_max(float x) {
+  x = fmaxf(x, __shfl_xor(x, 16));
+  return fmaxf(x, __shfl_xor(x, 32));
+}
+
+// Tokens of a 16-byte piece that are not finite (bf16) or NaN (e4m3).
+template <bool C8>
+__device__ __forceinline__ bool odd_piece(u32x4 w) {
+  uint32_t bad = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (C8)
+      bad |= ((w[i] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
+    else
+      bad |= (((w[i] & 0x7F807F80u) + 0x00800080u) & 0x80008000u);
+  }
+  return bad != 0;
+}
+
+template <int R, int P, bool C8, int WR>
+struct Shape {
+  static constexpr int W = R + P, E = C8 ? 1 : 2, ROWB = W * E, PIECES = ROWB / 16;
+  static constexpr int G = joint_gcd16(PIECES);
+  static constexpr int NW = joint_waves(WR), NG = NW / WR, THREADS = 64 * NW;
+  static constexpr int TILE = kJointTile * ROWB;      // bytes
+  // a second buffer, so that the next tile comes while this one is used; lone waves with
+  // wide bf16 tiles have no room for it, there the other waves use the time
+  static constexpr int NBUF = WR > 1 || 2 * NG * TILE <= 158000 ? 2 : 1;
+  static constexpr int CJ = R >= 256 ? 128 : 64;      // columns of a round of the join
+  static constexpr int JOIN = NG == 1 ? 0 : NW * 16 * (CJ + 4) * 4;
+  static constexpr int LDS = NG * NBUF * TILE > JOIN ? NG * NBUF * TILE : JOIN;
+  static constexpr int NL = PIECES / 2;               // 1 KB loads of a tile, dealt out to WR waves
+  static constexpr int LOADS = (NL + WR - 1) / WR;
+  static_assert(PIECES % 2 == 0, "whole loads");
+};
+
+template <int R, int P, bool C8, int WR>
+__global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(JointAttend a) {
+  using S = Shape<R, P, C8, WR>;
+  constexpr int W = S::W, ROWB = S::ROWB, G = S::G, NG = S::NG, NW = S::NW, NBUF = S::NBUF, LOADS = S::LOADS;
+  constexpr int KS = W / 32, CT = R / 16;             // steps of the scores, column tiles of the sums
+  __shared__ __align__(1024) unsigned char smem[S::LDS];
+  __shared__ float scale_of[C8 ? NW : 1][kJointTile];  // a wave's tile: exponents of its latents
+  __shared__ uint32_t odd_of[2][NW];                  // tokens of a tile's edge that hold a NaN, by loading wave
+  __shared__ float join_m[NW][16], join_l[NW][16], join_u[NW][16];
+
+  const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lq = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rw = w % WR, g = w / WR;                  // rows and token group of this wave
+  // ids w, w + 8, ... run on one XCD: the slices of a unit are neighbours there and share
+  // its tokens in one L2
+  const int id = blockIdx.x;
+  const int unit = (id / (8 * a.slices)) * 8 + (id & 7), slice = (id >> 3) % a.slices;
+  if (unit >= a.units) return;
+  const bool prefix = a.prefix_len > 0;
+  const int rows = a.queries * a.heads * (prefix ? a.batch : 1);
+  const int64_t total = prefix ? (a.prefix_len + kJointTile - 1) / kJointTile : a.start[a.batch];
+  const int64_t per = joint_tiles_a_unit(total, a.units, NG);
+  int64_t at = unit * per;
+  const int64_t end = min(at + per, total);
+  if (at >= end) return;
+
+  // the sequence that holds tile `at`: the last b with start[b] <= at, 64 candidates a round
+  int b = 0;
+  if (!prefix) {
+    int lo = 0, n = a.batch;                          // start[lo] <= at; the answer is in lo .. lo + n - 1
+    while (n > 1) {
+      const int step = (n + 63) / 64;
+      const int i = lo + lane * step;
+      const bool in = lane * step < n && a.start[i] <= at;
+      const int k = __popcll(__ballot(in)) - 1;       // starts ascend: the first k + 1 lanes hold
+      lo += k * step;
+      n = min(step, n - k * step);
+    }
+    b = __builtin_amdgcn_readfirstlane(lo);
+  }
+
+  unsigned char* bufs = smem + g * NBUF * S::TILE;
+  // addresses in a tile: of token lr's pieces as keys, of this lane's tokens as values (four
+  // lanes a token and 16 columns, two for e4m3).  Both meet the place of a piece by an
+  // exclusive or below G * 16 bytes.
+  int key_at = lr * ROWB + (lq ^ joint_swap(G, lr)) * 16, value_at;
+  if constexpr (C8) {
+    const int k = lr >> 1, t = 4 * lq + (k & 3);
+    value_at = (16 * (k >> 2) + t) * ROWB + joint_swap(G, t) * 16 + 8 * (lane & 1);
+  } else {
+    const int t = 4 * lq + (lr >> 2);
+    value_at = t * ROWB + (((lane >> 1) & 1) ^ joint_swap(G, t)) * 16 + 8 * (lane & 1);
+  }
+
+  while (at < end) {
+    // ---- a segment: tiles t0 .. t1 - 1 of sequence b
+    int64_t first = 0, last = total;
+    int T = a.prefix_len;
+    if (!prefix) {
+      while (b + 1 < a.batch && a.start[b + 1] <= at) ++b;           // over sequences without tokens
+      first = a.start[b];
+      last = a.start[b + 1];
+      T = min(max(a.seq_lens[b], 0), a.max_context);
+    }
+    const int t0 = int(at - first), t1 = int(min(end, last) - first);
+    at = first + t1;
+    const int32_t* table = a.table + (prefix ? 0 : int64_t(b) * a.max_pages);
+    const int see_all = T - a.queries + 1;            // tokens that every row sees
+
+    const int mine = t1 - t0 > g ? (t1 - t0 - g + NG - 1) / NG : 0;  // tiles of this group
+    const int rounds = (t1 - t0 + NG - 1) / NG;
+    int ids = -1;                                     // lane i: the page of round (64-round window) + i
+    auto load_ids = [&](int r0) {
+      const int i = r0 + lane;
+      ids = i < mine ? table[(t0 + g + i * NG) >> 1] : -1;
+      if (ids >= a.num_pages) ids = -1;
+    };
+    int scales_next = 0;
+    auto issue = [&](int r, bool& valid) {            // the tile of round r into its buffer
+      valid = false;
+      if (r >= mine) return;
+      if ((r & 63) == 0) load_ids(r);
+      const int page = __builtin_amdgcn_readlane(ids, r & 63);
+      valid = page >= 0;
+      if (!valid) return;
+      const int half = (t0 + g + r * NG) & 1;
+      const uint8_t* src = a.pool + int64_t(page) * a.page_bytes + half * S::TILE + rw * 1024 + lane * 16;
+      unsigned char* dst = bufs + (r & (NBUF - 1)) * S::TILE + rw * 1024;
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i)
+        if (S::NL % WR == 0 || i < LOADS - 1 || i * WR + rw < S::NL)
+          load_lds16(src + i * (WR * 1024), dst + i * (WR * 1024));
+      if constexpr (C8)                               // lanes 0 .. 31 the latents' exponents, 32 .. the keys'
+        scales_next = a.pool[int64_t(page) * a.page_bytes + DCKV_PAGE_TOKENS * (W + (lane >> 5)) + half * kJointTile +
+                             (lane & 31)];
+    };
+    bool valid = false, next_valid = false;
+    issue(0, next_valid);
+
+    // ---- queries: row lr of the wave's 16, 8 columns a step (e4m3: 16 of two steps)
+    const int row = (slice * WR + rw) * 16 + lr;
+    const int rowc = min(row, rows - 1);
+    const uint8_t* qrow = static_cast<const uint8_t*>(a.q) +
+                          ((prefix ? 0 : int64_t(b) * rows) + rowc) * (W * 2);
+    u32x4 q[KS];
+#pragma unroll
+    for (int i = 0; i < KS; ++i) {
+      const int col = C8 && (i | 1) < KS ? 64 * (i >> 1) + 16 * lq + 8 * (i & 1) : 32 * i + 8 * lq;
+      q[i] = *reinterpret_cast<const u32x4*>(qrow + 2 * col);
+    }
+    // tokens of the segment's sequence that the row sees
+    int limit;
+    if (prefix) {
+      const int bb = rowc / (a.queries * a.heads), i = rowc / a.heads % a.queries;
+      const int own = min(max(a.seq_lens[bb], 0), a.max_context);
+      limit = int(min(int64_t(T), int64_t(T) + own - a.queries + i + 1));
+    } else {
+      limit = T - a.queries + rowc / a.heads + 1;
+    }
+
+    floatx4 acc[CT];
+#pragma unroll
+    for (int i = 0; i < CT; ++i) acc[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+    // m, u: references of the weights in l and in the sums (one for bf16)
+    float m = -INFINITY, u = -INFINITY, l = 0.f;
+
+    for (int r = 0; r < rounds; ++r) {
+      unsigned char* buf = bufs + (r & (NBUF - 1)) * S::TILE;
+      valid = next_valid;
+      const int pos = (t0 + g + r * NG) * kJointTile;  // the tile's first token
+      const int scales = scales_next;
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's part of the tile is in LDS
+      const bool edge = valid && pos + kJointTile > see_all;
+      uint32_t odd = 0;
+      if (edge) {
+        // tokens behind the sequence become zeros; a NaN in one that some rows see and
+        // others do not is taken out of the values and given back through the scores
+        uint32_t mask = 0;
+#pragma unroll 1
+        for (int i = 0; i < LOADS; ++i) {
+          if (i * WR + rw >= S::NL) break;
+          const int n = (i * WR + rw) * 64 + lane, t = n / S::PIECES;
+          u32x4* p = reinterpret_cast<u32x4*>(buf + n * 16);
+          if (pos + t >= T) {
+            *p = u32x4{0u, 0u, 0u, 0u};
+          } else if (pos + t >= see_all && odd_piece<C8>(*p)) {
+            *p = u32x4{0u, 0u, 0u, 0u};
+            mask |= 1u << t;
+          }
+        }
+        if (a.queries > 1) {
+#pragma unroll
+          for (int o = 32; o >= 1; o >>= 1) mask |= __shfl_xor(int(mask), o);
+          if (lane == 0) odd_of[r & 1][w] = mask;
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      }
+      if constexpr (WR > 1) __syncthreads();          // the tile is whole, the one before is used up
+      if constexpr (NBUF == 2) issue(r + 1, next_valid);
+      if (valid) {
+        if (edge && a.queries > 1) {
+#pragma unroll
+          for (int i = 0; i < WR; ++i) odd |= odd_of[r & 1][g * WR + i];
+        }
+        // ---- scores: tokens pos + 16 n + 4 lq + v, row lr
+        floatx4 s[2] = {floatx4{0.f, 0.f, 0.f, 0.f}, floatx4{0.f, 0.f, 0.f, 0.f}};
+        int ka = key_at;
+        asm volatile("" : "+v"(ka));                  // places are formed here, not kept for all steps
+        if constexpr (C8) {
+          float sc[2], sk[2];                         // powers of two of tokens lr, 16 + lr: latent, key
+#pragma unroll
+          for (int n = 0; n < 2; ++n) {
+            sc[n] = __uint_as_float(uint32_t(__shfl(scales, 16 * n + lr)) << 23);
+            sk[n] = __uint_as_float(uint32_t(__shfl(scales, 32 + 16 * n + lr)) << 23);
+          }
+          if (lane < 32) scale_of[w][lane] = float(scales) - 127.f;
+#pragma unroll
+          for (int i = 0; i < KS / 2; ++i)            // 64 columns
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+              const u32x4 x = *reinterpret_cast<const u32x4*>(
+                  buf + place<G>(ka, i) + n * 16 * ROWB);
+              const float f = 64 * i < R ? sc[n] : sk[n];
+              s[n] = mfma(widen(x[0], x[1], f), q[2 * i], s[n]);
+              s[n] = mfma(widen(x[2], x[3], f), q[2 * i + 1], s[n]);
+            }
+          if constexpr (KS % 2 == 1) {                // the last 32: 8 bytes a lane
+            const int t = lr, at8 = t * ROWB + (((W / 16 - 2 + (lq >> 1)) ^ joint_swap(G, t)) * 16) + 8 * (lq & 1);
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+              const u32x2 x = *reinterpret_cast<const u32x2*>(buf + at8 + n * 16 * ROWB);
+              s[n] = mfma(widen(x[0], x[1], sk[n]), q[KS - 1], s[n]);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < KS; ++i)
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+              const u32x4 x = *reinterpret_cast<const u32x4*>(buf + place<G>(ka, i) + n * 16 * ROWB);
+              s[n] = mfma(x, q[i], s[n]);
+            }
+        }
+        // ---- softmax
+        auto exponents = [&](int n) { return *reinterpret_cast<const floatx4*>(&scale_of[w][16 * n + 4 * lq]); };
+        float top = -INFINITY, utop = -INFINITY;
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            s[n][v] *= a.scale;
+            if (edge) {
+              const int t = 16 * n + 4 * lq + v;
+              s[n][v] = pos + t < limit ? ((odd >> t) & 1 ? __builtin_nanf("") : s[n][v]) : -INFINITY;
+            }
+            top = fmaxf(top, s[n][v]);
+          }
+          if constexpr (C8) {
+            const floatx4 ex = exponents(n);
+#pragma unroll
+            for (int v = 0; v < 4; ++v) utop = fmaxf(utop, s[n][v] + ex[v]);
+          }
+        }
+        top = row_max(top);
+        utop = C8 ? row_max(utop) : top;
+        if (__any(top > m + kSlack || utop > u + kSlack)) {
+          const float m_new = fmaxf(m, top), u_new = C8 ? fmaxf(u, utop) : m_new;
+          l *= m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m_new);
+          const float keep = u == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(u - u_new);
+          if (r > 0) {
+#pragma unroll
+            for (int i = 0; i < CT; ++i)
+#pragma unroll
+              for (int v = 0; v < 4; ++v) acc[i][v] *= keep;
+          }
+          m = m_new;
+          u = u_new;
+        }
+        const float mb = m == -INFINITY ? 0.f : m;     // nothing seen yet: weights 0
+        u32x4 p;
+        if constexpr (C8) {
+          const float ub = u == -INFINITY ? 0.f : u;
+#pragma unroll
+          for (int n = 0; n < 2; ++n) {
+            const floatx4 ex = exponents(n);
+            float y[4];
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+              l += __builtin_amdgcn_exp2f(s[n][v] - mb);
+              y[v] = __builtin_amdgcn_exp2f(s[n][v] + (ex[v] - ub));
+            }
+            p[2 * n] = pair(y[0], y[1]);
+            p[2 * n + 1] = pair(y[2], y[3]);
+          }
+        } else {
+          // the sum of the rounded weights: the result is an exact mean under them
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const uint32_t x = pair(__builtin_amdgcn_exp2f(s[k >> 1][2 * (k & 1)] - mb),
+                                    __builtin_amdgcn_exp2f(s[k >> 1][2 * (k & 1) + 1] - mb));
+            l += __uint_as_float(x << 16) + __uint_as_float(x & 0xFFFF0000u);
+            p[k] = x;
+          }
+        }
+        // ---- output: column 16 i + lr of the A operand, tokens 4 lq + 0 .. 3 and 16 more
+        int va = value_at;
+        asm volatile("" : "+v"(va));
+        if constexpr (C8) {
+#pragma unroll
+          for (int i = 0; i < CT; ++i) {
+            const v2i x = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+                (lds_v2i)(buf + (va ^ ((i & (G - 1)) * 16)) + i / G * (G * 16)));
+            acc[i] = mfma(widen(uint32_t(x[0]), uint32_t(x[1]), 1.f), p, acc[i]);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < CT; ++i) {
+            unsigned char* at = buf + (va ^ ((i & (G / 2 - 1)) * 32)) + i / (G / 2) * (G * 16);
+            const short4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4)(at));
+            const short4_t z = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4)(at + 16 * ROWB));
+            const auto xz = __builtin_shufflevector(x, z, 0, 1, 2, 3, 4, 5, 6, 7);
+            acc[i] = mfma(__builtin_bit_cast(u32x4, xz), p, acc[i]);
+          }
+        }
+      }
+      if constexpr (NBUF == 1) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");    // the tile is used up
+        issue(r + 1, next_valid);
+      }
+    }
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+
+    // ---- the token groups' states, CJ columns at a time
+    const int64_t seg = int64_t(unit) + (prefix ? 0 : b);
+    const int64_t prow = (seg * a.slices + slice) * (16 * WR);
+    if constexpr (NG == 1) {
+      if (row < rows) {
+        float* dst = a.part_o + (prow + rw * 16 + lr) * R + 4 * lq;
+#pragma unroll
+        for (int i = 0; i < CT; ++i) *reinterpret_cast<floatx4*>(dst + 16 * i) = acc[i];
+        if (lq == 0) a.part_ml[prow + rw * 16 + lr] = make_float4(m, l, u, 0.f);
+      }
+      __syncthreads();                                // the tiles are used up
+    } else {
+      constexpr int CJ = S::CJ, ST = CJ + 4;
+      if (lq == 0) {
+        join_m[w][lr] = m;
+        join_l[w][lr] = l;
+        join_u[w][lr] = u;
+      }
+      __syncthreads();                                // the tiles are used up, m and u are there
+      float mm = -INFINITY, uu = -INFINITY;
+#pragma unroll
+      for (int k = 0; k < NG; ++k) {
+        mm = fmaxf(mm, join_m[k * WR + rw][lr]);
+        uu = fmaxf(uu, join_u[k * WR + rw][lr]);
+      }
+      const float keep = u == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(u - uu);
+      if (g == 0 && lq == 0 && row < rows) {
+        float ll = 0.f;
+#pragma unroll
+        for (int k = 0; k < NG; ++k) {
+          const float mk = join_m[k * WR + rw][lr];
+          if (mk != -INFINITY || join_l[k * WR + rw][lr] != 0.f)
+            ll += join_l[k * WR + rw][lr] * __builtin_amdgcn_exp2f(mk - mm);
+        }
+        a.part_ml[prow + rw * 16 + lr] = make_float4(mm, ll, uu, 0.f);
+      }
+      float* ex = reinterpret_cast<float*>(smem);     // [wave][16 rows][ST]
+#pragma unroll
+      for (int c0 = 0; c0 < R; c0 += CJ) {
+        if (c0 > 0) __syncthreads();
+#pragma unroll
+        for (int i = 0; i < CJ / 16; ++i) {
+          floatx4 x;
+#pragma unroll
+          for (int v = 0; v < 4; ++v) x[v] = acc[c0 / 16 + i][v] * keep;
+          *reinterpret_cast<floatx4*>(ex + (w * 16 + lr) * ST + 16 * i + 4 * lq) = x;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int e = tid; e < WR * 16 * (CJ / 4); e += S::THREADS) {
+          const int rr = e / (CJ / 4), c = e % (CJ / 4) * 4;
+          if (slice * WR * 16 + rr >= rows) continue;
+          floatx4 x = *reinterpret_cast<const floatx4*>(ex + rr * ST + c);
+#pragma unroll
+          for (int k = 1; k < NG; ++k) x += *reinterpret_cast<const floatx4*>(ex + (k * WR * 16 + rr) * ST + c);
+          *reinterpret_cast<floatx4*>(a.part_o + (prow + rr) * R + c0 + c) = x;
+        }
+      }
+      __syncthreads();                                // before the next segment's tiles
+    }
+  }
+}
+
+template <int R, int P, bool C8>
+hipError_t launch_rows(int row_waves, const JointAttend& a, hipStream_t stream) {
+  const uint32_t groups = uint32_t((a.units + 7) / 8 * 8) * uint32_t(a.slices);
+  switch (row_waves) {
+    case 1: hipLaunchKernelGGL((joint_attend<R, P, C8, 1>), dim3(groups), dim3(64 * joint_waves(row_waves)), 0, stream, a); break;
+    case 2: hipLaunchKernelGGL((joint_attend<R, P, C8, 2>), dim3(groups), dim3(64 * joint_waves(row_waves)), 0, stream, a); break;
+    case 4: hipLaunchKernelGGL((joint_attend<R, P, C8, 4>), dim3(groups), dim3(64 * joint_waves(row_waves)), 0, stream, a); break;
+    case 8: hipLaunchKernelGGL((joint_attend<R, P, C8, 8>), dim3(groups), dim3(64 * joint_waves(row_waves)), 0, stream, a); break;
+    default: return hipErrorInvalidValue;
+  }
+  return hipGetLastError();
+}
+
+template <int R>
+hipError_t launch(const dckv_joint_desc& d, int row_waves, const JointAttend& a, hipStream_t stream) {
+  const bool c8 = d.cache == DCKV_JOINT_E4M3;
+  switch (d.rope_dim) {
+    case 0: return c8 ? launch_rows<R, 0, true>(row_waves, a, stream) : launch_rows<R, 0, false>(row_waves, a, stream);
+    case 32: return c8 ? launch_rows<R, 32, true>(row_waves, a, stream) : launch_rows<R, 32, false>(row_waves, a, stream);
+    case 64: return c8 ? launch_rows<R, 64, true>(row_waves, a, stream) : launch_rows<R, 64, false>(row_waves, a, stream);
+  }
+  return hipErrorInvalidValue;
+}
+
+}  // namespace joint
+}  // namespace dckv

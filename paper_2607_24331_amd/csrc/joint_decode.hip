@@ -1,0 +1,421 @@
+// The ends of the absorbed decode (gfx950): queries folded into the latent space
+// before the attend kernels, their shares joined and taken to the heads' values after.
+//
+//   q~_r = W_keys,h^T q_r,   o_r = W_values,h a_r,   a_r = sum_s 2^(u_s - M) O_s / sum_s 2^(m_s - M) l_s
+//
+// joint_fold    a wave a (head, 32 latent columns, 128 rows): the head's factor columns lie
+//               in LDS once, read by the transposing load, as the contraction runs over
+//               the factor's rows; products on MFMA 32x32x16, rounded to bf16 (2^-9 of a
+//               coordinate, independent ones in a score's sum over r).  One more wave forms
+//               the sequences' first tiles.  Bound by latency and, once, by the factor's bytes.
+// joint_finish  a work-group 1 or 4 rows of a head: its shares' sums in fp32, 16 bytes a
+//               lane, the whole work-group on one row's shares; then the product with the
+//               head's factor rows, eight or sixteen lanes a value column.  Bound by the
+//               shares' bytes and the factors' reads from the caches.
+#include <algorithm>
+#include <cmath>
+
+#include "joint_attend.h"
+
+namespace dckv {
+namespace {
+
+using joint::floatx4;
+using joint::short4_t;
+using joint::u32x4;
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+__device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(joint::bf16x8, a),
+                                                 __builtin_bit_cast(joint::bf16x8, b), c, 0, 0, 0);
+}
+
+constexpr int kFoldRows = 128;            // rows a wave, 32 at a time
+
+// starts[b]: tiles of the sequences before b, starts[batch] of all.  One wave, 16
+// sequences a lane.
+__device__ void form_starts(const int32_t* __restrict__ seq_lens, int max_context, int batch,
+                            int64_t* __restrict__ starts) {
+  const int lane = threadIdx.x;
+  int64_t base = 0;
+  for (int b0 = 0; b0 < batch; b0 += 1024) {
+    int n[16];
+    int64_t own = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int b = b0 + 16 * lane + i;
+      const int T = b < batch ? min(max(seq_lens[b], 0), max_context) : 0;
+      n[i] = (T + kJointTile - 1) / kJointTile;
+      own += n[i];
+    }
+    int64_t sum = own;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int64_t x = __shfl_up((long long)sum, o);
+      if (lane >= o) sum += x;
+    }
+    int64_t at = base + sum - own;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int b = b0 + 16 * lane + i;
+      if (b < batch) starts[b] = at;
+      at += n[i];
+    }
+    base += __shfl((long long)sum, 63);
+  }
+  if (lane == 0) starts[batch] = base;
+}
+
+template <int D>
+__global__ __launch_bounds__(64) void joint_fold(const bf16* __restrict__ q, const bf16* __restrict__ W_keys,
+                                                 int n, int heads, int r, int p, bf16* __restrict__ folded,
+                                                 const int32_t* __restrict__ seq_lens, int max_context,
+                                                 int batch, int64_t* __restrict__ starts) {
+  constexpr int ST = 40;                                       // elements a row of the factor in LDS
+  __shared__ __align__(16) bf16 wk[D * ST];
+  const int cols = r / 32;
+  if (int(blockIdx.x) == heads * cols) {
+    if (blockIdx.y == 0) form_starts(seq_lens, max_context, batch, starts);
+    return;
+  }
+  const int head = blockIdx.x / cols, c0 = (blockIdx.x % cols) * 32;
+  const int lane = threadIdx.x, lr = lane & 31, h = lane >> 5;
+  const int row0 = blockIdx.y * kFoldRows;
+  const bf16* src = W_keys + (int64_t(head) * D) * r + c0;
+  u32x4 piece[D / 16];
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i)
+    piece[i] = *reinterpret_cast<const u32x4*>(src + int64_t(16 * i + (lane >> 2)) * r + 8 * (lane & 3));
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i)
+    *reinterpret_cast<u32x4*>(wk + (16 * i + (lane >> 2)) * ST + 8 * (lane & 3)) = piece[i];
+  __syncthreads();
+  // B operand of step i: column lr, rows 16 i + 8 h .. + 7 of the factor, four a load
+  unsigned char* base = reinterpret_cast<unsigned char*>(wk + (8 * h + ((lane & 15) >> 2)) * ST +
+                                                         16 * ((lane >> 4) & 1) + 4 * (lane & 3));
+  u32x4 f[D / 16];
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) {
+    const short4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((joint::lds_short4)(base + (16 * i) * ST * 2));
+    const short4_t y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((joint::lds_short4)(base + (16 * i + 4) * ST * 2));
+    const auto xy = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+    f[i] = __builtin_bit_cast(u32x4, xy);
+  }
+  const int W = r + p;
+#pragma unroll 1
+  for (int r0 = row0; r0 < min(row0 + kFoldRows, n); r0 += 32) {
+    const bf16* qrow = q + (int64_t(min(r0 + lr, n - 1)) * heads + head) * (D + p);
+    f32x16 acc;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) acc[v] = 0.f;
+    u32x4 x[D / 16];
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) x[i] = *reinterpret_cast<const u32x4*>(qrow + 16 * i + 8 * h);
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) acc = mfma(x[i], f[i], acc);
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      const int row = r0 + 8 * (v >> 2) + 4 * h + (v & 3);
+      if (row < n) folded[(int64_t(row) * heads + head) * W + c0 + lr] = from_f32<bf16>(acc[v]);
+    }
+    if (c0 == 0 && r0 + lr < n)                                // the position part stays as it is
+      for (int j = 8 * h; j < p; j += 16)
+        *reinterpret_cast<u32x4*>(folded + (int64_t(r0 + lr) * heads + head) * W + r + j) =
+            *reinterpret_cast<const u32x4*>(qrow + D + j);
+  }
+}
+
+struct FinishArgs {
+  const int64_t* start;
+  const float* part_o;
+  const float4* part_ml;
+  const float* pre_o;
+  const float4* pre_ml;
+  int batch, queries, heads, row_rows, slices, units, groups;      // own: rows a work-group
+  int pre_row_rows, pre_slices, pre_units, pre_groups, prefix_len;
+};
+
+// RB rows (sequence, query) of one head; rows beyond `n` are skipped.
+template <int R, int D, int RB>
+__global__ __launch_bounds__(1024) void joint_finish(FinishArgs a, const bf16* __restrict__ W_values, int n,
+                                                     bf16* __restrict__ out) {
+  constexpr int C = R / 4, GR = 1024 / C;              // lanes a share, shares at a time
+  __shared__ __align__(16) floatx4 red[GR][C];
+  __shared__ __align__(16) float mean[RB][R];
+  __shared__ float wo[2 * kJointMaxUnits];
+  __shared__ int64_t where[2 * kJointMaxUnits];        // element offset of a share; prefix ones complemented
+  __shared__ float wave_m[16], wave_l[16];
+  const int head = blockIdx.x % a.heads, r0 = blockIdx.x / a.heads * RB;
+  const int tid = threadIdx.x, g = tid / C, c = tid % C;
+#pragma unroll 1
+  for (int k = 0; k < RB; ++k) {
+    const int row = r0 + k;
+    if (row >= n) break;
+    const int b = row / a.queries, i = row % a.queries;
+    // shares: those of the sequence's units, then the prefix's
+    const int64_t s0 = a.start[b], s1 = a.start[b + 1];
+    const int64_t per = joint_tiles_a_unit(a.start[a.batch], a.units, a.groups);
+    const int64_t u0 = s0 / per;
+    const int own = s1 > s0 ? int((s1 - 1) / per - u0) + 1 : 0;
+    int pre = 0;
+    if (a.prefix_len > 0) {
+      const int64_t tiles = (a.prefix_len + kJointTile - 1) / kJointTile;
+      const int64_t pp = joint_tiles_a_unit(tiles, a.pre_units, a.pre_groups);
+      pre = int((tiles + pp - 1) / pp);
+    }
+    const int ns = own + pre;                          // at most 2 kJointMaxUnits: a share a thread
+    float4 ml = make_float4(-INFINITY, 0.f, -INFINITY, 0.f);
+    if (tid < ns) {
+      int64_t at;
+      if (tid < own) {
+        const int rr = i * a.heads + head;
+        at = ((u0 + tid + b) * a.slices + rr / a.row_rows) * a.row_rows + rr % a.row_rows;
+        ml = a.part_ml[at];
+        where[tid] = at * R;
+      } else {
+        const int64_t rr = int64_t(row) * a.heads + head;
+        at = (int64_t(tid - own) * a.pre_slices + rr / a.pre_row_rows) * a.pre_row_rows + rr % a.pre_row_rows;
+        ml = a.pre_ml[at];
+        where[tid] = ~(at * R);
+      }
+    }
+    float M = ml.x;
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
+    if ((tid & 63) == 0) wave_m[tid >> 6] = M;
+    __syncthreads();
+#pragma unroll
+    for (int o = 0; o < 16; ++o) M = fmaxf(M, wave_m[o]);
+    // a share that saw nothing of the row has l = 0 and m = -inf
+    const bool some = ml.y != 0.f;
+    float l = some ? ml.y * __builtin_amdgcn_exp2f(ml.x - M) : 0.f;
+    if (tid < ns) wo[tid] = some ? __builtin_amdgcn_exp2f(ml.z - M) : 0.f;
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) l += __shfl_xor(l, o);
+    if ((tid & 63) == 0) wave_l[tid >> 6] = l;
+    __syncthreads();
+    floatx4 sum = {0.f, 0.f, 0.f, 0.f};
+    constexpr int U = 8;
+    for (int s = g; s < ns; s += U * GR) {
+      floatx4 x[U];
+#pragma unroll
+      for (int j = 0; j < U; ++j) {
+        if (s + j * GR >= ns) continue;
+        const int64_t at = where[s + j * GR];
+        x[j] = *reinterpret_cast<const floatx4*>((at < 0 ? a.pre_o + ~at : a.part_o + at) + 4 * c);
+      }
+#pragma unroll
+      for (int j = 0; j < U; ++j) {
+        if (s + j * GR >= ns) continue;
+        const float y = wo[s + j * GR];
+        if (y == 0.f) continue;                        // nothing seen: the sums may be infinite
+#pragma unroll
+        for (int v = 0; v < 4; ++v) sum[v] = fmaf(y, x[j][v], sum[v]);
+      }
+    }
+    red[g][c] = sum;
+    __syncthreads();
+    if (g == 0) {
+      float L = 0.f;
+#pragma unroll
+      for (int o = 0; o < 16; ++o) L += wave_l[o];
+#pragma unroll
+      for (int o = 1; o < GR; ++o) sum += red[o][c];
+#pragma unroll
+      for (int v = 0; v < 4; ++v) mean[k][4 * c + v] = L == 0.f ? 0.f : sum[v] / L;
+    }
+    __syncthreads();
+  }
+  // ---- values: LD lanes a column, 8 latent coordinates at a time
+  constexpr int LD = 1024 / D, PC = R / 8;
+  const int d = tid / LD, part = tid % LD;
+  const bf16* w = W_values + (int64_t(head) * D + d) * R;
+  float o[RB];
+#pragma unroll
+  for (int k = 0; k < RB; ++k) o[k] = 0.f;
+#pragma unroll
+  for (int j = 0; j < PC / LD; ++j) {
+    const int col = 8 * (j * LD + part);
+    const u32x4 x = *reinterpret_cast<const u32x4*>(w + col);
+#pragma unroll
+    for (int k = 0; k < RB; ++k) {
+      const floatx4 lo = *reinterpret_cast<const floatx4*>(&mean[k][col]);
+      const floatx4 hi = *reinterpret_cast<const floatx4*>(&mean[k][col + 4]);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        o[k] = fmaf(__uint_as_float(x[e] << 16), lo[2 * e], o[k]);
+        o[k] = fmaf(__uint_as_float(x[e] & 0xFFFF0000u), lo[2 * e + 1], o[k]);
+        o[k] = fmaf(__uint_as_float(x[2 + e] << 16), hi[2 * e], o[k]);
+        o[k] = fmaf(__uint_as_float(x[2 + e] & 0xFFFF0000u), hi[2 * e + 1], o[k]);
+      }
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < RB; ++k) {
+#pragma unroll
+    for (int e = LD >> 1; e >= 1; e >>= 1) o[k] += __shfl_xor(o[k], e);
+    if (part == 0 && r0 + k < n) out[(int64_t(r0 + k) * a.heads + head) * D + d] = from_f32<bf16>(o[k]);
+  }
+}
+
+size_t align_up(size_t v) { return (v + 255) / 256 * 256; }
+
+// Work-groups that fill the chip once at a rank.
+int fill(int rank) { return rank == 128 ? 512 : 256; }
+
+int64_t tiles_of(int64_t tokens) { return (tokens + kJointTile - 1) / kJointTile; }
+
+// Rows of a work-group, 16 a wave: the least of 16, 32, 64 that takes all of them, else 128.
+int row_waves_of(int64_t rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : rows <= 64 ? 4 : 8; }
+
+int groups_of(int row_waves) { return joint_waves(row_waves) / row_waves; }
+
+// Units of a slice for at most `tiles` tiles: fill the chip with the slices, a round
+// of the token groups at least, none more than the join holds.
+int units_of(int rank, int64_t slices, int64_t tiles, int groups) {
+  const int64_t want = std::min<int64_t>(std::max<int64_t>(1, (fill(rank) + slices / 2) / slices), kJointMaxUnits);
+  return int(std::max<int64_t>(1, std::min(want, (tiles + groups - 1) / groups)));
+}
+
+template <int R, int D>
+hipError_t finish(const FinishArgs& a, const void* W_values, int n, void* out, hipStream_t stream) {
+  // a work-group of four rows reads the factor for four; few rows are spread instead
+  if (int64_t(n) * a.heads >= 2048) {
+    hipLaunchKernelGGL((joint_finish<R, D, 4>), dim3(uint32_t((n + 3) / 4) * a.heads), dim3(1024), 0, stream, a,
+                       static_cast<const bf16*>(W_values), n, static_cast<bf16*>(out));
+  } else {
+    hipLaunchKernelGGL((joint_finish<R, D, 1>), dim3(uint32_t(n) * a.heads), dim3(1024), 0, stream, a,
+                       static_cast<const bf16*>(W_values), n, static_cast<bf16*>(out));
+  }
+  return hipGetLastError();
+}
+
+hipError_t attend(const dckv_joint_desc& d, int row_waves, const JointAttend& a, hipStream_t stream) {
+  switch (d.rank) {
+    case 128: return launch_joint_attend_128(d, row_waves, a, stream);
+    case 256: return launch_joint_attend_256(d, row_waves, a, stream);
+    case 512: return launch_joint_attend_512(d, row_waves, a, stream);
+  }
+  return hipErrorInvalidValue;
+}
+
+}  // namespace
+
+int64_t joint_page_bytes(const dckv_joint_desc& d) {
+  const int64_t width = d.rank + d.rope_dim;
+  return DCKV_PAGE_TOKENS * (d.cache == DCKV_JOINT_E4M3 ? width + 2 : 2 * width);
+}
+
+JointShape joint_shape(const dckv_joint_desc& d, int32_t queries, int32_t batch, int32_t max_context,
+                       int32_t prefix_len) {
+  JointShape s{};
+  s.d = d;
+  s.queries = queries;
+  s.batch = batch;
+  s.max_context = max_context;
+  s.prefix_len = prefix_len;
+  s.rows = queries * d.num_heads;
+  s.row_waves = row_waves_of(s.rows);
+  s.slices = (s.rows + 16 * s.row_waves - 1) / (16 * s.row_waves);
+  const int64_t tiles = int64_t(batch) * tiles_of(max_context);
+  s.units = units_of(d.rank, s.slices, tiles, groups_of(s.row_waves));
+  const int64_t all = int64_t(s.rows) * batch;
+  s.pre_row_waves = row_waves_of(all);
+  s.pre_slices = int32_t((all + 16 * s.pre_row_waves - 1) / (16 * s.pre_row_waves));
+  s.pre_units = prefix_len > 0 ? units_of(d.rank, s.pre_slices, tiles_of(prefix_len), groups_of(s.pre_row_waves)) : 0;
+  const size_t width = size_t(d.rank + d.rope_dim);
+  s.off_start = align_up(size_t(all) * width * 2);
+  s.off_o = s.off_start + align_up(size_t(batch + 1) * 8);
+  const size_t own = size_t(s.units + batch) * s.slices * 16 * s.row_waves;
+  s.off_ml = s.off_o + align_up(own * d.rank * 4);
+  s.off_pre_o = s.off_ml + align_up(own * 16);
+  const size_t pre = size_t(s.pre_units) * s.pre_slices * 16 * s.pre_row_waves;
+  s.off_pre_ml = s.off_pre_o + align_up(pre * d.rank * 4);
+  s.bytes = s.off_pre_ml + align_up(pre * 16);
+  return s;
+}
+
+// Everything but the prefix's shares grows with the batch and the context.  Their rows
+// are slices * rows * units, units at most (fill + slices / 2) / slices or 1 and at most
+// the prefix's tiles: at most (fill + 1.5 slices) * 128 and all rows, padded, times the
+// tiles; both bounds grow with the batch and the prefix.
+size_t joint_workspace_bytes(const JointShape& s) {
+  if (s.prefix_len == 0) return s.bytes;
+  const size_t all = (size_t(s.rows) * s.batch + 127) / 128 * 128;
+  const size_t rows = std::min(size_t(fill(s.d.rank)) * 128 + all + all / 2, all * size_t(tiles_of(s.prefix_len)));
+  return s.off_pre_o + align_up(rows * s.d.rank * 4) + align_up(rows * 16);
+}
+
+hipError_t launch_joint_decode(const JointShape& s, const void* q, const void* pool, int64_t num_pages,
+                               const int32_t* page_table, int32_t max_pages, const int32_t* seq_lens,
+                               const int32_t* prefix_pages, const void* W_keys, const void* W_values,
+                               void* out, void* workspace, hipStream_t stream) {
+  char* ws = static_cast<char*>(workspace);
+  const dckv_joint_desc& d = s.d;
+  const int n = s.batch * s.queries;                   // at most 65535
+  int64_t* starts = reinterpret_cast<int64_t*>(ws + s.off_start);
+  const dim3 grid(d.num_heads * (d.rank / 32) + 1, (n + kFoldRows - 1) / kFoldRows);
+#define DCKV_FOLD(D)                                                                                         \
+  hipLaunchKernelGGL((joint_fold<D>), grid, dim3(64), 0, stream, static_cast<const bf16*>(q),                 \
+                     static_cast<const bf16*>(W_keys), n, d.num_heads, d.rank, d.rope_dim,                    \
+                     reinterpret_cast<bf16*>(ws), seq_lens, s.max_context, s.batch, starts)
+  if (d.head_dim == 64)
+    DCKV_FOLD(64);
+  else
+    DCKV_FOLD(128);
+#undef DCKV_FOLD
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  JointAttend a{};
+  a.q = ws;
+  a.pool = static_cast<const uint8_t*>(pool);
+  a.num_pages = num_pages;
+  a.page_bytes = joint_page_bytes(d);
+  a.start = starts;
+  a.seq_lens = seq_lens;
+  a.max_context = s.max_context;
+  a.batch = s.batch;
+  a.queries = s.queries;
+  a.heads = d.num_heads;
+  a.scale = kLog2e * (d.scale != 0.f ? d.scale : 1.f / std::sqrt(float(d.head_dim + d.rope_dim)));
+  if (s.prefix_len > 0) {
+    JointAttend p = a;
+    p.table = prefix_pages;
+    p.units = s.pre_units;
+    p.slices = s.pre_slices;
+    p.prefix_len = s.prefix_len;
+    p.part_o = reinterpret_cast<float*>(ws + s.off_pre_o);
+    p.part_ml = reinterpret_cast<float4*>(ws + s.off_pre_ml);
+    e = attend(d, s.pre_row_waves, p, stream);
+    if (e != hipSuccess) return e;
+  }
+  a.table = page_table;
+  a.max_pages = max_pages;
+  a.units = s.units;
+  a.slices = s.slices;
+  a.part_o = reinterpret_cast<float*>(ws + s.off_o);
+  a.part_ml = reinterpret_cast<float4*>(ws + s.off_ml);
+  if (s.max_context > 0) {
+    e = attend(d, s.row_waves, a, stream);
+    if (e != hipSuccess) return e;
+  }
+  const FinishArgs f{starts, a.part_o, a.part_ml, reinterpret_cast<const float*>(ws + s.off_pre_o),
+                     reinterpret_cast<const float4*>(ws + s.off_pre_ml), s.batch, s.queries, d.num_heads,
+                     16 * s.row_waves, s.slices, s.units, groups_of(s.row_waves), 16 * s.pre_row_waves,
+                     s.pre_slices, s.pre_units, groups_of(s.pre_row_waves), s.prefix_len};
+#define DCKV_FINISH(R, D) return finish<R, D>(f, W_values, n, out, stream)
+  if (d.rank == 128) {
+    if (d.head_dim == 64) DCKV_FINISH(128, 64);
+    DCKV_FINISH(128, 128);
+  }
+  if (d.rank == 256) {
+    if (d.head_dim == 64) DCKV_FINISH(256, 64);
+    DCKV_FINISH(256, 128);
+  }
+  if (d.head_dim == 64) DCKV_FINISH(512, 64);
+  DCKV_FINISH(512, 128);
+#undef DCKV_FINISH
+}
+
+}  // namespace dckv
