@@ -324,6 +324,7 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
 #pragma unroll
           for (int v = 0; v < 4; ++v) {
             s[n][v] *= a.scale;
+            s[n][v] += s[n][v] - s[n][v];              // an infinite score becomes NaN
             if (edge) {
               const int t = 16 * n + 4 * lq + v;
               s[n][v] = pos + t < limit ? ((odd >> t) & 1 ? __builtin_nanf("") : s[n][v]) : -INFINITY;

@@ -1,9 +1,565 @@
+// Prompts over the joint cache in the expanded form (gfx950).
+//
+//   key_h,t = [W_keys,h c_t ; k_t],  value_h,t = W_values,h c_t,
+//   o_r = sum_t softmax_t(scale q_r . key_t) value_t over the tokens t up to row r's own
+//
+// Four launches:
+//   prompt_plan    one work-group: the tiles of 64 tokens of the sequences that have rows,
+//                  and the tiles of 128 rows, those with the most tokens first.
+//   prompt_gather  a work-group a token tile: latents in bf16 side by side, position keys
+//                  as the attention's LDS wants them, and which tokens are there and finite.
+//   prompt_expand  every head's keys and values, a 128 x 128 product tile a work-group on
+//                  MFMA 16x16x32; the latents' and factors' rows come by the loads' LDS path.
+//                  Keys go out a token's coordinates side by side, values a coordinate's
+//                  tokens, both in the order in which a lane of the attention needs them
+//                  and in the places of its LDS tiles.
+//   prompt_attend  a work-group 128 rows of a head, 32 a wave, over token tiles that come in
+//                  two buffers: scores S[token][row] and sums O[coordinate][row] on MFMA 32x32x16,
+//                  so that the weights feed the second product from the registers they
+//                  were made in, and the running maximum is a lane's own.
+// Bound by the products: 4 T r d + 2 pairs (2 d + p) a head, and in the attention by LDS,
+// which 32 rows a wave read as fast as the products of a tile go.
+#include <algorithm>
+#include <cmath>
+
+#include "device.h"
 #include "joint.h"
+
 namespace dckv {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kRows = 128;                // rows of a tile
+constexpr int kTok = 64;                  // tokens of a tile
+constexpr float kSlack = 6.f;             // the maximum is raised by whole jumps of 2^6 and more
+constexpr float kMaxBf16 = 3.3895313892515355e38f;
+
+struct RowTile {
+  int32_t row, n, kv, first;              // first row, rows, first token tile (-1: does not fit), position of the first row
+};
+
+struct PromptArgs {
+  const int32_t *row_start, *seq_lens;
+  int32_t n_rows, batch, max_context;
+  int64_t total_context;
+  int32_t q_tiles, kv_tiles;              // at most
+  int32_t* counts;                        // row tiles, token tiles
+  RowTile* rows;
+  int2* toks;                             // sequence, tile
+  uint2* there;                           // per token tile: tokens that are there
+  uint2* odd;                             // and those that are not finite
+};
+
+__device__ __forceinline__ int wave_scan(int x, int lane) {
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int y = __shfl_up(x, o);
+    if (lane >= o) x += y;
+  }
+  return x;
+}
+
+__device__ __forceinline__ int64_t wave_scan(int64_t x, int lane) {
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int64_t y = __shfl_up((long long)x, o);
+    if (lane >= o) x += y;
+  }
+  return x;
+}
+
+__global__ __launch_bounds__(1024) void prompt_plan(PromptArgs a) {
+  constexpr int kBins = 128;
+  __shared__ int wave_rows[16], wave_toks[16];
+  __shared__ int64_t wave_len[16];
+  __shared__ int bins[kBins];
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  for (int i = tid; i < kBins; i += 1024) bins[i] = 0;
+  const int most = (a.max_context + kTok - 1) / kTok + 1;
+  // two walks over the sequences: the first counts row tiles by their tokens, the second
+  // writes them, most tokens first (which place a tile takes among those of a bin does
+  // not change what it computes)
+  for (int walk = 0; walk < 2; ++walk) {
+    int toks = 0;                         // token tiles of the sequences before
+    int64_t len = 0;                      // their tokens
+    for (int b0 = 0; b0 < a.batch; b0 += 1024) {
+      const int b = b0 + tid;
+      int lo = 0, n = 0, T = 0;
+      if (b < a.batch) {
+        lo = min(max(a.row_start[b], 0), a.n_rows);
+        n = min(max(a.row_start[b + 1], lo), a.n_rows) - lo;
+        T = n > 0 ? min(max(a.seq_lens[b], 0), a.max_context) : 0;
+      }
+      const int own = (T + kTok - 1) / kTok;
+      const int64_t len_to = wave_scan(int64_t(T), lane);
+      if (lane == 63) wave_len[w] = len_to;
+      __syncthreads();
+      int64_t before = len;
+      for (int i = 0; i < w; ++i) before += wave_len[i];
+      const bool fits = before + len_to <= a.total_context;
+      for (int i = 0; i < 16; ++i) len += wave_len[i];
+      const int toks_to = wave_scan(fits ? own : 0, lane);
+      if (lane == 63) wave_toks[w] = toks_to;
+      __syncthreads();
+      int kv = toks + toks_to - (fits ? own : 0);
+      for (int i = 0; i < w; ++i) kv += wave_toks[i];
+      for (int i = 0; i < 16; ++i) toks += wave_toks[i];
+      const bool room = fits && kv + own <= a.kv_tiles;         // always, where row_start ascends
+      if (walk == 1 && fits)
+        for (int i = 0; i < own; ++i)
+          if (kv + i < a.kv_tiles) a.toks[kv + i] = make_int2(b, i);
+      for (int i = 0; i * kRows < n; ++i) {
+        const int last = T - n + min((i + 1) * kRows, n);       // tokens that the tile's last row sees
+        const int bin = kBins - 1 - int(int64_t((max(last, 0) + kTok - 1) / kTok) * kBins / most);
+        if (walk == 0) {
+          atomicAdd(&bins[bin], 1);
+        } else {
+          const int at = atomicAdd(&bins[bin], 1);
+          if (at < a.q_tiles)
+            a.rows[at] = RowTile{lo + i * kRows, min(kRows, n - i * kRows), room ? kv : -1, T - n + i * kRows};
+        }
+      }
+      __syncthreads();
+    }
+    if (walk == 0) {
+      // bins to their first places
+      int x = 0;
+      if (w == 0) {
+        const int p = bins[2 * lane], q = bins[2 * lane + 1];
+        x = wave_scan(p + q, lane);
+        bins[2 * lane] = x - p - q;
+        bins[2 * lane + 1] = x - q;
+        if (lane == 63) a.counts[0] = min(x, a.q_tiles);
+      }
+    } else if (tid == 0) {
+      a.counts[1] = min(toks, a.kv_tiles);
+    }
+    __syncthreads();
+  }
+}
+
+__device__ __forceinline__ uint32_t pair(float a, float b) {
+  return uint32_t(__builtin_bit_cast(uint16_t, from_f32<bf16>(a))) |
+         uint32_t(__builtin_bit_cast(uint16_t, from_f32<bf16>(b))) << 16;
+}
+
+// Piece i of row s of an LDS tile of g-piece rows lies at piece i ^ joint_swap(g, s).
+struct GatherArgs {
+  const uint8_t* pool;
+  int64_t num_pages, page_bytes;
+  const int32_t* page_table;
+  int32_t max_pages, r, p;
+  bf16* c;                                // [tiles * 64][r]
+  uint8_t* rope;                          // [tiles][64 rows of p], in LDS places
+};
+
+template <bool C8>
+__global__ __launch_bounds__(256) void prompt_gather(PromptArgs a, GatherArgs s) {
+  __shared__ uint32_t odd[2];
+  const int tile = blockIdx.x, tid = threadIdx.x;
+  if (tile >= a.counts[1]) return;
+  const int2 at = a.toks[tile];
+  const int T = min(max(a.seq_lens[at.x], 0), a.max_context) - at.y * kTok;
+  int page = s.page_table[int64_t(at.x) * s.max_pages + at.y];
+  if (page >= s.num_pages) page = -1;
+  const int have = page < 0 ? 0 : min(T, kTok);
+  if (tid < 2) odd[tid] = 0;
+  __syncthreads();
+  const int w = s.r + s.p, per = C8 ? 16 : 8, pieces = w / per, g = joint_gcd16(pieces);
+  const int rg = joint_gcd16(s.p / 8);
+  const uint8_t* src = s.pool + int64_t(max(page, 0)) * s.page_bytes;
+  for (int i = tid; i < kTok * pieces; i += 256) {
+    const int t = i / pieces, piece = (i % pieces) ^ joint_swap(g, t);   // reads a page in order
+    const int col = piece * per;
+    u32x4 x[C8 ? 2 : 1];
+    bool bad = false;
+    if (t < have) {
+      const u32x4 y = *reinterpret_cast<const u32x4*>(src + i * 16);
+      if constexpr (C8) {
+        const float f = __uint_as_float(uint32_t(src[kTok * (w + (col < s.r ? 0 : 1)) + t]) << 23);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          bad |= (((y[k] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) != 0;
+          x[k >> 1][2 * (k & 1)] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(y[k], f, false));
+          x[k >> 1][2 * (k & 1) + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(y[k], f, true));
+        }
+      } else {
+        x[0] = y;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) bad |= (((y[k] & 0x7F807F80u) + 0x00800080u) & 0x80008000u) != 0;
+      }
+    }
+    if (bad) atomicOr(&odd[t >> 5], 1u << (t & 31));
+    if (bad || t >= have)
+#pragma unroll
+      for (int k = 0; k < (C8 ? 2 : 1); ++k) x[k] = u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int k = 0; k < (C8 ? 2 : 1); ++k) {
+      const int j = col + 8 * k;
+      if (j < s.r)
+        *reinterpret_cast<u32x4*>(s.c + (int64_t(tile) * kTok + t) * s.r + j) = x[k];
+      else
+        *reinterpret_cast<u32x4*>(s.rope + (int64_t(tile) * kTok + t) * s.p * 2 +
+                                  (((j - s.r) / 8) ^ joint_swap(rg, t)) * 16) = x[k];
+    }
+  }
+  __syncthreads();
+  if (tid == 0) {
+    a.odd[tile] = make_uint2(odd[0], odd[1]);
+    a.there[tile] = make_uint2(have >= 32 ? ~0u : (1u << have) - 1u,
+                               have >= 64 ? ~0u : have > 32 ? (1u << (have - 32)) - 1u : 0u);
+  }
+}
+
+__device__ __forceinline__ void load_lds16(const void* g, unsigned char* p) {
+  __builtin_amdgcn_global_load_lds(static_cast<const uint8_t*>(g), p, 16, 0, 0);
+}
+
+// 128 tokens x 128 of the heads' key and value coordinates, 64 x 64 a wave; k in stages
+// of 64 in two buffers.  LDS rows of 128 bytes, piece i of row s at i ^ s % 8.
+template <int D>
+__global__ __launch_bounds__(256, 2) void prompt_expand(const int32_t* __restrict__ counts,
+                                                        const bf16* __restrict__ c,
+                                                        const bf16* __restrict__ W_keys,
+                                                        const bf16* __restrict__ W_values, int heads, int r,
+                                                        int kv_tiles, uint8_t* __restrict__ keys,
+                                                        uint8_t* __restrict__ values) {
+  constexpr int HALF = 128 * 128, BUF = 2 * HALF;
+  __shared__ __align__(1024) unsigned char smem[2 * BUF];
+  const int tiles = D == 128 ? 2 * heads : heads;      // of 128 coordinates
+  const int f = blockIdx.x % tiles, blk = blockIdx.x / tiles;
+  const int n_tok = counts[1] * kTok;
+  if (blk * 128 >= n_tok) return;
+  const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lq = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wt = w & 1, wf = w >> 1;                   // this wave's 64 tokens, 64 coordinates
+  const int head = D == 128 ? f >> 1 : f;
+  // rows of a stage: 128 tokens, 128 coordinates; a load brings 8 of them
+  const int row = lane >> 3, piece = (lane & 7) ^ row;
+  const bf16* src[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int n = (8 * w + i) * 8 + row;               // waves 0, 1 the tokens, 2, 3 the coordinates
+    if (w < 2) {
+      src[i] = c + int64_t(min(blk * 128 + n, n_tok - 1)) * r;
+    } else {
+      const int k = n - 128;
+      const bf16* W = (D == 128 ? f & 1 : k >= 64) ? W_values : W_keys;
+      src[i] = W + (int64_t(head) * D + (D == 128 ? k : k & 63)) * r;
+    }
+    src[i] += 8 * piece;
+  }
+  auto issue = [&](int st) {
+    unsigned char* dst = smem + (st & 1) * BUF + w * 8192;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) load_lds16(src[i] + st * 64, dst + i * 1024);
+  };
+  const bool value = D == 128 ? f & 1 : wf == 1;       // what this wave forms
+  floatx4 acc[4][4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+  // rows of the product are coordinates for keys, tokens for values
+  const int arow = (value ? 0 : 128) + (value ? wt : wf) * 64, brow = (value ? 128 : 0) + (value ? wf : wt) * 64;
+  const int nst = r / 64;
+  issue(0);
+  for (int st = 0; st < nst; ++st) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();                                   // the stage is whole, the one before is used up
+    if (st + 1 < nst) issue(st + 1);
+    unsigned char* buf = smem + (st & 1) * BUF;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      u32x4 x[4], y[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int p = ((4 * k + lq) ^ (lr & 7)) * 16;
+        x[i] = *reinterpret_cast<const u32x4*>(buf + (arow + 16 * i + lr) * 128 + p);
+        y[i] = *reinterpret_cast<const u32x4*>(buf + (brow + 16 * i + lr) * 128 + p);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x[i]),
+                                                              __builtin_bit_cast(bf16x8, y[j]), acc[i][j], 0, 0, 0);
+    }
+  }
+  // a lane holds rows 16 i + 4 lq + v of column 16 j + lr; pieces 4 s + lq of a column hold
+  // its rows 32 s + 4 lq + 0 .. 3 and 32 s + 16 + 4 lq + 0 .. 3
+  const int tile = blk * 2 + wt;                       // of 64 tokens
+  if (tile * kTok >= n_tok) return;
+  uint8_t* out = (value ? values : keys) + (int64_t(head) * kv_tiles + tile) * (kTok * D * 2);
+  const int col0 = value ? (D == 128 ? wf * 64 : 0) : 0;     // a value tile's first coordinate
+  const int s0 = value ? 0 : (D == 128 ? wf * 2 : 0);        // a key's first 32 coordinates
+  constexpr int KG = D == 128 ? 16 : 8;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int col = col0 + 16 * j + lr;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      floatx4 lo = acc[2 * s][j], hi = acc[2 * s + 1][j];
+      if (value)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {                  // a weight of 0 times an infinity would be none
+          lo[v] = fminf(fmaxf(lo[v], -kMaxBf16), kMaxBf16);
+          hi[v] = fminf(fmaxf(hi[v], -kMaxBf16), kMaxBf16);
+        }
+      const u32x4 x = {pair(lo[0], lo[1]), pair(lo[2], lo[3]), pair(hi[0], hi[1]), pair(hi[2], hi[3])};
+      const int piece = 4 * (s0 + s) + lq;
+      const int at = value ? col * (kTok * 2) + (piece ^ joint_swap(8, col)) * 16
+                           : col * (D * 2) + (piece ^ joint_swap(KG, col)) * 16;
+      *reinterpret_cast<u32x4*>(out + at) = x;
+    }
+  }
+}
+
+__device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b),
+                                                 c, 0, 0, 0);
+}
+
+template <int D, int P>
+__global__ __launch_bounds__(256, 2) void prompt_attend(PromptArgs a, const uint8_t* __restrict__ keys,
+                                                        const uint8_t* __restrict__ rope,
+                                                        const uint8_t* __restrict__ values,
+                                                        const bf16* __restrict__ q, int heads, float scale,
+                                                        bf16* __restrict__ out) {
+  constexpr int KB = kTok * D * 2, PB = kTok * P * 2, TILE = 2 * KB + PB;
+  constexpr int KL = KB / 1024, PL = PB / 1024, NL = 2 * KL + PL;    // 1 KB loads
+  constexpr int KG = joint_gcd16(D / 8), PG = P > 0 ? joint_gcd16(P / 8) : 1;
+  constexpr int DS = D / 16, PS = P / 16, CT = D / 32;
+  __shared__ __align__(1024) unsigned char smem[2 * TILE];
+  const int head = blockIdx.x % heads, qt = blockIdx.x / heads;
+  if (qt >= a.counts[0]) return;
+  const RowTile rt = a.rows[qt];
+  const int tid = threadIdx.x, lane = tid & 63, lr = lane & 31, h = lane >> 5;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int my = w * 32 + lr;                          // row of the tile
+  const int64_t row = rt.row + min(my, rt.n - 1);
+  const int limit = rt.first + my + 1;                 // tokens that the row sees
+  const int all = rt.first + rt.n;                     // that the last row sees
+  const int tiles = rt.kv < 0 || all <= 0 ? 0 : (all + kTok - 1) / kTok;
+  const uint8_t* ksrc = keys + (int64_t(head) * a.kv_tiles + rt.kv) * KB + lane * 16;
+  const uint8_t* vsrc = values + (int64_t(head) * a.kv_tiles + rt.kv) * KB + lane * 16;
+  const uint8_t* psrc = rope + int64_t(rt.kv) * PB + lane * 16;
+  auto issue = [&](int t) {
+    unsigned char* dst = smem + (t & 1) * TILE;
+#pragma unroll
+    for (int i = 0; i < NL / 4; ++i) {
+      const int n = 4 * i + w;                         // keys, then position keys, then values
+      const uint8_t* src = n < KL ? ksrc + int64_t(t) * KB + n * 1024
+                                  : n < KL + PL ? psrc + int64_t(t) * PB + (n - KL) * 1024
+                                                : vsrc + int64_t(t) * KB + (n - KL - PL) * 1024;
+      load_lds16(src, dst + n * 1024);
+    }
+  };
+  static_assert(NL % 4 == 0, "whole loads");
+  if (tiles > 0) issue(0);
+
+  // queries: pieces 2 i + h of row lr, in the keys' order of coordinates
+  u32x4 qd[DS], qp[PS > 0 ? PS : 1];
+  const bf16* qrow = q + (row * heads + head) * (D + P);
+#pragma unroll
+  for (int i = 0; i < DS; ++i) {
+    const int piece = 2 * i + h, at = 32 * (piece >> 2) + 4 * (piece & 3);
+    const u32x2 lo = *reinterpret_cast<const u32x2*>(qrow + at), hi = *reinterpret_cast<const u32x2*>(qrow + at + 16);
+    qd[i] = u32x4{lo[0], lo[1], hi[0], hi[1]};
+  }
+#pragma unroll
+  for (int i = 0; i < PS; ++i) qp[i] = *reinterpret_cast<const u32x4*>(qrow + D + 16 * i + 8 * h);
+
+  f32x16 acc[CT];
+#pragma unroll
+  for (int i = 0; i < CT; ++i)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) acc[i][v] = 0.f;
+  float m = -INFINITY, l = 0.f;
+  const int ksw = joint_swap(KG, lr), psw = P > 0 ? joint_swap(PG, lr) : 0, vsw = joint_swap(8, lr);
+
+  for (int t = 0; t < tiles; ++t) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();                                   // the tile is whole, the one before is used up
+    if (t + 1 < tiles) issue(t + 1);
+    unsigned char* buf = smem + (t & 1) * TILE;
+    const uint2 there = a.there[rt.kv + t], odd = a.odd[rt.kv + t];
+    const int pos = t * kTok;
+    // rows of the wave that do not see the whole tile, or a tile with holes
+    const bool edge = pos + kTok > rt.first + w * 32 + 1 || (there.x & there.y) != ~0u || (odd.x | odd.y) != 0;
+
+    // ---- scores: tokens pos + 32 n + 8 b + 4 h + v (register 4 b + v), row lr
+    f32x16 s[2];
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+#pragma unroll
+      for (int v = 0; v < 16; ++v) s[n][v] = 0.f;
+#pragma unroll
+      for (int i = 0; i < DS; ++i)
+        s[n] = mfma(*reinterpret_cast<const u32x4*>(buf + (32 * n + lr) * (D * 2) + ((2 * i + h) ^ ksw) * 16), qd[i], s[n]);
+#pragma unroll
+      for (int i = 0; i < PS; ++i)
+        s[n] = mfma(*reinterpret_cast<const u32x4*>(buf + KB + (32 * n + lr) * (P * 2) + ((2 * i + h) ^ psw) * 16), qp[i], s[n]);
+    }
+    // ---- softmax; an infinite score becomes NaN
+    float top = -INFINITY;
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        float x = s[n][v] * scale;
+        x += x - x;
+        if (edge) {
+          const int b = 8 * (v >> 2) + 4 * h + (v & 3);
+          const uint32_t th = n ? there.y : there.x, od = n ? odd.y : odd.x;
+          x = pos + 32 * n + b < limit && ((th >> b) & 1) ? ((od >> b) & 1 ? __builtin_nanf("") : x) : -INFINITY;
+        }
+        s[n][v] = x;
+        top = fmaxf(top, x);
+      }
+    top = fmaxf(top, __shfl_xor(top, 32));
+    if (__any(top > m + kSlack)) {
+      const float m_new = fmaxf(m, top);
+      const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m_new);
+      l *= keep;
+      if (t > 0) {
+#pragma unroll
+        for (int i = 0; i < CT; ++i)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) acc[i][v] *= keep;
+      }
+      m = m_new;
+    }
+    const float mb = m == -INFINITY ? 0.f : m;
+    u32x4 p[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)                        // step k: tokens 32 n + 8 b + 4 h and 16 further, b = k % 2
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int n = k >> 1, v = 4 * (k & 1) + 8 * (e >> 1) + 2 * (e & 1);
+        const uint32_t x = pair(__builtin_amdgcn_exp2f(s[n][v] - mb), __builtin_amdgcn_exp2f(s[n][v + 1] - mb));
+        l += __uint_as_float(x << 16) + __uint_as_float(x & 0xFFFF0000u);
+        p[k][e] = x;
+      }
+    // ---- output: coordinate 32 i + lr of the A operand, piece 2 k + h of its tokens
+    const unsigned char* vb = buf + KB + PB + lr * (kTok * 2);
+#pragma unroll
+    for (int i = 0; i < CT; ++i)
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        acc[i] = mfma(*reinterpret_cast<const u32x4*>(vb + i * (32 * kTok * 2) + ((2 * k + h) ^ vsw) * 16), p[k], acc[i]);
+  }
+  l += __shfl_xor(l, 32);
+  if (my >= rt.n) return;
+  bf16* dst = out + (row * heads + head) * D + 4 * h;
+  const float inv = rt.kv < 0 ? __builtin_nanf("") : l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+  for (int i = 0; i < CT; ++i)
+#pragma unroll
+    for (int b = 0; b < 4; ++b)
+      *reinterpret_cast<u32x2*>(dst + 32 * i + 8 * b) = u32x2{pair(acc[i][4 * b] * inv, acc[i][4 * b + 1] * inv),
+                                                             pair(acc[i][4 * b + 2] * inv, acc[i][4 * b + 3] * inv)};
+}
+
+size_t align_up(size_t v) { return (v + 255) / 256 * 256; }
+
+}  // namespace
+
 JointPrompt joint_prompt(const dckv_joint_desc& d, int32_t batch, int32_t n_rows, int32_t max_context,
-                         int64_t total_context) { return JointPrompt{}; }
+                         int64_t total_context) {
+  JointPrompt s{};
+  s.d = d;
+  s.n_rows = n_rows;
+  s.batch = batch;
+  s.max_context = max_context;
+  s.total_context = total_context;
+  // a sequence with rows adds at most one tile that is not full
+  const int64_t some = std::min(batch, n_rows);
+  s.q_tiles = n_rows / kRows + some;
+  s.kv_tiles = std::min<int64_t>(total_context / kTok + some, some * ((int64_t(max_context) + kTok - 1) / kTok));
+  s.kv_tiles = (s.kv_tiles + 1) / 2 * 2;               // whole blocks of 128 tokens
+  const size_t kv = size_t(s.kv_tiles);
+  s.off_qtile = 256;
+  s.off_kvtile = s.off_qtile + align_up(size_t(s.q_tiles) * sizeof(RowTile));
+  s.off_flags = s.off_kvtile + align_up(kv * sizeof(int2));
+  s.off_c = s.off_flags + 2 * align_up(kv * sizeof(uint2));
+  s.off_rope = s.off_c + align_up(kv * kTok * d.rank * 2);
+  s.off_k = s.off_rope + align_up(kv * kTok * d.rope_dim * 2);
+  const size_t heads = kv * kTok * d.head_dim * 2 * d.num_heads;
+  s.off_v = s.off_k + align_up(heads);
+  s.bytes = s.off_v + align_up(heads);
+  return s;
+}
+
 hipError_t launch_joint_prefill(const JointPrompt& s, const void* q, const int32_t* row_start,
                                 const void* pool, int64_t num_pages, const int32_t* page_table,
                                 int32_t max_pages, const int32_t* seq_lens, const void* W_keys,
-                                const void* W_values, void* out, void* workspace, hipStream_t stream) { return hipErrorInvalidValue; }
+                                const void* W_values, void* out, void* workspace, hipStream_t stream) {
+  const dckv_joint_desc& d = s.d;
+  char* ws = static_cast<char*>(workspace);
+  PromptArgs a{};
+  a.row_start = row_start;
+  a.seq_lens = seq_lens;
+  a.n_rows = s.n_rows;
+  a.batch = s.batch;
+  a.max_context = s.max_context;
+  a.total_context = s.total_context;
+  a.q_tiles = int32_t(s.q_tiles);
+  a.kv_tiles = int32_t(s.kv_tiles);
+  a.counts = reinterpret_cast<int32_t*>(ws);
+  a.rows = reinterpret_cast<RowTile*>(ws + s.off_qtile);
+  a.toks = reinterpret_cast<int2*>(ws + s.off_kvtile);
+  a.there = reinterpret_cast<uint2*>(ws + s.off_flags);
+  a.odd = reinterpret_cast<uint2*>(ws + s.off_flags + (s.off_c - s.off_flags) / 2);
+  hipLaunchKernelGGL(prompt_plan, dim3(1), dim3(1024), 0, stream, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  uint8_t* rope = reinterpret_cast<uint8_t*>(ws + s.off_rope);
+  uint8_t* keys = reinterpret_cast<uint8_t*>(ws + s.off_k);
+  uint8_t* values = reinterpret_cast<uint8_t*>(ws + s.off_v);
+  bf16* c = reinterpret_cast<bf16*>(ws + s.off_c);
+  if (s.kv_tiles > 0) {
+    const GatherArgs ga{static_cast<const uint8_t*>(pool), num_pages, joint_page_bytes(d), page_table, max_pages,
+                        d.rank, d.rope_dim, c, rope};
+    if (d.cache == DCKV_JOINT_E4M3)
+      hipLaunchKernelGGL((prompt_gather<true>), dim3(uint32_t(s.kv_tiles)), dim3(256), 0, stream, a, ga);
+    else
+      hipLaunchKernelGGL((prompt_gather<false>), dim3(uint32_t(s.kv_tiles)), dim3(256), 0, stream, a, ga);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const uint32_t blocks = uint32_t(s.kv_tiles / 2) * (d.head_dim == 128 ? 2 : 1) * d.num_heads;
+#define DCKV_GO(D)                                                                                          \
+  hipLaunchKernelGGL((prompt_expand<D>), dim3(blocks), dim3(256), 0, stream, a.counts, c,                    \
+                     static_cast<const bf16*>(W_keys), static_cast<const bf16*>(W_values), d.num_heads,      \
+                     d.rank, a.kv_tiles, keys, values)
+    if (d.head_dim == 128)
+      DCKV_GO(128);
+    else
+      DCKV_GO(64);
+#undef DCKV_GO
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  const float scale = kLog2e * (d.scale != 0.f ? d.scale : 1.f / std::sqrt(float(d.head_dim + d.rope_dim)));
+#define DCKV_GO(D, P)                                                                                        \
+  hipLaunchKernelGGL((prompt_attend<D, P>), dim3(uint32_t(s.q_tiles) * d.num_heads), dim3(256), 0, stream, a, \
+                     keys, rope, values, static_cast<const bf16*>(q), d.num_heads, scale,                     \
+                     static_cast<bf16*>(out));                                                                \
+  return hipGetLastError()
+  if (d.head_dim == 128) {
+    if (d.rope_dim == 64) { DCKV_GO(128, 64); }
+    if (d.rope_dim == 32) { DCKV_GO(128, 32); }
+    DCKV_GO(128, 0);
+  }
+  if (d.rope_dim == 64) { DCKV_GO(64, 64); }
+  if (d.rope_dim == 32) { DCKV_GO(64, 32); }
+  DCKV_GO(64, 0);
+#undef DCKV_GO
 }
+
+}  // namespace dckv

@@ -231,3 +231,74 @@ def test_decode(H, d, r, p, cache, lens, Q, n):
     size = np.abs(want).max()
     check(host(out), want, max(size, 1e-30))
     assert torch.equal(out, joint_decode(j, q, pool, table, seq, top, wk, wv, prefix if n else None, n))
+
+
+def test_prompt_rows_that_do_not_ascend_stay_inside():
+    """row_start is data on the device: whatever it holds, nothing outside is touched."""
+    from paper_2607_24331_amd import joint_prefill
+    g = gen(3)
+    j = joint_of(4, 64, 128, 32, "bf16")
+    pool = filled(j, 4, g)
+    wk, wv = factors(j, g)
+    q = randn(g, 10, 4, 96).to(BF16)
+    table = torch.arange(4, dtype=torch.int32, device="cuda").view(4, 1)
+    seq = torch.tensor([64, 64, 64, 64], dtype=torch.int32, device="cuda")
+    for start in ([0, 10, 0, 10, 0], [-5, 20, 3, 1, 100], [9, 8, 7, 6, 5]):
+        rs = torch.tensor(start, dtype=torch.int32, device="cuda")
+        out = joint_prefill(j, q, rs, pool, table, seq, 64, wk, wv)
+        assert out.shape == (10, 4, 64)
+    torch.cuda.synchronize()
+
+
+# ------------------------------------------------------------------ prompts
+PROMPTS = [
+    # H, d, r, p, cache, cached, added, pad
+    (2, 64, 128, 0, "bf16", [0], [1], 0),
+    (8, 64, 128, 32, "bf16", [0, 0], [77, 130], 5),
+    (5, 64, 256, 64, "e4m3", [100, 0, 64, 7], [0, 129, 63, 1], 0),
+    (4, 128, 512, 64, "bf16", [0], [257], 3),
+    (4, 128, 512, 32, "e4m3", [300, 5], [40, 128], 0),
+    (3, 128, 256, 0, "bf16", [64, 1], [64, 200], 1),
+    (8, 128, 128, 64, "e4m3", [0, 0, 0], [65, 0, 2], 130),
+    (1, 64, 512, 0, "e4m3", [191], [1], 0),
+]
+
+
+def prompt_case(j, cached, added, pad, seed):
+    g = gen(seed)
+    lens = [c + a for c, a in zip(cached, added)]
+    B, top = len(lens), max(lens)
+    width = -(-top // PAGE) + 1
+    pool = filled(j, B * width + 2, g)
+    table = torch.randperm(B * width + 2, generator=g, device="cuda").to(torch.int32)[:B * width].view(B, width).contiguous()
+    start = np.concatenate([[0], np.cumsum(added)])
+    q = randn(g, int(start[-1]) + pad, j.num_heads, j.head_dim + j.rope_dim).to(BF16)
+    wk, wv = factors(j, g)
+    i32 = lambda x: torch.tensor(np.asarray(x), dtype=torch.int32, device="cuda")  # noqa: E731
+    return pool, table, start, q, wk, wv, i32(lens), i32(start), lens, top
+
+
+def oracle_prompt(j, pool, table, start, q, wk, wv, lens, added):
+    out = np.zeros((q.shape[0], j.num_heads, j.head_dim))
+    hp, hq = host(pool), host(q)
+    scale = j._desc.scale or 1.0 / math.sqrt(j.head_dim + j.rope_dim)
+    for b, (T, a) in enumerate(zip(lens, added)):
+        c, k = oj.tokens(hp, table[b].cpu().numpy(), T, j.rank, j.rope_dim, j.cache)
+        lo = int(start[b])
+        out[lo:lo + a] = oj.attend(hq[lo:lo + a], c, k, host(wk), host(wv), [T - a + i + 1 for i in range(a)], scale)
+    return out
+
+
+@pytest.mark.parametrize("H,d,r,p,cache,cached,added,pad", PROMPTS)
+def test_prompts(H, d, r, p, cache, cached, added, pad):
+    from paper_2607_24331_amd import joint_prefill
+    j = joint_of(H, d, r, p, cache)
+    pool, table, start, q, wk, wv, seq, rs, lens, top = prompt_case(j, cached, added, pad, H + d + r)
+    out = torch.full((*q.shape[:2], d), 7.0, dtype=BF16, device="cuda")
+    got = joint_prefill(j, q, rs, pool, table, seq, top, wk, wv, total_context=sum(lens), out=out)
+    assert got is out
+    want = oracle_prompt(j, pool, table, start, q, wk, wv, lens, added)
+    n = sum(added)
+    check(host(out[:n]), want[:n], np.abs(want).max())
+    assert torch.all(out[n:] == 7.0)                              # rows behind the last sequence
+    assert torch.equal(out[:n], joint_prefill(j, q, rs, pool, table, seq, top, wk, wv)[:n])
