@@ -40,11 +40,7 @@ HIPCC_FLAGS = [
 # ordinary VGPRs: with the default AGPR form the register allocator rotated
 # accumulators through AGPR copies inside the k loop, each copy waiting for
 # an in-flight MFMA.
-# The joint decode's 256 accumulators a lane beside its queries fit the
-# registers in that form only (in the other one 300 to 400 are spilled).
-VGPR_FORM = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
-HIPCC_EXTRA = {src: VGPR_FORM for src in ("append.hip", "joint_attend_128.hip", "joint_attend_256.hip",
-                                          "joint_attend_512.hip")}
+HIPCC_EXTRA = {"append.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 HOST_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-D__HIP_PLATFORM_AMD__", "-Wall", "-Wextra"]
 
 

@@ -26,7 +26,7 @@ struct JointShape {
   int32_t row_waves, slices;    // own tokens: waves that take 16 rows each of a work-group's slice; slices
   int32_t units;                // work-groups a slice
   int32_t pre_row_waves, pre_slices, pre_units;   // the same for the prefix, its rows those of all sequences
-  size_t off_start, off_o, off_ml, off_pre_o, off_pre_ml;   // workspace: queries first
+  size_t off_start, off_mean, off_o, off_ml, off_pre_o, off_pre_ml;   // workspace: queries first
   size_t bytes;                 // what this call uses
 };
 

@@ -39,10 +39,8 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef int v2i __attribute__((ext_vector_type(2)));
 typedef short short4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) short4_t* lds_short4;
-typedef __attribute__((address_space(3))) v2i* lds_v2i;
 
 constexpr float kSlack = 6.f;          // weights reach 2^6: the sums stay far from fp32's end
 
@@ -67,6 +65,54 @@ __device__ __forceinline__ u32x4 widen(uint32_t lo, uint32_t hi, float scale) {
 __device__ __forceinline__ uint32_t pair(float a, float b) {
   return uint32_t(__builtin_bit_cast(uint16_t, from_f32<bf16>(a))) |
          uint32_t(__builtin_bit_cast(uint16_t, from_f32<bf16>(b))) << 16;
+}
+
+// Values of four column tiles for the matrix unit, by the transposing LDS loads.  Written
+// out, with a wait of their own: the compiler waits for every load in flight, the next
+// tile's among them, before such a load.  a[j]: this lane's address for tile j, O* bytes on.
+__device__ __forceinline__ uint32_t lds_address(unsigned char* p) {
+  return uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) unsigned char*)(p)));
+}
+template <int O0, int O1, int O2, int O3, int HALF>
+__device__ __forceinline__ void read_tr16(u32x4 (&f)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
+  u32x2 x0 = {}, x1 = {}, x2 = {}, x3 = {}, z0 = {}, z1 = {}, z2 = {}, z3 = {};
+#ifdef __HIP_DEVICE_COMPILE__                      // the host pass knows no vector registers
+  asm volatile(
+      "ds_read_b64_tr_b16 %0, %8 offset:%12\n\tds_read_b64_tr_b16 %1, %8 offset:%16\n\t"
+      "ds_read_b64_tr_b16 %2, %9 offset:%13\n\tds_read_b64_tr_b16 %3, %9 offset:%17\n\t"
+      "ds_read_b64_tr_b16 %4, %10 offset:%14\n\tds_read_b64_tr_b16 %5, %10 offset:%18\n\t"
+      "ds_read_b64_tr_b16 %6, %11 offset:%15\n\tds_read_b64_tr_b16 %7, %11 offset:%19\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(x0), "=&v"(z0), "=&v"(x1), "=&v"(z1), "=&v"(x2), "=&v"(z2), "=&v"(x3), "=&v"(z3)
+      : "v"(a0), "v"(a1), "v"(a2), "v"(a3), "i"(O0), "i"(O1), "i"(O2), "i"(O3), "i"(O0 + HALF), "i"(O1 + HALF),
+        "i"(O2 + HALF), "i"(O3 + HALF)
+      : "memory");
+#endif
+  f[0] = u32x4{x0[0], x0[1], z0[0], z0[1]};
+  f[1] = u32x4{x1[0], x1[1], z1[0], z1[1]};
+  f[2] = u32x4{x2[0], x2[1], z2[0], z2[1]};
+  f[3] = u32x4{x3[0], x3[1], z3[0], z3[1]};
+}
+template <int O0, int O1, int O2, int O3>
+__device__ __forceinline__ void read_tr8(u32x2 (&f)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
+#ifdef __HIP_DEVICE_COMPILE__
+  asm volatile(
+      "ds_read_b64_tr_b8 %0, %4 offset:%8\n\tds_read_b64_tr_b8 %1, %5 offset:%9\n\t"
+      "ds_read_b64_tr_b8 %2, %6 offset:%10\n\tds_read_b64_tr_b8 %3, %7 offset:%11\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(f[0]), "=&v"(f[1]), "=&v"(f[2]), "=&v"(f[3])
+      : "v"(a0), "v"(a1), "v"(a2), "v"(a3), "i"(O0), "i"(O1), "i"(O2), "i"(O3)
+      : "memory");
+#endif
+}
+
+// A loop whose index is a constant.
+template <int N, typename F, int I = 0>
+__device__ __forceinline__ void unrolled(F&& f) {
+  if constexpr (I < N) {
+    f(std::integral_constant<int, I>{});
+    unrolled<N, F, I + 1>(static_cast<F&&>(f));
+  }
 }
 
 // Place of pieces 4 i + lq from that of lq (four pieces keep their places among
@@ -379,24 +425,27 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
           }
         }
         // ---- output: column 16 i + lr of the A operand, tokens 4 lq + 0 .. 3 and 16 more
-        int va = value_at;
-        asm volatile("" : "+v"(va));
+        const uint32_t base = lds_address(buf);
         if constexpr (C8) {
+          unrolled<CT / 4>([&](auto k) {
+            constexpr int I = 4 * decltype(k)::value, M = G - 1;
+            u32x2 x[4];
+            read_tr8<I / G * (G * 16), (I + 1) / G * (G * 16), (I + 2) / G * (G * 16), (I + 3) / G * (G * 16)>(
+                x, base + (value_at ^ ((I & M) * 16)), base + (value_at ^ (((I + 1) & M) * 16)),
+                base + (value_at ^ (((I + 2) & M) * 16)), base + (value_at ^ (((I + 3) & M) * 16)));
 #pragma unroll
-          for (int i = 0; i < CT; ++i) {
-            const v2i x = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
-                (lds_v2i)(buf + (va ^ ((i & (G - 1)) * 16)) + i / G * (G * 16)));
-            acc[i] = mfma(widen(uint32_t(x[0]), uint32_t(x[1]), 1.f), p, acc[i]);
-          }
+            for (int j = 0; j < 4; ++j) acc[I + j] = mfma(widen(x[j][0], x[j][1], 1.f), p, acc[I + j]);
+          });
         } else {
+          unrolled<CT / 4>([&](auto k) {
+            constexpr int I = 4 * decltype(k)::value, H = G / 2, M = H - 1;
+            u32x4 x[4];
+            read_tr16<I / H * (G * 16), (I + 1) / H * (G * 16), (I + 2) / H * (G * 16), (I + 3) / H * (G * 16), 16 * ROWB>(
+                x, base + (value_at ^ ((I & M) * 32)), base + (value_at ^ (((I + 1) & M) * 32)),
+                base + (value_at ^ (((I + 2) & M) * 32)), base + (value_at ^ (((I + 3) & M) * 32)));
 #pragma unroll
-          for (int i = 0; i < CT; ++i) {
-            unsigned char* at = buf + (va ^ ((i & (G / 2 - 1)) * 32)) + i / (G / 2) * (G * 16);
-            const short4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4)(at));
-            const short4_t z = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4)(at + 16 * ROWB));
-            const auto xz = __builtin_shufflevector(x, z, 0, 1, 2, 3, 4, 5, 6, 7);
-            acc[i] = mfma(__builtin_bit_cast(u32x4, xz), p, acc[i]);
-          }
+            for (int j = 0; j < 4; ++j) acc[I + j] = mfma(x[j], p, acc[I + j]);
+          });
         }
       }
       if constexpr (NBUF == 1) {

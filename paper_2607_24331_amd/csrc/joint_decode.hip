@@ -8,10 +8,10 @@
 //               the factor's rows; products on MFMA 32x32x16, rounded to bf16 (2^-9 of a
 //               coordinate, independent ones in a score's sum over r).  One more wave forms
 //               the sequences' first tiles.  Bound by latency and, once, by the factor's bytes.
-// joint_finish  a work-group 1 or 4 rows of a head: its shares' sums in fp32, 16 bytes a
-//               lane, the whole work-group on one row's shares; then the product with the
-//               head's factor rows, eight or sixteen lanes a value column.  Bound by the
-//               shares' bytes and the factors' reads from the caches.
+// joint_merge   a work-group a row: its shares' sums in fp32, 16 bytes a lane.  Bound by
+//               the shares' bytes.
+// joint_values  the product with the heads' factor rows on MFMA, 32 rows by 32 coordinates a
+//               work-group, its waves a quarter of the latent coordinates each.
 #include <algorithm>
 #include <cmath>
 
@@ -136,127 +136,169 @@ struct FinishArgs {
   int pre_row_rows, pre_slices, pre_units, pre_groups, prefix_len;
 };
 
-// RB rows (sequence, query) of one head; rows beyond `n` are skipped.
-template <int R, int D, int RB>
-__global__ __launch_bounds__(1024) void joint_finish(FinishArgs a, const bf16* __restrict__ W_values, int n,
-                                                     bf16* __restrict__ out) {
-  constexpr int C = R / 4, GR = 1024 / C;              // lanes a share, shares at a time
-  __shared__ __align__(16) floatx4 red[GR][C];
-  __shared__ __align__(16) float mean[RB][R];
+// A row's shares joined: C = R/4 lanes a share, GR shares at a time.  mean fp32 [row][R].
+template <int R, int GR>
+__global__ __launch_bounds__(R / 4 * GR) void joint_merge(FinishArgs a, float* __restrict__ mean) {
+  constexpr int C = R / 4, N = C * GR, NW = N / 64 > 0 ? N / 64 : 1;
+  __shared__ __align__(16) floatx4 red[GR > 1 ? GR : 1][C];
   __shared__ float wo[2 * kJointMaxUnits];
   __shared__ int64_t where[2 * kJointMaxUnits];        // element offset of a share; prefix ones complemented
-  __shared__ float wave_m[16], wave_l[16];
-  const int head = blockIdx.x % a.heads, r0 = blockIdx.x / a.heads * RB;
+  __shared__ float wave_m[NW], wave_l[NW];
+  const int64_t id = blockIdx.x;                       // (sequence, query, head)
+  const int head = int(id % a.heads), row = int(id / a.heads);
   const int tid = threadIdx.x, g = tid / C, c = tid % C;
-#pragma unroll 1
-  for (int k = 0; k < RB; ++k) {
-    const int row = r0 + k;
-    if (row >= n) break;
-    const int b = row / a.queries, i = row % a.queries;
-    // shares: those of the sequence's units, then the prefix's
-    const int64_t s0 = a.start[b], s1 = a.start[b + 1];
-    const int64_t per = joint_tiles_a_unit(a.start[a.batch], a.units, a.groups);
-    const int64_t u0 = s0 / per;
-    const int own = s1 > s0 ? int((s1 - 1) / per - u0) + 1 : 0;
-    int pre = 0;
-    if (a.prefix_len > 0) {
-      const int64_t tiles = (a.prefix_len + kJointTile - 1) / kJointTile;
-      const int64_t pp = joint_tiles_a_unit(tiles, a.pre_units, a.pre_groups);
-      pre = int((tiles + pp - 1) / pp);
+  const int b = row / a.queries, i = row % a.queries;
+  // shares: those of the sequence's units, then the prefix's
+  const int64_t s0 = a.start[b], s1 = a.start[b + 1];
+  const int64_t per = joint_tiles_a_unit(a.start[a.batch], a.units, a.groups);
+  const int64_t u0 = s0 / per;
+  const int own = s1 > s0 ? int((s1 - 1) / per - u0) + 1 : 0;
+  int pre = 0;
+  if (a.prefix_len > 0) {
+    const int64_t tiles = (a.prefix_len + kJointTile - 1) / kJointTile;
+    const int64_t pp = joint_tiles_a_unit(tiles, a.pre_units, a.pre_groups);
+    pre = int((tiles + pp - 1) / pp);
+  }
+  const int ns = own + pre;                            // at most 2 kJointMaxUnits
+  const int rr = i * a.heads + head;
+  const auto share = [&](int s, int64_t& at) {
+    if (s < own) {
+      at = ((u0 + s + b) * a.slices + rr / a.row_rows) * a.row_rows + rr % a.row_rows;
+      return a.part_ml[at];
     }
-    const int ns = own + pre;                          // at most 2 kJointMaxUnits: a share a thread
-    float4 ml = make_float4(-INFINITY, 0.f, -INFINITY, 0.f);
-    if (tid < ns) {
+    at = (int64_t(s - own) * a.pre_slices + id / a.pre_row_rows) * a.pre_row_rows + id % a.pre_row_rows;
+    const float4 ml = a.pre_ml[at];
+    at = ~(at * R);
+    return ml;
+  };
+  // a lane's shares wait in registers for the greatest m: at most 2 kJointMaxUnits / N
+  constexpr int PER = (2 * kJointMaxUnits + N - 1) / N;
+  float m_of[PER], l_of[PER], u_of[PER];
+  float M = -INFINITY;
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    m_of[k] = u_of[k] = -INFINITY;
+    l_of[k] = 0.f;
+    const int s = k * N + tid;
+    if (k * N >= ns) continue;
+    if (s < ns) {
       int64_t at;
-      if (tid < own) {
-        const int rr = i * a.heads + head;
-        at = ((u0 + tid + b) * a.slices + rr / a.row_rows) * a.row_rows + rr % a.row_rows;
-        ml = a.part_ml[at];
-        where[tid] = at * R;
-      } else {
-        const int64_t rr = int64_t(row) * a.heads + head;
-        at = (int64_t(tid - own) * a.pre_slices + rr / a.pre_row_rows) * a.pre_row_rows + rr % a.pre_row_rows;
-        ml = a.pre_ml[at];
-        where[tid] = ~(at * R);
-      }
+      const float4 ml = share(s, at);
+      m_of[k] = ml.x;
+      l_of[k] = ml.y;
+      u_of[k] = ml.z;
+      where[s] = at < 0 ? at : at * R;
+      M = fmaxf(M, ml.x);
     }
-    float M = ml.x;
+  }
 #pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
-    if ((tid & 63) == 0) wave_m[tid >> 6] = M;
-    __syncthreads();
+  for (int o = 32; o >= 1; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
+  if ((tid & 63) == 0) wave_m[tid >> 6] = M;
+  __syncthreads();
 #pragma unroll
-    for (int o = 0; o < 16; ++o) M = fmaxf(M, wave_m[o]);
-    // a share that saw nothing of the row has l = 0 and m = -inf
-    const bool some = ml.y != 0.f;
-    float l = some ? ml.y * __builtin_amdgcn_exp2f(ml.x - M) : 0.f;
-    if (tid < ns) wo[tid] = some ? __builtin_amdgcn_exp2f(ml.z - M) : 0.f;
+  for (int o = 0; o < NW; ++o) M = fmaxf(M, wave_m[o]);
+  float l = 0.f;
 #pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) l += __shfl_xor(l, o);
-    if ((tid & 63) == 0) wave_l[tid >> 6] = l;
-    __syncthreads();
-    floatx4 sum = {0.f, 0.f, 0.f, 0.f};
-    constexpr int U = 8;
-    for (int s = g; s < ns; s += U * GR) {
-      floatx4 x[U];
+  for (int k = 0; k < PER; ++k) {
+    const int s = k * N + tid;
+    const bool some = l_of[k] != 0.f;                  // a share that saw nothing has l = 0 and m = -inf
+    l += some ? l_of[k] * __builtin_amdgcn_exp2f(m_of[k] - M) : 0.f;
+    if (s < ns) wo[s] = some ? __builtin_amdgcn_exp2f(u_of[k] - M) : 0.f;
+  }
 #pragma unroll
-      for (int j = 0; j < U; ++j) {
-        if (s + j * GR >= ns) continue;
-        const int64_t at = where[s + j * GR];
-        x[j] = *reinterpret_cast<const floatx4*>((at < 0 ? a.pre_o + ~at : a.part_o + at) + 4 * c);
-      }
+  for (int o = 32; o >= 1; o >>= 1) l += __shfl_xor(l, o);
+  if ((tid & 63) == 0) wave_l[tid >> 6] = l;
+  __syncthreads();
+  floatx4 sum = {0.f, 0.f, 0.f, 0.f};
+  constexpr int U = 8;
+  for (int s = g; s < ns; s += U * GR) {
+    floatx4 x[U];
 #pragma unroll
-      for (int j = 0; j < U; ++j) {
-        if (s + j * GR >= ns) continue;
-        const float y = wo[s + j * GR];
-        if (y == 0.f) continue;                        // nothing seen: the sums may be infinite
-#pragma unroll
-        for (int v = 0; v < 4; ++v) sum[v] = fmaf(y, x[j][v], sum[v]);
-      }
+    for (int j = 0; j < U; ++j) {
+      if (s + j * GR >= ns) continue;
+      const int64_t at = where[s + j * GR];
+      x[j] = *reinterpret_cast<const floatx4*>((at < 0 ? a.pre_o + ~at : a.part_o + at) + 4 * c);
     }
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      if (s + j * GR >= ns) continue;
+      const float y = wo[s + j * GR];
+      if (y == 0.f) continue;                          // nothing seen: the sums may be infinite
+#pragma unroll
+      for (int v = 0; v < 4; ++v) sum[v] = fmaf(y, x[j][v], sum[v]);
+    }
+  }
+  if constexpr (GR > 1) {
     red[g][c] = sum;
     __syncthreads();
-    if (g == 0) {
-      float L = 0.f;
+  }
+  if (g == 0) {
+    float L = 0.f;
 #pragma unroll
-      for (int o = 0; o < 16; ++o) L += wave_l[o];
+    for (int o = 0; o < NW; ++o) L += wave_l[o];
 #pragma unroll
-      for (int o = 1; o < GR; ++o) sum += red[o][c];
+    for (int o = 1; o < GR; ++o) sum += red[o][c];
 #pragma unroll
-      for (int v = 0; v < 4; ++v) mean[k][4 * c + v] = L == 0.f ? 0.f : sum[v] / L;
+    for (int v = 0; v < 4; ++v) sum[v] = L == 0.f ? 0.f : sum[v] / L;
+    *reinterpret_cast<floatx4*>(mean + id * R + 4 * c) = sum;
+  }
+}
+
+// 32 rows (sequence, query) of a head by 32 value coordinates: four waves take a quarter
+// of the latent coordinates each, every operand straight from memory in one go.  The means
+// are fp32, taken as bf16 hi + lo.
+template <int R, int D>
+__global__ __launch_bounds__(256) void joint_values(const float* __restrict__ mean, const bf16* __restrict__ W_values,
+                                                    int n, int heads, bf16* __restrict__ out) {
+  constexpr int STEPS = R / 64;                        // of 16 coordinates a wave
+  __shared__ float red[4][16][64];
+  const int cols = D / 32;
+  const int head = blockIdx.x % heads, ct = blockIdx.x / heads % cols, r0 = blockIdx.x / heads / cols * 32;
+  const int tid = threadIdx.x, lane = tid & 63, lr = lane & 31, h = lane >> 5;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int k0 = w * (R / 4) + 8 * h;
+  const bf16* wrow = W_values + (int64_t(head) * D + 32 * ct + lr) * R + k0;
+  const float* mrow = mean + (int64_t(min(r0 + lr, n - 1)) * heads + head) * R + k0;
+  u32x4 x[STEPS];
+  floatx4 y[STEPS][2];
+#pragma unroll
+  for (int i = 0; i < STEPS; ++i) {
+    x[i] = *reinterpret_cast<const u32x4*>(wrow + 16 * i);
+    y[i][0] = *reinterpret_cast<const floatx4*>(mrow + 16 * i);
+    y[i][1] = *reinterpret_cast<const floatx4*>(mrow + 16 * i + 4);
+  }
+  f32x16 acc;
+#pragma unroll
+  for (int v = 0; v < 16; ++v) acc[v] = 0.f;
+#pragma unroll
+  for (int i = 0; i < STEPS; ++i) {
+    u32x4 hi, lo;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float p = y[i][j >> 1][2 * (j & 1)], q = y[i][j >> 1][2 * (j & 1) + 1];
+      hi[j] = joint::pair(p, q);
+      // a mean that is not finite has no rest
+      const float pr = p - __uint_as_float(hi[j] << 16), qr = q - __uint_as_float(hi[j] & 0xFFFF0000u);
+      lo[j] = joint::pair(pr == pr ? pr : 0.f, qr == qr ? qr : 0.f);
     }
-    __syncthreads();
-  }
-  // ---- values: LD lanes a column, 8 latent coordinates at a time
-  constexpr int LD = 1024 / D, PC = R / 8;
-  const int d = tid / LD, part = tid % LD;
-  const bf16* w = W_values + (int64_t(head) * D + d) * R;
-  float o[RB];
-#pragma unroll
-  for (int k = 0; k < RB; ++k) o[k] = 0.f;
-#pragma unroll
-  for (int j = 0; j < PC / LD; ++j) {
-    const int col = 8 * (j * LD + part);
-    const u32x4 x = *reinterpret_cast<const u32x4*>(w + col);
-#pragma unroll
-    for (int k = 0; k < RB; ++k) {
-      const floatx4 lo = *reinterpret_cast<const floatx4*>(&mean[k][col]);
-      const floatx4 hi = *reinterpret_cast<const floatx4*>(&mean[k][col + 4]);
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        o[k] = fmaf(__uint_as_float(x[e] << 16), lo[2 * e], o[k]);
-        o[k] = fmaf(__uint_as_float(x[e] & 0xFFFF0000u), lo[2 * e + 1], o[k]);
-        o[k] = fmaf(__uint_as_float(x[2 + e] << 16), hi[2 * e], o[k]);
-        o[k] = fmaf(__uint_as_float(x[2 + e] & 0xFFFF0000u), hi[2 * e + 1], o[k]);
-      }
-    }
+    acc = mfma(x[i], hi, acc);
+    acc = mfma(x[i], lo, acc);
   }
 #pragma unroll
-  for (int k = 0; k < RB; ++k) {
+  for (int v = 0; v < 16; ++v) red[w][v][lane] = acc[v];
+  __syncthreads();
+  // lane: row lr, coordinates 8 k + 4 h + v; wave w finishes k = w
+  const float* e = &red[0][0][0] + lane;
+  floatx4 o;
 #pragma unroll
-    for (int e = LD >> 1; e >= 1; e >>= 1) o[k] += __shfl_xor(o[k], e);
-    if (part == 0 && r0 + k < n) out[(int64_t(r0 + k) * a.heads + head) * D + d] = from_f32<bf16>(o[k]);
+  for (int v = 0; v < 4; ++v) {
+    o[v] = 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) o[v] += e[(k * 16 + 4 * w + v) * 64];
   }
+  if (r0 + lr < n)
+    *reinterpret_cast<joint::u32x2*>(out + (int64_t(r0 + lr) * heads + head) * D + 32 * ct + 8 * w + 4 * h) =
+        joint::u32x2{joint::pair(o[0], o[1]), joint::pair(o[2], o[3])};
 }
 
 size_t align_up(size_t v) { return (v + 255) / 256 * 256; }
@@ -279,15 +321,17 @@ int units_of(int rank, int64_t slices, int64_t tiles, int groups) {
 }
 
 template <int R, int D>
-hipError_t finish(const FinishArgs& a, const void* W_values, int n, void* out, hipStream_t stream) {
-  // a work-group of four rows reads the factor for four; few rows are spread instead
-  if (int64_t(n) * a.heads >= 2048) {
-    hipLaunchKernelGGL((joint_finish<R, D, 4>), dim3(uint32_t((n + 3) / 4) * a.heads), dim3(1024), 0, stream, a,
-                       static_cast<const bf16*>(W_values), n, static_cast<bf16*>(out));
-  } else {
-    hipLaunchKernelGGL((joint_finish<R, D, 1>), dim3(uint32_t(n) * a.heads), dim3(1024), 0, stream, a,
-                       static_cast<const bf16*>(W_values), n, static_cast<bf16*>(out));
-  }
+hipError_t finish(const FinishArgs& a, const void* W_values, int n, float* mean, void* out, hipStream_t stream) {
+  // few rows have many shares each and get a work-group of 1024
+  const uint32_t rows = uint32_t(n) * a.heads;
+  if (rows < 1024)
+    hipLaunchKernelGGL((joint_merge<R, 4096 / R>), dim3(rows), dim3(1024), 0, stream, a, mean);
+  else
+    hipLaunchKernelGGL((joint_merge<R, 1024 / R>), dim3(rows), dim3(256), 0, stream, a, mean);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((joint_values<R, D>), dim3(uint32_t((n + 31) / 32) * (D / 32) * a.heads), dim3(256), 0, stream,
+                     mean, static_cast<const bf16*>(W_values), n, a.heads, static_cast<bf16*>(out));
   return hipGetLastError();
 }
 
@@ -326,7 +370,8 @@ JointShape joint_shape(const dckv_joint_desc& d, int32_t queries, int32_t batch,
   s.pre_units = prefix_len > 0 ? units_of(d.rank, s.pre_slices, tiles_of(prefix_len), groups_of(s.pre_row_waves)) : 0;
   const size_t width = size_t(d.rank + d.rope_dim);
   s.off_start = align_up(size_t(all) * width * 2);
-  s.off_o = s.off_start + align_up(size_t(batch + 1) * 8);
+  s.off_mean = s.off_start + align_up(size_t(batch + 1) * 8);
+  s.off_o = s.off_mean + align_up(size_t(all) * d.rank * 4);
   const size_t own = size_t(s.units + batch) * s.slices * 16 * s.row_waves;
   s.off_ml = s.off_o + align_up(own * d.rank * 4);
   s.off_pre_o = s.off_ml + align_up(own * 16);
@@ -404,7 +449,7 @@ hipError_t launch_joint_decode(const JointShape& s, const void* q, const void* p
                      reinterpret_cast<const float4*>(ws + s.off_pre_ml), s.batch, s.queries, d.num_heads,
                      16 * s.row_waves, s.slices, s.units, groups_of(s.row_waves), 16 * s.pre_row_waves,
                      s.pre_slices, s.pre_units, groups_of(s.pre_row_waves), s.prefix_len};
-#define DCKV_FINISH(R, D) return finish<R, D>(f, W_values, n, out, stream)
+#define DCKV_FINISH(R, D) return finish<R, D>(f, W_values, n, reinterpret_cast<float*>(ws + s.off_mean), out, stream)
   if (d.rank == 128) {
     if (d.head_dim == 64) DCKV_FINISH(128, 64);
     DCKV_FINISH(128, 128);

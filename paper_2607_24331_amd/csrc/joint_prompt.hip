@@ -6,7 +6,7 @@
 // Four launches:
 //   prompt_plan    one work-group: the tiles of 64 tokens of the sequences that have rows,
 //                  and the tiles of 128 rows, those with the most tokens first.
-//   prompt_gather  a work-group a token tile: latents in bf16 side by side, position keys
+//   prompt_gather  a work-group 16 tokens: latents in bf16 side by side, position keys
 //                  as the attention's LDS wants them, and which tokens are there and finite.
 //   prompt_expand  every head's keys and values, a 128 x 128 product tile a work-group on
 //                  MFMA 16x16x32; the latents' and factors' rows come by the loads' LDS path.
@@ -51,8 +51,8 @@ struct PromptArgs {
   int32_t* counts;                        // row tiles, token tiles
   RowTile* rows;
   int2* toks;                             // sequence, tile
-  uint2* there;                           // per token tile: tokens that are there
-  uint2* odd;                             // and those that are not finite
+  uint16_t* there;                        // a bit a token of a tile: it is there
+  uint16_t* odd;                          // and is not finite
 };
 
 __device__ __forceinline__ int wave_scan(int x, int lane) {
@@ -73,21 +73,33 @@ __device__ __forceinline__ int64_t wave_scan(int64_t x, int lane) {
   return x;
 }
 
+// The first of n ascending ends that is above x.
+__device__ __forceinline__ int find_end(const int* ends, int n, int x) {
+  int lo = 0;
+  while (n > 1) {
+    const int half = n >> 1;
+    if (ends[lo + half - 1] <= x) lo += half;
+    n -= half;
+  }
+  return lo;
+}
+
 __global__ __launch_bounds__(1024) void prompt_plan(PromptArgs a) {
-  constexpr int kBins = 128;
+  constexpr int kBins = 128, N = 1024;
   __shared__ int wave_rows[16], wave_toks[16];
   __shared__ int64_t wave_len[16];
   __shared__ int bins[kBins];
+  __shared__ int row_end[N], tok_end[N], lo_of[N], n_of[N], len_of[N], kv_of[N];
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  for (int i = tid; i < kBins; i += 1024) bins[i] = 0;
+  for (int i = tid; i < kBins; i += N) bins[i] = 0;
   const int most = (a.max_context + kTok - 1) / kTok + 1;
-  // two walks over the sequences: the first counts row tiles by their tokens, the second
-  // writes them, most tokens first (which place a tile takes among those of a bin does
-  // not change what it computes)
+  // two walks over the sequences, 1024 at a time: the first counts row tiles by their
+  // tokens, the second writes them, most tokens first (which place a tile takes among
+  // those of a bin does not change what it computes)
   for (int walk = 0; walk < 2; ++walk) {
     int toks = 0;                         // token tiles of the sequences before
     int64_t len = 0;                      // their tokens
-    for (int b0 = 0; b0 < a.batch; b0 += 1024) {
+    for (int b0 = 0; b0 < a.batch; b0 += N) {
       const int b = b0 + tid;
       int lo = 0, n = 0, T = 0;
       if (b < a.batch) {
@@ -95,43 +107,56 @@ __global__ __launch_bounds__(1024) void prompt_plan(PromptArgs a) {
         n = min(max(a.row_start[b + 1], lo), a.n_rows) - lo;
         T = n > 0 ? min(max(a.seq_lens[b], 0), a.max_context) : 0;
       }
-      const int own = (T + kTok - 1) / kTok;
       const int64_t len_to = wave_scan(int64_t(T), lane);
       if (lane == 63) wave_len[w] = len_to;
       __syncthreads();
       int64_t before = len;
       for (int i = 0; i < w; ++i) before += wave_len[i];
-      const bool fits = before + len_to <= a.total_context;
       for (int i = 0; i < 16; ++i) len += wave_len[i];
-      const int toks_to = wave_scan(fits ? own : 0, lane);
-      if (lane == 63) wave_toks[w] = toks_to;
-      __syncthreads();
-      int kv = toks + toks_to - (fits ? own : 0);
-      for (int i = 0; i < w; ++i) kv += wave_toks[i];
-      for (int i = 0; i < 16; ++i) toks += wave_toks[i];
-      const bool room = fits && kv + own <= a.kv_tiles;         // always, where row_start ascends
-      if (walk == 1 && fits)
-        for (int i = 0; i < own; ++i)
-          if (kv + i < a.kv_tiles) a.toks[kv + i] = make_int2(b, i);
-      for (int i = 0; i * kRows < n; ++i) {
-        const int last = T - n + min((i + 1) * kRows, n);       // tokens that the tile's last row sees
-        const int bin = kBins - 1 - int(int64_t((max(last, 0) + kTok - 1) / kTok) * kBins / most);
-        if (walk == 0) {
-          atomicAdd(&bins[bin], 1);
-        } else {
-          const int at = atomicAdd(&bins[bin], 1);
-          if (at < a.q_tiles)
-            a.rows[at] = RowTile{lo + i * kRows, min(kRows, n - i * kRows), room ? kv : -1, T - n + i * kRows};
-        }
+      const bool fits = before + len_to <= a.total_context;
+      const int own = fits ? (T + kTok - 1) / kTok : 0;
+      const int toks_to = wave_scan(own, lane), rows_to = wave_scan((n + kRows - 1) / kRows, lane);
+      if (lane == 63) {
+        wave_toks[w] = toks_to;
+        wave_rows[w] = rows_to;
       }
+      __syncthreads();
+      int tok_at = toks_to, row_at = rows_to, all_toks = 0, all_rows = 0;
+      for (int i = 0; i < 16; ++i) {
+        if (i < w) tok_at += wave_toks[i], row_at += wave_rows[i];
+        all_toks += wave_toks[i];
+        all_rows += wave_rows[i];
+      }
+      row_end[tid] = row_at;
+      tok_end[tid] = tok_at;
+      lo_of[tid] = lo;
+      n_of[tid] = n;
+      len_of[tid] = T;
+      // its token tiles have room always, where row_start ascends
+      kv_of[tid] = fits && toks + tok_at <= a.kv_tiles ? toks + tok_at - own : -1;
+      __syncthreads();
+      for (int x = tid; x < all_rows; x += N) {
+        const int s = find_end(row_end, N, x);
+        const int n_s = n_of[s], T_s = len_of[s], i = x - (row_end[s] - (n_s + kRows - 1) / kRows);
+        const int last = T_s - n_s + min((i + 1) * kRows, n_s);       // tokens that the tile's last row sees
+        const int bin = kBins - 1 - int(int64_t((max(last, 0) + kTok - 1) / kTok) * kBins / most);
+        const int at = atomicAdd(&bins[bin], 1);
+        if (walk == 1 && at < a.q_tiles)
+          a.rows[at] = RowTile{lo_of[s] + i * kRows, min(kRows, n_s - i * kRows), kv_of[s], T_s - n_s + i * kRows};
+      }
+      if (walk == 1)
+        for (int x = tid; x < all_toks; x += N) {
+          const int s = find_end(tok_end, N, x);
+          if (toks + x < a.kv_tiles)
+            a.toks[toks + x] = make_int2(b0 + s, x - (tok_end[s] - (len_of[s] + kTok - 1) / kTok));
+        }
+      toks += all_toks;
       __syncthreads();
     }
     if (walk == 0) {
-      // bins to their first places
-      int x = 0;
-      if (w == 0) {
+      if (w == 0) {                       // bins to their first places
         const int p = bins[2 * lane], q = bins[2 * lane + 1];
-        x = wave_scan(p + q, lane);
+        const int x = wave_scan(p + q, lane);
         bins[2 * lane] = x - p - q;
         bins[2 * lane + 1] = x - q;
         if (lane == 63) a.counts[0] = min(x, a.q_tiles);
@@ -158,61 +183,69 @@ struct GatherArgs {
   uint8_t* rope;                          // [tiles][64 rows of p], in LDS places
 };
 
+// 16 tokens a work-group.
 template <bool C8>
 __global__ __launch_bounds__(256) void prompt_gather(PromptArgs a, GatherArgs s) {
-  __shared__ uint32_t odd[2];
-  const int tile = blockIdx.x, tid = threadIdx.x;
+  __shared__ uint32_t odd;
+  const int tile = blockIdx.x >> 2, t0 = (blockIdx.x & 3) * 16, tid = threadIdx.x;
   if (tile >= a.counts[1]) return;
   const int2 at = a.toks[tile];
   const int T = min(max(a.seq_lens[at.x], 0), a.max_context) - at.y * kTok;
   int page = s.page_table[int64_t(at.x) * s.max_pages + at.y];
   if (page >= s.num_pages) page = -1;
-  const int have = page < 0 ? 0 : min(T, kTok);
-  if (tid < 2) odd[tid] = 0;
+  const int have = page < 0 ? 0 : min(T, kTok) - t0;   // of the 16
+  if (tid == 0) odd = 0;
   __syncthreads();
   const int w = s.r + s.p, per = C8 ? 16 : 8, pieces = w / per, g = joint_gcd16(pieces);
   const int rg = joint_gcd16(s.p / 8);
   const uint8_t* src = s.pool + int64_t(max(page, 0)) * s.page_bytes;
-  for (int i = tid; i < kTok * pieces; i += 256) {
-    const int t = i / pieces, piece = (i % pieces) ^ joint_swap(g, t);   // reads a page in order
-    const int col = piece * per;
+  const uint8_t* rows = src + t0 * pieces * 16;
+  constexpr int U = C8 ? 3 : 5;                        // 16 rows of 36 or 72 pieces, at most
+  u32x4 y[U];
+#pragma unroll
+  for (int k = 0; k < U; ++k) {
+    const int i = k * 256 + tid;
+    y[k] = u32x4{0u, 0u, 0u, 0u};
+    if (i < 16 * pieces && i / pieces < have) y[k] = *reinterpret_cast<const u32x4*>(rows + i * 16);
+  }
+#pragma unroll
+  for (int k = 0; k < U; ++k) {
+    const int i = k * 256 + tid;
+    if (i >= 16 * pieces) break;
+    const int t = t0 + i / pieces, col = ((i % pieces) ^ joint_swap(g, t)) * per;
     u32x4 x[C8 ? 2 : 1];
     bool bad = false;
-    if (t < have) {
-      const u32x4 y = *reinterpret_cast<const u32x4*>(src + i * 16);
-      if constexpr (C8) {
-        const float f = __uint_as_float(uint32_t(src[kTok * (w + (col < s.r ? 0 : 1)) + t]) << 23);
+    if constexpr (C8) {
+      const float f = __uint_as_float(uint32_t(src[kTok * (w + (col < s.r ? 0 : 1)) + t]) << 23);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          bad |= (((y[k] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) != 0;
-          x[k >> 1][2 * (k & 1)] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(y[k], f, false));
-          x[k >> 1][2 * (k & 1) + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(y[k], f, true));
-        }
-      } else {
-        x[0] = y;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) bad |= (((y[k] & 0x7F807F80u) + 0x00800080u) & 0x80008000u) != 0;
+      for (int e = 0; e < 4; ++e) {
+        bad |= (((y[k][e] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) != 0;
+        x[e >> 1][2 * (e & 1)] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(y[k][e], f, false));
+        x[e >> 1][2 * (e & 1) + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(y[k][e], f, true));
       }
+    } else {
+      x[0] = y[k];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) bad |= (((y[k][e] & 0x7F807F80u) + 0x00800080u) & 0x80008000u) != 0;
     }
-    if (bad) atomicOr(&odd[t >> 5], 1u << (t & 31));
-    if (bad || t >= have)
+    if (bad) atomicOr(&odd, 1u << (t & 15));
+    if (bad || t - t0 >= have)
 #pragma unroll
-      for (int k = 0; k < (C8 ? 2 : 1); ++k) x[k] = u32x4{0u, 0u, 0u, 0u};
+      for (int e = 0; e < (C8 ? 2 : 1); ++e) x[e] = u32x4{0u, 0u, 0u, 0u};
 #pragma unroll
-    for (int k = 0; k < (C8 ? 2 : 1); ++k) {
-      const int j = col + 8 * k;
+    for (int e = 0; e < (C8 ? 2 : 1); ++e) {
+      const int j = col + 8 * e;
       if (j < s.r)
-        *reinterpret_cast<u32x4*>(s.c + (int64_t(tile) * kTok + t) * s.r + j) = x[k];
+        *reinterpret_cast<u32x4*>(s.c + (int64_t(tile) * kTok + t) * s.r + j) = x[e];
       else
         *reinterpret_cast<u32x4*>(s.rope + (int64_t(tile) * kTok + t) * s.p * 2 +
-                                  (((j - s.r) / 8) ^ joint_swap(rg, t)) * 16) = x[k];
+                                  (((j - s.r) / 8) ^ joint_swap(rg, t)) * 16) = x[e];
     }
   }
   __syncthreads();
   if (tid == 0) {
-    a.odd[tile] = make_uint2(odd[0], odd[1]);
-    a.there[tile] = make_uint2(have >= 32 ? ~0u : (1u << have) - 1u,
-                               have >= 64 ? ~0u : have > 32 ? (1u << (have - 32)) - 1u : 0u);
+    a.odd[tile * 4 + t0 / 16] = uint16_t(odd);
+    a.there[tile * 4 + t0 / 16] = uint16_t(have >= 16 ? 0xFFFFu : have > 0 ? (1u << have) - 1u : 0u);
   }
 }
 
@@ -388,7 +421,7 @@ __global__ __launch_bounds__(256, 2) void prompt_attend(PromptArgs a, const uint
     __syncthreads();                                   // the tile is whole, the one before is used up
     if (t + 1 < tiles) issue(t + 1);
     unsigned char* buf = smem + (t & 1) * TILE;
-    const uint2 there = a.there[rt.kv + t], odd = a.odd[rt.kv + t];
+    const uint2 there = reinterpret_cast<const uint2*>(a.there)[rt.kv + t], odd = reinterpret_cast<const uint2*>(a.odd)[rt.kv + t];
     const int pos = t * kTok;
     // rows of the wave that do not see the whole tile, or a tile with holes
     const bool edge = pos + kTok > rt.first + w * 32 + 1 || (there.x & there.y) != ~0u || (odd.x | odd.y) != 0;
@@ -514,8 +547,8 @@ hipError_t launch_joint_prefill(const JointPrompt& s, const void* q, const int32
   a.counts = reinterpret_cast<int32_t*>(ws);
   a.rows = reinterpret_cast<RowTile*>(ws + s.off_qtile);
   a.toks = reinterpret_cast<int2*>(ws + s.off_kvtile);
-  a.there = reinterpret_cast<uint2*>(ws + s.off_flags);
-  a.odd = reinterpret_cast<uint2*>(ws + s.off_flags + (s.off_c - s.off_flags) / 2);
+  a.there = reinterpret_cast<uint16_t*>(ws + s.off_flags);
+  a.odd = reinterpret_cast<uint16_t*>(ws + s.off_flags + (s.off_c - s.off_flags) / 2);
   hipLaunchKernelGGL(prompt_plan, dim3(1), dim3(1024), 0, stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
@@ -527,9 +560,9 @@ hipError_t launch_joint_prefill(const JointPrompt& s, const void* q, const int32
     const GatherArgs ga{static_cast<const uint8_t*>(pool), num_pages, joint_page_bytes(d), page_table, max_pages,
                         d.rank, d.rope_dim, c, rope};
     if (d.cache == DCKV_JOINT_E4M3)
-      hipLaunchKernelGGL((prompt_gather<true>), dim3(uint32_t(s.kv_tiles)), dim3(256), 0, stream, a, ga);
+      hipLaunchKernelGGL((prompt_gather<true>), dim3(uint32_t(s.kv_tiles) * 4), dim3(256), 0, stream, a, ga);
     else
-      hipLaunchKernelGGL((prompt_gather<false>), dim3(uint32_t(s.kv_tiles)), dim3(256), 0, stream, a, ga);
+      hipLaunchKernelGGL((prompt_gather<false>), dim3(uint32_t(s.kv_tiles) * 4), dim3(256), 0, stream, a, ga);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
     const uint32_t blocks = uint32_t(s.kv_tiles / 2) * (d.head_dim == 128 ? 2 : 1) * d.num_heads;
