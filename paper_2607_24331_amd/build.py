@@ -40,7 +40,10 @@ HIPCC_FLAGS = [
 # ordinary VGPRs: with the default AGPR form the register allocator rotated
 # accumulators through AGPR copies inside the k loop, each copy waiting for
 # an in-flight MFMA.
-HIPCC_EXTRA = {"append.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+# So does the joint decode, whose sums are scaled in ordinary registers: with
+# the AGPR form all of them were moved there and back for every tile.
+HIPCC_EXTRA = {src: ["-mllvm", "-amdgpu-mfma-vgpr-form"]
+               for src in ("append.hip", "joint_attend_128.hip", "joint_attend_256.hip", "joint_attend_512.hip")}
 HOST_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-D__HIP_PLATFORM_AMD__", "-Wall", "-Wextra"]
 
 

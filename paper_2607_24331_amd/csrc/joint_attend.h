@@ -49,9 +49,15 @@ __device__ __forceinline__ floatx4 mfma(u32x4 a, u32x4 b, floatx4 c) {
                                                  0, 0, 0);
 }
 
-// 16 bytes a lane from global memory to LDS, in lane order from p on.
-__device__ __forceinline__ void load_lds16(const uint8_t* g, unsigned char* p) {
-  __builtin_amdgcn_global_load_lds(g, p, 16, 0, 0);
+// 16 bytes a lane from global memory (base, uniform, + lane_at) to LDS, in lane order from
+// `lds` on.  Written out, as is the wait for them (loads_done): the compiler cannot tell
+// which buffer such a load fills and lets every LDS read wait for it.  It writes no
+// register.
+__device__ __forceinline__ void load_lds16(const uint8_t* base, uint32_t lane_at, uint32_t lds) {
+#ifdef __HIP_DEVICE_COMPILE__
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+               :: "s"(lds), "v"(lane_at), "s"(base) : "memory", "m0");
+#endif
 }
 
 // Eight e4m3 values times `scale`, a power of two, as bf16.
@@ -73,6 +79,13 @@ __device__ __forceinline__ uint32_t pair(float a, float b) {
 __device__ __forceinline__ uint32_t lds_address(unsigned char* p) {
   return uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) unsigned char*)(p)));
 }
+// Every load of the wave has landed: those written out, and those that the compiler knows of
+// (in a loop it would otherwise wait again for what was loaded before the loop).
+__device__ __forceinline__ void loads_done() {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0F70);                // vmcnt(0)
+}
+
 template <int O0, int O1, int O2, int O3, int HALF>
 __device__ __forceinline__ void read_tr16(u32x4 (&f)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
   u32x2 x0 = {}, x1 = {}, x2 = {}, x3 = {}, z0 = {}, z1 = {}, z2 = {}, z3 = {};
@@ -201,6 +214,7 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
   }
 
   unsigned char* bufs = smem + g * NBUF * S::TILE;
+  const uint32_t bufs_at = lds_address(bufs);
   // addresses in a tile: of token lr's pieces as keys, of this lane's tokens as values (four
   // lanes a token and 16 columns, two for e4m3).  Both meet the place of a piece by an
   // exclusive or below G * 16 bytes.
@@ -245,12 +259,12 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
       valid = page >= 0;
       if (!valid) return;
       const int half = (t0 + g + r * NG) & 1;
-      const uint8_t* src = a.pool + int64_t(page) * a.page_bytes + half * S::TILE + rw * 1024 + lane * 16;
-      unsigned char* dst = bufs + (r & (NBUF - 1)) * S::TILE + rw * 1024;
+      const uint8_t* src = a.pool + int64_t(page) * a.page_bytes + half * S::TILE + rw * 1024;
+      const uint32_t dst = bufs_at + (r & (NBUF - 1)) * S::TILE + rw * 1024;
 #pragma unroll
       for (int i = 0; i < LOADS; ++i)
         if (S::NL % WR == 0 || i < LOADS - 1 || i * WR + rw < S::NL)
-          load_lds16(src + i * (WR * 1024), dst + i * (WR * 1024));
+          load_lds16(src + i * (WR * 1024), lane * 16, dst + i * (WR * 1024));
       if constexpr (C8)                               // lanes 0 .. 31 the latents' exponents, 32 .. the keys'
         scales_next = a.pool[int64_t(page) * a.page_bytes + DCKV_PAGE_TOKENS * (W + (lane >> 5)) + half * kJointTile +
                              (lane & 31)];
@@ -290,7 +304,7 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
       valid = next_valid;
       const int pos = (t0 + g + r * NG) * kJointTile;  // the tile's first token
       const int scales = scales_next;
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's part of the tile is in LDS
+      loads_done();                                   // this wave's part of the tile is in LDS
       const bool edge = valid && pos + kJointTile > see_all;
       uint32_t odd = 0;
       if (edge) {
@@ -325,58 +339,79 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
         }
         // ---- scores: tokens pos + 16 n + 4 lq + v, row lr
         floatx4 s[2] = {floatx4{0.f, 0.f, 0.f, 0.f}, floatx4{0.f, 0.f, 0.f, 0.f}};
-        int ka = key_at;
-        asm volatile("" : "+v"(ka));                  // places are formed here, not kept for all steps
+        // pieces of a group of steps are read while the group before multiplies
+        constexpr int NP = C8 ? KS / 2 : KS, GP = (C8 ? 2 : 4) / (NW / 4);   // pieces a token, of a group
+        auto read_keys = [&](u32x4 (&x)[GP][2], int i0) {
+#pragma unroll
+          for (int i = 0; i < GP; ++i)
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+              if (i0 + i < NP) x[i][n] = *reinterpret_cast<const u32x4*>(buf + place<G>(key_at, i0 + i) + n * 16 * ROWB);
+        };
+        float sc[2] = {1.f, 1.f}, sk[2] = {1.f, 1.f};  // powers of two of tokens lr, 16 + lr: latent, key
+        u32x4 x0[GP][2], x1[GP][2];
+        u32x2 last[2];
+        read_keys(x0, 0);
         if constexpr (C8) {
-          float sc[2], sk[2];                         // powers of two of tokens lr, 16 + lr: latent, key
+          if constexpr (KS % 2 == 1) {                // the last 32 columns: 8 bytes a lane
+            const int at8 = lr * ROWB + (((W / 16 - 2 + (lq >> 1)) ^ joint_swap(G, lr)) * 16) + 8 * (lq & 1);
+#pragma unroll
+            for (int n = 0; n < 2; ++n) last[n] = *reinterpret_cast<const u32x2*>(buf + at8 + n * 16 * ROWB);
+          }
 #pragma unroll
           for (int n = 0; n < 2; ++n) {
             sc[n] = __uint_as_float(uint32_t(__shfl(scales, 16 * n + lr)) << 23);
             sk[n] = __uint_as_float(uint32_t(__shfl(scales, 32 + 16 * n + lr)) << 23);
           }
           if (lane < 32) scale_of[w][lane] = float(scales) - 127.f;
+        }
 #pragma unroll
-          for (int i = 0; i < KS / 2; ++i)            // 64 columns
+        for (int i0 = 0; i0 < NP; i0 += GP) {
+          u32x4(&x)[GP][2] = (i0 / GP) & 1 ? x1 : x0;
+          if (i0 + GP < NP) read_keys((i0 / GP) & 1 ? x0 : x1, i0 + GP);
+          __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int n = 0; n < 2; ++n) {
-              const u32x4 x = *reinterpret_cast<const u32x4*>(
-                  buf + place<G>(ka, i) + n * 16 * ROWB);
-              const float f = 64 * i < R ? sc[n] : sk[n];
-              s[n] = mfma(widen(x[0], x[1], f), q[2 * i], s[n]);
-              s[n] = mfma(widen(x[2], x[3], f), q[2 * i + 1], s[n]);
-            }
-          if constexpr (KS % 2 == 1) {                // the last 32: 8 bytes a lane
-            const int t = lr, at8 = t * ROWB + (((W / 16 - 2 + (lq >> 1)) ^ joint_swap(G, t)) * 16) + 8 * (lq & 1);
+          for (int i = 0; i < GP; ++i)
 #pragma unroll
             for (int n = 0; n < 2; ++n) {
-              const u32x2 x = *reinterpret_cast<const u32x2*>(buf + at8 + n * 16 * ROWB);
-              s[n] = mfma(widen(x[0], x[1], sk[n]), q[KS - 1], s[n]);
+              if (i0 + i >= NP) continue;
+              if constexpr (C8) {
+                const float f = 64 * (i0 + i) < R ? sc[n] : sk[n];
+                s[n] = mfma(widen(x[i][n][0], x[i][n][1], f), q[2 * (i0 + i)], s[n]);
+                s[n] = mfma(widen(x[i][n][2], x[i][n][3], f), q[2 * (i0 + i) + 1], s[n]);
+              } else {
+                s[n] = mfma(x[i][n], q[i0 + i], s[n]);
+              }
             }
-          }
-        } else {
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        if constexpr (C8 && KS % 2 == 1) {
 #pragma unroll
-          for (int i = 0; i < KS; ++i)
-#pragma unroll
-            for (int n = 0; n < 2; ++n) {
-              const u32x4 x = *reinterpret_cast<const u32x4*>(buf + place<G>(ka, i) + n * 16 * ROWB);
-              s[n] = mfma(x, q[i], s[n]);
-            }
+          for (int n = 0; n < 2; ++n) s[n] = mfma(widen(last[n][0], last[n][1], sk[n]), q[KS - 1], s[n]);
         }
         // ---- softmax
         auto exponents = [&](int n) { return *reinterpret_cast<const floatx4*>(&scale_of[w][16 * n + 4 * lq]); };
-        float top = -INFINITY, utop = -INFINITY;
 #pragma unroll
-        for (int n = 0; n < 2; ++n) {
+        for (int n = 0; n < 2; ++n)
 #pragma unroll
           for (int v = 0; v < 4; ++v) {
             s[n][v] *= a.scale;
             s[n][v] += s[n][v] - s[n][v];              // an infinite score becomes NaN
-            if (edge) {
+          }
+        if (edge) {
+#pragma unroll
+          for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
               const int t = 16 * n + 4 * lq + v;
               s[n][v] = pos + t < limit ? ((odd >> t) & 1 ? __builtin_nanf("") : s[n][v]) : -INFINITY;
             }
-            top = fmaxf(top, s[n][v]);
-          }
+        }
+        float top = -INFINITY, utop = -INFINITY;
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+#pragma unroll
+          for (int v = 0; v < 4; ++v) top = fmaxf(top, s[n][v]);
           if constexpr (C8) {
             const floatx4 ex = exponents(n);
 #pragma unroll

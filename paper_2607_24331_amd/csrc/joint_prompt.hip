@@ -353,6 +353,23 @@ __global__ __launch_bounds__(256, 2) void prompt_expand(const int32_t* __restric
   }
 }
 
+// Every load of the wave has landed, and the compiler knows it.
+__device__ __forceinline__ void loads_done() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0F70);                  // vmcnt(0)
+  asm volatile("" ::: "memory");
+}
+
+// LDS reads and products of one phase, `ahead` reads on their way.
+template <int READS, int AHEAD>
+__device__ __forceinline__ void reads_ahead() {
+#pragma unroll
+  for (int i = 0; i < READS + AHEAD; ++i) {
+    if (i < READS) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    if (i >= AHEAD) __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+  }
+}
+
 __device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b),
                                                  c, 0, 0, 0);
@@ -365,7 +382,7 @@ __global__ __launch_bounds__(256, 2) void prompt_attend(PromptArgs a, const uint
                                                         const bf16* __restrict__ q, int heads, float scale,
                                                         bf16* __restrict__ out) {
   constexpr int KB = kTok * D * 2, PB = kTok * P * 2, TILE = 2 * KB + PB;
-  constexpr int KL = KB / 1024, PL = PB / 1024, NL = 2 * KL + PL;    // 1 KB loads
+  constexpr int KL = KB / 1024, PL = PB / 1024;        // 1 KB loads
   constexpr int KG = joint_gcd16(D / 8), PG = P > 0 ? joint_gcd16(P / 8) : 1;
   constexpr int DS = D / 16, PS = P / 16, CT = D / 32;
   __shared__ __align__(1024) unsigned char smem[2 * TILE];
@@ -382,19 +399,30 @@ __global__ __launch_bounds__(256, 2) void prompt_attend(PromptArgs a, const uint
   const uint8_t* ksrc = keys + (int64_t(head) * a.kv_tiles + rt.kv) * KB + lane * 16;
   const uint8_t* vsrc = values + (int64_t(head) * a.kv_tiles + rt.kv) * KB + lane * 16;
   const uint8_t* psrc = rope + int64_t(rt.kv) * PB + lane * 16;
+  // keys, position keys, values; every wave a quarter of each
   auto issue = [&](int t) {
-    unsigned char* dst = smem + (t & 1) * TILE;
+    unsigned char* dst = smem + (t & 1) * TILE + w * 1024;
+    const uint8_t* ks = ksrc + int64_t(t) * KB + w * 1024;
+    const uint8_t* vs = vsrc + int64_t(t) * KB + w * 1024;
+    const uint8_t* ps = psrc + int64_t(t) * PB + w * 1024;
 #pragma unroll
-    for (int i = 0; i < NL / 4; ++i) {
-      const int n = 4 * i + w;                         // keys, then position keys, then values
-      const uint8_t* src = n < KL ? ksrc + int64_t(t) * KB + n * 1024
-                                  : n < KL + PL ? psrc + int64_t(t) * PB + (n - KL) * 1024
-                                                : vsrc + int64_t(t) * KB + (n - KL - PL) * 1024;
-      load_lds16(src, dst + n * 1024);
-    }
+    for (int i = 0; i < KL / 4; ++i) load_lds16(ks + i * 4096, dst + i * 4096);
+#pragma unroll
+    for (int i = 0; i < PL / 4; ++i) load_lds16(ps + i * 4096, dst + KB + i * 4096);
+#pragma unroll
+    for (int i = 0; i < KL / 4; ++i) load_lds16(vs + i * 4096, dst + KB + PB + i * 4096);
   };
-  static_assert(NL % 4 == 0, "whole loads");
-  if (tiles > 0) issue(0);
+  static_assert(KL % 4 == 0 && PL % 4 == 0, "whole loads a wave");
+  // which tokens are there and finite: on their way before a tile is
+  uint2 there = {}, odd = {};
+  auto marks = [&](int t) {
+    there = reinterpret_cast<const uint2*>(a.there)[rt.kv + t];
+    odd = reinterpret_cast<const uint2*>(a.odd)[rt.kv + t];
+  };
+  if (tiles > 0) {
+    marks(0);
+    issue(0);
+  }
 
   // queries: pieces 2 i + h of row lr, in the keys' order of coordinates
   u32x4 qd[DS], qp[PS > 0 ? PS : 1];
@@ -417,14 +445,17 @@ __global__ __launch_bounds__(256, 2) void prompt_attend(PromptArgs a, const uint
   const int ksw = joint_swap(KG, lr), psw = P > 0 ? joint_swap(PG, lr) : 0, vsw = joint_swap(8, lr);
 
   for (int t = 0; t < tiles; ++t) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    loads_done();
     __syncthreads();                                   // the tile is whole, the one before is used up
-    if (t + 1 < tiles) issue(t + 1);
+    const uint2 th2 = there, od2 = odd;
+    if (t + 1 < tiles) {
+      marks(t + 1);
+      issue(t + 1);
+    }
     unsigned char* buf = smem + (t & 1) * TILE;
-    const uint2 there = reinterpret_cast<const uint2*>(a.there)[rt.kv + t], odd = reinterpret_cast<const uint2*>(a.odd)[rt.kv + t];
     const int pos = t * kTok;
     // rows of the wave that do not see the whole tile, or a tile with holes
-    const bool edge = pos + kTok > rt.first + w * 32 + 1 || (there.x & there.y) != ~0u || (odd.x | odd.y) != 0;
+    const bool edge = pos + kTok > rt.first + w * 32 + 1 || (th2.x & th2.y) != ~0u || (od2.x | od2.y) != 0;
 
     // ---- scores: tokens pos + 32 n + 8 b + 4 h + v (register 4 b + v), row lr
     f32x16 s[2];
@@ -439,22 +470,31 @@ __global__ __launch_bounds__(256, 2) void prompt_attend(PromptArgs a, const uint
       for (int i = 0; i < PS; ++i)
         s[n] = mfma(*reinterpret_cast<const u32x4*>(buf + KB + (32 * n + lr) * (P * 2) + ((2 * i + h) ^ psw) * 16), qp[i], s[n]);
     }
+    reads_ahead<2 * (DS + PS), 4>();
+    __builtin_amdgcn_sched_barrier(0);
     // ---- softmax; an infinite score becomes NaN
-    float top = -INFINITY;
 #pragma unroll
     for (int n = 0; n < 2; ++n)
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
-        float x = s[n][v] * scale;
-        x += x - x;
-        if (edge) {
-          const int b = 8 * (v >> 2) + 4 * h + (v & 3);
-          const uint32_t th = n ? there.y : there.x, od = n ? odd.y : odd.x;
-          x = pos + 32 * n + b < limit && ((th >> b) & 1) ? ((od >> b) & 1 ? __builtin_nanf("") : x) : -INFINITY;
-        }
-        s[n][v] = x;
-        top = fmaxf(top, x);
+        s[n][v] *= scale;
+        s[n][v] += s[n][v] - s[n][v];
       }
+    if (edge) {
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const int b = 8 * (v >> 2) + 4 * h + (v & 3);
+          const uint32_t th = n ? th2.y : th2.x, od = n ? od2.y : od2.x;
+          s[n][v] = pos + 32 * n + b < limit && ((th >> b) & 1) ? ((od >> b) & 1 ? __builtin_nanf("") : s[n][v]) : -INFINITY;
+        }
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) top = fmaxf(top, s[n][v]);
     top = fmaxf(top, __shfl_xor(top, 32));
     if (__any(top > m + kSlack)) {
       const float m_new = fmaxf(m, top);
@@ -486,6 +526,8 @@ __global__ __launch_bounds__(256, 2) void prompt_attend(PromptArgs a, const uint
 #pragma unroll
       for (int k = 0; k < 4; ++k)
         acc[i] = mfma(*reinterpret_cast<const u32x4*>(vb + i * (32 * kTok * 2) + ((2 * k + h) ^ vsw) * 16), p[k], acc[i]);
+    reads_ahead<4 * CT, 4>();
+    __builtin_amdgcn_sched_barrier(0);
   }
   l += __shfl_xor(l, 32);
   if (my >= rt.n) return;
