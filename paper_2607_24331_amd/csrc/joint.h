@@ -15,8 +15,13 @@ constexpr int kJointMaxUnits = 512;     // work-groups of a row slice, at most (
 __host__ __device__ constexpr int joint_gcd16(int n) { return n % 16 == 0 ? 16 : n % 8 == 0 ? 8 : n % 4 == 0 ? 4 : n % 2 == 0 ? 2 : 1; }
 __host__ __device__ constexpr int joint_swap(int g, int s) { return (s / (16 / g)) & (g - 1); }
 
-// Waves of a work-group whose slice is row_waves x 16 rows.
-__host__ __device__ constexpr int joint_waves(int row_waves) { return row_waves <= 2 ? 4 : 8; }
+// Waves of a work-group whose slice is row_waves x 16 rows: eight, two a SIMD, which issue
+// vector instructions twice as fast as one, where LDS holds their token groups' tiles,
+// two each where waves share them, else four.
+__host__ __device__ constexpr int joint_waves(int row_waves, int tile_bytes) {
+  return 8 / row_waves * tile_bytes * (row_waves > 1 ? 2 : 1) <= 158000 ? 8 : 4;
+}
+__host__ __device__ constexpr int joint_tile_bytes(int width, bool e4m3) { return kJointTile * width * (e4m3 ? 1 : 2); }
 
 // Launch shape of one absorbed decode.
 struct JointShape {

@@ -135,6 +135,15 @@ __device__ __forceinline__ int place(int at, int i) {
   return G >= 4 ? (at ^ ((i & (G / 4 - 1)) * 64)) + i / (G / 4 > 0 ? G / 4 : 1) * (G * 16) : at + i * 64;
 }
 
+// A value that the compiler cannot form ahead of this place: what only the ends of a
+// segment need must not hold registers through its tiles.
+__device__ __forceinline__ int here(int x) {
+#ifdef __HIP_DEVICE_COMPILE__
+  asm volatile("" : "+v"(x));
+#endif
+  return x;
+}
+
 // Over the four lanes that hold a row.
 __device__ __forceinline__ float row_max(float x) {
   x = fmaxf(x, __shfl_xor(x, 16));
@@ -159,8 +168,8 @@ template <int R, int P, bool C8, int WR>
 struct Shape {
   static constexpr int W = R + P, E = C8 ? 1 : 2, ROWB = W * E, PIECES = ROWB / 16;
   static constexpr int G = joint_gcd16(PIECES);
-  static constexpr int NW = joint_waves(WR), NG = NW / WR, THREADS = 64 * NW;
-  static constexpr int TILE = kJointTile * ROWB;      // bytes
+  static constexpr int TILE = joint_tile_bytes(W, C8);
+  static constexpr int NW = joint_waves(WR, TILE), NG = NW / WR, THREADS = 64 * NW;
   // a second buffer, so that the next tile comes while this one is used; lone waves with
   // wide bf16 tiles have no room for it, there the other waves use the time
   static constexpr int NBUF = WR > 1 || 2 * NG * TILE <= 158000 ? 2 : 1;
@@ -258,16 +267,16 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
       const int page = __builtin_amdgcn_readlane(ids, r & 63);
       valid = page >= 0;
       if (!valid) return;
-      const int half = (t0 + g + r * NG) & 1;
+      const int half = (t0 + g + r * NG) & 1, ln = here(lane);
       const uint8_t* src = a.pool + int64_t(page) * a.page_bytes + half * S::TILE + rw * 1024;
       const uint32_t dst = bufs_at + (r & (NBUF - 1)) * S::TILE + rw * 1024;
 #pragma unroll
       for (int i = 0; i < LOADS; ++i)
         if (S::NL % WR == 0 || i < LOADS - 1 || i * WR + rw < S::NL)
-          load_lds16(src + i * (WR * 1024), lane * 16, dst + i * (WR * 1024));
+          load_lds16(src + i * (WR * 1024), ln * 16, dst + i * (WR * 1024));
       if constexpr (C8)                               // lanes 0 .. 31 the latents' exponents, 32 .. the keys'
-        scales_next = a.pool[int64_t(page) * a.page_bytes + DCKV_PAGE_TOKENS * (W + (lane >> 5)) + half * kJointTile +
-                             (lane & 31)];
+        scales_next = a.pool[int64_t(page) * a.page_bytes + DCKV_PAGE_TOKENS * (W + (ln >> 5)) + half * kJointTile +
+                             (ln & 31)];
     };
     bool valid = false, next_valid = false;
     issue(0, next_valid);
@@ -311,10 +320,11 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
         // tokens behind the sequence become zeros; a NaN in one that some rows see and
         // others do not is taken out of the values and given back through the scores
         uint32_t mask = 0;
+        const int ln = here(lane);
 #pragma unroll 1
         for (int i = 0; i < LOADS; ++i) {
           if (i * WR + rw >= S::NL) break;
-          const int n = (i * WR + rw) * 64 + lane, t = n / S::PIECES;
+          const int n = (i * WR + rw) * 64 + ln, t = n / S::PIECES;
           u32x4* p = reinterpret_cast<u32x4*>(buf + n * 16);
           if (pos + t >= T) {
             *p = u32x4{0u, 0u, 0u, 0u};
@@ -340,13 +350,14 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
         // ---- scores: tokens pos + 16 n + 4 lq + v, row lr
         floatx4 s[2] = {floatx4{0.f, 0.f, 0.f, 0.f}, floatx4{0.f, 0.f, 0.f, 0.f}};
         // pieces of a group of steps are read while the group before multiplies
-        constexpr int NP = C8 ? KS / 2 : KS, GP = (C8 ? 2 : 4) / (NW / 4);   // pieces a token, of a group
+        constexpr int NP = C8 ? KS / 2 : KS, GP = NW == 8 ? 1 : C8 ? 2 : 4;   // pieces a token, of a group
+        const int ka = here(key_at);
         auto read_keys = [&](u32x4 (&x)[GP][2], int i0) {
 #pragma unroll
           for (int i = 0; i < GP; ++i)
 #pragma unroll
             for (int n = 0; n < 2; ++n)
-              if (i0 + i < NP) x[i][n] = *reinterpret_cast<const u32x4*>(buf + place<G>(key_at, i0 + i) + n * 16 * ROWB);
+              if (i0 + i < NP) x[i][n] = *reinterpret_cast<const u32x4*>(buf + place<G>(ka, i0 + i) + n * 16 * ROWB);
         };
         float sc[2] = {1.f, 1.f}, sk[2] = {1.f, 1.f};  // powers of two of tokens lr, 16 + lr: latent, key
         u32x4 x0[GP][2], x1[GP][2];
@@ -461,13 +472,14 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
         }
         // ---- output: column 16 i + lr of the A operand, tokens 4 lq + 0 .. 3 and 16 more
         const uint32_t base = lds_address(buf);
+        const int va = here(value_at);
         if constexpr (C8) {
           unrolled<CT / 4>([&](auto k) {
             constexpr int I = 4 * decltype(k)::value, M = G - 1;
             u32x2 x[4];
             read_tr8<I / G * (G * 16), (I + 1) / G * (G * 16), (I + 2) / G * (G * 16), (I + 3) / G * (G * 16)>(
-                x, base + (value_at ^ ((I & M) * 16)), base + (value_at ^ (((I + 1) & M) * 16)),
-                base + (value_at ^ (((I + 2) & M) * 16)), base + (value_at ^ (((I + 3) & M) * 16)));
+                x, base + (va ^ ((I & M) * 16)), base + (va ^ (((I + 1) & M) * 16)),
+                base + (va ^ (((I + 2) & M) * 16)), base + (va ^ (((I + 3) & M) * 16)));
 #pragma unroll
             for (int j = 0; j < 4; ++j) acc[I + j] = mfma(widen(x[j][0], x[j][1], 1.f), p, acc[I + j]);
           });
@@ -476,8 +488,8 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
             constexpr int I = 4 * decltype(k)::value, H = G / 2, M = H - 1;
             u32x4 x[4];
             read_tr16<I / H * (G * 16), (I + 1) / H * (G * 16), (I + 2) / H * (G * 16), (I + 3) / H * (G * 16), 16 * ROWB>(
-                x, base + (value_at ^ ((I & M) * 32)), base + (value_at ^ (((I + 1) & M) * 32)),
-                base + (value_at ^ (((I + 2) & M) * 32)), base + (value_at ^ (((I + 3) & M) * 32)));
+                x, base + (va ^ ((I & M) * 32)), base + (va ^ (((I + 1) & M) * 32)),
+                base + (va ^ (((I + 2) & M) * 32)), base + (va ^ (((I + 3) & M) * 32)));
 #pragma unroll
             for (int j = 0; j < 4; ++j) acc[I + j] = mfma(x[j], p, acc[I + j]);
           });
@@ -492,40 +504,42 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
     l += __shfl_xor(l, 32);
 
     // ---- the token groups' states, CJ columns at a time
+    const int jt = here(tid), jr = jt & 15, jq = (jt >> 4) & 3;        // lane's row, quarter
+    const bool mine_too = (slice * WR + rw) * 16 + jr < rows;
     const int64_t seg = int64_t(unit) + (prefix ? 0 : b);
     const int64_t prow = (seg * a.slices + slice) * (16 * WR);
     if constexpr (NG == 1) {
-      if (row < rows) {
-        float* dst = a.part_o + (prow + rw * 16 + lr) * R + 4 * lq;
+      if (mine_too) {
+        float* dst = a.part_o + (prow + rw * 16 + jr) * R + 4 * jq;
 #pragma unroll
         for (int i = 0; i < CT; ++i) *reinterpret_cast<floatx4*>(dst + 16 * i) = acc[i];
-        if (lq == 0) a.part_ml[prow + rw * 16 + lr] = make_float4(m, l, u, 0.f);
+        if (jq == 0) a.part_ml[prow + rw * 16 + jr] = make_float4(m, l, u, 0.f);
       }
       __syncthreads();                                // the tiles are used up
     } else {
       constexpr int CJ = S::CJ, ST = CJ + 4;
-      if (lq == 0) {
-        join_m[w][lr] = m;
-        join_l[w][lr] = l;
-        join_u[w][lr] = u;
+      if (jq == 0) {
+        join_m[w][jr] = m;
+        join_l[w][jr] = l;
+        join_u[w][jr] = u;
       }
       __syncthreads();                                // the tiles are used up, m and u are there
       float mm = -INFINITY, uu = -INFINITY;
 #pragma unroll
       for (int k = 0; k < NG; ++k) {
-        mm = fmaxf(mm, join_m[k * WR + rw][lr]);
-        uu = fmaxf(uu, join_u[k * WR + rw][lr]);
+        mm = fmaxf(mm, join_m[k * WR + rw][jr]);
+        uu = fmaxf(uu, join_u[k * WR + rw][jr]);
       }
       const float keep = u == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(u - uu);
-      if (g == 0 && lq == 0 && row < rows) {
+      if (g == 0 && jq == 0 && mine_too) {
         float ll = 0.f;
 #pragma unroll
         for (int k = 0; k < NG; ++k) {
-          const float mk = join_m[k * WR + rw][lr];
-          if (mk != -INFINITY || join_l[k * WR + rw][lr] != 0.f)
-            ll += join_l[k * WR + rw][lr] * __builtin_amdgcn_exp2f(mk - mm);
+          const float mk = join_m[k * WR + rw][jr];
+          if (mk != -INFINITY || join_l[k * WR + rw][jr] != 0.f)
+            ll += join_l[k * WR + rw][jr] * __builtin_amdgcn_exp2f(mk - mm);
         }
-        a.part_ml[prow + rw * 16 + lr] = make_float4(mm, ll, uu, 0.f);
+        a.part_ml[prow + rw * 16 + jr] = make_float4(mm, ll, uu, 0.f);
       }
       float* ex = reinterpret_cast<float*>(smem);     // [wave][16 rows][ST]
 #pragma unroll
@@ -536,11 +550,11 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
           floatx4 x;
 #pragma unroll
           for (int v = 0; v < 4; ++v) x[v] = acc[c0 / 16 + i][v] * keep;
-          *reinterpret_cast<floatx4*>(ex + (w * 16 + lr) * ST + 16 * i + 4 * lq) = x;
+          *reinterpret_cast<floatx4*>(ex + (w * 16 + jr) * ST + 16 * i + 4 * jq) = x;
         }
         __syncthreads();
 #pragma unroll
-        for (int e = tid; e < WR * 16 * (CJ / 4); e += S::THREADS) {
+        for (int e = jt; e < WR * 16 * (CJ / 4); e += S::THREADS) {
           const int rr = e / (CJ / 4), c = e % (CJ / 4) * 4;
           if (slice * WR * 16 + rr >= rows) continue;
           floatx4 x = *reinterpret_cast<const floatx4*>(ex + rr * ST + c);
@@ -556,12 +570,13 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
 
 template <int R, int P, bool C8>
 hipError_t launch_rows(int row_waves, const JointAttend& a, hipStream_t stream) {
+  const uint32_t threads = 64 * joint_waves(row_waves, joint_tile_bytes(R + P, C8));
   const uint32_t groups = uint32_t((a.units + 7) / 8 * 8) * uint32_t(a.slices);
   switch (row_waves) {
-    case 1: hipLaunchKernelGGL((joint_attend<R, P, C8, 1>), dim3(groups), dim3(64 * joint_waves(row_waves)), 0, stream, a); break;
-    case 2: hipLaunchKernelGGL((joint_attend<R, P, C8, 2>), dim3(groups), dim3(64 * joint_waves(row_waves)), 0, stream, a); break;
-    case 4: hipLaunchKernelGGL((joint_attend<R, P, C8, 4>), dim3(groups), dim3(64 * joint_waves(row_waves)), 0, stream, a); break;
-    case 8: hipLaunchKernelGGL((joint_attend<R, P, C8, 8>), dim3(groups), dim3(64 * joint_waves(row_waves)), 0, stream, a); break;
+    case 1: hipLaunchKernelGGL((joint_attend<R, P, C8, 1>), dim3(groups), dim3(threads), 0, stream, a); break;
+    case 2: hipLaunchKernelGGL((joint_attend<R, P, C8, 2>), dim3(groups), dim3(threads), 0, stream, a); break;
+    case 4: hipLaunchKernelGGL((joint_attend<R, P, C8, 4>), dim3(groups), dim3(threads), 0, stream, a); break;
+    case 8: hipLaunchKernelGGL((joint_attend<R, P, C8, 8>), dim3(groups), dim3(threads), 0, stream, a); break;
     default: return hipErrorInvalidValue;
   }
   return hipGetLastError();

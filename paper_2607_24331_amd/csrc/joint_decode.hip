@@ -311,7 +311,9 @@ int64_t tiles_of(int64_t tokens) { return (tokens + kJointTile - 1) / kJointTile
 // Rows of a work-group, 16 a wave: the least of 16, 32, 64 that takes all of them, else 128.
 int row_waves_of(int64_t rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : rows <= 64 ? 4 : 8; }
 
-int groups_of(int row_waves) { return joint_waves(row_waves) / row_waves; }
+int groups_of(const dckv_joint_desc& d, int row_waves) {
+  return joint_waves(row_waves, joint_tile_bytes(d.rank + d.rope_dim, d.cache == DCKV_JOINT_E4M3)) / row_waves;
+}
 
 // Units of a slice for at most `tiles` tiles: fill the chip with the slices, a round
 // of the token groups at least, none more than the join holds.
@@ -363,11 +365,11 @@ JointShape joint_shape(const dckv_joint_desc& d, int32_t queries, int32_t batch,
   s.row_waves = row_waves_of(s.rows);
   s.slices = (s.rows + 16 * s.row_waves - 1) / (16 * s.row_waves);
   const int64_t tiles = int64_t(batch) * tiles_of(max_context);
-  s.units = units_of(d.rank, s.slices, tiles, groups_of(s.row_waves));
+  s.units = units_of(d.rank, s.slices, tiles, groups_of(d, s.row_waves));
   const int64_t all = int64_t(s.rows) * batch;
   s.pre_row_waves = row_waves_of(all);
   s.pre_slices = int32_t((all + 16 * s.pre_row_waves - 1) / (16 * s.pre_row_waves));
-  s.pre_units = prefix_len > 0 ? units_of(d.rank, s.pre_slices, tiles_of(prefix_len), groups_of(s.pre_row_waves)) : 0;
+  s.pre_units = prefix_len > 0 ? units_of(d.rank, s.pre_slices, tiles_of(prefix_len), groups_of(d, s.pre_row_waves)) : 0;
   const size_t width = size_t(d.rank + d.rope_dim);
   s.off_start = align_up(size_t(all) * width * 2);
   s.off_mean = s.off_start + align_up(size_t(batch + 1) * 8);
@@ -447,8 +449,8 @@ hipError_t launch_joint_decode(const JointShape& s, const void* q, const void* p
   }
   const FinishArgs f{starts, a.part_o, a.part_ml, reinterpret_cast<const float*>(ws + s.off_pre_o),
                      reinterpret_cast<const float4*>(ws + s.off_pre_ml), s.batch, s.queries, d.num_heads,
-                     16 * s.row_waves, s.slices, s.units, groups_of(s.row_waves), 16 * s.pre_row_waves,
-                     s.pre_slices, s.pre_units, groups_of(s.pre_row_waves), s.prefix_len};
+                     16 * s.row_waves, s.slices, s.units, groups_of(d, s.row_waves), 16 * s.pre_row_waves,
+                     s.pre_slices, s.pre_units, groups_of(d, s.pre_row_waves), s.prefix_len};
 #define DCKV_FINISH(R, D) return finish<R, D>(f, W_values, n, reinterpret_cast<float*>(ws + s.off_mean), out, stream)
   if (d.rank == 128) {
     if (d.head_dim == 64) DCKV_FINISH(128, 64);
