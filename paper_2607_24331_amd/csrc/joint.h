@@ -59,6 +59,24 @@ __host__ __device__ inline int64_t joint_tiles_a_unit(int64_t total, int units, 
   return n < groups ? groups : n;
 }
 
+// How `total` tiles of `batch` sequences are cut into units' segments.  Segments of sequence
+// b, whose first tile is start, are numbered from start / per + b on.
+//   whole   a unit is a segment: up to `per` tiles of one sequence; unit = segment.  The ends
+//           of a segment cost about what ten tiles do, so this is taken where it makes a
+//           unit no more than kJointWhole tiles longer than equal shares.
+//   shares  unit u takes tiles u * per .. of all, whatever sequences they are of; segment u + b.
+struct JointCut {
+  int64_t per;
+  bool whole;
+};
+constexpr int kJointWhole = 12;
+__host__ __device__ inline JointCut joint_cut(int64_t total, int units, int batch, int groups) {
+  const int spare = units - batch > units / 4 ? units - batch : (units + 3) / 4;
+  const int64_t per = joint_tiles_a_unit(total, spare, groups), share = joint_tiles_a_unit(total, units, groups);
+  if (per <= share + kJointWhole) return JointCut{per, true};
+  return JointCut{share, false};
+}
+
 struct JointPrompt {
   dckv_joint_desc d;
   int32_t n_rows, batch, max_context;

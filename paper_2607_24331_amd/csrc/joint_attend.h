@@ -23,8 +23,8 @@
 // under their power of two (exactly), as values without it: the weights take it, held
 // against a maximum u of score + exponent of their own, so that they are at most
 // 2^kSlack whatever the exponents are.
-// Work is cut into `units` equal shares of all sequences' tiles, whatever their lengths;
-// a unit walks over the sequences that it meets (segments, numbered unit + sequence).
+// Work is cut by the sequences' actual lengths (joint_cut): into equal shares of all
+// their tiles, a unit walking over the sequences that it meets, or a sequence at a time.
 #pragma once
 
 #include <type_traits>
@@ -106,15 +106,20 @@ __device__ __forceinline__ void read_tr16(u32x4 (&f)[4], uint32_t a0, uint32_t a
   f[2] = u32x4{x2[0], x2[1], z2[0], z2[1]};
   f[3] = u32x4{x3[0], x3[1], z3[0], z3[1]};
 }
-template <int O0, int O1, int O2, int O3>
-__device__ __forceinline__ void read_tr8(u32x2 (&f)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
+// Eight column tiles of e4m3, likewise.
+template <int O0, int O1, int O2, int O3, int O4, int O5, int O6, int O7>
+__device__ __forceinline__ void read_tr8(u32x2 (&f)[8], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                         uint32_t a4, uint32_t a5, uint32_t a6, uint32_t a7) {
 #ifdef __HIP_DEVICE_COMPILE__
   asm volatile(
-      "ds_read_b64_tr_b8 %0, %4 offset:%8\n\tds_read_b64_tr_b8 %1, %5 offset:%9\n\t"
-      "ds_read_b64_tr_b8 %2, %6 offset:%10\n\tds_read_b64_tr_b8 %3, %7 offset:%11\n\t"
+      "ds_read_b64_tr_b8 %0, %8 offset:%16\n\tds_read_b64_tr_b8 %1, %9 offset:%17\n\t"
+      "ds_read_b64_tr_b8 %2, %10 offset:%18\n\tds_read_b64_tr_b8 %3, %11 offset:%19\n\t"
+      "ds_read_b64_tr_b8 %4, %12 offset:%20\n\tds_read_b64_tr_b8 %5, %13 offset:%21\n\t"
+      "ds_read_b64_tr_b8 %6, %14 offset:%22\n\tds_read_b64_tr_b8 %7, %15 offset:%23\n\t"
       "s_waitcnt lgkmcnt(0)"
-      : "=&v"(f[0]), "=&v"(f[1]), "=&v"(f[2]), "=&v"(f[3])
-      : "v"(a0), "v"(a1), "v"(a2), "v"(a3), "i"(O0), "i"(O1), "i"(O2), "i"(O3)
+      : "=&v"(f[0]), "=&v"(f[1]), "=&v"(f[2]), "=&v"(f[3]), "=&v"(f[4]), "=&v"(f[5]), "=&v"(f[6]), "=&v"(f[7])
+      : "v"(a0), "v"(a1), "v"(a2), "v"(a3), "v"(a4), "v"(a5), "v"(a6), "v"(a7), "i"(O0), "i"(O1), "i"(O2), "i"(O3),
+        "i"(O4), "i"(O5), "i"(O6), "i"(O7)
       : "memory");
 #endif
 }
@@ -178,6 +183,8 @@ struct Shape {
   static constexpr int LDS = NG * NBUF * TILE > JOIN ? NG * NBUF * TILE : JOIN;
   static constexpr int NL = PIECES / 2;               // 1 KB loads of a tile, dealt out to WR waves
   static constexpr int LOADS = (NL + WR - 1) / WR;
+  // the last steps' queries stay in LDS where the registers of two waves a SIMD are full
+  static constexpr int QL = C8 && R == 512 && NW == 8 ? 4 : 0;
   static_assert(PIECES % 2 == 0, "whole loads");
 };
 
@@ -188,6 +195,8 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
   constexpr int KS = W / 32, CT = R / 16;             // steps of the scores, column tiles of the sums
   __shared__ __align__(1024) unsigned char smem[S::LDS];
   __shared__ float scale_of[C8 ? NW : 1][kJointTile];  // a wave's tile: exponents of its latents
+  constexpr int QL = S::QL, KQ = W / 32 - QL;
+  __shared__ u32x4 last_q[QL > 0 ? WR : 1][QL > 0 ? QL : 1][64];
   __shared__ uint32_t odd_of[2][NW];                  // tokens of a tile's edge that hold a NaN, by loading wave
   __shared__ float join_m[NW][16], join_l[NW][16], join_u[NW][16];
 
@@ -198,29 +207,61 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
   // its tokens in one L2
   const int id = blockIdx.x;
   const int unit = (id / (8 * a.slices)) * 8 + (id & 7), slice = (id >> 3) % a.slices;
-  if (unit >= a.units) return;
   const bool prefix = a.prefix_len > 0;
   const int rows = a.queries * a.heads * (prefix ? a.batch : 1);
-  const int64_t total = prefix ? (a.prefix_len + kJointTile - 1) / kJointTile : a.start[a.batch];
-  const int64_t per = joint_tiles_a_unit(total, a.units, NG);
-  int64_t at = unit * per;
-  const int64_t end = min(at + per, total);
-  if (at >= end) return;
-
-  // the sequence that holds tile `at`: the last b with start[b] <= at, 64 candidates a round
+  // 64 sequences at a time, a lane one: first tile, that of the next one, tokens
+  int win = 0, win_len = 0;
+  int64_t win_start = 0, win_end = 0;
+  auto load_window = [&](int b0) {
+    win = b0;
+    const int i = min(b0 + lane, a.batch - 1);
+    win_start = a.start[i];
+    win_end = a.start[i + 1];
+    win_len = min(max(a.seq_lens[i], 0), a.max_context);
+  };
+  auto lane64 = [](int64_t x, int l) {
+    const uint32_t lo = __builtin_amdgcn_readlane(int(uint32_t(x)), l), hi = __builtin_amdgcn_readlane(int(x >> 32), l);
+    return int64_t(uint64_t(hi) << 32 | lo);
+  };
   int b = 0;
-  if (!prefix) {
-    int lo = 0, n = a.batch;                          // start[lo] <= at; the answer is in lo .. lo + n - 1
-    while (n > 1) {
-      const int step = (n + 63) / 64;
-      const int i = lo + lane * step;
-      const bool in = lane * step < n && a.start[i] <= at;
-      const int k = __popcll(__ballot(in)) - 1;       // starts ascend: the first k + 1 lanes hold
+  int64_t at, end;                                    // tiles of this unit, among all
+  bool whole = false;
+  if (prefix) {
+    const int64_t total = (a.prefix_len + kJointTile - 1) / kJointTile, per = joint_tiles_a_unit(total, a.units, NG);
+    at = unit * per;
+    end = min(at + per, total);
+  } else {
+    load_window(0);
+    const int64_t total = a.start[a.batch];
+    const JointCut cut = joint_cut(total, a.units, a.batch, NG);
+    whole = cut.whole;
+    // the last sequence b whose first tile (whole: first segment) is at most this unit's
+    const int64_t want = cut.whole ? unit : unit * cut.per;
+    auto key = [&](int64_t start, int i) { return cut.whole ? start / cut.per + i : start; };
+    int lo = 0, n = a.batch;                          // the answer is in lo .. lo + n - 1
+    while (n > 64) {
+      const int step = (n + 63) / 64, i = lo + lane * step;
+      const bool in = lane * step < n && key(a.start[min(i, a.batch)], i) <= want;
+      const int k = max(__popcll(__ballot(in)) - 1, 0);      // keys ascend: the first lanes hold
       lo += k * step;
       n = min(step, n - k * step);
     }
-    b = __builtin_amdgcn_readfirstlane(lo);
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    if (lo != 0) load_window(lo);
+    const int k = max(__popcll(__ballot(lane < n && key(win_start, lo + lane) <= want)) - 1, 0);
+    b = __builtin_amdgcn_readfirstlane(lo + k);
+    const int64_t s0 = lane64(win_start, b - win), s1 = lane64(win_end, b - win);
+    if (cut.whole) {
+      at = s0 + (unit - key(s0, b)) * cut.per;
+      end = min(at + cut.per, s1);
+    } else {
+      at = want;
+      end = unit < a.units ? min(at + cut.per, total) : at;
+    }
   }
+  if (at >= end) return;
+  // whole units are segments; the others' are numbered unit + sequence
+  auto segment_of = [&](int bb) { return int64_t(unit) + (prefix || whole ? 0 : bb); };
 
   unsigned char* bufs = smem + g * NBUF * S::TILE;
   const uint32_t bufs_at = lds_address(bufs);
@@ -236,34 +277,49 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
     value_at = t * ROWB + (((lane >> 1) & 1) ^ joint_swap(G, t)) * 16 + 8 * (lane & 1);
   }
 
-  while (at < end) {
-    // ---- a segment: tiles t0 .. t1 - 1 of sequence b
-    int64_t first = 0, last = total;
-    int T = a.prefix_len;
+  // ---- a segment: tiles t0 .. t1 - 1 of sequence b; the next one's pages are on their way
+  // while this one is computed
+  struct Segment {
+    int b, t0, t1, T, ids;                            // ids: lane i the page of round (64-round window) + i
+  };
+  auto pages_of = [&](const Segment& sg, int r0) {
+    const int i = (r0 + lane) * NG + g + sg.t0;
+    const int id = i < sg.t1 ? a.table[(prefix ? 0 : int64_t(sg.b) * a.max_pages) + (i >> 1)] : -1;
+    return id >= a.num_pages ? -1 : id;
+  };
+  auto next_segment = [&]() {                         // the one that tile `at` is of
+    Segment sg{0, int(at), int(end), a.prefix_len, -1};
     if (!prefix) {
-      while (b + 1 < a.batch && a.start[b + 1] <= at) ++b;           // over sequences without tokens
-      first = a.start[b];
-      last = a.start[b + 1];
-      T = min(max(a.seq_lens[b], 0), a.max_context);
+      if (b - win >= 64) load_window(b);
+      int64_t s1 = lane64(win_end, b - win);
+      while (s1 <= at) {                              // over sequences without tokens
+        ++b;
+        if (b - win >= 64) load_window(b);
+        s1 = lane64(win_end, b - win);
+      }
+      const int64_t s0 = lane64(win_start, b - win);
+      sg = Segment{b, int(at - s0), int(min(end, s1) - s0), __builtin_amdgcn_readlane(win_len, b - win), -1};
     }
-    const int t0 = int(at - first), t1 = int(min(end, last) - first);
-    at = first + t1;
-    const int32_t* table = a.table + (prefix ? 0 : int64_t(b) * a.max_pages);
+    at += sg.t1 - sg.t0;
+    sg.ids = pages_of(sg, 0);
+    return sg;
+  };
+  Segment next = next_segment();
+  bool more = true;
+  while (more) {
+    const Segment sg = next;
+    const int T = sg.T, t0 = sg.t0, t1 = sg.t1;
+    int ids = sg.ids;
+    more = at < end;
+    if (more) next = next_segment();
     const int see_all = T - a.queries + 1;            // tokens that every row sees
-
     const int mine = t1 - t0 > g ? (t1 - t0 - g + NG - 1) / NG : 0;  // tiles of this group
     const int rounds = (t1 - t0 + NG - 1) / NG;
-    int ids = -1;                                     // lane i: the page of round (64-round window) + i
-    auto load_ids = [&](int r0) {
-      const int i = r0 + lane;
-      ids = i < mine ? table[(t0 + g + i * NG) >> 1] : -1;
-      if (ids >= a.num_pages) ids = -1;
-    };
     int scales_next = 0;
     auto issue = [&](int r, bool& valid) {            // the tile of round r into its buffer
       valid = false;
       if (r >= mine) return;
-      if ((r & 63) == 0) load_ids(r);
+      if (r > 0 && (r & 63) == 0) ids = pages_of(sg, r);
       const int page = __builtin_amdgcn_readlane(ids, r & 63);
       valid = page >= 0;
       if (!valid) return;
@@ -285,13 +341,19 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
     const int row = (slice * WR + rw) * 16 + lr;
     const int rowc = min(row, rows - 1);
     const uint8_t* qrow = static_cast<const uint8_t*>(a.q) +
-                          ((prefix ? 0 : int64_t(b) * rows) + rowc) * (W * 2);
-    u32x4 q[KS];
+                          ((prefix ? 0 : int64_t(sg.b) * rows) + rowc) * (W * 2);
+    u32x4 q[KQ];
 #pragma unroll
     for (int i = 0; i < KS; ++i) {
       const int col = C8 && (i | 1) < KS ? 64 * (i >> 1) + 16 * lq + 8 * (i & 1) : 32 * i + 8 * lq;
-      q[i] = *reinterpret_cast<const u32x4*>(qrow + 2 * col);
+      const u32x4 x = *reinterpret_cast<const u32x4*>(qrow + 2 * col);
+      if (i < KQ)
+        q[i] = x;
+      else if (g == 0)
+        last_q[rw][i - KQ][lane] = x;
     }
+    if constexpr (QL > 0 && WR == 1) __syncthreads();  // else the first tile's does it
+    auto query = [&](int i) { return i < KQ ? q[i < KQ ? i : 0] : last_q[rw][i < KQ ? 0 : i - KQ][lane]; };
     // tokens of the segment's sequence that the row sees
     int limit;
     if (prefix) {
@@ -388,17 +450,17 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
               if (i0 + i >= NP) continue;
               if constexpr (C8) {
                 const float f = 64 * (i0 + i) < R ? sc[n] : sk[n];
-                s[n] = mfma(widen(x[i][n][0], x[i][n][1], f), q[2 * (i0 + i)], s[n]);
-                s[n] = mfma(widen(x[i][n][2], x[i][n][3], f), q[2 * (i0 + i) + 1], s[n]);
+                s[n] = mfma(widen(x[i][n][0], x[i][n][1], f), query(2 * (i0 + i)), s[n]);
+                s[n] = mfma(widen(x[i][n][2], x[i][n][3], f), query(2 * (i0 + i) + 1), s[n]);
               } else {
-                s[n] = mfma(x[i][n], q[i0 + i], s[n]);
+                s[n] = mfma(x[i][n], query(i0 + i), s[n]);
               }
             }
           __builtin_amdgcn_sched_barrier(0);
         }
         if constexpr (C8 && KS % 2 == 1) {
 #pragma unroll
-          for (int n = 0; n < 2; ++n) s[n] = mfma(widen(last[n][0], last[n][1], sk[n]), q[KS - 1], s[n]);
+          for (int n = 0; n < 2; ++n) s[n] = mfma(widen(last[n][0], last[n][1], sk[n]), query(KS - 1), s[n]);
         }
         // ---- softmax
         auto exponents = [&](int n) { return *reinterpret_cast<const floatx4*>(&scale_of[w][16 * n + 4 * lq]); };
@@ -474,14 +536,15 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
         const uint32_t base = lds_address(buf);
         const int va = here(value_at);
         if constexpr (C8) {
-          unrolled<CT / 4>([&](auto k) {
-            constexpr int I = 4 * decltype(k)::value, M = G - 1;
-            u32x2 x[4];
-            read_tr8<I / G * (G * 16), (I + 1) / G * (G * 16), (I + 2) / G * (G * 16), (I + 3) / G * (G * 16)>(
-                x, base + (va ^ ((I & M) * 16)), base + (va ^ (((I + 1) & M) * 16)),
-                base + (va ^ (((I + 2) & M) * 16)), base + (va ^ (((I + 3) & M) * 16)));
+          unrolled<CT / 8>([&](auto k) {
+            constexpr int I = 8 * decltype(k)::value, M = G - 1;
+            u32x2 x[8];
+            auto at = [&](int j) { return base + (va ^ (((I + j) & M) * 16)); };
+            read_tr8<I / G * (G * 16), (I + 1) / G * (G * 16), (I + 2) / G * (G * 16), (I + 3) / G * (G * 16),
+                     (I + 4) / G * (G * 16), (I + 5) / G * (G * 16), (I + 6) / G * (G * 16), (I + 7) / G * (G * 16)>(
+                x, at(0), at(1), at(2), at(3), at(4), at(5), at(6), at(7));
 #pragma unroll
-            for (int j = 0; j < 4; ++j) acc[I + j] = mfma(widen(x[j][0], x[j][1], 1.f), p, acc[I + j]);
+            for (int j = 0; j < 8; ++j) acc[I + j] = mfma(widen(x[j][0], x[j][1], 1.f), p, acc[I + j]);
           });
         } else {
           unrolled<CT / 4>([&](auto k) {
@@ -506,7 +569,7 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
     // ---- the token groups' states, CJ columns at a time
     const int jt = here(tid), jr = jt & 15, jq = (jt >> 4) & 3;        // lane's row, quarter
     const bool mine_too = (slice * WR + rw) * 16 + jr < rows;
-    const int64_t seg = int64_t(unit) + (prefix ? 0 : b);
+    const int64_t seg = segment_of(sg.b);
     const int64_t prow = (seg * a.slices + slice) * (16 * WR);
     if constexpr (NG == 1) {
       if (mine_too) {
@@ -571,7 +634,9 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
 template <int R, int P, bool C8>
 hipError_t launch_rows(int row_waves, const JointAttend& a, hipStream_t stream) {
   const uint32_t threads = 64 * joint_waves(row_waves, joint_tile_bytes(R + P, C8));
-  const uint32_t groups = uint32_t((a.units + 7) / 8 * 8) * uint32_t(a.slices);
+  // a sequence more than a share's unit a sequence, at most
+  const uint32_t units = uint32_t(a.units) + (a.prefix_len > 0 ? 0 : uint32_t(a.batch));
+  const uint32_t groups = (units + 7) / 8 * 8 * uint32_t(a.slices);
   switch (row_waves) {
     case 1: hipLaunchKernelGGL((joint_attend<R, P, C8, 1>), dim3(groups), dim3(threads), 0, stream, a); break;
     case 2: hipLaunchKernelGGL((joint_attend<R, P, C8, 2>), dim3(groups), dim3(threads), 0, stream, a); break;

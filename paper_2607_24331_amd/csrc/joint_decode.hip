@@ -150,9 +150,9 @@ __global__ __launch_bounds__(R / 4 * GR) void joint_merge(FinishArgs a, float* _
   const int b = row / a.queries, i = row % a.queries;
   // shares: those of the sequence's units, then the prefix's
   const int64_t s0 = a.start[b], s1 = a.start[b + 1];
-  const int64_t per = joint_tiles_a_unit(a.start[a.batch], a.units, a.groups);
-  const int64_t u0 = s0 / per;
-  const int own = s1 > s0 ? int((s1 - 1) / per - u0) + 1 : 0;
+  const JointCut cut = joint_cut(a.start[a.batch], a.units, a.batch, a.groups);
+  const int64_t u0 = s0 / cut.per;
+  const int own = s1 <= s0 ? 0 : int(cut.whole ? (s1 - s0 + cut.per - 1) / cut.per : (s1 - 1) / cut.per - u0 + 1);
   int pre = 0;
   if (a.prefix_len > 0) {
     const int64_t tiles = (a.prefix_len + kJointTile - 1) / kJointTile;
@@ -315,11 +315,11 @@ int groups_of(const dckv_joint_desc& d, int row_waves) {
   return joint_waves(row_waves, joint_tile_bytes(d.rank + d.rope_dim, d.cache == DCKV_JOINT_E4M3)) / row_waves;
 }
 
-// Units of a slice for at most `tiles` tiles: fill the chip with the slices, a round
-// of the token groups at least, none more than the join holds.
-int units_of(int rank, int64_t slices, int64_t tiles, int groups) {
+// Units of a slice for at most `tiles` tiles: fill the chip with the slices, no more than
+// the join holds.
+int units_of(int rank, int64_t slices, int64_t tiles) {
   const int64_t want = std::min<int64_t>(std::max<int64_t>(1, (fill(rank) + slices / 2) / slices), kJointMaxUnits);
-  return int(std::max<int64_t>(1, std::min(want, (tiles + groups - 1) / groups)));
+  return int(std::max<int64_t>(1, std::min(want, tiles)));
 }
 
 template <int R, int D>
@@ -365,11 +365,11 @@ JointShape joint_shape(const dckv_joint_desc& d, int32_t queries, int32_t batch,
   s.row_waves = row_waves_of(s.rows);
   s.slices = (s.rows + 16 * s.row_waves - 1) / (16 * s.row_waves);
   const int64_t tiles = int64_t(batch) * tiles_of(max_context);
-  s.units = units_of(d.rank, s.slices, tiles, groups_of(d, s.row_waves));
+  s.units = units_of(d.rank, s.slices, tiles);
   const int64_t all = int64_t(s.rows) * batch;
   s.pre_row_waves = row_waves_of(all);
   s.pre_slices = int32_t((all + 16 * s.pre_row_waves - 1) / (16 * s.pre_row_waves));
-  s.pre_units = prefix_len > 0 ? units_of(d.rank, s.pre_slices, tiles_of(prefix_len), groups_of(d, s.pre_row_waves)) : 0;
+  s.pre_units = prefix_len > 0 ? units_of(d.rank, s.pre_slices, tiles_of(prefix_len)) : 0;
   const size_t width = size_t(d.rank + d.rope_dim);
   s.off_start = align_up(size_t(all) * width * 2);
   s.off_mean = s.off_start + align_up(size_t(batch + 1) * 8);
