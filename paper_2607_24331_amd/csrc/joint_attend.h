@@ -60,6 +60,13 @@ __device__ __forceinline__ void load_lds16(const uint8_t* base, uint32_t lane_at
 #endif
 }
 
+__device__ __forceinline__ void load_lds4(const uint8_t* base, uint32_t lane_at, uint32_t lds) {
+#ifdef __HIP_DEVICE_COMPILE__
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
+               :: "s"(lds), "v"(lane_at), "s"(base) : "memory", "m0");
+#endif
+}
+
 // Eight e4m3 values times `scale`, a power of two, as bf16.
 __device__ __forceinline__ u32x4 widen(uint32_t lo, uint32_t hi, float scale) {
   return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false)),
@@ -149,10 +156,15 @@ __device__ __forceinline__ int here(int x) {
   return x;
 }
 
-// Over the four lanes that hold a row.
+// The greatest over the four lanes that hold a row (lanes 16 and 32 apart), by moves
+// between vector registers: shuffles would each wait for LDS.
 __device__ __forceinline__ float row_max(float x) {
-  x = fmaxf(x, __shfl_xor(x, 16));
-  return fmaxf(x, __shfl_xor(x, 32));
+  uint32_t u = __float_as_uint(x);
+  auto p = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  x = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+  u = __float_as_uint(x);
+  p = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
 }
 
 // Tokens of a 16-byte piece that are not finite (bf16) or NaN (e4m3).
@@ -194,9 +206,10 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
   constexpr int W = S::W, ROWB = S::ROWB, G = S::G, NG = S::NG, NW = S::NW, NBUF = S::NBUF, LOADS = S::LOADS;
   constexpr int KS = W / 32, CT = R / 16;             // steps of the scores, column tiles of the sums
   __shared__ __align__(1024) unsigned char smem[S::LDS];
-  __shared__ float scale_of[C8 ? NW : 1][kJointTile];  // a wave's tile: exponents of its latents
   constexpr int QL = S::QL, KQ = W / 32 - QL;
   __shared__ u32x4 last_q[QL > 0 ? WR : 1][QL > 0 ? QL : 1][64];
+  // exponents of a tile: 32 bytes of latents, 32 of keys (and what lies behind them)
+  __shared__ __align__(256) uint8_t exps[C8 ? NG * NBUF : 1][C8 ? 256 : 1];
   __shared__ uint32_t odd_of[2][NW];                  // tokens of a tile's edge that hold a NaN, by loading wave
   __shared__ float join_m[NW][16], join_l[NW][16], join_u[NW][16];
 
@@ -315,7 +328,6 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
     const int see_all = T - a.queries + 1;            // tokens that every row sees
     const int mine = t1 - t0 > g ? (t1 - t0 - g + NG - 1) / NG : 0;  // tiles of this group
     const int rounds = (t1 - t0 + NG - 1) / NG;
-    int scales_next = 0;
     auto issue = [&](int r, bool& valid) {            // the tile of round r into its buffer
       valid = false;
       if (r >= mine) return;
@@ -330,9 +342,11 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
       for (int i = 0; i < LOADS; ++i)
         if (S::NL % WR == 0 || i < LOADS - 1 || i * WR + rw < S::NL)
           load_lds16(src + i * (WR * 1024), ln * 16, dst + i * (WR * 1024));
-      if constexpr (C8)                               // lanes 0 .. 31 the latents' exponents, 32 .. the keys'
-        scales_next = a.pool[int64_t(page) * a.page_bytes + DCKV_PAGE_TOKENS * (W + (ln >> 5)) + half * kJointTile +
-                             (ln & 31)];
+      if constexpr (C8) {                             // lanes 0 .. 7 the latents' exponents, 8 .. 15 the keys'
+        if (rw == 0)
+          load_lds4(a.pool + int64_t(page) * a.page_bytes + DCKV_PAGE_TOKENS * W + half * kJointTile,
+                    (ln & 8) * 8 + (ln & 7) * 4, lds_address(exps[g * NBUF + (r & (NBUF - 1))]));
+      }
     };
     bool valid = false, next_valid = false;
     issue(0, next_valid);
@@ -374,7 +388,6 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
       unsigned char* buf = bufs + (r & (NBUF - 1)) * S::TILE;
       valid = next_valid;
       const int pos = (t0 + g + r * NG) * kJointTile;  // the tile's first token
-      const int scales = scales_next;
       loads_done();                                   // this wave's part of the tile is in LDS
       const bool edge = valid && pos + kJointTile > see_all;
       uint32_t odd = 0;
@@ -422,6 +435,14 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
               if (i0 + i < NP) x[i][n] = *reinterpret_cast<const u32x4*>(buf + place<G>(ka, i0 + i) + n * 16 * ROWB);
         };
         float sc[2] = {1.f, 1.f}, sk[2] = {1.f, 1.f};  // powers of two of tokens lr, 16 + lr: latent, key
+        const uint8_t* ep = exps[C8 ? g * NBUF + (r & (NBUF - 1)) : 0];
+        if constexpr (C8) {
+#pragma unroll
+          for (int n = 0; n < 2; ++n) {
+            sc[n] = __uint_as_float(uint32_t(ep[16 * n + here(lr)]) << 23);
+            sk[n] = __uint_as_float(uint32_t(ep[32 + 16 * n + here(lr)]) << 23);
+          }
+        }
         u32x4 x0[GP][2], x1[GP][2];
         u32x2 last[2];
         read_keys(x0, 0);
@@ -431,12 +452,6 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
 #pragma unroll
             for (int n = 0; n < 2; ++n) last[n] = *reinterpret_cast<const u32x2*>(buf + at8 + n * 16 * ROWB);
           }
-#pragma unroll
-          for (int n = 0; n < 2; ++n) {
-            sc[n] = __uint_as_float(uint32_t(__shfl(scales, 16 * n + lr)) << 23);
-            sk[n] = __uint_as_float(uint32_t(__shfl(scales, 32 + 16 * n + lr)) << 23);
-          }
-          if (lane < 32) scale_of[w][lane] = float(scales) - 127.f;
         }
 #pragma unroll
         for (int i0 = 0; i0 < NP; i0 += GP) {
@@ -463,7 +478,13 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
           for (int n = 0; n < 2; ++n) s[n] = mfma(widen(last[n][0], last[n][1], sk[n]), query(KS - 1), s[n]);
         }
         // ---- softmax
-        auto exponents = [&](int n) { return *reinterpret_cast<const floatx4*>(&scale_of[w][16 * n + 4 * lq]); };
+        auto exponents = [&](int n) {                 // of the tokens' latents
+          const uint32_t four = *reinterpret_cast<const uint32_t*>(ep + 16 * n + 4 * here(lq));
+          floatx4 e;
+#pragma unroll
+          for (int v = 0; v < 4; ++v) e[v] = float((four >> (8 * v)) & 0xFFu) - 127.f;
+          return e;
+        };
 #pragma unroll
         for (int n = 0; n < 2; ++n)
 #pragma unroll

@@ -495,7 +495,9 @@ __global__ __launch_bounds__(256, 2) void prompt_attend(PromptArgs a, const uint
     for (int n = 0; n < 2; ++n)
 #pragma unroll
       for (int v = 0; v < 16; ++v) top = fmaxf(top, s[n][v]);
-    top = fmaxf(top, __shfl_xor(top, 32));
+    const uint32_t u = __float_as_uint(top);           // the other half's, by a move between registers
+    const auto both = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
     if (__any(top > m + kSlack)) {
       const float m_new = fmaxf(m, top);
       const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m_new);
