@@ -31,6 +31,7 @@
 
 #include "device.h"
 #include "joint.h"
+#include "lds.h"
 
 namespace dckv {
 namespace joint {
@@ -49,24 +50,6 @@ __device__ __forceinline__ floatx4 mfma(u32x4 a, u32x4 b, floatx4 c) {
                                                  0, 0, 0);
 }
 
-// 16 bytes a lane from global memory (base, uniform, + lane_at) to LDS, in lane order from
-// `lds` on.  Written out, as is the wait for them (loads_done): the compiler cannot tell
-// which buffer such a load fills and lets every LDS read wait for it.  It writes no
-// register.
-__device__ __forceinline__ void load_lds16(const uint8_t* base, uint32_t lane_at, uint32_t lds) {
-#ifdef __HIP_DEVICE_COMPILE__
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-               :: "s"(lds), "v"(lane_at), "s"(base) : "memory", "m0");
-#endif
-}
-
-__device__ __forceinline__ void load_lds4(const uint8_t* base, uint32_t lane_at, uint32_t lds) {
-#ifdef __HIP_DEVICE_COMPILE__
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
-               :: "s"(lds), "v"(lane_at), "s"(base) : "memory", "m0");
-#endif
-}
-
 // Eight e4m3 values times `scale`, a power of two, as bf16.
 __device__ __forceinline__ u32x4 widen(uint32_t lo, uint32_t hi, float scale) {
   return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false)),
@@ -83,16 +66,6 @@ __device__ __forceinline__ uint32_t pair(float a, float b) {
 // Values of four column tiles for the matrix unit, by the transposing LDS loads.  Written
 // out, with a wait of their own: the compiler waits for every load in flight, the next
 // tile's among them, before such a load.  a[j]: this lane's address for tile j, O* bytes on.
-__device__ __forceinline__ uint32_t lds_address(unsigned char* p) {
-  return uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) unsigned char*)(p)));
-}
-// Every load of the wave has landed: those written out, and those that the compiler knows of
-// (in a loop it would otherwise wait again for what was loaded before the loop).
-__device__ __forceinline__ void loads_done() {
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  __builtin_amdgcn_s_waitcnt(0x0F70);                // vmcnt(0)
-}
-
 template <int O0, int O1, int O2, int O3, int HALF>
 __device__ __forceinline__ void read_tr16(u32x4 (&f)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
   u32x2 x0 = {}, x1 = {}, x2 = {}, x3 = {}, z0 = {}, z1 = {}, z2 = {}, z3 = {};

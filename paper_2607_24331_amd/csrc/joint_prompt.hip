@@ -8,7 +8,7 @@
 //                  and the tiles of 128 rows, those with the most tokens first.
 //   prompt_gather  a work-group 16 tokens: latents in bf16 side by side, position keys
 //                  as the attention's LDS wants them, and which tokens are there and finite.
-//   prompt_expand  every head's keys and values, a 128 x 128 product tile a work-group on
+//   prompt_expand  every head's keys and values, a 256 x 256 product tile a work-group on
 //                  MFMA 16x16x32; the latents' and factors' rows come by the loads' LDS path.
 //                  Keys go out a token's coordinates side by side, values a coordinate's
 //                  tokens, both in the order in which a lane of the attention needs them
@@ -24,6 +24,7 @@
 
 #include "device.h"
 #include "joint.h"
+#include "lds.h"
 
 namespace dckv {
 namespace {
@@ -93,6 +94,7 @@ __global__ __launch_bounds__(1024) void prompt_plan(PromptArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   for (int i = tid; i < kBins; i += N) bins[i] = 0;
   const int most = (a.max_context + kTok - 1) / kTok + 1;
+  int all_toks = 0, all_rows = 0;         // of the round's sequences
   // two walks over the sequences, 1024 at a time: the first counts row tiles by their
   // tokens, the second writes them, most tokens first (which place a tile takes among
   // those of a bin does not change what it computes)
@@ -100,41 +102,44 @@ __global__ __launch_bounds__(1024) void prompt_plan(PromptArgs a) {
     int toks = 0;                         // token tiles of the sequences before
     int64_t len = 0;                      // their tokens
     for (int b0 = 0; b0 < a.batch; b0 += N) {
-      const int b = b0 + tid;
-      int lo = 0, n = 0, T = 0;
-      if (b < a.batch) {
-        lo = min(max(a.row_start[b], 0), a.n_rows);
-        n = min(max(a.row_start[b + 1], lo), a.n_rows) - lo;
-        T = n > 0 ? min(max(a.seq_lens[b], 0), a.max_context) : 0;
+      if (walk == 0 || a.batch > N) {     // a batch of one round is still there
+        const int b = b0 + tid;
+        int lo = 0, n = 0, T = 0;
+        if (b < a.batch) {
+          lo = min(max(a.row_start[b], 0), a.n_rows);
+          n = min(max(a.row_start[b + 1], lo), a.n_rows) - lo;
+          T = n > 0 ? min(max(a.seq_lens[b], 0), a.max_context) : 0;
+        }
+        const int64_t len_to = wave_scan(int64_t(T), lane);
+        if (lane == 63) wave_len[w] = len_to;
+        __syncthreads();
+        int64_t before = len;
+        for (int i = 0; i < w; ++i) before += wave_len[i];
+        for (int i = 0; i < 16; ++i) len += wave_len[i];
+        const bool fits = before + len_to <= a.total_context;
+        const int own = fits ? (T + kTok - 1) / kTok : 0;
+        const int toks_to = wave_scan(own, lane), rows_to = wave_scan((n + kRows - 1) / kRows, lane);
+        if (lane == 63) {
+          wave_toks[w] = toks_to;
+          wave_rows[w] = rows_to;
+        }
+        __syncthreads();
+        int tok_at = toks_to, row_at = rows_to;
+        all_toks = all_rows = 0;
+        for (int i = 0; i < 16; ++i) {
+          if (i < w) tok_at += wave_toks[i], row_at += wave_rows[i];
+          all_toks += wave_toks[i];
+          all_rows += wave_rows[i];
+        }
+        row_end[tid] = row_at;
+        tok_end[tid] = tok_at;
+        lo_of[tid] = lo;
+        n_of[tid] = n;
+        len_of[tid] = T;
+        // its token tiles have room always, where row_start ascends
+        kv_of[tid] = fits && toks + tok_at <= a.kv_tiles ? toks + tok_at - own : -1;
+        __syncthreads();
       }
-      const int64_t len_to = wave_scan(int64_t(T), lane);
-      if (lane == 63) wave_len[w] = len_to;
-      __syncthreads();
-      int64_t before = len;
-      for (int i = 0; i < w; ++i) before += wave_len[i];
-      for (int i = 0; i < 16; ++i) len += wave_len[i];
-      const bool fits = before + len_to <= a.total_context;
-      const int own = fits ? (T + kTok - 1) / kTok : 0;
-      const int toks_to = wave_scan(own, lane), rows_to = wave_scan((n + kRows - 1) / kRows, lane);
-      if (lane == 63) {
-        wave_toks[w] = toks_to;
-        wave_rows[w] = rows_to;
-      }
-      __syncthreads();
-      int tok_at = toks_to, row_at = rows_to, all_toks = 0, all_rows = 0;
-      for (int i = 0; i < 16; ++i) {
-        if (i < w) tok_at += wave_toks[i], row_at += wave_rows[i];
-        all_toks += wave_toks[i];
-        all_rows += wave_rows[i];
-      }
-      row_end[tid] = row_at;
-      tok_end[tid] = tok_at;
-      lo_of[tid] = lo;
-      n_of[tid] = n;
-      len_of[tid] = T;
-      // its token tiles have room always, where row_start ascends
-      kv_of[tid] = fits && toks + tok_at <= a.kv_tiles ? toks + tok_at - own : -1;
-      __syncthreads();
       for (int x = tid; x < all_rows; x += N) {
         const int s = find_end(row_end, N, x);
         const int n_s = n_of[s], T_s = len_of[s], i = x - (row_end[s] - (n_s + kRows - 1) / kRows);
@@ -249,115 +254,131 @@ __global__ __launch_bounds__(256) void prompt_gather(PromptArgs a, GatherArgs s)
   }
 }
 
-__device__ __forceinline__ void load_lds16(const void* g, unsigned char* p) {
-  __builtin_amdgcn_global_load_lds(static_cast<const uint8_t*>(g), p, 16, 0, 0);
+// 32 NT tokens x 256 of the heads' key and value coordinates: a head's keys and values (D =
+// 128), or two heads'.  Eight waves, 16 NT tokens x 64 coordinates each, k in stages of 64 in
+// two buffers.  LDS rows of 128 bytes, piece i of row s at i ^ s % 8.  With NT = 8 a stage takes about as
+// long in the products (2 x 64 x 16 cycles a SIMD) as in LDS (192 KB of operands, 64 KB of stage).
+// ROWS tiles of 16 rows and COLS of 16 columns: coordinates by tokens for keys, tokens by
+// coordinates for values, so that a lane ends up with what lies together in an LDS tile of
+// the attention.
+template <int ROWS, int COLS>
+__device__ __forceinline__ void expand_stage(floatx4 (&acc)[ROWS][COLS], const unsigned char* rows,
+                                             const unsigned char* cols, int lr, int lq) {
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int p = lr * 128 + ((4 * k + lq) ^ (lr & 7)) * 16;
+    u32x4 x[ROWS], y[COLS];
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) x[i] = *reinterpret_cast<const u32x4*>(rows + i * 2048 + p);
+#pragma unroll
+    for (int j = 0; j < COLS; ++j) y[j] = *reinterpret_cast<const u32x4*>(cols + j * 2048 + p);
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i)
+#pragma unroll
+      for (int j = 0; j < COLS; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x[i]),
+                                                            __builtin_bit_cast(bf16x8, y[j]), acc[i][j], 0, 0, 0);
+  }
 }
 
-// 128 tokens x 128 of the heads' key and value coordinates, 64 x 64 a wave; k in stages
-// of 64 in two buffers.  LDS rows of 128 bytes, piece i of row s at i ^ s % 8.
-template <int D>
-__global__ __launch_bounds__(256, 2) void prompt_expand(const int32_t* __restrict__ counts,
-                                                        const bf16* __restrict__ c,
-                                                        const bf16* __restrict__ W_keys,
-                                                        const bf16* __restrict__ W_values, int heads, int r,
-                                                        int kv_tiles, uint8_t* __restrict__ keys,
-                                                        uint8_t* __restrict__ values) {
-  constexpr int HALF = 128 * 128, BUF = 2 * HALF;
+template <int D, int NT>
+__global__ __launch_bounds__(512) void prompt_expand(const int32_t* __restrict__ counts,
+                                                     const bf16* __restrict__ c, const bf16* __restrict__ W_keys,
+                                                     const bf16* __restrict__ W_values, int heads, int r,
+                                                     int kv_tiles, uint8_t* __restrict__ keys,
+                                                     uint8_t* __restrict__ values) {
+  constexpr int TOK = 32 * NT, BUF = (TOK + 256) * 128;
   __shared__ __align__(1024) unsigned char smem[2 * BUF];
-  const int tiles = D == 128 ? 2 * heads : heads;      // of 128 coordinates
+  const int tiles = D == 128 ? heads : (heads + 1) / 2;  // of 256 coordinates
   const int f = blockIdx.x % tiles, blk = blockIdx.x / tiles;
-  const int n_tok = counts[1] * kTok;
-  if (blk * 128 >= n_tok) return;
+  const int n_tiles = counts[1];
+  if (blk * TOK >= n_tiles * kTok) return;
   const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lq = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wt = w & 1, wf = w >> 1;                   // this wave's 64 tokens, 64 coordinates
-  const int head = D == 128 ? f >> 1 : f;
-  // rows of a stage: 128 tokens, 128 coordinates; a load brings 8 of them
-  const int row = lane >> 3, piece = (lane & 7) ^ row;
-  const bf16* src[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int n = (8 * w + i) * 8 + row;               // waves 0, 1 the tokens, 2, 3 the coordinates
-    if (w < 2) {
-      src[i] = c + int64_t(min(blk * 128 + n, n_tok - 1)) * r;
-    } else {
-      const int k = n - 128;
-      const bf16* W = (D == 128 ? f & 1 : k >= 64) ? W_values : W_keys;
-      src[i] = W + (int64_t(head) * D + (D == 128 ? k : k & 63)) * r;
-    }
-    src[i] += 8 * piece;
-  }
+  const int wt = w & 1, wf = w >> 1;                   // this wave's 16 NT tokens, 64 coordinates
+  // what coordinates 64 x .. + 63 of the block are
+  auto head_of = [&](int x) { return D == 128 ? f : 2 * f + (x >> 1); };
+  auto value_of = [&](int x) { return D == 128 ? x >> 1 : x & 1; };
+  // loads of 8 rows: waves 0 .. 3 bring the tokens (the workspace has whole blocks), 4 .. 7 the
+  // coordinates
+  const int x = w & 3;
+  const bf16* base = w < 4 ? c + (int64_t(blk) * TOK + x * (8 * NT)) * r
+                           : (value_of(x) ? W_values : W_keys) +
+                                 (int64_t(min(head_of(x), heads - 1)) * D + (D == 128 ? (x & 1) * 64 : 0)) * r;
+  const uint32_t lane_at = (lane >> 3) * (r * 2) + ((lane & 7) ^ (lane >> 3)) * 16;
+  const uint32_t dst = lds_address(smem) + (w < 4 ? x * NT : 4 * NT + x * 8) * 1024;
   auto issue = [&](int st) {
-    unsigned char* dst = smem + (st & 1) * BUF + w * 8192;
+    const uint8_t* src = reinterpret_cast<const uint8_t*>(base + st * 64);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) load_lds16(src[i] + st * 64, dst + i * 1024);
+    for (int i = 0; i < 8; ++i)
+      if (i < NT || w >= 4) load_lds16(src + i * (16 * r), lane_at, dst + (st & 1) * BUF + i * 1024);
   };
-  const bool value = D == 128 ? f & 1 : wf == 1;       // what this wave forms
-  floatx4 acc[4][4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-  // rows of the product are coordinates for keys, tokens for values
-  const int arow = (value ? 0 : 128) + (value ? wt : wf) * 64, brow = (value ? 128 : 0) + (value ? wf : wt) * 64;
   const int nst = r / 64;
   issue(0);
-  for (int st = 0; st < nst; ++st) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();                                   // the stage is whole, the one before is used up
-    if (st + 1 < nst) issue(st + 1);
-    unsigned char* buf = smem + (st & 1) * BUF;
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      u32x4 x[4], y[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int p = ((4 * k + lq) ^ (lr & 7)) * 16;
-        x[i] = *reinterpret_cast<const u32x4*>(buf + (arow + 16 * i + lr) * 128 + p);
-        y[i] = *reinterpret_cast<const u32x4*>(buf + (brow + 16 * i + lr) * 128 + p);
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x[i]),
-                                                              __builtin_bit_cast(bf16x8, y[j]), acc[i][j], 0, 0, 0);
+  const int head = head_of(wf);
+  const bool value = value_of(wf);
+  const int tok_row = wt * (16 * NT) * 128, coord_row = (TOK + wf * 64) * 128;
+  auto stages = [&](auto& acc, int rows, int cols) {
+    for (int st = 0; st < nst; ++st) {
+      loads_done();
+      __syncthreads();                                 // the stage is whole, the one before is used up
+      if (st + 1 < nst) issue(st + 1);
+      unsigned char* buf = smem + (st & 1) * BUF;
+      expand_stage(acc, buf + rows, buf + cols, lr, lq);
     }
-  }
+  };
   // a lane holds rows 16 i + 4 lq + v of column 16 j + lr; pieces 4 s + lq of a column hold
   // its rows 32 s + 4 lq + 0 .. 3 and 32 s + 16 + 4 lq + 0 .. 3
-  const int tile = blk * 2 + wt;                       // of 64 tokens
-  if (tile * kTok >= n_tok) return;
-  uint8_t* out = (value ? values : keys) + (int64_t(head) * kv_tiles + tile) * (kTok * D * 2);
-  const int col0 = value ? (D == 128 ? wf * 64 : 0) : 0;     // a value tile's first coordinate
-  const int s0 = value ? 0 : (D == 128 ? wf * 2 : 0);        // a key's first 32 coordinates
+  const int64_t tile0 = int64_t(min(head, heads - 1)) * kv_tiles;
+  const int tok0 = blk * TOK + wt * (16 * NT);
+  const bool live = head < heads;
   constexpr int KG = D == 128 ? 16 : 8;
+  if (!value) {
+    floatx4 acc[4][NT];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int col = col0 + 16 * j + lr;
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      floatx4 lo = acc[2 * s][j], hi = acc[2 * s + 1][j];
-      if (value)
+      for (int j = 0; j < NT; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+    stages(acc, coord_row, tok_row);
+    if (!live) return;
+    const int s0 = D == 128 ? (wf & 1) * 2 : 0;        // the key's first 32 coordinates
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      const int tok = tok0 + 16 * j + lr;
+      uint8_t* out = keys + (tile0 + (tok >> 6)) * (kTok * D * 2) + (tok & 63) * (D * 2);
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const floatx4 lo = acc[2 * s][j], hi = acc[2 * s + 1][j];
+        *reinterpret_cast<u32x4*>(out + ((4 * (s0 + s) + lq) ^ joint_swap(KG, tok & 63)) * 16) =
+            u32x4{pair(lo[0], lo[1]), pair(lo[2], lo[3]), pair(hi[0], hi[1]), pair(hi[2], hi[3])};
+      }
+    }
+  } else {
+    floatx4 acc[NT][4];
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+    stages(acc, tok_row, coord_row);
+    if (!live) return;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int col = (D == 128 ? (wf & 1) * 64 : 0) + 16 * j + lr;
+#pragma unroll
+      for (int s = 0; s < NT / 2; ++s) {
+        const int tok = tok0 + 32 * s;
+        floatx4 lo = acc[2 * s][j], hi = acc[2 * s + 1][j];
 #pragma unroll
         for (int v = 0; v < 4; ++v) {                  // a weight of 0 times an infinity would be none
           lo[v] = fminf(fmaxf(lo[v], -kMaxBf16), kMaxBf16);
           hi[v] = fminf(fmaxf(hi[v], -kMaxBf16), kMaxBf16);
         }
-      const u32x4 x = {pair(lo[0], lo[1]), pair(lo[2], lo[3]), pair(hi[0], hi[1]), pair(hi[2], hi[3])};
-      const int piece = 4 * (s0 + s) + lq;
-      const int at = value ? col * (kTok * 2) + (piece ^ joint_swap(8, col)) * 16
-                           : col * (D * 2) + (piece ^ joint_swap(KG, col)) * 16;
-      *reinterpret_cast<u32x4*>(out + at) = x;
+        *reinterpret_cast<u32x4*>(values + (tile0 + (tok >> 6)) * (kTok * D * 2) + col * (kTok * 2) +
+                                  ((4 * (tok >> 5 & 1) + lq) ^ joint_swap(8, col)) * 16) =
+            u32x4{pair(lo[0], lo[1]), pair(lo[2], lo[3]), pair(hi[0], hi[1]), pair(hi[2], hi[3])};
+      }
     }
   }
-}
-
-// Every load of the wave has landed, and the compiler knows it.
-__device__ __forceinline__ void loads_done() {
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt(0x0F70);                  // vmcnt(0)
-  asm volatile("" ::: "memory");
 }
 
 // LDS reads and products of one phase, `ahead` reads on their way.
@@ -396,21 +417,19 @@ __global__ __launch_bounds__(256, 2) void prompt_attend(PromptArgs a, const uint
   const int limit = rt.first + my + 1;                 // tokens that the row sees
   const int all = rt.first + rt.n;                     // that the last row sees
   const int tiles = rt.kv < 0 || all <= 0 ? 0 : (all + kTok - 1) / kTok;
-  const uint8_t* ksrc = keys + (int64_t(head) * a.kv_tiles + rt.kv) * KB + lane * 16;
-  const uint8_t* vsrc = values + (int64_t(head) * a.kv_tiles + rt.kv) * KB + lane * 16;
-  const uint8_t* psrc = rope + int64_t(rt.kv) * PB + lane * 16;
+  const uint8_t* ksrc = keys + (int64_t(head) * a.kv_tiles + rt.kv) * KB + w * 1024;
+  const uint8_t* vsrc = values + (int64_t(head) * a.kv_tiles + rt.kv) * KB + w * 1024;
+  const uint8_t* psrc = rope + int64_t(rt.kv) * PB + w * 1024;
+  const uint32_t smem_at = lds_address(smem) + w * 1024, lane_at = lane * 16;
   // keys, position keys, values; every wave a quarter of each
   auto issue = [&](int t) {
-    unsigned char* dst = smem + (t & 1) * TILE + w * 1024;
-    const uint8_t* ks = ksrc + int64_t(t) * KB + w * 1024;
-    const uint8_t* vs = vsrc + int64_t(t) * KB + w * 1024;
-    const uint8_t* ps = psrc + int64_t(t) * PB + w * 1024;
+    const uint32_t dst = smem_at + (t & 1) * TILE;
 #pragma unroll
-    for (int i = 0; i < KL / 4; ++i) load_lds16(ks + i * 4096, dst + i * 4096);
+    for (int i = 0; i < KL / 4; ++i) load_lds16(ksrc + int64_t(t) * KB + i * 4096, lane_at, dst + i * 4096);
 #pragma unroll
-    for (int i = 0; i < PL / 4; ++i) load_lds16(ps + i * 4096, dst + KB + i * 4096);
+    for (int i = 0; i < PL / 4; ++i) load_lds16(psrc + int64_t(t) * PB + i * 4096, lane_at, dst + KB + i * 4096);
 #pragma unroll
-    for (int i = 0; i < KL / 4; ++i) load_lds16(vs + i * 4096, dst + KB + PB + i * 4096);
+    for (int i = 0; i < KL / 4; ++i) load_lds16(vsrc + int64_t(t) * KB + i * 4096, lane_at, dst + KB + PB + i * 4096);
   };
   static_assert(KL % 4 == 0 && PL % 4 == 0, "whole loads a wave");
   // which tokens are there and finite: on their way before a tile is
@@ -559,7 +578,7 @@ JointPrompt joint_prompt(const dckv_joint_desc& d, int32_t batch, int32_t n_rows
   const int64_t some = std::min(batch, n_rows);
   s.q_tiles = n_rows / kRows + some;
   s.kv_tiles = std::min<int64_t>(total_context / kTok + some, some * ((int64_t(max_context) + kTok - 1) / kTok));
-  s.kv_tiles = (s.kv_tiles + 1) / 2 * 2;               // whole blocks of 128 tokens
+  s.kv_tiles = (s.kv_tiles + 3) / 4 * 4;               // whole blocks of 256 tokens
   const size_t kv = size_t(s.kv_tiles);
   s.off_qtile = 256;
   s.off_kvtile = s.off_qtile + align_up(size_t(s.q_tiles) * sizeof(RowTile));
@@ -609,15 +628,24 @@ hipError_t launch_joint_prefill(const JointPrompt& s, const void* q, const int32
       hipLaunchKernelGGL((prompt_gather<false>), dim3(uint32_t(s.kv_tiles) * 4), dim3(256), 0, stream, a, ga);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
-    const uint32_t blocks = uint32_t(s.kv_tiles / 2) * (d.head_dim == 128 ? 2 : 1) * d.num_heads;
-#define DCKV_GO(D)                                                                                          \
-  hipLaunchKernelGGL((prompt_expand<D>), dim3(blocks), dim3(256), 0, stream, a.counts, c,                    \
-                     static_cast<const bf16*>(W_keys), static_cast<const bf16*>(W_values), d.num_heads,      \
-                     d.rank, a.kv_tiles, keys, values)
-    if (d.head_dim == 128)
-      DCKV_GO(128);
-    else
-      DCKV_GO(64);
+    // 256 coordinates a work-group, and 256 tokens where that fills the chip, else 64: ... 
+    const int64_t coords = d.head_dim == 128 ? d.num_heads : (d.num_heads + 1) / 2;
+    const bool wide = s.kv_tiles / 4 * coords >= 256;
+#define DCKV_GO(D, NT)                                                                                      \
+  hipLaunchKernelGGL((prompt_expand<D, NT>), dim3(uint32_t(s.kv_tiles / (NT / 2) * coords)), dim3(512), 0,   \
+                     stream, a.counts, c, static_cast<const bf16*>(W_keys),                                  \
+                     static_cast<const bf16*>(W_values), d.num_heads, d.rank, a.kv_tiles, keys, values)
+    if (d.head_dim == 128) {
+      if (wide)
+        DCKV_GO(128, 8);
+      else
+        DCKV_GO(128, 2);
+    } else {
+      if (wide)
+        DCKV_GO(64, 8);
+      else
+        DCKV_GO(64, 2);
+    }
 #undef DCKV_GO
     e = hipGetLastError();
     if (e != hipSuccess) return e;
