@@ -463,7 +463,6 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
 #pragma unroll
           for (int v = 0; v < 4; ++v) {
             s[n][v] *= a.scale;
-            s[n][v] += s[n][v] - s[n][v];              // an infinite score becomes NaN
           }
         if (edge) {
 #pragma unroll

@@ -461,6 +461,7 @@ __global__ __launch_bounds__(256, 2) void prompt_attend(PromptArgs a, const uint
 #pragma unroll
     for (int v = 0; v < 16; ++v) acc[i][v] = 0.f;
   float m = -INFINITY, l = 0.f;
+  const float slack = kSlack / scale;
   const int ksw = joint_swap(KG, lr), psw = P > 0 ? joint_swap(PG, lr) : 0, vsw = joint_swap(8, lr);
 
   for (int t = 0; t < tiles; ++t) {
@@ -491,14 +492,7 @@ __global__ __launch_bounds__(256, 2) void prompt_attend(PromptArgs a, const uint
     }
     reads_ahead<2 * (DS + PS), 4>();
     __builtin_amdgcn_sched_barrier(0);
-    // ---- softmax; an infinite score becomes NaN
-#pragma unroll
-    for (int n = 0; n < 2; ++n)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        s[n][v] *= scale;
-        s[n][v] += s[n][v] - s[n][v];
-      }
+    // ---- softmax, scores and maxima before their scale
     if (edge) {
 #pragma unroll
       for (int n = 0; n < 2; ++n)
@@ -517,9 +511,9 @@ __global__ __launch_bounds__(256, 2) void prompt_attend(PromptArgs a, const uint
     const uint32_t u = __float_as_uint(top);           // the other half's, by a move between registers
     const auto both = __builtin_amdgcn_permlane32_swap(u, u, false, false);
     top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
-    if (__any(top > m + kSlack)) {
+    if (__any(top > m + slack)) {
       const float m_new = fmaxf(m, top);
-      const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m_new);
+      const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - m_new) * scale);
       l *= keep;
       if (t > 0) {
 #pragma unroll
@@ -529,16 +523,18 @@ __global__ __launch_bounds__(256, 2) void prompt_attend(PromptArgs a, const uint
       }
       m = m_new;
     }
-    const float mb = m == -INFINITY ? 0.f : m;
+    const float mb = m == -INFINITY ? 0.f : m * scale;
     u32x4 p[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k)                        // step k: tokens 32 n + 8 b + 4 h and 16 further, b = k % 2
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int n = k >> 1, v = 4 * (k & 1) + 8 * (e >> 1) + 2 * (e & 1);
-        const uint32_t x = pair(__builtin_amdgcn_exp2f(s[n][v] - mb), __builtin_amdgcn_exp2f(s[n][v + 1] - mb));
-        l += __uint_as_float(x << 16) + __uint_as_float(x & 0xFFFF0000u);
-        p[k][e] = x;
+        const float x = __builtin_amdgcn_exp2f(fmaf(s[n][v], scale, -mb));
+        const float y = __builtin_amdgcn_exp2f(fmaf(s[n][v + 1], scale, -mb));
+        l += x;
+        l += y;
+        p[k][e] = pair(x, y);
       }
     // ---- output: coordinate 32 i + lr of the A operand, piece 2 k + h of its tokens
     const unsigned char* vb = buf + KB + PB + lr * (kTok * 2);
