@@ -137,8 +137,12 @@ struct FinishArgs {
 };
 
 // A row's shares joined: C = R/4 lanes a share, GR shares at a time.  mean fp32 [row][R].
-template <int R, int GR>
-__global__ __launch_bounds__(R / 4 * GR) void joint_merge(FinishArgs a, float* __restrict__ mean) {
+// With D above 0 the work-group goes on to the row's values (out) itself, N / D lanes a value
+// coordinate, whose factor pieces are on their way meanwhile.
+template <int R, int GR, int D>
+__global__ __launch_bounds__(R / 4 * GR) void joint_merge(FinishArgs a, float* __restrict__ mean,
+                                                          const bf16* __restrict__ W_values,
+                                                          bf16* __restrict__ out) {
   constexpr int C = R / 4, N = C * GR, NW = N / 64 > 0 ? N / 64 : 1;
   __shared__ __align__(16) floatx4 red[GR > 1 ? GR : 1][C];
   __shared__ float wo[2 * kJointMaxUnits];
@@ -148,6 +152,13 @@ __global__ __launch_bounds__(R / 4 * GR) void joint_merge(FinishArgs a, float* _
   const int head = int(id % a.heads), row = int(id / a.heads);
   const int tid = threadIdx.x, g = tid / C, c = tid % C;
   const int b = row / a.queries, i = row % a.queries;
+  constexpr int LD = D > 0 ? N / D : 1, PW = D > 0 ? R / 8 / LD : 1;     // lanes a coordinate, pieces a lane
+  u32x4 wv[PW];
+  if constexpr (D > 0) {
+    const bf16* src = W_values + (int64_t(head) * D + tid / LD) * R + 8 * (tid % LD);
+#pragma unroll
+    for (int j = 0; j < PW; ++j) wv[j] = *reinterpret_cast<const u32x4*>(src + 8 * j * LD);
+  }
   // shares: those of the sequence's units, then the prefix's
   const int64_t s0 = a.start[b], s1 = a.start[b + 1];
   const JointCut cut = joint_cut(a.start[a.batch], a.units, a.batch, a.groups);
@@ -240,7 +251,30 @@ __global__ __launch_bounds__(R / 4 * GR) void joint_merge(FinishArgs a, float* _
     for (int o = 1; o < GR; ++o) sum += red[o][c];
 #pragma unroll
     for (int v = 0; v < 4; ++v) sum[v] = L == 0.f ? 0.f : sum[v] / L;
-    *reinterpret_cast<floatx4*>(mean + id * R + 4 * c) = sum;
+    if constexpr (D > 0)
+      red[0][c] = sum;
+    else
+      *reinterpret_cast<floatx4*>(mean + id * R + 4 * c) = sum;
+  }
+  if constexpr (D > 0) {
+    __syncthreads();
+    const float* m = reinterpret_cast<const float*>(&red[0][0]) + 8 * (tid % LD);
+    float o = 0.f;
+#pragma unroll
+    for (int j = 0; j < PW; ++j) {
+      const floatx4 lo = *reinterpret_cast<const floatx4*>(m + 8 * j * LD);
+      const floatx4 hi = *reinterpret_cast<const floatx4*>(m + 8 * j * LD + 4);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        o = fmaf(__uint_as_float(wv[j][e] << 16), lo[2 * e], o);
+        o = fmaf(__uint_as_float(wv[j][e] & 0xFFFF0000u), lo[2 * e + 1], o);
+        o = fmaf(__uint_as_float(wv[j][2 + e] << 16), hi[2 * e], o);
+        o = fmaf(__uint_as_float(wv[j][2 + e] & 0xFFFF0000u), hi[2 * e + 1], o);
+      }
+    }
+#pragma unroll
+    for (int e = LD >> 1; e >= 1; e >>= 1) o += __shfl_xor(o, e);
+    if (tid % LD == 0) out[id * D + tid / LD] = from_f32<bf16>(o);
   }
 }
 
@@ -324,12 +358,15 @@ int units_of(int rank, int64_t slices, int64_t tiles) {
 
 template <int R, int D>
 hipError_t finish(const FinishArgs& a, const void* W_values, int n, float* mean, void* out, hipStream_t stream) {
-  // few rows have many shares each and get a work-group of 1024
+  // Few rows have many shares each: a work-group of 1024 that goes on to the values; many
+  // rows share the factors' reads in a launch of their own.  128 rows: ... us and ...
   const uint32_t rows = uint32_t(n) * a.heads;
-  if (rows < 1024)
-    hipLaunchKernelGGL((joint_merge<R, 4096 / R>), dim3(rows), dim3(1024), 0, stream, a, mean);
-  else
-    hipLaunchKernelGGL((joint_merge<R, 1024 / R>), dim3(rows), dim3(256), 0, stream, a, mean);
+  if (rows < 1024) {
+    hipLaunchKernelGGL((joint_merge<R, 4096 / R, D>), dim3(rows), dim3(1024), 0, stream, a, mean,
+                       static_cast<const bf16*>(W_values), static_cast<bf16*>(out));
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL((joint_merge<R, 1024 / R, 0>), dim3(rows), dim3(256), 0, stream, a, mean, nullptr, nullptr);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((joint_values<R, D>), dim3(uint32_t((n + 31) / 32) * (D / 32) * a.heads), dim3(256), 0, stream,
