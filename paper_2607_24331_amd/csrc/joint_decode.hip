@@ -3,7 +3,7 @@
 //
 //   q~_r = W_keys,h^T q_r,   o_r = W_values,h a_r,   a_r = sum_s 2^(u_s - M) O_s / sum_s 2^(m_s - M) l_s
 //
-// joint_fold    a wave a (head, 32 latent columns, 128 rows): the head's factor columns lie
+// joint_fold    a wave a (head, 32 latent columns, 32 or 128 rows): the head's factor columns lie
 //               in LDS once, read by the transposing load, as the contraction runs over
 //               the factor's rows; products on MFMA 32x32x16, rounded to bf16 (2^-9 of a
 //               coordinate, independent ones in a score's sum over r).  One more wave forms
@@ -31,7 +31,6 @@ __device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c) {
                                                  __builtin_bit_cast(joint::bf16x8, b), c, 0, 0, 0);
 }
 
-constexpr int kFoldRows = 128;            // rows a wave, 32 at a time
 
 // starts[b]: tiles of the sequences before b, starts[batch] of all.  One wave, 16
 // sequences a lane.
@@ -71,7 +70,7 @@ template <int D>
 __global__ __launch_bounds__(64) void joint_fold(const bf16* __restrict__ q, const bf16* __restrict__ W_keys,
                                                  int n, int heads, int r, int p, bf16* __restrict__ folded,
                                                  const int32_t* __restrict__ seq_lens, int max_context,
-                                                 int batch, int64_t* __restrict__ starts) {
+                                                 int batch, int64_t* __restrict__ starts, int wave_rows) {
   constexpr int ST = 40;                                       // elements a row of the factor in LDS
   __shared__ __align__(16) bf16 wk[D * ST];
   const int cols = r / 32;
@@ -81,7 +80,7 @@ __global__ __launch_bounds__(64) void joint_fold(const bf16* __restrict__ q, con
   }
   const int head = blockIdx.x / cols, c0 = (blockIdx.x % cols) * 32;
   const int lane = threadIdx.x, lr = lane & 31, h = lane >> 5;
-  const int row0 = blockIdx.y * kFoldRows;
+  const int row0 = blockIdx.y * wave_rows, row1 = min(row0 + wave_rows, n);
   const bf16* src = W_keys + (int64_t(head) * D) * r + c0;
   u32x4 piece[D / 16];
 #pragma unroll
@@ -90,6 +89,14 @@ __global__ __launch_bounds__(64) void joint_fold(const bf16* __restrict__ q, con
 #pragma unroll
   for (int i = 0; i < D / 16; ++i)
     *reinterpret_cast<u32x4*>(wk + (16 * i + (lane >> 2)) * ST + 8 * (lane & 3)) = piece[i];
+  const int W = r + p;
+  u32x4 x[D / 16];
+  auto load_rows = [&](int r0) {
+    const bf16* qrow = q + (int64_t(min(r0 + lr, n - 1)) * heads + head) * (D + p);
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) x[i] = *reinterpret_cast<const u32x4*>(qrow + 16 * i + 8 * h);
+  };
+  load_rows(row0);
   __syncthreads();
   // B operand of step i: column lr, rows 16 i + 8 h .. + 7 of the factor, four a load
   unsigned char* base = reinterpret_cast<unsigned char*>(wk + (8 * h + ((lane & 15) >> 2)) * ST +
@@ -102,23 +109,20 @@ __global__ __launch_bounds__(64) void joint_fold(const bf16* __restrict__ q, con
     const auto xy = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
     f[i] = __builtin_bit_cast(u32x4, xy);
   }
-  const int W = r + p;
 #pragma unroll 1
-  for (int r0 = row0; r0 < min(row0 + kFoldRows, n); r0 += 32) {
-    const bf16* qrow = q + (int64_t(min(r0 + lr, n - 1)) * heads + head) * (D + p);
+  for (int r0 = row0; r0 < row1; r0 += 32) {
     f32x16 acc;
 #pragma unroll
     for (int v = 0; v < 16; ++v) acc[v] = 0.f;
-    u32x4 x[D / 16];
-#pragma unroll
-    for (int i = 0; i < D / 16; ++i) x[i] = *reinterpret_cast<const u32x4*>(qrow + 16 * i + 8 * h);
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) acc = mfma(x[i], f[i], acc);
+    if (r0 + 32 < row1) load_rows(r0 + 32);
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
       const int row = r0 + 8 * (v >> 2) + 4 * h + (v & 3);
       if (row < n) folded[(int64_t(row) * heads + head) * W + c0 + lr] = from_f32<bf16>(acc[v]);
     }
+    const bf16* qrow = q + (int64_t(min(r0 + lr, n - 1)) * heads + head) * (D + p);
     if (c0 == 0 && r0 + lr < n)                                // the position part stays as it is
       for (int j = 8 * h; j < p; j += 16)
         *reinterpret_cast<u32x4*>(folded + (int64_t(r0 + lr) * heads + head) * W + r + j) =
@@ -439,11 +443,13 @@ hipError_t launch_joint_decode(const JointShape& s, const void* q, const void* p
   const dckv_joint_desc& d = s.d;
   const int n = s.batch * s.queries;                   // at most 65535
   int64_t* starts = reinterpret_cast<int64_t*>(ws + s.off_start);
-  const dim3 grid(d.num_heads * (d.rank / 32) + 1, (n + kFoldRows - 1) / kFoldRows);
+  // few rows are spread over more waves, each of which reads the factor again
+  const int wave_rows = n <= 256 ? 32 : 128;
+  const dim3 grid(d.num_heads * (d.rank / 32) + 1, (n + wave_rows - 1) / wave_rows);
 #define DCKV_FOLD(D)                                                                                         \
   hipLaunchKernelGGL((joint_fold<D>), grid, dim3(64), 0, stream, static_cast<const bf16*>(q),                 \
                      static_cast<const bf16*>(W_keys), n, d.num_heads, d.rank, d.rope_dim,                    \
-                     reinterpret_cast<bf16*>(ws), seq_lens, s.max_context, s.batch, starts)
+                     reinterpret_cast<bf16*>(ws), seq_lens, s.max_context, s.batch, starts, wave_rows)
   if (d.head_dim == 64)
     DCKV_FOLD(64);
   else
