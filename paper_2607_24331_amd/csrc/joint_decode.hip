@@ -409,7 +409,7 @@ JointShape joint_shape(const dckv_joint_desc& d, int32_t queries, int32_t batch,
   s.units = units_of(d.rank, s.slices, tiles);
   const int64_t all = int64_t(s.rows) * batch;
   s.pre_row_waves = row_waves_of(all);
-  s.pre_slices = int32_t((all + 16 * s.pre_row_waves - 1) / (16 * s.pre_row_waves));
+  s.pre_slices = int32_t(std::max<int64_t>(1, (all + 16 * s.pre_row_waves - 1) / (16 * s.pre_row_waves)));
   s.pre_units = prefix_len > 0 ? units_of(d.rank, s.pre_slices, tiles_of(prefix_len)) : 0;
   const size_t width = size_t(d.rank + d.rope_dim);
   s.off_start = align_up(size_t(all) * width * 2);
