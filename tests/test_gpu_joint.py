@@ -302,3 +302,466 @@ def test_prompts(H, d, r, p, cache, cached, added, pad):
     check(host(out[:n]), want[:n], np.abs(want).max())
     assert torch.all(out[n:] == 7.0)                              # rows behind the last sequence
     assert torch.equal(out[:n], joint_prefill(j, q, rs, pool, table, seq, top, wk, wv)[:n])
+
+
+def test_prompts_that_do_not_fit_get_nan():
+    from paper_2607_24331_amd import joint_prefill
+    j = joint_of(2, 64, 128, 32, "bf16")
+    cached, added = [10, 100, 0], [20, 30, 5]
+    pool, table, start, q, wk, wv, seq, rs, lens, top = prompt_case(j, cached, added, 0, 9)
+    whole = joint_prefill(j, q, rs, pool, table, seq, top, wk, wv)
+    got = joint_prefill(j, q, rs, pool, table, seq, top, wk, wv, total_context=30 + 129)
+    assert torch.equal(got[:20], whole[:20]) and torch.isnan(got[20:]).all()
+    none = joint_prefill(j, q, rs, pool, table, seq, top, wk, wv, total_context=0)
+    assert torch.isnan(none).all()
+
+
+def test_prompts_longer_than_their_sequences():
+    """Rows beyond a sequence's length see nothing; a length is clipped to max_context."""
+    from paper_2607_24331_amd import joint_prefill
+    j = joint_of(2, 64, 128, 0, "bf16")
+    pool, table, start, q, wk, wv, seq, rs, lens, top = prompt_case(j, [0, 0, 0], [70, 70, 70], 0, 11)
+    short = torch.tensor([3, -5, 1000], dtype=torch.int32, device="cuda")
+    got = joint_prefill(j, q, rs, pool, table, short, 100, wk, wv)
+    assert not got[:67].any() and not got[70:140].any() and got[67:70].any()
+    hp = host(pool)
+    c, k = oj.tokens(hp, table[0].cpu().numpy(), 3, 128, 0, "bf16")
+    want = oj.attend(host(q[67:70]), c, k, host(wk), host(wv), [1, 2, 3], 1 / 8)
+    check(host(got[67:70]), want, np.abs(want).max())
+    c, k = oj.tokens(hp, table[2].cpu().numpy(), 100, 128, 0, "bf16")
+    want = oj.attend(host(q[140:]), c, k, host(wk), host(wv), [31 + i for i in range(70)], 1 / 8)
+    check(host(got[140:]), want, np.abs(want).max())
+
+
+# ------------------------------------------------- what a query does not see
+def poison(j, pool, slots, value, part="c"):
+    """Make one element of each slot's latent (or key) `value`, or every byte 0xFF."""
+    r, w = j.rank, j.rank + j.rope_dim
+    col = 5 if part == "c" else r + 3
+    for sl in slots:
+        page, s = divmod(int(sl), PAGE)
+        if value == "all":
+            at = oj.place(r, j.rope_dim, j.cache, s, np.arange(w))
+            if j.cache == "bf16":
+                pool[page, at] = math.nan
+            else:
+                pool[page, at] = 0xFF
+                pool[page, PAGE * w + s] = 0xFF
+                pool[page, PAGE * (w + 1) + s] = 0xFF
+        else:
+            pool[page, int(oj.place(r, j.rope_dim, j.cache, s, col))] = value
+
+
+@pytest.mark.parametrize("H,d,r,p,cache", [(8, 64, 128, 32, "bf16"), (16, 64, 256, 64, "e4m3"), (32, 128, 512, 64, "bf16"),
+                                           (64, 64, 512, 32, "e4m3"), (40, 64, 128, 0, "e4m3"), (64, 128, 256, 32, "bf16")])
+@pytest.mark.parametrize("Q", [1, 4])
+def test_unseen_slots_do_not_reach_a_decode(H, d, r, p, cache, Q):
+    """Slots behind the sequences hold NaN everywhere, and so do tokens that only later queries see."""
+    from paper_2607_24331_amd import joint_decode
+    g = gen(H + Q)
+    j = joint_of(H, d, r, p, cache)
+    lens = [1, 31, 33, 64, 100, 161]
+    B, width = len(lens), 4
+    pool = filled(j, B * width, g)
+    table = torch.arange(B * width, dtype=torch.int32, device="cuda").view(B, width)
+    q = randn(g, B, Q, H, d + p).to(BF16)
+    wk, wv = factors(j, g)
+    seq = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    clean = joint_decode(j, q, pool, table, seq, 200, wk, wv)
+    dirty = pool.clone()
+    for b, T in enumerate(lens):
+        poison(j, dirty, range((b * width) * PAGE + T, (b + 1) * width * PAGE), "all")
+    assert torch.equal(clean, joint_decode(j, q, dirty, table, seq, 200, wk, wv))
+    if Q == 1:
+        return
+    for value in ([math.nan, math.inf] if cache == "bf16" else [0x7F, 0xFF]):
+        for part in ("c", "k") if p else ("c",):
+            bad = dirty.clone()
+            first = 2                                  # the token of query 2 of every sequence that has it
+            poison(j, bad, [b * width * PAGE + T - Q + first for b, T in enumerate(lens) if T - Q + first >= 0], value, part)
+            got = joint_decode(j, q, bad, table, seq, 200, wk, wv)
+            for b, T in enumerate(lens):
+                has = T - Q + first >= 0
+                assert torch.equal(got[b, :first], clean[b, :first])
+                assert torch.isnan(got[b, first:]).all() if has else torch.equal(got[b], clean[b])
+
+
+@pytest.mark.parametrize("H,d,r,p,cache", [(2, 64, 128, 32, "bf16"), (3, 128, 256, 0, "e4m3"), (2, 64, 512, 64, "bf16")])
+def test_unseen_slots_do_not_reach_a_prompt(H, d, r, p, cache):
+    from paper_2607_24331_amd import joint_prefill
+    j = joint_of(H, d, r, p, cache)
+    cached, added = [0, 70, 5], [130, 33, 64]
+    pool, table, start, q, wk, wv, seq, rs, lens, top = prompt_case(j, cached, added, 0, 5)
+    clean = joint_prefill(j, q, rs, pool, table, seq, top, wk, wv)
+    dirty = pool.clone()
+    tab = table.cpu().numpy()
+    used = set()
+    for b, T in enumerate(lens):
+        used |= {int(tab[b, t // PAGE]) * PAGE + t % PAGE for t in range(T)}
+    poison(j, dirty, [s for s in range(pool.shape[0] * PAGE) if s not in used], "all")
+    assert torch.equal(clean, joint_prefill(j, q, rs, dirty, table, seq, top, wk, wv))
+    for value in ([math.nan, -math.inf] if cache == "bf16" else [0x7F]):
+        for part in ("c", "k") if p else ("c",):
+            bad = dirty.clone()
+            at = 97                                     # a token of every sequence's prompt, where it is one
+            poison(j, bad, [int(tab[b, at // PAGE]) * PAGE + at % PAGE for b, T in enumerate(lens) if at < T], value, part)
+            got = joint_prefill(j, q, rs, bad, table, seq, top, wk, wv)
+            for b, (c, a) in enumerate(zip(cached, added)):
+                lo = int(start[b])
+                cut = lo + min(max(at - c, 0), a) if at < c + a else lo + a
+                assert torch.equal(got[lo:cut], clean[lo:cut])
+                assert torch.isnan(got[cut:lo + a]).all()
+
+
+def test_missing_pages_are_empty():
+    from paper_2607_24331_amd import joint_decode, joint_prefill
+    for cache in ("bf16", "e4m3"):
+        g = gen(3)
+        j = joint_of(8, 64, 128, 32, cache)
+        pool = filled(j, 12, g)
+        wk, wv = factors(j, g)
+        table = torch.randperm(12, generator=g, device="cuda").to(torch.int32).view(2, 6)
+        holes = table.clone()
+        holes[0, 1], holes[0, 3], holes[1, 0], holes[1, 5] = -1, 12, -(2 ** 31), 2 ** 31 - 1
+        q = randn(g, 2, 3, 8, 96).to(BF16)
+        seq = torch.tensor([300, 384], dtype=torch.int32, device="cuda")
+        got = joint_decode(j, q, pool, holes, seq, 384, wk, wv)
+        pre = joint_decode(j, q, pool, holes, torch.zeros_like(seq), 0, wk, wv, holes[0], 300)
+        rows = randn(g, 40, 8, 96).to(BF16)
+        start = torch.tensor([0, 20, 40], dtype=torch.int32, device="cuda")
+        prm = joint_prefill(j, rows, start, pool, holes, seq, 384, wk, wv)
+        hp, hk, hv = host(pool), host(wk), host(wv)
+        for b, T in enumerate([300, 384]):
+            ids = holes[b].cpu().numpy()
+            keep = np.array([t for t in range(T) if 0 <= ids[t // PAGE] < 12])
+            c, k = oj.tokens(hp, np.where((ids >= 0) & (ids < 12), ids, 0), T, 128, 32, cache)
+            def want(hq, pos):
+                return oj.attend(hq, c[keep], k[keep], hk, hv, [int((keep <= x).sum()) for x in pos], 96 ** -0.5)
+            w = want(host(q[b]), [T - 3 + i for i in range(3)])
+            check(host(got[b]), w, np.abs(w).max())
+            w = want(host(rows[20 * b:20 * b + 20]), [T - 20 + i for i in range(20)])
+            check(host(prm[20 * b:20 * b + 20]), w, np.abs(w).max())
+            if b == 0:
+                for x in range(2):
+                    w = want(host(q[x]), [300 - 3 + i for i in range(3)])
+                    check(host(pre[x]), w, np.abs(w).max())
+        none = torch.full_like(table, -1)
+        assert not joint_decode(j, q, pool, none, seq, 384, wk, wv).any()
+        assert not joint_prefill(j, rows, start, pool, none, seq, 384, wk, wv).any()
+
+
+# ------------------------------------------------------- scores out of the ordinary
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("H,r,p", [(8, 128, 0), (40, 512, 64)])
+def test_scores_that_grow(cache, H, r, p):
+    """Keys grow along the context, so that the running maximum is raised again and again, and
+    fall in the second half; scores up to several hundred."""
+    from paper_2607_24331_amd import joint_append, joint_decode, joint_prefill
+    g = gen(1)
+    j = joint_of(H, 64, r, p, cache)
+    T = 700
+    grow = torch.cat([torch.linspace(0.01, 12, 350), torch.linspace(12, 0.01, 350)]).cuda()[:, None]
+    c, k = randn(g, T, r) * grow, randn(g, T, p) * grow
+    pool = j.new_pool(11)
+    joint_append(j, c, k if p else None, torch.arange(T, device="cuda"), pool)
+    table = torch.arange(11, dtype=torch.int32, device="cuda").view(1, 11)
+    wk, wv = factors(j, g)
+    seq = torch.tensor([T], dtype=torch.int32, device="cuda")
+    rows = (randn(g, 130, H, 64 + p) * 3).to(BF16)
+    hp = host(pool)
+    hc, hk = oj.tokens(hp, table[0].cpu().numpy(), T, r, p, cache)
+    # peaked rows rest on few tokens: their scores' errors (2^-9 of terms that add up to s, so
+    # about 2^-9 |s| / sqrt(r), times 4) move the weights by that much
+    want = oj.attend(host(rows[:2]), hc, hk, host(wk), host(wv), [T - 1, T], (64 + p) ** -0.5)
+    got = joint_decode(j, rows[None, :2].contiguous(), pool, table, seq, T, wk, wv)[0]
+    size = np.abs(want).max()
+    assert np.all(np.abs(host(got) - want) <= 0.15 * size)
+    assert np.sqrt(np.mean((host(got) - want) ** 2)) <= 2.0 ** -6 * np.sqrt(np.mean(want ** 2)) * 2
+    start = torch.tensor([0, 130], dtype=torch.int32, device="cuda")
+    got = joint_prefill(j, rows, start, pool, table, seq, T, wk, wv)
+    pick = [0, 64, 129]
+    want = oj.attend(host(rows[pick]), hc, hk, host(wk), host(wv), [T - 129 + i for i in pick], (64 + p) ** -0.5)
+    assert np.all(np.abs(host(got[pick]) - want) <= 0.15 * np.abs(want).max())
+    assert np.sqrt(np.mean((host(got[pick]) - want) ** 2)) <= 2.0 ** -6 * np.sqrt(np.mean(want ** 2)) * 2
+
+
+def test_exponents_of_every_size():
+    """e4m3 rows whose powers of two span the format: a token's weight is independent of its
+    latent's size where the keys' part decides."""
+    from paper_2607_24331_amd import joint_decode
+    g = gen(7)
+    j = joint_of(4, 64, 128, 64, "e4m3")
+    pool = filled(j, 3, g)
+    exps = torch.randint(15, 100, (128,), generator=g, device="cuda").to(torch.uint8)      # 2^-112 .. 2^-28: scores of 0
+    for page in (0, 1):
+        pool[page, PAGE * 192:PAGE * 193] = exps[page * 64:page * 64 + 64]
+    q = randn(g, 1, 1, 4, 128).to(BF16)
+    wk, wv = factors(j, g)
+    table = torch.tensor([[0, 1]], dtype=torch.int32, device="cuda")
+    seq = torch.tensor([128], dtype=torch.int32, device="cuda")
+    got = joint_decode(j, q, pool, table, seq, 128, wk, wv)
+    want = oracle_decode(j, q, pool, table, [128], 128, wk, wv)
+    assert np.abs(want).max() < 1e-6                                   # nothing of unit size
+    check(host(got), want, np.abs(want).max())
+    # one huge latent that no row gives weight to must not wash the others out
+    pool[2] = pool[0]
+    pool[2, PAGE * 192] = 127 + 100
+    pool[2, oj.place(128, 64, "e4m3", 0, np.arange(128))] = 0
+    pool[2, int(oj.place(128, 64, "e4m3", 0, 0))] = 0x38               # 1.0, times 2^100
+    wk2 = torch.zeros_like(wk)
+    wk2[:, 0, 0] = 1.0
+    q2 = q.clone()
+    q2[..., 0] = -1.0
+    got = joint_decode(j, q2, pool, torch.tensor([[2]], dtype=torch.int32, device="cuda"),
+                       torch.tensor([64], dtype=torch.int32, device="cuda"), 64, wk2, wv)
+    want = oracle_decode(j, q2, pool, torch.tensor([[2]]), [64], 64, wk2, wv)
+    check(host(got), want, np.abs(want).max())
+
+
+def test_scale_is_the_callers():
+    from paper_2607_24331_amd import joint_decode, joint_prefill
+    g = gen(2)
+    j = joint_of(4, 64, 128, 32, "bf16", scale=0.37)
+    pool = filled(j, 2, g)
+    wk, wv = factors(j, g)
+    table = torch.tensor([[1, 0]], dtype=torch.int32, device="cuda")
+    seq = torch.tensor([100], dtype=torch.int32, device="cuda")
+    q = randn(g, 1, 1, 4, 96).to(BF16)
+    want = oracle_decode(j, q, pool, table, [100], 128, wk, wv)
+    check(host(joint_decode(j, q[:, 0].contiguous(), pool, table, seq, 128, wk, wv)), want[:, 0], np.abs(want).max())
+    start = torch.tensor([0, 1], dtype=torch.int32, device="cuda")
+    got = joint_prefill(j, q[0], start, pool, table, seq, 128, wk, wv)
+    check(host(got), want[0], np.abs(want).max())
+
+
+# ----------------------------------------------------------- batches and cuts
+def plain(j, q, pool, table, lens, wk, wv, prefix=None, n=0):
+    """The decode in float64 on the GPU, a sequence at a time (pages in order of `table`)."""
+    r, p, d, H = j.rank, j.rope_dim, j.head_dim, j.num_heads
+    w = r + p
+    at = torch.from_numpy(oj.place(r, p, j.cache, np.arange(PAGE)[:, None], np.arange(w)[None])).cuda()
+
+    def toks(ids):
+        x = pool[ids.long()]
+        v = x[:, at.view(-1)]
+        if j.cache == "bf16":
+            return v.double().view(-1, w)
+        e = torch.exp2(x[:, PAGE * w:].double() - 127).view(-1, 2, PAGE)
+        v = v.view(torch.float8_e4m3fn).double().view(-1, PAGE, w)
+        return torch.cat([v[..., :r] * e[:, 0, :, None], v[..., r:] * e[:, 1, :, None]], -1).view(-1, w)
+
+    out = torch.zeros(*q.shape[:3], d, dtype=torch.float64, device="cuda")
+    pre = toks(prefix)[:n] if n else None
+    qa = torch.matmul(q[..., :d].double().permute(2, 0, 1, 3), wk.double()[:, None]).permute(1, 2, 0, 3)
+    qa = torch.cat([qa, q[..., d:].double()], -1) / math.sqrt(d + p)
+    for b, T in enumerate(lens):
+        x = toks(table[b, :-(-T // PAGE)])[:T]
+        x = torch.cat([pre, x]) if n else x
+        for i in range(q.shape[1]):
+            m = n + T - q.shape[1] + i + 1
+            if m > 0:
+                a = torch.softmax(qa[b, i] @ x[:m].t(), -1) @ x[:m, :r]
+                out[b, i] = torch.matmul(wv.double(), a[:, :, None])[..., 0]
+    return out
+
+
+@pytest.mark.parametrize("H,d,r,p,cache,B,low,high,Q,n", [
+    (8, 64, 128, 0, "bf16", 300, 0, 40, 1, 0), (16, 64, 256, 32, "e4m3", 1500, 0, 9, 1, 0),
+    (16, 64, 128, 64, "bf16", 200, 1000, 2000, 1, 0), (32, 128, 512, 64, "e4m3", 64, 10, 3000, 1, 0),
+    (32, 64, 512, 0, "bf16", 100, 0, 1500, 1, 0), (8, 64, 128, 32, "e4m3", 65, 0, 300, 5, 0),
+    (64, 64, 128, 0, "bf16", 3, 100, 900, 64, 0), (16, 64, 256, 64, "bf16", 130, 0, 90, 2, 1000),
+    (32, 128, 512, 64, "bf16", 1, 20000, 20000, 1, 0), (16, 128, 512, 32, "e4m3", 2, 1, 40000, 1, 777),
+    (1, 64, 128, 0, "bf16", 2, 60000, 70000, 1, 0)])
+def test_batches_and_long_contexts(H, d, r, p, cache, B, low, high, Q, n):
+    from paper_2607_24331_amd import joint_decode
+    g = gen(B + r)
+    j = joint_of(H, d, r, p, cache)
+    lens = np.random.default_rng(B).integers(low, high + 1, B)
+    lens[-1] = high
+    width, shared = -(-high // PAGE), -(-n // PAGE)
+    some = min(B * width + shared, 300)
+    pool = filled(j, some, g)                          # sequences share pages: they only read
+    table = torch.randint(0, some, (B, width), generator=g, device="cuda", dtype=torch.int32)
+    prefix = torch.randint(0, some, (shared,), generator=g, device="cuda", dtype=torch.int32)
+    q = randn(g, B, Q, H, d + p).to(BF16)
+    wk, wv = factors(j, g)
+    seq = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    ws = torch.full((j.workspace_bytes(Q, B, high, n),), 255, dtype=torch.uint8, device="cuda")     # NaN all over
+    out = joint_decode(j, q, pool, table, seq, high, wk, wv, prefix if n else None, n, workspace=ws)
+    want = plain(j, q, pool, table, lens.tolist(), wk, wv, prefix, n)
+    size = want.abs().max().item()
+    err = (out.double() - want).abs()
+    # as check(); rows that see one token are that token's value, a few roundings off
+    assert (err <= 2.0 ** -6 * size + 2.0 ** -8 * want.abs()).all(), (err.max().item(), size)
+    assert (err.square().mean().sqrt() <= 2.0 ** -8 * want.square().mean().sqrt()).item()
+    # a smaller call in the same workspace, and again: the same bits
+    again = joint_decode(j, q, pool, table, seq, high, wk, wv, prefix if n else None, n, workspace=ws)
+    assert torch.equal(out, again)
+
+
+def test_offsets_past_32_bits():
+    from paper_2607_24331_amd import joint_append, joint_decode, joint_prefill, joint_read
+    g = gen(4)
+    j = joint_of(16, 64, 512, 64, "bf16")
+    pages = (5 << 30) // j.page_bytes                  # 5 GiB of pages
+    pool = torch.empty(pages, j.page_elems, dtype=BF16, device="cuda")
+    c, k = randn(g, 200, 512), randn(g, 200, 64)
+    ids = torch.tensor([pages - 1, pages - 3, 0, pages - 2], dtype=torch.int32, device="cuda")
+    t = torch.arange(200, device="cuda")
+    slot = ids.long()[t // PAGE] * PAGE + t % PAGE
+    joint_append(j, c, k, slot, pool)
+    rc, rk = joint_read(j, pool, slot, dtype=F32)
+    assert torch.equal(rc, c.to(BF16).float()) and torch.equal(rk, k.to(BF16).float())
+    wk, wv = factors(j, g)
+    q = randn(g, 1, 2, 16, 128).to(BF16)
+    seq = torch.tensor([200], dtype=torch.int32, device="cuda")
+    want = plain(j, q, pool, ids[None], [200], wk, wv)
+    got = joint_decode(j, q, pool, ids[None].contiguous(), seq, 256, wk, wv)
+    check(host(got), host(want), host(want).max())
+    start = torch.tensor([0, 2], dtype=torch.int32, device="cuda")
+    got = joint_prefill(j, q[0], start, pool, ids[None].contiguous(), seq, 256, wk, wv)
+    check(host(got), host(want[0]), host(want).max())
+
+
+# --------------------------------------------- streams, graphs, workspaces
+def test_another_stream_and_workspaces():
+    from paper_2607_24331_amd import DckvError, joint_append, joint_decode, joint_prefill, joint_read
+    g = gen(8)
+    j = joint_of(16, 64, 256, 32, "e4m3")
+    pool, wk_wv = filled(j, 8, g), factors(j, g)
+    wk, wv = wk_wv
+    table = torch.arange(8, dtype=torch.int32, device="cuda").view(2, 4)
+    seq = torch.tensor([200, 77], dtype=torch.int32, device="cuda")
+    q = randn(g, 2, 16, 96).to(BF16)
+    start = torch.tensor([0, 1, 2], dtype=torch.int32, device="cuda")
+    here = joint_decode(j, q, pool, table, seq, 256, wk, wv)
+    prm = joint_prefill(j, q, start, pool, table, seq, 256, wk, wv)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    there = joint_decode(j, q, pool, table, seq, 256, wk, wv, stream=s)
+    prm2 = joint_prefill(j, q, start, pool, table, seq, 256, wk, wv, stream=s)
+    c, k = joint_read(j, pool, torch.arange(9, device="cuda"), stream=s)
+    joint_append(j, c, k, torch.arange(9, device="cuda"), pool, stream=s)
+    s.synchronize()
+    assert torch.equal(here, there) and torch.equal(prm, prm2)
+    need = j.workspace_bytes(1, 2, 256)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    assert torch.equal(here, joint_decode(j, q, pool, table, seq, 256, wk, wv, workspace=ws))
+    with pytest.raises(DckvError, match="workspace"):
+        joint_decode(j, q, pool, table, seq, 256, wk, wv, workspace=ws[:1024].clone())
+    with pytest.raises(ValueError, match="contiguous"):
+        joint_decode(j, q[:, ::2], pool, table, seq, 256, wk[::2], wv[::2])
+    with pytest.raises(ValueError, match="heads"):
+        joint_decode(j, q[:, :8].contiguous(), pool, table, seq, 256, wk, wv)
+    with pytest.raises(ValueError, match="prefix_pages"):
+        joint_decode(j, q, pool, table, seq, 256, wk, wv, table[0], 300)
+    with pytest.raises(TypeError):
+        joint_decode(j, q.float(), pool, table, seq, 256, wk, wv)
+    with pytest.raises(DckvError):
+        joint_decode(j, q, pool, table, seq, 257, wk, wv)
+    with pytest.raises(ValueError, match="whole number"):
+        joint_decode(j, q, pool.view(-1)[:-64], table, seq, 256, wk, wv)
+    with pytest.raises(ValueError):
+        joint_append(j, c, k[:5], torch.arange(9, device="cuda"), pool)
+    with pytest.raises(ValueError):
+        joint_append(j, c.t().contiguous().t(), k, torch.arange(9, device="cuda"), pool)
+    empty = joint_decode(j, q[:0], pool, table[:0], seq[:0], 256, wk, wv)
+    assert empty.shape == (0, 16, 64)
+    assert joint_prefill(j, q[:0], start[:1], pool, table[:0], seq[:0], 256, wk, wv).shape == (0, 16, 64)
+    c0, k0 = joint_read(j, pool, torch.arange(0, device="cuda"))
+    assert c0.shape == (0, 256) and k0.shape == (0, 32)
+    joint_append(j, c0, k0, torch.arange(0, device="cuda"), pool)
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+def test_captured_steps_follow_the_lengths(cache):
+    """One graph of append, decode over a prefix and prompts, replayed as the sequences grow, with
+    eager calls of the same kind between the replays; another graph beside it with a workspace of
+    its own."""
+    from paper_2607_24331_amd import joint_append, joint_decode, joint_prefill
+    g = gen(6)
+    j = joint_of(16, 64, 256, 32, cache)
+    B, width, top = 3, 6, 384
+    pool = filled(j, B * width + 2, g)
+    ids = torch.randperm(B * width + 2, generator=g, device="cuda").to(torch.int32)
+    table, prefix = ids[:B * width].view(B, width).contiguous(), ids[B * width:].contiguous()
+    wk, wv = factors(j, g)
+    q, c, k = randn(g, B, 1, 16, 96).to(BF16), randn(g, B, 256), randn(g, B, 32)
+    seq = torch.tensor([0, 60, 300], dtype=torch.int32, device="cuda")
+    slot = torch.zeros(B, dtype=torch.int64, device="cuda")
+    start = torch.arange(B + 1, dtype=torch.int32, device="cuda")
+    out, prm = torch.zeros(B, 1, 16, 64, dtype=BF16, device="cuda"), torch.zeros(B, 16, 64, dtype=BF16, device="cuda")
+    ws = [torch.empty(j.workspace_bytes(1, B, top, 100), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    wp = torch.empty(j.prefill_workspace_bytes(B, B, top, B * top), dtype=torch.uint8, device="cuda")
+
+    def step(w, o):
+        joint_append(j, c, k, slot, pool)
+        joint_decode(j, q, pool, table, seq, top, wk, wv, prefix, 100, out=o, workspace=w)
+        joint_prefill(j, q[:, 0], start, pool, table, seq, top, wk, wv, out=prm, workspace=wp)
+
+    other = torch.zeros_like(out)
+    graphs = []
+    for w, o in ((ws[0], out), (ws[1], other)):
+        gr = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(gr):
+            step(w, o)
+        graphs.append(gr)
+    for turn in range(4):
+        pos = seq.long().clone()
+        slot.copy_(table.long().gather(1, (pos // PAGE)[:, None])[:, 0] * PAGE + pos % PAGE)
+        seq += 1
+        c.copy_(randn(g, B, 256))
+        k.copy_(randn(g, B, 32))
+        graphs[turn % 2].replay()
+        torch.cuda.synchronize()
+        got, gp = (out, other)[turn % 2].clone(), prm.clone()
+        eager = joint_decode(j, q, pool, table, seq, top, wk, wv, prefix, 100)
+        assert torch.equal(got, eager)
+        assert torch.equal(gp, joint_prefill(j, q[:, 0], start, pool, table, seq, top, wk, wv))
+        want = plain(j, q, pool, table, seq.tolist(), wk, wv, prefix, 100)
+        check(host(got), host(want), host(want.abs()).max())
+        seq += torch.tensor([30, 1, 15], dtype=torch.int32, device="cuda")
+
+
+# ------------------------------------------------------------- all together
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+def test_serving_loop(cache):
+    """Prompts of three sequences over two steps, then single tokens: pages from page_map, keys
+    and queries turned by position, each step's attention against float64 over everything that
+    was appended."""
+    from paper_2607_24331_amd import Rotary, joint_append, joint_decode, joint_prefill, joint_read, page_map, rotary
+    g = gen(10)
+    H, d, r, p = 8, 64, 128, 32
+    j = joint_of(H, d, r, p, cache)
+    rot = Rotary(p, layout="interleaved")
+    pool = j.new_pool(16)
+    B = 3
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    cached, table = i32([0] * B), torch.full((B, 5), -1, dtype=torch.int32, device="cuda")
+    free, count = torch.randperm(16, generator=g, device="cuda").to(torch.int32), i32([16])
+    wk, wv = factors(j, g)
+    for added in ([70, 0, 33], [1, 100, 31], [1, 1, 1], [1, 1, 1]):
+        rows = sum(added) + 2
+        m = page_map(cached, i32(added), table, free, count, rows)
+        x = randn(g, rows, r + p)
+        joint_append(j, x[:, :r], x[:, r:], m.slot, pool, rot, m.position)
+        q = randn(g, rows, H, d + p).to(BF16)
+        rotary(rot, q[..., d:], m.position, out=q[..., d:])
+        step = max(added) == 1
+        n = sum(added)
+        if step:
+            got = joint_decode(j, q[:n], pool, table, m.seq_lens, 320, wk, wv)
+        else:
+            got = joint_prefill(j, q, m.row_start, pool, table, m.seq_lens, 320, wk, wv)[:n]
+        lens, start = m.seq_lens.tolist(), m.row_start.tolist()
+        for b in range(B):
+            a = added[b]
+            if a == 0:
+                continue
+            want = plain(j, q[start[b]:start[b] + a][None], pool, table[b:b + 1], [lens[b]], wk, wv)[0]
+            check(host(got[start[b]:start[b] + a]), host(want), host(want.abs()).max())
+        c, k = joint_read(j, pool, m.slot, dtype=F32)
+        assert not c[n:].any()
+        tol = 2.0 ** -8 if cache == "bf16" else 2.0 ** -4
+        assert ((c[:n] - x[:n, :r]).abs() <= tol * x[:n, :r].abs().clamp(min=2.0 ** -6)).all()
+        cached, count = m.seq_lens, m.free_left
