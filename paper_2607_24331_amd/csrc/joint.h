@@ -82,7 +82,8 @@ struct JointPrompt {
   int32_t n_rows, batch, max_context;
   int64_t total_context;
   int64_t kv_tiles, q_tiles;    // 64-token tiles and row tiles, at most
-  size_t off_qtile, off_kvtile, off_flags, off_c, off_rope, off_k, off_v;
+  int32_t slot;                 // sequences, in whole lines of 128 bytes
+  size_t off_qtile, off_most, off_kvtile, off_flags, off_c, off_rope, off_k, off_v;
   size_t bytes;
 };
 

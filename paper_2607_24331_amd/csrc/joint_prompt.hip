@@ -17,6 +17,12 @@
 //                  two buffers: scores S[token][row] and sums O[coordinate][row] on MFMA 32x32x16,
 //                  so that the weights feed the second product from the registers they
 //                  were made in, and the running maximum is a lane's own.
+// Keys, values, queries and weights are f16 on the matrix unit, whose 11 bits keep each
+// rounding (2^-12) below that of the bf16 result; powers of two keep them in its range: one a
+// sequence for its keys (of all heads, with the position keys) and one for its values, from
+// bounds on their magnitude (greatest latent coordinate x r x greatest factor element: the
+// largest is below 2^15, and 28 binades below that are still normal numbers), one a query
+// row.  They meet in a row's score scale and in its result.
 // Bound by the products: 4 T r d + 2 pairs (2 d + p) a head, and in the attention by LDS,
 // which 32 rows a wave read as fast as the products of a tile go.
 #include <algorithm>
@@ -30,6 +36,10 @@ namespace dckv {
 namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef unsigned short ushort2_ __attribute__((ext_vector_type(2)));
+typedef _Float16 half2 __attribute__((ext_vector_type(2)));
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef float floatx2 __attribute__((ext_vector_type(2)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
@@ -38,10 +48,12 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr int kRows = 128;                // rows of a tile
 constexpr int kTok = 64;                  // tokens of a tile
 constexpr float kSlack = 6.f;             // the maximum is raised by whole jumps of 2^6 and more
-constexpr float kMaxBf16 = 3.3895313892515355e38f;
+constexpr float kMaxHalf = 65504.f;
+constexpr float kRaise = 8.f;             // weights are 2^8 as large in f16: 2^14 at most, 22 binades below 1 are normal
 
 struct RowTile {
   int32_t row, n, kv, first;              // first row, rows, first token tile (-1: does not fit), position of the first row
+  int32_t b, unused[3];                   // sequence
 };
 
 struct PromptArgs {
@@ -49,12 +61,57 @@ struct PromptArgs {
   int32_t n_rows, batch, max_context;
   int64_t total_context;
   int32_t q_tiles, kv_tiles;              // at most
-  int32_t* counts;                        // row tiles, token tiles
+  int32_t* counts;                        // row tiles, token tiles; bf16 bits of the greatest |W_keys|, |W_values|
+  int2* most;                             // [kSlots][slot] bf16 bits of a sequence's greatest |latent|, |key| coordinate
+  int32_t slot;                           // sequences a slot, whole lines of 128 bytes
   RowTile* rows;
   int2* toks;                             // sequence, tile
   uint16_t* there;                        // a bit a token of a tile: it is there
   uint16_t* odd;                          // and is not finite
 };
+
+// The least e with |x| < 2^e, from the bits of a bf16 |x| (subnormals: -126).
+__device__ __forceinline__ int exponent_above(int bits) { return max(bits >> 7, 1) - 126; }
+
+// Powers of two: keys are 2^keys, values 2^values times what the f16 tiles hold.
+struct Powers {
+  int keys, values;
+};
+__device__ __forceinline__ Powers powers_of(int2 most, int w_keys, int w_values, int log2_r) {
+  const int c = most.x == 0 ? -300 : exponent_above(most.x) + log2_r, k = most.y == 0 ? -300 : exponent_above(most.y);
+  const int above = max(w_keys == 0 ? -300 : c + exponent_above(w_keys), k);
+  const int values = w_values == 0 ? -300 : c + exponent_above(w_values);
+  return Powers{min(max(above - 15, -120), 120), min(max(values - 15, -120), 120)};
+}
+__device__ __forceinline__ float power(int e) { return __uint_as_float(uint32_t(127 + e) << 23); }   // |e| <= 126
+
+// The greater of two pairs of 16 bits; a wave's greatest 16 bits.
+__device__ __forceinline__ uint32_t most_pairs(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(ushort2_, a), __builtin_bit_cast(ushort2_, b)));
+}
+__device__ __forceinline__ int most_half(uint32_t m) { return int(max(m & 0xFFFFu, m >> 16)); }
+__device__ __forceinline__ int wave_most(int m) {
+#pragma unroll
+  for (int step = 32; step > 0; step >>= 1) m = max(m, __shfl_xor(m, step));
+  return m;
+}
+// Maxima that many work-groups raise at once: the work-groups of an XCD (as they are dealt) have
+// a slot of their own.  One line for all had the 10,000 work-groups of 40,000 tokens wait for
+// each other: 43 us.
+constexpr int kSlots = 8;
+__device__ __forceinline__ int2 most_of_slots(const PromptArgs& a, int b, int lane) {
+  int2 m = a.most[(lane & (kSlots - 1)) * a.slot + b];
+#pragma unroll
+  for (int step = kSlots / 2; step > 0; step >>= 1) {
+    m.x = max(m.x, __shfl_xor(m.x, step));
+    m.y = max(m.y, __shfl_xor(m.y, step));
+  }
+  return m;                                            // of the lane's eight, which ask for one b
+}
+
+__device__ __forceinline__ uint32_t pair_half(float a, float b) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((floatx2{a, b}), half2));
+}
 
 __device__ __forceinline__ int wave_scan(int x, int lane) {
 #pragma unroll
@@ -93,6 +150,8 @@ __global__ __launch_bounds__(1024) void prompt_plan(PromptArgs a) {
   __shared__ int row_end[N], tok_end[N], lo_of[N], n_of[N], len_of[N], kv_of[N];
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   for (int i = tid; i < kBins; i += N) bins[i] = 0;
+  for (int i = tid; i < kSlots * a.slot; i += N) a.most[i] = make_int2(0, 0);
+  if (tid < 2) a.counts[2 + tid] = 0;
   const int most = (a.max_context + kTok - 1) / kTok + 1;
   int all_toks = 0, all_rows = 0;         // of the round's sequences
   // two walks over the sequences, 1024 at a time: the first counts row tiles by their
@@ -147,7 +206,7 @@ __global__ __launch_bounds__(1024) void prompt_plan(PromptArgs a) {
         const int bin = kBins - 1 - int(int64_t((max(last, 0) + kTok - 1) / kTok) * kBins / most);
         const int at = atomicAdd(&bins[bin], 1);
         if (walk == 1 && at < a.q_tiles)
-          a.rows[at] = RowTile{lo_of[s] + i * kRows, min(kRows, n_s - i * kRows), kv_of[s], T_s - n_s + i * kRows};
+          a.rows[at] = RowTile{lo_of[s] + i * kRows, min(kRows, n_s - i * kRows), kv_of[s], T_s - n_s + i * kRows, b0 + s, {0, 0, 0}};
       }
       if (walk == 1)
         for (int x = tid; x < all_toks; x += N) {
@@ -185,13 +244,42 @@ struct GatherArgs {
   const int32_t* page_table;
   int32_t max_pages, r, p;
   bf16* c;                                // [tiles * 64][r]
-  uint8_t* rope;                          // [tiles][64 rows of p], in LDS places
+  uint8_t* rope;                          // [tiles][64 rows of p], in LDS places; bf16 here, f16 after prompt_expand
+  const void *W_keys, *W_values;
+  int64_t factor_pieces;                  // 16-byte pieces of a factor
+  int32_t factor_groups;                  // work-groups that look for its greatest element
 };
+constexpr int kFactorPieces = 4;          // 16-byte pieces a lane
 
 // 16 tokens a work-group.
 template <bool C8>
 __global__ __launch_bounds__(256) void prompt_gather(PromptArgs a, GatherArgs s) {
   __shared__ uint32_t odd;
+  __shared__ int most[2][4];
+  if (int(blockIdx.x) >= 4 * a.kv_tiles) {             // the factors' greatest elements
+    const int id = blockIdx.x - 4 * a.kv_tiles, which = id >= s.factor_groups, g = id - (which ? s.factor_groups : 0);
+    const u32x4* W = reinterpret_cast<const u32x4*>(which ? s.W_values : s.W_keys);
+    uint32_t m = 0;
+    u32x4 x[kFactorPieces];
+#pragma unroll
+    for (int k = 0; k < kFactorPieces; ++k) {
+      const int64_t i = (int64_t(g) * kFactorPieces + k) * 256 + threadIdx.x;
+      x[k] = u32x4{0u, 0u, 0u, 0u};
+      if (i < s.factor_pieces) x[k] = W[i];
+    }
+#pragma unroll
+    for (int k = 0; k < kFactorPieces; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {                    // one that is not finite spoils its head's coordinate anyway
+        const bool bad = (((x[k][e] & 0x7F807F80u) + 0x00800080u) & 0x80008000u) != 0;
+        m = most_pairs(m, bad ? 0u : x[k][e] & 0x7FFF7FFFu);
+      }
+    most[0][threadIdx.x >> 6] = wave_most(most_half(m));
+    __syncthreads();
+    if (threadIdx.x == 0)
+      atomicMax(&a.counts[2 + which], max(max(most[0][0], most[0][1]), max(most[0][2], most[0][3])));
+    return;
+  }
   const int tile = blockIdx.x >> 2, t0 = (blockIdx.x & 3) * 16, tid = threadIdx.x;
   if (tile >= a.counts[1]) return;
   const int2 at = a.toks[tile];
@@ -201,6 +289,7 @@ __global__ __launch_bounds__(256) void prompt_gather(PromptArgs a, GatherArgs s)
   const int have = page < 0 ? 0 : min(T, kTok) - t0;   // of the 16
   if (tid == 0) odd = 0;
   __syncthreads();
+  uint32_t most_c = 0, most_k = 0;
   const int w = s.r + s.p, per = C8 ? 16 : 8, pieces = w / per, g = joint_gcd16(pieces);
   const int rg = joint_gcd16(s.p / 8);
   const uint8_t* src = s.pool + int64_t(max(page, 0)) * s.page_bytes;
@@ -240,6 +329,12 @@ __global__ __launch_bounds__(256) void prompt_gather(PromptArgs a, GatherArgs s)
 #pragma unroll
     for (int e = 0; e < (C8 ? 2 : 1); ++e) {
       const int j = col + 8 * e;
+      const uint32_t m = most_pairs(most_pairs(x[e][0] & 0x7FFF7FFFu, x[e][1] & 0x7FFF7FFFu),
+                                    most_pairs(x[e][2] & 0x7FFF7FFFu, x[e][3] & 0x7FFF7FFFu));
+      if (j < s.r)
+        most_c = most_pairs(most_c, m);
+      else
+        most_k = most_pairs(most_k, m);
       if (j < s.r)
         *reinterpret_cast<u32x4*>(s.c + (int64_t(tile) * kTok + t) * s.r + j) = x[e];
       else
@@ -247,8 +342,13 @@ __global__ __launch_bounds__(256) void prompt_gather(PromptArgs a, GatherArgs s)
                                   (((j - s.r) / 8) ^ joint_swap(rg, t)) * 16) = x[e];
     }
   }
+  most[0][tid >> 6] = wave_most(most_half(most_c));
+  most[1][tid >> 6] = wave_most(most_half(most_k));
   __syncthreads();
   if (tid == 0) {
+    int2* most_at = a.most + (blockIdx.x & (kSlots - 1)) * a.slot + at.x;
+    atomicMax(&most_at->x, max(max(most[0][0], most[0][1]), max(most[0][2], most[0][3])));
+    if (s.p > 0) atomicMax(&most_at->y, max(max(most[1][0], most[1][1]), max(most[1][2], most[1][3])));
     a.odd[tile * 4 + t0 / 16] = uint16_t(odd);
     a.there[tile * 4 + t0 / 16] = uint16_t(have >= 16 ? 0xFFFFu : have > 0 ? (1u << have) - 1u : 0u);
   }
@@ -282,16 +382,15 @@ __device__ __forceinline__ void expand_stage(floatx4 (&acc)[ROWS][COLS], const u
 }
 
 template <int D, int NT>
-__global__ __launch_bounds__(512) void prompt_expand(const int32_t* __restrict__ counts,
-                                                     const bf16* __restrict__ c, const bf16* __restrict__ W_keys,
+__global__ __launch_bounds__(512) void prompt_expand(PromptArgs a, const bf16* __restrict__ c, const bf16* __restrict__ W_keys,
                                                      const bf16* __restrict__ W_values, int heads, int r,
-                                                     int kv_tiles, uint8_t* __restrict__ keys,
-                                                     uint8_t* __restrict__ values) {
+                                                     int p, uint8_t* __restrict__ rope,
+                                                     uint8_t* __restrict__ keys, uint8_t* __restrict__ values) {
   constexpr int TOK = 32 * NT, BUF = (TOK + 256) * 128;
   __shared__ __align__(1024) unsigned char smem[2 * BUF];
   const int tiles = D == 128 ? heads : (heads + 1) / 2;  // of 256 coordinates
   const int f = blockIdx.x % tiles, blk = blockIdx.x / tiles;
-  const int n_tiles = counts[1];
+  const int n_tiles = a.counts[1], kv_tiles = a.kv_tiles;
   if (blk * TOK >= n_tiles * kTok) return;
   const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lq = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -327,6 +426,30 @@ __global__ __launch_bounds__(512) void prompt_expand(const int32_t* __restrict__
       expand_stage(acc, buf + rows, buf + cols, lr, lq);
     }
   };
+  // powers of the block's tiles, in lanes 8 i .. 8 i + 7
+  constexpr int BT = TOK / kTok;
+  const int my_tile = blk * BT + ((lane >> 3) & (BT - 1));
+  const Powers pw = powers_of(most_of_slots(a, a.toks[min(my_tile, n_tiles - 1)].x, lane), a.counts[2], a.counts[3],
+                              31 - __builtin_clz(r));
+  // of the block's position keys, which become f16 in place, a share for each of its work-groups
+  const int per = kTok * p / 8, pieces = min(BT, n_tiles - blk * BT) * per;
+  u32x4* rope_at = reinterpret_cast<u32x4*>(rope) + int64_t(blk) * BT * per;
+  u32x4 first = {};
+  if (f * 512 + tid < pieces) first = rope_at[f * 512 + tid];
+  constexpr int WT = NT >= 4 ? NT / 4 : 1;
+  float down[WT];                                      // 2^-e of this wave's tiles
+#pragma unroll
+  for (int i = 0; i < WT; ++i)
+    down[i] = power(-__shfl(value ? pw.values : pw.keys, 8 * (wt * (16 * NT) / kTok + i)));
+  for (int i = f * 512 + tid; i < pieces; i += tiles * 512) {   // whole waves
+    u32x4 y = first;
+    if (i >= tiles * 512) y = rope_at[i];
+    const float by = power(-__shfl(pw.keys, 8 * (i / per)));
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      y[e] = pair_half(__uint_as_float(y[e] << 16) * by, __uint_as_float(y[e] & 0xFFFF0000u) * by);
+    rope_at[i] = y;
+  }
   // a lane holds rows 16 i + 4 lq + v of column 16 j + lr; pieces 4 s + lq of a column hold
   // its rows 32 s + 4 lq + 0 .. 3 and 32 s + 16 + 4 lq + 0 .. 3
   const int64_t tile0 = int64_t(min(head, heads - 1)) * kv_tiles;
@@ -348,9 +471,10 @@ __global__ __launch_bounds__(512) void prompt_expand(const int32_t* __restrict__
       uint8_t* out = keys + (tile0 + (tok >> 6)) * (kTok * D * 2) + (tok & 63) * (D * 2);
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-        const floatx4 lo = acc[2 * s][j], hi = acc[2 * s + 1][j];
+        const floatx4 lo = acc[2 * s][j] * down[j / 4], hi = acc[2 * s + 1][j] * down[j / 4];
         *reinterpret_cast<u32x4*>(out + ((4 * (s0 + s) + lq) ^ joint_swap(KG, tok & 63)) * 16) =
-            u32x4{pair(lo[0], lo[1]), pair(lo[2], lo[3]), pair(hi[0], hi[1]), pair(hi[2], hi[3])};
+            u32x4{pair_half(lo[0], lo[1]), pair_half(lo[2], lo[3]), pair_half(hi[0], hi[1]),
+                  pair_half(hi[2], hi[3])};
       }
     }
   } else {
@@ -367,15 +491,16 @@ __global__ __launch_bounds__(512) void prompt_expand(const int32_t* __restrict__
 #pragma unroll
       for (int s = 0; s < NT / 2; ++s) {
         const int tok = tok0 + 32 * s;
-        floatx4 lo = acc[2 * s][j], hi = acc[2 * s + 1][j];
+        floatx4 lo = acc[2 * s][j] * down[s / 2], hi = acc[2 * s + 1][j] * down[s / 2];
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {                  // a weight of 0 times an infinity would be none
-          lo[v] = fminf(fmaxf(lo[v], -kMaxBf16), kMaxBf16);
-          hi[v] = fminf(fmaxf(hi[v], -kMaxBf16), kMaxBf16);
+        for (int v = 0; v < 4; ++v) {                  // a weight of 0 times an overflow would be none
+          lo[v] = fminf(fmaxf(lo[v], -kMaxHalf), kMaxHalf);
+          hi[v] = fminf(fmaxf(hi[v], -kMaxHalf), kMaxHalf);
         }
         *reinterpret_cast<u32x4*>(values + (tile0 + (tok >> 6)) * (kTok * D * 2) + col * (kTok * 2) +
                                   ((4 * (tok >> 5 & 1) + lq) ^ joint_swap(8, col)) * 16) =
-            u32x4{pair(lo[0], lo[1]), pair(lo[2], lo[3]), pair(hi[0], hi[1]), pair(hi[2], hi[3])};
+            u32x4{pair_half(lo[0], lo[1]), pair_half(lo[2], lo[3]), pair_half(hi[0], hi[1]),
+                  pair_half(hi[2], hi[3])};
       }
     }
   }
@@ -392,15 +517,15 @@ __device__ __forceinline__ void reads_ahead() {
 }
 
 __device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c) {
-  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b),
-                                                 c, 0, 0, 0);
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, a), __builtin_bit_cast(half8, b), c, 0, 0,
+                                                0);
 }
 
 template <int D, int P>
 __global__ __launch_bounds__(256, 2) void prompt_attend(PromptArgs a, const uint8_t* __restrict__ keys,
                                                         const uint8_t* __restrict__ rope,
                                                         const uint8_t* __restrict__ values,
-                                                        const bf16* __restrict__ q, int heads, float scale,
+                                                        const bf16* __restrict__ q, int heads, int r, float scale,
                                                         bf16* __restrict__ out) {
   constexpr int KB = kTok * D * 2, PB = kTok * P * 2, TILE = 2 * KB + PB;
   constexpr int KL = KB / 1024, PL = PB / 1024;        // 1 KB loads
@@ -455,13 +580,38 @@ __global__ __launch_bounds__(256, 2) void prompt_attend(PromptArgs a, const uint
 #pragma unroll
   for (int i = 0; i < PS; ++i) qp[i] = *reinterpret_cast<const u32x4*>(qrow + D + 16 * i + 8 * h);
 
+  // in f16, times a power of two that brings the row's greatest below 2^15
+  uint32_t most = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+#pragma unroll
+    for (int i = 0; i < DS; ++i) most = most_pairs(most, qd[i][e] & 0x7FFF7FFFu);
+#pragma unroll
+    for (int i = 0; i < PS; ++i) most = most_pairs(most, qp[i][e] & 0x7FFF7FFFu);
+  }
+  const auto halves = __builtin_amdgcn_permlane32_swap(most, most, false, false);
+  most = most_pairs(halves[0], halves[1]);             // a row that is not finite becomes NaN whatever its power is
+  const int up = min(max(15 - exponent_above(most_half(most)), -120), 120);
+  auto to_half = [&](u32x4& x) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      x[e] = pair_half(__uint_as_float(x[e] << 16) * power(up), __uint_as_float(x[e] & 0xFFFF0000u) * power(up));
+  };
+#pragma unroll
+  for (int i = 0; i < DS; ++i) to_half(qd[i]);
+#pragma unroll
+  for (int i = 0; i < PS; ++i) to_half(qp[i]);
+  const Powers pw = powers_of(most_of_slots(a, rt.b, lane), a.counts[2], a.counts[3], 31 - __builtin_clz(r));
+  // from products to scores in powers of two; past the ends all weigh alike, or one alone weighs
+  const float fs = fminf(fmaxf(ldexpf(scale, pw.keys - up), 0x1p-100f), 0x1p100f);
+
   f32x16 acc[CT];
 #pragma unroll
   for (int i = 0; i < CT; ++i)
 #pragma unroll
     for (int v = 0; v < 16; ++v) acc[i][v] = 0.f;
   float m = -INFINITY, l = 0.f;
-  const float slack = kSlack / scale;
+  const float slack = kSlack / fs;
   const int ksw = joint_swap(KG, lr), psw = P > 0 ? joint_swap(PG, lr) : 0, vsw = joint_swap(8, lr);
 
   for (int t = 0; t < tiles; ++t) {
@@ -513,7 +663,7 @@ __global__ __launch_bounds__(256, 2) void prompt_attend(PromptArgs a, const uint
     top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
     if (__any(top > m + slack)) {
       const float m_new = fmaxf(m, top);
-      const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - m_new) * scale);
+      const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - m_new) * fs);
       l *= keep;
       if (t > 0) {
 #pragma unroll
@@ -523,18 +673,18 @@ __global__ __launch_bounds__(256, 2) void prompt_attend(PromptArgs a, const uint
       }
       m = m_new;
     }
-    const float mb = m == -INFINITY ? 0.f : m * scale;
+    const float mb = m == -INFINITY ? 0.f : m * fs - kRaise;
     u32x4 p[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k)                        // step k: tokens 32 n + 8 b + 4 h and 16 further, b = k % 2
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int n = k >> 1, v = 4 * (k & 1) + 8 * (e >> 1) + 2 * (e & 1);
-        const float x = __builtin_amdgcn_exp2f(fmaf(s[n][v], scale, -mb));
-        const float y = __builtin_amdgcn_exp2f(fmaf(s[n][v + 1], scale, -mb));
+        const float x = __builtin_amdgcn_exp2f(fmaf(s[n][v], fs, -mb));
+        const float y = __builtin_amdgcn_exp2f(fmaf(s[n][v + 1], fs, -mb));
         l += x;
         l += y;
-        p[k][e] = pair(x, y);
+        p[k][e] = pair_half(x, y);
       }
     // ---- output: coordinate 32 i + lr of the A operand, piece 2 k + h of its tokens
     const unsigned char* vb = buf + KB + PB + lr * (kTok * 2);
@@ -549,7 +699,7 @@ __global__ __launch_bounds__(256, 2) void prompt_attend(PromptArgs a, const uint
   l += __shfl_xor(l, 32);
   if (my >= rt.n) return;
   bf16* dst = out + (row * heads + head) * D + 4 * h;
-  const float inv = rt.kv < 0 ? __builtin_nanf("") : l == 0.f ? 0.f : 1.f / l;
+  const float inv = rt.kv < 0 ? __builtin_nanf("") : l == 0.f ? 0.f : ldexpf(1.f / l, pw.values);
 #pragma unroll
   for (int i = 0; i < CT; ++i)
 #pragma unroll
@@ -577,7 +727,9 @@ JointPrompt joint_prompt(const dckv_joint_desc& d, int32_t batch, int32_t n_rows
   s.kv_tiles = (s.kv_tiles + 3) / 4 * 4;               // whole blocks of 256 tokens
   const size_t kv = size_t(s.kv_tiles);
   s.off_qtile = 256;
-  s.off_kvtile = s.off_qtile + align_up(size_t(s.q_tiles) * sizeof(RowTile));
+  s.off_most = s.off_qtile + align_up(size_t(s.q_tiles) * sizeof(RowTile));
+  s.slot = (batch + 15) / 16 * 16;
+  s.off_kvtile = s.off_most + align_up(size_t(kSlots) * s.slot * sizeof(int2));
   s.off_flags = s.off_kvtile + align_up(kv * sizeof(int2));
   s.off_c = s.off_flags + 2 * align_up(kv * sizeof(uint2));
   s.off_rope = s.off_c + align_up(kv * kTok * d.rank * 2);
@@ -606,6 +758,8 @@ hipError_t launch_joint_prefill(const JointPrompt& s, const void* q, const int32
   a.counts = reinterpret_cast<int32_t*>(ws);
   a.rows = reinterpret_cast<RowTile*>(ws + s.off_qtile);
   a.toks = reinterpret_cast<int2*>(ws + s.off_kvtile);
+  a.most = reinterpret_cast<int2*>(ws + s.off_most);
+  a.slot = s.slot;
   a.there = reinterpret_cast<uint16_t*>(ws + s.off_flags);
   a.odd = reinterpret_cast<uint16_t*>(ws + s.off_flags + (s.off_c - s.off_flags) / 2);
   hipLaunchKernelGGL(prompt_plan, dim3(1), dim3(1024), 0, stream, a);
@@ -616,12 +770,15 @@ hipError_t launch_joint_prefill(const JointPrompt& s, const void* q, const int32
   uint8_t* values = reinterpret_cast<uint8_t*>(ws + s.off_v);
   bf16* c = reinterpret_cast<bf16*>(ws + s.off_c);
   if (s.kv_tiles > 0) {
+    const int64_t pieces = int64_t(d.num_heads) * d.head_dim * d.rank / 8;
+    const int32_t groups = int32_t((pieces + 256 * kFactorPieces - 1) / (256 * kFactorPieces));
     const GatherArgs ga{static_cast<const uint8_t*>(pool), num_pages, joint_page_bytes(d), page_table, max_pages,
-                        d.rank, d.rope_dim, c, rope};
+                        d.rank, d.rope_dim, c, rope, W_keys, W_values, pieces, groups};
+    const dim3 grid(uint32_t(s.kv_tiles) * 4 + 2 * uint32_t(groups));
     if (d.cache == DCKV_JOINT_E4M3)
-      hipLaunchKernelGGL((prompt_gather<true>), dim3(uint32_t(s.kv_tiles) * 4), dim3(256), 0, stream, a, ga);
+      hipLaunchKernelGGL((prompt_gather<true>), grid, dim3(256), 0, stream, a, ga);
     else
-      hipLaunchKernelGGL((prompt_gather<false>), dim3(uint32_t(s.kv_tiles) * 4), dim3(256), 0, stream, a, ga);
+      hipLaunchKernelGGL((prompt_gather<false>), grid, dim3(256), 0, stream, a, ga);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
     // 256 coordinates a work-group, and 256 tokens where that fills the chip, else 64: ... 
@@ -629,8 +786,8 @@ hipError_t launch_joint_prefill(const JointPrompt& s, const void* q, const int32
     const bool wide = s.kv_tiles / 4 * coords >= 256;
 #define DCKV_GO(D, NT)                                                                                      \
   hipLaunchKernelGGL((prompt_expand<D, NT>), dim3(uint32_t(s.kv_tiles / (NT / 2) * coords)), dim3(512), 0,   \
-                     stream, a.counts, c, static_cast<const bf16*>(W_keys),                                  \
-                     static_cast<const bf16*>(W_values), d.num_heads, d.rank, a.kv_tiles, keys, values)
+                     stream, a, c, static_cast<const bf16*>(W_keys), static_cast<const bf16*>(W_values),     \
+                     d.num_heads, d.rank, d.rope_dim, rope, keys, values)
     if (d.head_dim == 128) {
       if (wide)
         DCKV_GO(128, 8);
@@ -649,7 +806,7 @@ hipError_t launch_joint_prefill(const JointPrompt& s, const void* q, const int32
   const float scale = kLog2e * (d.scale != 0.f ? d.scale : 1.f / std::sqrt(float(d.head_dim + d.rope_dim)));
 #define DCKV_GO(D, P)                                                                                        \
   hipLaunchKernelGGL((prompt_attend<D, P>), dim3(uint32_t(s.q_tiles) * d.num_heads), dim3(256), 0, stream, a, \
-                     keys, rope, values, static_cast<const bf16*>(q), d.num_heads, scale,                     \
+                     keys, rope, values, static_cast<const bf16*>(q), d.num_heads, d.rank, scale,                     \
                      static_cast<bf16*>(out));                                                                \
   return hipGetLastError()
   if (d.head_dim == 128) {
