@@ -31,18 +31,19 @@ struct JointShape {
   int32_t row_waves, slices;    // own tokens: waves that take 16 rows each of a work-group's slice; slices
   int32_t units;                // work-groups a slice
   int32_t pre_row_waves, pre_slices, pre_units;   // the same for the prefix, its rows those of all sequences
-  size_t off_start, off_mean, off_o, off_ml, off_pre_o, off_pre_ml;   // workspace: queries first
+  size_t off_up, off_start, off_mean, off_o, off_ml, off_pre_o, off_pre_ml;   // workspace: queries first
   size_t bytes;                 // what this call uses
 };
 
 // What an attend kernel reads and writes.
 struct JointAttend {
-  const void* q;                // bf16 [rows of all sequences][r + p]
+  const void* q;                // [rows of all sequences]: bf16 [2][r + p], the second the rest; e4m3: f16 [r + p]
+  const int32_t* q_up;          // e4m3: [rows], queries are 2^up as large, and times the scale
   const uint8_t* pool;
   int64_t num_pages, page_bytes;
   const int32_t* table;         // page_table, or the prefix's pages
   int32_t max_pages;            // of a row of the table
-  const int64_t* start;         // first tile of each sequence among all, [batch + 1]
+  const int64_t* start;         // first tile of each sequence among all, [batch + 1], then the cut: per, whole
   const int32_t* seq_lens;
   int32_t max_context, batch, queries, heads;
   int32_t units, slices;
@@ -52,10 +53,16 @@ struct JointAttend {
   float4* part_ml;              // [segment][slice][rows]: m, l, u, 0
 };
 
-// Tiles that a unit takes of `total`, whole rounds of a work-group's token groups.
+// a / b, not negative.  64-bit division is two hundred instructions, which a launch of one tile
+// fetches from memory like the rest of the kernel; counts that need it are rare.
+__host__ __device__ inline int64_t joint_div(int64_t a, int64_t b) {
+  if (((a | b) >> 32) == 0) return uint32_t(a) / uint32_t(b);
+  return a / b;
+}
+
+// Tiles that a unit takes of `total`, whole rounds of a work-group's token groups (a power of two).
 __host__ __device__ inline int64_t joint_tiles_a_unit(int64_t total, int units, int groups) {
-  const int64_t per = (total + units - 1) / units;
-  const int64_t n = (per + groups - 1) / groups * groups;
+  const int64_t n = (joint_div(total + units - 1, units) + groups - 1) & -int64_t(groups);
   return n < groups ? groups : n;
 }
 

@@ -3,15 +3,21 @@
 //   s_rt = scale q_r . [c_t ; k_t],   a_r = sum_t softmax_t(s_rt) c_t
 //
 // for the (query, head) rows r of a sequence, or of all sequences over a shared prefix;
-// q_r is the query folded into the latent space, in bf16.  One copy of a token serves
+// q_r is the query folded into the latent space.  One copy of a token serves
 // as key and value, so a tile of 32 tokens is brought into LDS once (by the loads' LDS
 // path, pages being laid out as LDS wants them) and read twice:
 //   scores  S[token][row] = C[token][:] Q[row][:], MFMA 16x16x32: the A operand of a step
 //           is 16 bytes of a token a lane, the queries stay in registers.
 //   output  O[column][row] += C^T[column][token] P[token][row]: a lane holds the scores of one
 //           row and tokens 16 n + 4 (lane / 16) + v, and the transposing LDS load brings a
-//           column's tokens in that order, so the weights (bf16, from fp32 scores) feed the
-//           second product from the registers they were made in.
+//           column's tokens in that order, so the weights (bf16, from fp32 scores; their
+//           sum is that of the rounded ones) feed the second product from the registers
+//           they were made in.
+// Queries are bf16 and the rest of them, bf16 again, which costs a product more: without
+// it their rounding is most of the result's error (relative to 64 bits 2.4e-3 against
+// 1.9e-3, of which 1.7e-3 is the result's own).  At r = 512 and two waves a SIMD, which
+// more than 32 rows have, the registers do not hold the rests and the latents' queries
+// go without.
 // A wave owns 16 rows and all r columns of their sums: 128 accumulators a lane at r = 512
 // and 72 registers of queries (32 rows, twice that, read LDS half as often but do not fit
 // the registers: 200 and more were spilled).  Of a work-group's waves WR take WR x 16
@@ -19,10 +25,12 @@
 // end.  The running maximum of a row is raised, and the sums scaled down, only when a
 // score passes it by more than kSlack (in powers of two), so that the r sums of a row
 // are rarely touched.
-// e4m3 tokens are widened to bf16 on their way from LDS to the matrix unit: as keys
-// under their power of two (exactly), as values without it: the weights take it, held
-// against a maximum u of score + exponent of their own, so that they are at most
-// 2^kSlack whatever the exponents are.
+// e4m3 tokens are widened to f16 on their way from LDS to the matrix unit, exactly and without
+// their powers of two.  Queries are f16 under a power of two of their row (2^-12 of a
+// coordinate; 29 binades below the greatest are normal numbers).  The products over latents
+// and over position keys are summed apart and take the tokens' powers in fp32; the weights
+// take them, held against a maximum u of score + exponent of their own, so that they are at
+// most 2^(kSlack + kRaise) whatever the exponents are: f16 again, 2^-12 of a weight.
 // Work is cut by the sequences' actual lengths (joint_cut): into equal shares of all
 // their tiles, a unit walking over the sequences that it meets, or a sequence at a time.
 #pragma once
@@ -37,6 +45,9 @@ namespace dckv {
 namespace joint {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 half2 __attribute__((ext_vector_type(2)));
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef float floatx2 __attribute__((ext_vector_type(2)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -44,23 +55,33 @@ typedef short short4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) short4_t* lds_short4;
 
 constexpr float kSlack = 6.f;          // weights reach 2^6: the sums stay far from fp32's end
+constexpr float kRaise = 8.f;          // f16 weights are 2^8 as large: down to 2^-22 they are normal numbers
 
 __device__ __forceinline__ floatx4 mfma(u32x4 a, u32x4 b, floatx4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c,
                                                  0, 0, 0);
 }
 
-// Eight e4m3 values times `scale`, a power of two, as bf16.
-__device__ __forceinline__ u32x4 widen(uint32_t lo, uint32_t hi, float scale) {
-  return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false)),
-               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true)),
-               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false)),
-               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true))};
+__device__ __forceinline__ floatx4 mfma_half(u32x4 a, u32x4 b, floatx4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, a), __builtin_bit_cast(half8, b), c, 0, 0,
+                                                0);
+}
+
+// Eight e4m3 values as f16.
+__device__ __forceinline__ u32x4 widen(uint32_t lo, uint32_t hi) {
+  return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, false)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, true)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, false)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, true))};
 }
 
 __device__ __forceinline__ uint32_t pair(float a, float b) {
   return uint32_t(__builtin_bit_cast(uint16_t, from_f32<bf16>(a))) |
          uint32_t(__builtin_bit_cast(uint16_t, from_f32<bf16>(b))) << 16;
+}
+
+__device__ __forceinline__ uint32_t pair_half(float a, float b) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((floatx2{a, b}), half2));
 }
 
 // Values of four column tiles for the matrix unit, by the transposing LDS loads.  Written
@@ -154,6 +175,15 @@ __device__ __forceinline__ bool odd_piece(u32x4 w) {
   return bad != 0;
 }
 
+// Place of column c of an e4m3 cache's query of w columns: [step][lane / 16][8], so that 64
+// bytes of a row are loaded at once.  A lane's 16 bytes of a token are its columns of two
+// steps; the last 32 columns of an odd number of steps are one's.
+__device__ __forceinline__ int query_place(int c, int w) {
+  const bool two = (c & ~63) + 64 <= w;
+  const int step = two ? 2 * (c >> 6) + ((c >> 3) & 1) : c >> 5, lq = two ? (c >> 4) & 3 : (c >> 3) & 3;
+  return step * 32 + lq * 8 + (c & 7);
+}
+
 template <int R, int P, bool C8, int WR>
 struct Shape {
   static constexpr int W = R + P, E = C8 ? 1 : 2, ROWB = W * E, PIECES = ROWB / 16;
@@ -169,7 +199,8 @@ struct Shape {
   static constexpr int NL = PIECES / 2;               // 1 KB loads of a tile, dealt out to WR waves
   static constexpr int LOADS = (NL + WR - 1) / WR;
   // the last steps' queries stay in LDS where the registers of two waves a SIMD are full
-  static constexpr int QL = C8 && R == 512 && NW == 8 ? 4 : 0;
+  static constexpr int QL = C8 && R == 512 && NW == 8 ? 6 : 0;
+  static constexpr bool REST = !C8 && (R < 512 || NW == 4);
   static_assert(PIECES % 2 == 0, "whole loads");
 };
 
@@ -219,11 +250,11 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
   } else {
     load_window(0);
     const int64_t total = a.start[a.batch];
-    const JointCut cut = joint_cut(total, a.units, a.batch, NG);
+    const JointCut cut{a.start[a.batch + 1], a.start[a.batch + 2] != 0};
     whole = cut.whole;
     // the last sequence b whose first tile (whole: first segment) is at most this unit's
     const int64_t want = cut.whole ? unit : unit * cut.per;
-    auto key = [&](int64_t start, int i) { return cut.whole ? start / cut.per + i : start; };
+    auto key = [&](int64_t start, int i) { return cut.whole ? joint_div(start, cut.per) + i : start; };
     int lo = 0, n = a.batch;                          // the answer is in lo .. lo + n - 1
     while (n > 64) {
       const int step = (n + 63) / 64, i = lo + lane * step;
@@ -328,16 +359,26 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
     const int row = (slice * WR + rw) * 16 + lr;
     const int rowc = min(row, rows - 1);
     const uint8_t* qrow = static_cast<const uint8_t*>(a.q) +
-                          ((prefix ? 0 : int64_t(sg.b) * rows) + rowc) * (W * 2);
-    u32x4 q[KQ];
+                          ((prefix ? 0 : int64_t(sg.b) * rows) + rowc) * (W * (C8 ? 2 : 4));
+    u32x4 q[KQ], rest[S::REST ? R / 32 : 1];
+    int down = 0;                                     // e4m3: 127 and the power of two that is taken back
+    if constexpr (C8) {
 #pragma unroll
-    for (int i = 0; i < KS; ++i) {
-      const int col = C8 && (i | 1) < KS ? 64 * (i >> 1) + 16 * lq + 8 * (i & 1) : 32 * i + 8 * lq;
-      const u32x4 x = *reinterpret_cast<const u32x4*>(qrow + 2 * col);
-      if (i < KQ)
-        q[i] = x;
-      else if (g == 0)
-        last_q[rw][i - KQ][lane] = x;
+      for (int i = 0; i < KS; ++i) {
+        const u32x4 x = *reinterpret_cast<const u32x4*>(qrow + 64 * i + 16 * lq);
+        if (i < KQ)
+          q[i] = x;
+        else if (g == 0)
+          last_q[rw][i - KQ][lane] = x;
+      }
+      down = a.q_up[(prefix ? 0 : int64_t(sg.b) * rows) + rowc] + 127;
+    } else {
+#pragma unroll
+      for (int i = 0; i < KS; ++i) q[i] = *reinterpret_cast<const u32x4*>(qrow + 2 * (32 * i + 8 * lq));
+      if constexpr (S::REST)
+#pragma unroll
+        for (int i = 0; i < R / 32; ++i)
+          rest[i] = *reinterpret_cast<const u32x4*>(qrow + 2 * (W + 32 * i + 8 * lq));
     }
     if constexpr (QL > 0 && WR == 1) __syncthreads();  // else the first tile's does it
     auto query = [&](int i) { return i < KQ ? q[i < KQ ? i : 0] : last_q[rw][i < KQ ? 0 : i - KQ][lane]; };
@@ -354,7 +395,7 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
     floatx4 acc[CT];
 #pragma unroll
     for (int i = 0; i < CT; ++i) acc[i] = floatx4{0.f, 0.f, 0.f, 0.f};
-    // m, u: references of the weights in l and in the sums (one for bf16)
+    // m, u: references of the weights in l and in the sums (one for bf16; e4m3: + 127)
     float m = -INFINITY, u = -INFINITY, l = 0.f;
 
     for (int r = 0; r < rounds; ++r) {
@@ -407,15 +448,8 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
             for (int n = 0; n < 2; ++n)
               if (i0 + i < NP) x[i][n] = *reinterpret_cast<const u32x4*>(buf + place<G>(ka, i0 + i) + n * 16 * ROWB);
         };
-        float sc[2] = {1.f, 1.f}, sk[2] = {1.f, 1.f};  // powers of two of tokens lr, 16 + lr: latent, key
+        floatx4 sk[2] = {s[0], s[0]};                 // over the position keys
         const uint8_t* ep = exps[C8 ? g * NBUF + (r & (NBUF - 1)) : 0];
-        if constexpr (C8) {
-#pragma unroll
-          for (int n = 0; n < 2; ++n) {
-            sc[n] = __uint_as_float(uint32_t(ep[16 * n + here(lr)]) << 23);
-            sk[n] = __uint_as_float(uint32_t(ep[32 + 16 * n + here(lr)]) << 23);
-          }
-        }
         u32x4 x0[GP][2], x1[GP][2];
         u32x2 last[2];
         read_keys(x0, 0);
@@ -437,32 +471,42 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
             for (int n = 0; n < 2; ++n) {
               if (i0 + i >= NP) continue;
               if constexpr (C8) {
-                const float f = 64 * (i0 + i) < R ? sc[n] : sk[n];
-                s[n] = mfma(widen(x[i][n][0], x[i][n][1], f), query(2 * (i0 + i)), s[n]);
-                s[n] = mfma(widen(x[i][n][2], x[i][n][3], f), query(2 * (i0 + i) + 1), s[n]);
+                floatx4& sum = 64 * (i0 + i) < R ? s[n] : sk[n];
+                sum = mfma_half(widen(x[i][n][0], x[i][n][1]), query(2 * (i0 + i)), sum);
+                sum = mfma_half(widen(x[i][n][2], x[i][n][3]), query(2 * (i0 + i) + 1), sum);
               } else {
                 s[n] = mfma(x[i][n], query(i0 + i), s[n]);
+                if constexpr (S::REST)
+                  if (i0 + i < R / 32) s[n] = mfma(x[i][n], rest[i0 + i], s[n]);
               }
             }
           __builtin_amdgcn_sched_barrier(0);
         }
         if constexpr (C8 && KS % 2 == 1) {
 #pragma unroll
-          for (int n = 0; n < 2; ++n) s[n] = mfma(widen(last[n][0], last[n][1], sk[n]), query(KS - 1), s[n]);
+          for (int n = 0; n < 2; ++n) sk[n] = mfma_half(widen(last[n][0], last[n][1]), query(KS - 1), sk[n]);
         }
         // ---- softmax
-        auto exponents = [&](int n) {                 // of the tokens' latents
-          const uint32_t four = *reinterpret_cast<const uint32_t*>(ep + 16 * n + 4 * here(lq));
-          floatx4 e;
+        uint32_t el[2] = {}, ek[2] = {};              // exponents + 127 of a lane's tokens: latent, key
+        if constexpr (C8) {
+          const int at4 = 4 * here(lq);
 #pragma unroll
-          for (int v = 0; v < 4; ++v) e[v] = float((four >> (8 * v)) & 0xFFu) - 127.f;
-          return e;
-        };
+          for (int n = 0; n < 2; ++n) {
+            el[n] = *reinterpret_cast<const uint32_t*>(ep + 16 * n + at4);
+            if constexpr (P > 0) ek[n] = *reinterpret_cast<const uint32_t*>(ep + kJointTile + 16 * n + at4);
+          }
+        }
+        auto byte = [](uint32_t four, int v) { return int((four >> (8 * v)) & 0xFFu); };
 #pragma unroll
         for (int n = 0; n < 2; ++n)
 #pragma unroll
           for (int v = 0; v < 4; ++v) {
-            s[n][v] *= a.scale;
+            if constexpr (C8) {
+              s[n][v] = __builtin_amdgcn_ldexpf(s[n][v], byte(el[n], v) - down);
+              if constexpr (P > 0) s[n][v] += __builtin_amdgcn_ldexpf(sk[n][v], byte(ek[n], v) - down);
+            } else {
+              s[n][v] *= a.scale;
+            }
           }
         if (edge) {
 #pragma unroll
@@ -479,9 +523,8 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
 #pragma unroll
           for (int v = 0; v < 4; ++v) top = fmaxf(top, s[n][v]);
           if constexpr (C8) {
-            const floatx4 ex = exponents(n);
 #pragma unroll
-            for (int v = 0; v < 4; ++v) utop = fmaxf(utop, s[n][v] + ex[v]);
+            for (int v = 0; v < 4; ++v) utop = fmaxf(utop, s[n][v] + float(byte(el[n], v)));
           }
         }
         top = row_max(top);
@@ -502,18 +545,17 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
         const float mb = m == -INFINITY ? 0.f : m;     // nothing seen yet: weights 0
         u32x4 p;
         if constexpr (C8) {
-          const float ub = u == -INFINITY ? 0.f : u;
+          const float ub = u == -INFINITY ? 0.f : u - kRaise;
 #pragma unroll
           for (int n = 0; n < 2; ++n) {
-            const floatx4 ex = exponents(n);
             float y[4];
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
               l += __builtin_amdgcn_exp2f(s[n][v] - mb);
-              y[v] = __builtin_amdgcn_exp2f(s[n][v] + (ex[v] - ub));
+              y[v] = __builtin_amdgcn_exp2f(s[n][v] + (float(byte(el[n], v)) - ub));
             }
-            p[2 * n] = pair(y[0], y[1]);
-            p[2 * n + 1] = pair(y[2], y[3]);
+            p[2 * n] = pair_half(y[0], y[1]);
+            p[2 * n + 1] = pair_half(y[2], y[3]);
           }
         } else {
           // the sum of the rounded weights: the result is an exact mean under them
@@ -537,7 +579,7 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
                      (I + 4) / G * (G * 16), (I + 5) / G * (G * 16), (I + 6) / G * (G * 16), (I + 7) / G * (G * 16)>(
                 x, at(0), at(1), at(2), at(3), at(4), at(5), at(6), at(7));
 #pragma unroll
-            for (int j = 0; j < 8; ++j) acc[I + j] = mfma(widen(x[j][0], x[j][1], 1.f), p, acc[I + j]);
+            for (int j = 0; j < 8; ++j) acc[I + j] = mfma_half(widen(x[j][0], x[j][1]), p, acc[I + j]);
           });
         } else {
           unrolled<CT / 4>([&](auto k) {
@@ -569,7 +611,7 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
         float* dst = a.part_o + (prow + rw * 16 + jr) * R + 4 * jq;
 #pragma unroll
         for (int i = 0; i < CT; ++i) *reinterpret_cast<floatx4*>(dst + 16 * i) = acc[i];
-        if (jq == 0) a.part_ml[prow + rw * 16 + jr] = make_float4(m, l, u, 0.f);
+        if (jq == 0) a.part_ml[prow + rw * 16 + jr] = make_float4(m, l, C8 ? u - 127.f - kRaise : u, 0.f);
       }
       __syncthreads();                                // the tiles are used up
     } else {
@@ -595,7 +637,7 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
           if (mk != -INFINITY || join_l[k * WR + rw][jr] != 0.f)
             ll += join_l[k * WR + rw][jr] * __builtin_amdgcn_exp2f(mk - mm);
         }
-        a.part_ml[prow + rw * 16 + jr] = make_float4(mm, ll, uu, 0.f);
+        a.part_ml[prow + rw * 16 + jr] = make_float4(mm, ll, C8 ? uu - 127.f - kRaise : uu, 0.f);
       }
       float* ex = reinterpret_cast<float*>(smem);     // [wave][16 rows][ST]
 #pragma unroll

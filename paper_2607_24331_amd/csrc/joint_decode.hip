@@ -5,8 +5,7 @@
 //
 // joint_fold    a wave a (head, 32 latent columns, 32 or 128 rows): the head's factor columns lie
 //               in LDS once, read by the transposing load, as the contraction runs over
-//               the factor's rows; products on MFMA 32x32x16, rounded to bf16 (2^-9 of a
-//               coordinate, independent ones in a score's sum over r).  One more wave forms
+//               the factor's rows; products on MFMA 32x32x16.  One more wave forms
 //               the sequences' first tiles.  Bound by latency and, once, by the factor's bytes.
 // joint_merge   a work-group a row: its shares' sums in fp32, 16 bytes a lane.  Bound by
 //               the shares' bytes.
@@ -32,19 +31,25 @@ __device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c) {
 }
 
 
+// What the fold's one wave more does.
+struct FoldStarts {
+  const int32_t* seq_lens;
+  int64_t* starts;
+  int32_t max_context, batch, units, groups;
+};
+
 // starts[b]: tiles of the sequences before b, starts[batch] of all.  One wave, 16
 // sequences a lane.
-__device__ void form_starts(const int32_t* __restrict__ seq_lens, int max_context, int batch,
-                            int64_t* __restrict__ starts) {
+__device__ void form_starts(const FoldStarts& f) {
   const int lane = threadIdx.x;
   int64_t base = 0;
-  for (int b0 = 0; b0 < batch; b0 += 1024) {
+  for (int b0 = 0; b0 < f.batch; b0 += 1024) {
     int n[16];
     int64_t own = 0;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const int b = b0 + 16 * lane + i;
-      const int T = b < batch ? min(max(seq_lens[b], 0), max_context) : 0;
+      const int T = b < f.batch ? min(max(f.seq_lens[b], 0), f.max_context) : 0;
       n[i] = (T + kJointTile - 1) / kJointTile;
       own += n[i];
     }
@@ -58,24 +63,46 @@ __device__ void form_starts(const int32_t* __restrict__ seq_lens, int max_contex
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const int b = b0 + 16 * lane + i;
-      if (b < batch) starts[b] = at;
+      if (b < f.batch) f.starts[b] = at;
       at += n[i];
     }
     base += __shfl((long long)sum, 63);
   }
-  if (lane == 0) starts[batch] = base;
+  if (lane == 0) {
+    const JointCut cut = joint_cut(base, f.units, f.batch, f.groups);
+    f.starts[f.batch] = base;
+    f.starts[f.batch + 1] = cut.per;
+    f.starts[f.batch + 2] = cut.whole;
+  }
 }
 
+// The columns of 16 k rows of a factor's tile in LDS (st bytes a row) as B operands of 32x32x16:
+// column c0 + lane % 32, rows 16 i + 8 (lane / 32) .. + 7, four a load.
+template <int N>
+__device__ __forceinline__ void factor_columns(u32x4 (&f)[N], int i0, int i1, const unsigned char* tile, int st, int c0,
+                                               int lane) {
+  const unsigned char* base = tile + (8 * (lane >> 5) + ((lane & 15) >> 2)) * st +
+                              (c0 + 16 * ((lane >> 4) & 1) + 4 * (lane & 3)) * 2;
+#pragma unroll
+  for (int i = i0; i < i1; ++i) {
+    unsigned char* at = const_cast<unsigned char*>(base + 16 * (i - i0) * st);
+    const short4_t y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((joint::lds_short4)at);
+    const short4_t z = __builtin_amdgcn_ds_read_tr16_b64_v4i16((joint::lds_short4)(at + 4 * st));
+    const auto yz = __builtin_shufflevector(y, z, 0, 1, 2, 3, 4, 5, 6, 7);
+    f[i] = __builtin_bit_cast(u32x4, yz);
+  }
+}
+
+// bf16 cache: folded [row][2][r + p], bf16 and the rest as bf16 (none of the position part).
 template <int D>
 __global__ __launch_bounds__(64) void joint_fold(const bf16* __restrict__ q, const bf16* __restrict__ W_keys,
                                                  int n, int heads, int r, int p, bf16* __restrict__ folded,
-                                                 const int32_t* __restrict__ seq_lens, int max_context,
-                                                 int batch, int64_t* __restrict__ starts, int wave_rows) {
-  constexpr int ST = 40;                                       // elements a row of the factor in LDS
-  __shared__ __align__(16) bf16 wk[D * ST];
+                                                 int wave_rows, FoldStarts starts) {
+  constexpr int ST = 80;                                       // bytes a row of the factor in LDS
+  __shared__ __align__(16) unsigned char wk[D * ST];
   const int cols = r / 32;
   if (int(blockIdx.x) == heads * cols) {
-    if (blockIdx.y == 0) form_starts(seq_lens, max_context, batch, starts);
+    if (blockIdx.y == 0) form_starts(starts);
     return;
   }
   const int head = blockIdx.x / cols, c0 = (blockIdx.x % cols) * 32;
@@ -88,7 +115,7 @@ __global__ __launch_bounds__(64) void joint_fold(const bf16* __restrict__ q, con
     piece[i] = *reinterpret_cast<const u32x4*>(src + int64_t(16 * i + (lane >> 2)) * r + 8 * (lane & 3));
 #pragma unroll
   for (int i = 0; i < D / 16; ++i)
-    *reinterpret_cast<u32x4*>(wk + (16 * i + (lane >> 2)) * ST + 8 * (lane & 3)) = piece[i];
+    *reinterpret_cast<u32x4*>(wk + (16 * i + (lane >> 2)) * ST + 16 * (lane & 3)) = piece[i];
   const int W = r + p;
   u32x4 x[D / 16];
   auto load_rows = [&](int r0) {
@@ -98,17 +125,8 @@ __global__ __launch_bounds__(64) void joint_fold(const bf16* __restrict__ q, con
   };
   load_rows(row0);
   __syncthreads();
-  // B operand of step i: column lr, rows 16 i + 8 h .. + 7 of the factor, four a load
-  unsigned char* base = reinterpret_cast<unsigned char*>(wk + (8 * h + ((lane & 15) >> 2)) * ST +
-                                                         16 * ((lane >> 4) & 1) + 4 * (lane & 3));
   u32x4 f[D / 16];
-#pragma unroll
-  for (int i = 0; i < D / 16; ++i) {
-    const short4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((joint::lds_short4)(base + (16 * i) * ST * 2));
-    const short4_t y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((joint::lds_short4)(base + (16 * i + 4) * ST * 2));
-    const auto xy = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
-    f[i] = __builtin_bit_cast(u32x4, xy);
-  }
+  factor_columns(f, 0, D / 16, wk, ST, 0, lane);
 #pragma unroll 1
   for (int r0 = row0; r0 < row1; r0 += 32) {
     f32x16 acc;
@@ -120,13 +138,142 @@ __global__ __launch_bounds__(64) void joint_fold(const bf16* __restrict__ q, con
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
       const int row = r0 + 8 * (v >> 2) + 4 * h + (v & 3);
-      if (row < n) folded[(int64_t(row) * heads + head) * W + c0 + lr] = from_f32<bf16>(acc[v]);
+      if (row >= n) continue;
+      const bf16 y = from_f32<bf16>(acc[v]);
+      const float rest = acc[v] - float(y);                    // none of what is not finite
+      bf16* to = folded + (int64_t(row) * heads + head) * (2 * W) + c0 + lr;
+      to[0] = y;
+      to[W] = from_f32<bf16>(rest == rest ? rest : 0.f);
     }
-    const bf16* qrow = q + (int64_t(min(r0 + lr, n - 1)) * heads + head) * (D + p);
-    if (c0 == 0 && r0 + lr < n)                                // the position part stays as it is
+    if (c0 == 0 && r0 + lr < n) {                              // the position part stays as it is
+      const int64_t row = int64_t(r0 + lr) * heads + head;
       for (int j = 8 * h; j < p; j += 16)
-        *reinterpret_cast<u32x4*>(folded + (int64_t(r0 + lr) * heads + head) * W + r + j) =
-            *reinterpret_cast<const u32x4*>(qrow + D + j);
+        *reinterpret_cast<u32x4*>(folded + row * (2 * W) + r + j) =
+            *reinterpret_cast<const u32x4*>(q + row * (D + p) + D + j);
+    }
+  }
+}
+
+// e4m3 cache: folded [row][r + p] f16, times scale and 2^up, which brings a row's greatest below
+// 2^15.  A work-group has all columns of its rows, 32 a wave, so that it knows the greatest; it
+// shares the queries and the factor, 64 rows of it at a time, in LDS.
+template <int D>
+__global__ __launch_bounds__(1024) void joint_fold_e4m3(const bf16* __restrict__ q, const bf16* __restrict__ W_keys,
+                                                        int n, int heads, int r, int p, _Float16* __restrict__ folded,
+                                                        int32_t* __restrict__ ups, float scale, int wave_rows,
+                                                        FoldStarts starts) {
+  constexpr int DH = 64, QST = 2 * D + 16;                     // bytes a row of the queries
+  __shared__ __align__(16) unsigned char wk[DH * (2 * 512 + 32)], qs[2][32 * QST];
+  __shared__ uint32_t most[3][32];                             // bits of the rows' greatest magnitudes
+  const int tid = threadIdx.x, lane = tid & 63, lr = lane & 31, h = lane >> 5, threads = 2 * r;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6), c0 = 32 * w, st = 2 * r + 32;
+  if (int(blockIdx.x) == heads) {
+    if (blockIdx.y == 0 && w == 0) form_starts(starts);
+    return;
+  }
+  const int head = blockIdx.x, W = r + p;
+  const int row0 = blockIdx.y * wave_rows, row1 = min(row0 + wave_rows, n);
+  const bf16* src = W_keys + int64_t(head) * D * r;
+  const int pieces = r / 8, prow = tid / pieces, pcol = tid % pieces;   // 16 rows a step of all lanes
+  u32x4 x[2], piece[D / 16];
+  auto load_rows = [&](int r0) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int i = k * threads + tid;
+      if (i < 4 * D) {
+        const int64_t row = min(r0 + i / (D / 8), n - 1);
+        x[k] = *reinterpret_cast<const u32x4*>(q + (row * heads + head) * (D + p) + i % (D / 8) * 8);
+      }
+    }
+  };
+  auto keep_rows = [&](int buf) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int i = k * threads + tid;
+      if (i < 4 * D) *reinterpret_cast<u32x4*>(qs[buf] + i / (D / 8) * QST + i % (D / 8) * 16) = x[k];
+    }
+  };
+  load_rows(row0);
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i)
+    piece[i] = *reinterpret_cast<const u32x4*>(src + int64_t(16 * i + prow) * r + pcol * 8);
+  if (tid < 32) most[0][tid] = 0;
+  keep_rows(0);
+  u32x4 f[D / 16];
+#pragma unroll
+  for (int i0 = 0; i0 < D / 16; i0 += DH / 16) {
+    if (i0 > 0) __syncthreads();
+#pragma unroll
+    for (int i = 0; i < DH / 16; ++i)
+      *reinterpret_cast<u32x4*>(wk + (16 * i + prow) * st + pcol * 16) = piece[i0 + i];
+    __syncthreads();
+    factor_columns(f, i0, i0 + DH / 16, wk, st, c0, lane);
+  }
+  auto power = [](int e) { return __uint_as_float(uint32_t(127 + e) << 23); };
+  int it = 0, buf = 0;
+#pragma unroll 1
+  for (int r0 = row0; r0 < row1; r0 += 32) {
+    const bool more = r0 + 32 < row1;
+    if (more) load_rows(r0 + 32);
+    f32x16 acc;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) acc[v] = 0.f;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i)
+      acc = mfma(*reinterpret_cast<const u32x4*>(qs[buf] + lr * QST + 32 * i + 16 * h), f[i], acc);
+    auto row_of = [&](int v) { return 8 * (v >> 2) + 4 * h + (v & 3); };
+    // over the 32 lanes of a row: each exchange halves the rows that a lane holds
+    float top[16];
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      acc[v] *= scale;
+      top[v] = fabsf(acc[v]);
+    }
+#pragma unroll
+    for (int o = 1; o < 16; o *= 2)
+#pragma unroll
+      for (int v = 0; v < 8 / o; ++v) {
+        const float low = top[v], high = top[v + 8 / o];
+        top[v] = fmaxf(lane & o ? high : low, __shfl_xor(lane & o ? low : high, o));
+      }
+    const int v0 = 8 * (lane & 1) + 4 * (lane >> 1 & 1) + 2 * (lane >> 2 & 1) + (lane >> 3 & 1);
+    atomicMax(&most[it][row_of(v0)], __float_as_uint(top[0]));
+    // the position part, 8 coordinates a lane
+    const int64_t prow64 = min(r0 + tid / 8, n - 1);
+    const bool keys = tid < 256 && tid % 8 < p / 8;
+    u32x4 y = {0u, 0u, 0u, 0u};
+    if (keys) {
+      y = *reinterpret_cast<const u32x4*>(q + (prow64 * heads + head) * (D + p) + D + tid % 8 * 8);
+      float t = 0.f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        t = fmaxf(t, fmaxf(fabsf(__uint_as_float(y[e] << 16)), fabsf(__uint_as_float(y[e] & 0xFFFF0000u))));
+      atomicMax(&most[it][tid / 8], __float_as_uint(t * scale));
+    }
+    const int next = it == 2 ? 0 : it + 1;
+    if (tid < 32) most[next][tid] = 0;                         // last read before the barrier before
+    if (more) keep_rows(buf ^ 1);                              // likewise
+    __syncthreads();
+    auto up_of = [&](int row) { return min(max(15 + 126 - int(most[it][row] >> 23), -120), 120); };
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      const int row = r0 + row_of(v);
+      if (row < n)
+        folded[(int64_t(row) * heads + head) * W + joint::query_place(c0 + lr, W)] =
+            _Float16(acc[v] * power(up_of(row_of(v))));
+    }
+    if (keys && r0 + tid / 8 < n) {
+      const float by = power(up_of(tid / 8));
+      u32x4 z;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        z[e] = joint::pair_half(__uint_as_float(y[e] << 16) * scale * by,
+                                __uint_as_float(y[e] & 0xFFFF0000u) * scale * by);
+      *reinterpret_cast<u32x4*>(folded + (prow64 * heads + head) * W + joint::query_place(r + tid % 8 * 8, W)) = z;
+    }
+    if (tid < 32 && r0 + tid < n) ups[int64_t(r0 + tid) * heads + head] = up_of(tid);
+    it = next;
+    buf ^= 1;
   }
 }
 
@@ -136,8 +283,8 @@ struct FinishArgs {
   const float4* part_ml;
   const float* pre_o;
   const float4* pre_ml;
-  int batch, queries, heads, row_rows, slices, units, groups;      // own: rows a work-group
-  int pre_row_rows, pre_slices, pre_units, pre_groups, prefix_len;
+  int batch, queries, heads, row_log, slices;      // own: log2 of the rows a work-group
+  int pre_row_log, pre_slices, pre_units, pre_groups, prefix_len;
 };
 
 // A row's shares joined: C = R/4 lanes a share, GR shares at a time.  mean fp32 [row][R].
@@ -152,8 +299,8 @@ __global__ __launch_bounds__(R / 4 * GR) void joint_merge(FinishArgs a, float* _
   __shared__ float wo[2 * kJointMaxUnits];
   __shared__ int64_t where[2 * kJointMaxUnits];        // element offset of a share; prefix ones complemented
   __shared__ float wave_m[NW], wave_l[NW];
-  const int64_t id = blockIdx.x;                       // (sequence, query, head)
-  const int head = int(id % a.heads), row = int(id / a.heads);
+  const uint32_t id = blockIdx.x;                      // (sequence, query, head)
+  const int head = id % uint32_t(a.heads), row = id / uint32_t(a.heads);
   const int tid = threadIdx.x, g = tid / C, c = tid % C;
   const int b = row / a.queries, i = row % a.queries;
   constexpr int LD = D > 0 ? N / D : 1, PW = D > 0 ? R / 8 / LD : 1;     // lanes a coordinate, pieces a lane
@@ -165,23 +312,23 @@ __global__ __launch_bounds__(R / 4 * GR) void joint_merge(FinishArgs a, float* _
   }
   // shares: those of the sequence's units, then the prefix's
   const int64_t s0 = a.start[b], s1 = a.start[b + 1];
-  const JointCut cut = joint_cut(a.start[a.batch], a.units, a.batch, a.groups);
-  const int64_t u0 = s0 / cut.per;
-  const int own = s1 <= s0 ? 0 : int(cut.whole ? (s1 - s0 + cut.per - 1) / cut.per : (s1 - 1) / cut.per - u0 + 1);
+  const JointCut cut{a.start[a.batch + 1], a.start[a.batch + 2] != 0};
+  const int64_t u0 = joint_div(s0, cut.per);
+  const int own = s1 <= s0 ? 0 : int(joint_div(cut.whole ? s1 - s0 + cut.per - 1 : s1 - 1 - u0 * cut.per + cut.per, cut.per));
   int pre = 0;
   if (a.prefix_len > 0) {
     const int64_t tiles = (a.prefix_len + kJointTile - 1) / kJointTile;
     const int64_t pp = joint_tiles_a_unit(tiles, a.pre_units, a.pre_groups);
-    pre = int((tiles + pp - 1) / pp);
+    pre = int(joint_div(tiles + pp - 1, pp));
   }
   const int ns = own + pre;                            // at most 2 kJointMaxUnits
   const int rr = i * a.heads + head;
   const auto share = [&](int s, int64_t& at) {
     if (s < own) {
-      at = ((u0 + s + b) * a.slices + rr / a.row_rows) * a.row_rows + rr % a.row_rows;
+      at = ((u0 + s + b) * a.slices + (rr >> a.row_log)) * (1 << a.row_log) + (rr & ((1 << a.row_log) - 1));
       return a.part_ml[at];
     }
-    at = (int64_t(s - own) * a.pre_slices + id / a.pre_row_rows) * a.pre_row_rows + id % a.pre_row_rows;
+    at = (int64_t(s - own) * a.pre_slices + (id >> a.pre_row_log)) * (1 << a.pre_row_log) + (id & ((1u << a.pre_row_log) - 1));
     const float4 ml = a.pre_ml[at];
     at = ~(at * R);
     return ml;
@@ -258,7 +405,7 @@ __global__ __launch_bounds__(R / 4 * GR) void joint_merge(FinishArgs a, float* _
     if constexpr (D > 0)
       red[0][c] = sum;
     else
-      *reinterpret_cast<floatx4*>(mean + id * R + 4 * c) = sum;
+      *reinterpret_cast<floatx4*>(mean + int64_t(id) * R + 4 * c) = sum;
   }
   if constexpr (D > 0) {
     __syncthreads();
@@ -278,7 +425,7 @@ __global__ __launch_bounds__(R / 4 * GR) void joint_merge(FinishArgs a, float* _
     }
 #pragma unroll
     for (int e = LD >> 1; e >= 1; e >>= 1) o += __shfl_xor(o, e);
-    if (tid % LD == 0) out[id * D + tid / LD] = from_f32<bf16>(o);
+    if (tid % LD == 0) out[int64_t(id) * D + tid / LD] = from_f32<bf16>(o);
   }
 }
 
@@ -412,8 +559,10 @@ JointShape joint_shape(const dckv_joint_desc& d, int32_t queries, int32_t batch,
   s.pre_slices = int32_t(std::max<int64_t>(1, (all + 16 * s.pre_row_waves - 1) / (16 * s.pre_row_waves)));
   s.pre_units = prefix_len > 0 ? units_of(d.rank, s.pre_slices, tiles_of(prefix_len)) : 0;
   const size_t width = size_t(d.rank + d.rope_dim);
-  s.off_start = align_up(size_t(all) * width * 2);
-  s.off_mean = s.off_start + align_up(size_t(batch + 1) * 8);
+  const bool c8 = d.cache == DCKV_JOINT_E4M3;
+  s.off_up = align_up(size_t(all) * width * (c8 ? 2 : 4));
+  s.off_start = s.off_up + align_up(size_t(all) * (c8 ? 4 : 0));
+  s.off_mean = s.off_start + align_up(size_t(batch + 3) * 8);
   s.off_o = s.off_mean + align_up(size_t(all) * d.rank * 4);
   const size_t own = size_t(s.units + batch) * s.slices * 16 * s.row_waves;
   s.off_ml = s.off_o + align_up(own * d.rank * 4);
@@ -445,20 +594,31 @@ hipError_t launch_joint_decode(const JointShape& s, const void* q, const void* p
   int64_t* starts = reinterpret_cast<int64_t*>(ws + s.off_start);
   // few rows are spread over more waves, each of which reads the factor again
   const int wave_rows = n <= 256 ? 32 : 128;
-  const dim3 grid(d.num_heads * (d.rank / 32) + 1, (n + wave_rows - 1) / wave_rows);
-#define DCKV_FOLD(D)                                                                                         \
-  hipLaunchKernelGGL((joint_fold<D>), grid, dim3(64), 0, stream, static_cast<const bf16*>(q),                 \
-                     static_cast<const bf16*>(W_keys), n, d.num_heads, d.rank, d.rope_dim,                    \
-                     reinterpret_cast<bf16*>(ws), seq_lens, s.max_context, s.batch, starts, wave_rows)
-  if (d.head_dim == 64)
+  const bool c8 = d.cache == DCKV_JOINT_E4M3;
+  int32_t* ups = reinterpret_cast<int32_t*>(ws + s.off_up);
+  const float scale = kLog2e * (d.scale != 0.f ? d.scale : 1.f / std::sqrt(float(d.head_dim + d.rope_dim)));
+  const dim3 grid(d.num_heads * (c8 ? 1 : d.rank / 32) + 1, (n + wave_rows - 1) / wave_rows);
+  const FoldStarts first{seq_lens, starts, s.max_context, s.batch, s.units, groups_of(d, s.row_waves)};
+#define DCKV_FOLD(D)                                                                                              \
+  if (c8)                                                                                                         \
+    hipLaunchKernelGGL((joint_fold_e4m3<D>), grid, dim3(2 * d.rank), 0, stream, static_cast<const bf16*>(q),      \
+                       static_cast<const bf16*>(W_keys), n, d.num_heads, d.rank, d.rope_dim,                      \
+                       reinterpret_cast<_Float16*>(ws), ups, scale, wave_rows, first);                            \
+  else                                                                                                            \
+    hipLaunchKernelGGL((joint_fold<D>), grid, dim3(64), 0, stream, static_cast<const bf16*>(q),                   \
+                       static_cast<const bf16*>(W_keys), n, d.num_heads, d.rank, d.rope_dim,                      \
+                       reinterpret_cast<bf16*>(ws), wave_rows, first)
+  if (d.head_dim == 64) {
     DCKV_FOLD(64);
-  else
+  } else {
     DCKV_FOLD(128);
+  }
 #undef DCKV_FOLD
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   JointAttend a{};
   a.q = ws;
+  a.q_up = ups;
   a.pool = static_cast<const uint8_t*>(pool);
   a.num_pages = num_pages;
   a.page_bytes = joint_page_bytes(d);
@@ -468,7 +628,7 @@ hipError_t launch_joint_decode(const JointShape& s, const void* q, const void* p
   a.batch = s.batch;
   a.queries = s.queries;
   a.heads = d.num_heads;
-  a.scale = kLog2e * (d.scale != 0.f ? d.scale : 1.f / std::sqrt(float(d.head_dim + d.rope_dim)));
+  a.scale = scale;
   if (s.prefix_len > 0) {
     JointAttend p = a;
     p.table = prefix_pages;
@@ -492,7 +652,7 @@ hipError_t launch_joint_decode(const JointShape& s, const void* q, const void* p
   }
   const FinishArgs f{starts, a.part_o, a.part_ml, reinterpret_cast<const float*>(ws + s.off_pre_o),
                      reinterpret_cast<const float4*>(ws + s.off_pre_ml), s.batch, s.queries, d.num_heads,
-                     16 * s.row_waves, s.slices, s.units, groups_of(d, s.row_waves), 16 * s.pre_row_waves,
+                     31 - __builtin_clz(16 * s.row_waves), s.slices, 31 - __builtin_clz(16 * s.pre_row_waves),
                      s.pre_slices, s.pre_units, groups_of(d, s.pre_row_waves), s.prefix_len};
 #define DCKV_FINISH(R, D) return finish<R, D>(f, W_values, n, reinterpret_cast<float*>(ws + s.off_mean), out, stream)
   if (d.rank == 128) {
