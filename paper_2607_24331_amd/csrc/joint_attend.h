@@ -150,6 +150,15 @@ __device__ __forceinline__ int here(int x) {
   return x;
 }
 
+// An operand of the matrix unit that lies in its half of a lone wave's registers and is
+// read there: the compiler would move it over for every tile.
+__device__ __forceinline__ u32x4 in_agprs(u32x4& x) {
+#ifdef __HIP_DEVICE_COMPILE__
+  asm volatile("" : "+a"(x));
+#endif
+  return x;
+}
+
 // The greatest over the four lanes that hold a row (lanes 16 and 32 apart), by moves
 // between vector registers: shuffles would each wait for LDS.
 __device__ __forceinline__ float row_max(float x) {
@@ -201,6 +210,7 @@ struct Shape {
   // the last steps' queries stay in LDS where the registers of two waves a SIMD are full
   static constexpr int QL = C8 && R == 512 && NW == 8 ? 6 : 0;
   static constexpr bool REST = !C8 && (R < 512 || NW == 4);
+  static constexpr bool AGPR = REST && R == 512;      // a lone wave's queries
   static_assert(PIECES % 2 == 0, "whole loads");
 };
 
@@ -475,9 +485,11 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
                 sum = mfma_half(widen(x[i][n][0], x[i][n][1]), query(2 * (i0 + i)), sum);
                 sum = mfma_half(widen(x[i][n][2], x[i][n][3]), query(2 * (i0 + i) + 1), sum);
               } else {
-                s[n] = mfma(x[i][n], query(i0 + i), s[n]);
-                if constexpr (S::REST)
-                  if (i0 + i < R / 32) s[n] = mfma(x[i][n], rest[i0 + i], s[n]);
+                s[n] = mfma(x[i][n], S::AGPR ? in_agprs(q[i0 + i]) : query(i0 + i), s[n]);
+                if (S::REST && n == 1 && i0 + i < R / 32)
+#pragma unroll
+                  for (int k = 0; k < 2; ++k)
+                    s[k] = mfma(x[i][k], S::AGPR ? in_agprs(rest[i0 + i]) : rest[i0 + i], s[k]);
               }
             }
           __builtin_amdgcn_sched_barrier(0);
