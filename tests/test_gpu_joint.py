@@ -765,3 +765,119 @@ def test_serving_loop(cache):
         tol = 2.0 ** -8 if cache == "bf16" else 2.0 ** -4
         assert ((c[:n] - x[:n, :r]).abs() <= tol * x[:n, :r].abs().clamp(min=2.0 ** -6)).all()
         cached, count = m.seq_lens, m.free_left
+
+
+# ------------------------------------------------- exactness and numbers of any size
+def slack(got, want):
+    """The error relative to what rounding the right result to bf16 costs, in root mean square."""
+    rounded = host(torch.from_numpy(want).to(BF16))
+    return math.sqrt(np.mean((got - want) ** 2) / np.mean((rounded - want) ** 2))
+
+
+@pytest.mark.parametrize("H,d,r,p,cache,Q,n,most", [
+    # e4m3 and prompts: f16 weights and queries (and a prompt's keys and values), 2^-12 each
+    # against the result's 2^-9: sqrt(1 + 4 / 64) = 1.03, and a percent or two of chance
+    (16, 64, 128, 32, "e4m3", 1, 0, 1.06), (16, 128, 512, 64, "e4m3", 1, 0, 1.06), (32, 64, 256, 0, "e4m3", 4, 100, 1.06),
+    # bf16 weights, whose errors add up over the tokens as the weights themselves do: sqrt 2
+    (16, 64, 128, 32, "bf16", 1, 0, 1.45), (16, 128, 512, 64, "bf16", 1, 70, 1.45), (32, 64, 256, 0, "bf16", 4, 0, 1.45),
+    # queries without rests: a score of unit variance has an error of the same size, sqrt 3
+    (32, 128, 512, 64, "bf16", 4, 0, 1.77),
+])
+def test_decodes_are_as_exact_as_their_result(H, d, r, p, cache, Q, n, most):
+    from paper_2607_24331_amd import joint_decode
+    g = gen(H + r)
+    j = joint_of(H, d, r, p, cache)
+    B, T = 8, 300
+    pool = filled(j, B * 5 + 2, g)
+    perm = torch.randperm(B * 5 + 2, generator=g, device="cuda").to(torch.int32)
+    table, prefix = perm[:B * 5].view(B, 5).contiguous(), perm[B * 5:].contiguous()
+    q = randn(g, B, Q, H, d + p).to(BF16)
+    wk, wv = factors(j, g)
+    lens = [T - 7 * b for b in range(B)]
+    seq = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    got = joint_decode(j, q, pool, table, seq, T, wk, wv, prefix if n else None, n)
+    assert slack(host(got), oracle_decode(j, q, pool, table, lens, T, wk, wv, prefix, n)) <= most
+
+
+@pytest.mark.parametrize("H,d,r,p,cache", [(4, 64, 128, 32, "bf16"), (3, 128, 512, 64, "e4m3"), (2, 128, 256, 0, "bf16")])
+def test_prompts_are_as_exact_as_their_result(H, d, r, p, cache):
+    from paper_2607_24331_amd import joint_prefill
+    j = joint_of(H, d, r, p, cache)
+    added = [200, 129]
+    pool, table, start, q, wk, wv, seq, rs, lens, top = prompt_case(j, [100, 0], added, 0, 5)
+    got = joint_prefill(j, q, rs, pool, table, seq, top, wk, wv, total_context=sum(lens))
+    assert slack(host(got), oracle_prompt(j, pool, table, start, q, wk, wv, lens, added)) <= 1.06
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("tokens,queries", [(-40, 40), (35, -35), (-90, 60), (60, -90)])
+def test_sequences_of_other_sizes(cache, tokens, queries):
+    """The second of three sequences has latents and position keys 2^tokens as large and
+    queries 2^queries; its result is the one of unit sizes times 2^tokens, with the scores of
+    `tokens + queries`, and the others' are what they are without it."""
+    from paper_2607_24331_amd import joint_decode, joint_prefill
+    g = gen(3)
+    H, d, r, p = 4, 64, 128, 32
+    j = joint_of(H, d, r, p, cache)
+    pool = filled(j, 6, g)
+    if cache == "bf16":
+        pool[2:4] = (pool[2:4].double() * 2.0 ** tokens).to(BF16)
+    else:
+        pool[2:4, PAGE * (r + p):] = (pool[2:4, PAGE * (r + p):].int() + tokens).to(torch.uint8)
+    table = torch.arange(6, dtype=torch.int32, device="cuda").view(3, 2)
+    lens = [100, 128, 70]
+    seq = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    q = randn(g, 3, 2, H, d + p).to(BF16)
+    q[1] = (q[1].double() * 2.0 ** queries).to(BF16)
+    wk, wv = factors(j, g)
+    want = oracle_decode(j, q, pool, table, lens, 128, wk, wv)
+    got = host(joint_decode(j, q, pool, table, seq, 128, wk, wv))
+    start = torch.tensor([0, 2, 4, 6], dtype=torch.int32, device="cuda")
+    prompt = host(joint_prefill(j, q.view(6, H, d + p), start, pool, table, seq, 128, wk, wv)).reshape(3, 2, H, d)
+    for b in range(3):
+        check(got[b], want[b], np.abs(want[b]).max(), b)
+        check(prompt[b], want[b], np.abs(want[b]).max(), b)
+
+
+@pytest.mark.parametrize("size", [2.0 ** -60, 2.0 ** 50])
+def test_factors_of_other_sizes(size):
+    """Factors far from unit size, with queries that bring the scores back."""
+    from paper_2607_24331_amd import joint_decode, joint_prefill
+    for cache in ("bf16", "e4m3"):
+        g = gen(4)
+        j = joint_of(4, 64, 128, 0, cache)
+        pool = filled(j, 2, g)
+        table = torch.arange(2, dtype=torch.int32, device="cuda").view(1, 2)
+        seq = torch.tensor([99], dtype=torch.int32, device="cuda")
+        q = (randn(g, 1, 3, 4, 64) / size).to(BF16)
+        wk, wv = [(w.double() * size).to(BF16) for w in factors(j, g)]
+        want = oracle_decode(j, q, pool, table, [99], 128, wk, wv)
+        check(host(joint_decode(j, q, pool, table, seq, 128, wk, wv)), want, np.abs(want).max())
+        start = torch.tensor([0, 3], dtype=torch.int32, device="cuda")
+        check(host(joint_prefill(j, q[0], start, pool, table, seq, 128, wk, wv)), want[0], np.abs(want).max())
+
+
+def test_zero_tokens_factors_and_queries():
+    """Zeros throughout: the powers of two of nothing.  Scores of 0 weigh alike."""
+    from paper_2607_24331_amd import joint_decode, joint_prefill
+    for cache in ("bf16", "e4m3"):
+        g = gen(8)
+        j = joint_of(4, 64, 128, 32, cache)
+        table = torch.arange(2, dtype=torch.int32, device="cuda").view(1, 2)
+        seq = torch.tensor([99], dtype=torch.int32, device="cuda")
+        start = torch.tensor([0, 3], dtype=torch.int32, device="cuda")
+        wk, wv = factors(j, g)
+        q = randn(g, 1, 3, 4, 96).to(BF16)
+        for what in ("tokens", "keys' factor", "values' factor", "queries"):
+            pool = filled(j, 2, g)
+            a, b, x = wk.clone(), wv.clone(), q.clone()
+            if what == "tokens":
+                pool[:, :PAGE * 160] = 0
+            elif what == "queries":
+                x.zero_()
+            else:
+                (a if what == "keys' factor" else b).zero_()
+            want = oracle_decode(j, x, pool, table, [99], 128, a, b)
+            size = max(np.abs(want).max(), 1e-30)
+            check(host(joint_decode(j, x, pool, table, seq, 128, a, b)), want, size, (cache, what))
+            check(host(joint_prefill(j, x[0], start, pool, table, seq, 128, a, b)), want[0], size, (cache, what))
