@@ -622,10 +622,14 @@ int dckv_joint_read(const dckv_joint_desc* desc, const void* pool, int64_t num_p
  *              are read once for all; page_table, seq_lens and max_context then count a
  *              sequence's own tokens, whose positions start at prefix_len.  0: NULL
  *   out        device bf16 [batch, Q, H, d]
- * Folded queries and softmax weights are rounded to bf16 (relative 2^-9 each), sums
- * are fp32.  Whatever lies in slots that a query does not see (NaN included) does not
- * reach its result; a token that it sees and that is not finite makes it NaN, as does
- * an infinite score.
+ * Roundings (relative; sums are fp32): e4m3 caches, folded queries and softmax weights
+ * 2^-12 (f16, under powers of two that follow the magnitudes; parts 2^-29 of a query
+ * row's greatest coordinate and weights 2^-22 of the greatest lose bits); bf16 caches,
+ * weights 2^-9, queries 2^-17, or 2^-9 at rank 512 where a call's products are shared by
+ * more than 32 rows (Q*H, for the prefix batch*Q*H).
+ * Whatever lies in slots that a query does not see (NaN included) does not reach its
+ * result; a NaN in one that it sees makes it NaN, and an infinity or an infinite score
+ * does, but that a token whose score is minus infinity may weigh nothing.
  * A workspace (256-byte aligned; its contents do not matter) of
  * dckv_joint_workspace_bytes also serves fewer sequences, shorter contexts and shorter
  * prefixes (not a prefix where none was named).  Calls that may overlap need workspaces
@@ -654,9 +658,13 @@ int dckv_joint_decode(const dckv_joint_desc* desc, int32_t queries, const void* 
  *              0 .. max_context) that have rows; a sequence that does not fit it gets
  *              NaN
  *   out        device bf16 [n_rows, H, d]
- * Keys, values and softmax weights are rounded to bf16 (values beyond its range to
- * its greatest), sums are fp32.  Unseen slots, NaN, pages, alignment and errors as for
- * dckv_joint_decode; the workspace serves fewer sequences, rows and tokens too. */
+ * Keys, values, queries and softmax weights are rounded to f16 (relative 2^-12) under
+ * powers of two a sequence and a row, sums are fp32: keys and values 2^-29 of the
+ * sequence's bound (greatest |latent coordinate| * r * greatest |factor element|, or the
+ * greatest |position key|) lose bits.  Values that overflow fp32 count as the greatest
+ * number.  A token that is not finite makes every row that sees it NaN.  Unseen slots,
+ * pages, alignment and errors as for dckv_joint_decode; the workspace serves fewer
+ * sequences, rows and tokens too. */
 int dckv_joint_prefill_workspace_bytes(const dckv_joint_desc* desc, int32_t batch, int32_t n_rows,
                                        int32_t max_context, int64_t total_context, size_t* bytes);
 int dckv_joint_prefill(const dckv_joint_desc* desc, const void* q, int32_t n_rows,

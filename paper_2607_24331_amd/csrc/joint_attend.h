@@ -686,7 +686,12 @@ hipError_t launch_rows(int row_waves, const JointAttend& a, hipStream_t stream) 
   const uint32_t groups = (units + 7) / 8 * 8 * uint32_t(a.slices);
   switch (row_waves) {
     case 1: hipLaunchKernelGGL((joint_attend<R, P, C8, 1>), dim3(groups), dim3(threads), 0, stream, a); break;
-    case 2: hipLaunchKernelGGL((joint_attend<R, P, C8, 2>), dim3(groups), dim3(threads), 0, stream, a); break;
+    case 2:
+      if constexpr (C8) {                             // bf16 goes from one to four
+        hipLaunchKernelGGL((joint_attend<R, P, C8, 2>), dim3(groups), dim3(threads), 0, stream, a);
+        break;
+      }
+      return hipErrorInvalidValue;
     case 4: hipLaunchKernelGGL((joint_attend<R, P, C8, 4>), dim3(groups), dim3(threads), 0, stream, a); break;
     case 8: hipLaunchKernelGGL((joint_attend<R, P, C8, 8>), dim3(groups), dim3(threads), 0, stream, a); break;
     default: return hipErrorInvalidValue;

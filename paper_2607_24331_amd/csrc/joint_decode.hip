@@ -493,8 +493,24 @@ int fill(int rank) { return rank == 128 ? 512 : 256; }
 
 int64_t tiles_of(int64_t tokens) { return (tokens + kJointTile - 1) / kJointTile; }
 
-// Rows of a work-group, 16 a wave: the least of 16, 32, 64 that takes all of them, else 128.
-int row_waves_of(int64_t rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : rows <= 64 ? 4 : 8; }
+// Waves of a work-group that take rows, 16 each.  The slices of a unit read the same tokens on
+// one XCD at about one time, so that its L2 serves all but one, as long as they run together:
+// 32 slices (4,096 rows of bf16 at rank 512 over 16,384 tokens: 32 slices of 128 rows 144 us,
+// 64 of 64 rows 313 us).
+// e4m3: the fewest waves that keep to 32 slices; widening a tile costs about as much as its
+// products, and token groups that do not wait for each other hide it best (48 rows over
+// 4 x 32,768 tokens at rank 512: 34 us, in one slice of 64 rows 40; 512 rows over a prefix of
+// 16,384: 50 and 61 us with the share's join).
+// bf16: one up to 32 rows (4 x 32,768 tokens: 33 us, in one slice 34); from there reading a tile
+// from memory by one slice alone pays (64 rows: 4 waves 39 us, 2 slices 48, 4 slices 52), but
+// four waves' shares are half of eight's to join (128 rows over 131,072 tokens: attention and
+// join 64 us, eight waves 67).
+constexpr int kSlices = 32;
+int row_waves_of(bool e4m3, int64_t rows) {
+  if (rows <= (e4m3 ? 16 * kSlices : 32)) return 1;
+  if (e4m3 && rows <= 32 * kSlices) return 2;
+  return rows <= 64 * kSlices ? 4 : 8;
+}
 
 int groups_of(const dckv_joint_desc& d, int row_waves) {
   return joint_waves(row_waves, joint_tile_bytes(d.rank + d.rope_dim, d.cache == DCKV_JOINT_E4M3)) / row_waves;
@@ -550,16 +566,16 @@ JointShape joint_shape(const dckv_joint_desc& d, int32_t queries, int32_t batch,
   s.max_context = max_context;
   s.prefix_len = prefix_len;
   s.rows = queries * d.num_heads;
-  s.row_waves = row_waves_of(s.rows);
+  const bool c8 = d.cache == DCKV_JOINT_E4M3;
+  s.row_waves = row_waves_of(c8, s.rows);
   s.slices = (s.rows + 16 * s.row_waves - 1) / (16 * s.row_waves);
   const int64_t tiles = int64_t(batch) * tiles_of(max_context);
   s.units = units_of(d.rank, s.slices, tiles);
   const int64_t all = int64_t(s.rows) * batch;
-  s.pre_row_waves = row_waves_of(all);
+  s.pre_row_waves = row_waves_of(c8, all);
   s.pre_slices = int32_t(std::max<int64_t>(1, (all + 16 * s.pre_row_waves - 1) / (16 * s.pre_row_waves)));
   s.pre_units = prefix_len > 0 ? units_of(d.rank, s.pre_slices, tiles_of(prefix_len)) : 0;
   const size_t width = size_t(d.rank + d.rope_dim);
-  const bool c8 = d.cache == DCKV_JOINT_E4M3;
   s.off_up = align_up(size_t(all) * width * (c8 ? 2 : 4));
   s.off_start = s.off_up + align_up(size_t(all) * (c8 ? 4 : 0));
   s.off_mean = s.off_start + align_up(size_t(batch + 3) * 8);
