@@ -7,7 +7,7 @@
 namespace dckv {
 
 constexpr int kJointTile = 32;          // tokens a tile of the decode
-constexpr int kJointMaxUnits = 512;     // work-groups of a row slice, at most (the join holds 2 a row)
+constexpr int kJointMaxUnits = 512;     // work-groups of a row slice, at most
 
 // Pieces (16 bytes) of a row change places by the row, so that the 16 rows that a
 // quarter of a wave reads at one column lie in different LDS banks: piece i of slot s

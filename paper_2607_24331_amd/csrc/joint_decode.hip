@@ -8,7 +8,7 @@
 //               the factor's rows; products on MFMA 32x32x16.  One more wave forms
 //               the sequences' first tiles.  Bound by latency and, once, by the factor's bytes.
 // joint_merge   a work-group a row: its shares' sums in fp32, 16 bytes a lane.  Bound by
-//               the shares' bytes.
+//               the shares' bytes (4,096 rows of 10 shares at rank 512, 92 MB: 16 us, 5.7 TB/s).
 // joint_values  the product with the heads' factor rows on MFMA, 32 rows by 32 coordinates a
 //               work-group, its waves a quarter of the latent coordinates each.
 #include <algorithm>
@@ -296,8 +296,9 @@ __global__ __launch_bounds__(R / 4 * GR) void joint_merge(FinishArgs a, float* _
                                                           bf16* __restrict__ out) {
   constexpr int C = R / 4, N = C * GR, NW = N / 64 > 0 ? N / 64 : 1;
   __shared__ __align__(16) floatx4 red[GR > 1 ? GR : 1][C];
-  __shared__ float wo[2 * kJointMaxUnits];
-  __shared__ int64_t where[2 * kJointMaxUnits];        // element offset of a share; prefix ones complemented
+  constexpr int CH = N < 256 ? 64 : 256;
+  __shared__ float wo[CH];
+  __shared__ int64_t where[CH];                        // element offset of a share; prefix ones complemented
   __shared__ float wave_m[NW], wave_l[NW];
   const uint32_t id = blockIdx.x;                      // (sequence, query, head)
   const int head = id % uint32_t(a.heads), row = id / uint32_t(a.heads);
@@ -321,36 +322,31 @@ __global__ __launch_bounds__(R / 4 * GR) void joint_merge(FinishArgs a, float* _
     const int64_t pp = joint_tiles_a_unit(tiles, a.pre_units, a.pre_groups);
     pre = int(joint_div(tiles + pp - 1, pp));
   }
-  const int ns = own + pre;                            // at most 2 kJointMaxUnits
+  const int ns = own + pre;
   const int rr = i * a.heads + head;
   const auto share = [&](int s, int64_t& at) {
     if (s < own) {
       at = ((u0 + s + b) * a.slices + (rr >> a.row_log)) * (1 << a.row_log) + (rr & ((1 << a.row_log) - 1));
-      return a.part_ml[at];
+      const float4 ml = a.part_ml[at];
+      at *= R;
+      return ml;
     }
     at = (int64_t(s - own) * a.pre_slices + (id >> a.pre_row_log)) * (1 << a.pre_row_log) + (id & ((1u << a.pre_row_log) - 1));
     const float4 ml = a.pre_ml[at];
     at = ~(at * R);
     return ml;
   };
-  // a lane's shares wait in registers for the greatest m: at most 2 kJointMaxUnits / N
-  constexpr int PER = (2 * kJointMaxUnits + N - 1) / N;
-  float m_of[PER], l_of[PER], u_of[PER];
+  // the greatest m; a lane's first share waits in registers
+  float4 first = make_float4(-INFINITY, 0.f, -INFINITY, 0.f);
+  int64_t first_at = 0;
   float M = -INFINITY;
-#pragma unroll
-  for (int k = 0; k < PER; ++k) {
-    m_of[k] = u_of[k] = -INFINITY;
-    l_of[k] = 0.f;
-    const int s = k * N + tid;
-    if (k * N >= ns) continue;
-    if (s < ns) {
-      int64_t at;
-      const float4 ml = share(s, at);
-      m_of[k] = ml.x;
-      l_of[k] = ml.y;
-      u_of[k] = ml.z;
-      where[s] = at < 0 ? at : at * R;
-      M = fmaxf(M, ml.x);
+  for (int s = tid; s < ns; s += N) {
+    int64_t at;
+    const float4 ml = share(s, at);
+    M = fmaxf(M, ml.x);
+    if (s == tid) {
+      first = ml;
+      first_at = at;
     }
   }
 #pragma unroll
@@ -360,36 +356,43 @@ __global__ __launch_bounds__(R / 4 * GR) void joint_merge(FinishArgs a, float* _
 #pragma unroll
   for (int o = 0; o < NW; ++o) M = fmaxf(M, wave_m[o]);
   float l = 0.f;
+  floatx4 sum = {0.f, 0.f, 0.f, 0.f};
+  constexpr int U = 8;
+  for (int s0 = 0; s0 < ns; s0 += CH) {                // weights of CH shares at a time
+    const int n = min(ns - s0, CH);
+    if (s0 > 0) __syncthreads();
+    for (int s = tid; s < n; s += N) {
+      int64_t at = first_at;
+      float4 ml = first;
+      if (s0 + s != tid) ml = share(s0 + s, at);
+      const bool some = ml.y != 0.f;                   // a share that saw nothing has l = 0 and m = -inf
+      l += some ? ml.y * __builtin_amdgcn_exp2f(ml.x - M) : 0.f;
+      wo[s] = some ? __builtin_amdgcn_exp2f(ml.z - M) : 0.f;
+      where[s] = at;
+    }
+    __syncthreads();
+    for (int s = g; s < n; s += U * GR) {
+      floatx4 x[U];
 #pragma unroll
-  for (int k = 0; k < PER; ++k) {
-    const int s = k * N + tid;
-    const bool some = l_of[k] != 0.f;                  // a share that saw nothing has l = 0 and m = -inf
-    l += some ? l_of[k] * __builtin_amdgcn_exp2f(m_of[k] - M) : 0.f;
-    if (s < ns) wo[s] = some ? __builtin_amdgcn_exp2f(u_of[k] - M) : 0.f;
+      for (int j = 0; j < U; ++j) {
+        if (s + j * GR >= n) continue;
+        const int64_t at = where[s + j * GR];
+        x[j] = *reinterpret_cast<const floatx4*>((at < 0 ? a.pre_o + ~at : a.part_o + at) + 4 * c);
+      }
+#pragma unroll
+      for (int j = 0; j < U; ++j) {
+        if (s + j * GR >= n) continue;
+        const float y = wo[s + j * GR];
+        if (y == 0.f) continue;                        // nothing seen: the sums may be infinite
+#pragma unroll
+        for (int v = 0; v < 4; ++v) sum[v] = fmaf(y, x[j][v], sum[v]);
+      }
+    }
   }
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) l += __shfl_xor(l, o);
   if ((tid & 63) == 0) wave_l[tid >> 6] = l;
-  __syncthreads();
-  floatx4 sum = {0.f, 0.f, 0.f, 0.f};
-  constexpr int U = 8;
-  for (int s = g; s < ns; s += U * GR) {
-    floatx4 x[U];
-#pragma unroll
-    for (int j = 0; j < U; ++j) {
-      if (s + j * GR >= ns) continue;
-      const int64_t at = where[s + j * GR];
-      x[j] = *reinterpret_cast<const floatx4*>((at < 0 ? a.pre_o + ~at : a.part_o + at) + 4 * c);
-    }
-#pragma unroll
-    for (int j = 0; j < U; ++j) {
-      if (s + j * GR >= ns) continue;
-      const float y = wo[s + j * GR];
-      if (y == 0.f) continue;                          // nothing seen: the sums may be infinite
-#pragma unroll
-      for (int v = 0; v < 4; ++v) sum[v] = fmaf(y, x[j][v], sum[v]);
-    }
-  }
+  if (GR == 1) __syncthreads();
   if constexpr (GR > 1) {
     red[g][c] = sum;
     __syncthreads();
@@ -525,15 +528,19 @@ int units_of(int rank, int64_t slices, int64_t tiles) {
 
 template <int R, int D>
 hipError_t finish(const FinishArgs& a, const void* W_values, int n, float* mean, void* out, hipStream_t stream) {
-  // Few rows have many shares each: a work-group of 1024 that goes on to the values; many
-  // rows share the factors' reads in a launch of their own.  128 rows: ... us and ...
+  // Few rows have many shares each: a work-group of 1024 that goes on to the values (rank
+  // 512, 64 rows: 6.3 us, in two launches 11.2; 512 rows: 11.4 and 10.2).  Many rows share the
+  // factors' reads in a launch of their own (1,024 rows: 10.6 us, one launch 19.2), and few
+  // lanes a row keep more rows on their way (rank 256, 32,768 rows of a share: 64 lanes 19 us,
+  // 256 lanes 53).
   const uint32_t rows = uint32_t(n) * a.heads;
   if (rows < 1024) {
     hipLaunchKernelGGL((joint_merge<R, 4096 / R, D>), dim3(rows), dim3(1024), 0, stream, a, mean,
                        static_cast<const bf16*>(W_values), static_cast<bf16*>(out));
     return hipGetLastError();
   }
-  hipLaunchKernelGGL((joint_merge<R, 1024 / R, 0>), dim3(rows), dim3(256), 0, stream, a, mean, nullptr, nullptr);
+  constexpr int GR = R == 128 ? 2 : 1;
+  hipLaunchKernelGGL((joint_merge<R, GR, 0>), dim3(rows), dim3(R / 4 * GR), 0, stream, a, mean, nullptr, nullptr);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((joint_values<R, D>), dim3(uint32_t((n + 31) / 32) * (D / 32) * a.heads), dim3(256), 0, stream,

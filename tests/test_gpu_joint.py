@@ -599,6 +599,31 @@ def test_batches_and_long_contexts(H, d, r, p, cache, B, low, high, Q, n):
     assert torch.equal(out, again)
 
 
+@pytest.mark.parametrize("H,d,r,p,cache,Q", [(16, 64, 128, 32, "bf16", 1), (16, 128, 512, 64, "e4m3", 1),
+                                             (32, 64, 256, 0, "bf16", 1)])
+def test_one_long_sequence_among_many(H, d, r, p, cache, Q):
+    """Its rows' shares are most of a launch's, the others' one each: a join of hundreds and
+    of one, of more than a thousand rows."""
+    from paper_2607_24331_amd import joint_decode
+    g = gen(11)
+    j = joint_of(H, d, r, p, cache)
+    B, T = 70, 40000
+    lens = [40] * B
+    lens[0], lens[5], lens[6], lens[69] = 1, T, 0, 64
+    width = -(-T // PAGE)
+    pool = filled(j, width + 2 * B, g)
+    table = torch.full((B, width), -1, dtype=torch.int32, device="cuda")
+    table[:, 0] = torch.arange(B, device="cuda") + width
+    table[5] = torch.randperm(width, generator=g, device="cuda").to(torch.int32)
+    q = randn(g, B, Q, H, d + p).to(BF16)
+    wk, wv = factors(j, g)
+    seq = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    got = host(joint_decode(j, q, pool, table, seq, T, wk, wv))
+    for b in (0, 5, 6, 30, 69):
+        want = oracle_decode(j, q[b:b + 1], pool, table[b:b + 1], [lens[b]], T, wk, wv)
+        check(got[b], want[0], max(np.abs(want).max(), 1e-30), b)
+
+
 def test_offsets_past_32_bits():
     from paper_2607_24331_amd import joint_append, joint_decode, joint_prefill, joint_read
     g = gen(4)
