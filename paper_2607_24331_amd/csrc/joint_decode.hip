@@ -503,13 +503,17 @@ int64_t tiles_of(int64_t tokens) { return (tokens + kJointTile - 1) / kJointTile
 // e4m3: the fewest waves that keep to 32 slices; widening a tile costs about as much as its
 // products, and token groups that do not wait for each other hide it best (48 rows over
 // 4 x 32,768 tokens at rank 512: 34 us, in one slice of 64 rows 40; 512 rows over a prefix of
-// 16,384: 50 and 61 us with the share's join).
+// 16,384 and their own 32: 50 us, in slices of 128 rows 53).  Many sequences have many ends, at
+// which eight groups have less to do than four: two (32 rows, 64 sequences of up to 8,192
+// tokens: 46 us, one wave 57; 4 of 32,768: 29 and 28).
 // bf16: one up to 32 rows (4 x 32,768 tokens: 33 us, in one slice 34); from there reading a tile
 // from memory by one slice alone pays (64 rows: 4 waves 39 us, 2 slices 48, 4 slices 52), but
 // four waves' shares are half of eight's to join (128 rows over 131,072 tokens: attention and
 // join 64 us, eight waves 67).
 constexpr int kSlices = 32;
-int row_waves_of(bool e4m3, int64_t rows) {
+constexpr int kManySequences = 16;
+int row_waves_of(bool e4m3, int64_t rows, int sequences) {
+  if (e4m3 && rows > 16 && rows <= 32 * kSlices && sequences >= kManySequences) return 2;
   if (rows <= (e4m3 ? 16 * kSlices : 32)) return 1;
   if (e4m3 && rows <= 32 * kSlices) return 2;
   return rows <= 64 * kSlices ? 4 : 8;
@@ -574,12 +578,12 @@ JointShape joint_shape(const dckv_joint_desc& d, int32_t queries, int32_t batch,
   s.prefix_len = prefix_len;
   s.rows = queries * d.num_heads;
   const bool c8 = d.cache == DCKV_JOINT_E4M3;
-  s.row_waves = row_waves_of(c8, s.rows);
+  s.row_waves = row_waves_of(c8, s.rows, batch);
   s.slices = (s.rows + 16 * s.row_waves - 1) / (16 * s.row_waves);
   const int64_t tiles = int64_t(batch) * tiles_of(max_context);
   s.units = units_of(d.rank, s.slices, tiles);
   const int64_t all = int64_t(s.rows) * batch;
-  s.pre_row_waves = row_waves_of(c8, all);
+  s.pre_row_waves = row_waves_of(c8, all, 1);
   s.pre_slices = int32_t(std::max<int64_t>(1, (all + 16 * s.pre_row_waves - 1) / (16 * s.pre_row_waves)));
   s.pre_units = prefix_len > 0 ? units_of(d.rank, s.pre_slices, tiles_of(prefix_len)) : 0;
   const size_t width = size_t(d.rank + d.rope_dim);
