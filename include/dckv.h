@@ -661,7 +661,8 @@ int dckv_joint_decode(const dckv_joint_desc* desc, int32_t queries, const void* 
  * Keys, values, queries and softmax weights are rounded to f16 (relative 2^-12) under
  * powers of two a sequence and a row, sums are fp32: keys and values 2^-29 of the
  * sequence's bound (greatest |latent coordinate| * r * greatest |factor element|, or the
- * greatest |position key|) lose bits.  Values that overflow fp32 count as the greatest
+ * greatest |position key|, over all its tokens, those that a row does not see too) lose
+ * bits.  Values that overflow fp32 count as the greatest
  * number.  A token that is not finite makes every row that sees it NaN.  Unseen slots,
  * pages, alignment and errors as for dckv_joint_decode; the workspace serves fewer
  * sequences, rows and tokens too. */

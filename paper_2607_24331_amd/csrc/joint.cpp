@@ -14,7 +14,7 @@ namespace {
 
 constexpr int32_t kMaxTokens = 1 << 23;            // tokens a call: a lane 8 columns fits a grid
 constexpr int64_t kMaxStride = int64_t(1) << 38;   // elements: offsets stay within int64
-constexpr int64_t kMaxGroups = (int64_t(1) << 22) - 1;   // work-groups of up to 1024 threads in a grid
+constexpr int64_t kMaxGroups = (int64_t(1) << 22) - 1024;   // work-groups of up to 1024 threads in a grid, and a rest
 constexpr int64_t kMaxPages = int64_t(1) << 32;
 
 int check_desc(const char* where, const dckv_joint_desc* d) {

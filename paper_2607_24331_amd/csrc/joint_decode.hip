@@ -13,6 +13,7 @@
 //               work-group, its waves a quarter of the latent coordinates each.
 #include <algorithm>
 #include <cmath>
+#include <limits>
 
 #include "joint_attend.h"
 
@@ -154,14 +155,15 @@ __global__ __launch_bounds__(64) void joint_fold(const bf16* __restrict__ q, con
   }
 }
 
-// e4m3 cache: folded [row][r + p] f16, times scale and 2^up, which brings a row's greatest below
-// 2^15.  A work-group has all columns of its rows, 32 a wave, so that it knows the greatest; it
-// shares the queries and the factor, 64 rows of it at a time, in LDS.
+// e4m3 cache: folded [row][r + p] f16, times unit (the scale is unit * 2^unit_exp) and 2^up, which
+// brings a row's greatest below 2^15; ups: up - unit_exp.  A work-group has all columns of its
+// rows, 32 a wave, so that it knows the greatest; it shares the queries and the factor, 64
+// rows of it at a time, in LDS.
 template <int D>
 __global__ __launch_bounds__(1024) void joint_fold_e4m3(const bf16* __restrict__ q, const bf16* __restrict__ W_keys,
                                                         int n, int heads, int r, int p, _Float16* __restrict__ folded,
-                                                        int32_t* __restrict__ ups, float scale, int wave_rows,
-                                                        FoldStarts starts) {
+                                                        int32_t* __restrict__ ups, float unit, int unit_exp,
+                                                        int wave_rows, FoldStarts starts) {
   constexpr int DH = 64, QST = 2 * D + 16;                     // bytes a row of the queries
   __shared__ __align__(16) unsigned char wk[DH * (2 * 512 + 32)], qs[2][32 * QST];
   __shared__ uint32_t most[3][32];                             // bits of the rows' greatest magnitudes
@@ -226,7 +228,7 @@ __global__ __launch_bounds__(1024) void joint_fold_e4m3(const bf16* __restrict__
     float top[16];
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
-      acc[v] *= scale;
+      acc[v] *= unit;
       top[v] = fabsf(acc[v]);
     }
 #pragma unroll
@@ -248,7 +250,7 @@ __global__ __launch_bounds__(1024) void joint_fold_e4m3(const bf16* __restrict__
 #pragma unroll
       for (int e = 0; e < 4; ++e)
         t = fmaxf(t, fmaxf(fabsf(__uint_as_float(y[e] << 16)), fabsf(__uint_as_float(y[e] & 0xFFFF0000u))));
-      atomicMax(&most[it][tid / 8], __float_as_uint(t * scale));
+      atomicMax(&most[it][tid / 8], __float_as_uint(t * unit));
     }
     const int next = it == 2 ? 0 : it + 1;
     if (tid < 32) most[next][tid] = 0;                         // last read before the barrier before
@@ -267,11 +269,11 @@ __global__ __launch_bounds__(1024) void joint_fold_e4m3(const bf16* __restrict__
       u32x4 z;
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        z[e] = joint::pair_half(__uint_as_float(y[e] << 16) * scale * by,
-                                __uint_as_float(y[e] & 0xFFFF0000u) * scale * by);
+        z[e] = joint::pair_half(__uint_as_float(y[e] << 16) * unit * by,
+                                __uint_as_float(y[e] & 0xFFFF0000u) * unit * by);
       *reinterpret_cast<u32x4*>(folded + (prow64 * heads + head) * W + joint::query_place(r + tid % 8 * 8, W)) = z;
     }
-    if (tid < 32 && r0 + tid < n) ups[int64_t(r0 + tid) * heads + head] = up_of(tid);
+    if (tid < 32 && r0 + tid < n) ups[int64_t(r0 + tid) * heads + head] = up_of(tid) - unit_exp;
     it = next;
     buf ^= 1;
   }
@@ -625,14 +627,17 @@ hipError_t launch_joint_decode(const JointShape& s, const void* q, const void* p
   const int wave_rows = n <= 256 ? 32 : 128;
   const bool c8 = d.cache == DCKV_JOINT_E4M3;
   int32_t* ups = reinterpret_cast<int32_t*>(ws + s.off_up);
-  const float scale = kLog2e * (d.scale != 0.f ? d.scale : 1.f / std::sqrt(float(d.head_dim + d.rope_dim)));
+  const float scale = std::min(kLog2e * (d.scale != 0.f ? d.scale : 1.f / std::sqrt(float(d.head_dim + d.rope_dim))),
+                               std::numeric_limits<float>::max());
+  int unit_exp;
+  const float unit = std::frexp(scale, &unit_exp);     // at most 1: nothing overflows by it
   const dim3 grid(d.num_heads * (c8 ? 1 : d.rank / 32) + 1, (n + wave_rows - 1) / wave_rows);
   const FoldStarts first{seq_lens, starts, s.max_context, s.batch, s.units, groups_of(d, s.row_waves)};
 #define DCKV_FOLD(D)                                                                                              \
   if (c8)                                                                                                         \
     hipLaunchKernelGGL((joint_fold_e4m3<D>), grid, dim3(2 * d.rank), 0, stream, static_cast<const bf16*>(q),      \
                        static_cast<const bf16*>(W_keys), n, d.num_heads, d.rank, d.rope_dim,                      \
-                       reinterpret_cast<_Float16*>(ws), ups, scale, wave_rows, first);                            \
+                       reinterpret_cast<_Float16*>(ws), ups, unit, unit_exp, wave_rows, first);                          \
   else                                                                                                            \
     hipLaunchKernelGGL((joint_fold<D>), grid, dim3(64), 0, stream, static_cast<const bf16*>(q),                   \
                        static_cast<const bf16*>(W_keys), n, d.num_heads, d.rank, d.rope_dim,                      \

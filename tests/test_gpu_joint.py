@@ -882,6 +882,29 @@ def test_factors_of_other_sizes(size):
         check(host(joint_prefill(j, q[0], start, pool, table, seq, 128, wk, wv)), want[0], np.abs(want).max())
 
 
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+def test_scales_of_other_sizes(cache):
+    """A scale of 2^70 over tokens of 2^-40 and queries of 2^-30, and the reverse: the scores
+    are those of unit sizes."""
+    from paper_2607_24331_amd import joint_decode, joint_prefill
+    for tokens, queries in ((-40, -30), (30, 40)):
+        g = gen(6)
+        j = joint_of(4, 64, 128, 32, cache, scale=2.0 ** -(tokens + queries) / 10)
+        pool = filled(j, 2, g)
+        if cache == "bf16":
+            pool = (pool.double() * 2.0 ** tokens).to(BF16)
+        else:
+            pool[:, PAGE * 160:] = (pool[:, PAGE * 160:].int() + tokens).to(torch.uint8)
+        table = torch.arange(2, dtype=torch.int32, device="cuda").view(1, 2)
+        seq = torch.tensor([99], dtype=torch.int32, device="cuda")
+        q = (randn(g, 1, 3, 4, 96).double() * 2.0 ** queries).to(BF16)
+        wk, wv = factors(j, g)
+        want = oracle_decode(j, q, pool, table, [99], 128, wk, wv)
+        check(host(joint_decode(j, q, pool, table, seq, 128, wk, wv)), want, np.abs(want).max())
+        start = torch.tensor([0, 3], dtype=torch.int32, device="cuda")
+        check(host(joint_prefill(j, q[0], start, pool, table, seq, 128, wk, wv)), want[0], np.abs(want).max())
+
+
 def test_zero_tokens_factors_and_queries():
     """Zeros throughout: the powers of two of nothing.  Scores of 0 weigh alike."""
     from paper_2607_24331_amd import joint_decode, joint_prefill

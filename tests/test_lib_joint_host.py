@@ -172,6 +172,15 @@ def test_prefill_refusals(lib, change, status):
         assert lib.dckv_last_error().decode().startswith("joint_prefill:")
 
 
+def test_prompt_grids_end_before_the_devices(lib):
+    """Four work-groups of 256 threads a tile of 64 tokens, and some for the factors: 2^32
+    threads are out of a grid's reach."""
+    d = capi.JointDesc(1, 64, 128, 0, 0, 0.0)
+    n = ctypes.c_size_t()
+    for tiles, status in ((2 ** 22 - 1024, 0), (2 ** 22 - 1020, E), (2 ** 22, E)):
+        assert lib.dckv_joint_prefill_workspace_bytes(ctypes.byref(d), 1, 5, 64 * tiles, 2 ** 31, ctypes.byref(n)) == status
+
+
 def test_binding_refusals():
     from paper_2607_24331_amd import Joint, joint_append, joint_decode, joint_prefill, joint_read
     from paper_2607_24331_amd import DckvError
