@@ -147,13 +147,14 @@ __device__ __forceinline__ int find_end(const int* ends, int n, int x) {
 }
 
 __global__ __launch_bounds__(1024) void prompt_plan(PromptArgs a) {
-  constexpr int kBins = 128, N = 1024;
+  constexpr uint32_t kBins = 128;
+  constexpr int N = 1024;
   __shared__ int wave_rows[16], wave_toks[16];
   __shared__ int64_t wave_len[16];
   __shared__ int bins[kBins];
   __shared__ int row_end[N], tok_end[N], lo_of[N], n_of[N], len_of[N], kv_of[N];
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  for (int i = tid; i < kBins; i += N) bins[i] = 0;
+  for (int i = tid; i < int(kBins); i += N) bins[i] = 0;
   for (int i = tid; i < kSlots * a.slot; i += N) a.most[i] = make_int2(0, 0);
   if (tid < 2) a.counts[2 + tid] = 0;
   const int most = (a.max_context + kTok - 1) / kTok + 1;
@@ -204,17 +205,18 @@ __global__ __launch_bounds__(1024) void prompt_plan(PromptArgs a) {
         __syncthreads();
       }
       for (int x = tid; x < all_rows; x += N) {
-        const int s = find_end(row_end, N, x);
+        const int s = find_end(row_end, min(N, a.batch - b0), x);
         const int n_s = n_of[s], T_s = len_of[s], i = x - (row_end[s] - (n_s + kRows - 1) / kRows);
         const int last = T_s - n_s + min((i + 1) * kRows, n_s);       // tokens that the tile's last row sees
-        const int bin = kBins - 1 - int(int64_t((max(last, 0) + kTok - 1) / kTok) * kBins / most);
+        // at most 2^25 - 1 token tiles times 2^7
+        const int bin = int(kBins) - 1 - int(uint32_t((max(last, 0) + kTok - 1) / kTok) * kBins / uint32_t(most));
         const int at = atomicAdd(&bins[bin], 1);
         if (walk == 1 && at < a.q_tiles)
           a.rows[at] = RowTile{lo_of[s] + i * kRows, min(kRows, n_s - i * kRows), kv_of[s], T_s - n_s + i * kRows, b0 + s, {0, 0, 0}};
       }
       if (walk == 1)
         for (int x = tid; x < all_toks; x += N) {
-          const int s = find_end(tok_end, N, x);
+          const int s = find_end(tok_end, min(N, a.batch - b0), x);
           if (toks + x < a.kv_tiles)
             a.toks[toks + x] = make_int2(b0 + s, x - (tok_end[s] - (len_of[s] + kTok - 1) / kTok));
         }
