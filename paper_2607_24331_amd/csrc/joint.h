@@ -44,6 +44,7 @@ struct JointAttend {
   const int32_t* table;         // page_table, or the prefix's pages
   int32_t max_pages;            // of a row of the table
   const int64_t* start;         // first tile of each sequence among all, [batch + 1], then the cut: per, whole
+  const int32_t* segment;       // first segment of each, [batch + 1], where they are whole
   const int32_t* seq_lens;
   int32_t max_context, batch, queries, heads;
   int32_t units, slices;
@@ -66,23 +67,13 @@ __host__ __device__ inline int64_t joint_tiles_a_unit(int64_t total, int units, 
   return n < groups ? groups : n;
 }
 
-// How `total` tiles of `batch` sequences are cut into units' segments.  Segments of sequence
-// b, whose first tile is start, are numbered from start / per + b on.
-//   whole   a unit is a segment: up to `per` tiles of one sequence; unit = segment.  The ends
-//           of a segment cost about what ten tiles do, so this is taken where it makes a
-//           unit no more than kJointWhole tiles longer than equal shares.
-//   shares  unit u takes tiles u * per .. of all, whatever sequences they are of; segment u + b.
+// How the tiles of all sequences are cut into units' segments; the fold's extra wave decides.
+//   whole   a unit is a segment: up to `per` tiles of one sequence, numbered in order
+//   shares  unit u takes tiles u * per .. of all, whatever sequences they are of; segment u + b
 struct JointCut {
   int64_t per;
   bool whole;
 };
-constexpr int kJointWhole = 12;
-__host__ __device__ inline JointCut joint_cut(int64_t total, int units, int batch, int groups) {
-  const int spare = units - batch > units / 4 ? units - batch : (units + 3) / 4;
-  const int64_t per = joint_tiles_a_unit(total, spare, groups), share = joint_tiles_a_unit(total, units, groups);
-  if (per <= share + kJointWhole) return JointCut{per, true};
-  return JointCut{share, false};
-}
 
 struct JointPrompt {
   dckv_joint_desc d;

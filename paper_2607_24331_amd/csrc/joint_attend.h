@@ -38,7 +38,7 @@
 // and over position keys are summed apart and take the tokens' powers in fp32; the weights
 // take them, held against a maximum u of score + exponent of their own, so that they are at
 // most 2^(kSlack + kRaise) whatever the exponents are: f16 again, 2^-12 of a weight.
-// Work is cut by the sequences' actual lengths (joint_cut): into equal shares of all
+// Work is cut by the sequences' actual lengths (JointCut): into equal shares of all
 // their tiles, a unit walking over the sequences that it meets, or a sequence at a time.
 #pragma once
 
@@ -243,14 +243,17 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
   const int unit = (id / (8 * a.slices)) * 8 + (id & 7), slice = (id >> 3) % a.slices;
   const bool prefix = a.prefix_len > 0;
   const int rows = a.queries * a.heads * (prefix ? a.batch : 1);
+  bool whole = false;
   // 64 sequences at a time, a lane one: first tile, that of the next one, tokens
   int win = 0, win_len = 0;
   int64_t win_start = 0, win_end = 0;
+  int win_segment = 0;
   auto load_window = [&](int b0) {
     win = b0;
     const int i = min(b0 + lane, a.batch - 1);
     win_start = a.start[i];
     win_end = a.start[i + 1];
+    win_segment = whole ? a.segment[i] : 0;
     win_len = min(max(a.seq_lens[i], 0), a.max_context);
   };
   auto lane64 = [](int64_t x, int l) {
@@ -259,34 +262,33 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
   };
   int b = 0;
   int64_t at, end;                                    // tiles of this unit, among all
-  bool whole = false;
   if (prefix) {
     const int64_t total = (a.prefix_len + kJointTile - 1) / kJointTile, per = joint_tiles_a_unit(total, a.units, NG);
     at = unit * per;
     end = min(at + per, total);
   } else {
-    load_window(0);
     const int64_t total = a.start[a.batch];
     const JointCut cut{a.start[a.batch + 1], a.start[a.batch + 2] != 0};
     whole = cut.whole;
+    load_window(0);
     // the last sequence b whose first tile (whole: first segment) is at most this unit's
     const int64_t want = cut.whole ? unit : unit * cut.per;
-    auto key = [&](int64_t start, int i) { return cut.whole ? joint_div(start, cut.per) + i : start; };
     int lo = 0, n = a.batch;                          // the answer is in lo .. lo + n - 1
     while (n > 64) {
       const int step = (n + 63) / 64, i = lo + lane * step;
-      const bool in = lane * step < n && key(a.start[min(i, a.batch)], i) <= want;
+      const int ib = min(i, a.batch);
+      const bool in = lane * step < n && (cut.whole ? int64_t(a.segment[ib]) : a.start[ib]) <= want;
       const int k = max(__popcll(__ballot(in)) - 1, 0);      // keys ascend: the first lanes hold
       lo += k * step;
       n = min(step, n - k * step);
     }
     lo = __builtin_amdgcn_readfirstlane(lo);
     if (lo != 0) load_window(lo);
-    const int k = max(__popcll(__ballot(lane < n && key(win_start, lo + lane) <= want)) - 1, 0);
+    const int k = max(__popcll(__ballot(lane < n && (cut.whole ? int64_t(win_segment) : win_start) <= want)) - 1, 0);
     b = __builtin_amdgcn_readfirstlane(lo + k);
     const int64_t s0 = lane64(win_start, b - win), s1 = lane64(win_end, b - win);
     if (cut.whole) {
-      at = s0 + (unit - key(s0, b)) * cut.per;
+      at = s0 + int64_t(unit - __builtin_amdgcn_readlane(win_segment, b - win)) * cut.per;
       end = min(at + cut.per, s1);
     } else {
       at = want;

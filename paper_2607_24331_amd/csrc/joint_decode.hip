@@ -36,45 +36,84 @@ __device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c) {
 struct FoldStarts {
   const int32_t* seq_lens;
   int64_t* starts;
+  int32_t* segments;
   int32_t max_context, batch, units, groups;
 };
 
-// starts[b]: tiles of the sequences before b, starts[batch] of all.  One wave, 16
-// sequences a lane.
+// starts[b]: tiles of the sequences before b, starts[batch] of all; then the cut, and segments[b]
+// likewise where sequences are cut by themselves.  U sequences a lane at a time.
+//
+// The ends of a segment cost about what ten tiles do, so sequences are cut by themselves where that
+// makes a unit no more than kWhole tiles longer than equal shares.  A sequence loses half a
+// unit in the mean, one at most: of the shares that spare 1/2, 5/8, 3/4 or all of the
+// batch the first whose segments are no more than the units is taken (64 ragged e4m3 sequences:
+// 57 us, 61 where all is spared; batches above 64 spare all).  Where shares are short, segments
+// beyond the units run behind the first ones (300 sequences of up to 700 tokens: 63 us, in
+// shares 93; 250 of 4,000, whose shares are long: 230 and 140).
+constexpr int kWhole = 12, kShort = 40;
+template <int U>
 __device__ void form_starts(const FoldStarts& f) {
-  const int lane = threadIdx.x;
-  int64_t base = 0;
-  for (int b0 = 0; b0 < f.batch; b0 += 1024) {
-    int n[16];
-    int64_t own = 0;
+  const int lane = threadIdx.x & 63;
+  int n[U];
+  auto load = [&](int b0) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int b = b0 + 16 * lane + i;
+    for (int i = 0; i < U; ++i) {
+      const int b = b0 + U * lane + i;
       const int T = b < f.batch ? min(max(f.seq_lens[b], 0), f.max_context) : 0;
       n[i] = (T + kJointTile - 1) / kJointTile;
-      own += n[i];
     }
-    int64_t sum = own;
+  };
+  auto walk = [&](auto&& count, auto* out) {           // out[b]: the counts before b; their sum
+    int64_t base = 0;
+    for (int b0 = 0; b0 < f.batch; b0 += 64 * U) {
+      if (f.batch > 64 * U) load(b0);
+      int64_t own = 0;
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int64_t x = __shfl_up((long long)sum, o);
-      if (lane >= o) sum += x;
-    }
-    int64_t at = base + sum - own;
+      for (int i = 0; i < U; ++i) own += count(n[i]);
+      int64_t sum = own;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int b = b0 + 16 * lane + i;
-      if (b < f.batch) f.starts[b] = at;
-      at += n[i];
+      for (int o = 1; o < 64; o <<= 1) {
+        const int64_t x = __shfl_up((long long)sum, o);
+        if (lane >= o) sum += x;
+      }
+      int64_t at = base + sum - own;
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int b = b0 + U * lane + i;
+        if (b < f.batch) out[b] = at;
+        at += count(n[i]);
+      }
+      base += __shfl((long long)sum, 63);
     }
-    base += __shfl((long long)sum, 63);
+    if (lane == 0) out[f.batch] = base;
+    return base;
+  };
+  load(0);
+  const int64_t total = walk([](int t) { return int64_t(t); }, f.starts);
+  const int64_t share = joint_tiles_a_unit(total, f.units, f.groups);
+  auto tiles_spared = [&](int eighths) {
+    const int spare = f.units - f.batch * eighths / 8;
+    return joint_tiles_a_unit(total, spare > f.units / 4 ? spare : (f.units + 3) / 4, f.groups);
+  };
+  auto segments_of = [](int t, int64_t per) { return per >= t ? int64_t(t > 0) : int64_t((uint32_t(t) + uint32_t(per) - 1) / uint32_t(per)); };
+  int64_t per = tiles_spared(8);
+  if (U == 1) {                                        // the sequences are in the lanes
+#pragma unroll
+    for (int k = 6; k >= 4; --k) {
+      const int64_t tried = tiles_spared(k);
+      int sum = int(segments_of(n[0], tried));         // at most units + batch in all
+#pragma unroll
+      for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o);
+      if (sum <= f.units) per = tried;
+    }
   }
+  const bool whole = per <= share + kWhole || share <= kShort;
+  if (!whole) per = share;
   if (lane == 0) {
-    const JointCut cut = joint_cut(base, f.units, f.batch, f.groups);
-    f.starts[f.batch] = base;
-    f.starts[f.batch + 1] = cut.per;
-    f.starts[f.batch + 2] = cut.whole;
+    f.starts[f.batch + 1] = per;
+    f.starts[f.batch + 2] = whole;
   }
+  if (whole) walk([&](int t) { return segments_of(t, per); }, f.segments);
 }
 
 // The columns of 16 k rows of a factor's tile in LDS (st bytes a row) as B operands of 32x32x16:
@@ -103,7 +142,12 @@ __global__ __launch_bounds__(64) void joint_fold(const bf16* __restrict__ q, con
   __shared__ __align__(16) unsigned char wk[D * ST];
   const int cols = r / 32;
   if (int(blockIdx.x) == heads * cols) {
-    if (blockIdx.y == 0) form_starts(starts);
+    if (blockIdx.y == 0) {
+      if (starts.batch <= 64)
+        form_starts<1>(starts);
+      else
+        form_starts<16>(starts);
+    }
     return;
   }
   const int head = blockIdx.x / cols, c0 = (blockIdx.x % cols) * 32;
@@ -170,7 +214,12 @@ __global__ __launch_bounds__(1024) void joint_fold_e4m3(const bf16* __restrict__
   const int tid = threadIdx.x, lane = tid & 63, lr = lane & 31, h = lane >> 5, threads = 2 * r;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6), c0 = 32 * w, st = 2 * r + 32;
   if (int(blockIdx.x) == heads) {
-    if (blockIdx.y == 0 && w == 0) form_starts(starts);
+    if (blockIdx.y == 0 && w == 0) {
+      if (starts.batch <= 64)
+        form_starts<1>(starts);
+      else
+        form_starts<16>(starts);
+    }
     return;
   }
   const int head = blockIdx.x, W = r + p;
@@ -281,6 +330,7 @@ __global__ __launch_bounds__(1024) void joint_fold_e4m3(const bf16* __restrict__
 
 struct FinishArgs {
   const int64_t* start;
+  const int32_t* segment;
   const float* part_o;
   const float4* part_ml;
   const float* pre_o;
@@ -316,8 +366,11 @@ __global__ __launch_bounds__(R / 4 * GR) void joint_merge(FinishArgs a, float* _
   // shares: those of the sequence's units, then the prefix's
   const int64_t s0 = a.start[b], s1 = a.start[b + 1];
   const JointCut cut{a.start[a.batch + 1], a.start[a.batch + 2] != 0};
-  const int64_t u0 = joint_div(s0, cut.per);
-  const int own = s1 <= s0 ? 0 : int(joint_div(cut.whole ? s1 - s0 + cut.per - 1 : s1 - 1 - u0 * cut.per + cut.per, cut.per));
+  // its first segment and their number
+  const int64_t u0 = cut.whole ? a.segment[b] : joint_div(s0, cut.per);
+  const int64_t seg0 = cut.whole ? u0 : u0 + b;
+  const int own = cut.whole ? int(a.segment[b + 1] - u0)
+                            : s1 <= s0 ? 0 : int(joint_div(s1 - 1 - u0 * cut.per + cut.per, cut.per));
   int pre = 0;
   if (a.prefix_len > 0) {
     const int64_t tiles = (a.prefix_len + kJointTile - 1) / kJointTile;
@@ -328,7 +381,7 @@ __global__ __launch_bounds__(R / 4 * GR) void joint_merge(FinishArgs a, float* _
   const int rr = i * a.heads + head;
   const auto share = [&](int s, int64_t& at) {
     if (s < own) {
-      at = ((u0 + s + b) * a.slices + (rr >> a.row_log)) * (1 << a.row_log) + (rr & ((1 << a.row_log) - 1));
+      at = ((seg0 + s) * a.slices + (rr >> a.row_log)) * (1 << a.row_log) + (rr & ((1 << a.row_log) - 1));
       const float4 ml = a.part_ml[at];
       at *= R;
       return ml;
@@ -592,7 +645,7 @@ JointShape joint_shape(const dckv_joint_desc& d, int32_t queries, int32_t batch,
   const size_t width = size_t(d.rank + d.rope_dim);
   s.off_up = align_up(size_t(all) * width * (c8 ? 2 : 4));
   s.off_start = s.off_up + align_up(size_t(all) * (c8 ? 4 : 0));
-  s.off_mean = s.off_start + align_up(size_t(batch + 3) * 8);
+  s.off_mean = s.off_start + align_up(size_t(batch + 3) * 8 + size_t(batch + 1) * 4);
   s.off_o = s.off_mean + align_up(size_t(all) * d.rank * 4);
   const size_t own = size_t(s.units + batch) * s.slices * 16 * s.row_waves;
   s.off_ml = s.off_o + align_up(own * d.rank * 4);
@@ -632,7 +685,8 @@ hipError_t launch_joint_decode(const JointShape& s, const void* q, const void* p
   int unit_exp;
   const float unit = std::frexp(scale, &unit_exp);     // at most 1: nothing overflows by it
   const dim3 grid(d.num_heads * (c8 ? 1 : d.rank / 32) + 1, (n + wave_rows - 1) / wave_rows);
-  const FoldStarts first{seq_lens, starts, s.max_context, s.batch, s.units, groups_of(d, s.row_waves)};
+  int32_t* segments = reinterpret_cast<int32_t*>(starts + s.batch + 3);
+  const FoldStarts first{seq_lens, starts, segments, s.max_context, s.batch, s.units, groups_of(d, s.row_waves)};
 #define DCKV_FOLD(D)                                                                                              \
   if (c8)                                                                                                         \
     hipLaunchKernelGGL((joint_fold_e4m3<D>), grid, dim3(2 * d.rank), 0, stream, static_cast<const bf16*>(q),      \
@@ -657,6 +711,7 @@ hipError_t launch_joint_decode(const JointShape& s, const void* q, const void* p
   a.num_pages = num_pages;
   a.page_bytes = joint_page_bytes(d);
   a.start = starts;
+  a.segment = segments;
   a.seq_lens = seq_lens;
   a.max_context = s.max_context;
   a.batch = s.batch;
@@ -684,7 +739,7 @@ hipError_t launch_joint_decode(const JointShape& s, const void* q, const void* p
     e = attend(d, s.row_waves, a, stream);
     if (e != hipSuccess) return e;
   }
-  const FinishArgs f{starts, a.part_o, a.part_ml, reinterpret_cast<const float*>(ws + s.off_pre_o),
+  const FinishArgs f{starts, segments, a.part_o, a.part_ml, reinterpret_cast<const float*>(ws + s.off_pre_o),
                      reinterpret_cast<const float4*>(ws + s.off_pre_ml), s.batch, s.queries, d.num_heads,
                      31 - __builtin_clz(16 * s.row_waves), s.slices, 31 - __builtin_clz(16 * s.pre_row_waves),
                      s.pre_slices, s.pre_units, groups_of(d, s.pre_row_waves), s.prefix_len};
