@@ -599,6 +599,32 @@ def test_batches_and_long_contexts(H, d, r, p, cache, B, low, high, Q, n):
     assert torch.equal(out, again)
 
 
+@pytest.mark.parametrize("B,high", [(64, 3000), (65, 3000), (1024, 90), (1025, 90), (2500, 40)])
+@pytest.mark.parametrize("H,r,cache", [(8, 128, "bf16"), (20, 256, "e4m3")])
+def test_cuts_of_many_sequences(B, high, H, r, cache):
+    """Batches at the ends of what the cut is formed from, a third of the sequences empty."""
+    from paper_2607_24331_amd import joint_decode
+    g = gen(B)
+    j = joint_of(H, 64, r, 32, cache)
+    rng = np.random.default_rng(B)
+    lens = rng.integers(0, high + 1, B) * (rng.random(B) > 0.33)
+    lens[-1] = 0
+    lens[rng.integers(0, B - 1)] = high
+    width = -(-high // PAGE)
+    pages = 700
+    pool = filled(j, pages, g)
+    table = torch.randint(0, pages, (B, width), generator=g, device="cuda", dtype=torch.int32)
+    q = randn(g, B, 1, H, 96).to(BF16)
+    wk, wv = factors(j, g)
+    seq = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    got = host(joint_decode(j, q, pool, table, seq, high, wk, wv))
+    assert not got[lens == 0].any()
+    some = [*np.flatnonzero(lens)[:6], int(np.argmax(lens)), *np.flatnonzero(lens)[-6:]]
+    for b in some:
+        want = oracle_decode(j, q[b:b + 1], pool, table[b:b + 1], [lens[b]], high, wk, wv)
+        check(got[b], want[0], np.abs(want).max(), b)
+
+
 @pytest.mark.parametrize("H,d,r,p,cache,Q", [(16, 64, 128, 32, "bf16", 1), (16, 128, 512, 64, "e4m3", 1),
                                              (32, 64, 256, 0, "bf16", 1)])
 def test_one_long_sequence_among_many(H, d, r, p, cache, Q):
