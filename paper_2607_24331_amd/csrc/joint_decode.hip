@@ -6,11 +6,14 @@
 // joint_fold    a wave a (head, 32 latent columns, 32 or 128 rows): the head's factor columns lie
 //               in LDS once, read by the transposing load, as the contraction runs over
 //               the factor's rows; products on MFMA 32x32x16.  One more wave forms
-//               the sequences' first tiles.  Bound by latency and, once, by the factor's bytes.
+//               the sequences' first tiles and the cut of the work.  Bound by latency and,
+//               once, by the factor's bytes (32 heads at rank 512: 4 rows a head 3.9 us, 64 7.5).
+// joint_fold_e4m3   the same for f16 queries, a work-group all columns of a head (64 rows: 8.0 us).
 // joint_merge   a work-group a row: its shares' sums in fp32, 16 bytes a lane.  Bound by
 //               the shares' bytes (4,096 rows of 10 shares at rank 512, 92 MB: 16 us, 5.7 TB/s).
 // joint_values  the product with the heads' factor rows on MFMA, 32 rows by 32 coordinates a
-//               work-group, its waves a quarter of the latent coordinates each.
+//               work-group, its waves a quarter of the latent coordinates each (2,048 rows of
+//               128 coordinates at rank 512: 4.8 us).
 #include <algorithm>
 #include <cmath>
 #include <limits>
