@@ -629,7 +629,9 @@ int dckv_joint_read(const dckv_joint_desc* desc, const void* pool, int64_t num_p
  * more than 32 rows (Q*H, for the prefix batch*Q*H).
  * Whatever lies in slots that a query does not see (NaN included) does not reach its
  * result; a NaN in one that it sees makes it NaN, and an infinity or an infinite score
- * does, but that a token whose score is minus infinity may weigh nothing.
+ * does, but that a token whose score is minus infinity may weigh nothing.  A NaN in
+ * W_keys makes its head's results NaN, an element of W_values that is not finite its
+ * coordinate of its head NaN or infinite.
  * A workspace (256-byte aligned; its contents do not matter) of
  * dckv_joint_workspace_bytes also serves fewer sequences, shorter contexts and shorter
  * prefixes (not a prefix where none was named).  Calls that may overlap need workspaces
@@ -663,7 +665,8 @@ int dckv_joint_decode(const dckv_joint_desc* desc, int32_t queries, const void* 
  * sequence's bound (greatest |latent coordinate| * r * greatest |factor element|, or the
  * greatest |position key|, over all its tokens, those that a row does not see too) lose
  * bits.  Values that overflow fp32 count as the greatest
- * number.  A token that is not finite makes every row that sees it NaN.  Unseen slots,
+ * number.  A token that is not finite makes every row that sees it NaN, an element of
+ * W_values that is not finite its coordinate of its head.  Unseen slots,
  * pages, alignment and errors as for dckv_joint_decode; the workspace serves fewer
  * sequences, rows and tokens too. */
 int dckv_joint_prefill_workspace_bytes(const dckv_joint_desc* desc, int32_t batch, int32_t n_rows,

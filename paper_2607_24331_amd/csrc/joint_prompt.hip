@@ -65,7 +65,8 @@ struct PromptArgs {
   int32_t n_rows, batch, max_context;
   int64_t total_context;
   int32_t q_tiles, kv_tiles;              // at most
-  int32_t* counts;                        // row tiles, token tiles; bf16 bits of the greatest |W_keys|, |W_values|
+  int32_t* counts;                        // row tiles, token tiles; bf16 bits of the greatest finite |W_keys|,
+                                          // |W_values|; whether W_values has elements that are not finite
   int2* most;                             // [kSlots][slot] bf16 bits of a sequence's greatest |latent|, |key| coordinate
   int32_t slot;                           // sequences a slot, whole lines of 128 bytes
   RowTile* rows;
@@ -92,6 +93,10 @@ __device__ __forceinline__ float power(int e) { return __uint_as_float(uint32_t(
 // The greater of two pairs of 16 bits; a wave's greatest 16 bits.
 __device__ __forceinline__ uint32_t most_pairs(uint32_t a, uint32_t b) {
   return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(ushort2_, a), __builtin_bit_cast(ushort2_, b)));
+}
+// Whether one of a pair of bf16 is not finite.
+__device__ __forceinline__ bool not_finite(uint32_t w) {
+  return (((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u) != 0;
 }
 __device__ __forceinline__ int most_half(uint32_t m) { return int(max(m & 0xFFFFu, m >> 16)); }
 __device__ __forceinline__ int wave_most(int m) {
@@ -156,7 +161,7 @@ __global__ __launch_bounds__(1024) void prompt_plan(PromptArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   for (int i = tid; i < int(kBins); i += N) bins[i] = 0;
   for (int i = tid; i < kSlots * a.slot; i += N) a.most[i] = make_int2(0, 0);
-  if (tid < 2) a.counts[2 + tid] = 0;
+  if (tid < 3) a.counts[2 + tid] = 0;
   const int most = (a.max_context + kTok - 1) / kTok + 1;
   int all_toks = 0, all_rows = 0;         // of the round's sequences
   // two walks over the sequences, 1024 at a time: the first counts row tiles by their
@@ -266,6 +271,7 @@ __global__ __launch_bounds__(256) void prompt_gather(PromptArgs a, GatherArgs s)
     const int id = blockIdx.x - 4 * a.kv_tiles, which = id >= s.factor_groups, g = id - (which ? s.factor_groups : 0);
     const u32x4* W = reinterpret_cast<const u32x4*>(which ? s.W_values : s.W_keys);
     uint32_t m = 0;
+    bool odd_factor = false;
     u32x4 x[kFactorPieces];
 #pragma unroll
     for (int k = 0; k < kFactorPieces; ++k) {
@@ -276,10 +282,12 @@ __global__ __launch_bounds__(256) void prompt_gather(PromptArgs a, GatherArgs s)
 #pragma unroll
     for (int k = 0; k < kFactorPieces; ++k)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {                    // one that is not finite spoils its head's coordinate anyway
-        const bool bad = (((x[k][e] & 0x7F807F80u) + 0x00800080u) & 0x80008000u) != 0;
+      for (int e = 0; e < 4; ++e) {                    // one that is not finite spoils its head's coordinate
+        const bool bad = not_finite(x[k][e]);
+        odd_factor |= bad;
         m = most_pairs(m, bad ? 0u : x[k][e] & 0x7FFF7FFFu);
       }
+    if (which && __any(odd_factor) && (threadIdx.x & 63) == 0) atomicOr(&a.counts[4], 1);
     most[0][threadIdx.x >> 6] = wave_most(most_half(m));
     __syncthreads();
     if (threadIdx.x == 0)
@@ -326,7 +334,7 @@ __global__ __launch_bounds__(256) void prompt_gather(PromptArgs a, GatherArgs s)
     } else {
       x[0] = y[k];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) bad |= (((y[k][e] & 0x7F807F80u) + 0x00800080u) & 0x80008000u) != 0;
+      for (int e = 0; e < 4; ++e) bad |= not_finite(y[k][e]);
     }
     if (bad) atomicOr(&odd, 1u << (t & 15));
     if (bad || t - t0 >= have)
@@ -387,6 +395,18 @@ __device__ __forceinline__ void expand_stage(floatx4 (&acc)[ROWS][COLS], const u
   }
 }
 
+// Whether a factor's row of r elements has one that is not finite.
+__device__ __forceinline__ bool row_is_odd(const bf16* row, int r) {
+  bool odd = false;
+#pragma unroll 1
+  for (int i = 0; i < r; i += 8) {
+    const u32x4 x = *reinterpret_cast<const u32x4*>(row + i);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) odd |= not_finite(x[e]);
+  }
+  return odd;
+}
+
 template <int D, int NT>
 __global__ __launch_bounds__(512) void prompt_expand(PromptArgs a, const bf16* __restrict__ c, const bf16* __restrict__ W_keys,
                                                      const bf16* __restrict__ W_values, int heads, int r,
@@ -397,6 +417,7 @@ __global__ __launch_bounds__(512) void prompt_expand(PromptArgs a, const bf16* _
   const int tiles = D == 128 ? heads : (heads + 1) / 2;  // of 256 coordinates
   const int f = blockIdx.x % tiles, blk = blockIdx.x / tiles;
   const int n_tiles = a.counts[1], kv_tiles = a.kv_tiles;
+  const bool odd_factor = a.counts[4] != 0;
   if (blk * TOK >= n_tiles * kTok) return;
   const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lq = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -494,14 +515,17 @@ __global__ __launch_bounds__(512) void prompt_expand(PromptArgs a, const bf16* _
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int col = (D == 128 ? (wf & 1) * 64 : 0) + 16 * j + lr;
+      // elements that are not finite make their coordinate NaN, which the clamp would drop
+      bool odd_row = false;
+      if (odd_factor) odd_row = row_is_odd(W_values + (int64_t(head) * D + col) * r, r);
 #pragma unroll
       for (int s = 0; s < NT / 2; ++s) {
         const int tok = tok0 + 32 * s;
         floatx4 lo = acc[2 * s][j] * down[s / 2], hi = acc[2 * s + 1][j] * down[s / 2];
 #pragma unroll
         for (int v = 0; v < 4; ++v) {                  // a weight of 0 times an overflow would be none
-          lo[v] = fminf(fmaxf(lo[v], -kMaxHalf), kMaxHalf);
-          hi[v] = fminf(fmaxf(hi[v], -kMaxHalf), kMaxHalf);
+          lo[v] = odd_row ? __builtin_nanf("") : fminf(fmaxf(lo[v], -kMaxHalf), kMaxHalf);
+          hi[v] = odd_row ? __builtin_nanf("") : fminf(fmaxf(hi[v], -kMaxHalf), kMaxHalf);
         }
         *reinterpret_cast<u32x4*>(values + (tile0 + (tok >> 6)) * (kTok * D * 2) + col * (kTok * 2) +
                                   ((4 * (tok >> 5 & 1) + lq) ^ joint_swap(8, col)) * 16) =

@@ -955,3 +955,36 @@ def test_zero_tokens_factors_and_queries():
             size = max(np.abs(want).max(), 1e-30)
             check(host(joint_decode(j, x, pool, table, seq, 128, a, b)), want, size, (cache, what))
             check(host(joint_prefill(j, x[0], start, pool, table, seq, 128, a, b)), want[0], size, (cache, what))
+
+
+@pytest.mark.parametrize("H,d,r,p,cache,T", [(3, 64, 128, 32, "bf16", 150), (2, 128, 512, 64, "e4m3", 150),
+                                             (5, 64, 256, 0, "e4m3", 70), (34, 128, 128, 0, "bf16", 2100)])
+@pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
+def test_factors_that_are_not_finite(H, d, r, p, cache, T, value):
+    """One element of W_values spoils its coordinate of its head, a NaN in W_keys its head;
+    every other result keeps its bits.  34 heads over 2,100 tokens: blocks of 256 tokens."""
+    from paper_2607_24331_amd import joint_decode, joint_prefill
+    j = joint_of(H, d, r, p, cache)
+    added = 40
+    pool, table, start, q, wk, wv, seq, rs, lens, top = prompt_case(j, [T - added], [added], 0, 21)
+    h, i, col = H - 1, d - 3, 77
+    wk[h, i, col] = wv[h, i, col] = 0
+    qs = q.view(1, added, H, d + p)
+    forms = {"prompt": lambda k, v: joint_prefill(j, q, rs, pool, table, seq, top, k, v),
+             "decode": lambda k, v: joint_decode(j, qs, pool, table, seq, top, k, v)[0]}
+    for what, run in forms.items():
+        clean = run(wk, wv)
+        bad = wv.clone()
+        bad[h, i, col] = value
+        got = run(wk, bad)
+        assert not torch.isfinite(got[:, h, i]).any(), what
+        if math.isnan(value):
+            assert torch.isnan(got[:, h, i]).all(), what
+        got[:, h, i] = clean[:, h, i]
+        assert torch.equal(got, clean), what
+        bad = wk.clone()
+        bad[h, i, col] = value
+        got = run(bad, wv)
+        assert torch.equal(got[:, :h], clean[:, :h]), what
+        # an infinite element gives infinite scores of either sign: here every row sees both
+        assert torch.isnan(got[:, h]).all(), what
