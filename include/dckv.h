@@ -664,11 +664,11 @@ int dckv_joint_decode(const dckv_joint_desc* desc, int32_t queries, const void* 
  * powers of two a sequence and a row, sums are fp32: keys and values 2^-29 of the
  * sequence's bound (greatest |latent coordinate| * r * greatest |factor element|, or the
  * greatest |position key|, over all its tokens, those that a row does not see too) lose
- * bits.  Values that overflow fp32 count as the greatest
- * number.  A token that is not finite makes every row that sees it NaN, an element of
- * W_values that is not finite its coordinate of its head.  Unseen slots,
- * pages, alignment and errors as for dckv_joint_decode; the workspace serves fewer
- * sequences, rows and tokens too. */
+ * bits.  Values that overflow fp32 count as the greatest number; of scores that
+ * overflow it the greatest alone weighs.  A token that is not finite makes every row
+ * that sees it NaN, an element of W_values that is not finite its coordinate of its
+ * head.  Unseen slots, pages, alignment and errors as for dckv_joint_decode; the
+ * workspace serves fewer sequences, rows and tokens too. */
 int dckv_joint_prefill_workspace_bytes(const dckv_joint_desc* desc, int32_t batch, int32_t n_rows,
                                        int32_t max_context, int64_t total_context, size_t* bytes);
 int dckv_joint_prefill(const dckv_joint_desc* desc, const void* q, int32_t n_rows,

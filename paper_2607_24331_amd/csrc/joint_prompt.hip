@@ -632,8 +632,10 @@ __global__ __launch_bounds__(256, 2) void prompt_attend(PromptArgs a, const uint
 #pragma unroll
   for (int i = 0; i < PS; ++i) to_half(qp[i]);
   const Powers pw = powers_of(most_of_slots(a, rt.b, lane), a.counts[2], a.counts[3], 31 - __builtin_clz(r));
-  // from products to scores in powers of two; past the ends all weigh alike, or one alone weighs
-  const float fs = fminf(fmaxf(ldexpf(scale, pw.keys - up), 0x1p-100f), 0x1p100f);
+  // from products to scores in powers of two.  Products lie below 2^38 and, being sums of
+  // products of f16, 2^-48 or more apart, so past the ends all weigh alike, or one alone
+  // weighs; 2^38 x 2^80 is still a number
+  const float fs = fminf(fmaxf(ldexpf(scale, pw.keys - up), 0x1p-100f), 0x1p80f);
 
   f32x16 acc[CT];
 #pragma unroll

@@ -988,3 +988,33 @@ def test_factors_that_are_not_finite(H, d, r, p, cache, T, value):
         assert torch.equal(got[:, :h], clean[:, :h]), what
         # an infinite element gives infinite scores of either sign: here every row sees both
         assert torch.isnan(got[:, h]).all(), what
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("tokens,queries", [(75, 55), (100, 100), (60, 60)])
+def test_prompt_scores_past_fp32(cache, tokens, queries):
+    """Scores of 2^120 and more: the greatest one's token alone weighs, as in 64 bits.  Positive
+    queries' greatest is their own token, negative ones' the first."""
+    from paper_2607_24331_amd import joint_prefill
+    g = gen(9)
+    H, d, r, p, T = 3, 64, 128, 32, 150
+    j = joint_of(H, d, r, p, cache)
+    w = r + p
+    pool = filled(j, 3, g)
+    at = torch.from_numpy(oj.place(r, p, cache, np.arange(PAGE)[:, None], r + np.arange(p)[None])).cuda()
+    steps = 1.0 + torch.arange(3 * PAGE, device="cuda").view(3, PAGE, 1).expand(3, PAGE, p)
+    if cache == "bf16":                                # up to 192, exact in 8 bits
+        pool[:, at] = (steps.double() * 2.0 ** tokens).to(BF16)
+    else:                                              # one byte, the step in its exponent: eight tokens a power, which weigh alike
+        pool[:, at] = 0x38                             # 1.0
+        pool[:, PAGE * (w + 1):] = (127 + tokens + (steps[..., 0] / 8).floor()).clamp(max=246).to(torch.uint8)
+    table = torch.arange(3, dtype=torch.int32, device="cuda").view(1, 3)
+    seq = torch.tensor([T], dtype=torch.int32, device="cuda")
+    start = torch.tensor([0, T], dtype=torch.int32, device="cuda")
+    wk, wv = factors(j, g)
+    wk.zero_()
+    q = torch.ones(T, H, d + p, device="cuda")
+    q[:, 1] = -1.0
+    q = (q.double() * 2.0 ** queries).to(BF16)
+    want = oracle_prompt(j, pool, table, [0], q, wk, wv, [T], [T])
+    check(host(joint_prefill(j, q, start, pool, table, seq, T, wk, wv)), want, np.abs(want).max())
