@@ -51,7 +51,7 @@ struct JointAttend {
   int32_t prefix_len;           // above 0: this launch attends over the prefix
   float scale;                  // times log2(e)
   float* part_o;                // [segment][slice][rows of a work-group][r]
-  float4* part_ml;              // [segment][slice][rows]: m, l, u, 0
+  float4* part_ml;              // [segment][slice][rows]: m, l, u from m, 0
 };
 
 // a / b, not negative.  64-bit division is two hundred instructions, which a launch of one tile

@@ -36,8 +36,10 @@
 // their powers of two.  Queries are f16 under a power of two of their row (2^-12 of a
 // coordinate; 29 binades below the greatest are normal numbers).  The products over latents
 // and over position keys are summed apart and take the tokens' powers in fp32; the weights
-// take them, held against a maximum u of score + exponent of their own, so that they are at
-// most 2^(kSlack + kRaise) whatever the exponents are: f16 again, 2^-12 of a weight.
+// take them, held against a maximum of score + exponent of their own, so that they are at
+// most 2^(kSlack + kRaise) whatever the exponents are: f16 again, 2^-12 of a weight.  That
+// maximum is kept as its distance u from the scores' own, m: of scores past 2^24 a sum with an
+// exponent would lose the exponent.
 // Work is cut by the sequences' actual lengths (JointCut): into equal shares of all
 // their tiles, a unit walking over the sequences that it meets, or a sequence at a time.
 #pragma once
@@ -414,8 +416,8 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
     floatx4 acc[CT];
 #pragma unroll
     for (int i = 0; i < CT; ++i) acc[i] = floatx4{0.f, 0.f, 0.f, 0.f};
-    // m, u: references of the weights in l and in the sums (one for bf16; e4m3: + 127)
-    float m = -INFINITY, u = -INFINITY, l = 0.f;
+    // m, m + u: references of the weights in l and in the sums (one for bf16; e4m3: + 127)
+    float m = -INFINITY, u = C8 ? -INFINITY : 0.f, l = 0.f;
 
     for (int r = 0; r < rounds; ++r) {
       unsigned char* buf = bufs + (r & (NBUF - 1)) * S::TILE;
@@ -538,22 +540,32 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
               s[n][v] = pos + t < limit ? ((odd >> t) & 1 ? __builtin_nanf("") : s[n][v]) : -INFINITY;
             }
         }
-        float top = -INFINITY, utop = -INFINITY;
+        float top = -INFINITY, m_new = m;
 #pragma unroll
-        for (int n = 0; n < 2; ++n) {
+        for (int n = 0; n < 2; ++n)
 #pragma unroll
           for (int v = 0; v < 4; ++v) top = fmaxf(top, s[n][v]);
-          if constexpr (C8) {
-#pragma unroll
-            for (int v = 0; v < 4; ++v) utop = fmaxf(utop, s[n][v] + float(byte(el[n], v)));
-          }
-        }
         top = row_max(top);
-        utop = C8 ? row_max(utop) : top;
-        if (__any(top > m + kSlack || utop > u + kSlack)) {
-          const float m_new = fmaxf(m, top), u_new = C8 ? fmaxf(u, utop) : m_new;
-          l *= m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m_new);
-          const float keep = u == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(u - u_new);
+        bool raise = __any(top > m + kSlack);
+        if (raise) m_new = fmaxf(m, top);
+        const float mb = m_new == -INFINITY ? 0.f : m_new;     // nothing seen yet: weights 0
+        float u_old = u, utop = -INFINITY;
+        if constexpr (C8) {
+          if (raise) u_old = m == -INFINITY ? -INFINITY : u + (m - m_new);
+#pragma unroll
+          for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) utop = fmaxf(utop, (s[n][v] - mb) + float(byte(el[n], v)));
+          utop = row_max(utop);
+          raise |= __any(utop > u_old + kSlack) != 0;
+        }
+        if (raise) {
+          float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m_new);
+          l *= keep;
+          if constexpr (C8) {
+            u = fmaxf(u_old, utop);
+            keep = u_old == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(u_old - u);
+          }
           if (r > 0) {
 #pragma unroll
             for (int i = 0; i < CT; ++i)
@@ -561,9 +573,7 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
               for (int v = 0; v < 4; ++v) acc[i][v] *= keep;
           }
           m = m_new;
-          u = u_new;
         }
-        const float mb = m == -INFINITY ? 0.f : m;     // nothing seen yet: weights 0
         u32x4 p;
         if constexpr (C8) {
           const float ub = u == -INFINITY ? 0.f : u - kRaise;
@@ -573,7 +583,7 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
               l += __builtin_amdgcn_exp2f(s[n][v] - mb);
-              y[v] = __builtin_amdgcn_exp2f(s[n][v] + (float(byte(el[n], v)) - ub));
+              y[v] = __builtin_amdgcn_exp2f((s[n][v] - mb) + (float(byte(el[n], v)) - ub));
             }
             p[2 * n] = pair_half(y[0], y[1]);
             p[2 * n + 1] = pair_half(y[2], y[3]);
@@ -632,7 +642,7 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
         float* dst = a.part_o + (prow + rw * 16 + jr) * R + 4 * jq;
 #pragma unroll
         for (int i = 0; i < CT; ++i) *reinterpret_cast<floatx4*>(dst + 16 * i) = acc[i];
-        if (jq == 0) a.part_ml[prow + rw * 16 + jr] = make_float4(m, l, C8 ? u - 127.f - kRaise : u, 0.f);
+        if (jq == 0) a.part_ml[prow + rw * 16 + jr] = make_float4(m, l, C8 ? u - 127.f - kRaise : 0.f, 0.f);
       }
       __syncthreads();                                // the tiles are used up
     } else {
@@ -640,16 +650,19 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
       if (jq == 0) {
         join_m[w][jr] = m;
         join_l[w][jr] = l;
-        join_u[w][jr] = u;
+        if constexpr (C8) join_u[w][jr] = u;
       }
       __syncthreads();                                // the tiles are used up, m and u are there
-      float mm = -INFINITY, uu = -INFINITY;
+      float mm = -INFINITY, uu = C8 ? -INFINITY : 0.f;
 #pragma unroll
-      for (int k = 0; k < NG; ++k) {
-        mm = fmaxf(mm, join_m[k * WR + rw][jr]);
-        uu = fmaxf(uu, join_u[k * WR + rw][jr]);
-      }
-      const float keep = u == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(u - uu);
+      for (int k = 0; k < NG; ++k) mm = fmaxf(mm, join_m[k * WR + rw][jr]);
+      if constexpr (C8)
+#pragma unroll
+        for (int k = 0; k < NG; ++k) {
+          const float mk = join_m[k * WR + rw][jr];
+          if (mk != -INFINITY) uu = fmaxf(uu, join_u[k * WR + rw][jr] + (mk - mm));
+        }
+      const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - mm) + (C8 ? u - uu : 0.f));
       if (g == 0 && jq == 0 && mine_too) {
         float ll = 0.f;
 #pragma unroll
@@ -658,7 +671,7 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
           if (mk != -INFINITY || join_l[k * WR + rw][jr] != 0.f)
             ll += join_l[k * WR + rw][jr] * __builtin_amdgcn_exp2f(mk - mm);
         }
-        a.part_ml[prow + rw * 16 + jr] = make_float4(mm, ll, C8 ? uu - 127.f - kRaise : uu, 0.f);
+        a.part_ml[prow + rw * 16 + jr] = make_float4(mm, ll, C8 ? uu - 127.f - kRaise : 0.f, 0.f);
       }
       float* ex = reinterpret_cast<float*>(smem);     // [wave][16 rows][ST]
 #pragma unroll

@@ -1,7 +1,7 @@
 // The ends of the absorbed decode (gfx950): queries folded into the latent space
 // before the attend kernels, their shares joined and taken to the heads' values after.
 //
-//   q~_r = W_keys,h^T q_r,   o_r = W_values,h a_r,   a_r = sum_s 2^(u_s - M) O_s / sum_s 2^(m_s - M) l_s
+//   q~_r = W_keys,h^T q_r,   o_r = W_values,h a_r,   a_r = sum_s 2^(m_s - M + u_s) O_s / sum_s 2^(m_s - M) l_s
 //
 // joint_fold    a wave a (head, 32 latent columns, 32 or 128 rows): the head's factor columns lie
 //               in LDS once, read by the transposing load, as the contraction runs over
@@ -395,7 +395,7 @@ __global__ __launch_bounds__(R / 4 * GR) void joint_merge(FinishArgs a, float* _
     return ml;
   };
   // the greatest m; a lane's first share waits in registers
-  float4 first = make_float4(-INFINITY, 0.f, -INFINITY, 0.f);
+  float4 first = make_float4(-INFINITY, 0.f, 0.f, 0.f);
   int64_t first_at = 0;
   float M = -INFINITY;
   for (int s = tid; s < ns; s += N) {
@@ -425,7 +425,7 @@ __global__ __launch_bounds__(R / 4 * GR) void joint_merge(FinishArgs a, float* _
       if (s0 + s != tid) ml = share(s0 + s, at);
       const bool some = ml.y != 0.f;                   // a share that saw nothing has l = 0 and m = -inf
       l += some ? ml.y * __builtin_amdgcn_exp2f(ml.x - M) : 0.f;
-      wo[s] = some ? __builtin_amdgcn_exp2f(ml.z - M) : 0.f;
+      wo[s] = some ? __builtin_amdgcn_exp2f((ml.x - M) + ml.z) : 0.f;
       where[s] = at;
     }
     __syncthreads();

@@ -1018,3 +1018,43 @@ def test_prompt_scores_past_fp32(cache, tokens, queries):
     q = (q.double() * 2.0 ** queries).to(BF16)
     want = oracle_prompt(j, pool, table, [0], q, wk, wv, [T], [T])
     check(host(joint_prefill(j, q, start, pool, table, seq, T, wk, wv)), want, np.abs(want).max())
+
+
+@pytest.mark.parametrize("H,d,r,p,cache,Q,n", [
+    (3, 64, 128, 32, "bf16", 1, 0), (16, 64, 128, 32, "e4m3", 1, 0), (40, 128, 256, 64, "e4m3", 2, 100),
+    (32, 128, 512, 64, "e4m3", 4, 0), (32, 128, 512, 64, "bf16", 4, 70)])
+@pytest.mark.parametrize("size", [20, 33, 60, 80])
+def test_scores_of_any_size(H, d, r, p, cache, Q, n, size):
+    """Scores of 2^size, far above their tokens' exponents: the greatest one's token alone
+    weighs, so that the result is its value."""
+    from paper_2607_24331_amd import joint_decode
+    g = gen(size)
+    j = joint_of(H, d, r, p, cache)
+    w = r + p
+    lens = [200, 1, 0, 77]
+    pool = filled(j, 18, g)
+    perm = torch.randperm(18, generator=g, device="cuda").to(torch.int32)
+    table, prefix = perm[:16].view(4, 4).contiguous(), perm[16:].contiguous()
+    if cache == "e4m3":                                # every latent under another power of two
+        pool[:, PAGE * w:PAGE * (w + 1)] = torch.randint(107, 137, (18, PAGE), generator=g, device="cuda").to(torch.uint8)
+    # a token's position key says which of some hundreds of steps its score has; those of one
+    # step (e4m3) weigh alike
+    at = torch.from_numpy(oj.place(r, p, cache, np.arange(PAGE)[:, None], r + np.arange(p)[None])).cuda()
+    order = torch.randperm(18 * PAGE, generator=g, device="cuda").view(18, PAGE)
+    if cache == "bf16":
+        step = (1 + order % 128 / 128.0).double() * 2.0 ** (order // 128)
+        pool[:, at] = (step[..., None].expand(18, PAGE, p) * 2.0 ** (size // 2)).to(BF16)
+    else:
+        pool[:, at] = (0x38 + order % 8)[..., None].expand(18, PAGE, p).to(torch.uint8)
+        pool[:, PAGE * (w + 1):] = (127 + size // 2 + order // 8 % 32).to(torch.uint8)
+    wk, wv = factors(j, g)
+    wk.zero_()
+    q = torch.ones(4, Q, H, d + p, device="cuda")
+    q[:, :, 1::2] = -1.0
+    q = (q.double() * 2.0 ** (size - size // 2)).to(BF16)
+    seq = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    got = host(joint_decode(j, q, pool, table, seq, 256, wk, wv, prefix if n else None, n))
+    want = oracle_decode(j, q, pool, table, lens, 256, wk, wv, prefix, n)
+    for b in range(4):
+        size_b = np.maximum(np.abs(want[b]).max(-1, keepdims=True), 1e-30)
+        check(got[b], want[b], size_b, b)
