@@ -81,7 +81,7 @@ struct JointPrompt {
   int64_t total_context;
   int64_t kv_tiles, q_tiles;    // 64-token tiles and row tiles, at most
   int32_t slot;                 // sequences, in whole lines of 128 bytes
-  size_t off_qtile, off_most, off_kvtile, off_flags, off_c, off_rope, off_k, off_v;
+  size_t off_qtile, off_most, off_kvtile, off_flags, off_tokens, off_range, off_apart, off_c, off_rope, off_k, off_v;
   size_t bytes;
 };
 

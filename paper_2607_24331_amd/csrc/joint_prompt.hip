@@ -19,10 +19,15 @@
 //                  were made in, and the running maximum is a lane's own.
 // Keys, values, queries and weights are f16 on the matrix unit, whose 11 bits keep each
 // rounding (2^-12) below that of the bf16 result; powers of two keep them in its range: one a
-// sequence for its keys (of all heads, with the position keys) and one for its values, from
-// bounds on their magnitude (greatest latent coordinate x r x greatest factor element: the
-// largest is below 2^15, and 28 binades below that are still normal numbers), one a query
-// row.  They meet in a row's score scale and in its result.
+// query row, one a sequence for its keys (of all heads, with the position keys) and one for
+// its values.  They are formed from bounds on the magnitude (greatest latent coordinate x r x
+// greatest factor element) of the tokens that all rows of the sequence see, so that a later
+// token's size does not reach an earlier row, and leave 2^6 above those; a token above that,
+// or below 2^-12 of it, has powers of its own.  So every token's bound is below 2^15 and
+// above 2^3, 17 binades and more above the least normal number.  They meet in a row's score
+// scale and in its result; where a row tile meets a token with powers of its own, its scores and
+// weights take the tokens' powers one by one (8,191 tokens whose first is 2^-10 of the others: 1.33 ms
+// a call for 0.75).
 // Bound by the products: 4 T r d + 2 pairs (2 d + p) a head, and in the attention by LDS,
 // which 32 rows a wave read as fast as the products of a tile go.  8,191 new tokens of 32 heads
 // (d = 128, p = 64, r = 512): keys and values 77 us, 892 TFLOP/s; attention 651 us at best, 693 in
@@ -31,6 +36,8 @@
 // bound by memory (14 us), the plan by latency (7).
 #include <algorithm>
 #include <cmath>
+#include <limits>
+#include <type_traits>
 
 #include "device.h"
 #include "joint.h"
@@ -67,8 +74,13 @@ struct PromptArgs {
   int32_t q_tiles, kv_tiles;              // at most
   int32_t* counts;                        // row tiles, token tiles; bf16 bits of the greatest finite |W_keys|,
                                           // |W_values|; whether W_values has elements that are not finite
-  int2* most;                             // [kSlots][slot] bf16 bits of a sequence's greatest |latent|, |key| coordinate
+  int2* most;                             // [kSlots][slot] bf16 bits of a sequence's greatest |latent|, |key| coordinate,
+                                          // of the tokens that all its rows see
   int32_t slot;                           // sequences a slot, whole lines of 128 bytes
+  uint32_t* token_most;                   // the same of every token, latents' in the low half
+  uint2* range;                           // greatest and least of those of 16 tokens, zeros aside
+  uint32_t* powers;                       // a token's keys' (low half) and values' power beyond its sequence's
+  int32_t* apart;                         // [batch] first tile of a sequence that has such powers
   RowTile* rows;
   int2* toks;                             // sequence, tile
   uint16_t* there;                        // a bit a token of a tile: it is there
@@ -78,15 +90,35 @@ struct PromptArgs {
 // The least e with |x| < 2^e, from the bits of a bf16 |x| (subnormals: -126).
 __device__ __forceinline__ int exponent_above(int bits) { return max(bits >> 7, 1) - 126; }
 
-// Powers of two: keys are 2^keys, values 2^values times what the f16 tiles hold.
+// Exponents above the magnitude of keys and of values, from the greatest coordinates (kNothing: zeros).
+constexpr int kNothing = -300;
+struct Above {
+  int keys, values;
+};
+__device__ __forceinline__ Above above_of(int most_c, int most_k, int w_keys, int w_values, int log2_r) {
+  const int c = most_c == 0 ? kNothing : exponent_above(most_c) + log2_r;
+  const int k = most_k == 0 ? kNothing : exponent_above(most_k);
+  return Above{max(c == kNothing || w_keys == 0 ? kNothing : c + exponent_above(w_keys), k),
+               c == kNothing || w_values == 0 ? kNothing : c + exponent_above(w_values)};
+}
+// Powers of two: keys are 2^keys, values 2^values times what the f16 tiles hold.  A sequence's
+// are set by the tokens that all its rows see and hold what is up to 2^kRoom above them; a token
+// that is more, or less than 2^-kSpan of that, has powers of its own.
+constexpr int kRoom = 6, kSpan = 12;
 struct Powers {
   int keys, values;
 };
-__device__ __forceinline__ Powers powers_of(int2 most, int w_keys, int w_values, int log2_r) {
-  const int c = most.x == 0 ? -300 : exponent_above(most.x) + log2_r, k = most.y == 0 ? -300 : exponent_above(most.y);
-  const int above = max(w_keys == 0 ? -300 : c + exponent_above(w_keys), k);
-  const int values = w_values == 0 ? -300 : c + exponent_above(w_values);
-  return Powers{min(max(above - 15, -120), 120), min(max(values - 15, -120), 120)};
+__device__ __forceinline__ int power_below(int above) { return min(max(above - 15, -120), 120); }
+__device__ __forceinline__ Powers sequence_powers(Above x) {
+  return Powers{power_below(x.keys + kRoom), power_below(x.values + kRoom)};
+}
+__device__ __forceinline__ int own_power(int above, int sequence, int power) {
+  const int up = above - (sequence + kRoom);
+  return above == kNothing || (up <= 0 && up > -kSpan) ? power : power_below(above);
+}
+// Whether tokens whose exponents lie between low and high may have powers of their own.
+__device__ __forceinline__ bool may_differ(int low, int high, int sequence) {
+  return high > sequence + kRoom || low <= sequence + kRoom - kSpan;
 }
 __device__ __forceinline__ float power(int e) { return __uint_as_float(uint32_t(127 + e) << 23); }   // |e| <= 126
 
@@ -98,11 +130,22 @@ __device__ __forceinline__ uint32_t most_pairs(uint32_t a, uint32_t b) {
 __device__ __forceinline__ bool not_finite(uint32_t w) {
   return (((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u) != 0;
 }
+__device__ __forceinline__ uint32_t least_pairs(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(ushort2_, a), __builtin_bit_cast(ushort2_, b)));
+}
 __device__ __forceinline__ int most_half(uint32_t m) { return int(max(m & 0xFFFFu, m >> 16)); }
 __device__ __forceinline__ int wave_most(int m) {
 #pragma unroll
   for (int step = 32; step > 0; step >>= 1) m = max(m, __shfl_xor(m, step));
   return m;
+}
+// Rows of a sequence, as they are packed.
+struct Rows {
+  int first, n;
+};
+__device__ __forceinline__ Rows rows_of(const PromptArgs& a, int b) {
+  const int lo = min(max(a.row_start[b], 0), a.n_rows);
+  return Rows{lo, min(max(a.row_start[b + 1], lo), a.n_rows) - lo};
 }
 // Maxima that many work-groups raise at once: the work-groups of an XCD (as they are dealt) have
 // a slot of their own.  One line for all had the 1,900 work-groups of 30,061 tokens wait for
@@ -161,6 +204,7 @@ __global__ __launch_bounds__(1024) void prompt_plan(PromptArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   for (int i = tid; i < int(kBins); i += N) bins[i] = 0;
   for (int i = tid; i < kSlots * a.slot; i += N) a.most[i] = make_int2(0, 0);
+  for (int i = tid; i < a.batch; i += N) a.apart[i] = INT32_MAX;
   if (tid < 3) a.counts[2 + tid] = 0;
   const int most = (a.max_context + kTok - 1) / kTok + 1;
   int all_toks = 0, all_rows = 0;         // of the round's sequences
@@ -175,8 +219,9 @@ __global__ __launch_bounds__(1024) void prompt_plan(PromptArgs a) {
         const int b = b0 + tid;
         int lo = 0, n = 0, T = 0;
         if (b < a.batch) {
-          lo = min(max(a.row_start[b], 0), a.n_rows);
-          n = min(max(a.row_start[b + 1], lo), a.n_rows) - lo;
+          const Rows rows = rows_of(a, b);
+          lo = rows.first;
+          n = rows.n;
           T = n > 0 ? min(max(a.seq_lens[b], 0), a.max_context) : 0;
         }
         const int64_t len_to = wave_scan(int64_t(T), lane);
@@ -266,7 +311,8 @@ constexpr int kFactorPieces = 4;          // 16-byte pieces a lane
 template <bool C8>
 __global__ __launch_bounds__(256) void prompt_gather(PromptArgs a, GatherArgs s) {
   __shared__ uint32_t odd;
-  __shared__ int most[2][4];
+  __shared__ int most[4];
+  __shared__ uint32_t piece_most[16 * 72], wave_high[4], wave_low[4], wave_common[4];
   if (int(blockIdx.x) >= 4 * a.kv_tiles) {             // the factors' greatest elements
     const int id = blockIdx.x - 4 * a.kv_tiles, which = id >= s.factor_groups, g = id - (which ? s.factor_groups : 0);
     const u32x4* W = reinterpret_cast<const u32x4*>(which ? s.W_values : s.W_keys);
@@ -288,22 +334,22 @@ __global__ __launch_bounds__(256) void prompt_gather(PromptArgs a, GatherArgs s)
         m = most_pairs(m, bad ? 0u : x[k][e] & 0x7FFF7FFFu);
       }
     if (which && __any(odd_factor) && (threadIdx.x & 63) == 0) atomicOr(&a.counts[4], 1);
-    most[0][threadIdx.x >> 6] = wave_most(most_half(m));
+    most[threadIdx.x >> 6] = wave_most(most_half(m));
     __syncthreads();
     if (threadIdx.x == 0)
-      atomicMax(&a.counts[2 + which], max(max(most[0][0], most[0][1]), max(most[0][2], most[0][3])));
+      atomicMax(&a.counts[2 + which], max(max(most[0], most[1]), max(most[2], most[3])));
     return;
   }
   const int tile = blockIdx.x >> 2, t0 = (blockIdx.x & 3) * 16, tid = threadIdx.x;
   if (tile >= a.counts[1]) return;
   const int2 at = a.toks[tile];
-  const int T = min(max(a.seq_lens[at.x], 0), a.max_context) - at.y * kTok;
+  const int len = min(max(a.seq_lens[at.x], 0), a.max_context), T = len - at.y * kTok;
+  const int common = max(len - rows_of(a, at.x).n, 0) - at.y * kTok;   // the last token of the tile that all rows see
   int page = s.page_table[int64_t(at.x) * s.max_pages + at.y];
   if (page >= s.num_pages) page = -1;
   const int have = page < 0 ? 0 : min(T, kTok) - t0;   // of the 16
   if (tid == 0) odd = 0;
   __syncthreads();
-  uint32_t most_c = 0, most_k = 0;
   const int w = s.r + s.p, per = C8 ? 16 : 8, pieces = w / per, g = joint_gcd16(pieces);
   const int rg = joint_gcd16(s.p / 8);
   const uint8_t* src = s.pool + int64_t(max(page, 0)) * s.page_bytes;
@@ -340,29 +386,53 @@ __global__ __launch_bounds__(256) void prompt_gather(PromptArgs a, GatherArgs s)
     if (bad || t - t0 >= have)
 #pragma unroll
       for (int e = 0; e < (C8 ? 2 : 1); ++e) x[e] = u32x4{0u, 0u, 0u, 0u};
+    uint32_t m = 0;
 #pragma unroll
     for (int e = 0; e < (C8 ? 2 : 1); ++e) {
       const int j = col + 8 * e;
-      const uint32_t m = most_pairs(most_pairs(x[e][0] & 0x7FFF7FFFu, x[e][1] & 0x7FFF7FFFu),
-                                    most_pairs(x[e][2] & 0x7FFF7FFFu, x[e][3] & 0x7FFF7FFFu));
-      if (j < s.r)
-        most_c = most_pairs(most_c, m);
-      else
-        most_k = most_pairs(most_k, m);
+#pragma unroll
+      for (int v = 0; v < 4; ++v) m = most_pairs(m, x[e][v] & 0x7FFF7FFFu);
       if (j < s.r)
         *reinterpret_cast<u32x4*>(s.c + (int64_t(tile) * kTok + t) * s.r + j) = x[e];
       else
         *reinterpret_cast<u32x4*>(s.rope + (int64_t(tile) * kTok + t) * s.p * 2 +
                                   (((j - s.r) / 8) ^ joint_swap(rg, t)) * 16) = x[e];
     }
+    piece_most[i] = col < s.r ? uint32_t(most_half(m)) : uint32_t(most_half(m)) << 16;
   }
-  most[0][tid >> 6] = wave_most(most_half(most_c));
-  most[1][tid >> 6] = wave_most(most_half(most_k));
+  __syncthreads();
+  // 16 lanes a token
+  const int tt = tid >> 4;
+  uint32_t m = 0;
+  for (int i = tid & 15; i < pieces; i += 16) m = most_pairs(m, piece_most[tt * pieces + i]);
+#pragma unroll
+  for (int step = 8; step > 0; step >>= 1) m = most_pairs(m, __shfl_xor(m, step));
+  if ((tid & 15) == 0) a.token_most[tile * kTok + t0 + tt] = m;
+  uint32_t low = m == 0 ? ~0u : m, all_see = t0 + tt <= common ? m : 0;
+#pragma unroll
+  for (int step = 32; step > 8; step >>= 1) {
+    m = most_pairs(m, __shfl_xor(m, step));
+    low = least_pairs(low, __shfl_xor(low, step));
+    all_see = most_pairs(all_see, __shfl_xor(all_see, step));
+  }
+  if ((tid & 63) == 0) {
+    wave_high[tid >> 6] = m;
+    wave_low[tid >> 6] = low;
+    wave_common[tid >> 6] = all_see;
+  }
   __syncthreads();
   if (tid == 0) {
-    int2* most_at = a.most + (blockIdx.x & (kSlots - 1)) * a.slot + at.x;
-    atomicMax(&most_at->x, max(max(most[0][0], most[0][1]), max(most[0][2], most[0][3])));
-    if (s.p > 0) atomicMax(&most_at->y, max(max(most[1][0], most[1][1]), max(most[1][2], most[1][3])));
+    for (int i = 1; i < 4; ++i) {
+      m = most_pairs(m, wave_high[i]);
+      low = least_pairs(low, wave_low[i]);
+      all_see = most_pairs(all_see, wave_common[i]);
+    }
+    a.range[tile * 4 + t0 / 16] = make_uint2(m, low);
+    if (all_see != 0) {
+      int2* most_at = a.most + (blockIdx.x & (kSlots - 1)) * a.slot + at.x;
+      atomicMax(&most_at->x, int(all_see & 0xFFFFu));
+      if (s.p > 0) atomicMax(&most_at->y, int(all_see >> 16));
+    }
     a.odd[tile * 4 + t0 / 16] = uint16_t(odd);
     a.there[tile * 4 + t0 / 16] = uint16_t(have >= 16 ? 0xFFFFu : have > 0 ? (1u << have) - 1u : 0u);
   }
@@ -453,25 +523,53 @@ __global__ __launch_bounds__(512) void prompt_expand(PromptArgs a, const bf16* _
       expand_stage(acc, buf + rows, buf + cols, lr, lq);
     }
   };
-  // powers of the block's tiles, in lanes 8 i .. 8 i + 7
+  // of the block's tiles, in lanes 8 i .. 8 i + 7
   constexpr int BT = TOK / kTok;
-  const int my_tile = blk * BT + ((lane >> 3) & (BT - 1));
-  const Powers pw = powers_of(most_of_slots(a, a.toks[min(my_tile, n_tiles - 1)].x, lane), a.counts[2], a.counts[3],
-                              31 - __builtin_clz(r));
+  const int my_tile = min(blk * BT + ((lane >> 3) & (BT - 1)), n_tiles - 1), log2_r = 31 - __builtin_clz(r);
+  const int w_keys = a.counts[2], w_values = a.counts[3];
+  const int2 tile_at = a.toks[my_tile];
+  const uint2 range = a.range[my_tile * 4 + (lane & 3)];
+  const int2 most = most_of_slots(a, tile_at.x, lane);
+  auto above_bits = [&](uint32_t m) { return above_of(m & 0xFFFFu, m >> 16, w_keys, w_values, log2_r); };
+  const Above above = above_of(most.x, most.y, w_keys, w_values, log2_r), high = above_bits(range.x), low = above_bits(range.y);
+  const Powers pw = sequence_powers(above);
+  const uint64_t differ = __ballot(range.x != 0 && (may_differ(low.keys, high.keys, above.keys) ||
+                                                    may_differ(low.values, high.values, above.values)));
   // of the block's position keys, which become f16 in place, a share for each of its work-groups
   const int per = kTok * p / 8, pieces = min(BT, n_tiles - blk * BT) * per;
   u32x4* rope_at = reinterpret_cast<u32x4*>(rope) + int64_t(blk) * BT * per;
   u32x4 first = {};
   if (f * 512 + tid < pieces) first = rope_at[f * 512 + tid];
+  // 2^-e of this wave's tokens: one a tile, or, where tokens differ, 64 i + lane's
   constexpr int WT = NT >= 4 ? NT / 4 : 1;
-  float down[WT];                                      // 2^-e of this wave's tiles
+  const int bt0 = wt * (16 * NT) / kTok, t0 = wt * (16 * NT) + (lane & (16 * NT - 1));
+  const bool apart = (differ >> (8 * bt0) & (WT == 2 ? 0xFFFFu : 0xFFu)) != 0;
+  float down[WT], down_all[WT];
 #pragma unroll
-  for (int i = 0; i < WT; ++i)
-    down[i] = power(-__shfl(value ? pw.values : pw.keys, 8 * (wt * (16 * NT) / kTok + i)));
+  for (int i = 0; i < WT; ++i) {
+    const int tile = blk * BT + bt0 + i;
+    auto of_tile = [&](int x) { return __builtin_amdgcn_readlane(x, 8 * (bt0 + i)); };
+    const Powers all{of_tile(pw.keys), of_tile(pw.values)};
+    Powers own = all;
+    if (apart && tile < n_tiles) {
+      const Above x = above_bits(a.token_most[int64_t(blk) * TOK + t0 + 64 * i]);
+      own = Powers{own_power(x.keys, of_tile(above.keys), all.keys), own_power(x.values, of_tile(above.values), all.values)};
+    }
+    down[i] = power(-(value ? own.values : own.keys));
+    down_all[i] = apart ? 1.f : down[i];
+    if (f == 0 && wf == 0 && tile < n_tiles) {
+      const int dk = own.keys - all.keys, dv = own.values - all.values;
+      a.powers[int64_t(blk) * TOK + t0 + 64 * i] = uint32_t(uint16_t(dk)) | uint32_t(uint16_t(dv)) << 16;
+      if (dk != 0 || dv != 0) atomicMin(&a.apart[of_tile(tile_at.x)], of_tile(tile_at.y));
+    }
+  }
   for (int i = f * 512 + tid; i < pieces; i += tiles * 512) {   // whole waves
     u32x4 y = first;
     if (i >= tiles * 512) y = rope_at[i];
-    const float by = power(-__shfl(pw.keys, 8 * (i / per)));
+    const int bt = i / per, all = __shfl(pw.keys, 8 * bt), all_above = __shfl(above.keys, 8 * bt);
+    const float by = power(-(differ >> (8 * bt) & 0xFFu
+                                 ? own_power(above_bits(a.token_most[int64_t(blk) * TOK + i / (p / 8)]).keys, all_above, all)
+                                 : all));
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       y[e] = pair_half(__uint_as_float(y[e] << 16) * by, __uint_as_float(y[e] & 0xFFFF0000u) * by);
@@ -492,16 +590,26 @@ __global__ __launch_bounds__(512) void prompt_expand(PromptArgs a, const bf16* _
     stages(acc, coord_row, tok_row);
     if (!live) return;
     const int s0 = D == 128 ? (wf & 1) * 2 : 0;        // the key's first 32 coordinates
+    if (apart)
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        const float by = __shfl(down[j / 4], 16 * (j & 3) + lr);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i][j] *= by;
+        __builtin_amdgcn_sched_barrier(0);             // few registers are left
+      }
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
       const int tok = tok0 + 16 * j + lr;
+      const float by = down_all[j / 4];
       uint8_t* out = keys + (tile0 + (tok >> 6)) * (kTok * D * 2) + (tok & 63) * (D * 2);
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-        const floatx4 lo = acc[2 * s][j] * down[j / 4], hi = acc[2 * s + 1][j] * down[j / 4];
+        const floatx4 lo = acc[2 * s][j] * by, hi = acc[2 * s + 1][j] * by;
         *reinterpret_cast<u32x4*>(out + ((4 * (s0 + s) + lq) ^ joint_swap(KG, tok & 63)) * 16) =
             u32x4{pair_half(lo[0], lo[1]), pair_half(lo[2], lo[3]), pair_half(hi[0], hi[1]),
                   pair_half(hi[2], hi[3])};
+        __builtin_amdgcn_sched_barrier(0);             // each store as soon as it can go
       }
     }
   } else {
@@ -512,27 +620,42 @@ __global__ __launch_bounds__(512) void prompt_expand(PromptArgs a, const bf16* _
       for (int j = 0; j < 4; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
     stages(acc, tok_row, coord_row);
     if (!live) return;
+    if (apart)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int col = (D == 128 ? (wf & 1) * 64 : 0) + 16 * j + lr;
-      // elements that are not finite make their coordinate NaN, which the clamp would drop
-      bool odd_row = false;
-      if (odd_factor) odd_row = row_is_odd(W_values + (int64_t(head) * D + col) * r, r);
+      for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          const float by = __shfl(down[i / 4], 16 * (i & 3) + 4 * lq + v);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) acc[i][j][v] *= by;
+          __builtin_amdgcn_sched_barrier(0);
+        }
+    auto column = [&](int j) { return (D == 128 ? (wf & 1) * 64 : 0) + 16 * j + lr; };
+    auto put = [&](int col, int s, u32x4 x) {
+      const int tok = tok0 + 32 * s;
+      *reinterpret_cast<u32x4*>(values + (tile0 + (tok >> 6)) * (kTok * D * 2) + col * (kTok * 2) +
+                                ((4 * (tok >> 5 & 1) + lq) ^ joint_swap(8, col)) * 16) = x;
+    };
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
 #pragma unroll
       for (int s = 0; s < NT / 2; ++s) {
-        const int tok = tok0 + 32 * s;
-        floatx4 lo = acc[2 * s][j] * down[s / 2], hi = acc[2 * s + 1][j] * down[s / 2];
+        floatx4 lo = acc[2 * s][j] * down_all[s / 2], hi = acc[2 * s + 1][j] * down_all[s / 2];
 #pragma unroll
         for (int v = 0; v < 4; ++v) {                  // a weight of 0 times an overflow would be none
-          lo[v] = odd_row ? __builtin_nanf("") : fminf(fmaxf(lo[v], -kMaxHalf), kMaxHalf);
-          hi[v] = odd_row ? __builtin_nanf("") : fminf(fmaxf(hi[v], -kMaxHalf), kMaxHalf);
+          lo[v] = fminf(fmaxf(lo[v], -kMaxHalf), kMaxHalf);
+          hi[v] = fminf(fmaxf(hi[v], -kMaxHalf), kMaxHalf);
         }
-        *reinterpret_cast<u32x4*>(values + (tile0 + (tok >> 6)) * (kTok * D * 2) + col * (kTok * 2) +
-                                  ((4 * (tok >> 5 & 1) + lq) ^ joint_swap(8, col)) * 16) =
-            u32x4{pair_half(lo[0], lo[1]), pair_half(lo[2], lo[3]), pair_half(hi[0], hi[1]),
-                  pair_half(hi[2], hi[3])};
+        put(column(j), s, u32x4{pair_half(lo[0], lo[1]), pair_half(lo[2], lo[3]), pair_half(hi[0], hi[1]),
+                                pair_half(hi[2], hi[3])});
+        __builtin_amdgcn_sched_barrier(0);             // each store as soon as it can go
       }
-    }
+    // elements that are not finite make their coordinate NaN, which the clamp has dropped
+    if (odd_factor)
+#pragma unroll 1
+      for (int j = 0; j < 4; ++j)
+        if (row_is_odd(W_values + (int64_t(head) * D + column(j)) * r, r))
+          for (int s = 0; s < NT / 2; ++s) put(column(j), s, u32x4{0x7E007E00u, 0x7E007E00u, 0x7E007E00u, 0x7E007E00u});
   }
 }
 
@@ -551,12 +674,20 @@ __device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c) {
                                                 0);
 }
 
+// x 2^e; beyond 2^100 the powers of two of 2^100 are counted instead, in its units, so that
+// scores past fp32's end keep their order, far apart.  What is not finite stays so.
+__device__ __forceinline__ float score_of(float x, int e) {
+  const float y = __builtin_amdgcn_ldexpf(x, e);
+  if (fabsf(y) <= 0x1p100f || !(fabsf(x) < INFINITY)) return y;
+  const float far = __builtin_amdgcn_logf(fabsf(x)) + float(e - 100);   // log2
+  return copysignf(fmaf(far, 0x1p100f, 0x1p100f), x);
+}
+
 template <int D, int P>
-__global__ __launch_bounds__(256, 2) void prompt_attend(PromptArgs a, const uint8_t* __restrict__ keys,
-                                                        const uint8_t* __restrict__ rope,
-                                                        const uint8_t* __restrict__ values,
-                                                        const bf16* __restrict__ q, int heads, int r, float scale,
-                                                        bf16* __restrict__ out) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2, D == 64 ? 3 : 2))) void
+prompt_attend(PromptArgs a, const uint8_t* __restrict__ keys, const uint8_t* __restrict__ rope,
+              const uint8_t* __restrict__ values, const bf16* __restrict__ q, int heads, int r, float scale,
+              bf16* __restrict__ out) {
   constexpr int KB = kTok * D * 2, PB = kTok * P * 2, TILE = 2 * KB + PB;
   constexpr int KL = KB / 1024, PL = PB / 1024;        // 1 KB loads
   constexpr int KG = joint_gcd16(D / 8), PG = P > 0 ? joint_gcd16(P / 8) : 1;
@@ -631,107 +762,198 @@ __global__ __launch_bounds__(256, 2) void prompt_attend(PromptArgs a, const uint
   for (int i = 0; i < DS; ++i) to_half(qd[i]);
 #pragma unroll
   for (int i = 0; i < PS; ++i) to_half(qp[i]);
-  const Powers pw = powers_of(most_of_slots(a, rt.b, lane), a.counts[2], a.counts[3], 31 - __builtin_clz(r));
-  // from products to scores in powers of two.  Products lie below 2^38 and, being sums of
-  // products of f16, 2^-48 or more apart, so past the ends all weigh alike, or one alone
-  // weighs; 2^38 x 2^80 is still a number
-  const float fs = fminf(fmaxf(ldexpf(scale, pw.keys - up), 0x1p-100f), 0x1p80f);
+  const int2 most_seen = most_of_slots(a, rt.b, lane);
+  const Powers pw = sequence_powers(above_of(most_seen.x, most_seen.y, a.counts[2], a.counts[3], 31 - __builtin_clz(r)));
 
   f32x16 acc[CT];
 #pragma unroll
   for (int i = 0; i < CT; ++i)
 #pragma unroll
     for (int v = 0; v < 16; ++v) acc[i][v] = 0.f;
-  float m = -INFINITY, l = 0.f;
+  // Where a token has powers of its own, scores take its keys' and their scale first, and
+  // the weights in the sums its values', held against a maximum of score + power, which is
+  // kept as its distance u from the scores' own, m.
+  float m = -INFINITY, u = -INFINITY, l = 0.f;
+  const bool apart = a.apart[rt.b] < tiles;
+  const float scale_part = __builtin_amdgcn_frexp_mantf(scale);
+  const int scale_up = __builtin_amdgcn_frexp_expf(scale) + pw.keys - up;
+  // from products to scores in powers of two.  Products lie below 2^38 and, being sums of
+  // products of f16, 2^-48 or more apart, so past the ends all weigh alike, or one alone
+  // weighs; 2^38 x 2^80 is still a number
+  const float fs = fminf(fmaxf(ldexpf(scale_part, scale_up), 0x1p-100f), 0x1p80f);
   const float slack = kSlack / fs;
   const int ksw = joint_swap(KG, lr), psw = P > 0 ? joint_swap(PG, lr) : 0, vsw = joint_swap(8, lr);
 
-  for (int t = 0; t < tiles; ++t) {
-    loads_done();
-    __syncthreads();                                   // the tile is whole, the one before is used up
-    const uint2 th2 = there, od2 = odd;
-    if (t + 1 < tiles) {
-      marks(t + 1);
-      issue(t + 1);
-    }
-    unsigned char* buf = smem + (t & 1) * TILE;
-    const int pos = t * kTok;
-    // rows of the wave that do not see the whole tile, or a tile with holes
-    const bool edge = pos + kTok > rt.first + w * 32 + 1 || (th2.x & th2.y) != ~0u || (od2.x | od2.y) != 0;
+  auto walk = [&](auto own_powers) {
+    constexpr bool OWN = decltype(own_powers)::value;
+    for (int t = 0; t < tiles; ++t) {
+      loads_done();
+      __syncthreads();                                 // the tile is whole, the one before is used up
+      const uint2 th2 = there, od2 = odd;
+      if (t + 1 < tiles) {
+        marks(t + 1);
+        issue(t + 1);
+      }
+      unsigned char* buf = smem + (t & 1) * TILE;
+      const int pos = t * kTok;
+      // rows of the wave that do not see the whole tile, or a tile with holes
+      const bool edge = pos + kTok > rt.first + w * 32 + 1 || (th2.x & th2.y) != ~0u || (od2.x | od2.y) != 0;
 
-    // ---- scores: tokens pos + 32 n + 8 b + 4 h + v (register 4 b + v), row lr
-    f32x16 s[2];
+      // ---- scores: tokens pos + 32 n + 8 b + 4 h + v (register 4 b + v), row lr
+      f32x16 s[2];
 #pragma unroll
-    for (int n = 0; n < 2; ++n) {
+      for (int n = 0; n < 2; ++n) {
 #pragma unroll
-      for (int v = 0; v < 16; ++v) s[n][v] = 0.f;
+        for (int v = 0; v < 16; ++v) s[n][v] = 0.f;
 #pragma unroll
-      for (int i = 0; i < DS; ++i)
-        s[n] = mfma(*reinterpret_cast<const u32x4*>(buf + (32 * n + lr) * (D * 2) + ((2 * i + h) ^ ksw) * 16), qd[i], s[n]);
+        for (int i = 0; i < DS; ++i)
+          s[n] = mfma(*reinterpret_cast<const u32x4*>(buf + (32 * n + lr) * (D * 2) + ((2 * i + h) ^ ksw) * 16), qd[i], s[n]);
 #pragma unroll
-      for (int i = 0; i < PS; ++i)
-        s[n] = mfma(*reinterpret_cast<const u32x4*>(buf + KB + (32 * n + lr) * (P * 2) + ((2 * i + h) ^ psw) * 16), qp[i], s[n]);
-    }
-    reads_ahead<2 * (DS + PS), 4>();
-    __builtin_amdgcn_sched_barrier(0);
-    // ---- softmax, scores and maxima before their scale
-    if (edge) {
+        for (int i = 0; i < PS; ++i)
+          s[n] = mfma(*reinterpret_cast<const u32x4*>(buf + KB + (32 * n + lr) * (P * 2) + ((2 * i + h) ^ psw) * 16), qp[i], s[n]);
+      }
+      reads_ahead<2 * (DS + PS), 4>();
+      __builtin_amdgcn_sched_barrier(0);
+      // ---- softmax, scores and maxima before their scale
+      const u32x4* by = reinterpret_cast<const u32x4*>(a.powers + int64_t(rt.kv + t) * kTok);
+      if constexpr (OWN) {
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+          for (int b = 0; b < 4; ++b) {
+            const u32x4 d = by[8 * n + 2 * b + h];
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+              const int e = int16_t(d[v] & 0xFFFFu) + scale_up;
+              s[n][4 * b + v] = score_of(s[n][4 * b + v] * scale_part, e);
+            }
+          }
+      }
+      if (edge) {
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+          const int seen = limit - pos - 32 * n;       // bits of tokens that the row sees, and of NaN
+          const uint32_t there_seen = (n ? th2.y : th2.x) & (seen >= 32 ? ~0u : seen <= 0 ? 0u : (1u << seen) - 1u);
+          const uint32_t th = there_seen >> (4 * h), od = (n ? od2.y : od2.x) >> (4 * h);
+#pragma unroll
+          for (int v = 0; v < 16; ++v) {
+            const int b = 8 * (v >> 2) + (v & 3);
+            const uint32_t keep = __builtin_amdgcn_sbfe(int(th), b, 1), nan = __builtin_amdgcn_sbfe(int(od), b, 1);
+            s[n][v] = __uint_as_float(((__float_as_uint(s[n][v]) | nan) & keep) | (0xFF800000u & ~keep));
+          }
+        }
+      }
+      float top = -INFINITY;
 #pragma unroll
       for (int n = 0; n < 2; ++n)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          const int b = 8 * (v >> 2) + 4 * h + (v & 3);
-          const uint32_t th = n ? th2.y : th2.x, od = n ? od2.y : od2.x;
-          s[n][v] = pos + 32 * n + b < limit && ((th >> b) & 1) ? ((od >> b) & 1 ? __builtin_nanf("") : s[n][v]) : -INFINITY;
+        for (int v = 0; v < 16; ++v) top = fmaxf(top, s[n][v]);
+      auto of_both = [](float x) {                     // the other half's, by a move between registers
+        const uint32_t w = __float_as_uint(x);
+        const auto both = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+        return fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
+      };
+      top = of_both(top);
+      u32x4 p[4];
+      if constexpr (OWN) {
+        asm volatile("" ::: "memory");                 // read again: the powers would not fit the registers
+        bool raise = __any(top > m + kSlack);
+        const float m_new = raise ? fmaxf(m, top) : m, mb = m_new == -INFINITY ? 0.f : m_new;
+        const float u_old = m == -INFINITY ? -INFINITY : raise ? u + (m - m_new) : u;
+        float utop = -INFINITY;
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+          for (int b = 0; b < 4; ++b) {
+            const u32x4 d = by[8 * n + 2 * b + h];
+#pragma unroll
+            for (int v = 0; v < 4; ++v) utop = fmaxf(utop, (s[n][4 * b + v] - mb) + float(int32_t(d[v]) >> 16));
+          }
+        utop = of_both(utop);
+        raise |= __any(utop > u_old + kSlack) != 0;
+        if (raise) {
+          l *= m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m_new);
+          u = fmaxf(u_old, utop);
+          const float keep = u_old == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(u_old - u);
+          if (t > 0) {
+#pragma unroll
+            for (int i = 0; i < CT; ++i)
+#pragma unroll
+              for (int v = 0; v < 16; ++v) acc[i][v] *= keep;
+          }
+          m = m_new;
         }
-    }
-    float top = -INFINITY;
+        asm volatile("" ::: "memory");
+        const float ub = u == -INFINITY ? 0.f : u - kRaise;
 #pragma unroll
-    for (int n = 0; n < 2; ++n)
+        for (int k = 0; k < 4; ++k)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) top = fmaxf(top, s[n][v]);
-    const uint32_t u = __float_as_uint(top);           // the other half's, by a move between registers
-    const auto both = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-    top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
-    if (__any(top > m + slack)) {
-      const float m_new = fmaxf(m, top);
-      const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - m_new) * fs);
-      l *= keep;
-      if (t > 0) {
+          for (int g = 0; g < 2; ++g) {                // four tokens of step k
+            const int n = k >> 1, b = (k & 1) + 2 * g;
+            const u32x4 d = by[8 * n + 2 * b + h];
+            float y[4];
 #pragma unroll
-        for (int i = 0; i < CT; ++i)
+            for (int v = 0; v < 4; ++v) {
+              const float x = s[n][4 * b + v] - mb;
+              l += __builtin_amdgcn_exp2f(x);
+              y[v] = __builtin_amdgcn_exp2f(x + (float(int32_t(d[v]) >> 16) - ub));
+            }
+            p[k][2 * g] = pair_half(y[0], y[1]);
+            p[k][2 * g + 1] = pair_half(y[2], y[3]);
+          }
+      } else {
+        if (__any(top > m + slack)) {
+          const float m_new = fmaxf(m, top);
+          const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - m_new) * fs);
+          l *= keep;
+          if (t > 0) {
 #pragma unroll
-          for (int v = 0; v < 16; ++v) acc[i][v] *= keep;
+            for (int i = 0; i < CT; ++i)
+#pragma unroll
+              for (int v = 0; v < 16; ++v) acc[i][v] *= keep;
+          }
+          m = m_new;
+        }
+        const float mb = m == -INFINITY ? 0.f : m * fs - kRaise;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)                    // step k: tokens 32 n + 8 b + 4 h and 16 further, b = k % 2
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int n = k >> 1, v = 4 * (k & 1) + 8 * (e >> 1) + 2 * (e & 1);
+            const float x = __builtin_amdgcn_exp2f(fmaf(s[n][v], fs, -mb));
+            const float y = __builtin_amdgcn_exp2f(fmaf(s[n][v + 1], fs, -mb));
+            l += x;
+            l += y;
+            p[k][e] = pair_half(x, y);
+          }
       }
-      m = m_new;
+      // ---- output: coordinate 32 i + lr of the A operand, piece 2 k + h of its tokens
+      const unsigned char* vb = buf + KB + PB + lr * (kTok * 2);
+#pragma unroll
+      for (int i = 0; i < CT; ++i)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          acc[i] = mfma(*reinterpret_cast<const u32x4*>(vb + i * (32 * kTok * 2) + ((2 * k + h) ^ vsw) * 16), p[k], acc[i]);
+      reads_ahead<4 * CT, 4>();
+      __builtin_amdgcn_sched_barrier(0);
     }
-    const float mb = m == -INFINITY ? 0.f : m * fs - kRaise;
-    u32x4 p[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k)                        // step k: tokens 32 n + 8 b + 4 h and 16 further, b = k % 2
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int n = k >> 1, v = 4 * (k & 1) + 8 * (e >> 1) + 2 * (e & 1);
-        const float x = __builtin_amdgcn_exp2f(fmaf(s[n][v], fs, -mb));
-        const float y = __builtin_amdgcn_exp2f(fmaf(s[n][v + 1], fs, -mb));
-        l += x;
-        l += y;
-        p[k][e] = pair_half(x, y);
-      }
-    // ---- output: coordinate 32 i + lr of the A operand, piece 2 k + h of its tokens
-    const unsigned char* vb = buf + KB + PB + lr * (kTok * 2);
-#pragma unroll
-    for (int i = 0; i < CT; ++i)
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        acc[i] = mfma(*reinterpret_cast<const u32x4*>(vb + i * (32 * kTok * 2) + ((2 * k + h) ^ vsw) * 16), p[k], acc[i]);
-    reads_ahead<4 * CT, 4>();
-    __builtin_amdgcn_sched_barrier(0);
-  }
+  };
+  if (apart)
+    walk(std::true_type{});
+  else
+    walk(std::false_type{});
   l += __shfl_xor(l, 32);
   if (my >= rt.n) return;
   bf16* dst = out + (row * heads + head) * D + 4 * h;
-  const float inv = rt.kv < 0 ? __builtin_nanf("") : l == 0.f ? 0.f : ldexpf(1.f / l, pw.values);
+  float inv = rt.kv < 0 ? __builtin_nanf("") : l == 0.f ? 0.f : ldexpf(1.f / l, pw.values);
+  if (apart && l != 0.f) {                             // in two steps, each of which is a number
+    const float half = __builtin_amdgcn_exp2f(0.5f * (u - kRaise + float(pw.values)));
+    inv = half / l;
+#pragma unroll
+    for (int i = 0; i < CT; ++i)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[i][v] *= half;
+  }
 #pragma unroll
   for (int i = 0; i < CT; ++i)
 #pragma unroll
@@ -763,7 +985,10 @@ JointPrompt joint_prompt(const dckv_joint_desc& d, int32_t batch, int32_t n_rows
   s.slot = (batch + 15) / 16 * 16;
   s.off_kvtile = s.off_most + align_up(size_t(kSlots) * s.slot * sizeof(int2));
   s.off_flags = s.off_kvtile + align_up(kv * sizeof(int2));
-  s.off_c = s.off_flags + 2 * align_up(kv * sizeof(uint2));
+  s.off_tokens = s.off_flags + 2 * align_up(kv * sizeof(uint2));
+  s.off_range = s.off_tokens + 2 * align_up(kv * kTok * 4);
+  s.off_apart = s.off_range + align_up(kv * kTok / 16 * sizeof(uint2));
+  s.off_c = s.off_apart + align_up(size_t(batch) * 4);
   s.off_rope = s.off_c + align_up(kv * kTok * d.rank * 2);
   s.off_k = s.off_rope + align_up(kv * kTok * d.rope_dim * 2);
   const size_t heads = kv * kTok * d.head_dim * 2 * d.num_heads;
@@ -793,7 +1018,11 @@ hipError_t launch_joint_prefill(const JointPrompt& s, const void* q, const int32
   a.most = reinterpret_cast<int2*>(ws + s.off_most);
   a.slot = s.slot;
   a.there = reinterpret_cast<uint16_t*>(ws + s.off_flags);
-  a.odd = reinterpret_cast<uint16_t*>(ws + s.off_flags + (s.off_c - s.off_flags) / 2);
+  a.odd = reinterpret_cast<uint16_t*>(ws + s.off_flags + (s.off_tokens - s.off_flags) / 2);
+  a.token_most = reinterpret_cast<uint32_t*>(ws + s.off_tokens);
+  a.powers = reinterpret_cast<uint32_t*>(ws + s.off_tokens + (s.off_range - s.off_tokens) / 2);
+  a.range = reinterpret_cast<uint2*>(ws + s.off_range);
+  a.apart = reinterpret_cast<int32_t*>(ws + s.off_apart);
   hipLaunchKernelGGL(prompt_plan, dim3(1), dim3(1024), 0, stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
@@ -837,7 +1066,8 @@ hipError_t launch_joint_prefill(const JointPrompt& s, const void* q, const int32
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  const float scale = kLog2e * (d.scale != 0.f ? d.scale : 1.f / std::sqrt(float(d.head_dim + d.rope_dim)));
+  const float scale = std::min(kLog2e * (d.scale != 0.f ? d.scale : 1.f / std::sqrt(float(d.head_dim + d.rope_dim))),
+                               std::numeric_limits<float>::max());
 #define DCKV_GO(D, P)                                                                                        \
   hipLaunchKernelGGL((prompt_attend<D, P>), dim3(uint32_t(s.q_tiles) * d.num_heads), dim3(256), 0, stream, a, \
                      keys, rope, values, static_cast<const bf16*>(q), d.num_heads, d.rank, scale,                     \

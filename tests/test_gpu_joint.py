@@ -1058,3 +1058,72 @@ def test_scores_of_any_size(H, d, r, p, cache, Q, n, size):
     for b in range(4):
         size_b = np.maximum(np.abs(want[b]).max(-1, keepdims=True), 1e-30)
         check(got[b], want[b], size_b, b)
+
+
+def resize(j, pool, slots, power, part):
+    """Make the latents ("c") or position keys ("k") of the slots 2^power as large."""
+    r, w = j.rank, j.rank + j.rope_dim
+    lo, hi = (0, r) if part == "c" else (r, w)
+    for sl, e in zip(slots, power):
+        page, s = divmod(int(sl), PAGE)
+        if j.cache == "bf16":
+            at = torch.from_numpy(oj.place(r, j.rope_dim, j.cache, s, np.arange(lo, hi))).cuda()
+            pool[page, at] = (pool[page, at].double() * 2.0 ** int(e)).to(BF16)
+        else:
+            pool[page, PAGE * (w + (part == "k")) + s] += int(e)
+
+
+@pytest.mark.parametrize("H,d,r,p,cache,T", [
+    (3, 64, 128, 32, "bf16", 200), (2, 128, 512, 64, "e4m3", 200), (4, 64, 256, 64, "e4m3", 130),
+    (34, 128, 128, 32, "bf16", 2100)])                 # blocks of 256 tokens
+@pytest.mark.parametrize("what", ["later values", "a value that weighs little", "later keys", "a small first token",
+                                  "every size", "smaller from the middle on"])
+def test_tokens_of_other_sizes(H, d, r, p, cache, T, what):
+    """Each row is as exact as its own tokens allow, whatever others of its sequence hold, seen
+    later, or weighed little.  Factors of keys are 0 where latents are resized, so that
+    the scores stay of unit size (or, with resized keys, one token's alone counts)."""
+    from paper_2607_24331_amd import joint_decode, joint_prefill
+    rng = np.random.default_rng(T + r)
+    j = joint_of(H, d, r, p, cache)
+    added = [min(T, 150), 40]
+    pool, table, start, q, wk, wv, seq, rs, lens, top = prompt_case(j, [T - added[0], 30], added, 0, 5)
+    slot = [int(table[0, t // PAGE]) * PAGE + t % PAGE for t in range(T)]
+    mid = T - 70
+    wk.zero_()
+    if what == "later values":
+        resize(j, pool, slot[mid:], [60, 20] * 35, "c")
+    elif what == "a value that weighs little":         # 2^-70 of others' weight, 2^40 of their size
+        q[:, :, d] = 8.0
+        for t in (5, mid):
+            page, s = divmod(slot[t], PAGE)
+            at = int(oj.place(r, p, cache, s, r))
+            if cache == "bf16":
+                pool[page, at] = -50.0 * math.sqrt(d + p) / 8
+            else:
+                pool[page, at] = 0xFE                  # -448 under 2^0 or so: 2^-9 and more of it times q
+                pool[page, PAGE * (r + p + 1) + s] = 127 - 2
+        resize(j, pool, [slot[5], slot[mid]], [40, 40], "c")
+    elif what == "later keys":
+        resize(j, pool, slot[mid::30], [50, 55, 60], "k")
+    elif what == "a small first token":
+        resize(j, pool, slot[:1], [-60], "c")
+        resize(j, pool, slot[:1], [-60], "k")
+    elif what == "every size":
+        resize(j, pool, slot, rng.integers(-40, 41, T), "c")
+    else:
+        resize(j, pool, slot[mid:], [-50] * 70, "c")
+        resize(j, pool, slot[mid:], [-50] * 70, "k")
+    ask = [(0, t) for t in (*range(0, min(8, added[0])), *range(added[0] - 75, added[0], 3), added[0] - 1)] + [(1, 0), (1, 39)]
+    got = host(joint_prefill(j, q, rs, pool, table, seq, top, wk, wv, total_context=sum(lens)))
+    qs = torch.stack([q[added[0] - 40:added[0]], q[added[0]:]])
+    dec = host(joint_decode(j, qs, pool, table, seq, top, wk, wv))
+    hp, hk, hv, scale = host(pool), host(wk), host(wv), 1 / math.sqrt(d + p)
+    toks = [oj.tokens(hp, table[b].cpu().numpy(), lens[b], r, p, cache) for b in range(2)]
+    for b, i in ask:
+        row = int(start[b]) + i
+        seen = lens[b] - added[b] + i + 1
+        want = oj.attend(host(q[row:row + 1]), *toks[b], hk, hv, [seen], scale)[0]
+        size = np.abs(want).max(-1, keepdims=True)     # of the row's own heads
+        check(got[row], want, size, ("prompt", b, i))
+        if i >= added[b] - 40:
+            check(dec[b, i - added[b] + 40], want, size, ("decode", b, i))
