@@ -12,7 +12,8 @@ import torch
 
 from . import capi
 from .dckv import _check, _lib
-from .serve import _CODE, _INT32_MAX, Rotary, _context, _count, _gpu, _launch, _new, _vector, _width
+from .serve import (_CODE, _INT32_MAX, Rotary, _context, _count, _gpu, _launch, _new, _tangent, _vector,
+                    _width)
 
 _CACHES = {"bf16": (capi.DCKV_JOINT_BF16, torch.bfloat16), "e4m3": (capi.DCKV_JOINT_E4M3, torch.uint8)}
 
@@ -100,6 +101,8 @@ def _no_graph(what: str, *tensors) -> None:
     if torch.is_grad_enabled() and any(getattr(t, "requires_grad", False) for t in tensors):
         raise ValueError(f"{what} is outside autograd: its tensors must not require gradients here "
                          "(call it under torch.no_grad())")
+    if _tangent(*tensors):
+        raise ValueError(f"{what} is outside autograd: its tensors must not carry tangents here")
 
 
 def _rows(t: torch.Tensor, name: str, width: int, index: Optional[int] = None):

@@ -9,6 +9,7 @@ import functools
 from typing import NamedTuple, Optional
 
 import torch
+from torch.autograd import forward_ad
 
 from . import capi
 from .dckv import _check, _lib, dense_page_elems
@@ -34,6 +35,14 @@ def _gpu(t: torch.Tensor, name: str, dtype, index: Optional[int] = None, contigu
     if index is not None and on != index:
         raise ValueError(f"{name} is on device {on}, the call's other tensors on {index}")
     raise ValueError(f"{name} must be contiguous")
+
+
+def _tangent(*tensors) -> bool:
+    """Whether one carries a tangent of forward-mode differentiation, which torch.no_grad()
+    does not suspend."""
+    if getattr(forward_ad, "_current_level", 0) < 0:          # outside dual_level(): 3 us spared
+        return False
+    return any(isinstance(t, torch.Tensor) and forward_ad.unpack_dual(t).tangent is not None for t in tensors)
 
 
 def _count(value, name: str):

@@ -218,3 +218,33 @@ def test_binding_refusals():
         joint_decode(j, q.requires_grad_(), pool, i32.view(2, 1), i32, 64, q, q)
     with pytest.raises(ValueError, match="autograd"):
         joint_prefill(j, q, i32, pool, i32.view(2, 1), i32, 64, q, q)
+
+
+def test_tangents_are_refused():
+    """Forward-mode differentiation: a result without its tangent would be taken for a constant."""
+    import torch.autograd.forward_ad as forward
+    from paper_2607_24331_amd import Joint, joint_append, joint_decode, joint_prefill
+    j = Joint(1, 64, 128, 32)
+    c, k, w = torch.zeros(4, 128), torch.zeros(4, 32), torch.zeros(1, 64, 128, dtype=torch.bfloat16)
+    slot, i32 = torch.zeros(4, dtype=torch.int64), torch.zeros(2, dtype=torch.int32)
+    pool, q = torch.zeros(2, j.page_elems, dtype=torch.bfloat16), torch.zeros(2, 1, 96, dtype=torch.bfloat16)
+    out = torch.zeros(2, 1, 64, dtype=torch.bfloat16)
+
+    def append(c, k):
+        joint_append(j, c, k, slot, pool)
+
+    def decode(q, wk, wv, out):
+        joint_decode(j, q, pool, i32.view(2, 1), i32, 64, wk, wv, out=out)
+
+    def prefill(q, wk, wv, out):
+        joint_prefill(j, q, i32, pool, i32.view(2, 1), i32, 64, wk, wv, out=out)
+
+    for call, given in ((append, (c, k)), (decode, (q, w, w, out)), (prefill, (q, w, w, out))):
+        for i in range(len(given)):
+            with forward.dual_level():
+                dual = [*given]
+                dual[i] = forward.make_dual(given[i], torch.ones_like(given[i]))
+                with torch.no_grad(), pytest.raises(ValueError, match="tangents"):
+                    call(*dual)
+                with pytest.raises(ValueError, match="on the GPU"):    # no tangent: the next check
+                    call(*given)
