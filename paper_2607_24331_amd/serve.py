@@ -277,6 +277,9 @@ def rotary(rotation: Rotary, x: torch.Tensor, position: torch.Tensor, out: Optio
     if torch.is_grad_enabled() and (getattr(x, "requires_grad", False) or getattr(out, "requires_grad", False)):
         raise ValueError("rotary is outside autograd: x and out must not require gradients here (call it under "
                          "torch.no_grad() or from a torch.autograd.Function; inverse=True gives the gradient of x)")
+    if _tangent(x, out):
+        raise ValueError("rotary is outside autograd: x and out must not carry tangents here (call it from a "
+                         "torch.autograd.Function, whose jvp turns the tangent as forward turns x)")
     px, xc, xt, xh = _heads(x, "x")
     n, H, d = x.shape
     if d != rotation.head_dim:

@@ -144,6 +144,30 @@ def test_rotary_refuses_to_drop_a_gradient():
         rotary(r, leaf, pos)
 
 
+def test_rotary_refuses_to_drop_a_tangent():
+    import torch.autograd.forward_ad as forward
+    from paper_2607_24331_amd import Rotary, rotary
+    r, pos, plain = Rotary(64), torch.zeros(1, dtype=torch.int32), torch.zeros(1, 1, 64)
+    with forward.dual_level():
+        dual = forward.make_dual(plain, torch.ones(1, 1, 64))
+        for kw in (dict(x=dual), dict(x=2 * dual), dict(x=plain, out=dual)):
+            with torch.no_grad(), pytest.raises(ValueError, match="tangents"):
+                rotary(r, position=pos, **kw)
+
+        class Turn(torch.autograd.Function):
+            @staticmethod
+            def forward(ctx, x):
+                with pytest.raises(ValueError, match="GPU"):    # no tangent inside a function: the next check
+                    rotary(r, x, pos)
+                return x.clone()
+
+            @staticmethod
+            def jvp(ctx, t):
+                return t.clone()
+
+        assert forward.unpack_dual(Turn.apply(dual)).tangent.any()
+
+
 def test_decode_rotary_refuses_a_weight_beyond_fp32(lib):
     # a score weighs the square of the magnitude; a batch of 0 launches nothing
     from paper_2607_24331_amd import Plan, Rotary
