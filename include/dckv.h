@@ -620,7 +620,8 @@ int dckv_joint_read(const dckv_joint_desc* desc, const void* pool, int64_t num_p
  *   prefix     prefix_len > 0: every sequence goes on from the same prefix_len tokens
  *              (slots 0, 1, ... of prefix_pages, int32 [ceil(prefix_len/64)]), which
  *              are read once for all; page_table, seq_lens and max_context then count a
- *              sequence's own tokens, whose positions start at prefix_len.  0: NULL
+ *              sequence's own tokens, whose positions start at prefix_len.  0: NULL, else
+ *              the call is refused
  *   out        device bf16 [batch, Q, H, d]
  * Roundings (relative; sums are fp32): e4m3 caches, folded queries and softmax weights
  * 2^-12 (f16, under powers of two that follow the magnitudes; parts 2^-29 of a query

@@ -187,6 +187,7 @@ int dckv_joint_decode(const dckv_joint_desc* desc, int32_t queries, const void* 
   if (st != DCKV_OK || batch == 0) return st;
   if (!q || !pool || !page_table || !seq_lens || !W_keys || !W_values || !out || (prefix_len > 0 && !prefix_pages))
     return fail(DCKV_EINVAL, "%s: null device pointer", where);
+  if (prefix_len == 0 && prefix_pages) return fail(DCKV_EINVAL, "%s: prefix_pages given for a prefix_len of 0", where);
   st = check_pages(where, num_pages);
   if (st == DCKV_OK) st = check_table(where, max_pages, max_context);
   if (st != DCKV_OK) return st;

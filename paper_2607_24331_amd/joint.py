@@ -206,6 +206,8 @@ def joint_decode(joint: Joint, q: torch.Tensor, pool: torch.Tensor, page_table: 
         pre = _gpu(prefix_pages, "prefix_pages", torch.int32, dev)
         if prefix_pages.dim() != 1 or prefix_pages.shape[0] * capi.PAGE_TOKENS < n:
             raise ValueError(f"prefix_pages must be a vector of at least {-(-n // capi.PAGE_TOKENS)} pages")
+    elif prefix_pages is not None and prefix_pages.numel():
+        raise ValueError("prefix_pages given for a prefix_len of 0")
     shape = (*q.shape[:-1], d)
     if out is None:
         out = _new(shape, bf16, q.device, stream)

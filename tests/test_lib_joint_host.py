@@ -248,3 +248,26 @@ def test_tangents_are_refused():
                     call(*dual)
                 with pytest.raises(ValueError, match="on the GPU"):    # no tangent: the next check
                     call(*given)
+
+
+@fake
+def test_a_prefix_without_its_length_is_refused(lib):
+    a = dict(DECODE, prefix=A)
+    assert lib.dckv_joint_decode(ref(), *a.values(), None) == E
+    assert "prefix_len of 0" in lib.dckv_last_error().decode()
+
+
+def test_the_binding_refuses_a_prefix_without_its_length(monkeypatch):
+    """On the CPU with the checks of devices taken out: the call ends before the library's."""
+    from paper_2607_24331_amd import Joint, joint
+    monkeypatch.setattr(joint, "_gpu", lambda t, *a: t.data_ptr())
+    monkeypatch.setattr(joint, "_vector", lambda t, *a: t.data_ptr())
+    monkeypatch.setattr(joint, "_new", lambda *a: (_ for _ in ()).throw(RuntimeError("all checks passed")))
+    j = Joint(1, 64, 128, 32)
+    bf16, i32 = torch.bfloat16, torch.zeros(2, dtype=torch.int32)
+    q, w = torch.zeros(2, 1, 96, dtype=bf16), torch.zeros(1, 64, 128, dtype=bf16)
+    pool = torch.zeros(2, j.page_elems, dtype=bf16)
+    for pages, n, what in ((i32, 0, "prefix_len of 0"), (None, 5, "prefix_pages is needed"), (i32, 129, "at least 3 pages"),
+                           (i32, -1, "outside"), (i32[:0], 0, "all checks"), (None, 0, "all checks"), (i32, 128, "all checks")):
+        with pytest.raises((ValueError, RuntimeError), match=what):
+            joint.joint_decode(j, q, pool, i32.view(2, 1), i32, 64, w, w, prefix_pages=pages, prefix_len=n)
