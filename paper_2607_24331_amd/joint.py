@@ -126,7 +126,7 @@ def joint_append(joint: Joint, c: torch.Tensor, k: Optional[torch.Tensor], slot:
     """Write latents c [tokens, rank] and position keys k [tokens, rope_dim] (None
     where rope_dim is 0), turned by their positions where `rotation` is given, into
     their slots; a slot of -1 skips its token.  Rows may be strided."""
-    _no_graph("joint_append", c, k)
+    _no_graph("joint_append", c, k, pool)
     pc, code, cs = _rows(c, "c", joint.rank)
     n, dev = _count(c.shape[0], "tokens"), c.get_device()
     pk, ks = None, 0
@@ -152,6 +152,7 @@ def joint_read(joint: Joint, pool: torch.Tensor, slot: torch.Tensor, dtype=torch
     """Cached latents [tokens, rank] and keys [tokens, rope_dim] (None where that is
     0) of the given slots (zeros for a slot outside the pool), exactly, as bfloat16 or
     float32."""
+    _no_graph("joint_read", pool)
     if not isinstance(slot, torch.Tensor) or slot.dim() != 1:
         raise ValueError("slot must be a vector")
     n = _count(slot.shape[0], "the length of slot")
@@ -179,7 +180,7 @@ def joint_decode(joint: Joint, q: torch.Tensor, pool: torch.Tensor, page_table: 
     position seq_len - Q + i and sees every position up to its own.  With `prefix_len`
     every sequence goes on from the tokens in slots 0 .. prefix_len - 1 of
     `prefix_pages`; its own tokens (page_table, seq_lens, max_context) follow them."""
-    _no_graph("joint_decode", q, W_keys, W_values, out)
+    _no_graph("joint_decode", q, pool, W_keys, W_values, out)
     bf16 = torch.bfloat16
     pq = _gpu(q, "q", bf16)
     if q.dim() == 4:
@@ -233,7 +234,7 @@ def joint_prefill(joint: Joint, q: torch.Tensor, row_start: torch.Tensor, pool: 
     tensor.  `total_context` bounds the sum of the sequences' lengths (batch *
     max_context by default) and with it the workspace: a sequence that does not fit it
     gets NaN."""
-    _no_graph("joint_prefill", q, W_keys, W_values, out)
+    _no_graph("joint_prefill", q, pool, W_keys, W_values, out)
     bf16 = torch.bfloat16
     pq = _gpu(q, "q", bf16)
     if q.dim() != 3:

@@ -271,3 +271,18 @@ def test_the_binding_refuses_a_prefix_without_its_length(monkeypatch):
                            (i32, -1, "outside"), (i32[:0], 0, "all checks"), (None, 0, "all checks"), (i32, 128, "all checks")):
         with pytest.raises((ValueError, RuntimeError), match=what):
             joint.joint_decode(j, q, pool, i32.view(2, 1), i32, 64, w, w, prefix_pages=pages, prefix_len=n)
+
+
+def test_pools_that_record_gradients_are_refused():
+    from paper_2607_24331_amd import Joint, joint_append, joint_decode, joint_prefill, joint_read
+    j = Joint(1, 64, 128, 32)
+    bf16, i32, slot = torch.bfloat16, torch.zeros(2, dtype=torch.int32), torch.zeros(4, dtype=torch.int64)
+    q, w = torch.zeros(2, 1, 96, dtype=bf16), torch.zeros(1, 64, 128, dtype=bf16)
+    pool = torch.zeros(2, j.page_elems, dtype=bf16, requires_grad=True)
+    for call in (lambda: joint_append(j, torch.zeros(4, 128), torch.zeros(4, 32), slot, pool),
+                 lambda: joint_read(j, pool, slot), lambda: joint_decode(j, q, pool, i32.view(2, 1), i32, 64, w, w),
+                 lambda: joint_prefill(j, q, i32, pool, i32.view(2, 1), i32, 64, w, w)):
+        with pytest.raises(ValueError, match="autograd"):
+            call()
+        with torch.no_grad(), pytest.raises(ValueError, match="on the GPU"):
+            call()
