@@ -19,14 +19,14 @@
 //                  were made in, and the running maximum is a lane's own.
 // Keys, values, queries and weights are f16 on the matrix unit, whose 11 bits keep each
 // rounding (2^-12) below that of the bf16 result; powers of two keep them in its range: one a
-// query row, one a sequence for its keys (of all heads, with the position keys) and one for
-// its values.  They are formed from bounds on the magnitude (greatest latent coordinate x r x
-// greatest factor element) of the tokens that all rows of the sequence see, so that a later
-// token's size does not reach an earlier row, and leave 2^6 above those; a token above that,
-// or below 2^-12 of it, has powers of its own.  So every token's bound is below 2^15 and
-// above 2^3, 17 binades and more above the least normal number.  They meet in a row's score
-// scale and in its result; where a row tile meets a token with powers of its own, its scores and
-// weights take the tokens' powers one by one (8,191 tokens whose first is 2^-10 of the others: 1.33 ms
+// query row, one a sequence for its keys without position (of all heads), one for its position
+// keys and one for its values.  They are formed from bounds on the magnitude (greatest latent
+// coordinate x r x greatest factor element) of the tokens that all rows of the sequence see,
+// so that a later token's size does not reach an earlier row, and leave 2^6 above those; a
+// token above that, or below 2^-12 of it, shifts its own.  So every token's bound is below
+// 2^15 and above 2^3, 17 binades and more above the least normal number.  They meet in a row's
+// queries, score scale and result; where a row tile meets a token that shifts its own, its scores
+// and weights take the shifts one by one (8,191 tokens whose first is 2^-10 of the others: 1.33 ms
 // a call for 0.75).
 // Bound by the products: 4 T r d + 2 pairs (2 d + p) a head, and in the attention by LDS,
 // which 32 rows a wave read as fast as the products of a tile go.  8,191 new tokens of 32 heads
@@ -90,35 +90,49 @@ struct PromptArgs {
 // The least e with |x| < 2^e, from the bits of a bf16 |x| (subnormals: -126).
 __device__ __forceinline__ int exponent_above(int bits) { return max(bits >> 7, 1) - 126; }
 
-// Exponents above the magnitude of keys and of values, from the greatest coordinates (kNothing: zeros).
-constexpr int kNothing = -300;
+// Exponents above the magnitude of a token's keys without position, of its position key and of
+// its values, from the greatest coordinates (kNothing: zeros).
+constexpr int kNothing = -10000;
 struct Above {
-  int keys, values;
+  int keys, rope, values;
 };
 __device__ __forceinline__ Above above_of(int most_c, int most_k, int w_keys, int w_values, int log2_r) {
   const int c = most_c == 0 ? kNothing : exponent_above(most_c) + log2_r;
-  const int k = most_k == 0 ? kNothing : exponent_above(most_k);
-  return Above{max(c == kNothing || w_keys == 0 ? kNothing : c + exponent_above(w_keys), k),
+  return Above{c == kNothing || w_keys == 0 ? kNothing : c + exponent_above(w_keys),
+               most_k == 0 ? kNothing : exponent_above(most_k),
                c == kNothing || w_values == 0 ? kNothing : c + exponent_above(w_values)};
 }
-// Powers of two: keys are 2^keys, values 2^values times what the f16 tiles hold.  A sequence's
-// are set by the tokens that all its rows see and hold what is up to 2^kRoom above them; a token
-// that is more, or less than 2^-kSpan of that, has powers of its own.
+// Powers of two: keys are 2^keys, position keys 2^rope, values 2^values times what the f16 tiles
+// hold.  A sequence's are set by the tokens that all its rows see and hold what is up to 2^kRoom
+// above them; a token that is more, or less than 2^-kSpan of that, shifts its own (both parts of
+// its key alike: a row's products are summed over them, its query balanced between them).
 constexpr int kRoom = 6, kSpan = 12;
 struct Powers {
-  int keys, values;
+  int keys, rope, values;
 };
 __device__ __forceinline__ int power_below(int above) { return min(max(above - 15, -120), 120); }
 __device__ __forceinline__ Powers sequence_powers(Above x) {
-  return Powers{power_below(x.keys + kRoom), power_below(x.values + kRoom)};
+  return Powers{power_below((x.keys == kNothing ? x.rope : x.keys) + kRoom),
+                power_below((x.rope == kNothing ? x.keys : x.rope) + kRoom), power_below(x.values + kRoom)};
 }
-__device__ __forceinline__ int own_power(int above, int sequence, int power) {
-  const int up = above - (sequence + kRoom);
-  return above == kNothing || (up <= 0 && up > -kSpan) ? power : power_below(above);
+// By how much a token passes what a sequence's powers hold.
+struct Beyond {
+  int keys, values;
+};
+__device__ __forceinline__ Beyond beyond(Above x, Powers all) {
+  return Beyond{max(x.keys == kNothing ? kNothing : x.keys - 15 - all.keys,
+                    x.rope == kNothing ? kNothing : x.rope - 15 - all.rope),
+                x.values == kNothing ? kNothing : x.values - 15 - all.values};
 }
-// Whether tokens whose exponents lie between low and high may have powers of their own.
-__device__ __forceinline__ bool may_differ(int low, int high, int sequence) {
-  return high > sequence + kRoom || low <= sequence + kRoom - kSpan;
+__device__ __forceinline__ bool apart_by(int up) { return up != kNothing && (up > 0 || up <= -kSpan); }
+struct Shifts {
+  int keys, values;
+};
+__device__ __forceinline__ Shifts own_shifts(Above x, Powers all) {
+  const Beyond up = beyond(x, all);
+  const int low = min(all.keys, all.rope), high = max(all.keys, all.rope);
+  return Shifts{apart_by(up.keys) ? min(max(up.keys, -120 - low), 120 - high) : 0,
+                apart_by(up.values) ? min(max(up.values, -120 - all.values), 120 - all.values) : 0};
 }
 __device__ __forceinline__ float power(int e) { return __uint_as_float(uint32_t(127 + e) << 23); }   // |e| <= 126
 
@@ -531,10 +545,11 @@ __global__ __launch_bounds__(512) void prompt_expand(PromptArgs a, const bf16* _
   const uint2 range = a.range[my_tile * 4 + (lane & 3)];
   const int2 most = most_of_slots(a, tile_at.x, lane);
   auto above_bits = [&](uint32_t m) { return above_of(m & 0xFFFFu, m >> 16, w_keys, w_values, log2_r); };
-  const Above above = above_of(most.x, most.y, w_keys, w_values, log2_r), high = above_bits(range.x), low = above_bits(range.y);
-  const Powers pw = sequence_powers(above);
-  const uint64_t differ = __ballot(range.x != 0 && (may_differ(low.keys, high.keys, above.keys) ||
-                                                    may_differ(low.values, high.values, above.values)));
+  const Powers pw = sequence_powers(above_of(most.x, most.y, w_keys, w_values, log2_r));
+  // no token passes the greatest of them, nor falls below the least
+  const Beyond high = beyond(above_bits(range.x), pw), low = beyond(above_bits(range.y), pw);
+  const uint64_t differ = __ballot(range.x != 0 && (high.keys > 0 || low.keys <= -kSpan || high.values > 0 ||
+                                                    low.values <= -kSpan));
   // of the block's position keys, which become f16 in place, a share for each of its work-groups
   const int per = kTok * p / 8, pieces = min(BT, n_tiles - blk * BT) * per;
   u32x4* rope_at = reinterpret_cast<u32x4*>(rope) + int64_t(blk) * BT * per;
@@ -549,27 +564,24 @@ __global__ __launch_bounds__(512) void prompt_expand(PromptArgs a, const bf16* _
   for (int i = 0; i < WT; ++i) {
     const int tile = blk * BT + bt0 + i;
     auto of_tile = [&](int x) { return __builtin_amdgcn_readlane(x, 8 * (bt0 + i)); };
-    const Powers all{of_tile(pw.keys), of_tile(pw.values)};
-    Powers own = all;
-    if (apart && tile < n_tiles) {
-      const Above x = above_bits(a.token_most[int64_t(blk) * TOK + t0 + 64 * i]);
-      own = Powers{own_power(x.keys, of_tile(above.keys), all.keys), own_power(x.values, of_tile(above.values), all.values)};
-    }
-    down[i] = power(-(value ? own.values : own.keys));
+    const Powers all{of_tile(pw.keys), of_tile(pw.rope), of_tile(pw.values)};
+    Shifts own{0, 0};
+    if (apart && tile < n_tiles) own = own_shifts(above_bits(a.token_most[int64_t(blk) * TOK + t0 + 64 * i]), all);
+    down[i] = power(-(value ? all.values + own.values : all.keys + own.keys));
     down_all[i] = apart ? 1.f : down[i];
     if (f == 0 && wf == 0 && tile < n_tiles) {
-      const int dk = own.keys - all.keys, dv = own.values - all.values;
-      a.powers[int64_t(blk) * TOK + t0 + 64 * i] = uint32_t(uint16_t(dk)) | uint32_t(uint16_t(dv)) << 16;
-      if (dk != 0 || dv != 0) atomicMin(&a.apart[of_tile(tile_at.x)], of_tile(tile_at.y));
+      a.powers[int64_t(blk) * TOK + t0 + 64 * i] = uint32_t(uint16_t(own.keys)) | uint32_t(uint16_t(own.values)) << 16;
+      if (own.keys != 0 || own.values != 0) atomicMin(&a.apart[of_tile(tile_at.x)], of_tile(tile_at.y));
     }
   }
   for (int i = f * 512 + tid; i < pieces; i += tiles * 512) {   // whole waves
     u32x4 y = first;
     if (i >= tiles * 512) y = rope_at[i];
-    const int bt = i / per, all = __shfl(pw.keys, 8 * bt), all_above = __shfl(above.keys, 8 * bt);
-    const float by = power(-(differ >> (8 * bt) & 0xFFu
-                                 ? own_power(above_bits(a.token_most[int64_t(blk) * TOK + i / (p / 8)]).keys, all_above, all)
-                                 : all));
+    const int bt = i / per;
+    const Powers all{__shfl(pw.keys, 8 * bt), __shfl(pw.rope, 8 * bt), 0};
+    int e = all.rope;
+    if (differ >> (8 * bt) & 0xFFu) e += own_shifts(above_bits(a.token_most[int64_t(blk) * TOK + i / (p / 8)]), all).keys;
+    const float by = power(-e);
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       y[e] = pair_half(__uint_as_float(y[e] << 16) * by, __uint_as_float(y[e] & 0xFFFF0000u) * by);
@@ -741,29 +753,35 @@ prompt_attend(PromptArgs a, const uint8_t* __restrict__ keys, const uint8_t* __r
 #pragma unroll
   for (int i = 0; i < PS; ++i) qp[i] = *reinterpret_cast<const u32x4*>(qrow + D + 16 * i + 8 * h);
 
-  // in f16, times a power of two that brings the row's greatest below 2^15
-  uint32_t most = 0;
+  // in f16, times a power of two that brings the row's greatest below 2^15, the position part
+  // times what its keys' power is beyond the others'
+  const int2 most_seen = most_of_slots(a, rt.b, lane);
+  const Powers pw = sequence_powers(above_of(most_seen.x, most_seen.y, a.counts[2], a.counts[3], 31 - __builtin_clz(r)));
+  uint32_t most_d = 0, most_p = 0;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
 #pragma unroll
-    for (int i = 0; i < DS; ++i) most = most_pairs(most, qd[i][e] & 0x7FFF7FFFu);
+    for (int i = 0; i < DS; ++i) most_d = most_pairs(most_d, qd[i][e] & 0x7FFF7FFFu);
 #pragma unroll
-    for (int i = 0; i < PS; ++i) most = most_pairs(most, qp[i][e] & 0x7FFF7FFFu);
+    for (int i = 0; i < PS; ++i) most_p = most_pairs(most_p, qp[i][e] & 0x7FFF7FFFu);
   }
-  const auto halves = __builtin_amdgcn_permlane32_swap(most, most, false, false);
-  most = most_pairs(halves[0], halves[1]);             // a row that is not finite becomes NaN whatever its power is
-  const int up = min(max(15 - exponent_above(most_half(most)), -120), 120);
-  auto to_half = [&](u32x4& x) {
+  auto exponent_of_both = [](uint32_t most) {          // a row that is not finite becomes NaN whatever its power is
+    const auto halves = __builtin_amdgcn_permlane32_swap(most, most, false, false);
+    const int m = most_half(most_pairs(halves[0], halves[1]));
+    return m == 0 ? kNothing : exponent_above(m);
+  };
+  const int top_d = exponent_of_both(most_d), top_p = P > 0 ? exponent_of_both(most_p) : kNothing;
+  const int up = 15 - max(max(top_d, top_p + (pw.rope - pw.keys)), -1000);
+  auto to_half = [](u32x4& x, int e) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      x[e] = pair_half(__uint_as_float(x[e] << 16) * power(up), __uint_as_float(x[e] & 0xFFFF0000u) * power(up));
+    for (int i = 0; i < 4; ++i)
+      x[i] = pair_half(__builtin_amdgcn_ldexpf(__uint_as_float(x[i] << 16), e),
+                       __builtin_amdgcn_ldexpf(__uint_as_float(x[i] & 0xFFFF0000u), e));
   };
 #pragma unroll
-  for (int i = 0; i < DS; ++i) to_half(qd[i]);
+  for (int i = 0; i < DS; ++i) to_half(qd[i], up);
 #pragma unroll
-  for (int i = 0; i < PS; ++i) to_half(qp[i]);
-  const int2 most_seen = most_of_slots(a, rt.b, lane);
-  const Powers pw = sequence_powers(above_of(most_seen.x, most_seen.y, a.counts[2], a.counts[3], 31 - __builtin_clz(r)));
+  for (int i = 0; i < PS; ++i) to_half(qp[i], up + pw.rope - pw.keys);
 
   f32x16 acc[CT];
 #pragma unroll

@@ -1127,3 +1127,73 @@ def test_tokens_of_other_sizes(H, d, r, p, cache, T, what):
         check(got[row], want, size, ("prompt", b, i))
         if i >= added[b] - 40:
             check(dec[b, i - added[b] + 40], want, size, ("decode", b, i))
+
+
+# ------------------------------------------- forms that only large calls take
+def plain_prompt(j, q, pool, table, lens, start, wk, wv):
+    """The prompts in 64 bits on the GPU (matrix products by batches, right operands contiguous)."""
+    d, scale = j.head_dim, 1 / math.sqrt(j.head_dim + j.rope_dim)
+    r, p, w = j.rank, j.rope_dim, j.rank + j.rope_dim
+    at = torch.from_numpy(oj.place(r, p, j.cache, np.arange(PAGE)[:, None], np.arange(w)[None])).cuda()
+    out = torch.zeros(*q.shape[:2], d, dtype=torch.float64, device="cuda")
+    for b, T in enumerate(lens):
+        lo, hi = int(start[b]), int(start[b + 1])
+        if hi <= lo:
+            continue
+        x = pool[table[b, :max(1, -(-T // PAGE))].long()]
+        v = x[:, at.view(-1)]
+        if j.cache == "bf16":
+            v = v.double().view(-1, w)[:T]
+        else:
+            e = torch.exp2(x[:, PAGE * w:].double() - 127).view(-1, 2, PAGE)
+            v = v.view(torch.float8_e4m3fn).double().view(-1, PAGE, w)
+            v = torch.cat([v[..., :r] * e[:, 0, :, None], v[..., r:] * e[:, 1, :, None]], -1).view(-1, w)[:T]
+        keys = torch.matmul(v[:, :r], wk.double().transpose(1, 2).contiguous())              # [H, T, d]
+        values = torch.matmul(v[:, :r], wv.double().transpose(1, 2).contiguous())
+        x = q[lo:hi].double().transpose(0, 1).contiguous()                                   # [H, rows, d + p]
+        s = torch.matmul(x[..., :d].contiguous(), keys.transpose(1, 2).contiguous())
+        s = (s + torch.matmul(x[..., d:].contiguous(), v[:, r:].t().contiguous())) * scale
+        seen = torch.arange(T - (hi - lo), T, device="cuda")[:, None] >= torch.arange(T, device="cuda")
+        a = torch.softmax(s.masked_fill(~seen, -math.inf), -1)
+        out[lo:hi] = torch.matmul(a, values).transpose(0, 1)
+    return out
+
+
+def check_rows(got, want, what=""):
+    """check() with each row of each head against its own largest value."""
+    err, size = (got.double() - want).abs(), want.abs().amax(-1, keepdim=True).clamp(min=1e-300)
+    bad = ~(err <= 2.0 ** -6 * size + 2.0 ** -8 * want.abs())
+    assert not bad.any(), (what, bad.nonzero()[:5].tolist(), (err / size).max().item())
+
+
+@pytest.mark.parametrize("H,d", [(63, 64), (34, 128)])
+@pytest.mark.parametrize("r,p,cache", [(128, 0, "bf16"), (128, 32, "e4m3"), (256, 64, "bf16"), (512, 64, "e4m3"),
+                                       (512, 32, "bf16")])
+def test_prompts_in_blocks_of_256_tokens(H, d, r, p, cache):
+    """Blocks of the keys' and values' products that hold the ends of several sequences, these of sizes
+    2^-30 to 2^30 (values; their position keys of unit size where there are some, and
+    the factors of the keys as small as the latents are large), the last block partial."""
+    from paper_2607_24331_amd import joint_prefill
+    j = joint_of(H, d, r, p, cache)
+    cached, added = [660, 0, 50, 601, 3, 64, 180], [40, 70, 14, 23, 1, 64, 300]
+    power = [0, 30, -30, 12, -7, 5, -20]
+    pool, table, start, q, wk, wv, seq, rs, lens, top = prompt_case(j, cached, added, 5, H + r)
+    tiles = sum(-(-T // PAGE) for T in lens)
+    assert (tiles + 3) // 4 * (H if d == 128 else (H + 1) // 2) >= 256 and tiles % 4
+    w = r + p
+    at = torch.from_numpy(oj.place(r, p, cache, np.arange(PAGE)[:, None], np.arange(r)[None])).cuda().view(-1)
+    for b, e in enumerate(power):
+        pages = table[b].long()
+        if cache == "bf16":
+            pool[pages[:, None], at] = (pool[pages[:, None], at].double() * 2.0 ** e).to(BF16)
+        else:
+            pool[pages, PAGE * w:PAGE * (w + 1)] = (pool[pages, PAGE * w:PAGE * (w + 1)].int() + e).to(torch.uint8)
+        lo, hi = int(start[b]), int(start[b + 1])      # scores of unit size
+        q[lo:hi, :, :d] = (q[lo:hi, :, :d].double() * 2.0 ** -e).to(BF16)
+    out = torch.full((*q.shape[:2], d), 7.0, dtype=BF16, device="cuda")
+    ws = torch.full((j.prefill_workspace_bytes(len(lens), q.shape[0], top, sum(lens)),), 255, dtype=torch.uint8, device="cuda")
+    joint_prefill(j, q, rs, pool, table, seq, top, wk, wv, total_context=sum(lens), out=out, workspace=ws)
+    n = sum(added)
+    check_rows(out[:n], plain_prompt(j, q, pool, table, lens, start, wk, wv)[:n])
+    assert torch.all(out[n:] == 7.0)
+    assert torch.equal(out[:n], joint_prefill(j, q, rs, pool, table, seq, top, wk, wv, total_context=sum(lens), workspace=ws)[:n])
