@@ -1130,6 +1130,90 @@ def test_tokens_of_other_sizes(H, d, r, p, cache, T, what):
 
 
 # ------------------------------------------- forms that only large calls take
+def cut_of(j, ws, B, Q):
+    """(tiles a unit, whether units are of one sequence) as the call that used the workspace
+    decided: behind the queries (and their powers) B + 1 first tiles, then these."""
+    up = lambda v: (v + 255) // 256 * 256  # noqa: E731
+    rows, c8 = B * Q * j.num_heads, j.cache == "e4m3"
+    at = up(rows * (j.rank + j.rope_dim) * (2 if c8 else 4)) + (up(rows * 4) if c8 else 0)
+    starts = ws[at:at + 8 * (B + 3)].view(torch.int64).tolist()
+    return starts[B + 1], bool(starts[B + 2])
+
+
+@pytest.mark.parametrize("H,d,r,p,cache,B,high,Q,n", [
+    (64, 64, 128, 0, "bf16", 70, 6000, 8, 0), (64, 64, 256, 32, "e4m3", 70, 1200, 8, 0),
+    (32, 128, 512, 64, "bf16", 130, 6000, 4, 0), (32, 128, 512, 64, "e4m3", 200, 5500, 1, 0),
+    (16, 64, 128, 32, "bf16", 2500, 900, 1, 0), (8, 64, 128, 0, "bf16", 5000, 400, 1, 0),
+    (64, 64, 256, 64, "e4m3", 66, 900, 20, 100), (64, 64, 512, 0, "bf16", 65, 1500, 40, 0)])
+def test_units_that_walk_over_sequences(H, d, r, p, cache, B, high, Q, n):
+    """More than 40 tiles a unit and too many sequences to cut them one by one: equal shares of
+    all their tiles, a third of the sequences empty and runs of a hundred of them."""
+    from paper_2607_24331_amd import joint_decode
+    g = gen(B + Q)
+    j = joint_of(H, d, r, p, cache)
+    rng = np.random.default_rng(B)
+    lens = rng.integers(0, high + 1, B) * (rng.random(B) > 0.33)
+    lens[B // 3] = high
+    lens[0] = lens[-1] = 0
+    if B > 400:
+        lens[150:280] = 0
+    width, shared = -(-high // PAGE), -(-n // PAGE)
+    pages = 400
+    pool = filled(j, pages, g)                         # sequences share pages: they only read
+    table = torch.randint(0, pages, (B, width), generator=g, device="cuda", dtype=torch.int32)
+    prefix = torch.randint(0, pages, (shared,), generator=g, device="cuda", dtype=torch.int32) if n else None
+    q = randn(g, B, Q, H, d + p).to(BF16)
+    wk, wv = factors(j, g)
+    seq = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    ws = torch.full((j.workspace_bytes(Q, B, high, n),), 255, dtype=torch.uint8, device="cuda")     # NaN all over
+    out = joint_decode(j, q, pool, table, seq, high, wk, wv, prefix, n, workspace=ws)
+    per, whole = cut_of(j, ws, B, Q)
+    assert not whole and per > 40 and per * PAGE // 2 < lens.sum()
+    want = plain(j, q, pool, table, lens.tolist(), wk, wv, prefix, n)
+    err, size = (out.double() - want).abs(), want.abs().max().item()
+    assert (err <= 2.0 ** -6 * size + 2.0 ** -8 * want.abs()).all(), (err.max().item(), size)      # as check()
+    assert (err.square().mean().sqrt() <= 2.0 ** -8 * want.square().mean().sqrt()).item()
+    assert not out[torch.from_numpy(lens == 0).cuda()].any() or n
+    assert torch.equal(out, joint_decode(j, q, pool, table, seq, high, wk, wv, prefix, n, workspace=ws))
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("r", [128, 256, 512])
+@pytest.mark.parametrize("p", [0, 32, 64])
+@pytest.mark.parametrize("H,Q,n", [(33, 32, 70), (64, 33, 0)])
+def test_rows_by_the_thousand(cache, r, p, H, Q, n):
+    """1,056 rows of a sequence and 2,112 over the prefix, and 2,112 of a sequence: four and
+    eight waves that share a tile, with NaN behind the sequences and in a token that
+    only later queries see."""
+    from paper_2607_24331_amd import joint_decode
+    g = gen(r + p + H)
+    d = 64
+    j = joint_of(H, d, r, p, cache)
+    lens, width = [97, 40], 2
+    B, shared = 2, -(-n // PAGE)
+    pool = filled(j, B * width + shared, g)
+    table = torch.arange(B * width, dtype=torch.int32, device="cuda").view(B, width)
+    prefix = torch.arange(B * width, B * width + shared, dtype=torch.int32, device="cuda") if n else None
+    q = randn(g, B, Q, H, d + p).to(BF16)
+    wk, wv = factors(j, g)
+    seq = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    ws = torch.full((j.workspace_bytes(Q, B, 128, n),), 255, dtype=torch.uint8, device="cuda")
+    want = plain(j, q, pool, table, lens, wk, wv, prefix, n)
+    behind = [b * width * PAGE + t for b, T in enumerate(lens) for t in range(T, width * PAGE)]
+    behind += [B * width * PAGE + t for t in range(n, shared * PAGE)]
+    poison(j, pool, behind, "all")
+    clean = joint_decode(j, q, pool, table, seq, 128, wk, wv, prefix, n, workspace=ws)
+    err, size = (clean.double() - want).abs(), want.abs().max().item()
+    assert (err <= 2.0 ** -6 * size + 2.0 ** -8 * want.abs()).all(), (err.max().item(), size)      # as check()
+    assert (err.square().mean().sqrt() <= 2.0 ** -8 * want.square().mean().sqrt()).item()
+    first = 17
+    for part in ("c", "k") if p else ("c",):
+        bad = pool.clone()
+        poison(j, bad, [b * width * PAGE + T - Q + first for b, T in enumerate(lens)], math.nan if cache == "bf16" else 0x7F, part)
+        got = joint_decode(j, q, bad, table, seq, 128, wk, wv, prefix, n, workspace=ws)
+        assert torch.equal(got[:, :first], clean[:, :first]) and torch.isnan(got[:, first:]).all()
+
+
 def plain_prompt(j, q, pool, table, lens, start, wk, wv):
     """The prompts in 64 bits on the GPU (matrix products by batches, right operands contiguous)."""
     d, scale = j.head_dim, 1 / math.sqrt(j.head_dim + j.rope_dim)
@@ -1197,3 +1281,33 @@ def test_prompts_in_blocks_of_256_tokens(H, d, r, p, cache):
     check_rows(out[:n], plain_prompt(j, q, pool, table, lens, start, wk, wv)[:n])
     assert torch.all(out[n:] == 7.0)
     assert torch.equal(out[:n], joint_prefill(j, q, rs, pool, table, seq, top, wk, wv, total_context=sum(lens), workspace=ws)[:n])
+
+
+@pytest.mark.parametrize("B", [64, 65, 1023, 1024, 1025, 2500])
+@pytest.mark.parametrize("H,d,r,p,cache", [(3, 64, 128, 32, "bf16"), (2, 128, 256, 0, "e4m3")])
+def test_prompts_of_many_sequences(B, H, d, r, p, cache):
+    """The plan's walks over batches of more than a wave and more than a work-group, a third of the
+    sequences without rows, some without tokens; and one whose length spans several tiles."""
+    from paper_2607_24331_amd import joint_prefill
+    g = gen(B)
+    j = joint_of(H, d, r, p, cache)
+    rng = np.random.default_rng(B)
+    added = rng.integers(0, 9, B) * (rng.random(B) > 0.33)
+    lens = added + rng.integers(0, 90, B) * (rng.random(B) > 0.5)
+    added[B // 2], lens[B // 2], added[-1], lens[-1] = 300, 500, 0, 40
+    lens[B // 4] = added[B // 4] = 0
+    start = np.concatenate([[0], np.cumsum(added)])
+    width, pages = -(-int(lens.max()) // PAGE), 200
+    pool = filled(j, pages, g)
+    table = torch.randint(0, pages, (B, width), generator=g, device="cuda", dtype=torch.int32)
+    q = randn(g, int(start[-1]), H, d + p).to(BF16)
+    wk, wv = factors(j, g)
+    i32 = lambda x: torch.tensor(np.asarray(x), dtype=torch.int32, device="cuda")  # noqa: E731
+    total = int(lens[added > 0].sum())
+    ws = torch.full((j.prefill_workspace_bytes(B, len(q), int(lens.max()), total),), 255, dtype=torch.uint8, device="cuda")
+    out = joint_prefill(j, q, i32(start), pool, table, i32(lens), int(lens.max()), wk, wv, total_context=total, workspace=ws)
+    check_rows(out, plain_prompt(j, q, pool, table, lens.tolist(), start, wk, wv))
+    # one token less than fits: the last sequence that has rows gets NaN, the others stay
+    last = int(np.flatnonzero(added)[-1])
+    few = joint_prefill(j, q, i32(start), pool, table, i32(lens), int(lens.max()), wk, wv, total_context=total - 1)
+    assert torch.isnan(few[int(start[last]):]).all() and torch.equal(few[:int(start[last])], out[:int(start[last])])
