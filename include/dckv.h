@@ -624,8 +624,9 @@ int dckv_joint_read(const dckv_joint_desc* desc, const void* pool, int64_t num_p
  *              the call is refused
  *   out        device bf16 [batch, Q, H, d]
  * Roundings (relative; sums are fp32): e4m3 caches, folded queries and softmax weights
- * 2^-12 (f16, under powers of two that follow the magnitudes; parts 2^-29 of a query
- * row's greatest coordinate and weights 2^-22 of the greatest lose bits); bf16 caches,
+ * 2^-12 (f16, under powers of two that follow the magnitudes; coordinates 2^-29 of the
+ * greatest of their part, folded or position, of a query row and weights 2^-22 of the
+ * greatest lose bits); bf16 caches,
  * weights 2^-9, queries 2^-17, or 2^-9 at rank 512 where a call's products are shared by
  * more than 32 rows (Q*H, for the prefix batch*Q*H).
  * Whatever lies in slots that a query does not see (NaN included) does not reach its

@@ -38,7 +38,7 @@ struct JointShape {
 // What an attend kernel reads and writes.
 struct JointAttend {
   const void* q;                // [rows of all sequences]: bf16 [2][r + p], the second the rest; e4m3: f16 [r + p]
-  const int32_t* q_up;          // e4m3: [rows], queries are 2^up as large, and times the scale
+  const int32_t* q_up;          // e4m3: [rows], queries are 2^up as large (a half each part), and times the scale
   const uint8_t* pool;
   int64_t num_pages, page_bytes;
   const int32_t* table;         // page_table, or the prefix's pages

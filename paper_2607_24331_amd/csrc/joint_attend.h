@@ -33,8 +33,9 @@
 // for 27% of 54 us, LDS for half, three tenths of it the values' transposed reads in twos
 // of a bank).
 // e4m3 tokens are widened to f16 on their way from LDS to the matrix unit, exactly and without
-// their powers of two.  Queries are f16 under a power of two of their row (2^-12 of a
-// coordinate; 29 binades below the greatest are normal numbers).  The products over latents
+// their powers of two.  Queries are f16 under two powers of two of their row, one of the latents'
+// part and one of the position part (2^-12 of a coordinate; 29 binades below a part's greatest
+// are normal numbers).  The products over latents
 // and over position keys are summed apart and take the tokens' powers in fp32; the weights
 // take them, held against a maximum of score + exponent of their own, so that they are at
 // most 2^(kSlack + kRaise) whatever the exponents are: f16 again, 2^-12 of a weight.  That
@@ -382,7 +383,7 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
     const uint8_t* qrow = static_cast<const uint8_t*>(a.q) +
                           ((prefix ? 0 : int64_t(sg.b) * rows) + rowc) * (W * (C8 ? 2 : 4));
     u32x4 q[KQ], rest[S::REST ? R / 32 : 1];
-    int down = 0;                                     // e4m3: 127 and the power of two that is taken back
+    int up = 0;                                       // e4m3: powers of two that are taken back, latents' below
     if constexpr (C8) {
 #pragma unroll
       for (int i = 0; i < KS; ++i) {
@@ -392,7 +393,7 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
         else if (g == 0)
           last_q[rw][i - KQ][lane] = x;
       }
-      down = a.q_up[(prefix ? 0 : int64_t(sg.b) * rows) + rowc] + 127;
+      up = a.q_up[(prefix ? 0 : int64_t(sg.b) * rows) + rowc];
     } else {
 #pragma unroll
       for (int i = 0; i < KS; ++i) q[i] = *reinterpret_cast<const u32x4*>(qrow + 2 * (32 * i + 8 * lq));
@@ -520,13 +521,14 @@ __global__ __launch_bounds__((Shape<R, P, C8, WR>::THREADS)) void joint_attend(J
           }
         }
         auto byte = [](uint32_t four, int v) { return int((four >> (8 * v)) & 0xFFu); };
+        const int both = C8 ? here(up) : 0, down = int16_t(both & 0xFFFF) + 127, rope_down = (both >> 16) + 127;
 #pragma unroll
         for (int n = 0; n < 2; ++n)
 #pragma unroll
           for (int v = 0; v < 4; ++v) {
             if constexpr (C8) {
               s[n][v] = __builtin_amdgcn_ldexpf(s[n][v], byte(el[n], v) - down);
-              if constexpr (P > 0) s[n][v] += __builtin_amdgcn_ldexpf(sk[n][v], byte(ek[n], v) - down);
+              if constexpr (P > 0) s[n][v] += __builtin_amdgcn_ldexpf(sk[n][v], byte(ek[n], v) - rope_down);
             } else {
               s[n][v] *= a.scale;
             }

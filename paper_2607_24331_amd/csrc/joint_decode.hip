@@ -203,9 +203,10 @@ __global__ __launch_bounds__(64) void joint_fold(const bf16* __restrict__ q, con
 }
 
 // e4m3 cache: folded [row][r + p] f16, times unit (the scale is unit * 2^unit_exp) and 2^up, which
-// brings a row's greatest below 2^15; ups: up - unit_exp.  A work-group has all columns of its
-// rows, 32 a wave, so that it knows the greatest; it shares the queries and the factor, 64
-// rows of it at a time, in LDS.
+// brings the greatest of a row's part below 2^15; ups: up - unit_exp, of the latents' part in the
+// low half and of the position part.  A work-group has all columns of its rows, 32 a wave, so
+// that it knows the greatest; it shares the queries and the factor, 64 rows of it at a time,
+// in LDS.
 template <int D>
 __global__ __launch_bounds__(1024) void joint_fold_e4m3(const bf16* __restrict__ q, const bf16* __restrict__ W_keys,
                                                         int n, int heads, int r, int p, _Float16* __restrict__ folded,
@@ -213,7 +214,7 @@ __global__ __launch_bounds__(1024) void joint_fold_e4m3(const bf16* __restrict__
                                                         int wave_rows, FoldStarts starts) {
   constexpr int DH = 64, QST = 2 * D + 16;                     // bytes a row of the queries
   __shared__ __align__(16) unsigned char wk[DH * (2 * 512 + 32)], qs[2][32 * QST];
-  __shared__ uint32_t most[3][32];                             // bits of the rows' greatest magnitudes
+  __shared__ uint32_t most[3][2][32];                          // bits of the rows' greatest magnitudes, a part each
   const int tid = threadIdx.x, lane = tid & 63, lr = lane & 31, h = lane >> 5, threads = 2 * r;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6), c0 = 32 * w, st = 2 * r + 32;
   if (int(blockIdx.x) == heads) {
@@ -251,7 +252,7 @@ __global__ __launch_bounds__(1024) void joint_fold_e4m3(const bf16* __restrict__
 #pragma unroll
   for (int i = 0; i < D / 16; ++i)
     piece[i] = *reinterpret_cast<const u32x4*>(src + int64_t(16 * i + prow) * r + pcol * 8);
-  if (tid < 32) most[0][tid] = 0;
+  if (tid < 64) most[0][tid >> 5][tid & 31] = 0;
   keep_rows(0);
   u32x4 f[D / 16];
 #pragma unroll
@@ -291,7 +292,7 @@ __global__ __launch_bounds__(1024) void joint_fold_e4m3(const bf16* __restrict__
         top[v] = fmaxf(lane & o ? high : low, __shfl_xor(lane & o ? low : high, o));
       }
     const int v0 = 8 * (lane & 1) + 4 * (lane >> 1 & 1) + 2 * (lane >> 2 & 1) + (lane >> 3 & 1);
-    atomicMax(&most[it][row_of(v0)], __float_as_uint(top[0]));
+    atomicMax(&most[it][0][row_of(v0)], __float_as_uint(top[0]));
     // the position part, 8 coordinates a lane
     const int64_t prow64 = min(r0 + tid / 8, n - 1);
     const bool keys = tid < 256 && tid % 8 < p / 8;
@@ -302,22 +303,22 @@ __global__ __launch_bounds__(1024) void joint_fold_e4m3(const bf16* __restrict__
 #pragma unroll
       for (int e = 0; e < 4; ++e)
         t = fmaxf(t, fmaxf(fabsf(__uint_as_float(y[e] << 16)), fabsf(__uint_as_float(y[e] & 0xFFFF0000u))));
-      atomicMax(&most[it][tid / 8], __float_as_uint(t * unit));
+      atomicMax(&most[it][1][tid / 8], __float_as_uint(t * unit));
     }
     const int next = it == 2 ? 0 : it + 1;
-    if (tid < 32) most[next][tid] = 0;                         // last read before the barrier before
+    if (tid < 64) most[next][tid >> 5][tid & 31] = 0;          // last read before the barrier before
     if (more) keep_rows(buf ^ 1);                              // likewise
     __syncthreads();
-    auto up_of = [&](int row) { return min(max(15 + 126 - int(most[it][row] >> 23), -120), 120); };
+    auto up_of = [&](int part, int row) { return min(max(15 + 126 - int(most[it][part][row] >> 23), -120), 120); };
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
       const int row = r0 + row_of(v);
       if (row < n)
         folded[(int64_t(row) * heads + head) * W + joint::query_place(c0 + lr, W)] =
-            _Float16(acc[v] * power(up_of(row_of(v))));
+            _Float16(acc[v] * power(up_of(0, row_of(v))));
     }
     if (keys && r0 + tid / 8 < n) {
-      const float by = power(up_of(tid / 8));
+      const float by = power(up_of(1, tid / 8));
       u32x4 z;
 #pragma unroll
       for (int e = 0; e < 4; ++e)
@@ -325,7 +326,8 @@ __global__ __launch_bounds__(1024) void joint_fold_e4m3(const bf16* __restrict__
                                 __uint_as_float(y[e] & 0xFFFF0000u) * unit * by);
       *reinterpret_cast<u32x4*>(folded + (prow64 * heads + head) * W + joint::query_place(r + tid % 8 * 8, W)) = z;
     }
-    if (tid < 32 && r0 + tid < n) ups[int64_t(r0 + tid) * heads + head] = up_of(tid) - unit_exp;
+    if (tid < 32 && r0 + tid < n)                              // at most 120 + 149 either way
+      ups[int64_t(r0 + tid) * heads + head] = ((up_of(0, tid) - unit_exp) & 0xFFFF) | (up_of(1, tid) - unit_exp) * 65536;
     it = next;
     buf ^= 1;
   }

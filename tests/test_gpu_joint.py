@@ -1311,3 +1311,31 @@ def test_prompts_of_many_sequences(B, H, d, r, p, cache):
     last = int(np.flatnonzero(added)[-1])
     few = joint_prefill(j, q, i32(start), pool, table, i32(lens), int(lens.max()), wk, wv, total_context=total - 1)
     assert torch.isnan(few[int(start[last]):]).all() and torch.equal(few[:int(start[last])], out[:int(start[last])])
+
+
+@pytest.mark.parametrize("H,d,r,p,cache", [(4, 64, 128, 32, "bf16"), (16, 64, 128, 32, "e4m3"), (5, 128, 256, 64, "e4m3"),
+                                           (32, 128, 512, 64, "e4m3"), (32, 64, 512, 64, "bf16")])
+@pytest.mark.parametrize("size", [-60, -30, 30, 60])
+def test_parts_of_other_sizes(H, d, r, p, cache, size):
+    """Latents 2^size as large as position keys under queries whose parts are 2^-size so: the
+    parts of a score are of one size."""
+    from paper_2607_24331_amd import joint_decode, joint_prefill
+    g = gen(H + d)
+    j = joint_of(H, d, r, p, cache)
+    w, lens, Q = r + p, [130, 65], 3
+    pool = filled(j, 6, g)
+    at = torch.from_numpy(oj.place(r, p, cache, np.arange(PAGE)[:, None], np.arange(r)[None])).cuda().view(-1)
+    if cache == "bf16":
+        pool[:, at] = (pool[:, at].double() * 2.0 ** size).to(BF16)
+    else:
+        pool[:, PAGE * w:PAGE * (w + 1)] = (pool[:, PAGE * w:PAGE * (w + 1)].int() + size).to(torch.uint8)
+    table = torch.arange(6, dtype=torch.int32, device="cuda").view(2, 3)
+    q = randn(g, 2, Q, H, d + p).double()
+    q[..., :d] *= 2.0 ** -size
+    q = q.to(BF16)
+    wk, wv = factors(j, g)
+    seq = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    want = plain(j, q, pool, table, lens, wk, wv)
+    check_rows(joint_decode(j, q, pool, table, seq, 192, wk, wv), want, "decode")
+    start = torch.tensor([0, Q, 2 * Q], dtype=torch.int32, device="cuda")
+    check_rows(joint_prefill(j, q.view(2 * Q, H, d + p), start, pool, table, seq, 192, wk, wv), want.view(2 * Q, H, d), "prompt")
