@@ -1339,3 +1339,43 @@ def test_parts_of_other_sizes(H, d, r, p, cache, size):
     check_rows(joint_decode(j, q, pool, table, seq, 192, wk, wv), want, "decode")
     start = torch.tensor([0, Q, 2 * Q], dtype=torch.int32, device="cuda")
     check_rows(joint_prefill(j, q.view(2 * Q, H, d + p), start, pool, table, seq, 192, wk, wv), want.view(2 * Q, H, d), "prompt")
+
+
+@pytest.mark.parametrize("H,d,r,p,cache,T", [(3, 64, 128, 32, "bf16", 300), (34, 128, 128, 0, "e4m3", 2100)])
+def test_captured_prompts_forget_the_replay_before(H, d, r, p, cache, T):
+    """Tokens and factors far apart in one replay, or not finite, leave nothing to the next."""
+    from paper_2607_24331_amd import joint_prefill
+    j = joint_of(H, d, r, p, cache)
+    added = [90, 40]
+    pool, table, start, q, wk, wv, seq, rs, lens, top = prompt_case(j, [T - 90, 0], added, 0, 31)
+    ws = torch.empty(j.prefill_workspace_bytes(2, 130, top, sum(lens)), dtype=torch.uint8, device="cuda")
+    out = torch.zeros(130, H, d, dtype=BF16, device="cuda")
+
+    def run(o, w=None):
+        return joint_prefill(j, q, rs, pool, table, seq, top, wk, wv, total_context=sum(lens), out=o, workspace=w)
+
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(out, ws)
+    clean, was, factor = run(None), pool.clone(), wv.clone()
+    slot = [int(table[0, t // PAGE]) * PAGE + t % PAGE for t in range(T)]
+
+    def far():
+        resize(j, pool, slot[:5] + slot[-30:], [-30] * 5 + [25, -25] * 15, "c")
+
+    def odd():
+        wv[H - 1, 3, 5] = math.inf
+
+    def token():
+        poison(j, pool, slot[-4:-3], math.nan if cache == "bf16" else 0x7F)
+
+    for change in (None, far, None, odd, None, token, far, None):
+        pool.copy_(was)
+        wv.copy_(factor)
+        if change:
+            change()
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = run(None)
+        assert torch.equal(out.view(torch.int16), eager.view(torch.int16))
+        assert torch.equal(out, clean) == (change is None)
