@@ -18,8 +18,8 @@
 // of the result's error (relative to 64 bits 2.4e-3 against 1.9e-3, of which 1.7e-3 is the
 // result's own).  At r = 512 and two waves a SIMD, which more than 32 rows have, the
 // registers do not hold the rests and the queries go without: rests of 6 of 16 steps in
-// what LDS has left cost 128 rows over 131,072 tokens 63 us for 54, and lone waves that
-// hold them all 73.
+// what LDS has left made 128 rows over 131,072 tokens a sixth slower, lone waves that hold
+// them all a third.
 // A wave owns 16 rows and all r columns of their sums: 128 accumulators a lane at r = 512
 // and 72 registers of queries (32 rows, twice that, read LDS half as often but do not fit
 // the registers: 200 and more were spilled).  Of a work-group's waves WR take WR x 16
@@ -28,10 +28,10 @@
 // score passes it by more than kSlack (in powers of two), so that the r sums of a row
 // are rarely touched.
 // Few rows are bound by the tokens' bytes (32 rows over 4 x 32,768 tokens at r = 512, 151 MB:
-// 33.6 us, 4.5 TB/s), more by the latency of LDS at two waves a SIMD (128 rows over 131,072
-// tokens: 59 us, 618 TFLOP/s; 2,048 rows over a prefix of 16,384: 95 us, 768 TFLOP/s; the matrix unit is busy
-// for 27% of 54 us, LDS for half, three tenths of it the values' transposed reads in twos
-// of a bank).
+// 33.5 us, 4.5 TB/s), more by the latency of LDS at two waves a SIMD (128 rows over 131,072
+// tokens: 57 us, 640 TFLOP/s; 2,048 rows over a prefix of 16,384: 94 us, 779 TFLOP/s; the matrix
+// unit is busy for 32% and 38% of the cycles, LDS for half of them, three tenths of that
+// the values' transposed reads in twos of a bank).
 // e4m3 tokens are widened to f16 on their way from LDS to the matrix unit, exactly and without
 // their powers of two.  Queries are f16 under two powers of two of their row, one of the latents'
 // part and one of the position part (2^-12 of a coordinate; 29 binades below a part's greatest

@@ -8,7 +8,7 @@
 //               the factor's rows; products on MFMA 32x32x16.  One more wave forms
 //               the sequences' first tiles and the cut of the work.  Bound by latency and,
 //               once, by the factor's bytes (32 heads at rank 512: 4 rows a head 3.9 us, 64 7.5).
-// joint_fold_e4m3   the same for f16 queries, a work-group all columns of a head (64 rows: 8.0 us).
+// joint_fold_e4m3   the same for f16 queries, a work-group all columns of a head (64 rows: 7.8 us).
 // joint_merge   a work-group a row: its shares' sums in fp32, 16 bytes a lane.  Bound by
 //               the shares' bytes (4,096 rows of 10 shares at rank 512, 92 MB: 16 us, 5.7 TB/s).
 // joint_values  the product with the heads' factor rows on MFMA, 32 rows by 32 coordinates a
@@ -558,9 +558,10 @@ int fill(int rank) { return rank == 128 ? 512 : 256; }
 int64_t tiles_of(int64_t tokens) { return (tokens + kJointTile - 1) / kJointTile; }
 
 // Waves of a work-group that take rows, 16 each.  The slices of a unit read the same tokens on
-// one XCD at about one time, so that its L2 serves all but one, as long as they run together:
-// 32 slices (4,096 rows of bf16 at rank 512 over 16,384 tokens: 32 slices of 128 rows 144 us,
-// 64 of 64 rows 313 us).
+// one XCD at about one time, so that its L2 serves all but one.  A unit's slices all run on one
+// XCD and fill it from 32 on: with more of them there are fewer units than XCDs, and some
+// have no work (4,096 rows of bf16 at rank 512 over 16,384 tokens: eight units of 32 slices of
+// 128 rows 168 us; of 64 slices of 64 rows four, on four of the eight XCDs, 304).
 // e4m3: the fewest waves that keep to 32 slices; widening a tile costs about as much as its
 // products, and token groups that do not wait for each other hide it best (48 rows over
 // 4 x 32,768 tokens at rank 512: 34 us, in one slice of 64 rows 40; 512 rows over a prefix of
@@ -570,7 +571,7 @@ int64_t tiles_of(int64_t tokens) { return (tokens + kJointTile - 1) / kJointTile
 // bf16: one up to 32 rows (4 x 32,768 tokens: 33 us, in one slice 34); from there reading a tile
 // from memory by one slice alone pays (64 rows: 4 waves 39 us, 2 slices 48, 4 slices 52), but
 // four waves' shares are half of eight's to join (128 rows over 131,072 tokens: attention and
-// join 64 us, eight waves 67).
+// join 68 us, eight waves 74).
 constexpr int kSlices = 32;
 constexpr int kManySequences = 16;
 int row_waves_of(bool e4m3, int64_t rows, int sequences) {

@@ -30,10 +30,10 @@
 // a call for 0.75).
 // Bound by the products: 4 T r d + 2 pairs (2 d + p) a head, and in the attention by LDS,
 // which 32 rows a wave read as fast as the products of a tile go.  8,191 new tokens of 32 heads
-// (d = 128, p = 64, r = 512): keys and values 77 us, 892 TFLOP/s; attention 651 us at best, 693 in
-// the mean of calls on end, 1,055 and 991 TFLOP/s of the pairs that rows see, the matrix unit
-// busy for 63% of the cycles.  Gathering them is
-// bound by memory (14 us), the plan by latency (7).
+// (d = 128, p = 64, r = 512): keys and values 78 us, 881 TFLOP/s; attention 661 us at best, 701 in
+// the mean of calls on end, 1,040 and 981 TFLOP/s of the pairs that rows see, the matrix unit
+// busy for 64% of the cycles.  Gathering them is bound by memory (14 us), the plan by
+// latency (6).
 #include <algorithm>
 #include <cmath>
 #include <limits>
@@ -307,14 +307,14 @@ __device__ __forceinline__ uint32_t pair(float a, float b) {
          uint32_t(__builtin_bit_cast(uint16_t, from_f32<bf16>(b))) << 16;
 }
 
-// Piece i of row s of an LDS tile of g-piece rows lies at piece i ^ joint_swap(g, s).
 struct GatherArgs {
   const uint8_t* pool;
   int64_t num_pages, page_bytes;
   const int32_t* page_table;
   int32_t max_pages, r, p;
   bf16* c;                                // [tiles * 64][r]
-  uint8_t* rope;                          // [tiles][64 rows of p], in LDS places; bf16 here, f16 after prompt_expand
+  uint8_t* rope;                          // [tiles][64 rows of p], bf16 here, f16 after prompt_expand; piece i of row s
+                                          // lies at piece i ^ joint_swap(g, s) of the row, as in every LDS tile
   const void *W_keys, *W_values;
   int64_t factor_pieces;                  // 16-byte pieces of a factor
   int32_t factor_groups;                  // work-groups that look for its greatest element
@@ -1061,8 +1061,8 @@ hipError_t launch_joint_prefill(const JointPrompt& s, const void* q, const int32
     e = hipGetLastError();
     if (e != hipSuccess) return e;
     // 256 coordinates a work-group, and 256 tokens where that fills the chip (30,061 tokens of 32
-    // heads: 285 us, with 64 tokens 364; 8,191: 77 and 89), else 64 (two short prompts of 16
-    // heads: 6.4 us, with 256 tokens 11.9)
+    // heads: 292 us, with 64 tokens 364; 8,191: 78 and 89), else 64 (two short prompts of 16
+    // heads: 6.5 us, with 256 tokens 12.7)
     const int64_t coords = d.head_dim == 128 ? d.num_heads : (d.num_heads + 1) / 2;
     const bool wide = s.kv_tiles / 4 * coords >= 256;
 #define DCKV_GO(D, NT)                                                                                      \
