@@ -663,12 +663,12 @@ int dckv_joint_decode(const dckv_joint_desc* desc, int32_t queries, const void* 
  *              NaN
  *   out        device bf16 [n_rows, H, d]
  * Keys, values, queries and softmax weights are rounded to f16 (relative 2^-12) under
- * powers of two, sums are fp32.  They lose bits where they are small: a value below 2^-17
+ * powers of two, sums are fp32.  They lose bits where they are small: a value below 2^-13
  * of its token's bound (greatest |latent coordinate| * r * greatest |factor element|); a
- * key's coordinate below 2^-17 of the bound of its part (with or without position), of
+ * key's coordinate below 2^-13 of the bound of its part (with or without position), of
  * both parts where tokens differ in their ratio; a query's coordinate below 2^-29 of its
  * row's greatest, its parts weighed with their keys' bounds; a softmax weight below 2^-22
- * of the greatest (of weight times bound, where tokens differ more than 64-fold).  What
+ * of the greatest (of weight times bound, where tokens differ more than 256-fold).  What
  * a row does not see changes its result by roundings only.
  * Values that overflow fp32 count as the greatest number; of scores that
  * overflow it the greatest alone weighs.  A token that is not finite makes every row

@@ -22,12 +22,12 @@
 // query row, one a sequence for its keys without position (of all heads), one for its position
 // keys and one for its values.  They are formed from bounds on the magnitude (greatest latent
 // coordinate x r x greatest factor element) of the tokens that all rows of the sequence see,
-// so that a later token's size does not reach an earlier row, and leave 2^6 above those; a
-// token above that, or below 2^-12 of it, shifts its own.  So every token's bound is below
-// 2^15 and above 2^3, 17 binades and more above the least normal number.  They meet in a row's
+// so that a later token's size does not reach an earlier row, and leave 2^8 above those; a
+// token above that, or below 2^-16 of it, shifts its own.  So every token's bound is below
+// 2^15 and above 2^-1, 13 binades and more above the least normal number.  They meet in a row's
 // queries, score scale and result; where a row tile meets a token that shifts its own, its scores
-// and weights take the shifts one by one (8,191 tokens whose first is 2^-10 of the others: 1.33 ms
-// a call for 0.75).
+// and weights take the shifts one by one (8,191 tokens whose first is 2^-11 of the others: 1.27 ms
+// a call for 0.74).
 // Bound by the products: 4 T r d + 2 pairs (2 d + p) a head, and in the attention by LDS,
 // which 32 rows a wave read as fast as the products of a tile go.  8,191 new tokens of 32 heads
 // (d = 128, p = 64, r = 512): keys and values 78 us, 881 TFLOP/s; attention 661 us at best, 701 in
@@ -106,7 +106,7 @@ __device__ __forceinline__ Above above_of(int most_c, int most_k, int w_keys, in
 // hold.  A sequence's are set by the tokens that all its rows see and hold what is up to 2^kRoom
 // above them; a token that is more, or less than 2^-kSpan of that, shifts its own (both parts of
 // its key alike: a row's products are summed over them, its query balanced between them).
-constexpr int kRoom = 6, kSpan = 12;
+constexpr int kRoom = 8, kSpan = 16;
 struct Powers {
   int keys, rope, values;
 };
